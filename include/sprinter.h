@@ -68,7 +68,11 @@ typedef enum {
     SPR_OP_SPRINTER_STEP = 3,
     SPR_OP_SD_SHARD = 4,
     SPR_OP_VERIFIER_LABELS = 5,
-    SPR_OP_VERIFIER_TRAIN = 6
+    SPR_OP_VERIFIER_TRAIN = 6,
+    SPR_OP_HEAD_LOSS = 7,
+    SPR_OP_HEAD_LOSS_GRAD = 8,
+    SPR_OP_VERIFIER_LABELS_HEAD = 10,
+    SPR_OP_VERIFIER_TRAIN8 = 11
 } spr_op;
 
 /* Which verifier kernel sprinter_verify() uses.  AUTO picks the tensor-core
@@ -79,8 +83,10 @@ typedef enum { SPR_VERIFIER_AUTO = 0, SPR_VERIFIER_SIMT = 1, SPR_VERIFIER_TENSOR
  * B is the number of draws n and K, d, h are ignored; for SPR_OP_SD_VERIFY d
  * and h are ignored; for SPR_OP_SPRINTER_VERIFY V is ignored; SPR_OP_SPRINTER_STEP
  * uses all of them; for SPR_OP_SD_SHARD V is the width of this GPU's vocabulary
- * shard and d, h are ignored; SPR_OP_VERIFIER_LABELS uses B, K, V; SPR_OP_VERIFIER_TRAIN
- * uses d only.  Returns 0 for invalid arguments.  A workspace sized for the
+ * shard and d, h are ignored; SPR_OP_VERIFIER_LABELS uses B, K, V; SPR_OP_VERIFIER_TRAIN and
+ * SPR_OP_VERIFIER_TRAIN8 use d only; SPR_OP_HEAD_LOSS, SPR_OP_HEAD_LOSS_GRAD and
+ * SPR_OP_VERIFIER_LABELS_HEAD are for N = B*K >= 1 hidden states of width d, and
+ * SPR_OP_VERIFIER_LABELS_HEAD takes the target's width as d and the draft's as h.  Returns 0 for invalid arguments.  A workspace sized for the
  * largest op serves all of them. */
 size_t spr_workspace_bytes(int op, int B, int K, int V, int d, int h, int dt);
 
@@ -299,6 +305,92 @@ int verifier_labels(const void *p_logits, const void *q_logits, int64_t ldv, con
 int verifier_train_step(const void *hidden, const uint8_t *labels, int64_t N, int d, int dt, float *theta,
                         float *adam_m, float *adam_v, int t, float lr, float beta1, float beta2, float eps,
                         float *loss, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * head_loss - softmax cross entropy of hidden states under a vocabulary head.
+ *
+ * The paper has no counterpart: it takes the draft model as given.  This is the loss that a draft
+ * model is fitted with - on tokens of its target, say - before a verifier is fitted to the pair.
+ * The logits l = hidden W^T are formed tile by tile on the tensor cores and kept nowhere.
+ *
+ * hidden [N,d] dt, W [V,d] dt (nn.Linear layout, no bias), targets [N] int32:
+ *   lse[i]  = log sum_v exp(l_iv)                       (optional, NULL to skip)
+ *   loss[i] = lse[i] - l_{i,targets[i]}, 0 where targets[i] < 0 (a padded position)
+ * loss, lse [N] f32.  hidden and W are 16-byte aligned; any d and V.  bf16 operands with d a
+ * multiple of 8 are read where they are, others are first laid out in the workspace (fp32 as
+ * three bf16 parts, six products: as exact as fp32 products).
+ * A row of hidden that holds infinities or NaN makes its own outputs NaN, no others.
+ * Device-detected: targets[i] >= V -> loss[i] = -1, SPR_ERR_BAD_TOKEN.  If a bounded wait runs out
+ * (SPR_ERR_TIMEOUT, as for verifier_train_step sticky until read) loss and lse are NaN.
+ * Workspace: spr_workspace_bytes(SPR_OP_HEAD_LOSS, N, 1, V, d, 0, dt).
+ */
+int head_loss(const void *hidden, const void *W, const int32_t *targets, int N, int d, int V, int dt, float *loss,
+              float *lse, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * head_loss_grad - gradient of sum_i grad_loss[i] * loss[i] of head_loss.
+ *
+ * With lse as head_loss gives it for the same hidden and W, and
+ *   D_iv = grad_loss[i] * (exp(l_iv - lse[i]) - [v = targets[i]]),  0 where targets[i] < 0:
+ *   d_hidden [N,d] dt = D W,   d_W [V,d] dt = D^T hidden   (either may be NULL, not both)
+ * The logits are formed again, a piece of the vocabulary at a time; a piece's D is held in the
+ * workspace, rounded to bf16 (bf16 operands) or kept to fp32 (three bf16 parts); all sums are fp32.
+ * Rows without a target have no part in d_W whatever they hold, and a zero row in d_hidden.
+ * All-padded batches and N = 0 give zeros.  hidden, W, d_hidden, d_W are 16-byte aligned; outputs
+ * must not overlap inputs.  Device-detected: targets[i] >= V is treated as padding,
+ * SPR_ERR_BAD_TOKEN; after SPR_ERR_TIMEOUT the outputs are not valid.
+ * Workspace: spr_workspace_bytes(SPR_OP_HEAD_LOSS_GRAD, N, 1, V, d, 0, dt).
+ */
+int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, const float *lse, const float *grad_loss,
+                   int N, int d, int V, int dt, void *d_hidden, void *d_W, void *ws, size_t ws_bytes,
+                   void *cuda_stream);
+
+/*
+ * verifier_labels_head - training labels of the verifier where no logits are kept.
+ *
+ * Defined by: as verifier_labels (Section 3.2), with p = softmax(p_hidden p_W^T) and
+ * q = softmax(q_hidden q_W^T) formed from the two models' last hidden states and heads.
+ *
+ * p_hidden [N,dp], p_W [V,dp] (target), q_hidden [N,dq], q_W [V,dq] (draft), all dt and 16-byte
+ * aligned; draft_tokens [N] int32; lambdas: HOST array of n_lambda <= 8 thresholds.
+ *   labels [n_lambda,N] uint8: labels[l,i] = (q(x_i)/p(x_i) <= lambdas[l])
+ *   ratio  [N] f32 (optional): q(x_i)/p(x_i), formed from log-probabilities in double precision
+ * Device-detected: token outside [0,V) -> labels 0, ratio -1, SPR_ERR_BAD_TOKEN; after
+ * SPR_ERR_TIMEOUT labels are 0 and ratios NaN.
+ * Workspace: spr_workspace_bytes(SPR_OP_VERIFIER_LABELS_HEAD, N, 1, V, dp, dq, dt).
+ */
+int verifier_labels_head(const void *p_hidden, const void *p_W, int dp, const void *q_hidden, const void *q_W, int dq,
+                         const int32_t *draft_tokens, int N, int V, int dt, const float *lambdas, int n_lambda,
+                         uint8_t *labels, float *ratio, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * hidden_pack8, hidden_unpack8 - hidden states kept in 8 bits for the fit.
+ *
+ * The paper has no counterpart (it does not say how training states are stored).  A packed row of d
+ * elements takes spr_pack8_pitch(d) bytes: d signed bytes q, ceil(d/32) signed bytes e - one per block
+ * of 32 elements - and zeros up to a multiple of 16.  An element stands for q * 2^e:
+ *   e = max(floor(log2 m) - 6, -126), m the largest magnitude of the block;
+ *   q = clamp(round-to-even(x * 2^-e), -127, 127)
+ * so that |x - q 2^e| <= 2^(e-1) (below 2^e where |x| > 127.5 * 2^e).  A block that holds an infinity or
+ * NaN has e = -128 and q = 0, and stands for NaN.  Every other packed value is a bf16 number: unpacking
+ * to bf16 is exact.
+ * hidden [N,d] dt (any d <= 2^20, element-aligned), packed 16-byte aligned.  No workspace.
+ */
+size_t spr_pack8_pitch(int d);   /* 0 for d outside [1, 2^20] */
+int hidden_pack8(const void *hidden, int64_t N, int d, int dt, void *packed, void *cuda_stream);
+int hidden_unpack8(const void *packed, int64_t N, int d, int dt, void *hidden, void *cuda_stream);
+
+/*
+ * verifier_train_step8 - verifier_train_step on hidden states kept in 8 bits.
+ *
+ * Same step, arguments and errors as verifier_train_step with s_i = the values that the packed
+ * rows stand for (hidden_pack8), read once: 1.03 d bytes per sample.  packed: 16-byte aligned; d a
+ * multiple of 16 and at most 4096 (otherwise SPR_ERR_UNSUPPORTED).
+ * Workspace: spr_workspace_bytes(SPR_OP_VERIFIER_TRAIN8, 0, 0, 0, d, 0, SPR_F32 or SPR_BF16).
+ */
+int verifier_train_step8(const void *packed, const uint8_t *labels, int64_t N, int d, float *theta, float *adam_m,
+                         float *adam_v, int t, float lr, float beta1, float beta2, float eps, float *loss, void *ws,
+                         size_t ws_bytes, void *cuda_stream);
 
 /*
  * sprinter_simulate - run lengths of an i.i.d. verifier (Monte-Carlo of Theorems 2 and 3).

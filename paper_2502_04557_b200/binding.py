@@ -17,6 +17,7 @@ from . import build as _build
 F32, BF16 = 0, 1
 OP_SPRINTER_VERIFY, OP_REPLACE_SAMPLE, OP_SD_VERIFY, OP_SPRINTER_STEP, OP_SD_SHARD = 0, 1, 2, 3, 4
 OP_VERIFIER_LABELS, OP_VERIFIER_TRAIN = 5, 6
+OP_HEAD_LOSS, OP_HEAD_LOSS_GRAD, OP_VERIFIER_LABELS_HEAD, OP_VERIFIER_TRAIN8 = 7, 8, 10, 11
 PATH_AUTO, PATH_SIMT, PATH_TENSOR = 0, 1, 2
 
 EXPORTS = [
@@ -26,6 +27,8 @@ EXPORTS = [
     "spr_set_stage_events", "replace_sample_static", "sprinter_step", "sprinter_simulate",
     "sd_shard_stats", "sd_shard_decide", "sd_shard_weights", "sd_shard_draw", "sd_shard_decide_weights",
     "verifier_labels", "verifier_train_step", "spr_test_sprinter_verify", "spr_test_verifier_train_step",
+    "head_loss", "head_loss_grad", "verifier_labels_head", "spr_pack8_pitch", "hidden_pack8", "hidden_unpack8",
+    "verifier_train_step8",
 ]
 
 
@@ -94,6 +97,19 @@ def lib():
         L.verifier_train_step.argtypes = [vp, vp, i64, i32, i32, vp, vp, vp, i32, f32, f32, f32, f32, vp, vp, sz, vp]
         L.spr_test_verifier_train_step.restype = i32
         L.spr_test_verifier_train_step.argtypes = L.verifier_train_step.argtypes + [i32, C.c_uint]
+        L.head_loss.restype = i32
+        L.head_loss.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.head_loss_grad.restype = i32
+        L.head_loss_grad.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.verifier_labels_head.restype = i32
+        L.verifier_labels_head.argtypes = [vp, vp, i32, vp, vp, i32, vp, i32, i32, i32, vp, i32, vp, vp, vp, sz, vp]
+        L.spr_pack8_pitch.restype = sz
+        L.spr_pack8_pitch.argtypes = [i32]
+        for fn in (L.hidden_pack8, L.hidden_unpack8):
+            fn.restype = i32
+            fn.argtypes = [vp, i64, i32, i32, vp, vp]
+        L.verifier_train_step8.restype = i32
+        L.verifier_train_step8.argtypes = [vp, vp, i64, i32, vp, vp, vp, i32, f32, f32, f32, f32, vp, vp, sz, vp]
         L.spr_host_arena_bytes.restype = sz
         L.spr_host_arena_bytes.argtypes = [i32, i32, i32, i32, i64, i32, i32, i32]
         L.sprinter_verify_host.restype = i32
@@ -530,6 +546,152 @@ def verifier_train_step(hidden, labels, theta, adam_m, adam_v, t: int, lr: float
                                        _ptr(adam_v), t, lr, beta1, beta2, eps, _ptr(loss), _ptr(ws.buf), ws.nbytes,
                                        _stream())
     _check("verifier_train_step", rc)
+    return loss
+
+
+# ---------------------------------------------------------------------------- heads and 8-bit states
+
+
+def _head(hidden, W, tokens, name="hidden", token_name="targets"):
+    """Checks hidden [N,d], W [V,d] and int32 tokens [N] of one device; returns (N, d, V)."""
+    _dev(hidden, name=name)
+    _dev(W, hidden.dtype, "W")
+    _dev(tokens, torch.int32, token_name)
+    if hidden.dim() != 2 or W.dim() != 2 or W.shape[1] != hidden.shape[1]:
+        raise ValueError(f"{name} must be [N,d] and W [V,d]")
+    if tokens.numel() != hidden.shape[0]:
+        raise ValueError(f"{token_name} must have one entry per hidden state")
+    return hidden.shape[0], hidden.shape[1], W.shape[0]
+
+
+def _same_device(ws, *tensors):
+    """Every tensor and the workspace lie on the device whose stream is used."""
+    dev = torch.device("cuda", torch.cuda.current_device())
+    for t in tensors + ((ws.buf,) if ws is not None else ()):
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors and workspace must be on the current device {dev}, got one on {t.device}")
+
+
+def _result(t, shape, dtype, device, name):
+    """An output tensor: the caller's, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _dev(t, dtype, name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def head_loss(hidden, W, targets, ws: Workspace, want_lse: bool = True, out=None):
+    """Softmax cross entropy of hidden [N,d] under the head W [V,d]; targets i32 [N], negative = padding.
+
+    Returns (loss f32 [N], lse f32 [N] or None); out: the same two tensors."""
+    N, d, V = _head(hidden, W, targets)
+    loss, lse = (None, None) if out is None else out
+    loss = _result(loss, (N,), torch.float32, hidden.device, "loss")
+    lse = _result(lse, (N,), torch.float32, hidden.device, "lse") if want_lse or lse is not None else None
+    _same_device(ws, hidden, W, targets, loss, lse)
+    rc = lib().head_loss(_ptr(hidden), _ptr(W), _ptr(targets), N, d, V, _dt(hidden), _ptr(loss), _ptr(lse),
+                         _ptr(ws.buf), ws.nbytes, _stream())
+    _check("head_loss", rc)
+    return loss, lse
+
+
+def head_loss_grad(hidden, W, targets, lse, grad_loss, ws: Workspace, want_hidden: bool = True, want_W: bool = True,
+                   out=None):
+    """Gradient of sum(grad_loss * loss) of head_loss; lse as head_loss returned it, grad_loss f32 [N].
+
+    Returns (d_hidden [N,d] or None, d_W [V,d] or None) in the operands' type; out: the same two tensors."""
+    N, d, V = _head(hidden, W, targets)
+    for name, t in (("lse", lse), ("grad_loss", grad_loss)):
+        _dev(t, torch.float32, name)
+        if t.numel() != N:
+            raise ValueError(f"{name} must have one entry per hidden state")
+    d_hidden, d_W = (None, None) if out is None else out
+    d_hidden = _result(d_hidden, (N, d), hidden.dtype, hidden.device, "d_hidden") if want_hidden else None
+    d_W = _result(d_W, (V, d), hidden.dtype, hidden.device, "d_W") if want_W else None
+    if d_hidden is None and d_W is None:
+        raise ValueError("at least one of the two gradients must be wanted")
+    _same_device(ws, hidden, W, targets, lse, grad_loss, d_hidden, d_W)
+    if N == 0 and d_W is None:
+        return d_hidden, None
+    # an empty batch has no addresses to pass
+    rc = lib().head_loss_grad(_ptr(hidden), _ptr(W), _ptr(targets), _ptr(lse), _ptr(grad_loss), N, d, V, _dt(hidden),
+                              _ptr(d_hidden), _ptr(d_W), _ptr(ws.buf), ws.nbytes, _stream())
+    _check("head_loss_grad", rc)
+    return d_hidden, d_W
+
+
+def verifier_labels_head(p_hidden, p_W, q_hidden, q_W, draft_tokens, lambdas, ws: Workspace, want_ratio: bool = True):
+    """verifier_labels from hidden states and heads: p_hidden [N,dp], p_W [V,dp] of the target, q_hidden
+    [N,dq], q_W [V,dq] of the draft; draft_tokens i32 [N]; lambdas: up to 8 floats.
+
+    Returns (labels u8 [len(lambdas),N], ratio f32 [N] or None) with ratio = q(x)/p(x)."""
+    N, dp, V = _head(p_hidden, p_W, draft_tokens, "p_hidden", "draft_tokens")
+    Nq, dq, Vq = _head(q_hidden, q_W, draft_tokens, "q_hidden", "draft_tokens")
+    if V != Vq:
+        raise ValueError("the two heads must have one vocabulary")
+    if q_hidden.dtype != p_hidden.dtype:
+        raise TypeError("p_hidden and q_hidden must have one type")
+    lam = (C.c_float * len(lambdas))(*[float(x) for x in lambdas])
+    dev = p_hidden.device
+    labels = torch.empty((len(lambdas), N), dtype=torch.uint8, device=dev)
+    ratio = torch.empty((N,), dtype=torch.float32, device=dev) if want_ratio else None
+    _same_device(ws, p_hidden, p_W, q_hidden, q_W, draft_tokens)
+    rc = lib().verifier_labels_head(_ptr(p_hidden), _ptr(p_W), dp, _ptr(q_hidden), _ptr(q_W), dq, _ptr(draft_tokens), N, V,
+                                    _dt(p_hidden), C.cast(lam, C.c_void_p), len(lambdas), _ptr(labels), _ptr(ratio),
+                                    _ptr(ws.buf), ws.nbytes, _stream())
+    _check("verifier_labels_head", rc)
+    return labels, ratio
+
+
+def pack8_pitch(d: int) -> int:
+    """Bytes of a packed row of d elements."""
+    return int(lib().spr_pack8_pitch(d))
+
+
+def _packed(packed, d: int):
+    _dev(packed, torch.uint8, "packed")
+    if packed.dim() != 2 or packed.shape[1] != pack8_pitch(d) or d <= 0:
+        raise ValueError(f"packed must be [N, {pack8_pitch(d)}] for d = {d}, got {tuple(packed.shape)}")
+    return packed.shape[0]
+
+
+def hidden_pack8(hidden, out=None):
+    """hidden [N,d] in 8 bits with an exponent per 32 elements: u8 [N, pack8_pitch(d)]."""
+    _dev(hidden, name="hidden")
+    N, d = hidden.shape
+    packed = _result(out, (N, pack8_pitch(d)), torch.uint8, hidden.device, "packed")
+    _same_device(None, hidden, packed)
+    _check("hidden_pack8", lib().hidden_pack8(_ptr(hidden), N, d, _dt(hidden), _ptr(packed), _stream()))
+    return packed
+
+
+def hidden_unpack8(packed, d: int, dtype=torch.bfloat16, out=None):
+    """The values [N,d] that packed rows stand for (exact in bf16 and fp32)."""
+    N = _packed(packed, d)
+    hidden = _result(out, (N, d), dtype, packed.device, "hidden")
+    _same_device(None, packed, hidden)
+    _check("hidden_unpack8", lib().hidden_unpack8(_ptr(packed), N, d, _dt(hidden), _ptr(hidden), _stream()))
+    return hidden
+
+
+def verifier_train_step8(packed, d: int, labels, theta, adam_m, adam_v, t: int, lr: float, ws: Workspace,
+                         beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, loss=None):
+    """verifier_train_step on hidden states kept in 8 bits: packed u8 [N, pack8_pitch(d)]."""
+    N = _packed(packed, d)
+    _dev(labels, torch.uint8, "labels")
+    for name, a in (("theta", theta), ("adam_m", adam_m), ("adam_v", adam_v)):
+        _dev(a, torch.float32, name)
+        if a.numel() != d + 1:
+            raise ValueError(f"{name} must have d + 1 entries")
+    if labels.numel() != N:
+        raise ValueError("labels must have one entry per hidden state")
+    loss = _result(loss, (1,), torch.float32, packed.device, "loss")
+    _same_device(ws, packed, labels, theta, adam_m, adam_v, loss)
+    rc = lib().verifier_train_step8(_ptr(packed), _ptr(labels), N, d, _ptr(theta), _ptr(adam_m), _ptr(adam_v), t, lr,
+                                    beta1, beta2, eps, _ptr(loss), _ptr(ws.buf), ws.nbytes, _stream())
+    _check("verifier_train_step8", rc)
     return loss
 
 

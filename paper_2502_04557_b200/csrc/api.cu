@@ -200,6 +200,17 @@ size_t spr_workspace_bytes(int op, int B, int K, int V, int d, int h, int dt)
     case SPR_OP_VERIFIER_TRAIN:
         if (d <= 0) return 0;
         return ws_bytes_of([&](Carver &c) { train_ws_layout(c, d); });
+    case SPR_OP_HEAD_LOSS:
+    case SPR_OP_HEAD_LOSS_GRAD:
+    case SPR_OP_VERIFIER_LABELS_HEAD: {
+        if (K <= 0 || (int64_t)B * K > 0x7fffffff) return 0;
+        const int64_t N = (int64_t)B * K;
+        return op == SPR_OP_HEAD_LOSS ? head_loss_ws_bytes(N, d, V, dt)
+               : op == SPR_OP_HEAD_LOSS_GRAD ? head_grad_ws_bytes(N, d, V, dt) : head_labels_ws_bytes(N, d, h, V, dt);
+    }
+    case SPR_OP_VERIFIER_TRAIN8:
+        if (d <= 0) return 0;
+        return ws_bytes_of([&](Carver &c) { train_ws_layout(c, d); });
     default:
         return 0;
     }

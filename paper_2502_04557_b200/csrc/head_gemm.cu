@@ -1,0 +1,504 @@
+// Matrix products of the vocabulary head (softmax cross entropy and its gradient) on CTA pairs.
+//
+//   logits = H W^T        kept nowhere: the epilogue turns a tile into row statistics, or into
+//                         the tile of the softmax gradient D
+//   dH = D W, dW = D^T H  D comes from the workspace
+//
+// Bound by the tensor pipe for batches of a few hundred tokens and more, by the sweep over W
+// below that.  A pair of CTAs (cluster of 2) owns a 256 x 256 tile: each CTA stages 128 rows of A
+// and 128 of B per 64-deep stage (32 KB by TMA, 128-byte swizzle, no multicast), one thread of the
+// even CTA issues tcgen05.mma.cta_group::2 for both, and the accumulator (256 fp32 columns in each
+// CTA's TMEM) is double-buffered: while the four epilogue warps work on one tile the next is
+// multiplied.  The grid is persistent, one CTA per SM.  An operand tile is loaded as 64 x 64 boxes
+// whether its contiguous axis runs along the contraction or across it, so that D and D^T, W and
+// W^T are read from one copy of each; the matrix descriptors say which.
+//
+// fp32 operands: x = x0 + x1 + x2 with bf16 parts (8 significant bits each: the remainder is
+// below 2^-24 |x|).  The six products of parts with i + j <= 2 make the result exact to about
+// 2^-23; they are accumulated smallest first, so that the roundings of the accumulator that
+// count are those of the last product alone.
+//
+// Warp roles (192 threads): warp 0 = TMA producer, warp 1 = TMEM owner and MMA issuer, warps
+// 2..5 = epilogue (warp w reads TMEM lanes 32 (w % 4) .. + 31).  Every wait is bounded: when one
+// runs out the status word becomes SPR_ERR_TIMEOUT, all roles leave their loops, the even CTA
+// waits (again bounded) for the copies and products in flight, and both CTAs meet before they exit.
+#include <atomic>
+
+#include "head_gemm.h"
+#include "launch.h"
+#include "tensor_pair.cuh"
+#include "vocab_common.cuh"
+
+namespace spr {
+
+namespace {
+
+using namespace pairtc;
+
+constexpr int kPairThreads = 192;
+constexpr int kHalfBytes = 128 * kPairBlockK * 2;       // this CTA's half of an operand tile: two 64 x 64 boxes
+constexpr int kBoxBytes = 64 * 64 * 2;
+constexpr int kStageBytes = 2 * kHalfBytes;
+constexpr int kStages = 6;
+constexpr int kTmemCols = 512;                          // two accumulators of 256 columns
+
+struct PairControl {
+    uint64_t full[kStages];
+    uint64_t empty[kStages];
+    uint64_t acc_full[2];
+    uint64_t acc_empty[2];
+    uint64_t drain;
+    uint32_t tmem_base;
+    int abort;
+    long long consumed;      // stages whose operands the MMA issuer saw arrive
+};
+constexpr size_t kPairSmem = (size_t)kStages * kStageBytes + 1024 + sizeof(PairControl);
+
+// what a pair does, in order: its items of job 0, then its run of job 1
+struct Item {
+    int job, m, n, split;
+};
+__device__ __forceinline__ int items_of_pair(const PairParams &prm, int pair, int pairs)
+{
+    const int n0 = pair < prm.items[0] ? (prm.items[0] - pair + pairs - 1) / pairs : 0;
+    return n0 + (prm.items[1] ? prm.count1[pair] : 0);
+}
+__device__ __forceinline__ Item get_item(const PairParams &prm, int pair, int pairs, int i)
+{
+    const int n0 = pair < prm.items[0] ? (prm.items[0] - pair + pairs - 1) / pairs : 0;
+    Item it;
+    it.job = i < n0 ? 0 : 1;
+    const PairJob &j = prm.job[it.job];
+    int x = i < n0 ? pair + i * pairs : prm.begin1[pair] + (i - n0);
+    // rows run fastest where there are few row tiles (the tokens of a head product): concurrent
+    // tiles then share the columns' operand
+    const int tiles = j.tiles_m * j.tiles_n;
+    it.split = x / tiles;
+    x -= it.split * tiles;
+    if (j.tiles_m <= j.tiles_n) {
+        it.n = x / j.tiles_m;
+        it.m = x - it.n * j.tiles_m;
+    } else {
+        it.m = x / j.tiles_n;
+        it.n = x - it.m * j.tiles_n;
+    }
+    return it;
+}
+__device__ __forceinline__ int item_blocks(const PairJob &j, int split) { return min(j.kb_per, j.kb - split * j.kb_per); }
+
+// parts of A and B in product p of 6: (0,2) (2,0) (1,1) (0,1) (1,0) (0,0)
+__device__ __forceinline__ int part_a(int nprod, int p) { return nprod == 1 ? 0 : (0x021010 >> (4 * (5 - p))) & 15; }
+__device__ __forceinline__ int part_b(int nprod, int p) { return nprod == 1 ? 0 : (0x201100 >> (4 * (5 - p))) & 15; }
+
+// ---------------------------------------------------------------- epilogues (one thread = one row)
+struct Stats {
+    float m, s;
+};
+// (max, sum of exp) over 64 more logits of the row; v of them exist
+__device__ __forceinline__ void add_stats(Stats &a, float (&x)[2][32], int v)
+{
+    if (v < 64) {
+#pragma unroll
+        for (int j = 0; j < 64; ++j)
+            if (j >= v) x[j >> 5][j & 31] = neg_inf();
+    }
+    float t[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t[j] = fmaxf(x[0][j], x[1][j]);
+#pragma unroll
+    for (int k = 8; k < 32; k += 8)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = fmaxf(t[j], fmaxf(x[0][k + j], x[1][k + j]));
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1)
+#pragma unroll
+        for (int j = 0; j < o; ++j) t[j] = fmaxf(t[j], t[j + o]);
+    const float m = fmaxf(a.m, t[0]);
+    const float ref = m == neg_inf() ? 0.f : m;
+    // x - ref first: the largest term is then exactly 1 whatever the size of the logits
+    const uint64_t neg2 = pack2(-ref, -ref), log2 = pack2(kLog2e, kLog2e);
+    uint64_t s[2] = {pack2(a.s * ex2((a.m - ref) * kLog2e), 0.f), pack2(0.f, 0.f)};
+#pragma unroll
+    for (int j = 0; j < 64; j += 2) {
+        float t0, t1;
+        unpack2(mul2(add2(pack2(x[j >> 5][j & 31], x[j >> 5][(j & 31) + 1]), neg2), log2), t0, t1);
+        s[(j >> 1) & 1] = add2(s[(j >> 1) & 1], pack2(ex2(t0), ex2(t1)));
+    }
+    float t0, t1;
+    unpack2(add2(s[0], s[1]), t0, t1);
+    a.m = m;
+    a.s = t0 + t1;
+}
+
+// the caller's type: 32 consecutive elements of a row; `vec` says that 32-byte stores are aligned
+__device__ __forceinline__ void store_row32(float *p, const float (&x)[32], int v, bool vec)
+{
+    if (vec && v >= 32) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            uint32_t w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(x[8 * q + e]);
+            store32(p + 8 * q, w);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+            if (e < v) p[e] = x[e];
+    }
+}
+__device__ __forceinline__ void store_row32(__nv_bfloat16 *p, const float (&x)[32], int v, bool vec)
+{
+    if (vec && v >= 32) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            uint32_t w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = pack_bf16(x[16 * q + 2 * e], x[16 * q + 2 * e + 1]);
+            store32(p + 16 * q, w);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+            if (e < v) p[e] = __float2bfloat16(x[e]);
+    }
+}
+
+template <int EPI, typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ CUtensorMap map_b0,
+            const __grid_constant__ CUtensorMap map_a1, const __grid_constant__ CUtensorMap map_b1,
+            const __grid_constant__ PairParams prm)
+{
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *ring = reinterpret_cast<unsigned char *>(
+        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    PairControl *ctl = reinterpret_cast<PairControl *>(ring + kStages * kStageBytes);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = (int)cluster_rank();
+    const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
+    const int n_items = items_of_pair(prm, pair, pairs);
+    const uint32_t limit = prm.spin_limit;
+
+    if (tid == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            bar_init(&ctl->full[s], 1);
+            bar_init(&ctl->empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            bar_init(&ctl->acc_full[b], 1);
+            bar_init(&ctl->acc_empty[b], 8);       // four epilogue warps of each CTA
+        }
+        bar_init(&ctl->drain, 1);
+        ctl->abort = 0;
+        ctl->consumed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&ctl->tmem_base)),
+                     "r"((uint32_t)kTmemCols)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = ctl->tmem_base;
+    // both CTAs have set up their barriers: copies and commits of one count on the other's
+    cluster_arrive();
+    cluster_wait();
+
+    long long issued = 0;
+    if (warp == 0) {
+        // ---------------- producer: lanes 0, 1 load the boxes of A, lanes 2, 3 those of B
+        if (lane < 4 && !(prm.test_flags & PAIR_TEST_NO_LOADS)) {
+            const bool is_b = lane >> 1;
+            int s = 0;
+            uint32_t par = 1;
+            for (int i = 0; i < n_items; ++i) {
+                const Item it = get_item(prm, pair, pairs, i);
+                const PairJob &j = prm.job[it.job];
+                const CUtensorMap *map = it.job ? (is_b ? &map_b1 : &map_a1) : (is_b ? &map_b0 : &map_a0);
+                const bool across = is_b ? j.b_across : j.a_across;
+                const int seg = is_b ? j.b_seg : j.a_seg;
+                const int mn = (is_b ? it.n : it.m) * kPairTile + rank * 128 + (lane & 1) * 64;
+                const int kb0 = it.split * j.kb_per, kbs = item_blocks(j, it.split);
+                bool ok = true;
+                for (int p = 0; p < j.nprod && ok; ++p) {
+                    const int off = seg * (is_b ? part_b(j.nprod, p) : part_a(j.nprod, p));
+                    for (int k = 0; k < kbs; ++k) {
+                        ok = bar_wait(&ctl->empty[s], par, &ctl->abort, prm.status, limit);
+                        if (!ok) break;
+                        if (lane == 0 && rank == 0) bar_expect(&ctl->full[s], 2 * kStageBytes);
+                        const int kc = (kb0 + k) * kPairBlockK;
+                        load_box(smem_addr(ring + s * kStageBytes) + lane * kBoxBytes, map, across ? mn + off : kc + off,
+                                 across ? kc : mn, &ctl->full[s]);
+                        ++issued;
+                        if (++s == kStages) {
+                            s = 0;
+                            par ^= 1u;
+                        }
+                    }
+                }
+                if (!ok) break;
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA issuer: one thread of the even CTA, for both
+        if (lane == 0 && rank == 0) {
+            int s = 0;
+            uint32_t par = 0;
+            long long used = 0;
+            bool ok = true;
+            for (int i = 0; i < n_items && ok; ++i) {
+                const Item it = get_item(prm, pair, pairs, i);
+                const PairJob &j = prm.job[it.job];
+                const bool aa = j.a_across, ba = j.b_across;
+                // bf16 x bf16 -> fp32, M = N = 256
+                const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)aa << 15) | ((uint32_t)ba << 16) |
+                                       ((uint32_t)(kPairTile >> 3) << 17) | ((uint32_t)(kPairTile >> 4) << 24);
+                // 16 further along K: 32 bytes inside the swizzle row, or two 8-deep groups
+                const uint64_t a_step = (aa ? 2048 : 32) >> 4, b_step = (ba ? 2048 : 32) >> 4;
+                const int steps = j.nprod * item_blocks(j, it.split);
+                const int buf = i & 1;
+                const uint32_t acc = tmem + (uint32_t)(buf * kPairTile);
+                ok = bar_wait(&ctl->acc_empty[buf], (uint32_t)((i >> 1) & 1) ^ 1u, &ctl->abort, prm.status, limit);
+                if (!ok) break;
+                fence_after();
+                for (int k = 0; k < steps; ++k) {
+                    ok = bar_wait(&ctl->full[s], par, &ctl->abort, prm.status, limit);
+                    if (!ok) break;
+                    fence_after();
+                    const uint32_t a_addr = smem_addr(ring + s * kStageBytes);
+                    const uint64_t da = tile_desc(a_addr, aa), db = tile_desc(a_addr + kHalfBytes, ba);
+#pragma unroll
+                    for (int q = 0; q < kPairBlockK / 16; ++q)
+                        mma_pair(acc, da + q * a_step, db + q * b_step, idesc, (k | q) != 0 ? 1u : 0u);
+                    commit_pair(&ctl->empty[s]);
+                    ++used;
+                    if (++s == kStages) {
+                        s = 0;
+                        par ^= 1u;
+                    }
+                }
+                if (ok) commit_pair(&ctl->acc_full[buf]);
+            }
+            ctl->consumed = used;
+            if (!ok) commit_pair(&ctl->drain);
+        }
+    } else {
+        // ---------------- epilogue
+        const int quarter = warp & 3;
+        const int r_in = rank * 128 + quarter * 32 + lane;
+        for (int i = 0; i < n_items; ++i) {
+            const Item it = get_item(prm, pair, pairs, i);
+            const PairJob &j = prm.job[it.job];
+            const int buf = i & 1;
+            if (!bar_wait(&ctl->acc_full[buf], (uint32_t)(i >> 1) & 1u, &ctl->abort, prm.status, limit)) break;
+            __syncwarp();
+            fence_after();
+            const uint32_t acc = tmem + (uint32_t)(buf * kPairTile) + ((uint32_t)(quarter * 32) << 16);
+            const int64_t row = (int64_t)it.m * kPairTile + r_in;
+            const bool live = row < j.rows;
+            const int c0 = it.n * kPairTile;
+            const int width = min(kPairTile, j.cols - c0);        // columns of the tile that exist
+            if (EPI == PAIR_STATS) {
+                Stats st = {neg_inf(), 0.f};
+                for (int c = 0; c < width; c += 64) {
+                    float x[2][32];
+                    tmem_read32(acc + c, x[0]);
+                    tmem_read32(acc + c + 32, x[1]);
+                    tmem_wait();
+                    add_stats(st, x, width - c);
+                }
+                if (live) j.part[row * j.tiles_n + it.n] = make_float2(st.m, st.s);
+            } else if (EPI == PAIR_DLOGITS) {
+                // D = g (exp(l - lse) - [v = target]); rows without a target are zero whatever they hold
+                const int t = live ? j.targets[row] : -1;
+                const bool keep = t >= 0 && t < j.V;
+                const float lse = keep ? j.lse[row] : 0.f, g = keep ? j.grad_loss[row] : 0.f;
+                const int hot = keep ? t - j.v0 - c0 : -1;
+                __nv_bfloat16 *dst = j.dlogits + row * j.dl_pitch + c0;
+                const int stored = min(kPairTile, j.dl_seg - c0);     // the padding up to a multiple of 64 is zeroed
+                for (int c = 0; c < stored; c += 32) {
+                    float x[32];
+                    tmem_read32(acc + c, x);
+                    tmem_wait();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const float p = sizeof(T) == 4 ? expf(x[e] - lse) : ex2((x[e] - lse) * kLog2e);
+                        x[e] = keep && c + e < width ? g * p : 0.f;
+                    }
+                    if (__any_sync(0xffffffffu, hot >= c && hot < c + 32)) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (hot == c + e) x[e] -= g;
+                    }
+                    if (live) {
+                        for (int part = 0; part < (sizeof(T) == 4 ? 3 : 1); ++part) {
+                            store_row32(dst + (int64_t)part * j.dl_seg + c, x, 32, true);
+                            if (sizeof(T) == 4) {
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) x[e] -= __bfloat162float(__float2bfloat16(x[e]));
+                            }
+                        }
+                    }
+                    __syncwarp();
+                }
+            } else {
+                float *a = j.acc ? j.acc + (int64_t)it.split * j.acc_stride + row * j.acc_pitch + c0 : nullptr;
+                T *o = j.out ? static_cast<T *>(j.out) + row * j.out_pitch + c0 : nullptr;
+                const bool vec = ((reinterpret_cast<uintptr_t>(j.out) | (uintptr_t)(j.out_pitch * (int64_t)sizeof(T))) & 31) == 0;
+                for (int c = 0; c < width; c += 32) {
+                    float x[32];
+                    tmem_read32(acc + c, x);
+                    tmem_wait();
+                    if (live) {
+                        if (j.add_acc) {      // the pitch covers whole groups of 32
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) {
+                                const float4 y = *reinterpret_cast<const float4 *>(a + c + 4 * q);
+                                x[4 * q] += y.x;
+                                x[4 * q + 1] += y.y;
+                                x[4 * q + 2] += y.z;
+                                x[4 * q + 3] += y.w;
+                            }
+                        }
+                        if (o) store_row32(o + c, x, width - c, vec);
+                        else store_row32(a + c, x, 32, true);
+                    }
+                    __syncwarp();
+                }
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive_even(&ctl->acc_empty[buf]);
+        }
+    }
+
+    // ---------------- way out
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    if (*reinterpret_cast<volatile int *>(&ctl->abort)) {
+        // copies and products in flight get a bounded time to end
+        if (warp == 0 && lane == 0 && rank == 0) {
+            const long long used = *reinterpret_cast<volatile long long *>(&ctl->consumed);
+            for (long long st = used; st < issued; ++st)
+                bar_wait_quiet(&ctl->full[st % kStages], (uint32_t)(st / kStages) & 1u, 1u << 20);
+        }
+        if (warp == 1 && lane == 0 && rank == 0) bar_wait_quiet(&ctl->drain, 0, 1u << 20);
+        __syncthreads();
+    }
+    cluster_arrive();
+    cluster_wait();
+    if (warp == 1) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kTmemCols)
+                     : "memory");
+    }
+}
+
+// ---------------------------------------------------------------- host side
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                  CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn()
+{
+    static const EncodeTiledFn fn = [] {   // initialised once, thread-safe
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            return reinterpret_cast<EncodeTiledFn>(p);
+        return static_cast<EncodeTiledFn>(nullptr);
+    }();
+    return fn;
+}
+
+// boxes of 64 x 64 elements, 128-byte swizzle, zeros outside
+bool make_map(CUtensorMap *map, const PairOperand &t)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)t.cols, (cuuint64_t)t.rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)t.pitch * 2};
+    const cuuint32_t box[2] = {64, 64};
+    const cuuint32_t elem[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(t.base), dims, strides, box, elem,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int EPI, typename T>
+cudaError_t launch(const CUtensorMap (&maps)[4], const PairParams &prm, int ctas, int dev, cudaStream_t st)
+{
+    static std::atomic<bool> attr_set[64];   // host threads may race to set it: all of them store `true`
+    if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
+        const cudaError_t e = cudaFuncSetAttribute(pair_kernel<EPI, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   (int)kPairSmem);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
+    }
+    pair_kernel<EPI, T><<<ctas, kPairThreads, kPairSmem, st>>>(maps[0], maps[1], maps[2], maps[3], prm);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_pair(PairEpilogue epi, bool f32, PairParams &prm, int njobs, const PairOperand *a,
+                        const PairOperand *b, cudaStream_t st)
+{
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    CUtensorMap maps[4];
+    for (int i = 0; i < 2; ++i) {
+        const int k = i < njobs ? i : 0;
+        if (!make_map(&maps[2 * i], a[k]) || !make_map(&maps[2 * i + 1], b[k])) return cudaErrorInvalidValue;
+    }
+    int pairs = sms / 2 < kMaxPairs ? sms / 2 : kMaxPairs;
+    int64_t total = 0;
+    double work = 0.0, len[2] = {0.0, 0.0};
+    for (int i = 0; i < 2; ++i) {
+        prm.items[i] = 0;
+        if (i >= njobs) continue;
+        const PairJob &j = prm.job[i];
+        const int64_t n = (int64_t)j.tiles_m * j.tiles_n * j.splits;
+        if (n > 0x3fffffff) return cudaErrorInvalidValue;
+        prm.items[i] = (int)n;
+        total += n;
+        len[i] = (double)j.nprod * j.kb_per + 2.0;      // in blocks, with about two blocks' time of turn-around
+        work += len[i] * (double)n;
+    }
+    if (total < pairs) pairs = (int)total;
+    if (prm.items[1]) {
+        // job 1 fills every pair up to the same share of the work
+        const double share = work / pairs;
+        double owed = 0.0;
+        int next = 0;
+        for (int p = 0; p < pairs; ++p) {
+            const int n0 = p < prm.items[0] ? (prm.items[0] - p + pairs - 1) / pairs : 0;
+            owed += share - n0 * len[0];
+            int n1 = owed > 0.0 ? (int)(owed / len[1] + 0.5) : 0;
+            if (p == pairs - 1 || n1 > prm.items[1] - next) n1 = prm.items[1] - next;
+            prm.begin1[p] = next;
+            prm.count1[p] = n1;
+            next += n1;
+            owed -= n1 * len[1];
+        }
+    }
+    if (!prm.spin_limit) prm.spin_limit = pairtc::kSpinLimit;
+    switch (epi) {
+    case PAIR_STATS: return launch<PAIR_STATS, float>(maps, prm, 2 * pairs, dev, st);    // the same for both types
+    case PAIR_DLOGITS: return f32 ? launch<PAIR_DLOGITS, float>(maps, prm, 2 * pairs, dev, st)
+                                  : launch<PAIR_DLOGITS, __nv_bfloat16>(maps, prm, 2 * pairs, dev, st);
+    default: return f32 ? launch<PAIR_OUT, float>(maps, prm, 2 * pairs, dev, st)
+                        : launch<PAIR_OUT, __nv_bfloat16>(maps, prm, 2 * pairs, dev, st);
+    }
+}
+
+}  // namespace spr

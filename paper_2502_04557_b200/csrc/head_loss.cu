@@ -1,0 +1,574 @@
+// Softmax cross entropy of hidden states under a vocabulary head, its gradient, and training
+// labels of the verifier from the hidden states and heads of two models - logits are never kept.
+//
+// With l = H W^T (H [N,d] hidden states, W [V,d] head, as in nn.Linear):
+//   lse_i = log sum_v exp(l_iv),  loss_i = lse_i - l_{i,t_i}
+//   D_iv = g_i (exp(l_iv - lse_i) - [v = t_i]),  dH = D W,  dW = D^T H
+//   log p(x_i) = l_{i,x_i} - lse_i
+// The products run on CTA pairs (head_gemm.cu).  Forward: one product whose epilogue leaves (max,
+// sum of exp) per row and 256 columns, then a warp per row that merges them and forms the target's
+// logit as a dot product of its own - N rows of W, nothing beside the product, and exact to a few
+// units of fp32 however the product's accumulator rounds.  Backward: the vocabulary goes by in
+// pieces; a piece's D is kept in the workspace (bf16, or three bf16 parts for fp32), and one launch
+// then adds D W to dH and writes the piece's rows of dW.
+//
+// Rounding D to bf16 costs a relative 2^-9 per element, the size of the rounding of the bf16
+// result itself; sums over D are held in fp32 throughout.
+#include <string.h>
+
+#include "common.cuh"
+#include "head_gemm.h"
+#include "host_util.h"
+#include "launch.h"
+
+namespace spr {
+
+namespace {
+
+constexpr int kHeadMaxLambdas = 8;
+constexpr int kRowWarps = 8;                             // rows per CTA of the finish kernels
+constexpr size_t kPieceBytes = (size_t)256 << 20;        // D of one vocabulary piece (see pieces())
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+
+// ---------------------------------------------------------------- operands in tensor-core form
+// fp32 and rows that are not a multiple of 16 bytes are copied into [rows, parts * pitch] bf16, pitch
+// a multiple of 64, zeros behind column d.  Rows whose target is negative or outside the
+// vocabulary are zeroed, so that whatever a padded row holds (infinities, NaN) reaches no sum.
+template <typename T>
+__global__ void __launch_bounds__(256) head_pack_kernel(const T *src, int64_t rows, int d, int pitch,
+                                                        const int32_t *targets, int V, __nv_bfloat16 *dst, int *status)
+{
+    constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+    const int groups = pitch / 8;
+    const int64_t n = rows * groups;
+    const bool vec = sizeof(T) == 4 ? d % 4 == 0 : d % 8 == 0;      // whole 16-byte vectors (the base is aligned)
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t r = i / groups;
+        const int c = (int)(i - r * groups) * 8;
+        const T *p = src + r * d + c;
+        bool keep = true;
+        if (targets) {
+            const int t = targets[r];
+            keep = t >= 0 && t < V;
+            if (t >= V && c == 0) raise_status(status, SPR_ERR_BAD_TOKEN);
+        }
+        float x[8];
+        if (keep && vec && c + 8 <= d) {
+            if (sizeof(T) == 4) {
+                const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+                x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+            } else {
+                const uint4 a = *reinterpret_cast<const uint4 *>(p);
+                const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[2 * e] = __uint_as_float(w[e] << 16);
+                    x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = keep && c + e < d ? (float)p[e] : 0.f;
+        }
+        __nv_bfloat16 *q = dst + r * (int64_t)(kParts * pitch) + c;
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * e], x[2 * e + 1]);
+                w[e] = *reinterpret_cast<const uint32_t *>(&b);
+                x[2 * e] -= __low2float(b);
+                x[2 * e + 1] -= __high2float(b);
+            }
+            *reinterpret_cast<uint4 *>(q + (int64_t)part * pitch) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- row statistics -> outputs
+struct HeadRow {
+    const void *hidden, *W;
+    const float2 *part;      // [N, tiles]
+    int d, tiles;
+};
+
+// one warp: log-sum-exp of row i
+__device__ __forceinline__ double row_lse(const HeadRow &h, int64_t i, int lane)
+{
+    MS a = {neg_inf(), 0.f};
+    const float2 *p = h.part + i * h.tiles;
+    for (int t = lane; t < h.tiles; t += 32) {
+        const float2 x = p[t];
+        a = ms_merge(a, MS{x.x, x.y});
+    }
+    a = warp_ms(a);
+    return (double)a.m + log((double)a.s);
+}
+// one warp: hidden_i . W_t, fp32 products summed in double (lane and column order fixed)
+template <typename T>
+__device__ __forceinline__ double row_logit(const HeadRow &h, int64_t i, int t, int lane)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    const T *a = static_cast<const T *>(h.hidden) + i * h.d, *b = static_cast<const T *>(h.W) + (int64_t)t * h.d;
+    double s = 0.0;
+    if (h.d % N == 0) {
+        for (int c = lane * N; c < h.d; c += 32 * N) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(a + c), y = *reinterpret_cast<const uint4 *>(b + c);
+            const uint32_t u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
+            if (sizeof(T) == 4) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s += (double)__uint_as_float(u[e]) * (double)__uint_as_float(v[e]);
+            } else {
+                float f = 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    f = fmaf(__uint_as_float(u[e] << 16), __uint_as_float(v[e] << 16), f);
+                    f = fmaf(__uint_as_float(u[e] & 0xffff0000u), __uint_as_float(v[e] & 0xffff0000u), f);
+                }
+                s += (double)f;
+            }
+        }
+    } else {
+        for (int c = lane; c < h.d; c += 32) s += (double)(float)a[c] * (double)(float)b[c];
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    return s;
+}
+
+__device__ __forceinline__ bool gave_up(const int *status) { return *reinterpret_cast<const volatile int *>(status) == SPR_ERR_TIMEOUT; }
+
+template <typename T>
+__global__ void __launch_bounds__(32 * kRowWarps) head_finish_kernel(const HeadRow h, int64_t N, int V, const int32_t *targets,
+                                                                     float *loss, float *lse, int *status)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t i = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+    if (i >= N) return;
+    const double z = gave_up(status) ? (double)__int_as_float(0x7fc00000) : row_lse(h, i, lane);
+    const int t = targets[i];
+    double l = 0.0;
+    if (t >= 0 && t < V) {
+        l = z - row_logit<T>(h, i, t, lane);
+        if (l < 0.0) l = 0.0;        // -log p is not negative: rounding alone can make it so (NaN stays)
+    } else if (t >= V) {
+        l = -1.0;
+        if (lane == 0) raise_status(status, SPR_ERR_BAD_TOKEN);
+    }
+    if (lane == 0) {
+        loss[i] = (float)l;
+        if (lse) lse[i] = (float)z;
+    }
+}
+
+struct HeadLabels {
+    int n_lambda;
+    float lambdas[kHeadMaxLambdas];
+    uint8_t *labels;     // [n_lambda, N]
+    float *ratio;        // [N] or null
+};
+template <typename T>
+__global__ void __launch_bounds__(32 * kRowWarps) head_labels_kernel(const HeadRow p, const HeadRow q, int64_t N, int V,
+                                                                     const int32_t *tokens, const HeadLabels out, int *status)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t i = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+    if (i >= N) return;
+    const int x = tokens[i];
+    double ratio = -1.0;
+    const bool valid = x >= 0 && x < V;
+    if (valid) {
+        const double log_p = row_logit<T>(p, i, x, lane) - row_lse(p, i, lane);
+        const double log_q = row_logit<T>(q, i, x, lane) - row_lse(q, i, lane);
+        ratio = exp(log_q - log_p);
+        if (gave_up(status)) ratio = (double)__int_as_float(0x7fc00000);
+    } else if (lane == 0) {
+        raise_status(status, SPR_ERR_BAD_TOKEN);
+    }
+    if (lane < out.n_lambda) out.labels[(int64_t)lane * N + i] = (valid && ratio <= (double)out.lambdas[lane]) ? 1 : 0;
+    if (lane == 0 && out.ratio) out.ratio[i] = (float)ratio;
+}
+
+// out[r, c] = sum over the slices, in order
+template <typename T>
+__global__ void __launch_bounds__(256) head_sum_kernel(const float *acc, int slices, int64_t stride, int pitch, int64_t rows,
+                                                       int d, T *out)
+{
+    const int groups = (d + 3) / 4;
+    const int64_t n = rows * groups;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t r = i / groups;
+        const int c = (int)(i - r * groups) * 4;
+        const float *p = acc + r * pitch + c;
+        float4 s = *reinterpret_cast<const float4 *>(p);
+        for (int k = 1; k < slices; ++k) {
+            const float4 x = *reinterpret_cast<const float4 *>(p + k * stride);
+            s.x += x.x;
+            s.y += x.y;
+            s.z += x.z;
+            s.w += x.w;
+        }
+        const float v[4] = {s.x, s.y, s.z, s.w};
+        T *o = out + r * d + c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < d) o[e] = (T)v[e];
+    }
+}
+
+// ---------------------------------------------------------------- workspace
+bool needs_pack(int d, int dt) { return dt == SPR_F32 || d % 8 != 0; }
+int parts(int dt) { return dt == SPR_F32 ? 3 : 1; }
+size_t packed_bytes(int64_t rows, int d, int dt) { return 2 * (size_t)rows * parts(dt) * (size_t)round_up(d, 64); }
+
+struct HeadLossWs {
+    size_t hidden, W;     // packed operands (0 bytes where the caller's tensors serve)
+    size_t part;          // float2 [N, tiles]
+};
+HeadLossWs head_loss_layout(Carver &c, int64_t N, int d, int V, int dt)
+{
+    HeadLossWs w;
+    w.hidden = c.take_data(needs_pack(d, dt) ? packed_bytes(N, d, dt) : 0);
+    w.W = c.take_data(needs_pack(d, dt) ? packed_bytes(V, d, dt) : 0);
+    w.part = c.take_data(8 * (size_t)N * (size_t)ceil_div(V, kPairTile));
+    return w;
+}
+
+// How the vocabulary is cut.  A piece's D takes about 256 MB, so that the workspace does not grow with
+// N V, but has at least 8192 columns: dH is read and written once per piece, which a contraction that
+// deep hides.  The pieces are of one width, a multiple of the tile.
+struct Pieces {
+    int width, count;
+    int kb_per, splits;   // dH = D W: the contraction over a piece is cut into `splits` ranges
+};
+Pieces pieces(int64_t N, int d, int V, int dt)
+{
+    Pieces p;
+    int64_t most = (int64_t)(kPieceBytes / (2 * (size_t)parts(dt) * (size_t)N)) / kPairTile * kPairTile;
+    if (most < 8192) most = 8192;
+    p.count = (int)ceil_div(V, most);
+    p.width = (int)round_up(ceil_div(V, p.count), kPairTile);
+    p.count = (int)ceil_div(V, p.width);
+    // dH has few tiles with a long contraction, dW many with a short one, in one launch: no dH item is
+    // longer than half of a pair's share (74 pairs), so that dW evens the pairs out
+    const int64_t kb_v = ceil_div(p.count > 1 ? p.width : V, kPairBlockK), kb_n = ceil_div(N, kPairBlockK), td = ceil_div(d, kPairTile);
+    const double share = (double)(ceil_div(N, kPairTile) * td * kb_v + p.width / kPairTile * td * kb_n) / 74.0;
+    int64_t s = (int64_t)(2.0 * (double)kb_v / share) + 1;
+    if (s > kb_v / 4) s = kb_v / 4;
+    if (s > 32) s = 32;
+    if (s < 1) s = 1;
+    p.kb_per = (int)ceil_div(kb_v, s);
+    p.splits = (int)ceil_div(kb_v, p.kb_per);
+    return p;
+}
+
+struct HeadGradWs {
+    size_t hidden;        // packed hidden states, rows without a target zeroed
+    size_t W;             // packed head (0 bytes where the caller's serves)
+    size_t dlogits;       // bf16 [N, parts * width]
+    size_t acc;           // float [splits, N, round_up(d, 64)], where dH takes more than one launch or range
+};
+HeadGradWs head_grad_layout(Carver &c, int64_t N, int d, int V, int dt)
+{
+    const Pieces p = pieces(N, d, V, dt);
+    HeadGradWs w;
+    w.hidden = c.take_data(packed_bytes(N, d, dt));
+    w.W = c.take_data(needs_pack(d, dt) ? packed_bytes(V, d, dt) : 0);
+    w.dlogits = c.take_data(2 * (size_t)N * parts(dt) * (size_t)p.width);
+    w.acc = c.take_data(p.count * p.splits > 1 ? 4 * (size_t)p.splits * (size_t)N * (size_t)round_up(d, 64) : 0);
+    return w;
+}
+
+struct HeadLabelsWs {
+    HeadLossWs p, q;
+};
+HeadLabelsWs head_labels_layout(Carver &c, int64_t N, int dp, int dq, int V, int dt)
+{
+    HeadLabelsWs w;
+    w.p = head_loss_layout(c, N, dp, V, dt);
+    w.q = head_loss_layout(c, N, dq, V, dt);
+    return w;
+}
+
+// ---------------------------------------------------------------- launches
+template <typename T>
+cudaError_t pack_rows(const void *src, int64_t rows, int d, const int32_t *targets, int V, void *dst, int *status, cudaStream_t st)
+{
+    const int pitch = (int)round_up(d, 64);
+    const int64_t blocks = ceil_div(rows * (pitch / 8), 256);
+    head_pack_kernel<T><<<(unsigned)(blocks < 148 * 16 ? blocks : 148 * 16), 256, 0, st>>>(
+        static_cast<const T *>(src), rows, d, pitch, targets, V, static_cast<__nv_bfloat16 *>(dst), status);
+    return cudaGetLastError();
+}
+cudaError_t pack(const void *src, int64_t rows, int d, int dt, const int32_t *targets, int V, void *dst, int *status, cudaStream_t st)
+{
+    return dt == SPR_F32 ? pack_rows<float>(src, rows, d, targets, V, dst, status, st)
+                         : pack_rows<__nv_bfloat16>(src, rows, d, targets, V, dst, status, st);
+}
+// a packed operand, or the caller's tensor where it already has that form
+PairOperand packed_operand(const void *base, int64_t rows, int d, int dt)
+{
+    const int64_t pitch = parts(dt) * round_up(d, 64);
+    return PairOperand{base, rows, pitch, pitch};
+}
+PairOperand plain_operand(const void *base, int64_t rows, int d) { return PairOperand{base, rows, d, d}; }
+
+void contraction(PairJob &j, int64_t k, int dt)      // over k elements, in one range
+{
+    j.kb = j.kb_per = (int)ceil_div(k, kPairBlockK);
+    j.splits = 1;
+    j.nprod = dt == SPR_F32 ? 6 : 1;
+}
+
+// job and operands of the row statistics of hidden [N,d] under W [V,d]; packs what has to be packed
+cudaError_t stats_job(PairJob &j, PairOperand &a, PairOperand &b, const void *hidden, const void *W, int64_t N, int d, int V,
+                      int dt, void *ws, const HeadLossWs &lay, cudaStream_t st)
+{
+    cudaError_t e = cudaSuccess;
+    if (needs_pack(d, dt)) {
+        void *h = at<char>(ws, lay.hidden), *w = at<char>(ws, lay.W);
+        e = pack(hidden, N, d, dt, nullptr, 0, h, nullptr, st);
+        if (e == cudaSuccess) e = pack(W, V, d, dt, nullptr, 0, w, nullptr, st);
+        a = packed_operand(h, N, d, dt);
+        b = packed_operand(w, V, d, dt);
+    } else {
+        a = plain_operand(hidden, N, d);
+        b = plain_operand(W, V, d);
+    }
+    memset(&j, 0, sizeof j);
+    contraction(j, d, dt);
+    j.tiles_m = (int)ceil_div(N, kPairTile);
+    j.tiles_n = (int)ceil_div(V, kPairTile);
+    j.a_seg = j.b_seg = (int)round_up(d, 64);
+    j.rows = N;
+    j.cols = V;
+    j.part = at<float2>(ws, lay.part);
+    return e;
+}
+
+bool head_sizes_ok(int64_t N, int d, int V) { return N >= 0 && d > 0 && d <= (1 << 20) && V > 0 && V <= (1 << 30); }
+
+}  // namespace
+
+size_t head_loss_ws_bytes(int64_t N, int d, int V, int dt)
+{
+    if (N <= 0 || !head_sizes_ok(N, d, V)) return 0;
+    return ws_bytes_of([&](Carver &c) { head_loss_layout(c, N, d, V, dt); });
+}
+size_t head_grad_ws_bytes(int64_t N, int d, int V, int dt)
+{
+    if (N <= 0 || !head_sizes_ok(N, d, V)) return 0;
+    return ws_bytes_of([&](Carver &c) { head_grad_layout(c, N, d, V, dt); });
+}
+size_t head_labels_ws_bytes(int64_t N, int dp, int dq, int V, int dt)
+{
+    if (N <= 0 || !head_sizes_ok(N, dp, V) || !head_sizes_ok(N, dq, V)) return 0;
+    return ws_bytes_of([&](Carver &c) { head_labels_layout(c, N, dp, dq, V, dt); });
+}
+
+}  // namespace spr
+
+using namespace spr;
+
+extern "C" {
+
+int head_loss(const void *hidden, const void *W, const int32_t *targets, int N, int d, int V, int dt, float *loss, float *lse,
+              void *ws, size_t ws_bytes, void *cuda_stream)
+{
+    if (!dtype_ok(dt)) return SPR_ERR_UNSUPPORTED;
+    if (!head_sizes_ok(N, d, V)) return SPR_ERR_INVALID_ARG;
+    if (N == 0) return SPR_OK;
+    if (!hidden || !W || !targets || !loss) return SPR_ERR_INVALID_ARG;
+    if (!aligned(hidden, 16) || !aligned(W, 16) || !aligned(targets, 4) || !aligned(loss, 4) || (lse && !aligned(lse, 4)))
+        return SPR_ERR_INVALID_ARG;
+    Carver cv = carve(ws_bytes);
+    const HeadLossWs lay = head_loss_layout(cv, N, d, V, dt);
+    if (!ws || !aligned(ws, 256) || !cv.fits()) return SPR_ERR_WORKSPACE;
+    int rc = device_supported();
+    if (rc != SPR_OK) return rc;
+
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    PairParams prm;
+    memset(&prm, 0, sizeof prm);
+    prm.status = at<int>(ws, 0);
+    PairOperand a, b;
+    cudaError_t e = stats_job(prm.job[0], a, b, hidden, W, N, d, V, dt, ws, lay, st);
+    if (e == cudaSuccess) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, 1, &a, &b, st);
+    if (e == cudaSuccess) {
+        const HeadRow h = {hidden, W, prm.job[0].part, d, prm.job[0].tiles_n};
+        const unsigned ctas = (unsigned)ceil_div(N, kRowWarps);
+        if (dt == SPR_F32) head_finish_kernel<float><<<ctas, 32 * kRowWarps, 0, st>>>(h, N, V, targets, loss, lse, prm.status);
+        else head_finish_kernel<__nv_bfloat16><<<ctas, 32 * kRowWarps, 0, st>>>(h, N, V, targets, loss, lse, prm.status);
+        e = cudaGetLastError();
+    }
+    return finish(e);
+}
+
+int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, const float *lse, const float *grad_loss, int N,
+                   int d, int V, int dt, void *d_hidden, void *d_W, void *ws, size_t ws_bytes, void *cuda_stream)
+{
+    if (!dtype_ok(dt)) return SPR_ERR_UNSUPPORTED;
+    if (!head_sizes_ok(N, d, V)) return SPR_ERR_INVALID_ARG;
+    if (!d_hidden && !d_W) return SPR_ERR_INVALID_ARG;
+    if ((d_hidden && !aligned(d_hidden, 16)) || (d_W && !aligned(d_W, 16))) return SPR_ERR_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (N == 0) {        // no samples: the head's gradient is zero
+        if (!d_W) return SPR_OK;
+        const int rc = device_supported();
+        return rc != SPR_OK ? rc : finish(cudaMemsetAsync(d_W, 0, (size_t)V * d * elem_size(dt), st));
+    }
+    if (!hidden || !W || !targets || !lse || !grad_loss) return SPR_ERR_INVALID_ARG;
+    if (!aligned(hidden, 16) || !aligned(W, 16) || !aligned(targets, 4) || !aligned(lse, 4) || !aligned(grad_loss, 4))
+        return SPR_ERR_INVALID_ARG;
+    Carver cv = carve(ws_bytes);
+    const HeadGradWs lay = head_grad_layout(cv, N, d, V, dt);
+    if (!ws || !aligned(ws, 256) || !cv.fits()) return SPR_ERR_WORKSPACE;
+    int rc = device_supported();
+    if (rc != SPR_OK) return rc;
+
+    const bool f32 = dt == SPR_F32;
+    const size_t es = elem_size(dt);
+    const Pieces pc = pieces(N, d, V, dt);
+    const int dp = (int)round_up(d, 64);
+    void *hp = at<char>(ws, lay.hidden);
+    cudaError_t e = pack(hidden, N, d, dt, targets, V, hp, at<int>(ws, 0), st);
+    PairOperand wv = plain_operand(W, V, d);
+    if (e == cudaSuccess && needs_pack(d, dt)) {
+        e = pack(W, V, d, dt, nullptr, 0, at<char>(ws, lay.W), nullptr, st);
+        wv = packed_operand(at<char>(ws, lay.W), V, d, dt);
+    }
+    const PairOperand hv = packed_operand(hp, N, d, dt);
+    const PairOperand dv = {at<char>(ws, lay.dlogits), N, (int64_t)parts(dt) * pc.width, (int64_t)parts(dt) * pc.width};
+    for (int i = 0; i < pc.count && e == cudaSuccess; ++i) {
+        const int v0 = i * pc.width, width = V - v0 < pc.width ? V - v0 : pc.width;
+        PairOperand wp = wv;      // the piece's rows of W
+        wp.base = static_cast<const char *>(wv.base) + 2 * (size_t)v0 * (size_t)wv.pitch;
+        wp.rows = width;
+        PairParams prm;
+        memset(&prm, 0, sizeof prm);
+        prm.status = at<int>(ws, 0);
+        PairJob &j = prm.job[0];
+        contraction(j, d, dt);
+        j.tiles_m = (int)ceil_div(N, kPairTile);
+        j.tiles_n = (int)ceil_div(width, kPairTile);
+        j.a_seg = j.b_seg = dp;
+        j.rows = N;
+        j.cols = width;
+        j.dlogits = at<__nv_bfloat16>(ws, lay.dlogits);
+        j.dl_pitch = dv.pitch;
+        j.dl_seg = pc.width;
+        j.v0 = v0;
+        j.V = V;
+        j.lse = lse;
+        j.grad_loss = grad_loss;
+        j.targets = targets;
+        e = launch_pair(PAIR_DLOGITS, f32, prm, 1, &hv, &wp, st);
+        if (e != cudaSuccess) break;
+
+        memset(&prm, 0, sizeof prm);
+        prm.status = at<int>(ws, 0);
+        PairOperand a[2], b[2];
+        int jobs = 0;
+        if (d_hidden) {           // dH [N, d] += D [N, width] W [width, d]
+            PairJob &h = prm.job[jobs];
+            contraction(h, width, dt);
+            h.kb_per = pc.kb_per;
+            h.splits = (int)ceil_div(h.kb, h.kb_per);
+            h.tiles_m = (int)ceil_div(N, kPairTile);
+            h.tiles_n = (int)ceil_div(d, kPairTile);
+            h.b_across = 1;
+            h.a_seg = pc.width;
+            h.b_seg = dp;
+            h.rows = N;
+            h.cols = d;
+            if (pc.count * pc.splits > 1) {
+                h.acc = at<float>(ws, lay.acc);
+                h.acc_pitch = dp;
+                h.acc_stride = (int64_t)N * dp;
+                h.add_acc = i > 0;
+            }
+            if (pc.splits == 1 && i == pc.count - 1) {
+                h.out = d_hidden;
+                h.out_pitch = d;
+            }
+            a[jobs] = dv;
+            b[jobs] = wp;
+            ++jobs;
+        }
+        if (d_W) {                // dW [width, d] = D^T [width, N] H [N, d]
+            PairJob &w = prm.job[jobs];
+            contraction(w, N, dt);
+            w.tiles_m = (int)ceil_div(width, kPairTile);
+            w.tiles_n = (int)ceil_div(d, kPairTile);
+            w.a_across = w.b_across = 1;
+            w.a_seg = pc.width;
+            w.b_seg = dp;
+            w.rows = width;
+            w.cols = d;
+            w.out = static_cast<char *>(d_W) + (size_t)v0 * d * es;
+            w.out_pitch = d;
+            a[jobs] = dv;
+            b[jobs] = hv;
+            ++jobs;
+        }
+        e = launch_pair(PAIR_OUT, f32, prm, jobs, a, b, st);
+    }
+    if (e == cudaSuccess && d_hidden && pc.splits > 1) {
+        const int64_t blocks = ceil_div((int64_t)N * ((d + 3) / 4), 256);
+        const unsigned ctas = (unsigned)(blocks < 148 * 8 ? blocks : 148 * 8);
+        const float *acc = at<float>(ws, lay.acc);
+        if (f32) head_sum_kernel<float><<<ctas, 256, 0, st>>>(acc, pc.splits, (int64_t)N * dp, dp, N, d, static_cast<float *>(d_hidden));
+        else head_sum_kernel<__nv_bfloat16><<<ctas, 256, 0, st>>>(acc, pc.splits, (int64_t)N * dp, dp, N, d, static_cast<__nv_bfloat16 *>(d_hidden));
+        e = cudaGetLastError();
+    }
+    return finish(e);
+}
+
+int verifier_labels_head(const void *p_hidden, const void *p_W, int dp, const void *q_hidden, const void *q_W, int dq,
+                         const int32_t *draft_tokens, int N, int V, int dt, const float *lambdas, int n_lambda,
+                         uint8_t *labels, float *ratio, void *ws, size_t ws_bytes, void *cuda_stream)
+{
+    if (!dtype_ok(dt)) return SPR_ERR_UNSUPPORTED;
+    if (!head_sizes_ok(N, dp, V) || !head_sizes_ok(N, dq, V) || n_lambda <= 0 || n_lambda > kHeadMaxLambdas || !lambdas)
+        return SPR_ERR_INVALID_ARG;
+    if (N == 0) return SPR_OK;
+    if (!p_hidden || !p_W || !q_hidden || !q_W || !draft_tokens || !labels) return SPR_ERR_INVALID_ARG;
+    if (!aligned(p_hidden, 16) || !aligned(p_W, 16) || !aligned(q_hidden, 16) || !aligned(q_W, 16) ||
+        !aligned(draft_tokens, 4) || (ratio && !aligned(ratio, 4)))
+        return SPR_ERR_INVALID_ARG;
+    Carver cv = carve(ws_bytes);
+    const HeadLabelsWs lay = head_labels_layout(cv, N, dp, dq, V, dt);
+    if (!ws || !aligned(ws, 256) || !cv.fits()) return SPR_ERR_WORKSPACE;
+    int rc = device_supported();
+    if (rc != SPR_OK) return rc;
+
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    PairParams prm;
+    memset(&prm, 0, sizeof prm);
+    prm.status = at<int>(ws, 0);
+    PairOperand a[2], b[2];
+    const int ip = dp >= dq ? 0 : 1, iq = 1 - ip;       // the longer products first
+    cudaError_t e = stats_job(prm.job[ip], a[ip], b[ip], p_hidden, p_W, N, dp, V, dt, ws, lay.p, st);
+    if (e == cudaSuccess) e = stats_job(prm.job[iq], a[iq], b[iq], q_hidden, q_W, N, dq, V, dt, ws, lay.q, st);
+    if (e == cudaSuccess) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, 2, a, b, st);
+    if (e == cudaSuccess) {
+        const HeadRow p = {p_hidden, p_W, prm.job[ip].part, dp, prm.job[ip].tiles_n};
+        const HeadRow q = {q_hidden, q_W, prm.job[iq].part, dq, prm.job[iq].tiles_n};
+        HeadLabels out;
+        memset(&out, 0, sizeof out);
+        out.n_lambda = n_lambda;
+        for (int l = 0; l < n_lambda; ++l) out.lambdas[l] = lambdas[l];
+        out.labels = labels;
+        out.ratio = ratio;
+        const unsigned ctas = (unsigned)ceil_div(N, kRowWarps);
+        if (dt == SPR_F32) head_labels_kernel<float><<<ctas, 32 * kRowWarps, 0, st>>>(p, q, N, V, draft_tokens, out, prm.status);
+        else head_labels_kernel<__nv_bfloat16><<<ctas, 32 * kRowWarps, 0, st>>>(p, q, N, V, draft_tokens, out, prm.status);
+        e = cudaGetLastError();
+    }
+    return finish(e);
+}
+
+}  // extern "C"

@@ -145,6 +145,15 @@ struct VerifierTune {
     uint32_t spin_limit;   // 0: default
 };
 
+// Hidden states kept in 8 bits: bytes of a row of d elements (d bytes, an exponent byte per 32
+// elements, padding to 16 bytes).
+__host__ __device__ constexpr int pack8_pitch(int d) { return (d + (d + 31) / 32 + 15) / 16 * 16; }
+
+// workspace of head_loss, head_loss_grad and verifier_labels_head (head_loss.cu); 0 for bad sizes
+size_t head_loss_ws_bytes(int64_t N, int d, int V, int dt);
+size_t head_grad_ws_bytes(int64_t N, int d, int V, int dt);
+size_t head_labels_ws_bytes(int64_t N, int dp, int dq, int V, int dt);
+
 struct SimParams {
     uint64_t seed;
     int64_t first_run, runs;

@@ -222,7 +222,7 @@ def _workspace(s):
         code = spr.F32 if c["dt"] == "f32" else spr.BF16
         op = {"loss": spr.OP_HEAD_LOSS, "grad": spr.OP_HEAD_LOSS_GRAD, "labels": spr.OP_VERIFIER_LABELS_HEAD,
               "step": spr.OP_VERIFIER_TRAIN8}[c["op"]]
-        n = spr.workspace_bytes(op, c["N"], 1, c.get("V", 1), c.get("d", c.get("dp")), 0, code)
+        n = spr.workspace_bytes(op, c["N"], 1, c.get("V", 1), c.get("d", c.get("dp")), c.get("dq", 0), code)
         s["ws"] = spr.Workspace(n)
     return s["ws"]
 

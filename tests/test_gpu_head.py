@@ -1,0 +1,338 @@
+"""head_loss, head_loss_grad and verifier_labels_head against plain float64.
+
+Bounds, with u = 2^-23 (an accumulator that rounds or truncates loses at most u of its running
+magnitude per addition) and A = |hidden| |W|^T:
+  logit   a product of d terms is added up in groups of 16: off by at most (d/16 + 16) u A (fp32
+          operands: the three bf16 parts leave 2^-24 of each factor, inside the 16)
+  lse     as the worst logit of the row, plus a few u of |lse| and of the exponentials
+  D       exp(l - lse) is off by the two above; D is then rounded to bf16: 2^-8 |D| (bf16 operands)
+  dH, dW  the sum over |D| |W| or |D| |hidden| of these, (terms/16 + 16) u of the sum for the additions,
+          and the rounding of the result, 2^-8 in bf16
+"""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -23
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+IDS = {torch.bfloat16: "bf16", torch.float32: "f32"}
+
+
+@pytest.fixture(scope="module")
+def spr():
+    import paper_2502_04557_b200 as s
+    s.lib()
+    return s
+
+
+def problem(N, d, V, dtype, seed, ignore=0.2, scale=3.0):
+    g = torch.Generator().manual_seed(seed)
+    h = torch.randn((N, d), generator=g).to(dtype).cuda()
+    w = (torch.randn((V, d), generator=g) * (scale / d ** 0.5)).to(dtype).cuda()
+    t = torch.randint(0, V, (N,), generator=g, dtype=torch.int32)
+    if ignore:
+        t[torch.rand(N, generator=g) < ignore] = -1
+    gl = (torch.rand(N, generator=g) + 0.1) / max(N, 1)
+    return h, w, t.cuda(), gl.cuda()
+
+
+def code(spr, dtype):
+    return spr.F32 if dtype == torch.float32 else spr.BF16
+
+
+def workspace(spr, op, N, V, d, dtype, h=0):
+    n = spr.workspace_bytes(op, N, 1, V, d, h, code(spr, dtype))
+    assert n > 0
+    return spr.Workspace(n)
+
+
+def logit_bound(h, w):
+    d = h.shape[1]
+    return (d / 16 + 16) * U * (h.double().abs() @ w.double().abs().T)
+
+
+def reference_loss(h, w, t):
+    l = h.double() @ w.double().T
+    lse = torch.logsumexp(l, 1)
+    pick = l.gather(1, t.long().clamp(min=0)[:, None])[:, 0]
+    return l, lse, torch.where(t >= 0, lse - pick, torch.zeros_like(lse))
+
+
+def check_loss(spr, h, w, t, ws=None):
+    N, d = h.shape
+    ws = ws or workspace(spr, spr.OP_HEAD_LOSS, N, w.shape[0], d, h.dtype)
+    loss, lse = spr.head_loss(h, w, t, ws)
+    assert ws.device_status() == 0
+    _, want_lse, want = reference_loss(h, w, t)
+    tol = logit_bound(h, w).amax(1) + 16 * U * (1 + want_lse.abs())
+    assert bool(((lse.double() - want_lse).abs() <= tol).all()), float(((lse.double() - want_lse).abs() / tol).max())
+    assert bool(((loss.double() - want).abs() <= 2 * tol).all())
+    assert bool((loss[t < 0] == 0).all()) and bool((loss >= 0).all())
+    return loss, lse
+
+
+def check_grad(spr, h, w, t, gl, lse, ws=None, **kw):
+    N, d = h.shape
+    V = w.shape[0]
+    ws = ws or workspace(spr, spr.OP_HEAD_LOSS_GRAD, N, V, d, h.dtype)
+    dh, dw = spr.head_loss_grad(h, w, t, lse, gl, ws, **kw)
+    assert ws.device_status() == 0
+    keep = (t >= 0)[:, None]
+    H, W = torch.where(keep, h.double(), 0.0), w.double()
+    p = torch.exp(H @ W.T - lse.double()[:, None])
+    hot = torch.zeros_like(p).scatter_(1, t.long().clamp(min=0)[:, None], 1.0)
+    g = gl.double()[:, None]
+    D = torch.where(keep, g * (p - hot), 0.0)
+    # what D may be off by: the logit's error, exp and its argument, and the rounding to bf16
+    dD = torch.where(keep, g.abs() * p * (logit_bound(H, W) + (8 + lse.double().abs()[:, None] * 2) * U), 0.0) + 4 * U * D.abs()
+    # a probability below the smallest normal number, 2^-126, counts as zero (and products of g with one as
+    # small): off by less than (1 + g) 2^-126, which is all there is where the true value is of that size
+    dD += torch.where(keep, (1 + g.abs()) * 2.0 ** -126, 0.0)
+    dD += (2.0 ** -8 if h.dtype == torch.bfloat16 else 2.0 ** -23) * D.abs()
+    for got, X, off, k in ((dh, W, dD, V), (dw, H, dD.T, N)):
+        if got is None:
+            continue
+        Dm = D if got is dh else D.T
+        want = Dm @ X
+        tol = off @ X.abs() + (k / 16 + 16 + 40) * U * (Dm.abs() @ X.abs()) + 1.01 * HALF[h.dtype] * want.abs() + 1e-40
+        bad = (got.double() - want).abs() / tol
+        assert bool((bad <= 1).all()), float(bad.max())
+    return dh, dw
+
+
+SHAPES = [
+    (1, 1, 1), (1, 8, 3), (3, 64, 256), (4, 256, 1000), (129, 72, 257), (257, 200, 511), (300, 768, 1025),
+    (64, 2048, 700), (5, 7, 5000), (1000, 33, 300), (2, 4104, 130), (520, 136, 9001),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=IDS.get)
+@pytest.mark.parametrize("N,d,V", SHAPES)
+def test_loss_and_gradient(spr, N, d, V, dtype):
+    h, w, t, gl = problem(N, d, V, dtype, seed=N * 7 + d * 3 + V)
+    _, lse = check_loss(spr, h, w, t)
+    check_grad(spr, h, w, t, gl, lse)
+
+
+@pytest.mark.parametrize("N,d,V,dtype", [(2048, 512, 30011, torch.bfloat16), (4096, 256, 128256, torch.bfloat16),
+                                         (700, 264, 50257, torch.bfloat16), (1500, 136, 33000, torch.float32)],
+                         ids=lambda v: str(v).replace("torch.", ""))
+def test_vocabulary_pieces_and_split_contractions(spr, N, d, V, dtype):
+    """Sizes at which the vocabulary goes by in several pieces, or dH's contraction is cut."""
+    h, w, t, gl = problem(N, d, V, dtype, seed=5)
+    _, lse = check_loss(spr, h, w, t)
+    check_grad(spr, h, w, t, gl, lse)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=IDS.get)
+def test_one_gradient_alone_equals_both(spr, dtype):
+    h, w, t, gl = problem(130, 96, 700, dtype, seed=3)
+    _, lse = check_loss(spr, h, w, t)
+    dh, dw = check_grad(spr, h, w, t, gl, lse)
+    a, none = check_grad(spr, h, w, t, gl, lse, want_W=False)
+    assert none is None and torch.equal(a, dh)
+    none, b = check_grad(spr, h, w, t, gl, lse, want_hidden=False)
+    assert none is None and torch.equal(b, dw)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=IDS.get)
+@pytest.mark.parametrize("d", [64, 67])
+def test_padding_rows_hold_anything(spr, d, dtype):
+    """Rows without a target hold NaN and infinities: no other row and no sum sees them."""
+    N, V = 300, 515
+    h, w, t, gl = problem(N, d, V, dtype, seed=8, ignore=0.0)
+    pad = torch.arange(N, device="cuda") % 3 == 1
+    t[pad] = -100
+    _, clean_lse = check_loss(spr, h, w, t)
+    clean = check_grad(spr, h, w, t, gl, clean_lse)
+    dirty = h.clone()
+    dirty[pad] = float("nan")
+    dirty[4] = float("inf")
+    gl2, lse2 = gl.clone(), clean_lse.clone()
+    gl2[pad], lse2[pad] = float("nan"), float("-inf")
+    ws = workspace(spr, spr.OP_HEAD_LOSS, N, V, d, dtype)
+    loss, lse = spr.head_loss(dirty, w, t, ws)
+    assert bool((loss[pad] == 0).all())
+    assert torch.equal(lse[~pad], clean_lse[~pad])
+    wg = workspace(spr, spr.OP_HEAD_LOSS_GRAD, N, V, d, dtype)
+    got = spr.head_loss_grad(dirty, w, t, lse2, gl2, wg)
+    assert wg.device_status() == 0
+    assert torch.equal(got[0], clean[0]) and torch.equal(got[1], clean[1])
+    assert bool((got[0][pad] == 0).all())
+    # a live row that is not finite is its own affair in the loss
+    bad = h.clone()
+    bad[5] = float("nan")
+    loss, lse = spr.head_loss(bad, w, t, ws)
+    assert bool(lse[5].isnan()) and bool(loss[5].isnan())
+    other = torch.arange(N, device="cuda") != 5
+    assert torch.equal(lse[other & ~pad], clean_lse[other & ~pad])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=IDS.get)
+def test_all_padding_and_empty_batches(spr, dtype):
+    N, d, V = 70, 72, 400
+    h, w, t, gl = problem(N, d, V, dtype, seed=8, ignore=0.0)
+    t.fill_(-1)
+    _, lse = check_loss(spr, h, w, t)
+    dh, dw = check_grad(spr, h, w, t, gl, lse)
+    assert not dh.any() and not dw.any()
+    ws = workspace(spr, spr.OP_HEAD_LOSS_GRAD, 1, V, d, dtype)
+    empty = torch.empty((0, d), dtype=dtype, device="cuda")
+    none_t, none_f = torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty(0, device="cuda")
+    loss, lse = spr.head_loss(empty, w, none_t, ws)
+    assert loss.shape == (0,) and lse.shape == (0,)
+    dw = torch.full((V, d), 7.0, dtype=dtype, device="cuda")
+    dh, dw = spr.head_loss_grad(empty, w, none_t, none_f, none_f, ws, out=(None, dw))
+    assert dh.shape == (0, d) and not dw.any()
+
+
+def test_bad_targets_are_reported_and_have_no_gradient(spr):
+    N, d, V = 40, 64, 300
+    h, w, t, gl = problem(N, d, V, torch.bfloat16, seed=9, ignore=0.0)
+    _, lse = check_loss(spr, h, w, t)
+    pad = t.clone()
+    pad[7] = -1
+    want = check_grad(spr, h, w, pad, gl, lse)
+    t[7] = V
+    ws = workspace(spr, spr.OP_HEAD_LOSS, N, V, d, h.dtype)
+    loss, lse2 = spr.head_loss(h, w, t, ws)
+    assert ws.device_status() == 6 and ws.device_status() == 0
+    assert float(loss[7]) == -1.0 and torch.equal(lse, lse2)
+    wg = workspace(spr, spr.OP_HEAD_LOSS_GRAD, N, V, d, h.dtype)
+    got = spr.head_loss_grad(h, w, t, lse, gl, wg)
+    assert wg.device_status() == 6
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_extreme_logits(spr):
+    """One column far above the rest (loss 0 or huge), and logits that spread over hundreds."""
+    N, d, V = 6, 64, 1000
+    h = torch.zeros((N, d), dtype=torch.bfloat16, device="cuda")
+    w = torch.zeros((V, d), dtype=torch.bfloat16, device="cuda")
+    h[:, 0] = torch.tensor([1.0, 1.0, 30.0, -30.0, 0.0, 200.0])
+    w[:, 0] = torch.linspace(-8, 8, V).to(torch.bfloat16)
+    w[3, 0] = 100.0
+    t = torch.tensor([3, 4, 3, 3, 0, 10], dtype=torch.int32, device="cuda")
+    gl = torch.full((N,), 0.5, device="cuda")
+    loss, lse = check_loss(spr, h, w, t)
+    assert float(loss[0]) == 0.0 and float(loss[2]) == 0.0
+    assert float(loss[5]) == pytest.approx(200.0 * (100.0 - float(w[10, 0])), rel=1e-6)
+    check_grad(spr, h, w, t, gl, lse)
+
+
+def test_gradient_against_differences(spr):
+    """A step along a random direction changes sum(g loss) as the gradient says: fp32, the loss in
+    float64 (the operator's own loss has too few digits for a difference)."""
+    N, d, V = 33, 50, 211
+    h, w, t, gl = problem(N, d, V, torch.float32, seed=4)
+    ws = workspace(spr, spr.OP_HEAD_LOSS, N, V, d, torch.float32)
+    _, lse = spr.head_loss(h, w, t, ws)
+    wg = workspace(spr, spr.OP_HEAD_LOSS_GRAD, N, V, d, torch.float32)
+    dh, dw = spr.head_loss_grad(h, w, t, lse, gl, wg)
+    g = torch.Generator().manual_seed(1)
+    eh, ew = torch.randn((N, d), generator=g).double().cuda(), torch.randn((V, d), generator=g).double().cuda()
+
+    def total(s):
+        l = (h.double() + s * eh) @ (w.double() + s * ew).T
+        loss = torch.logsumexp(l, 1) - l.gather(1, t.long().clamp(min=0)[:, None])[:, 0]
+        return float((gl.double() * torch.where(t >= 0, loss, 0.0)).sum())
+    s = 1e-4
+    slope = (total(s) - total(-s)) / (2 * s)
+    assert slope == pytest.approx(float((dh.double() * eh).sum() + (dw.double() * ew).sum()), rel=1e-5)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=IDS.get)
+def test_runs_are_identical_and_one_workspace_serves_every_call(spr, dtype):
+    N, d, V = 333, 136, 3001
+    h, w, t, gl = problem(N, d, V, dtype, seed=12)
+    n = max(spr.workspace_bytes(op, N, 1, V, d, 0, code(spr, dtype)) for op in (spr.OP_HEAD_LOSS, spr.OP_HEAD_LOSS_GRAD))
+    ws = spr.Workspace(n)
+    first = spr.head_loss(h, w, t, ws)
+    grads = spr.head_loss_grad(h, w, t, first[1], gl, ws)
+    for _ in range(3):
+        ws.buf[256:].random_(0, 255)          # what an earlier call left behind does not matter
+        again = spr.head_loss(h, w, t, ws)
+        ws.buf[256:].random_(0, 255)
+        g2 = spr.head_loss_grad(h, w, t, again[1], gl, ws)
+        assert all(torch.equal(a, b) for a, b in zip(first + grads, again + g2))
+    assert ws.device_status() == 0
+
+
+def test_captured_and_replayed_with_new_inputs_and_on_another_stream(spr):
+    N, d, V = 200, 128, 2100
+    h, w, t, gl = problem(N, d, V, torch.bfloat16, seed=13)
+    h2, w2, t2, gl2 = problem(N, d, V, torch.bfloat16, seed=14)
+    ws = workspace(spr, spr.OP_HEAD_LOSS_GRAD, N, V, d, torch.bfloat16)
+    out = (torch.empty(N, device="cuda"), torch.empty(N, device="cuda"))
+    gout = (torch.empty_like(h), torch.empty_like(w))
+    want = []
+    for a in ((h, w, t, gl), (h2, w2, t2, gl2)):
+        loss, lse = spr.head_loss(*a[:3], ws)
+        want.append((loss, lse) + spr.head_loss_grad(*a[:3], lse, a[3], ws))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        spr.head_loss(h, w, t, ws, out=out)
+        spr.head_loss_grad(h, w, t, out[1], gl, ws, out=gout)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out + gout, want[0]))
+    for a, b in zip((h, w, t, gl), (h2, w2, t2, gl2)):
+        a.copy_(b)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out + gout, want[1]))
+    with torch.cuda.stream(side):
+        loss, lse = spr.head_loss(h, w, t, ws)
+    side.synchronize()
+    assert torch.equal(loss, want[1][0])
+
+
+# ---------------------------------------------------------------------------- labels
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=IDS.get)
+@pytest.mark.parametrize("N,dp,dq,V", [(1, 8, 8, 2), (5, 16, 8, 1000), (40, 72, 64, 513), (300, 256, 136, 5003),
+                                       (64, 33, 64, 257), (17, 128, 257, 700), (260, 2048, 1024, 4000)])
+def test_labels_from_hidden_states(spr, N, dp, dq, V, dtype):
+    g = torch.Generator().manual_seed(N + dp + dq + V)
+    ph, pw, x, _ = problem(N, dp, V, dtype, seed=N + V, ignore=0.0)
+    qh, qw, _, _ = problem(N, dq, V, dtype, seed=N + V + 1)
+    x[torch.rand(N, generator=g).cuda() < 0.1] = V + 2
+    lambdas = [1.0, 1.2, 1.5, 0.25, 1e30]
+    ws = workspace(spr, spr.OP_VERIFIER_LABELS_HEAD, N, V, dp, dtype, h=dq)
+    labels, ratio = spr.verifier_labels_head(ph, pw, qh, qw, x, lambdas, ws)
+    ok = x < V
+    assert ws.device_status() == (0 if bool(ok.all()) else 6)
+    at = x.long().clamp(max=V - 1)[:, None]
+    lp, lq = ph.double() @ pw.double().T, qh.double() @ qw.double().T
+    off = logit_bound(ph, pw).amax(1) + logit_bound(qh, qw).amax(1)
+    off += 16 * U * (2 + torch.logsumexp(lp, 1).abs() + torch.logsumexp(lq, 1).abs())
+    want = torch.exp(torch.log_softmax(lq, 1).gather(1, at)[:, 0] - torch.log_softmax(lp, 1).gather(1, at)[:, 0])
+    err = (ratio.double() / want - 1).abs()
+    assert bool((err[ok] <= 2 * off[ok]).all()), float((err / off)[ok].max())
+    assert bool((ratio[~ok] == -1).all()) and not labels[:, ~ok].any()
+    for i, lam in enumerate(lambdas):
+        lam = float(np.float32(lam))
+        clear = ok & ((want / lam - 1).abs() > 2 * off)
+        assert torch.equal(labels[i][clear].bool(), (want <= lam)[clear])
+        assert int((ok & ~clear).sum()) <= max(1, N // 20)
+
+
+def test_labels_agree_with_those_from_kept_logits(spr):
+    """The same batch through verifier_labels on fp32 logits and through the heads."""
+    B, K, d, V = 6, 5, 128, 4001
+    N = B * K
+    ph, pw, x, _ = problem(N, d, V, torch.float32, seed=1, ignore=0.0)
+    qh, qw, _, _ = problem(N, d, V, torch.float32, seed=2)
+    lp, lq = (ph.double() @ pw.double().T).float(), (qh.double() @ qw.double().T).float()
+    w0 = spr.Workspace(spr.workspace_bytes(spr.binding.OP_VERIFIER_LABELS, B, K, V, 0, 0, spr.F32))
+    a, ra = spr.binding.verifier_labels(lp.view(B, K, V), lq.view(B, K, V), V, x.view(B, K), [1.0, 1.2, 1.5], w0)
+    ws = workspace(spr, spr.OP_VERIFIER_LABELS_HEAD, N, V, d, torch.float32, h=d)
+    b, rb = spr.verifier_labels_head(ph, pw, qh, qw, x, [1.0, 1.2, 1.5], ws)
+    assert bool(((ra.view(-1) / rb - 1).abs() < 2e-4).all())
+    clear = torch.stack([(rb / lam - 1).abs() > 2e-4 for lam in (1.0, 1.2, 1.5)])
+    assert torch.equal(a.view(3, N)[clear], b[clear])

@@ -1,0 +1,227 @@
+"""hidden_pack8 / hidden_unpack8 and verifier_train_step8.
+
+Packing is compared bit for bit with a numpy statement of the format (nothing in it is inexact but
+the one rounding it defines); training with the float64 oracle on the values the packed rows stand for.
+"""
+import numpy as np
+import pytest
+import torch
+
+from helpers import to_np
+from oracle import training
+from test_gpu_fit import teacher_problem
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def spr():
+    import paper_2502_04557_b200 as s
+    s.lib()
+    return s
+
+
+def pack_ref(x):
+    """float64 [N,d] -> packed bytes [N, pitch]"""
+    N, d = x.shape
+    nb = (d + 31) // 32
+    out = np.zeros((N, (d + nb + 15) // 16 * 16), np.int8)
+    for b in range(nb):
+        blk = x[:, 32 * b:32 * b + 32]
+        finite = np.isfinite(blk).all(1)
+        blk = np.where(finite[:, None], blk, 0.0)
+        top = np.abs(blk).max(1)
+        e = np.maximum(np.frexp(top)[1] - 7, -126)
+        e[top == 0] = -126
+        q = np.clip(np.rint(np.ldexp(blk, -e[:, None])), -127, 127)
+        out[:, 32 * b:32 * b + blk.shape[1]] = np.where(finite[:, None], q, 0)
+        out[:, d + b] = np.where(finite, e, -128)
+    return out.view(np.uint8)
+
+
+def unpack_ref(p, d):
+    p = p.view(np.int8)
+    nb = (d + 31) // 32
+    e = p[:, d:d + nb].astype(np.int32).repeat(32, 1)[:, :d]
+    return np.where(e == -128, np.nan, np.ldexp(p[:, :d].astype(np.float64), e))
+
+
+def values(N, d, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((N, d), generator=g) * torch.exp(3 * torch.randn((N, 1), generator=g))
+    x[torch.rand((N, d), generator=g) < 0.05] = 0.0
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("N,d", [(1, 1), (3, 31), (2, 32), (5, 33), (7, 255), (4, 256), (3, 257), (2, 1000), (9, 768),
+                                 (300, 2048), (2, 4099), (3000, 40)])
+def test_pack_and_unpack(spr, N, d, dtype):
+    x = values(N, d, dtype, seed=N + d)
+    packed = spr.hidden_pack8(x.cuda())
+    assert packed.shape == (N, spr.pack8_pitch(d)) == (N, (d + (d + 31) // 32 + 15) // 16 * 16)
+    want = pack_ref(x.double().numpy())
+    assert np.array_equal(packed.cpu().numpy(), want)
+    for ty in (torch.float32, torch.bfloat16):
+        back = spr.hidden_unpack8(packed, d, ty)
+        assert np.array_equal(back.cpu().double().numpy(), unpack_ref(want, d))
+    # at most half a step off, a whole one where the byte is clamped
+    off = np.abs(unpack_ref(want, d) - x.double().numpy())
+    e = want.view(np.int8)[:, d:d + (d + 31) // 32].astype(np.int32).repeat(32, 1)[:, :d]
+    clamped = np.abs(np.ldexp(x.double().numpy(), -e)) > 127.5
+    assert np.all(off <= np.ldexp(np.where(clamped, 1.0, 0.5), e))
+
+
+def test_pack_extremes(spr):
+    big, tiny = 3.3895313892515355e38, 2.0 ** -133
+    x = torch.zeros((8, 64), dtype=torch.bfloat16)
+    x[0, 0], x[0, 1] = big, -big
+    x[1, 5] = tiny
+    x[2, :] = 2.0 ** -126
+    x[3, 3] = float("inf")
+    x[4, 40] = float("nan")
+    x[5, :] = torch.arange(64) - 31.5
+    x[6, 0] = -0.0
+    x[7, :3] = torch.tensor([127.0, 127.5, 0.5])
+    packed = spr.hidden_pack8(x.cuda())
+    assert np.array_equal(packed.cpu().numpy(), pack_ref(x.double().numpy()))
+    back = spr.hidden_unpack8(packed, 64).cpu()
+    assert back[3, :32].isnan().all() and not back[3, 32:].isnan().any()
+    assert back[4, 32:].isnan().all() and not back[4, :32].isnan().any()
+    assert float(back[7, 1]) == 127.0 or float(back[7, 1]) == 128.0
+
+
+def test_pack_of_an_unaligned_view_and_of_nothing(spr):
+    x = values(6, 512, torch.bfloat16, 3).cuda().flatten()
+    view = x[1:1 + 5 * 512].view(5, 512)                      # contiguous, two bytes past a 16-byte boundary
+    assert np.array_equal(spr.hidden_pack8(view).cpu().numpy(), pack_ref(view.cpu().double().numpy()))
+    buf = torch.empty(5 * 512 + 1, dtype=torch.bfloat16, device="cuda")[1:].view(5, 512)
+    packed = spr.hidden_pack8(view)
+    assert torch.equal(spr.hidden_unpack8(packed, 512, out=buf), spr.hidden_unpack8(packed, 512))
+    none = spr.hidden_pack8(torch.empty((0, 40), device="cuda"))
+    assert none.shape == (0, 48) and spr.hidden_unpack8(none, 40).shape == (0, 40)
+
+
+def step_ws(spr, d):
+    return spr.Workspace(spr.workspace_bytes(spr.OP_VERIFIER_TRAIN8, 0, 0, 0, d, 0, spr.BF16))
+
+
+@pytest.mark.parametrize("N,d", [(1, 16), (7, 64), (5000, 768), (20000, 256), (3000, 2048), (2000, 4096), (4001, 1008),
+                                 (60000, 512), (30001, 1024), (24000, 2048), (9000, 2560), (12000, 4096), (70001, 128),
+                                 (50003, 528), (8000, 1536), (33, 1040)])
+def test_training_steps_match_the_oracle(spr, N, d):
+    """As for verifier_train_step: fp32 sums against float64, loss to 2e-5, and a relative gradient error e
+    moves a parameter by about lr e per step: bound 1e-3 lr t.  The loss of a step is that of the parameters
+    before it, which already differ by some delta (at most that bound): ln(1 + e^z) - y z changes by no more
+    than z does, so the mean loss by at most mean_i sum_j |s_ij| |delta_j|, and by the rounding of the fp32
+    dot product, 2^-24 (d/32 + 16) sum_j |s_ij theta_j| (a lane adds d/32 terms).  Once a small set is
+    separated the loss is tiny, and these terms, not 2e-5 of it, are what it can be held to."""
+    S, y = teacher_problem(N, d, torch.bfloat16, seed=N + d)
+    packed = spr.hidden_pack8(S.cuda())
+    Sn = unpack_ref(packed.cpu().numpy(), d)
+    lr, steps = 0.02, 8
+    ws = step_ws(spr, d)
+    theta, m, v = (torch.zeros(d + 1, device="cuda") for _ in range(3))
+    rt, rm, rv = np.zeros(d + 1), np.zeros(d + 1), np.zeros(d + 1)
+    for t in range(1, steps + 1):
+        before = theta.cpu().double().numpy()
+        slack = np.mean(np.abs(Sn) @ np.abs(before - rt)[:d]) + abs(before[d] - rt[d])
+        slack += 2.0 ** -24 * (d / 32 + 16) * (np.mean(np.abs(Sn) @ np.abs(rt[:d])) + abs(rt[d]))
+        loss = spr.verifier_train_step8(packed, d, y.cuda(), theta, m, v, t, lr, ws)
+        want, rt, rm, rv = training.verifier_train_step(Sn, y.numpy(), rt, rm, rv, t, lr)
+        assert abs(float(loss) - want) < 2e-5 * want + slack
+        assert np.abs(theta.cpu().double().numpy() - rt).max() <= 1e-3 * lr * t
+    assert ws.device_status() == 0
+
+
+@pytest.mark.parametrize("N,d", [(5000, 768), (9001, 2048), (3000, 4096), (700, 128)])
+def test_a_step_equals_the_step_on_unpacked_states(spr, N, d):
+    """The packed values are bf16 numbers, so verifier_train_step on the unpacked states is the same
+    problem: the two differ by the order of their sums alone.  Loss: a mean of N terms, fp32 logits."""
+    S, y = teacher_problem(N, d, torch.bfloat16, seed=N)
+    packed = spr.hidden_pack8(S.cuda())
+    U = spr.hidden_unpack8(packed, d)
+    g = torch.Generator().manual_seed(1)
+    theta = (0.05 * torch.randn(d + 1, generator=g)).cuda()
+    state = [(theta.clone(), torch.zeros_like(theta), torch.zeros_like(theta)) for _ in range(2)]
+    ws = step_ws(spr, d)
+    w2 = spr.Workspace(spr.workspace_bytes(spr.binding.OP_VERIFIER_TRAIN, 0, 0, 0, d, 0, spr.BF16))
+    a = spr.verifier_train_step8(packed, d, y.cuda(), *state[0], 1, 0.01, ws)
+    b = spr.binding.verifier_train_step(U, y.cuda(), *state[1], 1, 0.01, w2)
+    assert float(a) == pytest.approx(float(b), rel=2e-6)
+    # m = 0.1 g: compared to the size of the gradient's terms, mean |s_ij|, over N / teams of them in fp32
+    scale = U.float().abs().mean(0).amax()
+    assert float((state[0][1] - state[1][1]).abs().max()) <= 0.1 * 1e-5 * max(1.0, float(scale))
+
+
+def test_a_step_is_reproducible_and_a_marked_block_shows(spr):
+    S, y = teacher_problem(6000, 768, torch.bfloat16, seed=9)
+    packed = spr.hidden_pack8(S.cuda())
+    ws, yg = step_ws(spr, 768), y.cuda()
+    runs = []
+    for _ in range(2):
+        st = [torch.zeros(769, device="cuda") for _ in range(3)]
+        loss = [spr.verifier_train_step8(packed, 768, yg, *st, t, 0.02, ws).clone() for t in (1, 2, 3)]
+        runs.append(loss + st)
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
+    S[17, 100] = float("nan")
+    st = [torch.zeros(769, device="cuda") for _ in range(3)]
+    assert bool(spr.verifier_train_step8(spr.hidden_pack8(S.cuda()), 768, yg, *st, 1, 0.02, ws).isnan().all())
+
+
+def test_a_captured_step(spr):
+    S, y = teacher_problem(3000, 512, torch.bfloat16, seed=19)
+    packed, yg, ws = spr.hidden_pack8(S.cuda()), y.cuda(), step_ws(spr, 512)
+    a, b = ([torch.zeros(513, device="cuda") for _ in range(3)] for _ in range(2))
+    loss = torch.empty(1, device="cuda")
+    spr.verifier_train_step8(packed, 512, yg, *a, 1, 0.02, ws, loss=loss)
+    want = [x.clone() for x in a] + [loss.clone()]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        spr.verifier_train_step8(packed, 512, yg, *b, 1, 0.02, ws, loss=loss)
+    for x in b:
+        x.zero_()
+    loss.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(b + [loss], want))
+
+
+def test_widths_that_are_refused(spr):
+    for d in (8, 40, 4112, 8192):
+        packed = torch.zeros((4, spr.pack8_pitch(d)), dtype=torch.uint8, device="cuda")
+        z = torch.zeros(d + 1, device="cuda")
+        with pytest.raises(spr.SprinterError) as e:
+            spr.verifier_train_step8(packed, d, torch.zeros(4, dtype=torch.uint8, device="cuda"), z, z.clone(), z.clone(), 1,
+                                     0.01, step_ws(spr, d))
+        assert e.value.status == 2
+
+
+def test_states_labelled_packed_fitted_and_used(spr):
+    """A run as it would be used: draft and target heads label the draft's tokens, the draft's states are
+    packed, the verifier is fitted on them, and sprinter_verify scores with the fitted weights."""
+    g = torch.Generator().manual_seed(3)
+    N, d, V = 4096, 256, 2000
+    qh = torch.randn((N, d), generator=g).to(torch.bfloat16).cuda()
+    qw = (torch.randn((V, d), generator=g) * (3.0 / d ** 0.5)).to(torch.bfloat16).cuda()
+    pw = (qw.float().cpu() + torch.randn((V, d), generator=g) * (1.0 / d ** 0.5)).to(torch.bfloat16).cuda()
+    x = torch.randint(0, V, (N,), generator=g, dtype=torch.int32).cuda()
+    wl = spr.Workspace(spr.workspace_bytes(spr.OP_VERIFIER_LABELS_HEAD, N, 1, V, d, d, spr.BF16))
+    labels, ratio = spr.verifier_labels_head(qh, pw, qh, qw, x, [1.0], wl)
+    assert wl.device_status() == 0
+    packed = spr.hidden_pack8(qh)
+    ws = step_ws(spr, d)
+    theta, m, v = (torch.zeros(d + 1, device="cuda") for _ in range(3))
+    losses = [float(spr.verifier_train_step8(packed, d, labels[0].contiguous(), theta, m, v, t, 0.05, ws)) for t in range(1, 5)]
+    assert losses[0] == pytest.approx(np.log(2.0), rel=1e-6) and all(np.isfinite(losses))
+    assert ws.device_status() == 0
+    wv = spr.Workspace(spr.workspace_bytes(spr.binding.OP_SPRINTER_VERIFY, N // 8, 8, 1, d, 0, spr.BF16))
+    scores, accept, first = spr.sprinter_verify(spr.hidden_unpack8(packed, d).view(N // 8, 8, d), theta[:d].to(torch.bfloat16),
+                                                None, None, theta[d:].clone(), 0.5, wv)
+    S = unpack_ref(packed.cpu().numpy(), d)
+    z = S @ to_float(theta[:d].to(torch.bfloat16)) + float(theta[d])
+    assert np.allclose(scores.cpu().numpy().reshape(-1), 1 / (1 + np.exp(-z)), rtol=1e-3)
+
+
+def to_float(t):
+    return t.cpu().double().numpy()
