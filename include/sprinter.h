@@ -384,13 +384,14 @@ int hidden_unpack8(const void *packed, int64_t N, int d, int dt, void *hidden, v
  * verifier_train_step8 - verifier_train_step on hidden states kept in 8 bits.
  *
  * Same step, arguments and errors as verifier_train_step with s_i = the values that the packed
- * rows stand for (hidden_pack8), read once: 1.03 d bytes per sample.  packed: 16-byte aligned; d a
+ * rows stand for (hidden_pack8), read once: 1.03 d bytes per sample.  The hyper-parameters are
+ * doubles: 1 - beta2 would lose 1e-5 of itself if 0.999 were rounded to float.  packed: 16-byte aligned; d a
  * multiple of 16 and at most 4096 (otherwise SPR_ERR_UNSUPPORTED).
  * Workspace: spr_workspace_bytes(SPR_OP_VERIFIER_TRAIN8, 0, 0, 0, d, 0, SPR_F32 or SPR_BF16).
  */
 int verifier_train_step8(const void *packed, const uint8_t *labels, int64_t N, int d, float *theta, float *adam_m,
-                         float *adam_v, int t, float lr, float beta1, float beta2, float eps, float *loss, void *ws,
-                         size_t ws_bytes, void *cuda_stream);
+                         float *adam_v, int t, double lr, double beta1, double beta2, double eps, float *loss,
+                         void *ws, size_t ws_bytes, void *cuda_stream);
 
 /*
  * sprinter_simulate - run lengths of an i.i.d. verifier (Monte-Carlo of Theorems 2 and 3).

@@ -109,7 +109,7 @@ def lib():
             fn.restype = i32
             fn.argtypes = [vp, i64, i32, i32, vp, vp]
         L.verifier_train_step8.restype = i32
-        L.verifier_train_step8.argtypes = [vp, vp, i64, i32, vp, vp, vp, i32, f32, f32, f32, f32, vp, vp, sz, vp]
+        L.verifier_train_step8.argtypes = [vp, vp, i64, i32, vp, vp, vp, i32] + [C.c_double] * 4 + [vp, vp, sz, vp]
         L.spr_host_arena_bytes.restype = sz
         L.spr_host_arena_bytes.argtypes = [i32, i32, i32, i32, i64, i32, i32, i32]
         L.sprinter_verify_host.restype = i32

@@ -8,18 +8,26 @@
 // below that.  A pair of CTAs (cluster of 2) owns a 256 x 256 tile: each CTA stages 128 rows of A
 // and 128 of B per 64-deep stage (32 KB by TMA, 128-byte swizzle, no multicast), one thread of the
 // even CTA issues tcgen05.mma.cta_group::2 for both, and the accumulator (256 fp32 columns in each
-// CTA's TMEM) is double-buffered: while the four epilogue warps work on one tile the next is
-// multiplied.  The grid is persistent, one CTA per SM.  An operand tile is loaded as 64 x 64 boxes
+// CTA's TMEM) is double-buffered: while the eight epilogue warps work on one the other is filled.
+// The grid is persistent, one CTA per SM.  An operand tile is loaded as 64 x 64 boxes
 // whether its contiguous axis runs along the contraction or across it, so that D and D^T, W and
 // W^T are read from one copy of each; the matrix descriptors say which.
 //
+// The tensor pipe truncates when it adds to the accumulator: every 16 elements of the contraction
+// cost up to one unit in the last place, always towards zero (measured: a log-sum-exp of products
+// 2048 deep came out 2.3e-6 low, a ratio of two such probabilities 1.2e-5 off).  Where the result is
+// wanted to fp32 - row statistics, and everything with fp32 operands - an accumulator therefore
+// takes only `kc` blocks of 64, and the epilogue warps add such chunks up in registers, rounding
+// to nearest.  They have the time: a chunk is read in about a quarter of the time it takes to form.
+//
 // fp32 operands: x = x0 + x1 + x2 with bf16 parts (8 significant bits each: the remainder is
 // below 2^-24 |x|).  The six products of parts with i + j <= 2 make the result exact to about
-// 2^-23; they are accumulated smallest first, so that the roundings of the accumulator that
-// count are those of the last product alone.
+// 2^-23; in each chunk they are accumulated smallest first, so that the truncations that count
+// are those of the last product alone.
 //
-// Warp roles (192 threads): warp 0 = TMA producer, warp 1 = TMEM owner and MMA issuer, warps
-// 2..5 = epilogue (warp w reads TMEM lanes 32 (w % 4) .. + 31).  Every wait is bounded: when one
+// Warp roles (320 threads): warp 0 = TMA producer, warp 1 = TMEM owner and MMA issuer, warps
+// 2..9 = epilogue (warp w reads TMEM lanes 32 (w % 4) .. + 31, one row per thread, and half of the
+// tile's columns).  Every wait is bounded: when one
 // runs out the status word becomes SPR_ERR_TIMEOUT, all roles leave their loops, the even CTA
 // waits (again bounded) for the copies and products in flight, and both CTAs meet before they exit.
 #include <atomic>
@@ -35,7 +43,7 @@ namespace {
 
 using namespace pairtc;
 
-constexpr int kPairThreads = 192;
+constexpr int kPairThreads = 320;
 constexpr int kHalfBytes = 128 * kPairBlockK * 2;       // this CTA's half of an operand tile: two 64 x 64 boxes
 constexpr int kBoxBytes = 64 * 64 * 2;
 constexpr int kStageBytes = 2 * kHalfBytes;
@@ -94,40 +102,41 @@ __device__ __forceinline__ int part_b(int nprod, int p) { return nprod == 1 ? 0 
 struct Stats {
     float m, s;
 };
-// (max, sum of exp) over 64 more logits of the row; v of them exist
-__device__ __forceinline__ void add_stats(Stats &a, float (&x)[2][32], int v)
+// (max, sum of exp) of `v` of the row's 128 logits in this thread's registers
+__device__ __forceinline__ Stats row_stats(float (&x)[4][32], int v)
 {
-    if (v < 64) {
+    if (v < 128) {
 #pragma unroll
-        for (int j = 0; j < 64; ++j)
+        for (int j = 0; j < 128; ++j)
             if (j >= v) x[j >> 5][j & 31] = neg_inf();
     }
     float t[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) t[j] = fmaxf(x[0][j], x[1][j]);
+    for (int j = 0; j < 8; ++j) t[j] = x[0][j];
 #pragma unroll
-    for (int k = 8; k < 32; k += 8)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] = fmaxf(t[j], fmaxf(x[0][k + j], x[1][k + j]));
+    for (int j = 8; j < 128; ++j) t[j & 7] = fmaxf(t[j & 7], x[j >> 5][j & 31]);
 #pragma unroll
     for (int o = 4; o > 0; o >>= 1)
 #pragma unroll
         for (int j = 0; j < o; ++j) t[j] = fmaxf(t[j], t[j + o]);
-    const float m = fmaxf(a.m, t[0]);
-    const float ref = m == neg_inf() ? 0.f : m;
+    Stats a;
+    a.m = t[0];
+    const float ref = a.m == neg_inf() ? 0.f : a.m;
     // x - ref first: the largest term is then exactly 1 whatever the size of the logits
     const uint64_t neg2 = pack2(-ref, -ref), log2 = pack2(kLog2e, kLog2e);
-    uint64_t s[2] = {pack2(a.s * ex2((a.m - ref) * kLog2e), 0.f), pack2(0.f, 0.f)};
+    uint64_t s[4];
 #pragma unroll
-    for (int j = 0; j < 64; j += 2) {
+    for (int j = 0; j < 4; ++j) s[j] = pack2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < 128; j += 2) {
         float t0, t1;
         unpack2(mul2(add2(pack2(x[j >> 5][j & 31], x[j >> 5][(j & 31) + 1]), neg2), log2), t0, t1);
-        s[(j >> 1) & 1] = add2(s[(j >> 1) & 1], pack2(ex2(t0), ex2(t1)));
+        s[(j >> 1) & 3] = add2(s[(j >> 1) & 3], pack2(ex2(t0), ex2(t1)));
     }
     float t0, t1;
-    unpack2(add2(s[0], s[1]), t0, t1);
-    a.m = m;
+    unpack2(add2(add2(s[0], s[1]), add2(s[2], s[3])), t0, t1);
     a.s = t0 + t1;
+    return a;
 }
 
 // the caller's type: 32 consecutive elements of a row; `vec` says that 32-byte stores are aligned
@@ -187,7 +196,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
         }
         for (int b = 0; b < 2; ++b) {
             bar_init(&ctl->acc_full[b], 1);
-            bar_init(&ctl->acc_empty[b], 8);       // four epilogue warps of each CTA
+            bar_init(&ctl->acc_empty[b], 16);      // eight epilogue warps of each CTA
         }
         bar_init(&ctl->drain, 1);
         ctl->abort = 0;
@@ -224,20 +233,25 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                 const int mn = (is_b ? it.n : it.m) * kPairTile + rank * 128 + (lane & 1) * 64;
                 const int kb0 = it.split * j.kb_per, kbs = item_blocks(j, it.split);
                 bool ok = true;
-                for (int p = 0; p < j.nprod && ok; ++p) {
+                for (int kc = 0, p = 0; kc < kbs && ok;) {        // chunk by chunk, product by product
                     const int off = seg * (is_b ? part_b(j.nprod, p) : part_a(j.nprod, p));
-                    for (int k = 0; k < kbs; ++k) {
+                    const int k_end = min(kc + j.kc, kbs);
+                    for (int k = kc; k < k_end; ++k) {
                         ok = bar_wait(&ctl->empty[s], par, &ctl->abort, prm.status, limit);
                         if (!ok) break;
                         if (lane == 0 && rank == 0) bar_expect(&ctl->full[s], 2 * kStageBytes);
-                        const int kc = (kb0 + k) * kPairBlockK;
-                        load_box(smem_addr(ring + s * kStageBytes) + lane * kBoxBytes, map, across ? mn + off : kc + off,
-                                 across ? kc : mn, &ctl->full[s]);
+                        const int at = (kb0 + k) * kPairBlockK;
+                        load_box(smem_addr(ring + s * kStageBytes) + lane * kBoxBytes, map, across ? mn + off : at + off,
+                                 across ? at : mn, &ctl->full[s]);
                         ++issued;
                         if (++s == kStages) {
                             s = 0;
                             par ^= 1u;
                         }
+                    }
+                    if (++p == j.nprod) {
+                        p = 0;
+                        kc = k_end;
                     }
                 }
                 if (!ok) break;
@@ -249,6 +263,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
             int s = 0;
             uint32_t par = 0;
             long long used = 0;
+            uint32_t chunk = 0;
             bool ok = true;
             for (int i = 0; i < n_items && ok; ++i) {
                 const Item it = get_item(prm, pair, pairs, i);
@@ -259,59 +274,82 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                                        ((uint32_t)(kPairTile >> 3) << 17) | ((uint32_t)(kPairTile >> 4) << 24);
                 // 16 further along K: 32 bytes inside the swizzle row, or two 8-deep groups
                 const uint64_t a_step = (aa ? 2048 : 32) >> 4, b_step = (ba ? 2048 : 32) >> 4;
-                const int steps = j.nprod * item_blocks(j, it.split);
-                const int buf = i & 1;
-                const uint32_t acc = tmem + (uint32_t)(buf * kPairTile);
-                ok = bar_wait(&ctl->acc_empty[buf], (uint32_t)((i >> 1) & 1) ^ 1u, &ctl->abort, prm.status, limit);
-                if (!ok) break;
-                fence_after();
-                for (int k = 0; k < steps; ++k) {
-                    ok = bar_wait(&ctl->full[s], par, &ctl->abort, prm.status, limit);
+                const int kbs = item_blocks(j, it.split);
+                for (int kc = 0; kc < kbs && ok; kc += j.kc, ++chunk) {
+                    const int steps = j.nprod * min(j.kc, kbs - kc);
+                    const int buf = (int)(chunk & 1u);
+                    const uint32_t acc = tmem + (uint32_t)(buf * kPairTile);
+                    ok = bar_wait(&ctl->acc_empty[buf], ((chunk >> 1) & 1u) ^ 1u, &ctl->abort, prm.status, limit);
                     if (!ok) break;
                     fence_after();
-                    const uint32_t a_addr = smem_addr(ring + s * kStageBytes);
-                    const uint64_t da = tile_desc(a_addr, aa), db = tile_desc(a_addr + kHalfBytes, ba);
+                    for (int k = 0; k < steps; ++k) {
+                        ok = bar_wait(&ctl->full[s], par, &ctl->abort, prm.status, limit);
+                        if (!ok) break;
+                        fence_after();
+                        const uint32_t a_addr = smem_addr(ring + s * kStageBytes);
+                        const uint64_t da = tile_desc(a_addr, aa), db = tile_desc(a_addr + kHalfBytes, ba);
 #pragma unroll
-                    for (int q = 0; q < kPairBlockK / 16; ++q)
-                        mma_pair(acc, da + q * a_step, db + q * b_step, idesc, (k | q) != 0 ? 1u : 0u);
-                    commit_pair(&ctl->empty[s]);
-                    ++used;
-                    if (++s == kStages) {
-                        s = 0;
-                        par ^= 1u;
+                        for (int q = 0; q < kPairBlockK / 16; ++q)
+                            mma_pair(acc, da + q * a_step, db + q * b_step, idesc, (k | q) != 0 ? 1u : 0u);
+                        commit_pair(&ctl->empty[s]);
+                        ++used;
+                        if (++s == kStages) {
+                            s = 0;
+                            par ^= 1u;
+                        }
                     }
+                    if (ok) commit_pair(&ctl->acc_full[buf]);
                 }
-                if (ok) commit_pair(&ctl->acc_full[buf]);
             }
             ctl->consumed = used;
             if (!ok) commit_pair(&ctl->drain);
         }
     } else {
-        // ---------------- epilogue
-        const int quarter = warp & 3;
+        // ---------------- epilogue: a row and 128 columns of the tile per thread
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
         const int r_in = rank * 128 + quarter * 32 + lane;
-        for (int i = 0; i < n_items; ++i) {
+        const uint32_t lane_base = tmem + (uint32_t)(half * 128) + ((uint32_t)(quarter * 32) << 16);
+        uint32_t chunk = 0;
+        bool ok = true;
+        for (int i = 0; i < n_items && ok; ++i) {
             const Item it = get_item(prm, pair, pairs, i);
             const PairJob &j = prm.job[it.job];
-            const int buf = i & 1;
-            if (!bar_wait(&ctl->acc_full[buf], (uint32_t)(i >> 1) & 1u, &ctl->abort, prm.status, limit)) break;
-            __syncwarp();
-            fence_after();
-            const uint32_t acc = tmem + (uint32_t)(buf * kPairTile) + ((uint32_t)(quarter * 32) << 16);
+            float x[4][32];
+            const int kbs = item_blocks(j, it.split);
+            for (int kc = 0; kc < kbs; kc += j.kc, ++chunk) {
+                const int buf = (int)(chunk & 1u);
+                ok = bar_wait(&ctl->acc_full[buf], (chunk >> 1) & 1u, &ctl->abort, prm.status, limit);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                fence_after();
+                const uint32_t acc = lane_base + (uint32_t)(buf * kPairTile);
+                if (kc == 0) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) tmem_read32(acc + 32 * q, x[q]);
+                    tmem_wait();
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float y[32];
+                        tmem_read32(acc + 32 * q, y);
+                        tmem_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2)
+                            unpack2(add2(pack2(x[q][e], x[q][e + 1]), pack2(y[e], y[e + 1])), x[q][e], x[q][e + 1]);
+                    }
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive_even(&ctl->acc_empty[buf]);
+            }
+            if (!ok) break;
             const int64_t row = (int64_t)it.m * kPairTile + r_in;
             const bool live = row < j.rows;
-            const int c0 = it.n * kPairTile;
-            const int width = min(kPairTile, j.cols - c0);        // columns of the tile that exist
+            const int c0 = it.n * kPairTile + half * 128;
+            const int width = min(128, j.cols - c0);              // columns that exist (not positive: none)
             if (EPI == PAIR_STATS) {
-                Stats st = {neg_inf(), 0.f};
-                for (int c = 0; c < width; c += 64) {
-                    float x[2][32];
-                    tmem_read32(acc + c, x[0]);
-                    tmem_read32(acc + c + 32, x[1]);
-                    tmem_wait();
-                    add_stats(st, x, width - c);
-                }
-                if (live) j.part[row * j.tiles_n + it.n] = make_float2(st.m, st.s);
+                const Stats st = row_stats(x, width);
+                if (live) j.part[row * (2 * j.tiles_n) + 2 * it.n + half] = make_float2(st.m, st.s);
             } else if (EPI == PAIR_DLOGITS) {
                 // D = g (exp(l - lse) - [v = target]); rows without a target are zero whatever they hold
                 const int t = live ? j.targets[row] : -1;
@@ -319,60 +357,53 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                 const float lse = keep ? j.lse[row] : 0.f, g = keep ? j.grad_loss[row] : 0.f;
                 const int hot = keep ? t - j.v0 - c0 : -1;
                 __nv_bfloat16 *dst = j.dlogits + row * j.dl_pitch + c0;
-                const int stored = min(kPairTile, j.dl_seg - c0);     // the padding up to a multiple of 64 is zeroed
-                for (int c = 0; c < stored; c += 32) {
-                    float x[32];
-                    tmem_read32(acc + c, x);
-                    tmem_wait();
+                const int stored = min(128, j.dl_seg - c0);       // the padding up to a multiple of 64 is zeroed
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (32 * q >= stored) break;
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
-                        const float p = sizeof(T) == 4 ? expf(x[e] - lse) : ex2((x[e] - lse) * kLog2e);
-                        x[e] = keep && c + e < width ? g * p : 0.f;
+                        const float p = sizeof(T) == 4 ? expf(x[q][e] - lse) : ex2((x[q][e] - lse) * kLog2e);
+                        x[q][e] = keep && 32 * q + e < width ? g * p : 0.f;
                     }
-                    if (__any_sync(0xffffffffu, hot >= c && hot < c + 32)) {
+                    if (hot >= 32 * q && hot < 32 * q + 32) {
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
-                            if (hot == c + e) x[e] -= g;
+                            if (hot == 32 * q + e) x[q][e] -= g;
                     }
                     if (live) {
+#pragma unroll
                         for (int part = 0; part < (sizeof(T) == 4 ? 3 : 1); ++part) {
-                            store_row32(dst + (int64_t)part * j.dl_seg + c, x, 32, true);
+                            store_row32(dst + (int64_t)part * j.dl_seg + 32 * q, x[q], 32, true);
                             if (sizeof(T) == 4) {
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) x[e] -= __bfloat162float(__float2bfloat16(x[e]));
+                                for (int e = 0; e < 32; ++e) x[q][e] -= __bfloat162float(__float2bfloat16(x[q][e]));
                             }
                         }
                     }
-                    __syncwarp();
                 }
-            } else {
+            } else if (live) {
                 float *a = j.acc ? j.acc + (int64_t)it.split * j.acc_stride + row * j.acc_pitch + c0 : nullptr;
                 T *o = j.out ? static_cast<T *>(j.out) + row * j.out_pitch + c0 : nullptr;
                 const bool vec = ((reinterpret_cast<uintptr_t>(j.out) | (uintptr_t)(j.out_pitch * (int64_t)sizeof(T))) & 31) == 0;
-                for (int c = 0; c < width; c += 32) {
-                    float x[32];
-                    tmem_read32(acc + c, x);
-                    tmem_wait();
-                    if (live) {
-                        if (j.add_acc) {      // the pitch covers whole groups of 32
 #pragma unroll
-                            for (int q = 0; q < 8; ++q) {
-                                const float4 y = *reinterpret_cast<const float4 *>(a + c + 4 * q);
-                                x[4 * q] += y.x;
-                                x[4 * q + 1] += y.y;
-                                x[4 * q + 2] += y.z;
-                                x[4 * q + 3] += y.w;
-                            }
+                for (int q = 0; q < 4; ++q) {
+                    if (32 * q >= width) break;
+                    if (j.add_acc) {      // the pitch covers whole groups of 32
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) {
+                            const float4 y = *reinterpret_cast<const float4 *>(a + 32 * q + e);
+                            x[q][e] += y.x;
+                            x[q][e + 1] += y.y;
+                            x[q][e + 2] += y.z;
+                            x[q][e + 3] += y.w;
                         }
-                        if (o) store_row32(o + c, x, width - c, vec);
-                        else store_row32(a + c, x, 32, true);
                     }
-                    __syncwarp();
+                    if (o) store_row32(o + 32 * q, x[q], width - 32 * q, vec);
+                    else store_row32(a + 32 * q, x[q], 32, true);
                 }
             }
-            fence_before();
             __syncwarp();
-            if (lane == 0) bar_arrive_even(&ctl->acc_empty[buf]);
         }
     }
 

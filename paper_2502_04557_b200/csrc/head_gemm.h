@@ -28,11 +28,12 @@ struct PairJob {
     int splits;                   // ranges of the contraction, each with a result of its own
     int kb, kb_per;               // blocks of the contraction; blocks per split
     int nprod;                    // 1, or 6
+    int kc;                       // blocks that one accumulator takes before registers add it up
     int a_across, b_across;
     int a_seg, b_seg;
     int64_t rows;
     int cols;
-    // PAIR_STATS: part[row * tiles_n + tile_n]
+    // PAIR_STATS: part[row * 2 tiles_n + 2 tile_n + half of the tile]
     float2 *part;
     // PAIR_DLOGITS: dlogits[row * dl_pitch + part * dl_seg + column], columns v0 .. v0 + cols of the vocabulary
     __nv_bfloat16 *dlogits;

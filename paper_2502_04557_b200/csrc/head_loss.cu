@@ -6,7 +6,7 @@
 //   D_iv = g_i (exp(l_iv - lse_i) - [v = t_i]),  dH = D W,  dW = D^T H
 //   log p(x_i) = l_{i,x_i} - lse_i
 // The products run on CTA pairs (head_gemm.cu).  Forward: one product whose epilogue leaves (max,
-// sum of exp) per row and 256 columns, then a warp per row that merges them and forms the target's
+// sum of exp) per row and 128 columns, then a warp per row that merges them and forms the target's
 // logit as a dot product of its own - N rows of W, nothing beside the product, and exact to a few
 // units of fp32 however the product's accumulator rounds.  Backward: the vocabulary goes by in
 // pieces; a piece's D is kept in the workspace (bf16, or three bf16 parts for fp32), and one launch
@@ -26,6 +26,8 @@ namespace spr {
 namespace {
 
 constexpr int kHeadMaxLambdas = 8;
+// Blocks of 64 that an accumulator takes (head_gemm.cu): results in bf16 do not show its truncation.
+constexpr int kChunkStats = 4, kChunkF32 = 2;
 constexpr int kRowWarps = 8;                             // rows per CTA of the finish kernels
 constexpr size_t kPieceBytes = (size_t)256 << 20;        // D of one vocabulary piece (see pieces())
 
@@ -91,16 +93,16 @@ __global__ void __launch_bounds__(256) head_pack_kernel(const T *src, int64_t ro
 // ---------------------------------------------------------------- row statistics -> outputs
 struct HeadRow {
     const void *hidden, *W;
-    const float2 *part;      // [N, tiles]
-    int d, tiles;
+    const float2 *part;      // [N, parts]: (max, sum of exp) per 128 columns
+    int d, parts;
 };
 
 // one warp: log-sum-exp of row i
 __device__ __forceinline__ double row_lse(const HeadRow &h, int64_t i, int lane)
 {
     MS a = {neg_inf(), 0.f};
-    const float2 *p = h.part + i * h.tiles;
-    for (int t = lane; t < h.tiles; t += 32) {
+    const float2 *p = h.part + i * h.parts;
+    for (int t = lane; t < h.parts; t += 32) {
         const float2 x = p[t];
         a = ms_merge(a, MS{x.x, x.y});
     }
@@ -233,7 +235,7 @@ HeadLossWs head_loss_layout(Carver &c, int64_t N, int d, int V, int dt)
     HeadLossWs w;
     w.hidden = c.take_data(needs_pack(d, dt) ? packed_bytes(N, d, dt) : 0);
     w.W = c.take_data(needs_pack(d, dt) ? packed_bytes(V, d, dt) : 0);
-    w.part = c.take_data(8 * (size_t)N * (size_t)ceil_div(V, kPairTile));
+    w.part = c.take_data(16 * (size_t)N * (size_t)ceil_div(V, kPairTile));
     return w;
 }
 
@@ -321,6 +323,7 @@ void contraction(PairJob &j, int64_t k, int dt)      // over k elements, in one 
     j.kb = j.kb_per = (int)ceil_div(k, kPairBlockK);
     j.splits = 1;
     j.nprod = dt == SPR_F32 ? 6 : 1;
+    j.kc = dt == SPR_F32 ? kChunkF32 : j.kb;
 }
 
 // job and operands of the row statistics of hidden [N,d] under W [V,d]; packs what has to be packed
@@ -340,6 +343,7 @@ cudaError_t stats_job(PairJob &j, PairOperand &a, PairOperand &b, const void *hi
     }
     memset(&j, 0, sizeof j);
     contraction(j, d, dt);
+    if (dt != SPR_F32) j.kc = kChunkStats;
     j.tiles_m = (int)ceil_div(N, kPairTile);
     j.tiles_n = (int)ceil_div(V, kPairTile);
     j.a_seg = j.b_seg = (int)round_up(d, 64);
@@ -398,7 +402,7 @@ int head_loss(const void *hidden, const void *W, const int32_t *targets, int N, 
     cudaError_t e = stats_job(prm.job[0], a, b, hidden, W, N, d, V, dt, ws, lay, st);
     if (e == cudaSuccess) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, 1, &a, &b, st);
     if (e == cudaSuccess) {
-        const HeadRow h = {hidden, W, prm.job[0].part, d, prm.job[0].tiles_n};
+        const HeadRow h = {hidden, W, prm.job[0].part, d, 2 * prm.job[0].tiles_n};
         const unsigned ctas = (unsigned)ceil_div(N, kRowWarps);
         if (dt == SPR_F32) head_finish_kernel<float><<<ctas, 32 * kRowWarps, 0, st>>>(h, N, V, targets, loss, lse, prm.status);
         else head_finish_kernel<__nv_bfloat16><<<ctas, 32 * kRowWarps, 0, st>>>(h, N, V, targets, loss, lse, prm.status);
@@ -555,8 +559,8 @@ int verifier_labels_head(const void *p_hidden, const void *p_W, int dp, const vo
     if (e == cudaSuccess) e = stats_job(prm.job[iq], a[iq], b[iq], q_hidden, q_W, N, dq, V, dt, ws, lay.q, st);
     if (e == cudaSuccess) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, 2, a, b, st);
     if (e == cudaSuccess) {
-        const HeadRow p = {p_hidden, p_W, prm.job[ip].part, dp, prm.job[ip].tiles_n};
-        const HeadRow q = {q_hidden, q_W, prm.job[iq].part, dq, prm.job[iq].tiles_n};
+        const HeadRow p = {p_hidden, p_W, prm.job[ip].part, dp, 2 * prm.job[ip].tiles_n};
+        const HeadRow q = {q_hidden, q_W, prm.job[iq].part, dq, 2 * prm.job[iq].tiles_n};
         HeadLabels out;
         memset(&out, 0, sizeof out);
         out.n_lambda = n_lambda;

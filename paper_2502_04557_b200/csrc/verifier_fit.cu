@@ -100,7 +100,7 @@ struct TrainParams {
     int d;
     float *theta, *m, *v;    // [d+1]: weights, then the bias
     int t;
-    float lr, beta1, beta2, eps;
+    double lr, beta1, beta2, eps;
     float *loss;             // [1] or null
     float *part;             // [ctas, d+2]: per-CTA sums of the gradient terms, then of the loss
     int ctas;
@@ -434,14 +434,14 @@ __global__ void __launch_bounds__(256) train_adam_kernel(const TrainParams prm)
         if (prm.loss) *prm.loss = (float)sum;
         return;
     }
-    const double b1 = (double)prm.beta1, b2 = (double)prm.beta2;
+    const double b1 = prm.beta1, b2 = prm.beta2;
     const double m = b1 * (double)prm.m[j] + (1.0 - b1) * sum;
     const double v = b2 * (double)prm.v[j] + (1.0 - b2) * sum * sum;
     const double m_hat = m / (1.0 - pow(b1, (double)prm.t));
     const double v_hat = v / (1.0 - pow(b2, (double)prm.t));
     prm.m[j] = (float)m;
     prm.v[j] = (float)v;
-    prm.theta[j] = (float)((double)prm.theta[j] - (double)prm.lr * m_hat / (sqrt(v_hat) + (double)prm.eps));
+    prm.theta[j] = (float)((double)prm.theta[j] - prm.lr * m_hat / (sqrt(v_hat) + prm.eps));
 }
 
 template <typename T, int VPL, int WPR, int R, int SLOTS, int G = 1>
@@ -563,12 +563,12 @@ int verifier_labels(const void *p_logits, const void *q_logits, int64_t ldv, con
 static constexpr int kPacked8 = 2;
 
 static int train_step(const void *hidden, const uint8_t *labels, int64_t N, int d, int dt, float *theta,
-                      float *adam_m, float *adam_v, int t, float lr, float beta1, float beta2, float eps,
+                      float *adam_m, float *adam_v, int t, double lr, double beta1, double beta2, double eps,
                       float *loss, void *ws, size_t ws_bytes, void *cuda_stream, int flags, unsigned spin_limit)
 {
     if (!dtype_ok(dt) && dt != kPacked8) return SPR_ERR_UNSUPPORTED;
-    if (N < 0 || d <= 0 || t < 1 || !(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f) ||
-        !(eps >= 0.f) || !(lr == lr))
+    if (N < 0 || d <= 0 || t < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) ||
+        !(eps >= 0.0) || !(lr == lr))
         return SPR_ERR_INVALID_ARG;
     const int vec = dt == kPacked8 ? Vec<Packed8>::N : vec_elems(dt);
     if (d % vec != 0 || d / vec > 32 * (dt == kPacked8 ? kTrainMaxVpl / 2 : kTrainMaxVpl)) return SPR_ERR_UNSUPPORTED;
@@ -616,7 +616,7 @@ int verifier_train_step(const void *hidden, const uint8_t *labels, int64_t N, in
 }
 
 int verifier_train_step8(const void *packed, const uint8_t *labels, int64_t N, int d, float *theta, float *adam_m,
-                         float *adam_v, int t, float lr, float beta1, float beta2, float eps, float *loss, void *ws,
+                         float *adam_v, int t, double lr, double beta1, double beta2, double eps, float *loss, void *ws,
                          size_t ws_bytes, void *cuda_stream)
 {
     return train_step(packed, labels, N, d, kPacked8, theta, adam_m, adam_v, t, lr, beta1, beta2, eps, loss, ws, ws_bytes,
