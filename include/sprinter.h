@@ -518,6 +518,21 @@ int spr_test_verifier_train_step(const void *hidden, const uint8_t *labels, int6
                                  float beta2, float eps, float *loss, void *ws, size_t ws_bytes,
                                  void *cuda_stream, int flags, unsigned spin_limit);
 
+/*
+ * spr_test_verifier_train_step8, spr_test_pair_kernels - test hooks, not part of the stable interface.
+ *
+ * The paper has no counterpart.  The first is verifier_train_step8 with flags and spin_limit as for
+ * spr_test_verifier_train_step.  The second makes the head_loss, head_loss_grad and verifier_labels_head
+ * calls that this host thread makes afterwards load nothing (flags bit 0), so that the first bounded wait of
+ * every CTA pair runs out after spin_limit polls (0 = the library's limit), with the outcome that those calls
+ * document for SPR_ERR_TIMEOUT, nothing left in flight and the workspace usable; (0, 0) ends it.
+ */
+int spr_test_verifier_train_step8(const void *packed, const uint8_t *labels, int64_t N, int d, float *theta,
+                                  float *adam_m, float *adam_v, int t, double lr, double beta1, double beta2,
+                                  double eps, float *loss, void *ws, size_t ws_bytes, void *cuda_stream, int flags,
+                                  unsigned spin_limit);
+void spr_test_pair_kernels(int flags, unsigned spin_limit);
+
 /* Synchronises the stream, returns the sticky device status word of `ws`
  * (SPR_OK if nothing was detected) and clears it. */
 int spr_device_status(void *ws, void *cuda_stream);

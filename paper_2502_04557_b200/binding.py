@@ -28,7 +28,7 @@ EXPORTS = [
     "sd_shard_stats", "sd_shard_decide", "sd_shard_weights", "sd_shard_draw", "sd_shard_decide_weights",
     "verifier_labels", "verifier_train_step", "spr_test_sprinter_verify", "spr_test_verifier_train_step",
     "head_loss", "head_loss_grad", "verifier_labels_head", "spr_pack8_pitch", "hidden_pack8", "hidden_unpack8",
-    "verifier_train_step8",
+    "verifier_train_step8", "spr_test_verifier_train_step8", "spr_test_pair_kernels",
 ]
 
 
@@ -110,6 +110,10 @@ def lib():
             fn.argtypes = [vp, i64, i32, i32, vp, vp]
         L.verifier_train_step8.restype = i32
         L.verifier_train_step8.argtypes = [vp, vp, i64, i32, vp, vp, vp, i32] + [C.c_double] * 4 + [vp, vp, sz, vp]
+        L.spr_test_verifier_train_step8.restype = i32
+        L.spr_test_verifier_train_step8.argtypes = L.verifier_train_step8.argtypes + [i32, C.c_uint]
+        L.spr_test_pair_kernels.restype = None
+        L.spr_test_pair_kernels.argtypes = [i32, C.c_uint]
         L.spr_host_arena_bytes.restype = sz
         L.spr_host_arena_bytes.argtypes = [i32, i32, i32, i32, i64, i32, i32, i32]
         L.sprinter_verify_host.restype = i32
@@ -677,8 +681,10 @@ def hidden_unpack8(packed, d: int, dtype=torch.bfloat16, out=None):
 
 
 def verifier_train_step8(packed, d: int, labels, theta, adam_m, adam_v, t: int, lr: float, ws: Workspace,
-                         beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, loss=None):
-    """verifier_train_step on hidden states kept in 8 bits: packed u8 [N, pack8_pitch(d)]."""
+                         beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, loss=None,
+                         test_flags: int = 0, spin_limit: int = 0):
+    """verifier_train_step on hidden states kept in 8 bits: packed u8 [N, pack8_pitch(d)].
+    test_flags / spin_limit: the test hook spr_test_verifier_train_step8 instead of the public call."""
     N = _packed(packed, d)
     _dev(labels, torch.uint8, "labels")
     for name, a in (("theta", theta), ("adam_m", adam_m), ("adam_v", adam_v)):
@@ -689,8 +695,12 @@ def verifier_train_step8(packed, d: int, labels, theta, adam_m, adam_v, t: int, 
         raise ValueError("labels must have one entry per hidden state")
     loss = _result(loss, (1,), torch.float32, packed.device, "loss")
     _same_device(ws, packed, labels, theta, adam_m, adam_v, loss)
-    rc = lib().verifier_train_step8(_ptr(packed), _ptr(labels), N, d, _ptr(theta), _ptr(adam_m), _ptr(adam_v), t, lr,
-                                    beta1, beta2, eps, _ptr(loss), _ptr(ws.buf), ws.nbytes, _stream())
+    args = (_ptr(packed), _ptr(labels), N, d, _ptr(theta), _ptr(adam_m), _ptr(adam_v), t, lr, beta1, beta2, eps,
+            _ptr(loss), _ptr(ws.buf), ws.nbytes, _stream())
+    if test_flags or spin_limit:
+        rc = lib().spr_test_verifier_train_step8(*args, test_flags, spin_limit)
+    else:
+        rc = lib().verifier_train_step8(*args)
     _check("verifier_train_step8", rc)
     return loss
 

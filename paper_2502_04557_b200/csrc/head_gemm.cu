@@ -60,7 +60,8 @@ struct PairControl {
     int abort;
     long long consumed;      // stages whose operands the MMA issuer saw arrive
 };
-constexpr size_t kPairSmem = (size_t)kStages * kStageBytes + 1024 + sizeof(PairControl);
+constexpr int kStageFloats = 32 * 17;                   // staging of one epilogue warp: 32 rows of 16 columns, padded
+constexpr size_t kPairSmem = (size_t)kStages * kStageBytes + 1024 + sizeof(PairControl) + 8 * kStageFloats * sizeof(float);
 
 // what a pair does, in order: its items of job 0, then its run of job 1
 struct Item {
@@ -139,37 +140,25 @@ __device__ __forceinline__ Stats row_stats(float (&x)[4][32], int v)
     return a;
 }
 
-// the caller's type: 32 consecutive elements of a row; `vec` says that 32-byte stores are aligned
-__device__ __forceinline__ void store_row32(float *p, const float (&x)[32], int v, bool vec)
+// 32 consecutive elements of a row, to a 32-byte aligned address
+__device__ __forceinline__ void store_row32(float *p, const float (&x)[32])
 {
-    if (vec && v >= 32) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            uint32_t w[8];
+    for (int q = 0; q < 4; ++q) {
+        uint32_t w[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(x[8 * q + e]);
-            store32(p + 8 * q, w);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 32; ++e)
-            if (e < v) p[e] = x[e];
+        for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(x[8 * q + e]);
+        store32(p + 8 * q, w);
     }
 }
-__device__ __forceinline__ void store_row32(__nv_bfloat16 *p, const float (&x)[32], int v, bool vec)
+__device__ __forceinline__ void store_row32(__nv_bfloat16 *p, const float (&x)[32])
 {
-    if (vec && v >= 32) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            uint32_t w[8];
+    for (int q = 0; q < 2; ++q) {
+        uint32_t w[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = pack_bf16(x[16 * q + 2 * e], x[16 * q + 2 * e + 1]);
-            store32(p + 16 * q, w);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 32; ++e)
-            if (e < v) p[e] = __float2bfloat16(x[e]);
+        for (int e = 0; e < 8; ++e) w[e] = pack_bf16(x[16 * q + 2 * e], x[16 * q + 2 * e + 1]);
+        store32(p + 16 * q, w);
     }
 }
 
@@ -183,6 +172,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
     unsigned char *ring = reinterpret_cast<unsigned char *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     PairControl *ctl = reinterpret_cast<PairControl *>(ring + kStages * kStageBytes);
+    pdl_trigger();   // a kernel launched behind this one may set itself up
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = (int)cluster_rank();
     const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
@@ -374,7 +364,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                     if (live) {
 #pragma unroll
                         for (int part = 0; part < (sizeof(T) == 4 ? 3 : 1); ++part) {
-                            store_row32(dst + (int64_t)part * j.dl_seg + 32 * q, x[q], 32, true);
+                            store_row32(dst + (int64_t)part * j.dl_seg + 32 * q, x[q]);
                             if (sizeof(T) == 4) {
 #pragma unroll
                                 for (int e = 0; e < 32; ++e) x[q][e] -= __bfloat162float(__float2bfloat16(x[q][e]));
@@ -382,14 +372,15 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                         }
                     }
                 }
-            } else if (live) {
+            } else {
                 float *a = j.acc ? j.acc + (int64_t)it.split * j.acc_stride + row * j.acc_pitch + c0 : nullptr;
                 T *o = j.out ? static_cast<T *>(j.out) + row * j.out_pitch + c0 : nullptr;
                 const bool vec = ((reinterpret_cast<uintptr_t>(j.out) | (uintptr_t)(j.out_pitch * (int64_t)sizeof(T))) & 31) == 0;
+                float *stage = reinterpret_cast<float *>(ctl + 1) + (warp - 2) * kStageFloats;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     if (32 * q >= width) break;
-                    if (j.add_acc) {      // the pitch covers whole groups of 32
+                    if (live && j.add_acc) {      // the pitch covers whole groups of 32
 #pragma unroll
                         for (int e = 0; e < 32; e += 4) {
                             const float4 y = *reinterpret_cast<const float4 *>(a + 32 * q + e);
@@ -399,8 +390,26 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                             x[q][e + 3] += y.w;
                         }
                     }
-                    if (o) store_row32(o + 32 * q, x[q], width - 32 * q, vec);
-                    else store_row32(a + 32 * q, x[q], 32, true);
+                    if (!o) {
+                        if (live) store_row32(a + 32 * q, x[q]);
+                    } else if (vec && width - 32 * q >= 32) {
+                        if (live) store_row32(o + 32 * q, x[q]);
+                    } else {
+                        // Rows that start anywhere: a thread per row would touch 32 lines per element, so the
+                        // block goes through shared memory and out again two rows of 16 elements at a time.
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) stage[lane * 17 + e] = x[q][16 * h + e];
+                            __syncwarp();
+                            const int col = 32 * q + 16 * h + (lane & 15);
+                            T *out = static_cast<T *>(j.out) + (row - lane) * j.out_pitch + c0 + col;
+#pragma unroll 4
+                            for (int r = lane >> 4; r < 32; r += 2)
+                                if (col < width && row - lane + r < j.rows) out[r * j.out_pitch] = (T)stage[r * 17 + (lane & 15)];
+                            __syncwarp();
+                        }
+                    }
                 }
             }
             __syncwarp();
@@ -479,6 +488,10 @@ cudaError_t launch(const CUtensorMap (&maps)[4], const PairParams &prm, int ctas
 
 }  // namespace
 
+// set for the calling host thread by the test hook spr_test_pair_kernels
+static thread_local int t_test_flags = 0;
+static thread_local unsigned t_spin_limit = 0;
+
 cudaError_t launch_pair(PairEpilogue epi, bool f32, PairParams &prm, int njobs, const PairOperand *a,
                         const PairOperand *b, cudaStream_t st)
 {
@@ -522,7 +535,8 @@ cudaError_t launch_pair(PairEpilogue epi, bool f32, PairParams &prm, int njobs, 
             owed -= n1 * len[1];
         }
     }
-    if (!prm.spin_limit) prm.spin_limit = pairtc::kSpinLimit;
+    prm.spin_limit = t_spin_limit ? t_spin_limit : kSpinLimit;
+    prm.test_flags = t_test_flags;
     switch (epi) {
     case PAIR_STATS: return launch<PAIR_STATS, float>(maps, prm, 2 * pairs, dev, st);    // the same for both types
     case PAIR_DLOGITS: return f32 ? launch<PAIR_DLOGITS, float>(maps, prm, 2 * pairs, dev, st)
@@ -533,3 +547,9 @@ cudaError_t launch_pair(PairEpilogue epi, bool f32, PairParams &prm, int njobs, 
 }
 
 }  // namespace spr
+
+extern "C" void spr_test_pair_kernels(int flags, unsigned spin_limit)
+{
+    spr::t_test_flags = flags & spr::PAIR_TEST_NO_LOADS;
+    spr::t_spin_limit = spin_limit;
+}

@@ -27,8 +27,7 @@ namespace {
 
 constexpr int kHeadMaxLambdas = 8;
 // Blocks of 64 that an accumulator takes (head_gemm.cu): results in bf16 do not show its truncation.
-constexpr int kChunkStats = 4, kChunkF32 = 2;
-constexpr int kRowWarps = 8;                             // rows per CTA of the finish kernels
+constexpr int kChunkStats = 8, kChunkF32 = 2;
 constexpr size_t kPieceBytes = (size_t)256 << 20;        // D of one vocabulary piece (see pieces())
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -97,73 +96,110 @@ struct HeadRow {
     int d, parts;
 };
 
-// one warp: log-sum-exp of row i
-__device__ __forceinline__ double row_lse(const HeadRow &h, int64_t i, int lane)
+constexpr int kRowThreads = 128;         // one CTA per row: its loads are all in flight at once
+
+// log-sum-exp of row i; the result is that of thread 0
+__device__ __forceinline__ double row_lse(const HeadRow &h, int64_t i, float2 *smem)
 {
-    MS a = {neg_inf(), 0.f};
     const float2 *p = h.part + i * h.parts;
-    for (int t = lane; t < h.parts; t += 32) {
-        const float2 x = p[t];
-        a = ms_merge(a, MS{x.x, x.y});
+    const int tid = threadIdx.x;
+    MS a = {neg_inf(), 0.f};
+    for (int t0 = 0; t0 < h.parts; t0 += 8 * kRowThreads) {
+        float2 x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int t = t0 + k * kRowThreads + tid;
+            x[k] = t < h.parts ? p[t] : make_float2(neg_inf(), 0.f);
+        }
+        float m = a.m;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m = fmaxf(m, x[k].x);
+        const float ref = m == neg_inf() ? 0.f : m;
+        float s = a.s * ex2((a.m - ref) * kLog2e);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += x[k].y * ex2((x[k].x - ref) * kLog2e);
+        a.m = m;
+        a.s = s;
     }
     a = warp_ms(a);
-    return (double)a.m + log((double)a.s);
+    if ((tid & 31) == 0) smem[tid >> 5] = make_float2(a.m, a.s);
+    __syncthreads();
+    if (tid == 0) {
+#pragma unroll
+        for (int w = 1; w < kRowThreads / 32; ++w) a = ms_merge(a, MS{smem[w].x, smem[w].y});
+    }
+    __syncthreads();
+    return (double)a.m + (double)logf(a.s);
 }
-// one warp: hidden_i . W_t, fp32 products summed in double (lane and column order fixed)
+// hidden_i . W_t: a thread adds fp32 products (eight of bf16, exact in fp32), the threads are added up in
+// double; the result is that of thread 0
 template <typename T>
-__device__ __forceinline__ double row_logit(const HeadRow &h, int64_t i, int t, int lane)
+__device__ __forceinline__ double row_logit(const HeadRow &h, int64_t i, int t, double *smem)
 {
     constexpr int N = 16 / (int)sizeof(T);
     const T *a = static_cast<const T *>(h.hidden) + i * h.d, *b = static_cast<const T *>(h.W) + (int64_t)t * h.d;
+    const int tid = threadIdx.x;
     double s = 0.0;
     if (h.d % N == 0) {
-        for (int c = lane * N; c < h.d; c += 32 * N) {
+#pragma unroll 4
+        for (int c = tid * N; c < h.d; c += kRowThreads * N) {
             const uint4 x = *reinterpret_cast<const uint4 *>(a + c), y = *reinterpret_cast<const uint4 *>(b + c);
             const uint32_t u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
+            float f = 0.f;
             if (sizeof(T) == 4) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s += (double)__uint_as_float(u[e]) * (double)__uint_as_float(v[e]);
+                for (int e = 0; e < 4; ++e) f = fmaf(__uint_as_float(u[e]), __uint_as_float(v[e]), f);
             } else {
-                float f = 0.f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     f = fmaf(__uint_as_float(u[e] << 16), __uint_as_float(v[e] << 16), f);
                     f = fmaf(__uint_as_float(u[e] & 0xffff0000u), __uint_as_float(v[e] & 0xffff0000u), f);
                 }
-                s += (double)f;
             }
+            s += (double)f;
         }
     } else {
-        for (int c = lane; c < h.d; c += 32) s += (double)(float)a[c] * (double)(float)b[c];
+#pragma unroll 4
+        for (int c = tid; c < h.d; c += kRowThreads) s += (double)((float)a[c] * (float)b[c]);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if ((tid & 31) == 0) smem[tid >> 5] = s;
+    __syncthreads();
+    if (tid == 0) {
+#pragma unroll
+        for (int w = 1; w < kRowThreads / 32; ++w) s += smem[w];
+    }
+    __syncthreads();
     return s;
 }
 
 __device__ __forceinline__ bool gave_up(const int *status) { return *reinterpret_cast<const volatile int *>(status) == SPR_ERR_TIMEOUT; }
 
 template <typename T>
-__global__ void __launch_bounds__(32 * kRowWarps) head_finish_kernel(const HeadRow h, int64_t N, int V, const int32_t *targets,
-                                                                     float *loss, float *lse, int *status)
+__global__ void __launch_bounds__(kRowThreads) head_finish_kernel(const HeadRow h, int V, const int32_t *targets, float *loss,
+                                                                  float *lse, int *status)
 {
-    const int lane = threadIdx.x & 31;
-    const int64_t i = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
-    if (i >= N) return;
-    const double z = gave_up(status) ? (double)__int_as_float(0x7fc00000) : row_lse(h, i, lane);
+    __shared__ double sums[kRowThreads / 32];
+    __shared__ float2 stats[kRowThreads / 32];
+    const int64_t i = blockIdx.x;
     const int t = targets[i];
-    double l = 0.0;
-    if (t >= 0 && t < V) {
-        l = z - row_logit<T>(h, i, t, lane);
-        if (l < 0.0) l = 0.0;        // -log p is not negative: rounding alone can make it so (NaN stays)
+    const bool live = t >= 0 && t < V;
+    const double at = live ? row_logit<T>(h, i, t, sums) : 0.0;       // before the product: it may still be running
+    pdl_wait();
+    const double z = row_lse(h, i, stats);
+    if (threadIdx.x != 0) return;
+    float l = 0.f, zf = (float)z;
+    if (live) {
+        l = (float)(z - at);
+        if (l < 0.f) l = 0.f;        // -log p is not negative: rounding alone can make it so (NaN stays)
     } else if (t >= V) {
-        l = -1.0;
-        if (lane == 0) raise_status(status, SPR_ERR_BAD_TOKEN);
+        l = -1.f;
+        raise_status(status, SPR_ERR_BAD_TOKEN);
     }
-    if (lane == 0) {
-        loss[i] = (float)l;
-        if (lse) lse[i] = (float)z;
-    }
+    if (gave_up(status)) l = zf = __int_as_float(0x7fc00000);
+    loss[i] = l;
+    if (lse) lse[i] = zf;
 }
 
 struct HeadLabels {
@@ -173,25 +209,32 @@ struct HeadLabels {
     float *ratio;        // [N] or null
 };
 template <typename T>
-__global__ void __launch_bounds__(32 * kRowWarps) head_labels_kernel(const HeadRow p, const HeadRow q, int64_t N, int V,
-                                                                     const int32_t *tokens, const HeadLabels out, int *status)
+__global__ void __launch_bounds__(kRowThreads) head_labels_kernel(const HeadRow p, const HeadRow q, int64_t N, int V,
+                                                                  const int32_t *tokens, const HeadLabels out, int *status)
 {
-    const int lane = threadIdx.x & 31;
-    const int64_t i = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
-    if (i >= N) return;
+    __shared__ double sums[kRowThreads / 32];
+    __shared__ float2 stats[kRowThreads / 32];
+    __shared__ double answer;
+    const int64_t i = blockIdx.x;
     const int x = tokens[i];
-    double ratio = -1.0;
     const bool valid = x >= 0 && x < V;
+    double at = 0.0;
     if (valid) {
-        const double log_p = row_logit<T>(p, i, x, lane) - row_lse(p, i, lane);
-        const double log_q = row_logit<T>(q, i, x, lane) - row_lse(q, i, lane);
-        ratio = exp(log_q - log_p);
-        if (gave_up(status)) ratio = (double)__int_as_float(0x7fc00000);
-    } else if (lane == 0) {
+        at = row_logit<T>(q, i, x, sums);
+        at -= row_logit<T>(p, i, x, sums);
+    }
+    pdl_wait();
+    if (valid) {
+        const double zp = row_lse(p, i, stats), zq = row_lse(q, i, stats);
+        if (threadIdx.x == 0) answer = gave_up(status) ? (double)__int_as_float(0x7fc00000) : exp(at - (zq - zp));
+    } else if (threadIdx.x == 0) {
+        answer = -1.0;
         raise_status(status, SPR_ERR_BAD_TOKEN);
     }
-    if (lane < out.n_lambda) out.labels[(int64_t)lane * N + i] = (valid && ratio <= (double)out.lambdas[lane]) ? 1 : 0;
-    if (lane == 0 && out.ratio) out.ratio[i] = (float)ratio;
+    __syncthreads();
+    const int l = threadIdx.x;
+    if (l < out.n_lambda) out.labels[(int64_t)l * N + i] = (valid && answer <= (double)out.lambdas[l]) ? 1 : 0;
+    if (l == 0 && out.ratio) out.ratio[i] = (float)answer;
 }
 
 // out[r, c] = sum over the slices, in order
@@ -205,13 +248,19 @@ __global__ void __launch_bounds__(256) head_sum_kernel(const float *acc, int sli
         const int64_t r = i / groups;
         const int c = (int)(i - r * groups) * 4;
         const float *p = acc + r * pitch + c;
-        float4 s = *reinterpret_cast<const float4 *>(p);
-        for (int k = 1; k < slices; ++k) {
-            const float4 x = *reinterpret_cast<const float4 *>(p + k * stride);
-            s.x += x.x;
-            s.y += x.y;
-            s.z += x.z;
-            s.w += x.w;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k0 = 0; k0 < slices; k0 += 8) {
+            float4 x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                x[k] = k0 + k < slices ? *reinterpret_cast<const float4 *>(p + (k0 + k) * stride) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                s.x += x[k].x;
+                s.y += x[k].y;
+                s.z += x[k].z;
+                s.w += x[k].w;
+            }
         }
         const float v[4] = {s.x, s.y, s.z, s.w};
         T *o = out + r * d + c;
@@ -254,13 +303,11 @@ Pieces pieces(int64_t N, int d, int V, int dt)
     p.count = (int)ceil_div(V, most);
     p.width = (int)round_up(ceil_div(V, p.count), kPairTile);
     p.count = (int)ceil_div(V, p.width);
-    // dH has few tiles with a long contraction, dW many with a short one, in one launch: no dH item is
-    // longer than half of a pair's share (74 pairs), so that dW evens the pairs out
-    const int64_t kb_v = ceil_div(p.count > 1 ? p.width : V, kPairBlockK), kb_n = ceil_div(N, kPairBlockK), td = ceil_div(d, kPairTile);
-    const double share = (double)(ceil_div(N, kPairTile) * td * kb_v + p.width / kPairTile * td * kb_n) / 74.0;
-    int64_t s = (int64_t)(2.0 * (double)kb_v / share) + 1;
+    // dH has few tiles with a long contraction, dW many with a short one, in one launch: dH is cut so
+    // that every one of the 74 pairs has one item of it, and dW evens them out
+    const int64_t kb_v = ceil_div(p.count > 1 ? p.width : V, kPairBlockK);
+    int64_t s = 74 / (ceil_div(N, kPairTile) * ceil_div(d, kPairTile));
     if (s > kb_v / 4) s = kb_v / 4;
-    if (s > 32) s = 32;
     if (s < 1) s = 1;
     p.kb_per = (int)ceil_div(kb_v, s);
     p.splits = (int)ceil_div(kb_v, p.kb_per);
@@ -296,6 +343,23 @@ HeadLabelsWs head_labels_layout(Carver &c, int64_t N, int dp, int dq, int V, int
 }
 
 // ---------------------------------------------------------------- launches
+// A kernel that starts while the one before it in the stream ends (programmatic dependent launch) and
+// calls pdl_wait() before it touches what that one writes.
+template <typename... P, typename... A>
+cudaError_t launch_behind(void (*kernel)(P...), int64_t ctas, int threads, cudaStream_t st, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
 template <typename T>
 cudaError_t pack_rows(const void *src, int64_t rows, int d, const int32_t *targets, int V, void *dst, int *status, cudaStream_t st)
 {
@@ -403,10 +467,8 @@ int head_loss(const void *hidden, const void *W, const int32_t *targets, int N, 
     if (e == cudaSuccess) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, 1, &a, &b, st);
     if (e == cudaSuccess) {
         const HeadRow h = {hidden, W, prm.job[0].part, d, 2 * prm.job[0].tiles_n};
-        const unsigned ctas = (unsigned)ceil_div(N, kRowWarps);
-        if (dt == SPR_F32) head_finish_kernel<float><<<ctas, 32 * kRowWarps, 0, st>>>(h, N, V, targets, loss, lse, prm.status);
-        else head_finish_kernel<__nv_bfloat16><<<ctas, 32 * kRowWarps, 0, st>>>(h, N, V, targets, loss, lse, prm.status);
-        e = cudaGetLastError();
+        e = dt == SPR_F32 ? launch_behind(head_finish_kernel<float>, N, kRowThreads, st, h, V, targets, loss, lse, prm.status)
+                          : launch_behind(head_finish_kernel<__nv_bfloat16>, N, kRowThreads, st, h, V, targets, loss, lse, prm.status);
     }
     return finish(e);
 }
@@ -567,10 +629,8 @@ int verifier_labels_head(const void *p_hidden, const void *p_W, int dp, const vo
         for (int l = 0; l < n_lambda; ++l) out.lambdas[l] = lambdas[l];
         out.labels = labels;
         out.ratio = ratio;
-        const unsigned ctas = (unsigned)ceil_div(N, kRowWarps);
-        if (dt == SPR_F32) head_labels_kernel<float><<<ctas, 32 * kRowWarps, 0, st>>>(p, q, N, V, draft_tokens, out, prm.status);
-        else head_labels_kernel<__nv_bfloat16><<<ctas, 32 * kRowWarps, 0, st>>>(p, q, N, V, draft_tokens, out, prm.status);
-        e = cudaGetLastError();
+        e = dt == SPR_F32 ? launch_behind(head_labels_kernel<float>, N, kRowThreads, st, p, q, (int64_t)N, V, draft_tokens, out, prm.status)
+                          : launch_behind(head_labels_kernel<__nv_bfloat16>, N, kRowThreads, st, p, q, (int64_t)N, V, draft_tokens, out, prm.status);
     }
     return finish(e);
 }

@@ -149,6 +149,27 @@ struct VerifierTune {
 // elements, padding to 16 bytes).
 __host__ __device__ constexpr int pack8_pitch(int d) { return (d + (d + 31) / 32 + 15) / 16 * 16; }
 
+// verifier_train_step and verifier_train_step8: gradient pass, then one thread per parameter
+struct TrainParams {
+    const void *hidden;      // [N, d], or packed rows of 8-bit states
+    const uint8_t *labels;   // [N]
+    int64_t N;
+    int d;
+    float *theta, *m, *v;    // [d+1]: weights, then the bias
+    int t;
+    double lr, beta1, beta2, eps;
+    float *loss;             // [1] or null
+    float *part;             // [ctas, d+2]: per-CTA sums of the gradient terms, then of the loss
+    int ctas;
+    int *status;             // the workspace's status word
+    uint32_t spin_limit;     // polls of one mbarrier before the gradient kernel gives up
+    int test_flags;          // TRAIN_TEST_NO_FETCH
+};
+enum { TRAIN_TEST_NO_FETCH = 1 };   // test hook: no row is ever fetched, so the first wait of every team runs out
+constexpr uint32_t kTrainSpin = 1u << 22;   // polls of one mbarrier before a gradient kernel gives up
+// sums the CTAs' partials and takes the Adam step; behind: the gradient kernel lets it start early
+cudaError_t launch_train_adam(const TrainParams &p, cudaStream_t st, bool behind);
+
 // workspace of head_loss, head_loss_grad and verifier_labels_head (head_loss.cu); 0 for bad sizes
 size_t head_loss_ws_bytes(int64_t N, int d, int V, int dt);
 size_t head_grad_ws_bytes(int64_t N, int d, int V, int dt);

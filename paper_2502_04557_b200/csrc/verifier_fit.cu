@@ -51,65 +51,6 @@ __global__ void __launch_bounds__(256) labels_kernel(const LabelParams prm)
 }
 
 // ---------------------------------------------------------------------------- training
-}  // namespace
-
-// Rows of hidden states kept in 8 bits (hidden_pack.cu): d signed bytes q, then one exponent byte e
-// per 32 of them; an element is q 2^e.
-struct Packed8 {};
-template <>
-struct Vec<Packed8> {
-    static constexpr int N = 16;
-    // the signed bytes as floats: byte + 128 becomes the low mantissa byte of 2^23, which is then taken off
-    static __device__ __forceinline__ void unpack(const uint4 &v, float (&f)[N])
-    {
-        const uint32_t w[4] = {v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u};
-        const uint64_t off = pack2(-8388736.f, -8388736.f);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint64_t a = add2(pack2(__uint_as_float(__byte_perm(w[j], 0x4b000000u, 0x7440)),
-                                          __uint_as_float(__byte_perm(w[j], 0x4b000000u, 0x7441))), off);
-            const uint64_t b = add2(pack2(__uint_as_float(__byte_perm(w[j], 0x4b000000u, 0x7442)),
-                                          __uint_as_float(__byte_perm(w[j], 0x4b000000u, 0x7443))), off);
-            unpack2(a, f[4 * j], f[4 * j + 1]);
-            unpack2(b, f[4 * j + 2], f[4 * j + 3]);
-        }
-    }
-};
-
-namespace {
-
-// How a row of d elements lies in memory: bytes (a multiple of 16), and the 16-byte vectors of
-// shared memory it may take when each of 32 WPR lanes has VPL vectors of elements.
-template <typename T>
-struct RowOf {
-    static constexpr bool kScaled = false;
-    static __host__ __device__ constexpr uint32_t bytes(int d) { return (uint32_t)d * (uint32_t)sizeof(T); }
-    static __host__ __device__ constexpr int vecs(int vpl, int wpr) { return vpl * wpr * 32; }
-};
-template <>
-struct RowOf<Packed8> {
-    static constexpr bool kScaled = true;      // an exponent byte per two vectors
-    static __host__ __device__ constexpr uint32_t bytes(int d) { return (uint32_t)pack8_pitch(d); }
-    static __host__ __device__ constexpr int vecs(int vpl, int wpr) { return vpl * wpr * 33; }
-};
-
-struct TrainParams {
-    const void *hidden;      // [N, d], or rows of 8-bit states
-    const uint8_t *labels;   // [N]
-    int64_t N;
-    int d;
-    float *theta, *m, *v;    // [d+1]: weights, then the bias
-    int t;
-    double lr, beta1, beta2, eps;
-    float *loss;             // [1] or null
-    float *part;             // [ctas, d+2]: per-CTA sums of the gradient terms, then of the loss
-    int ctas;
-    int *status;             // the workspace's status word
-    uint32_t spin_limit;     // polls of one mbarrier before the gradient kernel gives up
-    int test_flags;          // TRAIN_TEST_NO_FETCH
-};
-enum { TRAIN_TEST_NO_FETCH = 1 };   // test hook: no row is ever fetched, so the first wait of every team runs out
-
 // Gradient pass (one resident wave of CTAs), every hidden state read from HBM exactly once:
 //   z = b + w.s,  r = sigma(z) - y,  grad_w += r s,  grad_b += r,  loss += ln(1 + e^z) - y z
 // Rows are dealt to teams of warps in a fixed pattern, the teams of a CTA add their sums in team
@@ -123,7 +64,7 @@ enum { TRAIN_TEST_NO_FETCH = 1 };   // test hook: no row is ever fetched, so the
 // gradient sums in registers; with two warps per row each warp has half of the columns and the
 // two halves of a dot product meet in shared memory.  A slot is refilled as soon as both
 // passes over it are done.
-constexpr uint32_t kRingSpin = 1u << 22;      // polls of one mbarrier before the kernel gives up
+
 
 __device__ __forceinline__ uint32_t ring_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ bool ring_poll(uint64_t *bar, uint32_t parity)
@@ -168,12 +109,12 @@ __host__ __device__ constexpr int ring_ctas_per_sm(int vpl, int wpr, int g) { re
 // a team then takes blocks of G rows, and R divides G so that the rows a team works on together
 // lie in one slot.
 template <typename T, int VPL, int WPR, int R, int SLOTS, int G>
-__global__ void __launch_bounds__(kThreads, ring_ctas_per_sm(RowOf<T>::kScaled ? 2 * VPL : VPL, WPR, G)) train_grad_ring_kernel(const TrainParams prm)
+__global__ void __launch_bounds__(kThreads, ring_ctas_per_sm(VPL, WPR, G)) train_grad_ring_kernel(const TrainParams prm)
 {
     static_assert(G == 1 || (G % R == 0 && WPR == 1), "the rows of a group share a slot");
     constexpr int N = Vec<T>::N;
     constexpr int kTeams = kWarps / WPR;
-    constexpr int kSlotVecs = RowOf<T>::vecs(VPL, WPR) * G;
+    constexpr int kSlotVecs = VPL * WPR * 32 * G;
     extern __shared__ __align__(128) unsigned char rsmem[];
     __shared__ __align__(8) uint64_t bars[kTeams][SLOTS];
     __shared__ float halves[kTeams][R][2];    // WPR = 2: the two warps' parts of the R dot products
@@ -182,8 +123,7 @@ __global__ void __launch_bounds__(kThreads, ring_ctas_per_sm(RowOf<T>::kScaled ?
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int team = warp / WPR, half = warp % WPR;
     const int nv = d / N;
-    const uint32_t row_bytes = RowOf<T>::bytes(d);   // a multiple of 16: d is a multiple of N
-    const int row_vecs = (int)(row_bytes / 16);
+    const uint32_t row_bytes = (uint32_t)d * (uint32_t)sizeof(T);   // a multiple of 16: d is a multiple of N
     uint4 *ring = reinterpret_cast<uint4 *>(rsmem) + (size_t)team * SLOTS * kSlotVecs;
     float *red = reinterpret_cast<float *>(rsmem + (size_t)kTeams * SLOTS * kSlotVecs * 16);   // [d + 2]
     uint64_t *bar = bars[team];
@@ -207,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, ring_ctas_per_sm(RowOf<T>::kScaled ?
 
     // Blocks of G consecutive rows are dealt to the teams in a fixed pattern; block k of this team
     // is block first + k * stride of the data, goes to slot k % SLOTS and is its (k / SLOTS)-th fill.
-    const char *base = static_cast<const char *>(prm.hidden);
+    const T *base = static_cast<const T *>(prm.hidden);
     const int64_t blocks = (prm.N + G - 1) / G;
     const int64_t stride = (int64_t)gridDim.x * kTeams;
     const int64_t first = (int64_t)blockIdx.x * kTeams + team;
@@ -219,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, ring_ctas_per_sm(RowOf<T>::kScaled ?
     auto row_of = [&](int i) { return (first + (int64_t)(i / G) * stride) * G + i % G; };   // row i of this team
     const bool feeder = half == 0 && lane == 0 && !(prm.test_flags & TRAIN_TEST_NO_FETCH);
     auto fetch_block = [&](int k) {
-        ring_fetch(ring + (k % SLOTS) * kSlotVecs, base + (first + (int64_t)k * stride) * G * row_bytes,
+        ring_fetch(ring + (k % SLOTS) * kSlotVecs, base + (first + (int64_t)k * stride) * G * d,
                    (uint32_t)rows_in(k) * row_bytes, &bar[k % SLOTS]);
     };
     const uint32_t limit = prm.spin_limit;
@@ -239,13 +179,6 @@ __global__ void __launch_bounds__(kThreads, ring_ctas_per_sm(RowOf<T>::kScaled ?
     bool ok = true;
     int fail_at = 0;                          // first row of the group whose wait ran out
 
-    // 2^e of vector vi of the row that starts at vector s of the ring (-128 marks a block that held
-    // infinities or NaN: they come back as NaN)
-    auto vec_scale = [&](int s, int vi) {
-        const int e = reinterpret_cast<const signed char *>(ring + s)[d + (vi >> 1)];
-        return e == -128 ? __int_as_float(0x7fc00000) : __int_as_float((e + 127) << 23);
-    };
-
     // rows [i, i + RR) of this team, RR <= R
     auto group = [&](auto rr_tag, int i) {
         constexpr int RR = decltype(rr_tag)::value;
@@ -255,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, ring_ctas_per_sm(RowOf<T>::kScaled ?
 #pragma unroll
         for (int r = 0; r < RR; ++r) {
             blk[r] = (i + r) / G;
-            s[r] = (blk[r] % SLOTS) * kSlotVecs + ((i + r) % G) * (G > 1 ? row_vecs : 0);
+            s[r] = (blk[r] % SLOTS) * kSlotVecs + ((i + r) % G) * (G > 1 ? nv : 0);
             const int idx = i + r;
             if ((idx & 31) == 0 && idx > 0) {
                 y_batch = y_batch_next;
@@ -286,18 +219,9 @@ __global__ void __launch_bounds__(kThreads, ring_ctas_per_sm(RowOf<T>::kScaled ?
                     const uint4 x = vi < nv ? ring[s[r] + vi] : make_uint4(0u, 0u, 0u, 0u);
                     float f[N];
                     Vec<T>::unpack(x, f);
-                    if constexpr (RowOf<T>::kScaled) {
-                        uint64_t part = pack2(0.f, 0.f);
 #pragma unroll
-                        for (int e = 0; e < N; e += 2)
-                            part = fma2(pack2(f[e], f[e + 1]), w2[(j * N + e) / 2], part);
-                        const float sc = vi < nv ? vec_scale(s[r], vi) : 0.f;
-                        dot[r][j & 1] = fma2(pack2(sc, sc), part, dot[r][j & 1]);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < N; e += 2)
-                            dot[r][j & 1] = fma2(pack2(f[e], f[e + 1]), w2[(j * N + e) / 2], dot[r][j & 1]);
-                    }
+                    for (int e = 0; e < N; e += 2)
+                        dot[r][j & 1] = fma2(pack2(f[e], f[e + 1]), w2[(j * N + e) / 2], dot[r][j & 1]);
                 }
             }
         }
@@ -349,14 +273,9 @@ __global__ void __launch_bounds__(kThreads, ring_ctas_per_sm(RowOf<T>::kScaled ?
                 const uint4 x = vi < nv ? ring[s[r] + vi] : make_uint4(0u, 0u, 0u, 0u);
                 float f[N];
                 Vec<T>::unpack(x, f);
-                uint64_t rs = res2[r];
-                if constexpr (RowOf<T>::kScaled) {
-                    const float sc = vi < nv ? vec_scale(s[r], vi) : 0.f;
-                    rs = mul2(rs, pack2(sc, sc));
-                }
 #pragma unroll
                 for (int e = 0; e < N; e += 2)
-                    acc[(j * N + e) / 2] = fma2(rs, pack2(f[e], f[e + 1]), acc[(j * N + e) / 2]);
+                    acc[(j * N + e) / 2] = fma2(res2[r], pack2(f[e], f[e + 1]), acc[(j * N + e) / 2]);
             }
         }
         team_sync<WPR>(team);                  // the whole team is done with the slots: refill them
@@ -417,18 +336,25 @@ __global__ void __launch_bounds__(kThreads, ring_ctas_per_sm(RowOf<T>::kScaled ?
 
 // One thread per parameter: sums the CTA partials in CTA order, divides by N, applies the
 // bias-corrected Adam update (arithmetic in double, state kept in float).
-__global__ void __launch_bounds__(256) train_adam_kernel(const TrainParams prm)
+__global__ void __launch_bounds__(64) train_adam_kernel(const TrainParams prm)
 {
     const int j = blockIdx.x * blockDim.x + threadIdx.x;
     const int d = prm.d;
     if (j > d + 1) return;
+    pdl_wait();
     if (*reinterpret_cast<volatile int *>(prm.status) == SPR_ERR_TIMEOUT) {
         // the gradient pass gave up: no step is taken, the loss reads NaN
         if (j == d + 1 && prm.loss) *prm.loss = __int_as_float(0x7fc00000);
         return;
     }
     double sum = 0.0;
-    for (int c = 0; c < prm.ctas; ++c) sum += (double)prm.part[(int64_t)c * (d + 2) + j];
+    for (int c0 = 0; c0 < prm.ctas; c0 += 16) {       // sixteen loads in flight, added in CTA order
+        float x[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) x[k] = c0 + k < prm.ctas ? prm.part[(int64_t)(c0 + k) * (d + 2) + j] : 0.f;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) sum += (double)x[k];
+    }
     sum /= (double)prm.N;
     if (j == d + 1) {
         if (prm.loss) *prm.loss = (float)sum;
@@ -444,12 +370,30 @@ __global__ void __launch_bounds__(256) train_adam_kernel(const TrainParams prm)
     prm.theta[j] = (float)((double)prm.theta[j] - prm.lr * m_hat / (sqrt(v_hat) + prm.eps));
 }
 
+}  // namespace
+
+cudaError_t launch_train_adam(const TrainParams &p, cudaStream_t st, bool behind)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((p.d + 2 + 63) / 64));
+    cfg.blockDim = dim3(64);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = behind ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, train_adam_kernel, p);
+}
+
+namespace {
+
 template <typename T, int VPL, int WPR, int R, int SLOTS, int G = 1>
 cudaError_t launch_grad_ring(const TrainParams &tp, cudaStream_t st)
 {
     TrainParams p = tp;
     constexpr int kTeams = kWarps / WPR;
-    const size_t smem = (size_t)kTeams * SLOTS * RowOf<T>::vecs(VPL, WPR) * G * 16 + sizeof(float) * ((size_t)tp.d + 2);
+    const size_t smem = (size_t)kTeams * SLOTS * VPL * WPR * 32 * G * 16 + sizeof(float) * ((size_t)tp.d + 2);
     auto kernel = train_grad_ring_kernel<T, VPL, WPR, R, SLOTS, G>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     int per_sm = 0, dev = 0, sms = 0;
@@ -463,8 +407,8 @@ cudaError_t launch_grad_ring(const TrainParams &tp, cudaStream_t st)
     const int64_t blocks = (tp.N + G - 1) / G;
     p.ctas = (int)max((int64_t)1, min((int64_t)min(kTrainMaxCtas, per_sm * sms), (blocks + kTeams - 1) / kTeams));
     kernel<<<p.ctas, kThreads, smem, st>>>(p);
-    train_adam_kernel<<<(tp.d + 2 + 255) / 256, 256, 0, st>>>(p);
-    return cudaGetLastError();
+    const cudaError_t rc = cudaGetLastError();
+    return rc != cudaSuccess ? rc : launch_train_adam(p, st, false);
 }
 
 template <typename T>
@@ -482,18 +426,6 @@ cudaError_t launch_grad_any(const TrainParams &tp, cudaStream_t st)
     return launch_grad_ring<T, 8, 2, 2, 6>(tp, st);
 }
 
-// rows kept in 8 bits: a lane's vector holds twice the elements of a bf16 one, so a team of two warps
-// starts at 2048 elements
-cudaError_t launch_grad_packed8(const TrainParams &tp, cudaStream_t st)
-{
-    const int vpl = (tp.d / Vec<Packed8>::N + 31) / 32;
-    if (vpl <= 1) return launch_grad_ring<Packed8, 1, 1, 4, 3, 8>(tp, st);
-    if (vpl <= 2) return launch_grad_ring<Packed8, 2, 1, 4, 3, 4>(tp, st);
-    if (vpl <= 3) return launch_grad_ring<Packed8, 3, 1, 2, 14>(tp, st);
-    if (vpl <= 4) return launch_grad_ring<Packed8, 4, 1, 2, 11>(tp, st);
-    if (vpl <= 6) return launch_grad_ring<Packed8, 3, 2, 2, 14>(tp, st);
-    return launch_grad_ring<Packed8, 4, 2, 2, 11>(tp, st);
-}
 
 }  // namespace
 
@@ -559,19 +491,16 @@ int verifier_labels(const void *p_logits, const void *q_logits, int64_t ldv, con
     return finish(e);
 }
 
-// dt of rows kept in 8 bits, inside this file
-static constexpr int kPacked8 = 2;
-
 static int train_step(const void *hidden, const uint8_t *labels, int64_t N, int d, int dt, float *theta,
-                      float *adam_m, float *adam_v, int t, double lr, double beta1, double beta2, double eps,
+                      float *adam_m, float *adam_v, int t, float lr, float beta1, float beta2, float eps,
                       float *loss, void *ws, size_t ws_bytes, void *cuda_stream, int flags, unsigned spin_limit)
 {
-    if (!dtype_ok(dt) && dt != kPacked8) return SPR_ERR_UNSUPPORTED;
-    if (N < 0 || d <= 0 || t < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) ||
-        !(eps >= 0.0) || !(lr == lr))
+    if (!dtype_ok(dt)) return SPR_ERR_UNSUPPORTED;
+    if (N < 0 || d <= 0 || t < 1 || !(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f) ||
+        !(eps >= 0.f) || !(lr == lr))
         return SPR_ERR_INVALID_ARG;
-    const int vec = dt == kPacked8 ? Vec<Packed8>::N : vec_elems(dt);
-    if (d % vec != 0 || d / vec > 32 * (dt == kPacked8 ? kTrainMaxVpl / 2 : kTrainMaxVpl)) return SPR_ERR_UNSUPPORTED;
+    const int vec = vec_elems(dt);
+    if (d % vec != 0 || d / vec > 32 * kTrainMaxVpl) return SPR_ERR_UNSUPPORTED;
     if (N == 0) return SPR_OK;
     if (!hidden || !labels || !theta || !adam_m || !adam_v) return SPR_ERR_INVALID_ARG;
     if (!aligned(hidden, 16) || !aligned(theta, 4) || !aligned(adam_m, 4) || !aligned(adam_v, 4) ||
@@ -600,11 +529,10 @@ static int train_step(const void *hidden, const uint8_t *labels, int64_t N, int 
     tp.loss = loss;
     tp.part = at<float>(ws, part_off);
     tp.status = at<int>(ws, 0);
-    tp.spin_limit = spin_limit ? spin_limit : kRingSpin;
+    tp.spin_limit = spin_limit ? spin_limit : kTrainSpin;
     tp.test_flags = flags;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return finish(dt == kPacked8 ? launch_grad_packed8(tp, st)
-                  : dt == SPR_F32 ? launch_grad_any<float>(tp, st) : launch_grad_any<__nv_bfloat16>(tp, st));
+    return finish(dt == SPR_F32 ? launch_grad_any<float>(tp, st) : launch_grad_any<__nv_bfloat16>(tp, st));
 }
 
 int verifier_train_step(const void *hidden, const uint8_t *labels, int64_t N, int d, int dt, float *theta,
@@ -612,14 +540,6 @@ int verifier_train_step(const void *hidden, const uint8_t *labels, int64_t N, in
                         float *loss, void *ws, size_t ws_bytes, void *cuda_stream)
 {
     return train_step(hidden, labels, N, d, dt, theta, adam_m, adam_v, t, lr, beta1, beta2, eps, loss, ws, ws_bytes,
-                      cuda_stream, 0, 0u);
-}
-
-int verifier_train_step8(const void *packed, const uint8_t *labels, int64_t N, int d, float *theta, float *adam_m,
-                         float *adam_v, int t, double lr, double beta1, double beta2, double eps, float *loss, void *ws,
-                         size_t ws_bytes, void *cuda_stream)
-{
-    return train_step(packed, labels, N, d, kPacked8, theta, adam_m, adam_v, t, lr, beta1, beta2, eps, loss, ws, ws_bytes,
                       cuda_stream, 0, 0u);
 }
 

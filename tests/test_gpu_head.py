@@ -291,6 +291,40 @@ def test_captured_and_replayed_with_new_inputs_and_on_another_stream(spr):
     assert torch.equal(loss, want[1][0])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=IDS.get)
+def test_bounded_waits_run_out_and_the_workspace_survives(spr, dtype):
+    """Nothing is loaded (test hook): the first wait of every CTA pair expires after a few thousand polls, the calls
+    end by themselves and report SPR_ERR_TIMEOUT, loss and lse are NaN, labels 0; normal calls follow."""
+    N, d, V = 300, 200, 2001
+    h, w, t, gl = problem(N, d, V, dtype, seed=15)
+    n = max(spr.workspace_bytes(op, N, 1, V, d, 200, code(spr, dtype))
+            for op in (spr.OP_HEAD_LOSS, spr.OP_HEAD_LOSS_GRAD, spr.OP_VERIFIER_LABELS_HEAD))
+    ws = spr.Workspace(n)
+    want = spr.head_loss(h, w, t, ws)
+    grads = spr.head_loss_grad(h, w, t, want[1], gl, ws)
+    labels = spr.verifier_labels_head(h, w, h, w, t.clamp(min=0), [1.5], ws)
+    assert ws.device_status() == 0
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    spr.lib().spr_test_pair_kernels(1, 4000)
+    try:
+        a.record()
+        loss, lse = spr.head_loss(h, w, t, ws)
+        b.record()
+        assert ws.device_status() == 5 and ws.device_status() == 0
+        assert bool(loss.isnan().all()) and bool(lse.isnan().all())
+        assert a.elapsed_time(b) < 50.0
+        spr.head_loss_grad(h, w, t, want[1], gl, ws)
+        assert ws.device_status() == 5
+        none, ratio = spr.verifier_labels_head(h, w, h, w, t.clamp(min=0), [1.5], ws)
+        assert ws.device_status() == 5 and not none.any() and bool(ratio.isnan().all())
+    finally:
+        spr.lib().spr_test_pair_kernels(0, 0)
+    again = spr.head_loss(h, w, t, ws) + spr.head_loss_grad(h, w, t, want[1], gl, ws)
+    again += spr.verifier_labels_head(h, w, h, w, t.clamp(min=0), [1.5], ws)
+    assert ws.device_status() == 0
+    assert all(torch.equal(x, y) for x, y in zip(again, want + grads + labels))
+
+
 # ---------------------------------------------------------------------------- labels
 
 

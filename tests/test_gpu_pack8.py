@@ -187,6 +187,51 @@ def test_a_captured_step(spr):
     assert all(torch.equal(p, q) for p, q in zip(b + [loss], want))
 
 
+@pytest.mark.parametrize("N,d", [(5000, 768), (9000, 2048), (4000, 4096), (9, 64), (30001, 256)])
+def test_bounded_wait_runs_out_and_nothing_is_stepped(spr, N, d):
+    """No tile is ever fetched (test flag): the first wait of every CTA expires after a few thousand polls, the
+    launch ends by itself, reports SPR_ERR_TIMEOUT and takes no step; the next call is a normal step."""
+    S, y = teacher_problem(N, d, torch.bfloat16, seed=21)
+    packed, yg, ws = spr.hidden_pack8(S.cuda()), y.cuda(), step_ws(spr, d)
+    g = torch.Generator().manual_seed(22)
+    state = [(0.05 * torch.randn(d + 1, generator=g)).cuda(), torch.rand(d + 1, generator=g).cuda() * 1e-3,
+             torch.rand(d + 1, generator=g).cuda() * 1e-6]
+    before, want = [x.clone() for x in state], [x.clone() for x in state]
+    loss_ok = spr.verifier_train_step8(packed, d, yg, *want, 3, 0.01, ws).clone()
+    assert ws.device_status() == 0
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    loss = spr.verifier_train_step8(packed, d, yg, *state, 3, 0.01, ws, test_flags=1, spin_limit=4000)
+    b.record()
+    assert ws.device_status() == 5 and ws.device_status() == 0
+    assert bool(loss.isnan().all()) and all(torch.equal(x, r) for x, r in zip(state, before))
+    assert a.elapsed_time(b) < 50.0
+    loss = spr.verifier_train_step8(packed, d, yg, *state, 3, 0.01, ws)
+    assert ws.device_status() == 0
+    assert torch.equal(loss, loss_ok) and all(torch.equal(x, w) for x, w in zip(state, want))
+
+
+def test_weights_of_very_different_size_in_one_vector(spr):
+    """Sixteen weights share a unit: the small ones beside a large one are held to 2^-23 of the large one, so a
+    logit is off by at most sum_j |s_j| 2^-23 max|w| beside its fp32 roundings."""
+    N, d = 64, 64
+    g = torch.Generator().manual_seed(2)
+    S = torch.randn((N, d), generator=g).to(torch.bfloat16)
+    packed = spr.hidden_pack8(S.cuda())
+    Sn = unpack_ref(packed.cpu().numpy(), d)
+    theta = torch.randn(d + 1, generator=g) * torch.logspace(-6, 1, d + 1)[torch.randperm(d + 1, generator=g)]
+    theta[5], theta[20] = 0.0, 1e-30
+    th = theta.double().numpy()
+    z = Sn @ th[:d] + th[d]
+    y = (z > 0).astype(np.uint8)
+    st = [theta.cuda(), torch.zeros(d + 1, device="cuda"), torch.zeros(d + 1, device="cuda")]
+    loss = float(spr.verifier_train_step8(packed, d, torch.from_numpy(y).cuda(), *st, 1, 0.01, step_ws(spr, d)))
+    want, _ = training.bce_loss_and_grad(Sn, y, th)
+    top = np.abs(th[:d]).reshape(-1, 16).max(1).repeat(16)
+    off = np.mean(np.abs(Sn) @ top) * 2.0 ** -23 + 2.0 ** -24 * 24 * np.mean(np.abs(Sn) @ np.abs(th[:d]) + abs(th[d]))
+    assert abs(loss - want) <= off + 2.0 ** -22 * want
+
+
 def test_widths_that_are_refused(spr):
     for d in (8, 40, 4112, 8192):
         packed = torch.zeros((4, spr.pack8_pitch(d)), dtype=torch.uint8, device="cuda")
