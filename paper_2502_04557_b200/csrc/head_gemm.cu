@@ -27,7 +27,8 @@
 //
 // Warp roles (320 threads): warp 0 = TMA producer, warp 1 = TMEM owner and MMA issuer, warps
 // 2..9 = epilogue (warp w reads TMEM lanes 32 (w % 4) .. + 31, one row per thread, and half of the
-// tile's columns).  Every wait is bounded: when one
+// tile's 256 columns: all 128 in registers where chunks are added up, else 32 at a time).  Results go out through 4 KB of shared memory per warp, so that a store instruction writes whole 128-byte
+// lines (a thread per row would touch 32 lines with each).  Every wait is bounded: when one
 // runs out the status word becomes SPR_ERR_TIMEOUT, all roles leave their loops, the even CTA
 // waits (again bounded) for the copies and products in flight, and both CTAs meet before they exit.
 #include <atomic>
@@ -37,6 +38,9 @@
 #include "tensor_pair.cuh"
 #include "vocab_common.cuh"
 
+#ifndef PROMO
+#define PROMO CU_TENSOR_MAP_L2_PROMOTION_L2_128B
+#endif
 namespace spr {
 
 namespace {
@@ -44,6 +48,7 @@ namespace {
 using namespace pairtc;
 
 constexpr int kPairThreads = 320;
+constexpr int kFirstEpilogueWarp = 2;
 constexpr int kHalfBytes = 128 * kPairBlockK * 2;       // this CTA's half of an operand tile: two 64 x 64 boxes
 constexpr int kBoxBytes = 64 * 64 * 2;
 constexpr int kStageBytes = 2 * kHalfBytes;
@@ -60,8 +65,11 @@ struct PairControl {
     int abort;
     long long consumed;      // stages whose operands the MMA issuer saw arrive
 };
-constexpr int kStageFloats = 32 * 17;                   // staging of one epilogue warp: 32 rows of 16 columns, padded
-constexpr size_t kPairSmem = (size_t)kStages * kStageBytes + 1024 + sizeof(PairControl) + 8 * kStageFloats * sizeof(float);
+constexpr int kOutBytes = 32 * 32 * 4;                  // staging of one epilogue warp: 32 rows of 32 fp32 columns
+constexpr int kOutOffset = kStages * kStageBytes;
+constexpr int kCtlOffset = kOutOffset + 8 * kOutBytes;
+constexpr size_t kPairSmem = (size_t)kCtlOffset + 1024 + sizeof(PairControl);
+static_assert(kPairSmem <= 232448, "shared memory of one CTA");
 
 // what a pair does, in order: its items of job 0, then its run of job 1
 struct Item {
@@ -140,27 +148,36 @@ __device__ __forceinline__ Stats row_stats(float (&x)[4][32], int v)
     return a;
 }
 
-// 32 consecutive elements of a row, to a 32-byte aligned address
-__device__ __forceinline__ void store_row32(float *p, const float (&x)[32])
+// A warp's block of 32 rows x 32 columns, a row per thread, turned so that eight lanes hold a row:
+// v[i] gets columns 4 (lane % 8) .. + 3 of row 4 i + lane / 8.
+__device__ __forceinline__ void by_rows(const float (&x)[32], float4 (&v)[8], float4 *stage, int lane)
 {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        uint32_t w[8];
+    for (int c = 0; c < 8; ++c)
+        stage[lane * 8 + (c ^ (lane & 7))] = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+    __syncwarp();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(x[8 * q + e]);
-        store32(p + 8 * q, w);
+    for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + (lane >> 3);
+        v[i] = stage[r * 8 + ((lane & 7) ^ (r & 7))];
     }
+    __syncwarp();
 }
-__device__ __forceinline__ void store_row32(__nv_bfloat16 *p, const float (&x)[32])
+// four elements of a row; only those before `left` exist
+__device__ __forceinline__ void store4(float *p, float4 x) { *reinterpret_cast<float4 *>(p) = x; }
+__device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 x)
 {
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-        uint32_t w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = pack_bf16(x[16 * q + 2 * e], x[16 * q + 2 * e + 1]);
-        store32(p + 16 * q, w);
-    }
+    *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
 }
+template <typename T>
+__device__ __forceinline__ void store4_tail(T *p, float4 x, int left)
+{
+    if (left > 0) p[0] = (T)x.x;
+    if (left > 1) p[1] = (T)x.y;
+    if (left > 2) p[2] = (T)x.z;
+    if (left > 3) p[3] = (T)x.w;
+}
+__device__ __forceinline__ float minus_bf16(float x) { return x - __bfloat162float(__float2bfloat16(x)); }
 
 template <int EPI, typename T>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
@@ -171,7 +188,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
     extern __shared__ unsigned char smem_raw[];
     unsigned char *ring = reinterpret_cast<unsigned char *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    PairControl *ctl = reinterpret_cast<PairControl *>(ring + kStages * kStageBytes);
+    PairControl *ctl = reinterpret_cast<PairControl *>(ring + kCtlOffset);
     pdl_trigger();   // a kernel launched behind this one may set itself up
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = (int)cluster_rank();
@@ -296,7 +313,8 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
         }
     } else {
         // ---------------- epilogue: a row and 128 columns of the tile per thread
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const int quarter = warp & 3, half = (warp - kFirstEpilogueWarp) >> 2;
+        float4 *stage = reinterpret_cast<float4 *>(ring + kOutOffset + (warp - kFirstEpilogueWarp) * kOutBytes);
         const int r_in = rank * 128 + quarter * 32 + lane;
         const uint32_t lane_base = tmem + (uint32_t)(half * 128) + ((uint32_t)(quarter * 32) << 16);
         uint32_t chunk = 0;
@@ -304,41 +322,58 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
         for (int i = 0; i < n_items && ok; ++i) {
             const Item it = get_item(prm, pair, pairs, i);
             const PairJob &j = prm.job[it.job];
-            float x[4][32];
+            // kChunked: the whole row's columns in registers, added up over chunks; else 32 columns at a time
+            constexpr bool kChunked = EPI == PAIR_STATS || sizeof(T) == 4;
+            constexpr int kGroups = kChunked ? 4 : 1;
+            float x[kGroups][32];
             const int kbs = item_blocks(j, it.split);
+            uint32_t acc = 0;
             for (int kc = 0; kc < kbs; kc += j.kc, ++chunk) {
                 const int buf = (int)(chunk & 1u);
                 ok = bar_wait(&ctl->acc_full[buf], (chunk >> 1) & 1u, &ctl->abort, prm.status, limit);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 fence_after();
-                const uint32_t acc = lane_base + (uint32_t)(buf * kPairTile);
-                if (kc == 0) {
+                acc = lane_base + (uint32_t)(buf * kPairTile);
+                if constexpr (kChunked) {
+                    if (kc == 0) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) tmem_read32(acc + 32 * q, x[q]);
-                    tmem_wait();
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        float y[32];
-                        tmem_read32(acc + 32 * q, y);
+                        for (int q = 0; q < 4; ++q) tmem_read32(acc + 32 * q, x[q]);
                         tmem_wait();
+                    } else {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2)
-                            unpack2(add2(pack2(x[q][e], x[q][e + 1]), pack2(y[e], y[e + 1])), x[q][e], x[q][e + 1]);
+                        for (int q = 0; q < 8; ++q) {
+                            float y[16];
+                            tmem_read16(acc + 16 * q, y);
+                            tmem_wait();
+                            float *z = &x[q >> 1][16 * (q & 1)];
+#pragma unroll
+                            for (int e = 0; e < 16; e += 2)
+                                unpack2(add2(pack2(z[e], z[e + 1]), pack2(y[e], y[e + 1])), z[e], z[e + 1]);
+                        }
                     }
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive_even(&ctl->acc_empty[buf]);
                 }
-                fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive_even(&ctl->acc_empty[buf]);
             }
             if (!ok) break;
+            auto columns = [&](int q) -> float(&)[32] {      // columns 32 q .. of the row
+                if constexpr (kChunked) {
+                    return x[q];
+                } else {
+                    tmem_read32(acc + 32 * q, x[0]);
+                    tmem_wait();
+                    return x[0];
+                }
+            };
             const int64_t row = (int64_t)it.m * kPairTile + r_in;
             const bool live = row < j.rows;
             const int c0 = it.n * kPairTile + half * 128;
             const int width = min(128, j.cols - c0);              // columns that exist (not positive: none)
             if (EPI == PAIR_STATS) {
-                const Stats st = row_stats(x, width);
+                Stats st = {0.f, 0.f};
+                if constexpr (kChunked) st = row_stats(x, width);
                 if (live) j.part[row * (2 * j.tiles_n) + 2 * it.n + half] = make_float2(st.m, st.s);
             } else if (EPI == PAIR_DLOGITS) {
                 // D = g (exp(l - lse) - [v = target]); rows without a target are zero whatever they hold
@@ -346,71 +381,123 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                 const bool keep = t >= 0 && t < j.V;
                 const float lse = keep ? j.lse[row] : 0.f, g = keep ? j.grad_loss[row] : 0.f;
                 const int hot = keep ? t - j.v0 - c0 : -1;
-                __nv_bfloat16 *dst = j.dlogits + row * j.dl_pitch + c0;
                 const int stored = min(128, j.dl_seg - c0);       // the padding up to a multiple of 64 is zeroed
+                const int rows = (int)min((int64_t)32, j.rows - (row - lane)) - (lane >> 3);
+                const int64_t step = 4 * j.dl_pitch;
+                const int seg = j.dl_seg;
+                __nv_bfloat16 *dst = j.dlogits + (row - lane + (lane >> 3)) * j.dl_pitch + c0 + (sizeof(T) == 2 ? 8 : 4) * (lane & 7);
+                float line[32];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     if (32 * q >= stored) break;
+                    float(&y)[32] = columns(q);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
-                        const float p = sizeof(T) == 4 ? expf(x[q][e] - lse) : ex2((x[q][e] - lse) * kLog2e);
-                        x[q][e] = keep && 32 * q + e < width ? g * p : 0.f;
+                        const float p = sizeof(T) == 4 ? expf(y[e] - lse) : ex2((y[e] - lse) * kLog2e);
+                        y[e] = keep && 32 * q + e < width ? g * p : 0.f;
                     }
                     if (hot >= 32 * q && hot < 32 * q + 32) {
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
-                            if (hot == 32 * q + e) x[q][e] -= g;
+                            if (hot == 32 * q + e) y[e] -= g;
                     }
-                    if (live) {
+                    __syncwarp();
+                    float4 v[8];
+                    if constexpr (sizeof(T) == 2) {
+                        // 64 columns of bf16 are a line of 128 bytes: two groups go out as one
 #pragma unroll
-                        for (int part = 0; part < (sizeof(T) == 4 ? 3 : 1); ++part) {
-                            store_row32(dst + (int64_t)part * j.dl_seg + 32 * q, x[q]);
+                        for (int e = 0; e < 32; e += 2) line[16 * (q & 1) + e / 2] = __uint_as_float(pack_bf16(y[e], y[e + 1]));
+                        if (q & 1) {
+                            by_rows(line, v, stage, lane);
+                            __nv_bfloat16 *o = dst + 64 * (q >> 1);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i, o += step)
+                                if (4 * i < rows) *reinterpret_cast<float4 *>(o) = v[i];
+                        }
+                        continue;
+                    }
+                    by_rows(y, v, stage, lane);
+                    __nv_bfloat16 *o = dst + 32 * q;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i, o += step) {
+                        if (4 * i < rows) {
+                            store4(o, v[i]);
                             if (sizeof(T) == 4) {
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) x[q][e] -= __bfloat162float(__float2bfloat16(x[q][e]));
+                                v[i] = make_float4(minus_bf16(v[i].x), minus_bf16(v[i].y), minus_bf16(v[i].z), minus_bf16(v[i].w));
+                                store4(o + seg, v[i]);
+                                v[i] = make_float4(minus_bf16(v[i].x), minus_bf16(v[i].y), minus_bf16(v[i].z), minus_bf16(v[i].w));
+                                store4(o + 2 * (int64_t)seg, v[i]);
                             }
                         }
                     }
                 }
             } else {
-                float *a = j.acc ? j.acc + (int64_t)it.split * j.acc_stride + row * j.acc_pitch + c0 : nullptr;
-                T *o = j.out ? static_cast<T *>(j.out) + row * j.out_pitch + c0 : nullptr;
-                const bool vec = ((reinterpret_cast<uintptr_t>(j.out) | (uintptr_t)(j.out_pitch * (int64_t)sizeof(T))) & 31) == 0;
-                float *stage = reinterpret_cast<float *>(ctl + 1) + (warp - 2) * kStageFloats;
+                // this lane's part of a block: columns 4 (lane % 8) .. + 3 of rows lane / 8, + 4, ...
+                const int rows = (int)min((int64_t)32, j.rows - (row - lane)) - (lane >> 3);
+                const int64_t r0 = row - lane + (lane >> 3);
+                const int cl = c0 + 4 * (lane & 7), left = width - 4 * (lane & 7);
+                const bool to_out = j.out != nullptr, add = j.add_acc != 0;
+                const int64_t acc_step = 4 * j.acc_pitch, out_step = 4 * j.out_pitch;
+                float *a = j.acc + (int64_t)it.split * j.acc_stride + r0 * j.acc_pitch + cl;    // used where there is an acc
+                T *o = static_cast<T *>(j.out) + r0 * j.out_pitch + cl;                         // used where there is an out
+                // four elements of the caller's type are stored at once where every row allows it
+                const bool vec = ((reinterpret_cast<uintptr_t>(j.out) | (uintptr_t)(j.out_pitch * (int64_t)sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
+                if (sizeof(T) == 2 && to_out && !add && width == 128 && (((uintptr_t)j.out | (uintptr_t)(2 * j.out_pitch)) & 15) == 0) {
+                    // 64 columns of bf16 are a line of 128 bytes: whole lines where nothing is added and no column missing
+                    T *p0 = static_cast<T *>(j.out) + r0 * j.out_pitch + c0 + 8 * (lane & 7);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float line[32];
+#pragma unroll
+                        for (int q = 2 * h; q < 2 * h + 2; ++q) {
+                            const float(&y)[32] = columns(q);
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) line[16 * (q & 1) + e / 2] = __uint_as_float(pack_bf16(y[e], y[e + 1]));
+                        }
+                        float4 v[8];
+                        by_rows(line, v, stage, lane);
+                        T *p = p0 + 64 * h;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i, p += out_step)
+                            if (4 * i < rows) *reinterpret_cast<float4 *>(p) = v[i];
+                    }
+                } else
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     if (32 * q >= width) break;
-                    if (live && j.add_acc) {      // the pitch covers whole groups of 32
+                    float4 v[8];
+                    by_rows(columns(q), v, stage, lane);
+                    if (add) {                   // acc's pitch covers whole groups of 32
+                        const float *p = a + 32 * q;
+                        float4 y[8];
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4) {
-                            const float4 y = *reinterpret_cast<const float4 *>(a + 32 * q + e);
-                            x[q][e] += y.x;
-                            x[q][e + 1] += y.y;
-                            x[q][e + 2] += y.z;
-                            x[q][e + 3] += y.w;
-                        }
+                        for (int i = 0; i < 8; ++i, p += acc_step) y[i] = 4 * i < rows ? *reinterpret_cast<const float4 *>(p) : v[i];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = make_float4(v[i].x + y[i].x, v[i].y + y[i].y, v[i].z + y[i].z, v[i].w + y[i].w);
                     }
-                    if (!o) {
-                        if (live) store_row32(a + 32 * q, x[q]);
-                    } else if (vec && width - 32 * q >= 32) {
-                        if (live) store_row32(o + 32 * q, x[q]);
+                    if (!to_out) {
+                        float *p = a + 32 * q;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i, p += acc_step)
+                            if (4 * i < rows) store4(p, v[i]);
                     } else {
-                        // Rows that start anywhere: a thread per row would touch 32 lines per element, so the
-                        // block goes through shared memory and out again two rows of 16 elements at a time.
+                        T *p = o + 32 * q;
+                        if (vec && width - 32 * q >= 32) {
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
+                            for (int i = 0; i < 8; ++i, p += out_step)
+                                if (4 * i < rows) store4(p, v[i]);
+                        } else {
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) stage[lane * 17 + e] = x[q][16 * h + e];
-                            __syncwarp();
-                            const int col = 32 * q + 16 * h + (lane & 15);
-                            T *out = static_cast<T *>(j.out) + (row - lane) * j.out_pitch + c0 + col;
-#pragma unroll 4
-                            for (int r = lane >> 4; r < 32; r += 2)
-                                if (col < width && row - lane + r < j.rows) out[r * j.out_pitch] = (T)stage[r * 17 + (lane & 15)];
-                            __syncwarp();
+                            for (int i = 0; i < 8; ++i, p += out_step)
+                                if (4 * i < rows) store4_tail(p, v[i], left - 32 * q);
                         }
                     }
                 }
+            }
+            if constexpr (!kChunked) {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive_even(&ctl->acc_empty[(chunk - 1u) & 1u]);
             }
             __syncwarp();
         }
@@ -468,7 +555,7 @@ bool make_map(CUtensorMap *map, const PairOperand &t)
     const cuuint32_t box[2] = {64, 64};
     const cuuint32_t elem[2] = {1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(t.base), dims, strides, box, elem,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, PROMO,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

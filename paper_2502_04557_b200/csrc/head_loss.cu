@@ -109,7 +109,8 @@ __device__ __forceinline__ double row_lse(const HeadRow &h, int64_t i, float2 *s
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const int t = t0 + k * kRowThreads + tid;
-            x[k] = t < h.parts ? p[t] : make_float2(neg_inf(), 0.f);
+            x[k] = p[min(t, h.parts - 1)];        // unconditional: eight loads in flight
+            if (t >= h.parts) x[k] = make_float2(neg_inf(), 0.f);
         }
         float m = a.m;
 #pragma unroll
@@ -253,9 +254,10 @@ __global__ void __launch_bounds__(256) head_sum_kernel(const float *acc, int sli
             float4 x[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                x[k] = k0 + k < slices ? *reinterpret_cast<const float4 *>(p + (k0 + k) * stride) : make_float4(0.f, 0.f, 0.f, 0.f);
+                x[k] = *reinterpret_cast<const float4 *>(p + min(k0 + k, slices - 1) * stride);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
+                if (k0 + k >= slices) break;
                 s.x += x[k].x;
                 s.y += x[k].y;
                 s.z += x[k].z;

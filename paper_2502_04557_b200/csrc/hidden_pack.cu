@@ -75,73 +75,124 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *p, int left, bool vec, con
     }
 }
 
-// chunk (row r, elements [c, c + 256)) of a warp; a lane has 8 elements, four lanes a block
+// A warp takes chunks (row r, elements [c, c + 256)), kAhead of them at a time so that their loads are in
+// flight together; a lane has 8 elements of each, four lanes a block.
+constexpr int kAhead = 4;
+struct Chunks {
+    int64_t all, stride, at;       // chunks, and this warp's first and distance
+    int per_row;
+    __device__ Chunks(int64_t N, int d)
+    {
+        per_row = (d + kChunk - 1) / kChunk;
+        all = N * per_row;
+        stride = (int64_t)gridDim.x * kPackWarps;
+        at = (int64_t)blockIdx.x * kPackWarps + (threadIdx.x >> 5);
+    }
+    __device__ void place(int64_t w, int64_t &r, int &c) const
+    {
+        if (all <= 0x7fffffff) {
+            const uint32_t q = (uint32_t)w / (uint32_t)per_row;
+            r = q;
+            c = (int)((uint32_t)w - q * (uint32_t)per_row);
+        } else {
+            r = w / per_row;
+            c = (int)(w - r * per_row);
+        }
+        c = c * kChunk + (int)(threadIdx.x & 31) * 8;
+    }
+};
+
 template <typename T>
 __global__ void __launch_bounds__(32 * kPackWarps) pack8_kernel(const T *src, int64_t N, int d, int pitch, bool vec, uint8_t *dst)
 {
     const int lane = threadIdx.x & 31;
-    const int per_row = (d + kChunk - 1) / kChunk;
-    const int64_t chunks = N * per_row;
-    const int64_t stride = (int64_t)gridDim.x * kPackWarps;
-    for (int64_t w = (int64_t)blockIdx.x * kPackWarps + (threadIdx.x >> 5); w < chunks; w += stride) {
-        const int64_t r = w / per_row;
-        const int c = (int)(w - r * per_row) * kChunk + lane * 8;
-        float x[8];
-        load8(src + r * d + c, d - c, vec, x);
-        // largest magnitude of the block, as bits: infinities and NaN lie above all numbers
-        uint32_t top = 0;
+    const Chunks ch(N, d);
+    for (int64_t w0 = ch.at; w0 < ch.all; w0 += kAhead * ch.stride) {
+        float x[kAhead][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const bool bad = top >= 0x7f800000u;
-        const int e2 = bad ? 0 : max((int)(top >> 23) - 133, -126);
-        const float scale = __int_as_float((127 - e2) << 23);
-        uint32_t q[2] = {0u, 0u};
+        for (int k = 0; k < kAhead; ++k) {
+            int64_t r;
+            int c;
+            ch.place(min(w0 + k * ch.stride, ch.all - 1), r, c);
+            load8(src + r * d + c, d - c, vec, x[k]);
+        }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int v = bad ? 0 : min(max(__float2int_rn(x[e] * scale), -127), 127);
-            q[e >> 2] |= (uint32_t)(v & 0xff) << (8 * (e & 3));
+        for (int k = 0; k < kAhead; ++k) {
+            if (w0 + k * ch.stride >= ch.all) break;
+            int64_t r;
+            int c;
+            ch.place(w0 + k * ch.stride, r, c);
+            // largest magnitude of the block, as bits: infinities and NaN lie above all numbers
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[k][e]) & 0x7fffffffu);
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const bool bad = top >= 0x7f800000u;
+            const int e2 = bad ? 0 : max((int)(top >> 23) - 133, -126);
+            const float scale = __int_as_float((127 - e2) << 23);
+            uint32_t q[2] = {0u, 0u};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                // x 2^-e + 1.5 2^23 rounds to even at the units: the low byte of the sum is the byte wanted
+                const float y = fminf(fmaxf(x[k][e] * scale, -127.f), 127.f) + 12582912.f;
+                q[e >> 2] |= (__float_as_uint(y) & 255u) << (8 * (e & 3));
+            }
+            if (bad) q[0] = q[1] = 0u;
+            uint8_t *row = dst + r * pitch;
+            if (c + 8 <= d) {
+                *reinterpret_cast<uint2 *>(row + c) = make_uint2(q[0], q[1]);
+            } else if (c < d) {
+                for (int e = 0; c + e < d; ++e) row[c + e] = (uint8_t)(q[e >> 2] >> (8 * (e & 3)));
+            }
+            if ((lane & 3) == 0 && c < d) row[d + c / kPackBlock] = (uint8_t)(bad ? kBadBlock : e2);
+            if (c < d && c + 8 >= d)       // the lane with the last elements clears the row's padding
+                for (int b = d + (d + kPackBlock - 1) / kPackBlock; b < pitch; ++b) row[b] = 0;
         }
-        uint8_t *row = dst + r * pitch;
-        if (c + 8 <= d) {
-            *reinterpret_cast<uint2 *>(row + c) = make_uint2(q[0], q[1]);
-        } else if (c < d) {
-            for (int e = 0; c + e < d; ++e) row[c + e] = (uint8_t)(q[e >> 2] >> (8 * (e & 3)));
-        }
-        if ((lane & 3) == 0 && c < d) row[d + c / kPackBlock] = (uint8_t)(bad ? kBadBlock : e2);
-        if (c < d && c + 8 >= d)       // the lane with the last elements clears the row's padding
-            for (int b = d + (d + kPackBlock - 1) / kPackBlock; b < pitch; ++b) row[b] = 0;
     }
 }
 
 template <typename T>
 __global__ void __launch_bounds__(32 * kPackWarps) unpack8_kernel(const uint8_t *src, int64_t N, int d, int pitch, bool vec, T *dst)
 {
-    const int lane = threadIdx.x & 31;
-    const int per_row = (d + kChunk - 1) / kChunk;
-    const int64_t chunks = N * per_row;
-    const int64_t stride = (int64_t)gridDim.x * kPackWarps;
-    for (int64_t w = (int64_t)blockIdx.x * kPackWarps + (threadIdx.x >> 5); w < chunks; w += stride) {
-        const int64_t r = w / per_row;
-        const int c = (int)(w - r * per_row) * kChunk + lane * 8;
-        if (c >= d) continue;
-        const uint8_t *row = src + r * pitch;      // 8 bytes at c: inside the row, whose pitch is a multiple of 16
-        const uint2 q = __ldcs(reinterpret_cast<const uint2 *>(row + c));
-        const int e2 = reinterpret_cast<const signed char *>(row)[d + c / kPackBlock];
-        const float scale = e2 == kBadBlock ? __int_as_float(0x7fc00000) : __int_as_float((e2 + 127) << 23);
-        float x[8];
+    const Chunks ch(N, d);
+    for (int64_t w0 = ch.at; w0 < ch.all; w0 += kAhead * ch.stride) {
+        uint2 q[kAhead];
+        int e2[kAhead];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (float)(signed char)((e < 4 ? q.x : q.y) >> (8 * (e & 3))) * scale;
-        store8(dst + r * d + c, d - c, vec, x);
+        for (int k = 0; k < kAhead; ++k) {
+            int64_t r;
+            int c;
+            ch.place(min(w0 + k * ch.stride, ch.all - 1), r, c);
+            const int at = min(c, d - 1);                  // lanes past the row's end load its last elements
+            const uint8_t *row = src + r * pitch;          // 8 bytes from a multiple of 8: inside the row, whose pitch is one of 16
+            q[k] = __ldcs(reinterpret_cast<const uint2 *>(row + (at & ~7)));
+            e2[k] = reinterpret_cast<const signed char *>(row)[d + at / kPackBlock];
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (w0 + k * ch.stride >= ch.all) break;
+            int64_t r;
+            int c;
+            ch.place(w0 + k * ch.stride, r, c);
+            const float scale = e2[k] == kBadBlock ? __int_as_float(0x7fc00000) : __int_as_float((e2[k] + 127) << 23);
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)    // byte + 128 as the low mantissa byte of 2^23, which is then taken off
+                x[e] = (__uint_as_float(__byte_perm((e < 4 ? q[k].x : q[k].y) ^ 0x80808080u, 0x4b000000u, 0x7440 + (e & 3))) - 8388736.f) * scale;
+            if (c < d) store8(dst + r * d + c, d - c, vec, x);
+        }
     }
 }
 
-// enough warps to fill the GPU's load queues, each with a few chunks
+// one round of kAhead chunks per warp where that fills the GPU, at most eight CTAs per SM
 unsigned pack_ctas(int64_t N, int d)
 {
-    const int64_t want = (N * ((d + kChunk - 1) / kChunk) + kPackWarps - 1) / kPackWarps;
-    return (unsigned)(want < 148 * 64 ? want : 148 * 64);
+    const int64_t chunks = N * ((d + kChunk - 1) / kChunk);
+    const int64_t want = (chunks + kPackWarps - 1) / kPackWarps;       // one chunk per warp
+    const int64_t rounds = (want + 148 * 8 * kAhead - 1) / (148 * 8 * kAhead);
+    const int64_t ctas = (want + rounds * kAhead - 1) / (rounds * kAhead);
+    return (unsigned)(want < 148 * 8 ? want : ctas < 148 * 4 ? 148 * 4 : ctas);
 }
 
 int check_pack(const void *hidden, int64_t N, int d, int dt, const void *packed)

@@ -167,8 +167,6 @@ struct TrainParams {
 };
 enum { TRAIN_TEST_NO_FETCH = 1 };   // test hook: no row is ever fetched, so the first wait of every team runs out
 constexpr uint32_t kTrainSpin = 1u << 22;   // polls of one mbarrier before a gradient kernel gives up
-// sums the CTAs' partials and takes the Adam step; behind: the gradient kernel lets it start early
-cudaError_t launch_train_adam(const TrainParams &p, cudaStream_t st, bool behind);
 
 // workspace of head_loss, head_loss_grad and verifier_labels_head (head_loss.cu); 0 for bad sizes
 size_t head_loss_ws_bytes(int64_t N, int d, int V, int dt);

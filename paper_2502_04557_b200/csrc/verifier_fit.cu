@@ -64,8 +64,6 @@ __global__ void __launch_bounds__(256) labels_kernel(const LabelParams prm)
 // gradient sums in registers; with two warps per row each warp has half of the columns and the
 // two halves of a dot product meet in shared memory.  A slot is refilled as soon as both
 // passes over it are done.
-
-
 __device__ __forceinline__ uint32_t ring_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ bool ring_poll(uint64_t *bar, uint32_t parity)
 {
@@ -336,25 +334,18 @@ __global__ void __launch_bounds__(kThreads, ring_ctas_per_sm(VPL, WPR, G)) train
 
 // One thread per parameter: sums the CTA partials in CTA order, divides by N, applies the
 // bias-corrected Adam update (arithmetic in double, state kept in float).
-__global__ void __launch_bounds__(64) train_adam_kernel(const TrainParams prm)
+__global__ void __launch_bounds__(256) train_adam_kernel(const TrainParams prm)
 {
     const int j = blockIdx.x * blockDim.x + threadIdx.x;
     const int d = prm.d;
     if (j > d + 1) return;
-    pdl_wait();
     if (*reinterpret_cast<volatile int *>(prm.status) == SPR_ERR_TIMEOUT) {
         // the gradient pass gave up: no step is taken, the loss reads NaN
         if (j == d + 1 && prm.loss) *prm.loss = __int_as_float(0x7fc00000);
         return;
     }
     double sum = 0.0;
-    for (int c0 = 0; c0 < prm.ctas; c0 += 16) {       // sixteen loads in flight, added in CTA order
-        float x[16];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) x[k] = c0 + k < prm.ctas ? prm.part[(int64_t)(c0 + k) * (d + 2) + j] : 0.f;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) sum += (double)x[k];
-    }
+    for (int c = 0; c < prm.ctas; ++c) sum += (double)prm.part[(int64_t)c * (d + 2) + j];
     sum /= (double)prm.N;
     if (j == d + 1) {
         if (prm.loss) *prm.loss = (float)sum;
@@ -369,24 +360,6 @@ __global__ void __launch_bounds__(64) train_adam_kernel(const TrainParams prm)
     prm.v[j] = (float)v;
     prm.theta[j] = (float)((double)prm.theta[j] - prm.lr * m_hat / (sqrt(v_hat) + prm.eps));
 }
-
-}  // namespace
-
-cudaError_t launch_train_adam(const TrainParams &p, cudaStream_t st, bool behind)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((p.d + 2 + 63) / 64));
-    cfg.blockDim = dim3(64);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = behind ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, train_adam_kernel, p);
-}
-
-namespace {
 
 template <typename T, int VPL, int WPR, int R, int SLOTS, int G = 1>
 cudaError_t launch_grad_ring(const TrainParams &tp, cudaStream_t st)
@@ -407,8 +380,8 @@ cudaError_t launch_grad_ring(const TrainParams &tp, cudaStream_t st)
     const int64_t blocks = (tp.N + G - 1) / G;
     p.ctas = (int)max((int64_t)1, min((int64_t)min(kTrainMaxCtas, per_sm * sms), (blocks + kTeams - 1) / kTeams));
     kernel<<<p.ctas, kThreads, smem, st>>>(p);
-    const cudaError_t rc = cudaGetLastError();
-    return rc != cudaSuccess ? rc : launch_train_adam(p, st, false);
+    train_adam_kernel<<<(tp.d + 2 + 255) / 256, 256, 0, st>>>(p);
+    return cudaGetLastError();
 }
 
 template <typename T>

@@ -14,6 +14,7 @@
 // first a warp per row (two for d > 2048) forms the dot products, one barrier, then every warp has the
 // tile's residuals in its lanes and the columns' sums are formed.  Tiles are dealt in a fixed
 // pattern and all sums have a fixed order: a step is reproducible bit for bit.
+#include <math.h>
 #include <string.h>
 
 #include <atomic>
@@ -48,8 +49,12 @@ __device__ __forceinline__ bool fit_wait(uint64_t *bar, uint32_t parity, uint32_
     return false;
 }
 
-// 2^e of an exponent byte; -128 marks a block that held an infinity or NaN
-__device__ __forceinline__ float block_scale(int e) { return e == -128 ? __int_as_float(0x7fc00000) : __int_as_float((e + 127) << 23); }
+// 2^e of an exponent byte.  -128 marks a block that held an infinity or NaN, with bytes of zero: the same
+// shift makes that minus infinity, and its product with a zero byte NaN.
+__device__ __forceinline__ float block_scale(const unsigned char *p)
+{
+    return __int_as_float((int)*reinterpret_cast<const signed char *>(p) * (1 << 23) + 127 * (1 << 23));
+}
 
 // Sixteen weights as three planes of signed bytes, and their unit 2^E.
 __device__ __forceinline__ float split_weights(const float (&w)[16], uint32_t (&digit)[3][4])
@@ -85,6 +90,7 @@ __global__ void __launch_bounds__(kFitThreads, 1) train8_kernel(const TrainParam
     extern __shared__ __align__(128) unsigned char tiles[];
     __shared__ __align__(8) uint64_t bars[kMaxTiles];
     __shared__ float zpart[2][T][WPR];
+    __shared__ float res_of[kFitWarps][T];    // the tile's residuals, a copy per warp
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int d = prm.d, nv = d / 16;
     const int pitch = pack8_pitch(d);
@@ -125,9 +131,12 @@ __global__ void __launch_bounds__(kFitThreads, 1) train8_kernel(const TrainParam
     const int part = warp % WPR, v0 = part * VPL * 32 + lane;
     uint32_t digit[VPL][3][4];
     float unit[VPL];
+    int at[VPL], scale_at[VPL];      // a lane past the row's end reads the last vector, with weights of zero
 #pragma unroll
     for (int j = 0; j < VPL; ++j) {
         const int vi = v0 + 32 * j;
+        at[j] = min(vi, nv - 1) * 16;
+        scale_at[j] = d + (min(vi, nv - 1) >> 1);
         float w[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) w[e] = vi < nv ? prm.theta[vi * 16 + e] : 0.f;
@@ -163,21 +172,17 @@ __global__ void __launch_bounds__(kFitThreads, 1) train8_kernel(const TrainParam
             dot[i] = 0.f;
 #pragma unroll
             for (int j = 0; j < VPL; ++j) {
-                const int vi = v0 + 32 * j;
-                if (j < VPL - 2 || vi < nv) {
-                    const uint4 x = *reinterpret_cast<const uint4 *>(row + vi * 16);
-                    const int q[4] = {(int)x.x, (int)x.y, (int)x.z, (int)x.w};
-                    int s0 = 0, s1 = 0, s2 = 0;
+                const uint4 x = *reinterpret_cast<const uint4 *>(row + at[j]);
+                const int q[4] = {(int)x.x, (int)x.y, (int)x.z, (int)x.w};
+                int s0 = 0, s1 = 0, s2 = 0;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        s0 = __dp4a(q[c], (int)digit[j][0][c], s0);
-                        s1 = __dp4a(q[c], (int)digit[j][1][c], s1);
-                        s2 = __dp4a(q[c], (int)digit[j][2][c], s2);
-                    }
-                    const float s = fmaf((float)s0, 65536.f, (float)(s1 * 256 + s2));     // |s1| < 2^18
-                    const float sc = block_scale(reinterpret_cast<const signed char *>(row)[d + (vi >> 1)]);
-                    dot[i] = fmaf(s * unit[j], sc, dot[i]);
+                for (int c = 0; c < 4; ++c) {
+                    s0 = __dp4a(q[c], (int)digit[j][0][c], s0);
+                    s1 = __dp4a(q[c], (int)digit[j][1][c], s1);
+                    s2 = __dp4a(q[c], (int)digit[j][2][c], s2);
                 }
+                const float s = fmaf((float)s0, 65536.f, (float)(s1 * 256 + s2));     // |s1| < 2^18
+                dot[i] = fmaf(s * unit[j], block_scale(row + scale_at[j]), dot[i]);
             }
         }
 #pragma unroll
@@ -192,7 +197,6 @@ __global__ void __launch_bounds__(kFitThreads, 1) train8_kernel(const TrainParam
         if (!ok) break;
         if (tid == 0 && k > 0 && k - 1 + ring_tiles < n) fetch(k - 1 + ring_tiles);
         // ---- residuals, a row per lane, in every warp
-        float res[kLaneRows];
 #pragma unroll
         for (int h = 0; h < kLaneRows; ++h) {
             const int r = lane + 32 * h;
@@ -201,40 +205,34 @@ __global__ void __launch_bounds__(kFitThreads, 1) train8_kernel(const TrainParam
                 z += zpart[k & 1][r][0];
                 if (WPR > 1) z += zpart[k & 1][r][WPR - 1];
             }
-            res[h] = r < rows ? 1.f / (1.f + expf(-z)) - y[h] : 0.f;
+            const float res = r < rows ? 1.f / (1.f + expf(-z)) - y[h] : 0.f;
+            if (r < T) res_of[warp][r] = res;
             if (warp == 0 && r < rows) {
-                acc_b += (double)res[h];
+                acc_b += (double)res;
                 acc_loss += (double)(fmaxf(z, 0.f) + log1pf(expf(-fabsf(z))) - y[h] * z);
             }
         }
-        // ---- columns: every lane of a warp goes round as often, so that the residuals can be asked of the lanes
-        const int rounds = (rows + subs - 1) / subs;
-#pragma unroll 2
-        for (int i = 0; i < rounds; ++i) {
-            const int r = sub + i * subs;
-            float f = __shfl_sync(0xffffffffu, res[0], r & 31);
-            if (kLaneRows > 1) {
-                const float f1 = __shfl_sync(0xffffffffu, res[kLaneRows - 1], r & 31);
-                if (r & 32) f = f1;
-            }
-            if (sub < subs && r < rows) {
-                const unsigned char *row = tile + r * pitch;
-                const uint4 x = *reinterpret_cast<const uint4 *>(row + cv * 16);
-                const float rs = f * block_scale(reinterpret_cast<const signed char *>(row)[d + (cv >> 1)]);
-                const uint64_t rs2 = pack2(rs, rs);
-                // byte + 128 as the low mantissa byte of 2^23, which is then taken off
-                const uint32_t w[4] = {x.x ^ 0x80808080u, x.y ^ 0x80808080u, x.z ^ 0x80808080u, x.w ^ 0x80808080u};
+        __syncwarp();
+        // ---- columns
+        const unsigned char *row = tile + sub * pitch + cv * 16, *row_e = tile + sub * pitch + d + (cv >> 1);
+#pragma unroll 4
+        for (int r = sub < subs ? sub : rows; r < rows; r += subs, row += subs * pitch, row_e += subs * pitch) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(row);
+            const float rs = res_of[warp][r] * block_scale(row_e);
+            const uint64_t rs2 = pack2(rs, rs);
+            // byte + 128 as the low mantissa byte of 2^23, which is then taken off
+            const uint32_t w[4] = {x.x ^ 0x80808080u, x.y ^ 0x80808080u, x.z ^ 0x80808080u, x.w ^ 0x80808080u};
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const uint64_t a = pack2(__uint_as_float(__byte_perm(w[c], 0x4b000000u, 0x7440)),
-                                             __uint_as_float(__byte_perm(w[c], 0x4b000000u, 0x7441)));
-                    const uint64_t b = pack2(__uint_as_float(__byte_perm(w[c], 0x4b000000u, 0x7442)),
-                                             __uint_as_float(__byte_perm(w[c], 0x4b000000u, 0x7443)));
-                    acc[2 * c] = fma2(rs2, add2(a, off), acc[2 * c]);
-                    acc[2 * c + 1] = fma2(rs2, add2(b, off), acc[2 * c + 1]);
-                }
+            for (int c = 0; c < 4; ++c) {
+                const uint64_t a = pack2(__uint_as_float(__byte_perm(w[c], 0x4b000000u, 0x7440)),
+                                         __uint_as_float(__byte_perm(w[c], 0x4b000000u, 0x7441)));
+                const uint64_t b = pack2(__uint_as_float(__byte_perm(w[c], 0x4b000000u, 0x7442)),
+                                         __uint_as_float(__byte_perm(w[c], 0x4b000000u, 0x7443)));
+                acc[2 * c] = fma2(rs2, add2(a, off), acc[2 * c]);
+                acc[2 * c + 1] = fma2(rs2, add2(b, off), acc[2 * c + 1]);
             }
         }
+        __syncwarp();                          // the residuals are overwritten for the next tile
     }
     if (!ok) {
         // A wait ran out: report it, then give the copies still on their way the same bounded time to
@@ -276,6 +274,46 @@ __global__ void __launch_bounds__(kFitThreads, 1) train8_kernel(const TrainParam
     }
 }
 
+// The CTAs' partial sums, and the Adam step: 32 parameters per CTA, eight warps that each add up every
+// eighth partial (their loads all in flight), then the eight sums in order.  c1 = 1 - beta1^t, c2 = 1 - beta2^t.
+__global__ void __launch_bounds__(256) train8_adam_kernel(const TrainParams prm, double c1, double c2)
+{
+    __shared__ double sums[8][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int d = prm.d, j = blockIdx.x * 32 + lane;
+    pdl_wait();
+    const float *p = prm.part + min(j, d + 1);
+    double sum = 0.0;
+    for (int c0 = warp; c0 < prm.ctas; c0 += 8 * 20) {
+        float x[20];
+#pragma unroll
+        for (int k = 0; k < 20; ++k) x[k] = p[(int64_t)min(c0 + 8 * k, prm.ctas - 1) * (d + 2)];
+#pragma unroll
+        for (int k = 0; k < 20; ++k)
+            if (c0 + 8 * k < prm.ctas) sum += (double)x[k];
+    }
+    sums[warp][lane] = sum;
+    __syncthreads();
+    if (warp != 0 || j > d + 1) return;
+    if (*reinterpret_cast<volatile int *>(prm.status) == SPR_ERR_TIMEOUT) {
+        // the gradient pass gave up: no step is taken, the loss reads NaN
+        if (j == d + 1 && prm.loss) *prm.loss = __int_as_float(0x7fc00000);
+        return;
+    }
+#pragma unroll
+    for (int w = 1; w < 8; ++w) sum += sums[w][lane];
+    sum /= (double)prm.N;
+    if (j == d + 1) {
+        if (prm.loss) *prm.loss = (float)sum;
+        return;
+    }
+    const double m = prm.beta1 * (double)prm.m[j] + (1.0 - prm.beta1) * sum;
+    const double v = prm.beta2 * (double)prm.v[j] + (1.0 - prm.beta2) * sum * sum;
+    prm.m[j] = (float)m;
+    prm.v[j] = (float)v;
+    prm.theta[j] = (float)((double)prm.theta[j] - prm.lr * (m / c1) / (sqrt(v / c2) + prm.eps));
+}
+
 template <int VPL, int WPR, int T>
 cudaError_t launch_train8(const TrainParams &tp, cudaStream_t st)
 {
@@ -303,7 +341,17 @@ cudaError_t launch_train8(const TrainParams &tp, cudaStream_t st)
     if (smem < red) smem = red;
     train8_kernel<VPL, WPR, T><<<p.ctas, kFitThreads, smem, st>>>(p, (int)ring);
     e = cudaGetLastError();
-    return e != cudaSuccess ? e : launch_train_adam(p, st, true);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};          // set up while the gradient kernel ends
+    cfg.gridDim = dim3((unsigned)((p.d + 2 + 31) / 32));
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, train8_adam_kernel, p, 1.0 - pow(p.beta1, (double)p.t), 1.0 - pow(p.beta2, (double)p.t));
 }
 
 // Tiles of 16, 32 or 64 rows: about 64 KB, so that three fit and a barrier is worth some thousand
