@@ -75,124 +75,193 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *p, int left, bool vec, con
     }
 }
 
-// A warp takes chunks (row r, elements [c, c + 256)), kAhead of them at a time so that their loads are in
-// flight together; a lane has 8 elements of each, four lanes a block.
-constexpr int kAhead = 4;
-struct Chunks {
-    int64_t all, stride, at;       // chunks, and this warp's first and distance
-    int per_row;
-    __device__ Chunks(int64_t N, int d)
-    {
-        per_row = (d + kChunk - 1) / kChunk;
-        all = N * per_row;
-        stride = (int64_t)gridDim.x * kPackWarps;
-        at = (int64_t)blockIdx.x * kPackWarps + (threadIdx.x >> 5);
+// 8 elements of a block whose largest magnitude has the bits `top`: their bytes and the exponent byte.
+// x 2^-e is exact; with 1.5 2^23 added it is rounded to even at the units, and the low byte of the sum is
+// the byte wanted.
+__device__ __forceinline__ uint2 quantise(const float (&x)[8], uint32_t top, int &e2)
+{
+    const bool bad = top >= 0x7f800000u;
+    e2 = max((int)(top >> 23) - 133, -126);
+    const float scale = __int_as_float((127 - e2) << 23);
+    uint32_t b[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) b[e] = __float_as_uint(fmaf(x[e], scale, 12582912.f));
+    // above 127.5 2^e a byte would be 128: only a block whose largest element starts 1.1111111 1 can hold one
+    if (__any_sync(__activemask(), (top & 0x7fffffu) >= 0x7f0000u)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] = min(max(b[e], 0x4b400000u - 127u), 0x4b400000u + 127u);
     }
-    __device__ void place(int64_t w, int64_t &r, int &c) const
-    {
-        if (all <= 0x7fffffff) {
-            const uint32_t q = (uint32_t)w / (uint32_t)per_row;
-            r = q;
-            c = (int)((uint32_t)w - q * (uint32_t)per_row);
-        } else {
-            r = w / per_row;
-            c = (int)(w - r * per_row);
-        }
-        c = c * kChunk + (int)(threadIdx.x & 31) * 8;
+    uint2 q;
+    q.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+    q.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+    if (bad) {
+        q = make_uint2(0u, 0u);
+        e2 = kBadBlock;
     }
-};
+    return q;
+}
+// byte + 128 as the low mantissa byte of 2^23; (2^23 + 128 + q) 2^e - (2^23 + 128) 2^e is exact
+__device__ __forceinline__ void dequantise(uint2 q, int e2, float (&x)[8])
+{
+    const float scale = e2 == kBadBlock ? __int_as_float(0x7fc00000) : __int_as_float((e2 + 127) << 23);
+    const float off = -8388736.f * scale;
+    const uint32_t w[2] = {q.x ^ 0x80808080u, q.y ^ 0x80808080u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = fmaf(__uint_as_float(__byte_perm(w[e >> 2], 0x4b000000u, 0x7440 + (e & 3))), scale, off);
+}
 
+// ---------------------------------------------------------------- any width and alignment
+// chunk (row r, elements [c, c + 256)) of a warp; a lane has 8 elements, four lanes a block
 template <typename T>
-__global__ void __launch_bounds__(32 * kPackWarps) pack8_kernel(const T *src, int64_t N, int d, int pitch, bool vec, uint8_t *dst)
+__global__ void __launch_bounds__(32 * kPackWarps) pack8_any_kernel(const T *src, int64_t N, int d, int pitch, bool vec, uint8_t *dst)
 {
     const int lane = threadIdx.x & 31;
-    const Chunks ch(N, d);
-    for (int64_t w0 = ch.at; w0 < ch.all; w0 += kAhead * ch.stride) {
-        float x[kAhead][8];
+    const int per_row = (d + kChunk - 1) / kChunk;
+    const int64_t chunks = N * per_row, stride = (int64_t)gridDim.x * kPackWarps;
+    for (int64_t w = (int64_t)blockIdx.x * kPackWarps + (threadIdx.x >> 5); w < chunks; w += stride) {
+        const int64_t r = w / per_row;
+        const int c = (int)(w - r * per_row) * kChunk + lane * 8;
+        float x[8];
+        load8(src + r * d + c, d - c, vec, x);
+        // largest magnitude of the block, as bits: infinities and NaN lie above all numbers
+        uint32_t top = 0;
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            int64_t r;
-            int c;
-            ch.place(min(w0 + k * ch.stride, ch.all - 1), r, c);
-            load8(src + r * d + c, d - c, vec, x[k]);
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        int e2;
+        const uint2 q = quantise(x, top, e2);
+        uint8_t *row = dst + r * pitch;
+        if (c + 8 <= d) {
+            *reinterpret_cast<uint2 *>(row + c) = q;
+        } else if (c < d) {
+            for (int e = 0; c + e < d; ++e) row[c + e] = (uint8_t)((e < 4 ? q.x : q.y) >> (8 * (e & 3)));
         }
+        if ((lane & 3) == 0 && c < d) row[d + c / kPackBlock] = (uint8_t)e2;
+        if (c < d && c + 8 >= d)       // the lane with the last elements clears the row's padding
+            for (int b = d + (d + kPackBlock - 1) / kPackBlock; b < pitch; ++b) row[b] = 0;
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(32 * kPackWarps) unpack8_any_kernel(const uint8_t *src, int64_t N, int d, int pitch, bool vec, T *dst)
+{
+    const int lane = threadIdx.x & 31;
+    const int per_row = (d + kChunk - 1) / kChunk;
+    const int64_t chunks = N * per_row, stride = (int64_t)gridDim.x * kPackWarps;
+    for (int64_t w = (int64_t)blockIdx.x * kPackWarps + (threadIdx.x >> 5); w < chunks; w += stride) {
+        const int64_t r = w / per_row;
+        const int c = (int)(w - r * per_row) * kChunk + lane * 8;
+        if (c >= d) continue;
+        const uint8_t *row = src + r * pitch;      // 8 bytes at c: inside the row, whose pitch is a multiple of 16
+        float x[8];
+        dequantise(*reinterpret_cast<const uint2 *>(row + c), reinterpret_cast<const signed char *>(row)[d + c / kPackBlock], x);
+        store8(dst + r * d + c, d - c, vec, x);
+    }
+}
+
+// ---------------------------------------------------------------- aligned rows of whole blocks
+// A CTA of (x, y) threads takes kRows rows per thread row at a time, so that as many loads per thread are in
+// flight; a thread has 8 elements of each.  d is a multiple of 32 and rows are 16-byte aligned.
+constexpr int kRows = 4;
+
+template <typename T>
+__global__ void __launch_bounds__(256) pack8_kernel(const T *src, int64_t N, int d, int pitch, uint8_t *dst)
+{
+    const int64_t r0 = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * kRows;
+    const int nv = d / 8;
+    for (int v0 = 0; v0 < nv; v0 += blockDim.x) {
+        const int v = v0 + threadIdx.x;
+        float x[kRows][8];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            if (w0 + k * ch.stride >= ch.all) break;
-            int64_t r;
-            int c;
-            ch.place(w0 + k * ch.stride, r, c);
-            // largest magnitude of the block, as bits: infinities and NaN lie above all numbers
+        for (int k = 0; k < kRows; ++k)     // the last row and vector again where there is none: loads without a branch
+            load8(src + min(r0 + k, N - 1) * d + min(v, nv - 1) * 8, 8, true, x[k]);
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
             uint32_t top = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[k][e]) & 0x7fffffffu);
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const bool bad = top >= 0x7f800000u;
-            const int e2 = bad ? 0 : max((int)(top >> 23) - 133, -126);
-            const float scale = __int_as_float((127 - e2) << 23);
-            uint32_t q[2] = {0u, 0u};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                // x 2^-e + 1.5 2^23 rounds to even at the units: the low byte of the sum is the byte wanted
-                const float y = fminf(fmaxf(x[k][e] * scale, -127.f), 127.f) + 12582912.f;
-                q[e >> 2] |= (__float_as_uint(y) & 255u) << (8 * (e & 3));
-            }
-            if (bad) q[0] = q[1] = 0u;
-            uint8_t *row = dst + r * pitch;
-            if (c + 8 <= d) {
-                *reinterpret_cast<uint2 *>(row + c) = make_uint2(q[0], q[1]);
-            } else if (c < d) {
-                for (int e = 0; c + e < d; ++e) row[c + e] = (uint8_t)(q[e >> 2] >> (8 * (e & 3)));
-            }
-            if ((lane & 3) == 0 && c < d) row[d + c / kPackBlock] = (uint8_t)(bad ? kBadBlock : e2);
-            if (c < d && c + 8 >= d)       // the lane with the last elements clears the row's padding
-                for (int b = d + (d + kPackBlock - 1) / kPackBlock; b < pitch; ++b) row[b] = 0;
+            int e2;
+            const uint2 q = quantise(x[k], top, e2);
+            if (v >= nv || r0 + k >= N) continue;
+            uint8_t *row = dst + (r0 + k) * pitch;
+            *reinterpret_cast<uint2 *>(row + v * 8) = q;
+            if ((v & 3) == 0) row[d + v / 4] = (uint8_t)e2;
+            if (v == nv - 1)
+                for (int b = d + d / kPackBlock; b < pitch; ++b) row[b] = 0;
         }
     }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(32 * kPackWarps) unpack8_kernel(const uint8_t *src, int64_t N, int d, int pitch, bool vec, T *dst)
+__global__ void __launch_bounds__(256) unpack8_kernel(const uint8_t *src, int64_t N, int d, int pitch, T *dst)
 {
-    const Chunks ch(N, d);
-    for (int64_t w0 = ch.at; w0 < ch.all; w0 += kAhead * ch.stride) {
-        uint2 q[kAhead];
-        int e2[kAhead];
+    const int64_t r0 = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * kRows;
+    const int nv = d / 8;
+    for (int v = threadIdx.x; v < nv; v += blockDim.x) {
+        uint2 q[kRows];
+        int e2[kRows];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            int64_t r;
-            int c;
-            ch.place(min(w0 + k * ch.stride, ch.all - 1), r, c);
-            const int at = min(c, d - 1);                  // lanes past the row's end load its last elements
-            const uint8_t *row = src + r * pitch;          // 8 bytes from a multiple of 8: inside the row, whose pitch is one of 16
-            q[k] = __ldcs(reinterpret_cast<const uint2 *>(row + (at & ~7)));
-            e2[k] = reinterpret_cast<const signed char *>(row)[d + at / kPackBlock];
+        for (int k = 0; k < kRows; ++k) {
+            const uint8_t *row = src + min(r0 + k, N - 1) * pitch;
+            q[k] = *reinterpret_cast<const uint2 *>(row + v * 8);
+            e2[k] = reinterpret_cast<const signed char *>(row)[d + v / 4];
         }
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            if (w0 + k * ch.stride >= ch.all) break;
-            int64_t r;
-            int c;
-            ch.place(w0 + k * ch.stride, r, c);
-            const float scale = e2[k] == kBadBlock ? __int_as_float(0x7fc00000) : __int_as_float((e2[k] + 127) << 23);
+        for (int k = 0; k < kRows; ++k) {
             float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)    // byte + 128 as the low mantissa byte of 2^23, which is then taken off
-                x[e] = (__uint_as_float(__byte_perm((e < 4 ? q[k].x : q[k].y) ^ 0x80808080u, 0x4b000000u, 0x7440 + (e & 3))) - 8388736.f) * scale;
-            if (c < d) store8(dst + r * d + c, d - c, vec, x);
+            dequantise(q[k], e2[k], x);
+            if (r0 + k < N) store8(dst + (r0 + k) * d + v * 8, 8, true, x);
         }
     }
 }
 
-// one round of kAhead chunks per warp where that fills the GPU, at most eight CTAs per SM
-unsigned pack_ctas(int64_t N, int d)
+unsigned any_ctas(int64_t N, int d)
 {
-    const int64_t chunks = N * ((d + kChunk - 1) / kChunk);
-    const int64_t want = (chunks + kPackWarps - 1) / kPackWarps;       // one chunk per warp
-    const int64_t rounds = (want + 148 * 8 * kAhead - 1) / (148 * 8 * kAhead);
-    const int64_t ctas = (want + rounds * kAhead - 1) / (rounds * kAhead);
-    return (unsigned)(want < 148 * 8 ? want : ctas < 148 * 4 ? 148 * 4 : ctas);
+    const int64_t want = (N * ((d + kChunk - 1) / kChunk) + kPackWarps - 1) / kPackWarps;
+    return (unsigned)(want < 148 * 64 ? want : 148 * 64);
+}
+// (d >= 32) a thread per 8 elements of a row, as many rows side by side as 256 threads hold
+dim3 row_threads(int d)
+{
+    const int x = d / 8 >= 256 ? 256 : (d / 8 + 31) / 32 * 32;
+    return dim3((unsigned)x, (unsigned)(256 / x));
+}
+unsigned row_ctas(int64_t N, dim3 threads)
+{
+    const int64_t rows = (int64_t)threads.y * kRows;
+    return (unsigned)((N + rows - 1) / rows);
+}
+bool whole_rows(const void *hidden, int64_t N, int d)
+{
+    return aligned(hidden, 16) && d % kPackBlock == 0 && N <= ((int64_t)1 << 32);
+}
+
+template <typename T>
+cudaError_t pack_rows(const void *hidden, int64_t N, int d, void *packed, cudaStream_t st)
+{
+    const T *src = static_cast<const T *>(hidden);
+    uint8_t *dst = static_cast<uint8_t *>(packed);
+    if (whole_rows(hidden, N, d)) {
+        const dim3 threads = row_threads(d);
+        pack8_kernel<<<row_ctas(N, threads), threads, 0, st>>>(src, N, d, pack8_pitch(d), dst);
+    } else
+        pack8_any_kernel<<<any_ctas(N, d), 32 * kPackWarps, 0, st>>>(src, N, d, pack8_pitch(d), aligned(hidden, 16) && d % 8 == 0, dst);
+    return cudaGetLastError();
+}
+template <typename T>
+cudaError_t unpack_rows(const void *packed, int64_t N, int d, void *hidden, cudaStream_t st)
+{
+    const uint8_t *src = static_cast<const uint8_t *>(packed);
+    T *dst = static_cast<T *>(hidden);
+    if (whole_rows(hidden, N, d)) {
+        const dim3 threads = row_threads(d);
+        unpack8_kernel<<<row_ctas(N, threads), threads, 0, st>>>(src, N, d, pack8_pitch(d), dst);
+    } else
+        unpack8_any_kernel<<<any_ctas(N, d), 32 * kPackWarps, 0, st>>>(src, N, d, pack8_pitch(d), aligned(hidden, 16) && d % 8 == 0, dst);
+    return cudaGetLastError();
 }
 
 int check_pack(const void *hidden, int64_t N, int d, int dt, const void *packed)
@@ -218,30 +287,16 @@ int hidden_pack8(const void *hidden, int64_t N, int d, int dt, void *packed, voi
 {
     const int rc = check_pack(hidden, N, d, dt, packed);
     if (rc != SPR_OK || N == 0) return rc;
-    const bool vec = aligned(hidden, 16) && d % 8 == 0;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == SPR_F32)
-        pack8_kernel<<<pack_ctas(N, d), 32 * kPackWarps, 0, st>>>(static_cast<const float *>(hidden), N, d, pack8_pitch(d), vec,
-                                                                  static_cast<uint8_t *>(packed));
-    else
-        pack8_kernel<<<pack_ctas(N, d), 32 * kPackWarps, 0, st>>>(static_cast<const __nv_bfloat16 *>(hidden), N, d,
-                                                                  pack8_pitch(d), vec, static_cast<uint8_t *>(packed));
-    return finish(cudaGetLastError());
+    return finish(dt == SPR_F32 ? pack_rows<float>(hidden, N, d, packed, st) : pack_rows<__nv_bfloat16>(hidden, N, d, packed, st));
 }
 
 int hidden_unpack8(const void *packed, int64_t N, int d, int dt, void *hidden, void *cuda_stream)
 {
     const int rc = check_pack(hidden, N, d, dt, packed);
     if (rc != SPR_OK || N == 0) return rc;
-    const bool vec = aligned(hidden, 16) && d % 8 == 0;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == SPR_F32)
-        unpack8_kernel<<<pack_ctas(N, d), 32 * kPackWarps, 0, st>>>(static_cast<const uint8_t *>(packed), N, d, pack8_pitch(d),
-                                                                    vec, static_cast<float *>(hidden));
-    else
-        unpack8_kernel<<<pack_ctas(N, d), 32 * kPackWarps, 0, st>>>(static_cast<const uint8_t *>(packed), N, d, pack8_pitch(d),
-                                                                    vec, static_cast<__nv_bfloat16 *>(hidden));
-    return finish(cudaGetLastError());
+    return finish(dt == SPR_F32 ? unpack_rows<float>(packed, N, d, hidden, st) : unpack_rows<__nv_bfloat16>(packed, N, d, hidden, st));
 }
 
 }  // extern "C"
