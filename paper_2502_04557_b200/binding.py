@@ -554,50 +554,71 @@ def verifier_train_step(hidden, labels, theta, adam_m, adam_v, t: int, lr: float
 
 
 # ---------------------------------------------------------------------------- heads and 8-bit states
+#
+# These calls may take a few microseconds on the GPU, so their checks are kept short: addresses are passed as
+# plain integers, and devices are compared by index.
 
 
-def _head(hidden, W, tokens, name="hidden", token_name="targets"):
-    """Checks hidden [N,d], W [V,d] and int32 tokens [N] of one device; returns (N, d, V)."""
-    _dev(hidden, name=name)
-    _dev(W, hidden.dtype, "W")
-    _dev(tokens, torch.int32, token_name)
-    if hidden.dim() != 2 or W.dim() != 2 or W.shape[1] != hidden.shape[1]:
-        raise ValueError(f"{name} must be [N,d] and W [V,d]")
-    if tokens.numel() != hidden.shape[0]:
-        raise ValueError(f"{token_name} must have one entry per hidden state")
-    return hidden.shape[0], hidden.shape[1], W.shape[0]
+def _on(device: int, dtype, name: str, t: torch.Tensor) -> int:
+    """Address of a contiguous tensor of this type on this device."""
+    if t.get_device() != device:
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a CUDA tensor")
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, the current device is cuda:{device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
-def _same_device(ws, *tensors):
-    """Every tensor and the workspace lie on the device whose stream is used."""
-    dev = torch.device("cuda", torch.cuda.current_device())
-    for t in tensors + ((ws.buf,) if ws is not None else ()):
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors and workspace must be on the current device {dev}, got one on {t.device}")
-
-
-def _result(t, shape, dtype, device, name):
-    """An output tensor: the caller's, checked, or a new one."""
+def _result(device: int, t, shape, dtype, name: str):
+    """An output tensor and its address: the caller's, checked, or a new one."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    _dev(t, dtype, name)
+        t = torch.empty(shape, dtype=dtype, device=torch.device("cuda", device))
+        return t, t.data_ptr()
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
-    return t
+    return t, _on(device, dtype, name, t)
+
+
+def _ws(device: int, ws: "Workspace"):
+    if ws.buf.get_device() != device:
+        raise ValueError(f"the workspace is on cuda:{ws.buf.get_device()}, the current device is cuda:{device}")
+    return ws.buf.data_ptr(), ws.buf.numel()
+
+
+def _raw_stream(device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _head(device, hidden, W, tokens, name="hidden", W_name="W", token_name="targets"):
+    """Checks hidden [N,d], W [V,d] and int32 tokens [N]; returns (N, d, V, their addresses, dt)."""
+    dtype = hidden.dtype
+    dt = _dt(hidden)
+    h, w = _on(device, dtype, name, hidden), _on(device, dtype, W_name, W)
+    t = _on(device, torch.int32, token_name, tokens)
+    if hidden.dim() != 2 or W.dim() != 2 or W.shape[1] != hidden.shape[1]:
+        raise ValueError(f"{name} must be [N,d] and {W_name} [V,d]")
+    N, d = hidden.shape
+    if tokens.numel() != N:
+        raise ValueError(f"{token_name} must have one entry per hidden state")
+    return N, d, W.shape[0], h, w, t, dt
 
 
 def head_loss(hidden, W, targets, ws: Workspace, want_lse: bool = True, out=None):
     """Softmax cross entropy of hidden [N,d] under the head W [V,d]; targets i32 [N], negative = padding.
 
     Returns (loss f32 [N], lse f32 [N] or None); out: the same two tensors."""
-    N, d, V = _head(hidden, W, targets)
+    dev = torch.cuda.current_device()
+    N, d, V, h, w, t, dt = _head(dev, hidden, W, targets)
     loss, lse = (None, None) if out is None else out
-    loss = _result(loss, (N,), torch.float32, hidden.device, "loss")
-    lse = _result(lse, (N,), torch.float32, hidden.device, "lse") if want_lse or lse is not None else None
-    _same_device(ws, hidden, W, targets, loss, lse)
-    rc = lib().head_loss(_ptr(hidden), _ptr(W), _ptr(targets), N, d, V, _dt(hidden), _ptr(loss), _ptr(lse),
-                         _ptr(ws.buf), ws.nbytes, _stream())
-    _check("head_loss", rc)
+    loss, a = _result(dev, loss, (N,), torch.float32, "loss")
+    lse, b = _result(dev, lse, (N,), torch.float32, "lse") if want_lse or lse is not None else (None, None)
+    p, n = _ws(dev, ws)
+    rc = lib().head_loss(h, w, t, N, d, V, dt, a, b, p, n, _raw_stream(dev))
+    if rc != 0:
+        _check("head_loss", rc)
     return loss, lse
 
 
@@ -606,23 +627,22 @@ def head_loss_grad(hidden, W, targets, lse, grad_loss, ws: Workspace, want_hidde
     """Gradient of sum(grad_loss * loss) of head_loss; lse as head_loss returned it, grad_loss f32 [N].
 
     Returns (d_hidden [N,d] or None, d_W [V,d] or None) in the operands' type; out: the same two tensors."""
-    N, d, V = _head(hidden, W, targets)
-    for name, t in (("lse", lse), ("grad_loss", grad_loss)):
-        _dev(t, torch.float32, name)
-        if t.numel() != N:
-            raise ValueError(f"{name} must have one entry per hidden state")
+    dev = torch.cuda.current_device()
+    N, d, V, h, w, t, dt = _head(dev, hidden, W, targets)
+    z, g = _on(dev, torch.float32, "lse", lse), _on(dev, torch.float32, "grad_loss", grad_loss)
+    if lse.numel() != N or grad_loss.numel() != N:
+        raise ValueError("lse and grad_loss must have one entry per hidden state")
     d_hidden, d_W = (None, None) if out is None else out
-    d_hidden = _result(d_hidden, (N, d), hidden.dtype, hidden.device, "d_hidden") if want_hidden else None
-    d_W = _result(d_W, (V, d), hidden.dtype, hidden.device, "d_W") if want_W else None
+    d_hidden, a = _result(dev, d_hidden, (N, d), hidden.dtype, "d_hidden") if want_hidden else (None, None)
+    d_W, b = _result(dev, d_W, (V, d), hidden.dtype, "d_W") if want_W else (None, None)
     if d_hidden is None and d_W is None:
         raise ValueError("at least one of the two gradients must be wanted")
-    _same_device(ws, hidden, W, targets, lse, grad_loss, d_hidden, d_W)
     if N == 0 and d_W is None:
         return d_hidden, None
-    # an empty batch has no addresses to pass
-    rc = lib().head_loss_grad(_ptr(hidden), _ptr(W), _ptr(targets), _ptr(lse), _ptr(grad_loss), N, d, V, _dt(hidden),
-                              _ptr(d_hidden), _ptr(d_W), _ptr(ws.buf), ws.nbytes, _stream())
-    _check("head_loss_grad", rc)
+    p, n = _ws(dev, ws)
+    rc = lib().head_loss_grad(h, w, t, z, g, N, d, V, dt, a, b, p, n, _raw_stream(dev))
+    if rc != 0:
+        _check("head_loss_grad", rc)
     return d_hidden, d_W
 
 
@@ -631,21 +651,21 @@ def verifier_labels_head(p_hidden, p_W, q_hidden, q_W, draft_tokens, lambdas, ws
     [N,dq], q_W [V,dq] of the draft; draft_tokens i32 [N]; lambdas: up to 8 floats.
 
     Returns (labels u8 [len(lambdas),N], ratio f32 [N] or None) with ratio = q(x)/p(x)."""
-    N, dp, V = _head(p_hidden, p_W, draft_tokens, "p_hidden", "draft_tokens")
-    Nq, dq, Vq = _head(q_hidden, q_W, draft_tokens, "q_hidden", "draft_tokens")
+    dev = torch.cuda.current_device()
+    N, dp, V, ph, pw, x, dt = _head(dev, p_hidden, p_W, draft_tokens, "p_hidden", "p_W", "draft_tokens")
+    _, dq, Vq, qh, qw, _, dtq = _head(dev, q_hidden, q_W, draft_tokens, "q_hidden", "q_W", "draft_tokens")
     if V != Vq:
         raise ValueError("the two heads must have one vocabulary")
-    if q_hidden.dtype != p_hidden.dtype:
+    if dt != dtq:
         raise TypeError("p_hidden and q_hidden must have one type")
-    lam = (C.c_float * len(lambdas))(*[float(x) for x in lambdas])
-    dev = p_hidden.device
-    labels = torch.empty((len(lambdas), N), dtype=torch.uint8, device=dev)
-    ratio = torch.empty((N,), dtype=torch.float32, device=dev) if want_ratio else None
-    _same_device(ws, p_hidden, p_W, q_hidden, q_W, draft_tokens)
-    rc = lib().verifier_labels_head(_ptr(p_hidden), _ptr(p_W), dp, _ptr(q_hidden), _ptr(q_W), dq, _ptr(draft_tokens), N, V,
-                                    _dt(p_hidden), C.cast(lam, C.c_void_p), len(lambdas), _ptr(labels), _ptr(ratio),
-                                    _ptr(ws.buf), ws.nbytes, _stream())
-    _check("verifier_labels_head", rc)
+    lam = (C.c_float * len(lambdas))(*lambdas)
+    labels, a = _result(dev, None, (len(lambdas), N), torch.uint8, "labels")
+    ratio, b = _result(dev, None, (N,), torch.float32, "ratio") if want_ratio else (None, None)
+    p, n = _ws(dev, ws)
+    rc = lib().verifier_labels_head(ph, pw, dp, qh, qw, dq, x, N, V, dt, lam, len(lambdas), a, b, p, n,
+                                    _raw_stream(dev))
+    if rc != 0:
+        _check("verifier_labels_head", rc)
     return labels, ratio
 
 
@@ -654,29 +674,34 @@ def pack8_pitch(d: int) -> int:
     return int(lib().spr_pack8_pitch(d))
 
 
-def _packed(packed, d: int):
-    _dev(packed, torch.uint8, "packed")
-    if packed.dim() != 2 or packed.shape[1] != pack8_pitch(d) or d <= 0:
+def _packed(device: int, packed, d: int):
+    p = _on(device, torch.uint8, "packed", packed)
+    if d <= 0 or packed.dim() != 2 or packed.shape[1] != (d + (d + 31) // 32 + 15) // 16 * 16:
         raise ValueError(f"packed must be [N, {pack8_pitch(d)}] for d = {d}, got {tuple(packed.shape)}")
-    return packed.shape[0]
+    return packed.shape[0], p
 
 
 def hidden_pack8(hidden, out=None):
     """hidden [N,d] in 8 bits with an exponent per 32 elements: u8 [N, pack8_pitch(d)]."""
-    _dev(hidden, name="hidden")
+    dev = torch.cuda.current_device()
+    dt = _dt(hidden)
+    h = _on(dev, hidden.dtype, "hidden", hidden)
     N, d = hidden.shape
-    packed = _result(out, (N, pack8_pitch(d)), torch.uint8, hidden.device, "packed")
-    _same_device(None, hidden, packed)
-    _check("hidden_pack8", lib().hidden_pack8(_ptr(hidden), N, d, _dt(hidden), _ptr(packed), _stream()))
+    packed, p = _result(dev, out, (N, (d + (d + 31) // 32 + 15) // 16 * 16), torch.uint8, "packed")
+    rc = lib().hidden_pack8(h, N, d, dt, p, _raw_stream(dev))
+    if rc != 0:
+        _check("hidden_pack8", rc)
     return packed
 
 
 def hidden_unpack8(packed, d: int, dtype=torch.bfloat16, out=None):
     """The values [N,d] that packed rows stand for (exact in bf16 and fp32)."""
-    N = _packed(packed, d)
-    hidden = _result(out, (N, d), dtype, packed.device, "hidden")
-    _same_device(None, packed, hidden)
-    _check("hidden_unpack8", lib().hidden_unpack8(_ptr(packed), N, d, _dt(hidden), _ptr(hidden), _stream()))
+    dev = torch.cuda.current_device()
+    N, p = _packed(dev, packed, d)
+    hidden, h = _result(dev, out, (N, d), dtype, "hidden")
+    rc = lib().hidden_unpack8(p, N, d, _dt(hidden), h, _raw_stream(dev))
+    if rc != 0:
+        _check("hidden_unpack8", rc)
     return hidden
 
 
@@ -685,23 +710,23 @@ def verifier_train_step8(packed, d: int, labels, theta, adam_m, adam_v, t: int, 
                          test_flags: int = 0, spin_limit: int = 0):
     """verifier_train_step on hidden states kept in 8 bits: packed u8 [N, pack8_pitch(d)].
     test_flags / spin_limit: the test hook spr_test_verifier_train_step8 instead of the public call."""
-    N = _packed(packed, d)
-    _dev(labels, torch.uint8, "labels")
-    for name, a in (("theta", theta), ("adam_m", adam_m), ("adam_v", adam_v)):
-        _dev(a, torch.float32, name)
-        if a.numel() != d + 1:
-            raise ValueError(f"{name} must have d + 1 entries")
+    dev = torch.cuda.current_device()
+    N, p = _packed(dev, packed, d)
+    y = _on(dev, torch.uint8, "labels", labels)
+    w, m, v = (_on(dev, torch.float32, name, a) for name, a in (("theta", theta), ("adam_m", adam_m), ("adam_v", adam_v)))
+    if theta.numel() != d + 1 or adam_m.numel() != d + 1 or adam_v.numel() != d + 1:
+        raise ValueError("theta, adam_m and adam_v must have d + 1 entries")
     if labels.numel() != N:
         raise ValueError("labels must have one entry per hidden state")
-    loss = _result(loss, (1,), torch.float32, packed.device, "loss")
-    _same_device(ws, packed, labels, theta, adam_m, adam_v, loss)
-    args = (_ptr(packed), _ptr(labels), N, d, _ptr(theta), _ptr(adam_m), _ptr(adam_v), t, lr, beta1, beta2, eps,
-            _ptr(loss), _ptr(ws.buf), ws.nbytes, _stream())
+    loss, a = _result(dev, loss, (1,), torch.float32, "loss")
+    wsp, n = _ws(dev, ws)
+    args = (p, y, N, d, w, m, v, t, lr, beta1, beta2, eps, a, wsp, n, _raw_stream(dev))
     if test_flags or spin_limit:
         rc = lib().spr_test_verifier_train_step8(*args, test_flags, spin_limit)
     else:
         rc = lib().verifier_train_step8(*args)
-    _check("verifier_train_step8", rc)
+    if rc != 0:
+        _check("verifier_train_step8", rc)
     return loss
 
 
