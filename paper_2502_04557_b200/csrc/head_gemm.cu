@@ -163,19 +163,28 @@ __device__ __forceinline__ void by_rows(const float (&x)[32], float4 (&v)[8], fl
     }
     __syncwarp();
 }
-// four elements of a row; only those before `left` exist
+// four elements of a row
 __device__ __forceinline__ void store4(float *p, float4 x) { *reinterpret_cast<float4 *>(p) = x; }
 __device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 x)
 {
     *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
 }
+// The same block where rows start anywhere or columns are missing: out[r * pitch] of the first `rows` rows, a lane per
+// column (a store instruction is then one run of a row), lanes below `width`.  v is as by_rows leaves it.
 template <typename T>
-__device__ __forceinline__ void store4_tail(T *p, float4 x, int left)
+__device__ __forceinline__ void store_any(T *out, int64_t pitch, const float4 (&v)[8], float4 *stage, int lane, int rows, int width)
 {
-    if (left > 0) p[0] = (T)x.x;
-    if (left > 1) p[1] = (T)x.y;
-    if (left > 2) p[2] = (T)x.z;
-    if (left > 3) p[3] = (T)x.w;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + (lane >> 3);
+        stage[r * 8 + ((lane & 7) ^ (r & 7))] = v[i];
+    }
+    __syncwarp();
+    const float *s = reinterpret_cast<const float *>(stage);
+#pragma unroll 8
+    for (int r = 0; r < 32; ++r, out += pitch)
+        if (r < rows && lane < width) out[0] = (T)s[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)];
+    __syncwarp();
 }
 __device__ __forceinline__ float minus_bf16(float x) { return x - __bfloat162float(__float2bfloat16(x)); }
 
@@ -435,7 +444,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                 // this lane's part of a block: columns 4 (lane % 8) .. + 3 of rows lane / 8, + 4, ...
                 const int rows = (int)min((int64_t)32, j.rows - (row - lane)) - (lane >> 3);
                 const int64_t r0 = row - lane + (lane >> 3);
-                const int cl = c0 + 4 * (lane & 7), left = width - 4 * (lane & 7);
+                const int cl = c0 + 4 * (lane & 7);
                 const bool to_out = j.out != nullptr, add = j.add_acc != 0;
                 const int64_t acc_step = 4 * j.acc_pitch, out_step = 4 * j.out_pitch;
                 float *a = j.acc + (int64_t)it.split * j.acc_stride + r0 * j.acc_pitch + cl;    // used where there is an acc
@@ -487,9 +496,8 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                             for (int i = 0; i < 8; ++i, p += out_step)
                                 if (4 * i < rows) store4(p, v[i]);
                         } else {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i, p += out_step)
-                                if (4 * i < rows) store4_tail(p, v[i], left - 32 * q);
+                            store_any(static_cast<T *>(j.out) + (row - lane) * j.out_pitch + c0 + 32 * q + lane, j.out_pitch, v, stage, lane,
+                                      rows + (lane >> 3), width - 32 * q);
                         }
                     }
                 }

@@ -18,6 +18,7 @@
 
 #include "common.cuh"
 #include "head_gemm.h"
+#include "head_small.h"
 #include "host_util.h"
 #include "launch.h"
 
@@ -277,6 +278,17 @@ bool needs_pack(int d, int dt) { return dt == SPR_F32 || d % 8 != 0; }
 int parts(int dt) { return dt == SPR_F32 ? 3 : 1; }
 size_t packed_bytes(int64_t rows, int d, int dt) { return 2 * (size_t)rows * parts(dt) * (size_t)round_up(d, 64); }
 
+// fp32 problems of up to 2^26 multiply-adds, rows counted in tiles of 32, go to the CUDA cores
+// (head_small.cu); above that the six bf16 products on the tensor cores are faster.  Measured (us, CUDA cores /
+// tensor cores): loss 4x256x1000 9 / 19, 64x256x4000 18.5 / 20, 64x512x4000 31 / 30; gradient 67x257x1003
+// 30 / 69, 64x256x4000 66 / 76, 256x128x4000 103 / 71.  (bf16: 16x256x4000 11 / 9 and worse from there.)
+bool small_head(int64_t N, int d, int64_t V, int dt)
+{
+    return dt == SPR_F32 && (double)round_up(N, 32) * (double)V * (double)d <= (double)(1 << 26);
+}
+// dH's contraction over the vocabulary there: 256 of it per CTA
+int small_splits(int V) { return (int)(ceil_div(V, 256) < 64 ? ceil_div(V, 256) : 64); }
+
 struct HeadLossWs {
     size_t hidden, W;     // packed operands (0 bytes where the caller's tensors serve)
     size_t part;          // float2 [N, tiles]
@@ -284,6 +296,11 @@ struct HeadLossWs {
 HeadLossWs head_loss_layout(Carver &c, int64_t N, int d, int V, int dt)
 {
     HeadLossWs w;
+    if (small_head(N, d, V, dt)) {
+        w.hidden = w.W = 0;
+        w.part = c.take_data(8 * (size_t)N * (size_t)ceil_div(V, kSmallTile));
+        return w;
+    }
     w.hidden = c.take_data(needs_pack(d, dt) ? packed_bytes(N, d, dt) : 0);
     w.W = c.take_data(needs_pack(d, dt) ? packed_bytes(V, d, dt) : 0);
     w.part = c.take_data(16 * (size_t)N * (size_t)ceil_div(V, kPairTile));
@@ -321,11 +338,21 @@ struct HeadGradWs {
     size_t W;             // packed head (0 bytes where the caller's serves)
     size_t dlogits;       // bf16 [N, parts * width]
     size_t acc;           // float [splits, N, round_up(d, 64)], where dH takes more than one launch or range
+    size_t tickets;       // int32 per tile of dH (ticket zone; CUDA cores only)
 };
 HeadGradWs head_grad_layout(Carver &c, int64_t N, int d, int V, int dt)
 {
-    const Pieces p = pieces(N, d, V, dt);
     HeadGradWs w;
+    if (small_head(N, d, V, dt)) {
+        const size_t tiles = (size_t)ceil_div(N, kSmallTile) * (size_t)ceil_div(d, kSmallTile);
+        w.hidden = w.W = 0;
+        w.tickets = c.take_tickets(tiles);
+        w.dlogits = c.take_data(4 * (size_t)N * (size_t)V);       // fp32 here
+        w.acc = c.take_data(4 * 1024 * tiles * (size_t)small_splits(V));
+        return w;
+    }
+    const Pieces p = pieces(N, d, V, dt);
+    w.tickets = 0;
     w.hidden = c.take_data(packed_bytes(N, d, dt));
     w.W = c.take_data(needs_pack(d, dt) ? packed_bytes(V, d, dt) : 0);
     w.dlogits = c.take_data(2 * (size_t)N * parts(dt) * (size_t)p.width);
@@ -419,6 +446,63 @@ cudaError_t stats_job(PairJob &j, PairOperand &a, PairOperand &b, const void *hi
     return e;
 }
 
+// the same on the CUDA cores
+void small_stats_job(SmallJob &j, const void *hidden, const void *W, int N, int d, int V, const float2 *part)
+{
+    j.a = SmallOperand{hidden, d, 1, 0, 0};
+    j.b = SmallOperand{W, d, 1, 0, 0};
+    j.rows = N;
+    j.cols = V;
+    j.K = d;
+    j.part = const_cast<float2 *>(part);
+}
+
+// head_loss_grad on the CUDA cores: D in fp32, then both products in one launch
+cudaError_t small_grad(const void *hidden, const void *W, const int32_t *targets, const float *lse, const float *grad_loss, int N,
+                       int d, int V, int dt, void *d_hidden, void *d_W, float *D, float *acc, int *tickets, int *status, cudaStream_t st)
+{
+    SmallParams sp;
+    memset(&sp, 0, sizeof sp);
+    sp.V = V;
+    sp.status = status;
+    SmallJob &j = sp.job[0];
+    small_stats_job(j, hidden, W, N, d, V, nullptr);
+    j.d = D;
+    j.d_pitch = V;
+    j.targets = targets;
+    j.lse = lse;
+    j.grad_loss = grad_loss;
+    cudaError_t e = launch_small(SMALL_DLOGITS, dt == SPR_F32, sp, 1, st);
+    if (e != cudaSuccess) return e;
+    memset(sp.job, 0, sizeof sp.job);
+    int jobs = 0;
+    if (d_hidden) {               // dH [N, d] = D [N, V] W [V, d]: the longer contraction first
+        SmallJob &h = sp.job[jobs++];
+        h.a = SmallOperand{D, V, 1, 1, 0};
+        h.b = SmallOperand{W, 1, d, 0, 1};
+        h.rows = N;
+        h.cols = d;
+        h.K = V;
+        h.splits = small_splits(V);
+        h.acc = acc;
+        h.tickets = tickets;
+        h.out = d_hidden;
+        h.out_pitch = d;
+    }
+    if (d_W) {                    // dW [V, d] = D^T [V, N] H [N, d]
+        SmallJob &w = sp.job[jobs++];
+        w.a = SmallOperand{D, 1, V, 1, 1};
+        w.b = SmallOperand{hidden, 1, d, 0, 1};
+        w.live = targets;         // a row without a target may hold anything
+        w.rows = V;
+        w.cols = d;
+        w.K = N;
+        w.out = d_W;
+        w.out_pitch = d;
+    }
+    return launch_small(SMALL_OUT, dt == SPR_F32, sp, jobs, st);
+}
+
 bool head_sizes_ok(int64_t N, int d, int V) { return N >= 0 && d > 0 && d <= (1 << 20) && V > 0 && V <= (1 << 30); }
 
 }  // namespace
@@ -464,11 +548,23 @@ int head_loss(const void *hidden, const void *W, const int32_t *targets, int N, 
     PairParams prm;
     memset(&prm, 0, sizeof prm);
     prm.status = at<int>(ws, 0);
-    PairOperand a, b;
-    cudaError_t e = stats_job(prm.job[0], a, b, hidden, W, N, d, V, dt, ws, lay, st);
-    if (e == cudaSuccess) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, 1, &a, &b, st);
+    HeadRow h = {hidden, W, at<float2>(ws, lay.part), d, 0};
+    cudaError_t e;
+    if (small_head(N, d, V, dt)) {
+        SmallParams sp;
+        memset(&sp, 0, sizeof sp);
+        sp.V = V;
+        sp.status = prm.status;
+        small_stats_job(sp.job[0], hidden, W, N, d, V, h.part);
+        e = launch_small(SMALL_STATS, dt == SPR_F32, sp, 1, st);
+        h.parts = sp.job[0].tiles_n;
+    } else {
+        PairOperand a, b;
+        e = stats_job(prm.job[0], a, b, hidden, W, N, d, V, dt, ws, lay, st);
+        if (e == cudaSuccess) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, 1, &a, &b, st);
+        h.parts = 2 * prm.job[0].tiles_n;
+    }
     if (e == cudaSuccess) {
-        const HeadRow h = {hidden, W, prm.job[0].part, d, 2 * prm.job[0].tiles_n};
         e = dt == SPR_F32 ? launch_behind(head_finish_kernel<float>, N, kRowThreads, st, h, V, targets, loss, lse, prm.status)
                           : launch_behind(head_finish_kernel<__nv_bfloat16>, N, kRowThreads, st, h, V, targets, loss, lse, prm.status);
     }
@@ -497,6 +593,9 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
     int rc = device_supported();
     if (rc != SPR_OK) return rc;
 
+    if (small_head(N, d, V, dt))
+        return finish(small_grad(hidden, W, targets, lse, grad_loss, N, d, V, dt, d_hidden, d_W, at<float>(ws, lay.dlogits),
+                                 at<float>(ws, lay.acc), at<int>(ws, lay.tickets), at<int>(ws, 0), st));
     const bool f32 = dt == SPR_F32;
     const size_t es = elem_size(dt);
     const Pieces pc = pieces(N, d, V, dt);
@@ -618,13 +717,30 @@ int verifier_labels_head(const void *p_hidden, const void *p_W, int dp, const vo
     memset(&prm, 0, sizeof prm);
     prm.status = at<int>(ws, 0);
     PairOperand a[2], b[2];
-    const int ip = dp >= dq ? 0 : 1, iq = 1 - ip;       // the longer products first
-    cudaError_t e = stats_job(prm.job[ip], a[ip], b[ip], p_hidden, p_W, N, dp, V, dt, ws, lay.p, st);
-    if (e == cudaSuccess) e = stats_job(prm.job[iq], a[iq], b[iq], q_hidden, q_W, N, dq, V, dt, ws, lay.q, st);
-    if (e == cudaSuccess) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, 2, a, b, st);
+    HeadRow p = {p_hidden, p_W, at<float2>(ws, lay.p.part), dp, 0}, q = {q_hidden, q_W, at<float2>(ws, lay.q.part), dq, 0};
+    const bool p_small = small_head(N, dp, V, dt), q_small = small_head(N, dq, V, dt);
+    cudaError_t e = cudaSuccess;
+    SmallParams sp;
+    memset(&sp, 0, sizeof sp);
+    sp.V = V;
+    sp.status = prm.status;
+    int smalls = 0, pairs = 0;
+    // the longer products first; a model whose head is small goes to the CUDA cores
+    for (int i = 0; i < 2 && e == cudaSuccess; ++i) {
+        const bool is_p = (i == 0) == (dp >= dq);
+        HeadRow &r = is_p ? p : q;
+        if (is_p ? p_small : q_small) {
+            small_stats_job(sp.job[smalls++], r.hidden, r.W, N, r.d, V, r.part);
+            r.parts = (int)ceil_div(V, kSmallTile);
+        } else {
+            e = stats_job(prm.job[pairs], a[pairs], b[pairs], r.hidden, r.W, N, r.d, V, dt, ws, is_p ? lay.p : lay.q, st);
+            ++pairs;
+            r.parts = 2 * (int)ceil_div(V, kPairTile);
+        }
+    }
+    if (e == cudaSuccess && smalls) e = launch_small(SMALL_STATS, dt == SPR_F32, sp, smalls, st);
+    if (e == cudaSuccess && pairs) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, pairs, a, b, st);
     if (e == cudaSuccess) {
-        const HeadRow p = {p_hidden, p_W, prm.job[ip].part, dp, 2 * prm.job[ip].tiles_n};
-        const HeadRow q = {q_hidden, q_W, prm.job[iq].part, dq, 2 * prm.job[iq].tiles_n};
         HeadLabels out;
         memset(&out, 0, sizeof out);
         out.n_lambda = n_lambda;

@@ -370,3 +370,29 @@ def test_labels_agree_with_those_from_kept_logits(spr):
     assert bool(((ra.view(-1) / rb - 1).abs() < 2e-4).all())
     clear = torch.stack([(rb / lam - 1).abs() > 2e-4 for lam in (1.0, 1.2, 1.5)])
     assert torch.equal(a.view(3, N)[clear], b[clear])
+
+
+@pytest.mark.parametrize("N,d,V", [(67, 257, 1003), (33, 64, 31), (100, 3, 20000), (32, 129, 2048), (1, 40, 33), (500, 65, 900)])
+def test_fp32_problems_small_enough_for_the_cuda_cores(spr, N, d, V):
+    h, w, t, gl = problem(N, d, V, torch.float32, seed=N + d)
+    _, lse = check_loss(spr, h, w, t)
+    dh, dw = check_grad(spr, h, w, t, gl, lse)
+    ws = workspace(spr, spr.OP_HEAD_LOSS_GRAD, N, V, d, torch.float32)
+    for _ in range(3):                                       # the tickets are back at zero after every call
+        again = spr.head_loss_grad(h, w, t, lse, gl, ws)
+        assert torch.equal(again[0], dh) and torch.equal(again[1], dw)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=IDS.get)
+def test_labels_with_heads_on_different_kernels(spr, dtype):
+    """A draft head small enough for the CUDA cores (fp32) beside a target head that is not."""
+    N, dp, dq, V = 64, 640, 40, 3001
+    ph, pw, x, _ = problem(N, dp, V, dtype, seed=1, ignore=0.0)
+    qh, qw, _, _ = problem(N, dq, V, dtype, seed=2)
+    for a in ((ph, pw, qh, qw), (qh, qw, ph, pw)):
+        ws = workspace(spr, spr.OP_VERIFIER_LABELS_HEAD, N, V, a[0].shape[1], dtype, h=a[2].shape[1])
+        _, ratio = spr.verifier_labels_head(*a, x, [1.0], ws)
+        l = [b.double() @ c.double().T for b, c in ((a[0], a[1]), (a[2], a[3]))]
+        off = logit_bound(a[0], a[1]).amax(1) + logit_bound(a[2], a[3]).amax(1) + 64 * U * 10
+        p, q = (torch.log_softmax(m, 1).gather(1, x.long()[:, None])[:, 0] for m in l)
+        assert bool(((ratio.double() / torch.exp(q - p) - 1).abs() <= 2 * off).all()) and ws.device_status() == 0
