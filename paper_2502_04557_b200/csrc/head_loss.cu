@@ -19,6 +19,7 @@
 #include "common.cuh"
 #include "head_gemm.h"
 #include "head_small.h"
+#include "head_stream.h"
 #include "host_util.h"
 #include "launch.h"
 
@@ -239,37 +240,51 @@ __global__ void __launch_bounds__(kRowThreads) head_labels_kernel(const HeadRow 
     if (l == 0 && out.ratio) out.ratio[i] = (float)answer;
 }
 
-// out[r, c] = sum over the slices, in order
+// out[r, c] = sum over the slices: 32 groups of four columns per CTA and round; each of eight warps adds up
+// every eighth slice, eight loads at a time, and the eight sums are added in order
 template <typename T>
 __global__ void __launch_bounds__(256) head_sum_kernel(const float *acc, int slices, int64_t stride, int pitch, int64_t rows,
                                                        int d, T *out)
 {
+    __shared__ float4 sums[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int groups = (d + 3) / 4;
     const int64_t n = rows * groups;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
+    pdl_wait();
+    for (int64_t i0 = (int64_t)blockIdx.x * 32; i0 < n; i0 += (int64_t)gridDim.x * 32) {
+        const int64_t i = min(i0 + lane, n - 1);
         const int64_t r = i / groups;
         const int c = (int)(i - r * groups) * 4;
         const float *p = acc + r * pitch + c;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k0 = 0; k0 < slices; k0 += 8) {
+        for (int k0 = warp; k0 < slices; k0 += 64) {
             float4 x[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                x[k] = *reinterpret_cast<const float4 *>(p + min(k0 + k, slices - 1) * stride);
+            for (int k = 0; k < 8; ++k) x[k] = *reinterpret_cast<const float4 *>(p + min(k0 + 8 * k, slices - 1) * stride);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                if (k0 + k >= slices) break;
-                s.x += x[k].x;
-                s.y += x[k].y;
-                s.z += x[k].z;
-                s.w += x[k].w;
+                const bool there = k0 + 8 * k < slices;
+                s.x += there ? x[k].x : 0.f;
+                s.y += there ? x[k].y : 0.f;
+                s.z += there ? x[k].z : 0.f;
+                s.w += there ? x[k].w : 0.f;
             }
         }
-        const float v[4] = {s.x, s.y, s.z, s.w};
-        T *o = out + r * d + c;
+        __syncthreads();
+        sums[warp][lane] = s;
+        __syncthreads();
+        if (warp == 0 && i0 + lane < n) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (c + e < d) o[e] = (T)v[e];
+            for (int k = 1; k < 8; ++k) {
+                const float4 x = sums[k][lane];
+                s = make_float4(s.x + x.x, s.y + x.y, s.z + x.z, s.w + x.w);
+            }
+            const float v[4] = {s.x, s.y, s.z, s.w};
+            T *o = out + r * d + c;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < d) o[e] = (T)v[e];
+        }
     }
 }
 
@@ -286,6 +301,15 @@ bool small_head(int64_t N, int d, int64_t V, int dt)
 {
     return dt == SPR_F32 && (double)round_up(N, 32) * (double)V * (double)d <= (double)(1 << 26);
 }
+// A handful of tokens: one pass over W as it is (head_stream.cu).  fp32 heads that would have to be laid out in
+// three parts first: up to eight tokens; bf16 heads with rows that TMA cannot take: up to four; others: one.
+// Measured (us, one pass / tensor cores, d = 2048, V = 32000): f32 N = 8 loss 99 / 293, gradient 259 / 887; bf16
+// N = 1 34 / 46 and 119 / 145, N = 4 46 / 39 and 159 / 135; bf16 d = 1001, N = 4 40 / 55 and 155 / 187.
+bool stream_head(bool grad, int64_t N, int d, int64_t V, int dt)
+{
+    const int most = dt == SPR_F32 ? kStreamTokens : d % 8 != 0 ? 4 : 1;
+    return N <= most && !small_head(N, d, V, dt) && stream_fits(grad, (int)N, d, dt == SPR_F32);
+}
 // dH's contraction over the vocabulary there: 256 of it per CTA
 int small_splits(int V) { return (int)(ceil_div(V, 256) < 64 ? ceil_div(V, 256) : 64); }
 
@@ -299,6 +323,11 @@ HeadLossWs head_loss_layout(Carver &c, int64_t N, int d, int V, int dt)
     if (small_head(N, d, V, dt)) {
         w.hidden = w.W = 0;
         w.part = c.take_data(8 * (size_t)N * (size_t)ceil_div(V, kSmallTile));
+        return w;
+    }
+    if (stream_head(false, N, d, V, dt)) {
+        w.hidden = w.W = 0;
+        w.part = c.take_data(8 * (size_t)N * (size_t)stream_ctas(false, (int)N, d, V));
         return w;
     }
     w.hidden = c.take_data(needs_pack(d, dt) ? packed_bytes(N, d, dt) : 0);
@@ -349,6 +378,11 @@ HeadGradWs head_grad_layout(Carver &c, int64_t N, int d, int V, int dt)
         w.tickets = c.take_tickets(tiles);
         w.dlogits = c.take_data(4 * (size_t)N * (size_t)V);       // fp32 here
         w.acc = c.take_data(4 * 1024 * tiles * (size_t)small_splits(V));
+        return w;
+    }
+    if (stream_head(true, N, d, V, dt)) {
+        w.hidden = w.W = w.tickets = w.dlogits = 0;
+        w.acc = c.take_data(4 * (size_t)stream_ctas(true, (int)N, d, V) * (size_t)N * (size_t)round_up(d, 64));
         return w;
     }
     const Pieces p = pieces(N, d, V, dt);
@@ -457,6 +491,50 @@ void small_stats_job(SmallJob &j, const void *hidden, const void *W, int N, int 
     j.part = const_cast<float2 *>(part);
 }
 
+// d_hidden [N, d] = the sum over acc [slices, N, round_up(d, 64)]
+cudaError_t sum_slices(const float *acc, int slices, int N, int d, int dt, void *d_hidden, cudaStream_t st)
+{
+    const int pitch = (int)round_up(d, 64);
+    const int64_t blocks = ceil_div((int64_t)N * ((d + 3) / 4), 32);
+    const unsigned ctas = (unsigned)(blocks < 148 * 16 ? blocks : 148 * 16);
+    return dt == SPR_F32 ? launch_behind(head_sum_kernel<float>, ctas, 256, st, acc, slices, (int64_t)N * pitch, pitch, (int64_t)N, d,
+                                         static_cast<float *>(d_hidden))
+                         : launch_behind(head_sum_kernel<__nv_bfloat16>, ctas, 256, st, acc, slices, (int64_t)N * pitch, pitch,
+                                         (int64_t)N, d, static_cast<__nv_bfloat16 *>(d_hidden));
+}
+
+StreamParams stream_params(const void *hidden, const void *W, int N, int d, int V, int dt)
+{
+    StreamParams p;
+    memset(&p, 0, sizeof p);
+    p.hidden = hidden;
+    p.W = W;
+    p.N = N;
+    p.d = d;
+    p.V = V;
+    p.pitch = (int)round_up(d, 64);
+    p.vec = (size_t)d * elem_size(dt) % 16 == 0;      // the bases are 16-byte aligned
+    return p;
+}
+
+// row statistics of one model by whichever kernel the sizes call for, except the tensor cores'
+cudaError_t other_stats(HeadRow &r, int N, int V, int dt, int *status, cudaStream_t st)
+{
+    if (stream_head(false, N, r.d, V, dt)) {
+        StreamParams p = stream_params(r.hidden, r.W, N, r.d, V, dt);
+        p.part = const_cast<float2 *>(r.part);
+        r.parts = stream_ctas(false, N, r.d, V);
+        return launch_stream(false, dt == SPR_F32, p, st);
+    }
+    SmallParams sp;
+    memset(&sp, 0, sizeof sp);
+    sp.V = V;
+    sp.status = status;
+    small_stats_job(sp.job[0], r.hidden, r.W, N, r.d, V, r.part);
+    r.parts = (int)ceil_div(V, kSmallTile);
+    return launch_small(SMALL_STATS, dt == SPR_F32, sp, 1, st);
+}
+
 // head_loss_grad on the CUDA cores: D in fp32, then both products in one launch
 cudaError_t small_grad(const void *hidden, const void *W, const int32_t *targets, const float *lse, const float *grad_loss, int N,
                        int d, int V, int dt, void *d_hidden, void *d_W, float *D, float *acc, int *tickets, int *status, cudaStream_t st)
@@ -550,14 +628,8 @@ int head_loss(const void *hidden, const void *W, const int32_t *targets, int N, 
     prm.status = at<int>(ws, 0);
     HeadRow h = {hidden, W, at<float2>(ws, lay.part), d, 0};
     cudaError_t e;
-    if (small_head(N, d, V, dt)) {
-        SmallParams sp;
-        memset(&sp, 0, sizeof sp);
-        sp.V = V;
-        sp.status = prm.status;
-        small_stats_job(sp.job[0], hidden, W, N, d, V, h.part);
-        e = launch_small(SMALL_STATS, dt == SPR_F32, sp, 1, st);
-        h.parts = sp.job[0].tiles_n;
+    if (small_head(N, d, V, dt) || stream_head(false, N, d, V, dt)) {
+        e = other_stats(h, N, V, dt, prm.status, st);
     } else {
         PairOperand a, b;
         e = stats_job(prm.job[0], a, b, hidden, W, N, d, V, dt, ws, lay, st);
@@ -598,6 +670,19 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
                                  at<float>(ws, lay.acc), at<int>(ws, lay.tickets), at<int>(ws, 0), st));
     const bool f32 = dt == SPR_F32;
     const size_t es = elem_size(dt);
+    if (stream_head(true, N, d, V, dt)) {
+        StreamParams p = stream_params(hidden, W, N, d, V, dt);
+        p.targets = targets;
+        p.lse = lse;
+        p.grad_loss = grad_loss;
+        p.d_hidden = d_hidden;
+        p.d_W = d_W;
+        p.acc = at<float>(ws, lay.acc);
+        p.status = at<int>(ws, 0);
+        cudaError_t e = launch_stream(true, f32, p, st);
+        if (e == cudaSuccess && d_hidden) e = sum_slices(p.acc, stream_ctas(true, N, d, V), N, d, dt, d_hidden, st);
+        return finish(e);
+    }
     const Pieces pc = pieces(N, d, V, dt);
     const int dp = (int)round_up(d, 64);
     void *hp = at<char>(ws, lay.hidden);
@@ -683,14 +768,7 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
         }
         e = launch_pair(PAIR_OUT, f32, prm, jobs, a, b, st);
     }
-    if (e == cudaSuccess && d_hidden && pc.splits > 1) {
-        const int64_t blocks = ceil_div((int64_t)N * ((d + 3) / 4), 256);
-        const unsigned ctas = (unsigned)(blocks < 148 * 8 ? blocks : 148 * 8);
-        const float *acc = at<float>(ws, lay.acc);
-        if (f32) head_sum_kernel<float><<<ctas, 256, 0, st>>>(acc, pc.splits, (int64_t)N * dp, dp, N, d, static_cast<float *>(d_hidden));
-        else head_sum_kernel<__nv_bfloat16><<<ctas, 256, 0, st>>>(acc, pc.splits, (int64_t)N * dp, dp, N, d, static_cast<__nv_bfloat16 *>(d_hidden));
-        e = cudaGetLastError();
-    }
+    if (e == cudaSuccess && d_hidden && pc.splits > 1) e = sum_slices(at<float>(ws, lay.acc), pc.splits, N, d, dt, d_hidden, st);
     return finish(e);
 }
 
@@ -718,27 +796,20 @@ int verifier_labels_head(const void *p_hidden, const void *p_W, int dp, const vo
     prm.status = at<int>(ws, 0);
     PairOperand a[2], b[2];
     HeadRow p = {p_hidden, p_W, at<float2>(ws, lay.p.part), dp, 0}, q = {q_hidden, q_W, at<float2>(ws, lay.q.part), dq, 0};
-    const bool p_small = small_head(N, dp, V, dt), q_small = small_head(N, dq, V, dt);
     cudaError_t e = cudaSuccess;
-    SmallParams sp;
-    memset(&sp, 0, sizeof sp);
-    sp.V = V;
-    sp.status = prm.status;
-    int smalls = 0, pairs = 0;
-    // the longer products first; a model whose head is small goes to the CUDA cores
+    int pairs = 0;
+    // the longer products first
     for (int i = 0; i < 2 && e == cudaSuccess; ++i) {
         const bool is_p = (i == 0) == (dp >= dq);
         HeadRow &r = is_p ? p : q;
-        if (is_p ? p_small : q_small) {
-            small_stats_job(sp.job[smalls++], r.hidden, r.W, N, r.d, V, r.part);
-            r.parts = (int)ceil_div(V, kSmallTile);
+        if (small_head(N, r.d, V, dt) || stream_head(false, N, r.d, V, dt)) {
+            e = other_stats(r, N, V, dt, prm.status, st);
         } else {
             e = stats_job(prm.job[pairs], a[pairs], b[pairs], r.hidden, r.W, N, r.d, V, dt, ws, is_p ? lay.p : lay.q, st);
             ++pairs;
             r.parts = 2 * (int)ceil_div(V, kPairTile);
         }
     }
-    if (e == cudaSuccess && smalls) e = launch_small(SMALL_STATS, dt == SPR_F32, sp, smalls, st);
     if (e == cudaSuccess && pairs) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, pairs, a, b, st);
     if (e == cudaSuccess) {
         HeadLabels out;

@@ -1,0 +1,271 @@
+// The vocabulary head for a handful of tokens (at most eight): one pass over W.
+//
+// With so few rows a product reads W and does little with it: it is bound by memory, and the tensor-core
+// kernels would lay out fp32 or unaligned heads in the workspace first, three to six times the traffic.
+// Here the hidden states lie in shared memory as fp32 and W streams through registers as it is:
+//   forward    a warp takes four rows of W at a time, a lane 16 bytes of each; the 4 x N logits are
+//              formed by one scatter-reduction across the lanes, and every lane keeps (max, sum of exp) of its own
+//   gradient   a CTA takes 32 rows: first their logits, hence D (in shared memory), as above; then a
+//              thread per 16 bytes of columns reads the rows again (out of L2), writes dW = D^T H for them and adds
+//              D W to its columns of dH, which it keeps in registers.  W is read from memory once, dW
+//              written once: the floor.  The CTAs' dH are added up in order by the kernel behind.
+#include "head_stream.h"
+
+#include "common.cuh"
+#include "launch.h"
+#include "vocab_common.cuh"
+
+namespace spr {
+
+namespace {
+
+constexpr int kStatWarps = 16;
+constexpr int kGradThreads = 512, kGradWarps = kGradThreads / 32;
+constexpr int kGradRows = 32;              // rows of W a CTA takes at a time
+
+// hidden states as fp32 [NT][pitch], zeros behind column d, in rows past N and in rows without a target
+template <typename T>
+__device__ __forceinline__ void stage_hidden(const StreamParams &prm, int nt, float *h, bool masked)
+{
+    const T *src = static_cast<const T *>(prm.hidden);
+    for (int i = threadIdx.x; i < nt * prm.pitch; i += blockDim.x) {
+        const int n = i / prm.pitch, c = i - n * prm.pitch;
+        bool there = n < prm.N && c < prm.d;
+        if (there && masked) {
+            const int t = prm.targets[n];
+            there = t >= 0 && t < prm.V;
+        }
+        h[i] = there ? (float)src[(int64_t)n * prm.d + c] : 0.f;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 load_vec(const T *row, int c, int d, bool vec)      // elements c .. of a row, zeros past d
+{
+    constexpr int N = Vec<T>::N;
+    if (vec) return c < d ? __ldg(reinterpret_cast<const uint4 *>(row + c)) : make_uint4(0u, 0u, 0u, 0u);
+    T x[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = c + e < d ? row[c + e] : (T)0.f;
+    return *reinterpret_cast<const uint4 *>(x);
+}
+
+// v[R * NT] summed over the lanes: lane l gets the sum of value l >> (5 - log2(R NT))
+template <int NV>
+__device__ __forceinline__ float scatter_sum(float (&v)[NV], int lane)
+{
+    int n = NV;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        if (n > 1) {
+            n /= 2;
+#pragma unroll
+            for (int i = 0; i < NV / 2; ++i) {
+                if (i < n) {
+                    const bool up = lane & o;
+                    const float keep = up ? v[i + n] : v[i], send = up ? v[i] : v[i + n];
+                    v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+                }
+            }
+        } else {
+            v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+        }
+    }
+    return v[0];
+}
+__host__ __device__ constexpr int log2i(int x) { return x <= 1 ? 0 : 1 + log2i(x / 2); }
+
+// logits of R rows of W (row0, row0 + 1, ...) and NT tokens; the lane's is the one that scatter_sum gives it
+template <typename T, int NT, int R>
+__device__ __forceinline__ float row_logits(const StreamParams &prm, const float *h, int64_t row0, int lane)
+{
+    constexpr int N = Vec<T>::N;
+    const T *w = static_cast<const T *>(prm.W);
+    uint64_t acc[R * NT];
+#pragma unroll
+    for (int i = 0; i < R * NT; ++i) acc[i] = pack2(0.f, 0.f);
+#pragma unroll 2
+    for (int c = lane * N; c < prm.pitch; c += 32 * N) {
+        uint4 x[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) x[r] = load_vec(w + min(row0 + r, (int64_t)prm.V - 1) * prm.d, c, prm.d, prm.vec);
+        float f[R][N];
+#pragma unroll
+        for (int r = 0; r < R; ++r) Vec<T>::unpack(x[r], f[r]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int e = 0; e < N; e += 4) {
+                const float4 y = *reinterpret_cast<const float4 *>(h + n * prm.pitch + c + e);
+                const uint64_t y0 = pack2(y.x, y.y), y1 = pack2(y.z, y.w);
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    acc[r * NT + n] = fma2(pack2(f[r][e + 2], f[r][e + 3]), y1, fma2(pack2(f[r][e], f[r][e + 1]), y0, acc[r * NT + n]));
+            }
+        }
+    }
+    float v[R * NT];
+#pragma unroll
+    for (int i = 0; i < R * NT; ++i) {
+        float lo, hi;
+        unpack2(acc[i], lo, hi);
+        v[i] = lo + hi;
+    }
+    return scatter_sum<R * NT>(v, lane);
+}
+
+template <typename T, int NT>
+__global__ void __launch_bounds__(32 * kStatWarps) stream_stats_kernel(const StreamParams prm)
+{
+    constexpr int R = 4, kShift = 5 - log2i(R * NT);
+    extern __shared__ float4 hidden4[];
+    float *h = reinterpret_cast<float *>(hidden4);
+    __shared__ float2 part[kStatWarps][8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    pdl_trigger();
+    stage_hidden<T>(prm, NT, h, false);
+    __syncthreads();
+    MS a = {neg_inf(), 0.f};
+    const int idx = lane >> kShift, my_row = idx / NT;
+    const int64_t stride = (int64_t)gridDim.x * kStatWarps * R;
+    for (int64_t row0 = ((int64_t)blockIdx.x * kStatWarps + warp) * R; row0 < prm.V; row0 += stride) {
+        const float l = row_logits<T, NT, R>(prm, h, row0, lane);
+        if (row0 + my_row < prm.V) a = ms_merge(a, MS{l, 1.f});
+    }
+    // merge the four rows' slots of a token (the lanes that differ in the row bits), then the warps
+#pragma unroll
+    for (int o = NT << kShift; o < 32; o <<= 1) {
+        MS b;
+        b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
+        b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
+        a = ms_merge(a, b);
+    }
+    if (lane < (NT << kShift) && (lane & ((1 << kShift) - 1)) == 0) part[warp][idx] = make_float2(a.m, a.s);
+    __syncthreads();
+    const int n = threadIdx.x;
+    if (n < prm.N) {
+        MS s = {part[0][n].x, part[0][n].y};
+#pragma unroll
+        for (int w = 1; w < kStatWarps; ++w) s = ms_merge(s, MS{part[w][n].x, part[w][n].y});
+        prm.part[(int64_t)n * gridDim.x + blockIdx.x] = make_float2(s.m, s.s);
+    }
+}
+
+template <typename T, int NT>
+__global__ void __launch_bounds__(kGradThreads, 1) stream_grad_kernel(const StreamParams prm)
+{
+    constexpr int N = Vec<T>::N, R = kGradRows / kGradWarps, kShift = 5 - log2i(R * NT);
+    extern __shared__ float4 hidden4[];
+    float *h = reinterpret_cast<float *>(hidden4);
+    __shared__ __align__(16) float D[2][kGradRows][NT < 4 ? 4 : NT];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    pdl_trigger();
+    stage_hidden<T>(prm, NT, h, true);
+    // this lane's logit of a row: row idx / NT of the warp's, token idx % NT
+    const int idx = lane >> kShift, my_row = idx / NT, my_tok = idx % NT;
+    int tok = -1;
+    if (my_tok < prm.N) tok = prm.targets[my_tok];
+    const bool keep = tok >= 0 && tok < prm.V;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        for (int n = 0; n < prm.N; ++n)
+            if (prm.targets[n] >= prm.V) raise_status(prm.status, SPR_ERR_BAD_TOKEN);
+    }
+    const float lse = keep ? prm.lse[my_tok] : 0.f, g = keep ? prm.grad_loss[my_tok] : 0.f;
+    __syncthreads();
+    const T *w = static_cast<const T *>(prm.W);
+    T *dw = static_cast<T *>(prm.d_W);
+    const int c0 = threadIdx.x * N;                       // this thread's columns
+    const bool mine = c0 < prm.d;
+    float hr[NT][N], acc[NT][N];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            hr[n][e] = mine ? h[n * prm.pitch + c0 + e] : 0.f;
+            acc[n][e] = 0.f;
+        }
+    int buf = 0;
+    for (int64_t base = (int64_t)blockIdx.x * kGradRows; base < prm.V; base += (int64_t)gridDim.x * kGradRows, buf ^= 1) {
+        const int64_t row = base + warp * R + my_row;
+        const float l = row_logits<T, NT, R>(prm, h, base + warp * R, lane);
+        if ((lane & ((1 << kShift) - 1)) == 0 && idx < R * NT)
+            D[buf][warp * R + my_row][my_tok] = keep && row < prm.V ? g * expf(l - lse) - (row == tok ? g : 0.f) : 0.f;
+        __syncthreads();          // D is there; the other buffer's readers are a barrier behind
+        const int rows = (int)min((int64_t)kGradRows, prm.V - base);
+        if (mine) {
+#pragma unroll 4
+            for (int r = 0; r < rows; ++r) {
+                float f[N];
+                if (prm.d_hidden) Vec<T>::unpack(load_vec(w + (base + r) * prm.d, c0, prm.d, prm.vec), f);
+                float o[N];
+#pragma unroll
+                for (int e = 0; e < N; ++e) o[e] = 0.f;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const float x = D[buf][r][n];
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        o[e] = fmaf(x, hr[n][e], o[e]);
+                        if (prm.d_hidden) acc[n][e] = fmaf(x, f[e], acc[n][e]);
+                    }
+                }
+                if (dw) {
+                    T *p = dw + (base + r) * prm.d + c0;
+                    T y[N];
+#pragma unroll
+                    for (int e = 0; e < N; ++e) y[e] = (T)o[e];
+                    if (prm.vec) {
+                        *reinterpret_cast<uint4 *>(p) = *reinterpret_cast<const uint4 *>(y);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < N; ++e)
+                            if (c0 + e < prm.d) p[e] = y[e];
+                    }
+                }
+            }
+        }
+    }
+    if (prm.d_hidden && mine) {      // acc [cta][N][pitch]
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            if (n < prm.N)
+#pragma unroll
+                for (int e = 0; e < N; e += 4)
+                    *reinterpret_cast<float4 *>(prm.acc + ((int64_t)blockIdx.x * prm.N + n) * prm.pitch + c0 + e) =
+                        make_float4(acc[n][e], acc[n][e + 1], acc[n][e + 2], acc[n][e + 3]);
+    }
+}
+
+template <typename K>
+cudaError_t start(K kernel, const StreamParams &prm, int ctas, int threads, size_t smem, cudaStream_t st)
+{
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    kernel<<<ctas, threads, smem, st>>>(prm);
+    return cudaGetLastError();
+}
+template <typename T, int NT>
+cudaError_t start_any(bool grad, const StreamParams &prm, int ctas, cudaStream_t st)
+{
+    const size_t smem = 4 * (size_t)NT * prm.pitch;
+    return grad ? start(stream_grad_kernel<T, NT>, prm, ctas, kGradThreads, smem, st)
+                : start(stream_stats_kernel<T, NT>, prm, ctas, 32 * kStatWarps, smem, st);
+}
+template <typename T>
+cudaError_t start_typed(bool grad, const StreamParams &prm, int ctas, cudaStream_t st)
+{
+    if (prm.N <= 1) return start_any<T, 1>(grad, prm, ctas, st);
+    if (prm.N <= 2) return start_any<T, 2>(grad, prm, ctas, st);
+    if (prm.N <= 4) return start_any<T, 4>(grad, prm, ctas, st);
+    return start_any<T, 8>(grad, prm, ctas, st);
+}
+
+}  // namespace
+
+cudaError_t launch_stream(bool grad, bool f32, const StreamParams &prm, cudaStream_t st)
+{
+    const int ctas = stream_ctas(grad, prm.N, prm.d, prm.V);
+    return f32 ? start_typed<float>(grad, prm, ctas, st) : start_typed<__nv_bfloat16>(grad, prm, ctas, st);
+}
+
+}  // namespace spr

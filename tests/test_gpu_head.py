@@ -396,3 +396,33 @@ def test_labels_with_heads_on_different_kernels(spr, dtype):
         off = logit_bound(a[0], a[1]).amax(1) + logit_bound(a[2], a[3]).amax(1) + 64 * U * 10
         p, q = (torch.log_softmax(m, 1).gather(1, x.long()[:, None])[:, 0] for m in l)
         assert bool(((ratio.double() / torch.exp(q - p) - 1).abs() <= 2 * off).all()) and ws.device_status() == 0
+
+
+@pytest.mark.parametrize("N,d,V,dtype", [
+    (1, 768, 50257, torch.bfloat16), (1, 4096, 9001, torch.bfloat16), (1, 8, 70000, torch.bfloat16), (4, 1001, 8000, torch.bfloat16),
+    (3, 4095, 3001, torch.bfloat16), (2, 30, 40000, torch.bfloat16), (1, 9000, 2000, torch.bfloat16),
+    (8, 2048, 5003, torch.float32), (7, 1028, 9000, torch.float32), (5, 513, 33000, torch.float32), (2, 100, 99999, torch.float32),
+    (1, 2047, 6001, torch.float32), (4, 4096, 3000, torch.float32), (8, 40, 50257, torch.float32)],
+    ids=lambda v: str(v).replace("torch.", ""))
+def test_a_handful_of_tokens(spr, N, d, V, dtype):
+    """One pass over W: widths that leave lanes or threads idle, rows that start anywhere, a token padded."""
+    h, w, t, gl = problem(N, d, V, dtype, seed=N + d, ignore=0.0)
+    if N > 2:
+        t[1] = -1
+        h[1] = float("nan")
+        clean = h.clone()
+        clean[1] = 0.0
+        ws = workspace(spr, spr.OP_HEAD_LOSS, N, V, d, dtype)
+        loss, lse = spr.head_loss(h, w, t, ws)
+        want = check_loss(spr, clean, w, t)
+        ok = torch.arange(N, device="cuda") != 1
+        assert torch.equal(loss, want[0]) and torch.equal(lse[ok], want[1][ok])
+        wg = workspace(spr, spr.OP_HEAD_LOSS_GRAD, N, V, d, dtype)
+        got = spr.head_loss_grad(h, w, t, want[1], gl, wg)
+        ref = check_grad(spr, clean, w, t, gl, want[1])
+        assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+    else:
+        _, lse = check_loss(spr, h, w, t)
+        dh, dw = check_grad(spr, h, w, t, gl, lse)
+        assert torch.equal(check_grad(spr, h, w, t, gl, lse, want_W=False)[0], dh)
+        assert torch.equal(check_grad(spr, h, w, t, gl, lse, want_hidden=False)[1], dw)
