@@ -1,19 +1,21 @@
 // One Adam step of the linear verifier on hidden states kept in 8 bits (hidden_pack.cu):
 //   z_i = b + sum_j w_j q_ij 2^e_ij,  r = sigma(z) - y,  grad_j = sum_i r_i 2^e_ij q_ij
 // Floor: the packed rows once, 1.03 d bytes a sample.  At that rate an SM takes in some 24 elements a
-// clock, and turning a byte into a float costs as much as the two products it goes into: the pass
-// is bound by instructions before it is bound by memory.  So:
-//   - the dot product stays in integers.  A weight is written as 24 bits relative to the largest of
-//     its 16 (a lane's vector), in three signed bytes, w = 2^E (d0 2^16 + d1 2^8 + d2); then sum q d is
-//     four dp4a per 16 elements and byte, exact, and one conversion per vector is left.  Rounding a
-//     weight costs at most 2^-23 of the largest weight beside it, what fp32 products cost.
-//   - the gradient is formed with columns, not rows, in registers: a thread owns 16 columns and walks
-//     over the rows of a tile.  Its sums are 16 registers instead of the 64 that a warp per row needs, so
-//     that 16 warps fit on an SM, and rows are independent.
-// A CTA takes tiles of consecutive rows (one bulk copy each, a ring of tiles in shared memory):
-// first a warp per row (two for d > 2048) forms the dot products, one barrier, then every warp has the
-// tile's residuals in its lanes and the columns' sums are formed.  Tiles are dealt in a fixed
-// pattern and all sums have a fixed order: a step is reproducible bit for bit.
+// clock, and on the CUDA cores it is instructions that bound the pass: a byte turned into a float costs
+// as much as the two products it goes into (measured: 244 us for 2^18 rows of 2048 that way, 180 us with the dot
+// products in dp4a).  So both sums are integer products on the tensor cores (mma.m16n8k32, s8 x s8 -> s32):
+//   - a block of 32 columns shares its exponent within a row, so a block is one step of the contraction of
+//     the dot products.  A weight is written as 24 bits relative to the largest of its block, in three balanced
+//     signed digits, w = 2^E (256^2 d0 + 256 d1 + d2): three columns of the second operand.  What is left per
+//     block and row is one conversion and the row's scale.  Rounding a weight costs at most 2^-24 of twice
+//     the largest weight of its block, what fp32 products cost.
+//   - for the gradient the contraction runs over the rows of a tile: r_i 2^e_ij of the block, written as 22 bits
+//     relative to the largest of the tile in three digits, times the bytes, which ldmatrix transposes.  The
+//     integer sums are exact; per tile and column one conversion, and an fp32 sum over tiles.
+// A CTA takes tiles of consecutive rows (a bulk copy per row, a ring of tiles in shared memory with a pitch
+// that keeps ldmatrix free of bank conflicts): dot products by all warps, a barrier, residuals by one warp while the
+// others form the sums of their blocks of columns in the tile before.  Tiles are dealt in a
+// fixed pattern and all sums have a fixed order: a step is reproducible bit for bit.
 #include <math.h>
 #include <string.h>
 
@@ -27,10 +29,10 @@ namespace spr {
 
 namespace {
 
-constexpr int kFitThreads = 512;
+constexpr int kFitThreads = 1024;
 constexpr int kFitWarps = kFitThreads / 32;
 constexpr int kMaxTiles = 8;             // tiles of the ring
-constexpr size_t kRingBytes = 200 * 1024;
+constexpr size_t kSmemBytes = 222 * 1024;     // dynamic; the static arrays take some 4.5 KB more
 
 __device__ __forceinline__ uint32_t fit_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ bool fit_wait(uint64_t *bar, uint32_t parity, uint32_t limit)
@@ -49,52 +51,64 @@ __device__ __forceinline__ bool fit_wait(uint64_t *bar, uint32_t parity, uint32_
     return false;
 }
 
-// 2^e of an exponent byte.  -128 marks a block that held an infinity or NaN, with bytes of zero: the same
-// shift makes that minus infinity, and its product with a zero byte NaN.
-__device__ __forceinline__ float block_scale(const unsigned char *p)
+// 2^e of an exponent byte.  -128 marks a block that held an infinity or NaN, with bytes of zero: the same shift
+// makes that minus infinity, and its product with a zero sum NaN.
+__device__ __forceinline__ float block_scale(unsigned char byte)
 {
-    return __int_as_float((int)*reinterpret_cast<const signed char *>(p) * (1 << 23) + 127 * (1 << 23));
+    return __int_as_float((int)(signed char)byte * (1 << 23) + 127 * (1 << 23));
+}
+// three balanced digits of a 24-bit integer: v = 256^2 d0 + 256 d1 + d2, as the bytes 2, 1, 0
+__device__ __forceinline__ uint32_t digits(int v) { return ((uint32_t)v + 0x808080u) ^ 0x808080u; }
+
+// Digits of 32 numbers (a lane each) where the lanes of a product want them: plane p (d0, d1, d2), then for each t
+// of 4 the numbers 4 t .. 4 t + 3 and 16 + 4 t .. + 3.  96 bytes.
+__device__ __forceinline__ void put_digits(unsigned char *dst, uint32_t u, int lane)
+{
+    unsigned char *p = dst + ((lane & 15) >> 2) * 8 + (lane >> 4) * 4 + (lane & 3);
+    p[0] = (unsigned char)(u >> 16);
+    p[32] = (unsigned char)(u >> 8);
+    p[64] = (unsigned char)u;
+}
+// the second operand of a product: column n of it is plane n % 3 (columns past the third are not used)
+__device__ __forceinline__ int digits_at(int lane) { return ((lane >> 2) % 3) * 32 + (lane & 3) * 8; }
+__device__ __forceinline__ uint2 get_digits(const unsigned char *src, int at) { return *reinterpret_cast<const uint2 *>(src + at); }
+
+__device__ __forceinline__ void mma_s8(int (&c)[4], const uint32_t (&a)[4], uint2 b)      // c = A (16 x 32) B (32 x 8)
+{
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y), "r"(0));
+}
+__device__ __forceinline__ void mma_s8_k16(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t b)   // c = A (16 x 16) B (16 x 8)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%7,%7,%7,%7};"
+                 : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3])
+                 : "r"(a0), "r"(a1), "r"(b), "r"(0));
 }
 
-// Sixteen weights as three planes of signed bytes, and their unit 2^E.
-__device__ __forceinline__ float split_weights(const float (&w)[16], uint32_t (&digit)[3][4])
-{
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) top = max(top, __float_as_uint(w[e]) & 0x7fffffffu);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) digit[0][k] = digit[1][k] = digit[2][k] = 0u;
-    if (top >= 0x7f800000u) return __int_as_float(0x7fc00000);      // a weight that is not finite shows
-    // unit 2^E with |w| <= 8355711 units (three digits reach that); weights below 2^-100 count as zero
-    int E = max((int)(top >> 23) - 127, -100) - 22;
-    if (rintf(ldexpf(__uint_as_float(top), -E)) > 8355711.f) ++E;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        const int v = __float2int_rn(ldexpf(w[e], -E));
-        const int d2 = (int)(signed char)(v & 255), v1 = (v - d2) >> 8;
-        const int d1 = (int)(signed char)(v1 & 255), d0 = (v1 - d1) >> 8;
-        digit[0][e >> 2] |= (uint32_t)(d0 & 255) << (8 * (e & 3));
-        digit[1][e >> 2] |= (uint32_t)(d1 & 255) << (8 * (e & 3));
-        digit[2][e >> 2] |= (uint32_t)(d2 & 255) << (8 * (e & 3));
-    }
-    return ldexpf(1.f, E);
-}
+// shared memory of a row: ldmatrix reads eight rows at once, 16 bytes of each, so the pitch is an odd number of those
+__host__ __device__ constexpr int row_pitch(int d) { return (pack8_pitch(d) / 16) % 2 ? pack8_pitch(d) : pack8_pitch(d) + 16; }
 
-// VPL: 16-byte vectors per lane of a row; WPR: warps per row; T: rows per tile
-template <int VPL, int WPR, int T>
+// NB: blocks of 32 columns per warp; T: rows per tile (16 or 32)
+template <int NB, int T>
 __global__ void __launch_bounds__(kFitThreads, 1) train8_kernel(const TrainParams prm, int ring_tiles)
 {
-    constexpr int kRowsPerWarp = T * WPR / kFitWarps;     // rows a warp forms dot products of, per tile
-    static_assert(kRowsPerWarp >= 1 && T <= 64, "tile height");
-    constexpr int kLaneRows = (T + 31) / 32;
-    extern __shared__ __align__(128) unsigned char tiles[];
+    constexpr int kRowGroups = T / 16;                     // of 16 rows, for the dot products
+    constexpr int kNB1 = NB * kRowGroups;                  // blocks a warp takes of its row group there
+    constexpr int kSlices = kFitWarps / kRowGroups;        // warps that share a row's dot product
+    constexpr int kDig = NB < 2 ? NB : 2;                  // blocks whose residuals a warp splits at a time
+    extern __shared__ __align__(128) unsigned char smem[];
     __shared__ __align__(8) uint64_t bars[kMaxTiles];
-    __shared__ float zpart[2][T][WPR];
-    __shared__ float res_of[kFitWarps][T];    // the tile's residuals, a copy per warp
+    __shared__ float zpart[2][kSlices][T];
+    __shared__ float residual[2][32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int d = prm.d, nv = d / 16;
-    const int pitch = pack8_pitch(d);
-    const uint32_t tile_bytes = (uint32_t)(T * pitch);
+    const int d = prm.d, blocks = (d + 31) / 32;
+    const int gpitch = pack8_pitch(d), pitch = row_pitch(d);
+    const int tile_bytes = T * pitch;
+    // digits of the weights [blocks][96], of the scaled residuals (kDig blocks per warp), units of the weights [blocks], the ring
+    unsigned char *wdig = smem, *rdig = wdig + kFitWarps * NB * 96 + warp * kDig * 96;
+    float *unit = reinterpret_cast<float *>(smem + kFitWarps * (NB + kDig) * 96);
+    unsigned char *tiles = reinterpret_cast<unsigned char *>(unit + kFitWarps * NB);
     pdl_trigger();
 
     // this CTA's tiles: blockIdx.x, + gridDim.x, ...; only the last tile of the data can be short
@@ -102,166 +116,195 @@ __global__ void __launch_bounds__(kFitThreads, 1) train8_kernel(const TrainParam
     const int n = (int64_t)blockIdx.x < all ? (int)((all - blockIdx.x + gridDim.x - 1) / gridDim.x) : 0;
     auto first_row = [&](int k) { return ((int64_t)blockIdx.x + (int64_t)k * gridDim.x) * T; };
     auto rows_of = [&](int k) { return (int)min((int64_t)T, prm.N - first_row(k)); };
+    // Every warp asks for a row of tile k: a copy takes about 100 clocks to issue, and 32 of them in one warp as long as a tile
     auto fetch = [&](int k) {
-        const uint32_t bytes = (uint32_t)(rows_of(k) * pitch);
-        uint64_t *bar = &bars[k % ring_tiles];
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(fit_addr(bar)), "r"(bytes) : "memory");
-        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                         fit_addr(tiles + (size_t)(k % ring_tiles) * tile_bytes)),
-                     "l"(static_cast<const unsigned char *>(prm.hidden) + first_row(k) * pitch), "r"(bytes), "r"(fit_addr(bar))
-                     : "memory");
+        if (lane == 0 && warp < T) {
+            const int rows = rows_of(k);
+            uint64_t *bar = &bars[k % ring_tiles];
+            if (warp == 0)
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(fit_addr(bar)), "r"((uint32_t)(rows * gpitch)) : "memory");
+            if (warp < rows)
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                                 fit_addr(tiles + (k % ring_tiles) * tile_bytes + warp * pitch)),
+                             "l"(static_cast<const unsigned char *>(prm.hidden) + (first_row(k) + warp) * gpitch), "r"((uint32_t)gpitch),
+                             "r"(fit_addr(bar))
+                             : "memory");
+        }
     };
     if (tid == 0) {
         for (int s = 0; s < ring_tiles; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(fit_addr(&bars[s])) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int k = 0; !(prm.test_flags & TRAIN_TEST_NO_FETCH) && k < ring_tiles && k < n; ++k) fetch(k);
     }
-    // labels of the next tile, one row per lane (a label fetched when it is wanted would cost a trip to memory)
-    auto tile_labels = [&](int k, float (&y)[kLaneRows]) {
-#pragma unroll
-        for (int h = 0; h < kLaneRows; ++h) {
-            const int r = lane + 32 * h;
-            y[h] = k < n && r < rows_of(k) && r < T ? (float)prm.labels[first_row(k) + r] : 0.f;
-        }
+    __syncthreads();
+    for (int k = 0; !(prm.test_flags & TRAIN_TEST_NO_FETCH) && k < ring_tiles && k < n; ++k) fetch(k);
+    // Labels, one row per lane, two tiles ahead and as the bytes they are: a label fetched when it is wanted would cost
+    // a trip to memory.
+    auto tile_label = [&](int k) -> uint32_t {
+        const int64_t i = first_row(k) + lane;
+        return prm.labels[k < n && lane < T && i < prm.N ? i : 0];
     };
-    float y_next[kLaneRows];
-    tile_labels(0, y_next);
+    uint32_t y_raw[2] = {0u, 0u};
+    if (warp < 2) {
+        y_raw[0] = tile_label(0);
+        y_raw[1] = tile_label(1);
+    }
 
-    // weights of this lane's vectors of a row: v0 + 32 j
-    const int part = warp % WPR, v0 = part * VPL * 32 + lane;
-    uint32_t digit[VPL][3][4];
-    float unit[VPL];
-    int at[VPL], scale_at[VPL];      // a lane past the row's end reads the last vector, with weights of zero
-#pragma unroll
-    for (int j = 0; j < VPL; ++j) {
-        const int vi = v0 + 32 * j;
-        at[j] = min(vi, nv - 1) * 16;
-        scale_at[j] = d + (min(vi, nv - 1) >> 1);
-        float w[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = vi < nv ? prm.theta[vi * 16 + e] : 0.f;
-        unit[j] = split_weights(w, digit[j]);
+    for (int b = warp; b < kFitWarps * NB; b += kFitWarps) {
+        const int c = b * 32 + lane;
+        const float w = c < d ? prm.theta[c] : 0.f;
+        const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(w) & 0x7fffffffu);
+        // unit 2^E with |w| <= 8355711 units (three digits reach that); weights below 2^-100 count as zero
+        int E = max((int)(top >> 23) - 127, -100) - 22;
+        if (rintf(ldexpf(__uint_as_float(top), -E)) > 8355711.f) ++E;
+        const bool finite = top < 0x7f800000u;             // a weight that is not finite shows in every sum
+        put_digits(wdig + b * 96, finite ? digits(__float2int_rn(ldexpf(w, -E))) : 0u, lane);
+        if (lane == 0) unit[b] = finite ? ldexpf(1.f, E) : __int_as_float(0x7fc00000);
     }
     const float bias = prm.theta[d];
 
-    // columns of this thread: vector cv, rows sub, sub + subs, ... of every tile
-    const int subs = min(kFitThreads / nv, T);
-    const int cv = tid % nv, sub = tid / nv;
-    uint64_t acc[8];
+    // a lane's part of a product's result: columns 2 (lane % 4) and + 1, hence d0 and d1, or d2, or nothing
+    const float k0 = (lane & 3) == 0 ? 65536.f : (lane & 3) == 1 ? 1.f : 0.f, k1 = (lane & 3) == 0 ? 256.f : 0.f;
+    const int rg = warp % kRowGroups, slice = warp / kRowGroups;
+    const uint32_t row_at = (uint32_t)((rg * 16 + (lane & 7) + ((lane >> 3) & 1) * 8) * pitch + (lane >> 4) * 16);      // ldmatrix of 16 x 32
+    const uint32_t col_at = (uint32_t)((lane & (T - 1)) * pitch);                                                       // and of T x 16
+    const int dig_at = digits_at(lane);
+    float grad[NB][4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = pack2(0.f, 0.f);
-    double acc_b = 0.0, acc_loss = 0.0;        // warp 0
-    const uint64_t off = pack2(-8388736.f, -8388736.f);
-    __syncthreads();                           // the barriers are set up
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) grad[i][e] = 0.f;
+    double acc_b = 0.0, acc_loss = 0.0;        // warp 1
+    __syncthreads();                           // the barriers are set up and the weights' digits there
 
+    // One barrier per tile: after that of tile k its dot products are there, and while one warp turns them into
+    // residuals the others are at the columns of tile k - 1.
     bool ok = true;
     int k = 0;
-    for (; k < n; ++k) {
-        const unsigned char *tile = tiles + (size_t)(k % ring_tiles) * tile_bytes;
-        ok = fit_wait(&bars[k % ring_tiles], (uint32_t)(k / ring_tiles) & 1u, prm.spin_limit);
-        float y[kLaneRows];
+    for (; k <= n; ++k) {
+        if (k < n) {
+            // ---- dot products of tile k: 16 rows by this warp's blocks; rows behind the last hold older bytes and are not used
+            const unsigned char *tile = tiles + (k % ring_tiles) * tile_bytes;
+            const uint32_t tile_addr = fit_addr(tile);
+            ok = fit_wait(&bars[k % ring_tiles], (uint32_t)(k / ring_tiles) & 1u, prm.spin_limit);
+            float z0 = 0.f, z1 = 0.f;              // rows lane / 4 and + 8
+            const unsigned char *e0 = tile + (rg * 16 + (lane >> 2)) * pitch + d + slice * kNB1, *e1 = e0 + 8 * pitch;
 #pragma unroll
-        for (int h = 0; h < kLaneRows; ++h) y[h] = y_next[h];
-        tile_labels(k + 1, y_next);
-        const int rows = rows_of(k);
-        // ---- dot products, a warp (pair) per row; rows behind the last hold older bytes and are not used
-        float dot[kRowsPerWarp];
-#pragma unroll
-        for (int i = 0; i < kRowsPerWarp; ++i) {
-            const unsigned char *row = tile + (warp / WPR + i * (kFitWarps / WPR)) * pitch;
-            dot[i] = 0.f;
-#pragma unroll
-            for (int j = 0; j < VPL; ++j) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(row + at[j]);
-                const int q[4] = {(int)x.x, (int)x.y, (int)x.z, (int)x.w};
-                int s0 = 0, s1 = 0, s2 = 0;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    s0 = __dp4a(q[c], (int)digit[j][0][c], s0);
-                    s1 = __dp4a(q[c], (int)digit[j][1][c], s1);
-                    s2 = __dp4a(q[c], (int)digit[j][2][c], s2);
+            for (int i = 0; i < kNB1; ++i) {
+                const int b = slice * kNB1 + i;
+                if (b < blocks) {
+                    uint32_t a[4];
+                    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                                 : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3])
+                                 : "r"(tile_addr + row_at + b * 32));
+                    int c[4];
+                    mma_s8(c, a, get_digits(wdig + b * 96, dig_at));
+                    const float u = unit[b];
+                    z0 = fmaf(fmaf((float)c[0], k0, (float)c[1] * k1) * u, block_scale(e0[i]), z0);
+                    z1 = fmaf(fmaf((float)c[2], k0, (float)c[3] * k1) * u, block_scale(e1[i]), z1);
                 }
-                const float s = fmaf((float)s0, 65536.f, (float)(s1 * 256 + s2));     // |s1| < 2^18
-                dot[i] = fmaf(s * unit[j], block_scale(row + scale_at[j]), dot[i]);
+            }
+            z0 += __shfl_xor_sync(0xffffffffu, z0, 1);
+            z1 += __shfl_xor_sync(0xffffffffu, z1, 1);
+            if ((lane & 3) == 0) {
+                zpart[k & 1][slice][rg * 16 + (lane >> 2)] = z0;
+                zpart[k & 1][slice][rg * 16 + (lane >> 2) + 8] = z1;
             }
         }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-            for (int i = 0; i < kRowsPerWarp; ++i) dot[i] += __shfl_xor_sync(0xffffffffu, dot[i], o);
-        if (lane == 0) {
-#pragma unroll
-            for (int i = 0; i < kRowsPerWarp; ++i) zpart[k & 1][warp / WPR + i * (kFitWarps / WPR)][part] = dot[i];
-        }
-        ok = __syncthreads_and(ok) != 0;       // the dot products are there, and the tile before this one is done with
+        ok = __syncthreads_and(ok) != 0;
         if (!ok) break;
-        if (tid == 0 && k > 0 && k - 1 + ring_tiles < n) fetch(k - 1 + ring_tiles);
-        // ---- residuals, a row per lane, in every warp
-#pragma unroll
-        for (int h = 0; h < kLaneRows; ++h) {
-            const int r = lane + 32 * h;
+        // tile k - 2 is done with
+        if (k > 1 && k - 2 + ring_tiles < n) fetch(k - 2 + ring_tiles);
+        if (warp < 2 && k < n) {
+            // ---- residuals of tile k, a row per lane: warp 0 hands them on, warp 1 has the loss and the bias's gradient
+            const int rows = rows_of(k);
+            const float y = (float)y_raw[0];
+            y_raw[0] = y_raw[1];
+            y_raw[1] = tile_label(k + 2);
             float z = bias;
-            if (r < T) {
-                z += zpart[k & 1][r][0];
-                if (WPR > 1) z += zpart[k & 1][r][WPR - 1];
-            }
-            const float res = r < rows ? 1.f / (1.f + expf(-z)) - y[h] : 0.f;
-            if (r < T) res_of[warp][r] = res;
-            if (warp == 0 && r < rows) {
-                acc_b += (double)res;
-                acc_loss += (double)(fmaxf(z, 0.f) + log1pf(expf(-fabsf(z))) - y[h] * z);
-            }
-        }
-        __syncwarp();
-        // ---- columns
-        const unsigned char *row = tile + sub * pitch + cv * 16, *row_e = tile + sub * pitch + d + (cv >> 1);
-#pragma unroll 4
-        for (int r = sub < subs ? sub : rows; r < rows; r += subs, row += subs * pitch, row_e += subs * pitch) {
-            const uint4 x = *reinterpret_cast<const uint4 *>(row);
-            const float rs = res_of[warp][r] * block_scale(row_e);
-            const uint64_t rs2 = pack2(rs, rs);
-            // byte + 128 as the low mantissa byte of 2^23, which is then taken off
-            const uint32_t w[4] = {x.x ^ 0x80808080u, x.y ^ 0x80808080u, x.z ^ 0x80808080u, x.w ^ 0x80808080u};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const uint64_t a = pack2(__uint_as_float(__byte_perm(w[c], 0x4b000000u, 0x7440)),
-                                         __uint_as_float(__byte_perm(w[c], 0x4b000000u, 0x7441)));
-                const uint64_t b = pack2(__uint_as_float(__byte_perm(w[c], 0x4b000000u, 0x7442)),
-                                         __uint_as_float(__byte_perm(w[c], 0x4b000000u, 0x7443)));
-                acc[2 * c] = fma2(rs2, add2(a, off), acc[2 * c]);
-                acc[2 * c + 1] = fma2(rs2, add2(b, off), acc[2 * c + 1]);
+            for (int s = 0; s < kSlices; ++s) z += zpart[k & 1][s][lane & (T - 1)];
+            const float r = lane < rows ? 1.f / (1.f + expf(-z)) - y : 0.f;
+            if (warp == 0) {
+                residual[k & 1][lane] = r;
+            } else if (lane < rows) {
+                acc_b += (double)r;
+                acc_loss += (double)(fmaxf(z, 0.f) + log1pf(expf(-fabsf(z))) - y * z);
             }
         }
-        __syncwarp();                          // the residuals are overwritten for the next tile
+        if (k > 0) {
+            // ---- columns of this warp's blocks in tile k - 1
+            const unsigned char *tile = tiles + ((k - 1) % ring_tiles) * tile_bytes;
+            const uint32_t tile_addr = fit_addr(tile);
+            const float r = residual[(k - 1) & 1][lane];
+            const float show = __any_sync(0xffffffffu, r != r) ? __int_as_float(0x7fc00000) : 1.f;    // NaN has no digits
+            const unsigned char *er = tile + (lane & (T - 1)) * pitch + d + warp * NB;
+#pragma unroll
+            for (int i0 = 0; i0 < NB; i0 += kDig) {
+                float scale[kDig];
+                __syncwarp();                      // the digits that stood there are read
+#pragma unroll
+                for (int i = 0; i < kDig; ++i) {
+                    // blocks that the row has (the exponent bytes end with them), and rows that the tile has (r is zero past them)
+                    const bool there = i0 + i < NB && warp * NB + i0 + i < blocks && r != 0.f;
+                    const float v = there ? r * block_scale(er[i0 + i]) : 0.f;
+                    const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu);
+                    const int E = max((int)(top >> 23) - 127, -100) - 21;          // |v| < 2^22 units of 2^E
+                    // v 2^-E + 1.5 2^23 rounds to the unit; the integer stands in the low bits of the sum
+                    const int q = (int)(__float_as_uint(fmaf(v, __int_as_float((127 - E) << 23), 12582912.f)) - 0x4b400000u);
+                    put_digits(rdig + i * 96, digits(q), lane);
+                    scale[i] = __int_as_float((E + 127) << 23) * show;
+                }
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < kDig; ++i) {
+                    const int b = warp * NB + i0 + i;
+                    if (i0 + i >= NB || b >= blocks) break;
+                    const uint2 bd = get_digits(rdig + i * 96, dig_at);
+                    const float s = scale[i];
+                    float *g = grad[i0 + i];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t at = tile_addr + col_at + b * 32 + h * 16;      // a last block of 16 reads on, into the row's padding
+                        int c[4];
+                        if constexpr (T == 32) {
+                            uint32_t a[4];
+                            asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];"
+                                         : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3])
+                                         : "r"(at));
+                            mma_s8(c, a, bd);
+                        } else {
+                            uint32_t a0, a1;
+                            asm volatile("ldmatrix.sync.aligned.m16n16.x1.trans.shared.b8 {%0,%1}, [%2];" : "=r"(a0), "=r"(a1) : "r"(at));
+                            mma_s8_k16(c, a0, a1, bd.x);
+                        }
+                        g[2 * h] = fmaf(fmaf((float)c[0], k0, (float)c[1] * k1), s, g[2 * h]);
+                        g[2 * h + 1] = fmaf(fmaf((float)c[2], k0, (float)c[3] * k1), s, g[2 * h + 1]);
+                    }
+                }
+            }
+        }
     }
     if (!ok) {
         // A wait ran out: report it, then give the copies still on their way the same bounded time to
         // land before the CTA's shared memory goes away.
         if (tid == 0) {
             raise_status(prm.status, SPR_ERR_TIMEOUT);
-            for (int i = k; !(prm.test_flags & TRAIN_TEST_NO_FETCH) && i < n && i < k - 1 + ring_tiles; ++i)
+            for (int i = k; !(prm.test_flags & TRAIN_TEST_NO_FETCH) && i < n && i < k - 2 + ring_tiles; ++i)
                 fit_wait(&bars[i % ring_tiles], (uint32_t)(i / ring_tiles) & 1u, prm.spin_limit);
         }
+        __syncthreads();
     }
-    __syncthreads();
-    // sums of the row subsets, in order
-    float *red = reinterpret_cast<float *>(tiles);
-    if (sub < subs) {
+    float *out = prm.part + (int64_t)blockIdx.x * (d + 2);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float lo, hi;
-            unpack2(acc[e], lo, hi);
-            *reinterpret_cast<float2 *>(red + (size_t)sub * d + cv * 16 + 2 * e) = make_float2(lo, hi);
+    for (int i = 0; i < NB; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float s = grad[i][e] + __shfl_xor_sync(0xffffffffu, grad[i][e], 1);
+            const int c = (warp * NB + i) * 32 + (e >> 1) * 16 + (e & 1) * 8 + (lane >> 2);
+            if ((lane & 3) == 0 && c < d) out[c] = s;
         }
     }
-    __syncthreads();
-    float *out = prm.part + (int64_t)blockIdx.x * (d + 2);
-    for (int j = tid; j < d; j += kFitThreads) {
-        float s = red[j];
-        for (int i = 1; i < subs; ++i) s += red[(size_t)i * d + j];
-        out[j] = s;
-    }
-    if (warp == 0) {
+    if (warp == 1) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             acc_b += __shfl_xor_sync(0xffffffffu, acc_b, o);
@@ -314,7 +357,7 @@ __global__ void __launch_bounds__(256) train8_adam_kernel(const TrainParams prm,
     prm.theta[j] = (float)((double)prm.theta[j] - prm.lr * (m / c1) / (sqrt(v / c2) + prm.eps));
 }
 
-template <int VPL, int WPR, int T>
+template <int NB, int T>
 cudaError_t launch_train8(const TrainParams &tp, cudaStream_t st)
 {
     static std::atomic<bool> attr_set[64];
@@ -322,9 +365,8 @@ cudaError_t launch_train8(const TrainParams &tp, cudaStream_t st)
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
-    const size_t tile = (size_t)T * pack8_pitch(tp.d);
     if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-        e = cudaFuncSetAttribute(train8_kernel<VPL, WPR, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes + 4096);
+        e = cudaFuncSetAttribute(train8_kernel<NB, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
         if (e != cudaSuccess) return e;
         if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
     }
@@ -332,14 +374,13 @@ cudaError_t launch_train8(const TrainParams &tp, cudaStream_t st)
     const int64_t all = (tp.N + T - 1) / T;
     p.ctas = (int)(all < sms ? all : sms);
     if (p.ctas > kTrainMaxCtas) p.ctas = kTrainMaxCtas;
-    int64_t ring = (int64_t)(kRingBytes + 4096) / (int64_t)tile;
+    const size_t tables = kFitWarps * ((NB + (NB < 2 ? NB : 2)) * 96 + NB * sizeof(float)), tile = (size_t)T * row_pitch(tp.d);
+    int64_t ring = (int64_t)((kSmemBytes - tables) / tile);
     if (ring > kMaxTiles) ring = kMaxTiles;
     const int64_t most = (all + p.ctas - 1) / p.ctas;       // tiles of one CTA
+    if (ring < 3 && most >= 3) return cudaErrorInvalidConfiguration;      // two tiles are in use while the next arrives
     if (ring > most) ring = most;
-    size_t smem = (size_t)ring * tile;
-    const size_t red = 4 * (size_t)kFitThreads * 16;        // the row subsets' sums: subs * d <= 512 * 16 floats
-    if (smem < red) smem = red;
-    train8_kernel<VPL, WPR, T><<<p.ctas, kFitThreads, smem, st>>>(p, (int)ring);
+    train8_kernel<NB, T><<<p.ctas, kFitThreads, tables + (size_t)ring * tile, st>>>(p, (int)ring);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};          // set up while the gradient kernel ends
@@ -354,18 +395,14 @@ cudaError_t launch_train8(const TrainParams &tp, cudaStream_t st)
     return cudaLaunchKernelEx(&cfg, train8_adam_kernel, p, 1.0 - pow(p.beta1, (double)p.t), 1.0 - pow(p.beta2, (double)p.t));
 }
 
-// Tiles of 16, 32 or 64 rows: about 64 KB, so that three fit and a barrier is worth some thousand
-// elements; no higher than what deals every SM a tile.
+// Tiles of 32 rows, of 16 above 2048 columns: three of every width fit the ring.
 cudaError_t launch_train8_any(const TrainParams &tp, cudaStream_t st)
 {
-    const int vpl = (tp.d / 16 + 31) / 32;
-    const bool few = tp.N < (int64_t)148 * 64;
-    if (vpl <= 1) return few ? launch_train8<1, 1, 16>(tp, st) : launch_train8<1, 1, 64>(tp, st);
-    if (vpl <= 2) return few ? launch_train8<2, 1, 16>(tp, st) : launch_train8<2, 1, 64>(tp, st);
-    if (vpl <= 3) return few ? launch_train8<3, 1, 16>(tp, st) : launch_train8<3, 1, 32>(tp, st);
-    if (vpl <= 4) return few ? launch_train8<4, 1, 16>(tp, st) : launch_train8<4, 1, 32>(tp, st);
-    if (vpl <= 6) return launch_train8<3, 2, 16>(tp, st);
-    return launch_train8<4, 2, 16>(tp, st);
+    const int nb = ((tp.d + 31) / 32 + kFitWarps - 1) / kFitWarps;
+    if (nb <= 1) return launch_train8<1, 32>(tp, st);
+    if (nb <= 2) return launch_train8<2, 32>(tp, st);
+    if (nb <= 3) return launch_train8<3, 16>(tp, st);
+    return launch_train8<4, 16>(tp, st);
 }
 
 }  // namespace
