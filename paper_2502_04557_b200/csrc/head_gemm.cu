@@ -232,6 +232,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
     // both CTAs have set up their barriers: copies and commits of one count on the other's
     cluster_arrive();
     cluster_wait();
+    pdl_wait();      // launched behind a kernel of the same call: nothing of its results is touched before this
 
     long long issued = 0;
     if (warp == 0) {
@@ -568,7 +569,7 @@ bool make_map(CUtensorMap *map, const PairOperand &t)
 }
 
 template <int EPI, typename T>
-cudaError_t launch(const CUtensorMap (&maps)[4], const PairParams &prm, int ctas, int dev, cudaStream_t st)
+cudaError_t launch(const CUtensorMap (&maps)[4], const PairParams &prm, int ctas, int dev, bool behind, cudaStream_t st)
 {
     static std::atomic<bool> attr_set[64];   // host threads may race to set it: all of them store `true`
     if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
@@ -577,8 +578,17 @@ cudaError_t launch(const CUtensorMap (&maps)[4], const PairParams &prm, int ctas
         if (e != cudaSuccess) return e;
         if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
     }
-    pair_kernel<EPI, T><<<ctas, kPairThreads, kPairSmem, st>>>(maps[0], maps[1], maps[2], maps[3], prm);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(kPairThreads);
+    cfg.dynamicSmemBytes = kPairSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = behind ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, pair_kernel<EPI, T>, maps[0], maps[1], maps[2], maps[3], prm);
 }
 
 }  // namespace
@@ -588,16 +598,18 @@ static thread_local int t_test_flags = 0;
 static thread_local unsigned t_spin_limit = 0;
 
 cudaError_t launch_pair(PairEpilogue epi, bool f32, PairParams &prm, int njobs, const PairOperand *a,
-                        const PairOperand *b, cudaStream_t st)
+                        const PairOperand *b, bool behind, cudaStream_t st)
 {
     int dev = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
     CUtensorMap maps[4];
-    for (int i = 0; i < 2; ++i) {
-        const int k = i < njobs ? i : 0;
-        if (!make_map(&maps[2 * i], a[k]) || !make_map(&maps[2 * i + 1], b[k])) return cudaErrorInvalidValue;
+    for (int i = 0; i < njobs; ++i)
+        if (!make_map(&maps[2 * i], a[i]) || !make_map(&maps[2 * i + 1], b[i])) return cudaErrorInvalidValue;
+    if (njobs == 1) {       // not used
+        maps[2] = maps[0];
+        maps[3] = maps[1];
     }
     int pairs = sms / 2 < kMaxPairs ? sms / 2 : kMaxPairs;
     int64_t total = 0;
@@ -633,11 +645,11 @@ cudaError_t launch_pair(PairEpilogue epi, bool f32, PairParams &prm, int njobs, 
     prm.spin_limit = t_spin_limit ? t_spin_limit : kSpinLimit;
     prm.test_flags = t_test_flags;
     switch (epi) {
-    case PAIR_STATS: return launch<PAIR_STATS, float>(maps, prm, 2 * pairs, dev, st);    // the same for both types
-    case PAIR_DLOGITS: return f32 ? launch<PAIR_DLOGITS, float>(maps, prm, 2 * pairs, dev, st)
-                                  : launch<PAIR_DLOGITS, __nv_bfloat16>(maps, prm, 2 * pairs, dev, st);
-    default: return f32 ? launch<PAIR_OUT, float>(maps, prm, 2 * pairs, dev, st)
-                        : launch<PAIR_OUT, __nv_bfloat16>(maps, prm, 2 * pairs, dev, st);
+    case PAIR_STATS: return launch<PAIR_STATS, float>(maps, prm, 2 * pairs, dev, behind, st);    // the same for both types
+    case PAIR_DLOGITS: return f32 ? launch<PAIR_DLOGITS, float>(maps, prm, 2 * pairs, dev, behind, st)
+                                  : launch<PAIR_DLOGITS, __nv_bfloat16>(maps, prm, 2 * pairs, dev, behind, st);
+    default: return f32 ? launch<PAIR_OUT, float>(maps, prm, 2 * pairs, dev, behind, st)
+                        : launch<PAIR_OUT, __nv_bfloat16>(maps, prm, 2 * pairs, dev, behind, st);
     }
 }
 

@@ -69,8 +69,9 @@ struct PairOperand {
     int64_t pitch;      // elements, a multiple of 8
 };
 
-// njobs products; a[i], b[i] are the operands of job[i].  Fills in the schedule.
+// njobs products; a[i], b[i] are the operands of job[i].  Fills in the schedule.  behind: the kernel before it in the
+// stream is one of the same call, and this one may set itself up while that ends.
 cudaError_t launch_pair(PairEpilogue epi, bool f32, PairParams &prm, int njobs, const PairOperand *a,
-                        const PairOperand *b, cudaStream_t st);
+                        const PairOperand *b, bool behind, cudaStream_t st);
 
 }  // namespace spr

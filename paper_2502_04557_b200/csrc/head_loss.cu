@@ -633,7 +633,7 @@ int head_loss(const void *hidden, const void *W, const int32_t *targets, int N, 
     } else {
         PairOperand a, b;
         e = stats_job(prm.job[0], a, b, hidden, W, N, d, V, dt, ws, lay, st);
-        if (e == cudaSuccess) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, 1, &a, &b, st);
+        if (e == cudaSuccess) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, 1, &a, &b, needs_pack(d, dt), st);
         h.parts = 2 * prm.job[0].tiles_n;
     }
     if (e == cudaSuccess) {
@@ -717,7 +717,7 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
         j.lse = lse;
         j.grad_loss = grad_loss;
         j.targets = targets;
-        e = launch_pair(PAIR_DLOGITS, f32, prm, 1, &hv, &wp, st);
+        e = launch_pair(PAIR_DLOGITS, f32, prm, 1, &hv, &wp, true, st);
         if (e != cudaSuccess) break;
 
         memset(&prm, 0, sizeof prm);
@@ -766,7 +766,7 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
             b[jobs] = hv;
             ++jobs;
         }
-        e = launch_pair(PAIR_OUT, f32, prm, jobs, a, b, st);
+        e = launch_pair(PAIR_OUT, f32, prm, jobs, a, b, true, st);
     }
     if (e == cudaSuccess && d_hidden && pc.splits > 1) e = sum_slices(at<float>(ws, lay.acc), pc.splits, N, d, dt, d_hidden, st);
     return finish(e);
@@ -810,7 +810,7 @@ int verifier_labels_head(const void *p_hidden, const void *p_W, int dp, const vo
             r.parts = 2 * (int)ceil_div(V, kPairTile);
         }
     }
-    if (e == cudaSuccess && pairs) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, pairs, a, b, st);
+    if (e == cudaSuccess && pairs) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, pairs, a, b, false, st);
     if (e == cudaSuccess) {
         HeadLabels out;
         memset(&out, 0, sizeof out);
