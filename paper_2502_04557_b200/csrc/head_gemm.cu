@@ -38,9 +38,6 @@
 #include "tensor_pair.cuh"
 #include "vocab_common.cuh"
 
-#ifndef PROMO
-#define PROMO CU_TENSOR_MAP_L2_PROMOTION_L2_128B
-#endif
 namespace spr {
 
 namespace {
@@ -564,7 +561,7 @@ bool make_map(CUtensorMap *map, const PairOperand &t)
     const cuuint32_t box[2] = {64, 64};
     const cuuint32_t elem[2] = {1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(t.base), dims, strides, box, elem,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, PROMO,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
