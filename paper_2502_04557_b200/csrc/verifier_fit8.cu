@@ -1,6 +1,6 @@
 // One Adam step of the linear verifier on hidden states kept in 8 bits (hidden_pack.cu):
 //   z_i = b + sum_j w_j q_ij 2^e_ij,  r = sigma(z) - y,  grad_j = sum_i r_i 2^e_ij q_ij
-// Floor: the packed rows once, 1.03 d bytes a sample (2^18 rows of 2048: 554 MB, 86 us; measured 157 us).  At that
+// Floor: the packed rows once, 1.03 d bytes a sample (2^18 rows of 2048: 554 MB, 86 us; measured 111 us).  At that
 // rate an SM takes in some 24 elements a clock, and on the CUDA cores it is instructions that bound the pass: a byte
 // turned into a float costs as much as the two products it goes into (measured: 244 us that way, 180 us with the
 // dot products in dp4a).  So both sums are integer products on the tensor cores (mma.m16n8k32, s8 x s8 -> s32):
@@ -12,12 +12,16 @@
 //   - for the gradient the contraction runs over the rows of a tile: r_i 2^e_ij of the block, written as 22 bits
 //     relative to the largest of the tile in three digits, times the bytes, which ldmatrix transposes.  The
 //     integer sums are exact; per tile and column one conversion, and an fp32 sum over tiles.
-// A CTA takes tiles of consecutive rows through a ring in shared memory, by TMA in boxes of 128 bytes by all rows
-// with the 128-byte swizzle, which keeps ldmatrix free of bank conflicts (a copy per row into a padded pitch took
-// 100 clocks each to issue, half of a tile's time: 181 us).  Dot products by all warps, a barrier, then residuals
-// by two warps while the others form the sums of their blocks of columns in the tile before (a row's residual by a
-// warp of its own instead: 178 us; every warp then has the latency of a sigmoid in its way).  What bounds it now is
-// instructions again, a conversion, a scale and the digits of every block and row, and the barrier per tile.
+// A CTA takes tiles of consecutive rows through a ring in shared memory.  A warp has 128 columns (256 above 2048) of
+// every tile: it fetches them itself, by TMA in boxes of 128 bytes by all rows with the 128-byte swizzle, which keeps
+// ldmatrix free of bank conflicts; it forms its part of the tile's dot products, then the sums of its columns of
+// the tile before, and asks for the next columns at once.  One more warp turns dot products into residuals in the
+// meantime and fetches the exponent bytes, which all warps read.  Nothing but these residuals joins the warps: with a
+// barrier per tile and the tile fetched as one the step took 158 us at 2^18 x 2048, with the residuals by a warp of
+// their own 132 us, with every warp its own fetches 111 us (5.0 TB/s).  What is left to the floor is the
+// latency of a tile: two of the three that fit are in use, and the third arrives while they are worked on.  Up to 1024
+// columns shared memory holds several CTAs, which fill each other's gaps (2^18 x 1024: 113 us with one, 65 us; 2^19 x 512:
+// 198, 67 us).  Below some 10^4 rows the step is two launches and one trip to memory, 8 us.
 // Tiles are dealt in a fixed pattern and all sums have a fixed order: a step is reproducible bit for bit.
 #include <cuda.h>
 #include <math.h>
@@ -33,11 +37,8 @@ namespace spr {
 
 namespace {
 
-constexpr int kFitThreads = 1024;
-constexpr int kFitWarps = kFitThreads / 32;
-constexpr int kMaxTiles = 8;             // tiles of the ring
+constexpr int kMaxTiles = 8;             // tiles of the ring, and twice as many of their exponent bytes
 constexpr int kAhead = 2;                // tiles on their way into L2 behind those of the ring
-constexpr size_t kSmemBytes = 221 * 1024;     // dynamic; the static arrays take some 5 KB more
 
 __device__ __forceinline__ uint32_t fit_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ bool fit_wait(uint64_t *bar, uint32_t parity, uint32_t limit)
@@ -54,6 +55,23 @@ __device__ __forceinline__ bool fit_wait(uint64_t *bar, uint32_t parity, uint32_
         if (done) return true;
     }
     return false;
+}
+
+__device__ __forceinline__ void fit_init(uint64_t *bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(fit_addr(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void fit_init_fence() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+// what the warp's lanes did before is there for whom the barrier lets through
+__device__ __forceinline__ void fit_arrive(uint64_t *bar, int lane)
+{
+    __syncwarp();
+    if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(fit_addr(bar)) : "memory");
+}
+
+__device__ __forceinline__ void fit_expect(uint64_t *bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(fit_addr(bar)), "r"(bytes) : "memory");
 }
 
 __device__ __forceinline__ void fetch_box(uint32_t dst, const CUtensorMap *map, int c0, int c1, uint64_t *bar)
@@ -76,27 +94,25 @@ __device__ __forceinline__ float block_scale(uint32_t word, int k)      // byte 
 {
     return __int_as_float(((int)(word << (24 - 8 * k)) >> 24) * (1 << 23) + 127 * (1 << 23));
 }
-// 1, 2 or 4 exponent bytes from a shared address that is a multiple of as many
+// N exponent bytes, 4 or 8, from a shared address that is a multiple of N
 template <int N>
-__device__ __forceinline__ uint32_t load_exponents(uint32_t addr)
+__device__ __forceinline__ void load_exponents(uint32_t (&x)[N / 4], uint32_t addr)
 {
-    static_assert(N == 1 || N == 2 || N == 4, "exponent bytes");
-    uint32_t w;
-    if (N == 1) asm volatile("ld.shared.u8 %0, [%1];" : "=r"(w) : "r"(addr));
-    else if (N == 2) asm volatile("ld.shared.u16 %0, [%1];" : "=r"(w) : "r"(addr));
-    else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(addr));
-    return w;
+    static_assert(N == 4 || N == 8, "exponent bytes");
+    if constexpr (N == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x[0]) : "r"(addr));
+    else asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(addr));
 }
 // three balanced digits of a 24-bit integer: v = 256^2 d0 + 256 d1 + d2, as the bytes 2, 1, 0
 __device__ __forceinline__ uint32_t digits(int v) { return ((uint32_t)v + 0x808080u) ^ 0x808080u; }
 
-// Digits of 32 numbers (a lane each) where the lanes of a product want them: plane p (d0, d1, d2), then for each t
-// of 4 the numbers 4 t .. 4 t + 3 and 16 + 4 t .. + 3.  96 bytes.
-__device__ __forceinline__ void put_digits(uint32_t dst, uint32_t u, int lane)
+// Digits of number i of K (16 or 32) where the lanes of a product want them: plane p (d0, d1, d2), then of 32 numbers for each t
+// of 4 the numbers 4 t .. 4 t + 3 and 16 + 4 t .. + 3, of 16 numbers one after the other.  3 K bytes.
+template <int K>
+__device__ __forceinline__ void put_digits(uint32_t dst, uint32_t u, int i)
 {
-    const uint32_t at = dst + (uint32_t)(((lane & 15) >> 2) * 8 + (lane >> 4) * 4 + (lane & 3));
-    asm volatile("st.shared.u8 [%0], %1;\n\tst.shared.u8 [%0 + 32], %2;\n\tst.shared.u8 [%0 + 64], %3;" ::"r"(at), "r"(u >> 16),
-                 "r"(u >> 8), "r"(u)
+    const uint32_t at = dst + (uint32_t)(K == 32 ? ((i & 15) >> 2) * 8 + (i >> 4) * 4 + (i & 3) : i);
+    asm volatile("st.shared.u8 [%0], %1;\n\tst.shared.u8 [%0 + %4], %2;\n\tst.shared.u8 [%0 + %5], %3;" ::"r"(at), "r"(u >> 16),
+                 "r"(u >> 8), "r"(u), "n"(K), "n"(2 * K)
                  : "memory");
 }
 // The second operand of a product: column n is plane n, and the columns from the fourth on are zero (lanes that stand for
@@ -105,6 +121,12 @@ __device__ __forceinline__ uint2 get_digits(uint32_t addr)
 {
     uint2 v;
     asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t get_digits_k16(uint32_t addr)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }
 
@@ -121,6 +143,14 @@ __device__ __forceinline__ void mma_s8_k16(int (&c)[4], uint32_t a0, uint32_t a1
                  : "r"(a0), "r"(a1), "r"(b), "r"(0));
 }
 
+// Residuals of a tile relative to the largest of them (its bits): |v| < 2^22 units of 2^E
+__device__ __forceinline__ int residual_exponent(uint32_t top) { return max((int)(top >> 23), 27) - 148; }
+// v 2^-E + 1.5 2^23 rounds to the unit; the integer stands in the low bits of the sum
+__device__ __forceinline__ int residual_integer(float v, int E)
+{
+    return (int)(__float_as_uint(fmaf(v, __int_as_float((127 - E) << 23), 12582912.f)) - 0x4b400000u);
+}
+
 // A tile in shared memory: boxes of 128 bytes x T rows, one after the other; inside, 16-byte units are swizzled.
 // Byte c of row r:
 template <int T>
@@ -130,28 +160,50 @@ __device__ __forceinline__ uint32_t tile_at(int r, int c)
 }
 // Unit k past a unit whose own index is a multiple of the units asked for: the swizzle's exclusive or is linear in it.
 __device__ __forceinline__ uint32_t unit_at(uint32_t base, int k) { return base ^ (uint32_t)(k << 4); }
-__host__ __device__ constexpr int tile_boxes(int d) { return (pack8_pitch(d) + 127) / 128; }
-
-// NB: blocks of 32 columns per warp; T: rows per tile (16 or 32)
-template <int NB, int T>
-__global__ void __launch_bounds__(kFitThreads, 1) train8_kernel(const TrainParams prm, const __grid_constant__ CUtensorMap map, int ring_tiles)
+// Behind the boxes of the d bytes a box of the rows' exponent bytes: 16, 32, 64 or 128 bytes x T rows, swizzled in as many bytes.
+__host__ __device__ constexpr int tile_boxes(int d) { return (d + 127) / 128; }
+__host__ __device__ constexpr int exponent_width(int d) { return d <= 512 ? 16 : d <= 1024 ? 32 : d <= 2048 ? 64 : 128; }
+__host__ __device__ constexpr int tile_share(int d, int rows) { return rows * (tile_boxes(d) * 128 + 2 * exponent_width(d)); }       // of the ring
+__device__ __forceinline__ uint32_t exponent_at(int width, int r, int b)
 {
-    constexpr int kRowGroups = T / 16;                     // of 16 rows, for the dot products
-    constexpr int kNB1 = NB * kRowGroups;                  // blocks a warp takes of its row group there
-    constexpr int kSlices = kFitWarps / kRowGroups;        // warps that share a row's dot product
-    constexpr int kDig = NB < 2 ? NB : 2;                  // blocks whose residuals a warp splits at a time
-    extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ __align__(8) uint64_t bars[kMaxTiles];
-    __shared__ __align__(16) uint32_t zeros[4];
-    __shared__ float zpart[2][kSlices][T];
-    __shared__ float residual[2][32];
+    return (uint32_t)(r * width + (((b >> 4) ^ ((r * width) >> 7)) & (width / 16 - 1)) * 16 + (b & 15));
+}
+
+// NB: blocks of 32 columns per warp; T: rows per tile (16 or 32); W: warps that have columns; C: CTAs on an SM
+template <int NB, int T, int W>
+struct Fit8 {
+    static constexpr int kThreads = (W + 1) * 32;
+    static constexpr int kDig = 2;                         // blocks whose residuals a warp splits at a time
+    // shared memory behind the ring: digits of the weights, of the scaled residuals, units of the weights, parts of the
+    // dot products, residuals, zeros, barriers (a warp's columns of a tile there, exponents there, exponents done with, dot
+    // products there, residuals there)
+    static constexpr int kWdig = 0, kRdig = kWdig + W * NB * 96, kUnit = kRdig + W * kDig * 3 * T, kZpart = kUnit + W * NB * 4;
+    static constexpr int kResidual = kZpart + 2 * W * T * 4, kZeros = kResidual + 2 * 32 * 4, kBars = kZeros + 16;
+    static constexpr int kBytes = kBars + (kMaxTiles * W + 4 * kMaxTiles + 4) * 8;
+    static constexpr int kBoxes = NB / 4;      // a warp's columns are as many boxes
+    static_assert(NB % 4 == 0 && kUnit % 16 == 0 && kZeros % 16 == 0 && kBars % 8 == 0, "alignment");
+};
+
+template <int NB, int T, int W, int C>
+__global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainParams prm, const __grid_constant__ CUtensorMap map,
+                                                                     const __grid_constant__ CUtensorMap emap, int ring_tiles)
+{
+    using F = Fit8<NB, T, W>;
+    constexpr int kRowGroups = T / 16, kDig = F::kDig, kWords = NB / 4;
+    extern __shared__ __align__(1024) unsigned char smem[];        // the ring comes first: swizzled boxes repeat every 1024 bytes
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int d = prm.d, blocks = (d + 31) / 32;
-    const int boxes = tile_boxes(d), tile_bytes = boxes * T * 128;
-    // digits of the weights [blocks][96], of the scaled residuals (kDig blocks per warp), units of the weights [blocks], the ring
-    const uint32_t wdig = fit_addr(smem), rdig = wdig + (uint32_t)(kFitWarps * NB * 96 + warp * kDig * 96);
-    float *unit = reinterpret_cast<float *>(smem + kFitWarps * (NB + kDig) * 96);
-    const uint32_t ring = (fit_addr(unit + kFitWarps * NB) + 1023u) & ~1023u;
+    const int d = prm.d, blocks = (d + 31) / 32, workers = (blocks + NB - 1) / NB;
+    const int boxes = tile_boxes(d), ewidth = exponent_width(d), tile_bytes = boxes * T * 128, exp_bytes = T * ewidth;
+    const int ring_exps = 2 * ring_tiles;
+    const uint32_t ring = fit_addr(smem), exps = ring + (uint32_t)(ring_tiles * tile_bytes);
+    unsigned char *tables = smem + ring_tiles * tile_bytes + ring_exps * exp_bytes;
+    const uint32_t wdig = fit_addr(tables + F::kWdig);
+    float *unit = reinterpret_cast<float *>(tables + F::kUnit);
+    float(*zpart)[W][T] = reinterpret_cast<float(*)[W][T]>(tables + F::kZpart);
+    float(*residual)[32] = reinterpret_cast<float(*)[32]>(tables + F::kResidual);
+    uint32_t *zeros = reinterpret_cast<uint32_t *>(tables + F::kZeros);
+    uint64_t *there = reinterpret_cast<uint64_t *>(tables + F::kBars), *ethere = there + kMaxTiles * W, *edone = ethere + 2 * kMaxTiles;
+    uint64_t *dots = edone + 2 * kMaxTiles, *resid = dots + 2;
     pdl_trigger();
 
     // this CTA's tiles: blockIdx.x, + gridDim.x, ...; only the last tile of the data can be short
@@ -159,40 +211,112 @@ __global__ void __launch_bounds__(kFitThreads, 1) train8_kernel(const TrainParam
     const int all = (N + T - 1) / T;
     const int n = (int)blockIdx.x < all ? (all - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
     const int row_step = (int)gridDim.x * T;
-    const bool feed = !(prm.test_flags & TRAIN_TEST_NO_FETCH);
-    // Every warp asks for a box of the tile at row0 (the first for a 33rd); rows and bytes that do not exist arrive as zeros.
-    auto fetch = [&](int slot, int row0) {
-        if (lane == 0) {
-            if (warp == 0)
-                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(fit_addr(&bars[slot])), "r"((uint32_t)tile_bytes) : "memory");
-            for (int b = warp; b < boxes; b += kFitWarps)
-                fetch_box(ring + (uint32_t)(slot * tile_bytes + b * T * 128), &map, b * 128, row0, &bars[slot]);
-        }
-    };
-    // Three tiles of 2048 columns are all that shared memory holds, and two of them are in use: what comes after the next
-    // tile is asked for as far as L2, so that memory always has kAhead tiles to bring.
-    auto prefetch = [&](int row0) {
-        if (lane == 0)
-            for (int b = warp; b < boxes; b += kFitWarps) prefetch_box(&map, b * 128, row0);
-    };
-    if (tid == 0) {
-        for (int s = 0; s < ring_tiles; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(fit_addr(&bars[s])) : "memory");
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
+    float *out = prm.part + (int64_t)blockIdx.x * (d + 2);
     if (tid < 4) zeros[tid] = 0u;
-    __syncthreads();
-    for (int k = 0; feed && k < ring_tiles && k < n; ++k) fetch(k, (int)blockIdx.x * T + k * row_step);
-    for (int k = ring_tiles; feed && k < ring_tiles + kAhead && k < n; ++k) prefetch((int)blockIdx.x * T + k * row_step);
-    // Labels, one row per lane, two tiles ahead and as the bytes they are: a label fetched when it is wanted would cost
-    // a trip to memory.
-    auto tile_label = [&](int64_t row) -> uint32_t { return prm.labels[lane < T && row + lane < prm.N ? row + lane : 0]; };
-    uint32_t y_raw[2] = {0u, 0u};
-    if (warp < 2) {
-        y_raw[0] = tile_label((int64_t)blockIdx.x * T);
-        y_raw[1] = tile_label((int64_t)blockIdx.x * T + row_step);
+    bool ok = true;
+    const bool feed = !(prm.test_flags & TRAIN_TEST_NO_FETCH);
+    int row0 = (int)blockIdx.x * T, asked = 0;             // first row of the tile at hand; tiles asked for
+    if (warp == W) {
+        // ---- the warp that fetches exponent bytes and turns dot products into residuals, a row per lane
+        auto fetch = [&](int slot, int row) {              // rows and bytes that do not exist arrive as zeros
+            if (lane == 0) {
+                fit_expect(&ethere[slot], (uint32_t)exp_bytes);
+                fetch_box(exps + (uint32_t)(slot * exp_bytes), &emap, d, row, &ethere[slot]);
+            }
+        };
+        if (lane == 0) {                                   // (the other barriers: below)
+            for (int s = 0; s < ring_exps; ++s) {
+                fit_init(&ethere[s], 1);
+                fit_init(&edone[s], workers);
+            }
+            for (int s = 0; s < 2; ++s) {
+                fit_init(&dots[s], workers);
+                fit_init(&resid[s], 1);
+            }
+            fit_init_fence();
+        }
+        const float bias = prm.theta[d];
+        for (; feed && asked < ring_exps && asked < n; ++asked) fetch(asked, row0 + asked * row_step);
+        // labels two tiles ahead and as the bytes they are: a label fetched when it is wanted would cost a trip to memory
+        auto tile_label = [&](int64_t row) -> uint32_t { return prm.labels[lane < T && row + lane < prm.N ? row + lane : 0]; };
+        uint32_t y_raw[2] = {tile_label(row0), tile_label((int64_t)row0 + row_step)};
+        double acc_b = 0.0, acc_loss = 0.0;
+        int slot = 0;                              // of tile k - 1
+        uint32_t parity = 0;
+        __syncthreads();                           // the barriers are set up, and the weights' digits there
+        for (int k = 0; k < n; ++k) {
+            const float y = (float)y_raw[0];
+            y_raw[0] = y_raw[1];
+            y_raw[1] = tile_label((int64_t)row0 + 2 * (int64_t)row_step);
+            ok = __all_sync(0xffffffffu, fit_wait(&dots[k & 1], (uint32_t)(k >> 1) & 1u, prm.spin_limit));
+            if (!ok) break;
+            float z = bias;
+#pragma unroll
+            for (int s = 0; s < W; ++s) z += s < workers ? zpart[k & 1][s][lane & (T - 1)] : 0.f;
+            const bool live = lane < T && row0 + lane < N;
+            const float r = live ? 1.f / (1.f + expf(-z)) - y : 0.f;
+            residual[k & 1][lane] = r;
+            fit_arrive(&resid[k & 1], lane);
+            if (live) {
+                acc_b += (double)r;
+                acc_loss += (double)(fmaxf(z, 0.f) + log1pf(expf(-fabsf(z))) - y * z);
+            }
+            if (k > 0) {
+                if (asked < n) {
+                    ok = __all_sync(0xffffffffu, fit_wait(&edone[slot], parity, prm.spin_limit));
+                    if (!ok) break;
+                    if (feed) fetch(slot, row0 + (ring_exps - 1) * row_step);
+                    ++asked;
+                }
+                if (++slot == ring_exps) {
+                    slot = 0;
+                    parity ^= 1u;
+                }
+            }
+            row0 += row_step;
+        }
+        if (!ok) {
+            // A wait ran out: report it, then give the copies still on their way the same bounded time to land
+            // before the CTA's shared memory goes away.
+            if (lane == 0) raise_status(prm.status, SPR_ERR_TIMEOUT);
+            for (int i = max(0, asked - ring_exps); feed && i < asked; ++i)
+                fit_wait(&ethere[i % ring_exps], (uint32_t)(i / ring_exps) & 1u, prm.spin_limit);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            acc_b += __shfl_xor_sync(0xffffffffu, acc_b, o);
+            acc_loss += __shfl_xor_sync(0xffffffffu, acc_loss, o);
+        }
+        if (lane == 0) {
+            out[d] = (float)acc_b;
+            out[d + 1] = (float)acc_loss;
+        }
+        __syncthreads();                           // no warp is at the tiles any more
+        return;
     }
 
-    for (int b = warp; b < kFitWarps * NB; b += kFitWarps) {
+    // ---- the warps that have columns: each fetches its own, and asks for the next as soon as it is done with a tile
+    const int b0 = warp * NB, nb = min(NB, blocks - b0), box0 = warp * F::kBoxes, nbox = min(F::kBoxes, boxes - box0);
+    uint64_t *mine = there + warp * kMaxTiles;
+    auto fetch = [&](int slot, int row) {                  // rows and bytes that do not exist arrive as zeros
+        fit_expect(&mine[slot], (uint32_t)(nbox * T * 128));
+        for (int b = 0; b < nbox; ++b)
+            fetch_box(ring + (uint32_t)(slot * tile_bytes + (box0 + b) * T * 128), &map, (box0 + b) * 128, row, &mine[slot]);
+    };
+    // Three tiles of 2048 columns are all that shared memory holds, and two of them are in use: what comes after the
+    // next tile is asked for as far as L2, so that memory always has kAhead tiles to bring.
+    auto prefetch = [&](int row) {
+        for (int b = 0; b < nbox; ++b) prefetch_box(&map, (box0 + b) * 128, row);
+    };
+    if (nb > 0 && lane == 0) {
+        for (int s = 0; s < ring_tiles; ++s) fit_init(&mine[s], 1);
+        fit_init_fence();
+        for (int k = 0; feed && k < ring_tiles && k < n; ++k) fetch(k, row0 + k * row_step);
+        for (int k = ring_tiles; feed && k < ring_tiles + kAhead && k < n; ++k) prefetch(row0 + k * row_step);
+    }
+    asked = min(ring_tiles, n);
+
+    for (int b = warp; b < W * NB; b += W) {
         const int c = b * 32 + lane;
         const float w = c < d ? prm.theta[c] : 0.f;
         const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(w) & 0x7fffffffu);
@@ -200,10 +324,9 @@ __global__ void __launch_bounds__(kFitThreads, 1) train8_kernel(const TrainParam
         int E = max((int)(top >> 23) - 127, -100) - 22;
         if (rintf(ldexpf(__uint_as_float(top), -E)) > 8355711.f) ++E;
         const bool finite = top < 0x7f800000u;             // a weight that is not finite shows in every sum
-        put_digits(wdig + (uint32_t)(b * 96), finite ? digits(__float2int_rn(ldexpf(w, -E))) : 0u, lane);
+        put_digits<32>(wdig + (uint32_t)(b * 96), finite ? digits(__float2int_rn(ldexpf(w, -E))) : 0u, lane);
         if (lane == 0) unit[b] = finite ? ldexpf(1.f, E) : __int_as_float(0x7fc00000);
     }
-    const float bias = prm.theta[d];
 
     // A lane's part of a product's result: columns 2 (lane % 4) and + 1, hence d0 and d1, or d2 and 0, or nothing.  The
     // integers 256 d0 + d1 and d2 are added up apart and weighted at the very end.
@@ -212,115 +335,114 @@ __global__ void __launch_bounds__(kFitThreads, 1) train8_kernel(const TrainParam
     // where the second operand stands, block by block
     const bool holds = lane < 12;
     const uint32_t dig_lane = (uint32_t)((lane >> 2) * 32 + (lane & 3) * 8), dig_step = holds ? 96u : 0u;
-    // dot products: 16 rows of row group rg by blocks b1 .. b1 + kNB1 - 1
-    const int rg = warp % kRowGroups, slice = warp / kRowGroups, b1 = slice * kNB1;
-    const int n1 = min(kNB1, blocks - b1);
-    const uint32_t a1 = tile_at<T>(rg * 16 + (lane & 7) + ((lane >> 3) & 1) * 8, b1 * 32 + (lane >> 4) * 16);      // ldmatrix of 16 x 32
-    const uint32_t e1 = tile_at<T>(rg * 16 + (lane >> 2), d + b1);         // rows lane / 4 and, 8 x 128 bytes on, + 8
-    const uint32_t d1 = holds ? wdig + (uint32_t)(b1 * 96) + dig_lane : fit_addr(zeros);
-    // columns: blocks b2 .. b2 + NB - 1, a row per lane
-    const int my_row = lane & (T - 1), b2 = warp * NB, n2 = min(NB, blocks - b2);
-    const uint32_t a2 = tile_at<T>(my_row, b2 * 32), e2 = tile_at<T>(my_row, d + b2);
-    const uint32_t d2 = holds ? rdig + dig_lane : fit_addr(zeros);
+    // blocks b0 .. b0 + NB - 1 are this warp's: dot products by 16 rows at a time, columns with a row per lane
+    const uint32_t a1 = tile_at<T>((lane & 7) + ((lane >> 3) & 1) * 8, b0 * 32 + (lane >> 4) * 16);      // ldmatrix of 16 x 32
+    const uint32_t e1 = exponent_at(ewidth, lane >> 2, b0);         // rows lane / 4 and, 8 * ewidth on, + 8
+    const uint32_t d1 = holds ? wdig + (uint32_t)(b0 * 96) + dig_lane : fit_addr(zeros);
+    const int my_row = lane & (T - 1);
+    const uint32_t a2 = tile_at<T>(my_row, b0 * 32), e2 = exponent_at(ewidth, my_row, b0);
+    const uint32_t rdig = fit_addr(tables + F::kRdig) + (uint32_t)(warp * kDig * 3 * T);
+    const uint32_t d2 = holds ? rdig + (T == 32 ? dig_lane : (uint32_t)((lane >> 2) * 16 + (lane & 3) * 4)) : fit_addr(zeros);
+    const uint32_t d2_step = holds ? 3u * T : 0u;
     float grad[NB][4];
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) grad[i][e] = 0.f;
-    double acc_b = 0.0, acc_loss = 0.0;        // warp 1
-    __syncthreads();                           // the weights' digits are there
+    __syncthreads();                           // the barriers are set up, and the weights' digits there
 
-    // One barrier per tile: after that of tile k its dot products are there, and while two warps turn them into
-    // residuals first, the others are at the columns of tile k - 1.
-    bool ok = true;
-    int k = 0, slot = 0, before = 0, row0 = (int)blockIdx.x * T;      // slot of tile k, of tile k - 1; first row of tile k
-    uint32_t parity = 0;
-    for (; k <= n; ++k) {
+    // Dot products of tile k, then columns of tile k - 1, whose residuals came in the meantime.  zpart and residual have two
+    // halves: a warp is at tile k + 2 only once it has the residuals of tile k, hence when zpart's half is read; and
+    // residual's half is written when every warp has handed in tile k + 2, behind the columns of tile k.
+    int slot = 0, before = 0;                  // of tile k, of tile k - 1
+    uint32_t parity = 0, xnow = exps, xbefore = exps;          // exponent bytes of tile k, of tile k - 1
+    int eslot = 0, ebefore = 0;
+    uint32_t eparity = 0;
+    for (int k = 0; k <= n && nb > 0; ++k) {
         const uint32_t now = ring + (uint32_t)(slot * tile_bytes);
         if (k < n) {
-            // ---- dot products of tile k
-            ok = fit_wait(&bars[slot], parity, prm.spin_limit);
-            float z0 = 0.f, z1 = 0.f;
-            if (n1 > 0) {
-                const uint32_t x0 = load_exponents<kNB1>(now + e1), x1 = load_exponents<kNB1>(now + e1 + 1024);
+            ok = fit_wait(&ethere[eslot], eparity, prm.spin_limit);
+            ok = __all_sync(0xffffffffu, ok && fit_wait(&mine[slot], parity, prm.spin_limit));
+            if (!ok) break;
+            float z[2 * kRowGroups];
+            uint32_t x1[2 * kRowGroups][kWords];
 #pragma unroll
-                for (int i = 0; i < kNB1; ++i) {
-                    if (i < n1) {
+            for (int g = 0; g < 2 * kRowGroups; ++g) {
+                z[g] = 0.f;
+                load_exponents<NB>(x1[g], xnow + e1 + (uint32_t)(g * 8 * ewidth));
+            }
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                if (i < nb) {
+                    const uint2 bd = get_digits(d1 + (uint32_t)i * dig_step);
+                    const float u = unit[b0 + i];
+#pragma unroll
+                    for (int g = 0; g < kRowGroups; ++g) {
                         uint32_t a[4];
                         asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                                      : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3])
-                                     : "r"(unit_at(now + a1, 2 * i)));
+                                     : "r"(unit_at(now + a1 + (uint32_t)(g * 2048 + (i / 4) * (T * 128)), 2 * (i & 3))));
                         int c[4];
-                        mma_s8(c, a, get_digits(d1 + (uint32_t)i * dig_step));
-                        const float u = unit[b1 + i];
-                        z0 = fmaf((float)(c[0] * m0 + c[1]) * u, block_scale(x0, i), z0);
-                        z1 = fmaf((float)(c[2] * m0 + c[3]) * u, block_scale(x1, i), z1);
+                        mma_s8(c, a, bd);
+                        z[2 * g] = fmaf((float)(c[0] * m0 + c[1]) * u, block_scale(x1[2 * g][i / 4], i & 3), z[2 * g]);
+                        z[2 * g + 1] = fmaf((float)(c[2] * m0 + c[3]) * u, block_scale(x1[2 * g + 1][i / 4], i & 3), z[2 * g + 1]);
                     }
                 }
             }
-            z0 *= weight;
-            z1 *= weight;
-            z0 += __shfl_xor_sync(0xffffffffu, z0, 1);
-            z1 += __shfl_xor_sync(0xffffffffu, z1, 1);
-            if ((lane & 3) == 0) {
-                zpart[k & 1][slice][rg * 16 + (lane >> 2)] = z0;
-                zpart[k & 1][slice][rg * 16 + (lane >> 2) + 8] = z1;
-            }
-        }
-        ok = __syncthreads_and(ok) != 0;
-        if (!ok) break;
-        if (k > 1 && k - 2 + ring_tiles < n) {         // tile k - 2 is done with: its slot is the one before that of tile k - 1
-            const int free_slot = before == 0 ? ring_tiles - 1 : before - 1;
-            fetch(free_slot, row0 + (ring_tiles - 2) * row_step);
-            if (k - 2 + ring_tiles + kAhead < n) prefetch(row0 + (ring_tiles - 2 + kAhead) * row_step);
-        }
-        if (warp < 2 && k < n) {
-            // ---- residuals of tile k, a row per lane: warp 0 hands them on, warp 1 has the loss and the bias's gradient
-            const float y = (float)y_raw[0];
-            y_raw[0] = y_raw[1];
-            y_raw[1] = tile_label((int64_t)row0 + 2 * (int64_t)row_step);
-            float z = bias;
 #pragma unroll
-            for (int s = 0; s < kSlices; ++s) z += zpart[k & 1][s][lane & (T - 1)];
-            const bool live = lane < T && row0 + lane < N;
-            const float r = live ? 1.f / (1.f + expf(-z)) - y : 0.f;
-            if (warp == 0) {
-                residual[k & 1][lane] = r;
-            } else if (live) {
-                acc_b += (double)r;
-                acc_loss += (double)(fmaxf(z, 0.f) + log1pf(expf(-fabsf(z))) - y * z);
+            for (int g = 0; g < 2 * kRowGroups; ++g) {
+                z[g] *= weight;
+                z[g] += __shfl_xor_sync(0xffffffffu, z[g], 1);
+                if ((lane & 3) == 0) zpart[k & 1][warp][g * 8 + (lane >> 2)] = z[g];
             }
+            fit_arrive(&dots[k & 1], lane);
         }
-        if (k > 0 && n2 > 0) {
+        if (k > 0) {
             // ---- columns of this warp's blocks in tile k - 1
             const uint32_t tile = ring + (uint32_t)(before * tile_bytes);
-            const float r = residual[(k - 1) & 1][lane];
+            ok = __all_sync(0xffffffffu, fit_wait(&resid[(k - 1) & 1], (uint32_t)((k - 1) >> 1) & 1u, prm.spin_limit));
+            if (!ok) break;
+            const float r = residual[(k - 1) & 1][my_row];
             const float show = __any_sync(0xffffffffu, r != r) ? __int_as_float(0x7fc00000) : 1.f;    // NaN has no digits
-            const uint32_t x = load_exponents<NB>(tile + e2);
+            uint32_t x[kWords];
+            load_exponents<NB>(x, xbefore + e2);
+            if (T == 16)
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) x[w] >>= (lane >> 4) * 8;
 #pragma unroll
             for (int i0 = 0; i0 < NB; i0 += kDig) {
                 float scale[kDig];
                 __syncwarp();                      // the digits that stood there are read
+                // a row that does not exist has r = 0, a block that does not exist is not read below
+                if constexpr (T == 32) {
 #pragma unroll
-                for (int i = 0; i < kDig; ++i) {
-                    // a row that does not exist has r = 0, a block that does not exist is not read below
-                    const float v = r != 0.f ? r * block_scale(x, i0 + i) : 0.f;
-                    const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu);
-                    const int E = max((int)(top >> 23), 27) - 148;                 // |v| < 2^22 units of 2^E
-                    // v 2^-E + 1.5 2^23 rounds to the unit; the integer stands in the low bits of the sum
-                    const int q = (int)(__float_as_uint(fmaf(v, __int_as_float((127 - E) << 23), 12582912.f)) - 0x4b400000u);
-                    put_digits(rdig + (uint32_t)(i * 96), digits(q), lane);
-                    scale[i] = __int_as_float((E + 127) << 23) * show;
+                    for (int i = 0; i < kDig; ++i) {
+                        const float v = r != 0.f ? r * block_scale(x[(i0 + i) / 4], (i0 + i) & 3) : 0.f;
+                        const int E = residual_exponent(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu));
+                        put_digits<T>(rdig + (uint32_t)(i * 3 * T), digits(residual_integer(v, E)), lane);
+                        scale[i] = __int_as_float((E + 127) << 23) * show;
+                    }
+                } else {
+                    // 16 rows: two blocks at a time, one by each half of the warp
+                    const float v = r != 0.f ? r * block_scale(x[i0 / 4], i0 & 3) : 0.f;
+                    const uint32_t size = __float_as_uint(v) & 0x7fffffffu;
+                    const int Ea = residual_exponent(__reduce_max_sync(0xffffffffu, lane < 16 ? size : 0u));
+                    const int Eb = residual_exponent(__reduce_max_sync(0xffffffffu, lane < 16 ? 0u : size));
+                    put_digits<T>(rdig + (uint32_t)((lane >> 4) * 3 * T), digits(residual_integer(v, lane < 16 ? Ea : Eb)), lane & 15);
+                    scale[0] = __int_as_float((Ea + 127) << 23) * show;
+                    scale[1] = __int_as_float((Eb + 127) << 23) * show;
                 }
                 __syncwarp();
 #pragma unroll
                 for (int i = 0; i < kDig; ++i) {
-                    if (i0 + i < n2) {
-                        const uint2 bd = get_digits(d2 + (uint32_t)i * dig_step);
+                    if (i0 + i < nb) {
+                        uint2 bd;
+                        if constexpr (T == 32) bd = get_digits(d2 + (uint32_t)i * d2_step);
+                        else bd.x = get_digits_k16(d2 + (uint32_t)i * d2_step);
                         float *g = grad[i0 + i];
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const uint32_t at = unit_at(tile + a2, 2 * (i0 + i) + h);      // a last block of 16 reads on, into what follows in the row
+                            const uint32_t at = unit_at(tile + a2 + (uint32_t)((i0 + i) / 4 * (T * 128)), 2 * ((i0 + i) & 3) + h);      // a last block of 16 reads on, into what follows in the row
                             int c[4];
                             if constexpr (T == 32) {
                                 uint32_t a[4];
@@ -339,25 +461,35 @@ __global__ void __launch_bounds__(kFitThreads, 1) train8_kernel(const TrainParam
                     }
                 }
             }
+            fit_arrive(&edone[ebefore], lane);
+            if (asked < n) {                           // row0: the first row of tile k
+                if (feed && lane == 0) {
+                    fetch(before, row0 + (ring_tiles - 1) * row_step);
+                    if (asked + kAhead < n) prefetch(row0 + (ring_tiles - 1 + kAhead) * row_step);
+                }
+                ++asked;
+            }
         }
+        row0 += row_step;
         before = slot;
         if (++slot == ring_tiles) {
             slot = 0;
             parity ^= 1u;
         }
-        row0 += row_step;
-    }
-    if (!ok) {
-        // A wait ran out: report it, then give the copies still on their way the same bounded time to
-        // land before the CTA's shared memory goes away.
-        if (tid == 0) {
-            raise_status(prm.status, SPR_ERR_TIMEOUT);
-            for (int i = k; feed && i < n && i < k - 2 + ring_tiles; ++i)
-                fit_wait(&bars[i % ring_tiles], (uint32_t)(i / ring_tiles) & 1u, prm.spin_limit);
+        xbefore = xnow;
+        ebefore = eslot;
+        xnow += (uint32_t)exp_bytes;
+        if (++eslot == ring_exps) {
+            eslot = 0;
+            eparity ^= 1u;
+            xnow = exps;
         }
-        __syncthreads();
     }
-    float *out = prm.part + (int64_t)blockIdx.x * (d + 2);
+    if (!ok) {                                 // as above
+        if (lane == 0) raise_status(prm.status, SPR_ERR_TIMEOUT);
+        for (int i = max(0, asked - ring_tiles); feed && i < asked; ++i)
+            fit_wait(&mine[i % ring_tiles], (uint32_t)(i / ring_tiles) & 1u, prm.spin_limit);
+    }
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
 #pragma unroll
@@ -367,17 +499,7 @@ __global__ void __launch_bounds__(kFitThreads, 1) train8_kernel(const TrainParam
             if ((lane & 3) == 0 && c < d) out[c] = s;
         }
     }
-    if (warp == 1) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            acc_b += __shfl_xor_sync(0xffffffffu, acc_b, o);
-            acc_loss += __shfl_xor_sync(0xffffffffu, acc_loss, o);
-        }
-        if (lane == 0) {
-            out[d] = (float)acc_b;
-            out[d + 1] = (float)acc_loss;
-        }
-    }
+    __syncthreads();
 }
 
 // The CTAs' partial sums, and the Adam step: 32 parameters per CTA, eight warps that each add up every
@@ -425,8 +547,8 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
                                   CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
                                   CUtensorMapFloatOOBfill);
 
-// [N, pack8_pitch(d)] bytes in boxes of 128 bytes x `rows` rows
-bool packed_map(CUtensorMap *map, const void *base, int64_t N, int d, int rows)
+// [N, pack8_pitch(d)] bytes in boxes of `width` bytes x `rows` rows, swizzled in `width` bytes
+bool packed_map(CUtensorMap *map, const void *base, int64_t N, int d, int width, int rows)
 {
     static const EncodeTiledFn fn = [] {   // initialised once, thread-safe
         void *p = nullptr;
@@ -439,38 +561,44 @@ bool packed_map(CUtensorMap *map, const void *base, int64_t N, int d, int rows)
     if (!fn) return false;
     const cuuint64_t dims[2] = {(cuuint64_t)pack8_pitch(d), (cuuint64_t)N};
     const cuuint64_t strides[1] = {(cuuint64_t)pack8_pitch(d)};
-    const cuuint32_t box[2] = {128, (cuuint32_t)rows}, elem[2] = {1, 1};
+    const cuuint32_t box[2] = {(cuuint32_t)width, (cuuint32_t)rows}, elem[2] = {1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, elem,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_INTERLEAVE_NONE,
+              width == 16   ? CU_TENSOR_MAP_SWIZZLE_NONE
+              : width == 32 ? CU_TENSOR_MAP_SWIZZLE_32B
+              : width == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                            : CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int NB, int T>
+template <int NB, int T, int W, int C>
 cudaError_t launch_train8(const TrainParams &tp, cudaStream_t st)
 {
     static std::atomic<bool> attr_set[64];
+    constexpr size_t room = (size_t)(228 / C - 1) * 1024;
     int dev = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-        e = cudaFuncSetAttribute(train8_kernel<NB, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
+        e = cudaFuncSetAttribute(train8_kernel<NB, T, W, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room);
         if (e != cudaSuccess) return e;
         if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
     }
     TrainParams p = tp;
-    const int64_t all = (tp.N + T - 1) / T;
-    p.ctas = (int)(all < sms ? all : sms);
+    const int64_t all = (tp.N + T - 1) / T, most_ctas = (int64_t)sms * C;
+    p.ctas = (int)(all < most_ctas ? all : most_ctas);
     if (p.ctas > kTrainMaxCtas) p.ctas = kTrainMaxCtas;
-    const size_t tables = kFitWarps * ((NB + (NB < 2 ? NB : 2)) * 96 + NB * sizeof(float)), tile = (size_t)tile_boxes(tp.d) * T * 128;
-    int64_t ring = (int64_t)((kSmemBytes - tables - 1024) / tile);
+    const size_t tile = (size_t)tile_share(tp.d, T);
+    int64_t ring = (int64_t)((room - Fit8<NB, T, W>::kBytes) / tile);
     if (ring > kMaxTiles) ring = kMaxTiles;
     const int64_t most = (all + p.ctas - 1) / p.ctas;       // tiles of one CTA
     if (ring < 3 && most >= 3) return cudaErrorInvalidConfiguration;      // two tiles are in use while the next arrives
     if (ring > most) ring = most;
-    CUtensorMap map;
-    if (!packed_map(&map, tp.hidden, tp.N, tp.d, T)) return cudaErrorInvalidValue;
-    train8_kernel<NB, T><<<p.ctas, kFitThreads, tables + 1024 + (size_t)ring * tile, st>>>(p, map, (int)ring);
+    CUtensorMap map, emap;
+    if (!packed_map(&map, tp.hidden, tp.N, tp.d, 128, T) || !packed_map(&emap, tp.hidden, tp.N, tp.d, exponent_width(tp.d), T)) return cudaErrorInvalidValue;
+    train8_kernel<NB, T, W, C><<<p.ctas, Fit8<NB, T, W>::kThreads, (size_t)ring * tile + Fit8<NB, T, W>::kBytes, st>>>(p, map, emap, (int)ring);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};          // set up while the gradient kernel ends
@@ -485,13 +613,14 @@ cudaError_t launch_train8(const TrainParams &tp, cudaStream_t st)
     return cudaLaunchKernelEx(&cfg, train8_adam_kernel, p, 1.0 - pow(p.beta1, (double)p.t), 1.0 - pow(p.beta2, (double)p.t));
 }
 
-// Tiles of 32 rows, of 16 above 2048 columns: three of every width fit the ring.
+// Three tiles of 32 rows fit four CTAs to an SM up to 512 columns, two up to 1024 and one up to 2048; above that
+// three of 16 rows, whose residuals two blocks share a warp for.
 cudaError_t launch_train8_any(const TrainParams &tp, cudaStream_t st)
 {
-    const int nb = ((tp.d + 31) / 32 + kFitWarps - 1) / kFitWarps;
-    if (nb <= 1) return launch_train8<1, 32>(tp, st);
-    if (nb <= 2) return launch_train8<2, 32>(tp, st);
-    return launch_train8<4, 16>(tp, st);
+    if (tp.d <= 512) return launch_train8<4, 32, 4, 4>(tp, st);
+    if (tp.d <= 1024) return launch_train8<4, 32, 8, 2>(tp, st);
+    if (tp.d <= 2048) return launch_train8<4, 32, 16, 1>(tp, st);
+    return launch_train8<8, 16, 16, 1>(tp, st);
 }
 
 }  // namespace
