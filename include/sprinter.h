@@ -316,9 +316,10 @@ int verifier_train_step(const void *hidden, const uint8_t *labels, int64_t N, in
  * hidden [N,d] dt, W [V,d] dt (nn.Linear layout, no bias), targets [N] int32:
  *   lse[i]  = log sum_v exp(l_iv)                       (optional, NULL to skip)
  *   loss[i] = lse[i] - l_{i,targets[i]}, 0 where targets[i] < 0 (a padded position)
- * loss, lse [N] f32.  hidden and W are 16-byte aligned; any d and V.  bf16 operands with d a
- * multiple of 8 are read where they are, others are first laid out in the workspace (fp32 as
- * three bf16 parts, six products: as exact as fp32 products).
+ * loss, lse [N] f32.  hidden and W are 16-byte aligned; d up to 2^20, V up to 2^30.  bf16 operands with
+ * d a multiple of 8 are read where they are, others are first laid out in the workspace (fp32 as
+ * three bf16 parts, six products: as exact as fp32 products); small fp32 problems and a handful of
+ * tokens are worked on as they are, on the CUDA cores.
  * A row of hidden that holds infinities or NaN makes its own outputs NaN, no others.
  * Device-detected: targets[i] >= V -> loss[i] = -1, SPR_ERR_BAD_TOKEN.  If a bounded wait runs out
  * (SPR_ERR_TIMEOUT, as for verifier_train_step sticky until read) loss and lse are NaN.
@@ -386,7 +387,7 @@ int hidden_unpack8(const void *packed, int64_t N, int d, int dt, void *hidden, v
  * Same step, arguments and errors as verifier_train_step with s_i = the values that the packed
  * rows stand for (hidden_pack8), read once: 1.03 d bytes per sample.  The hyper-parameters are
  * doubles: 1 - beta2 would lose 1e-5 of itself if 0.999 were rounded to float.  packed: 16-byte aligned; d a
- * multiple of 16 and at most 4096 (otherwise SPR_ERR_UNSUPPORTED).
+ * multiple of 16 and at most 4096, N at most 0x7fff0000 (otherwise SPR_ERR_UNSUPPORTED).
  * Workspace: spr_workspace_bytes(SPR_OP_VERIFIER_TRAIN8, 0, 0, 0, d, 0, SPR_F32 or SPR_BF16).
  */
 int verifier_train_step8(const void *packed, const uint8_t *labels, int64_t N, int d, float *theta, float *adam_m,

@@ -211,8 +211,37 @@ def test_bounded_wait_runs_out_and_nothing_is_stepped(spr, N, d):
     assert torch.equal(loss, loss_ok) and all(torch.equal(x, w) for x, w in zip(state, want))
 
 
+@pytest.mark.parametrize("N,d", [(400001, 48), (330007, 512), (170001, 528), (90003, 1040), (85001, 2048), (50001, 2064)])
+def test_many_tiles_per_cta(spr, N, d):
+    """Rings of tiles go round several times, for every way the columns are dealt to warps.  Against float64: a
+    logit is off by dz = 2^-24 (d/32 + 16) sum_j |s_ij w_j|, hence a residual by dz / 4 and two roundings of its
+    own; residuals are written in 22 bits relative to the largest of a tile (at most 1), and at most 50 tiles are
+    added up in fp32.  So m = 0.1 grad is off by at most 0.1 mean_i |s_ij| times all that."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    S = torch.randn((N, d), generator=g, device="cuda", dtype=torch.float32).to(torch.bfloat16)
+    y = (torch.rand(N, generator=g, device="cuda") < 0.3).to(torch.uint8)
+    theta = torch.randn(d + 1, generator=g, device="cuda") / d ** 0.5
+    packed = spr.hidden_pack8(S)
+    X = spr.hidden_unpack8(packed, d, dtype=torch.float32).double()
+    w = theta.double()
+    z = X @ w[:d] + w[d]
+    r = torch.sigmoid(z) - y
+    state = [theta.clone(), torch.zeros_like(theta), torch.zeros_like(theta)]
+    ws = step_ws(spr, d)
+    loss = spr.verifier_train_step8(packed, d, y, *state, 1, 0.01, ws)
+    assert ws.device_status() == 0
+    A = X.abs()
+    dz = float((A @ w[:d].abs()).max() + w[d].abs()) * 2.0 ** -24 * (d / 32 + 16)
+    off = 2.0 ** -22 + 60 * 2.0 ** -24 + dz / 4
+    want = torch.cat([X.t() @ r, r.sum().reshape(1)]) / N
+    size = torch.cat([A.mean(0), torch.ones(1, device="cuda", dtype=torch.float64)])
+    assert bool(((state[1].double() - 0.1 * want).abs() <= 0.1 * off * size).all())
+    mean = float((torch.clamp(z, min=0) + torch.log1p(torch.exp(-z.abs())) - y * z).mean())
+    assert abs(float(loss) - mean) <= dz + 4 * 2.0 ** -24 * mean
+
+
 def test_weights_of_very_different_size_in_one_vector(spr):
-    """Sixteen weights share a unit: the small ones beside a large one are held to 2^-23 of the large one, so a
+    """The 32 weights of a block share a unit: the small ones beside a large one are held to 2^-23 of the large one, so a
     logit is off by at most sum_j |s_j| 2^-23 max|w| beside its fp32 roundings."""
     N, d = 64, 64
     g = torch.Generator().manual_seed(2)
@@ -227,7 +256,7 @@ def test_weights_of_very_different_size_in_one_vector(spr):
     st = [theta.cuda(), torch.zeros(d + 1, device="cuda"), torch.zeros(d + 1, device="cuda")]
     loss = float(spr.verifier_train_step8(packed, d, torch.from_numpy(y).cuda(), *st, 1, 0.01, step_ws(spr, d)))
     want, _ = training.bce_loss_and_grad(Sn, y, th)
-    top = np.abs(th[:d]).reshape(-1, 16).max(1).repeat(16)
+    top = np.abs(th[:d]).reshape(-1, 32).max(1).repeat(32)
     off = np.mean(np.abs(Sn) @ top) * 2.0 ** -23 + 2.0 ** -24 * 24 * np.mean(np.abs(Sn) @ np.abs(th[:d]) + abs(th[d]))
     assert abs(loss - want) <= off + 2.0 ** -22 * want
 
