@@ -483,8 +483,8 @@ cudaError_t stats_job(PairJob &j, PairOperand &a, PairOperand &b, const void *hi
 // the same on the CUDA cores
 void small_stats_job(SmallJob &j, const void *hidden, const void *W, int N, int d, int V, const float2 *part)
 {
-    j.a = SmallOperand{hidden, d, 1, 0, 0};
-    j.b = SmallOperand{W, d, 1, 0, 0};
+    j.a = SmallOperand{static_cast<const float *>(hidden), d, 1};
+    j.b = SmallOperand{static_cast<const float *>(W), d, 1};
     j.rows = N;
     j.cols = V;
     j.K = d;
@@ -532,12 +532,12 @@ cudaError_t other_stats(HeadRow &r, int N, int V, int dt, int *status, cudaStrea
     sp.status = status;
     small_stats_job(sp.job[0], r.hidden, r.W, N, r.d, V, r.part);
     r.parts = (int)ceil_div(V, kSmallTile);
-    return launch_small(SMALL_STATS, dt == SPR_F32, sp, 1, st);
+    return launch_small(SMALL_STATS, sp, 1, st);
 }
 
 // head_loss_grad on the CUDA cores: D in fp32, then both products in one launch
 cudaError_t small_grad(const void *hidden, const void *W, const int32_t *targets, const float *lse, const float *grad_loss, int N,
-                       int d, int V, int dt, void *d_hidden, void *d_W, float *D, float *acc, int *tickets, int *status, cudaStream_t st)
+                       int d, int V, void *d_hidden, void *d_W, float *D, float *acc, int *tickets, int *status, cudaStream_t st)
 {
     SmallParams sp;
     memset(&sp, 0, sizeof sp);
@@ -550,35 +550,36 @@ cudaError_t small_grad(const void *hidden, const void *W, const int32_t *targets
     j.targets = targets;
     j.lse = lse;
     j.grad_loss = grad_loss;
-    cudaError_t e = launch_small(SMALL_DLOGITS, dt == SPR_F32, sp, 1, st);
+    cudaError_t e = launch_small(SMALL_DLOGITS, sp, 1, st);
     if (e != cudaSuccess) return e;
     memset(sp.job, 0, sizeof sp.job);
     int jobs = 0;
     if (d_hidden) {               // dH [N, d] = D [N, V] W [V, d]: the longer contraction first
         SmallJob &h = sp.job[jobs++];
-        h.a = SmallOperand{D, V, 1, 1, 0};
-        h.b = SmallOperand{W, 1, d, 0, 1};
+        h.a = SmallOperand{D, V, 1};
+        h.b = SmallOperand{static_cast<const float *>(W), 1, d};
         h.rows = N;
         h.cols = d;
         h.K = V;
         h.splits = small_splits(V);
         h.acc = acc;
         h.tickets = tickets;
-        h.out = d_hidden;
+        h.out = static_cast<float *>(d_hidden);
         h.out_pitch = d;
     }
     if (d_W) {                    // dW [V, d] = D^T [V, N] H [N, d]
         SmallJob &w = sp.job[jobs++];
-        w.a = SmallOperand{D, 1, V, 1, 1};
-        w.b = SmallOperand{hidden, 1, d, 0, 1};
+        w.a = SmallOperand{D, 1, V};
+        w.a_across = 1;
+        w.b = SmallOperand{static_cast<const float *>(hidden), 1, d};
         w.live = targets;         // a row without a target may hold anything
         w.rows = V;
         w.cols = d;
         w.K = N;
-        w.out = d_W;
+        w.out = static_cast<float *>(d_W);
         w.out_pitch = d;
     }
-    return launch_small(SMALL_OUT, dt == SPR_F32, sp, jobs, st);
+    return launch_small(SMALL_OUT, sp, jobs, st);
 }
 
 bool head_sizes_ok(int64_t N, int d, int V) { return N >= 0 && d > 0 && d <= (1 << 20) && V > 0 && V <= (1 << 30); }
@@ -666,7 +667,7 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
     if (rc != SPR_OK) return rc;
 
     if (small_head(N, d, V, dt))
-        return finish(small_grad(hidden, W, targets, lse, grad_loss, N, d, V, dt, d_hidden, d_W, at<float>(ws, lay.dlogits),
+        return finish(small_grad(hidden, W, targets, lse, grad_loss, N, d, V, d_hidden, d_W, at<float>(ws, lay.dlogits),
                                  at<float>(ws, lay.acc), at<int>(ws, lay.tickets), at<int>(ws, 0), st));
     const bool f32 = dt == SPR_F32;
     const size_t es = elem_size(dt);

@@ -1,10 +1,14 @@
-// The vocabulary head's products where they are small: a few million multiply-adds, bound by latency.
+// The vocabulary head's products in fp32 where they are small: some million multiply-adds, bound by latency.
 //
 // The tensor-core kernels (head_gemm.cu) want operands laid out for them, tiles of 256 x 256 and some
 // microseconds to start: a problem of 67 x 257 x 1003 keeps 8 of 148 SMs busy there.  Here a CTA forms
-// a 32 x 32 tile in fp32 on the CUDA cores from the caller's own tensors, whatever their alignment.  Its
-// 1024 threads are four groups that each take a quarter of the contraction (the chain of loads is what
-// takes the time), double-buffered through registers; the four sums are added in order.
+// a 32 x 32 tile on the CUDA cores from the caller's own tensors, whatever their alignment.  Its 1024 threads
+// fetch 256 entries of the contraction at once, all loads in flight (a product of that depth then waits for memory once);
+// 16 groups of 64 threads take a sixteenth of them each, 4 x 4 results per thread (with 2 x 2 it was shared
+// memory that took the time: 30 us for the gradient of 67 x 257 x 1003), and a thread per result adds up the groups,
+// in order.
+#include <atomic>
+
 #include "head_small.h"
 
 #include "common.cuh"
@@ -15,46 +19,61 @@ namespace spr {
 namespace {
 
 constexpr int kTile = 32;
-constexpr int kGroups = 4;
-constexpr int kSmallThreads = 256 * kGroups;
-constexpr int kPitch = kTile + 2;        // even: pairs are read as float2
+constexpr int kDepth = 256;              // entries of the contraction in shared memory
+constexpr int kGroups = 16;
+constexpr int kSmallThreads = 1024;
+constexpr int kLoads = kTile * kDepth / kSmallThreads;
+constexpr int kPitch = kTile + 4;        // rows of 16-byte vectors
+constexpr int kOperand = kDepth * kPitch;
+constexpr size_t kSmallSmem = 2 * kOperand * sizeof(float);
+static_assert(kGroups * kTile * kTile <= 2 * kOperand, "the groups' sums take the operands' place");
 
-template <typename T>
-__device__ __forceinline__ float load_one(const SmallOperand &o, int64_t at)
+// A thread's elements of a 32 (m) x 256 (k) piece, u = 0 .. 7: neighbouring threads follow the contiguous axis, across
+// it in runs of eight so that the copies to shared memory meet no bank twice.
+template <bool ACROSS>
+struct Place {
+    int m, k;
+    __device__ __forceinline__ explicit Place(int t) : m(ACROSS ? t & 31 : (t & 31) >> 3), k(ACROSS ? t >> 5 : 8 * (t >> 5) + (t & 7)) {}
+    __device__ __forceinline__ int mu(int u) const { return ACROSS ? m : m + 4 * u; }
+    __device__ __forceinline__ int ku(int u) const { return ACROSS ? k + 32 * u : k; }
+};
+// Entries k0 .. k0 + depth - 1 of the contraction.  Every address is inside the operand (ms, depth >= 1; operands have less
+// than 2^31 elements), so that all loads are issued at once; what does not count is dropped behind them.  Where `live` is
+// given, entry k counts only if live[k] is a token of the vocabulary.
+template <bool ACROSS>
+__device__ __forceinline__ void fetch(const SmallOperand &o, int m0, int ms, int k0, int depth, const int32_t *live, int V,
+                                      float (&x)[kLoads])
 {
-    return o.f32 ? static_cast<const float *>(o.p)[at] : (float)static_cast<const T *>(o.p)[at];
-}
-// Four elements per thread of a 32 (k) x 32 (m) tile; neighbouring threads follow the contiguous axis.
-// Where `live` is given, entry k of the contraction counts only if live[k] is a token of the vocabulary.
-template <typename T>
-__device__ __forceinline__ void fetch(const SmallOperand &o, int m0, int ms, int k0, int k_end, int t, const int32_t *live, int V,
-                                      float (&x)[4])
-{
+    const Place<ACROSS> p(threadIdx.x);
+    const int stride = (int)(ACROSS ? o.sk : o.sm), rest = ms - m0;
+    const float *base = o.p + (ACROSS ? (int64_t)k0 * o.sk + m0 + min(p.m, rest - 1) : (int64_t)m0 * o.sm + k0 + min(p.k, depth - 1));
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int a = t & 31, b = (t >> 5) + 8 * u;
-        const int k = k0 + (o.across ? b : a), m = m0 + (o.across ? a : b);
-        bool there = k < k_end && m < ms;
-        if (there && live) {
-            const int tok = live[k];
-            there = tok >= 0 && tok < V;
-        }
-        x[u] = there ? load_one<T>(o, (int64_t)m * o.sm + (int64_t)k * o.sk) : 0.f;
-    }
-}
-__device__ __forceinline__ void put(float (*s)[kPitch], bool across, int t, const float (&x)[4])
-{
+    for (int u = 0; u < kLoads; ++u) x[u] = base[(ACROSS ? min(p.ku(u), depth - 1) : min(p.mu(u), rest - 1)) * stride];
+    if (live) {
+        int tok[kLoads];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int a = t & 31, b = (t >> 5) + 8 * u;
-        s[across ? b : a][across ? a : b] = x[u];
+        for (int u = 0; u < kLoads; ++u) tok[u] = live[k0 + min(p.ku(u), depth - 1)];
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u)
+            if (tok[u] < 0 || tok[u] >= V) x[u] = 0.f;
     }
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u)
+        if (p.ku(u) >= depth || p.mu(u) >= rest) x[u] = 0.f;
+}
+template <bool ACROSS>
+__device__ __forceinline__ void put(float *s, const float (&x)[kLoads])
+{
+    const Place<ACROSS> p(threadIdx.x);
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) s[p.ku(u) * kPitch + p.mu(u)] = x[u];
 }
 
-template <int MODE, typename T>
+template <int MODE>
 __global__ void __launch_bounds__(kSmallThreads) small_kernel(const SmallParams prm)
 {
-    __shared__ float sa[kGroups][kTile][kPitch], sb[kGroups][kTile][kPitch];
+    extern __shared__ __align__(16) float smem[];
+    float *sa = smem, *sb = smem + kOperand;
     pdl_trigger();
     int tile = blockIdx.x;
     const int first = prm.job[0].tiles_m * prm.job[0].tiles_n * prm.job[0].splits;      // CTAs of the first product
@@ -64,126 +83,122 @@ __global__ void __launch_bounds__(kSmallThreads) small_kernel(const SmallParams 
     const int tiles = j.tiles_m * j.tiles_n, split = tile / tiles;
     tile -= split * tiles;
     const int m0 = (tile / j.tiles_n) * kTile, n0 = (tile % j.tiles_n) * kTile;
-    const int g = threadIdx.x >> 8, t = threadIdx.x & 255;
-    const int ty = t >> 4, tx = t & 15;
-    const int per = (j.K + kGroups * j.splits - 1) / (kGroups * j.splits);
-    const int k_lo = min(j.K, (split * kGroups + g) * per), k_hi = min(j.K, k_lo + per);
-    float c[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
-    float xa[4], xb[4];
-    if (MODE == SMALL_OUT) pdl_wait();
-    fetch<T>(j.a, m0, j.rows, k_lo, k_hi, t, nullptr, 0, xa);
-    fetch<T>(j.b, n0, j.cols, k_lo, k_hi, t, j.live, prm.V, xb);
-    for (int k = k_lo; k < k_hi; k += kTile) {
-        put(sa[g], j.a.across, t, xa);
-        put(sb[g], j.b.across, t, xb);
-        asm volatile("bar.sync %0, 256;" ::"r"(g + 1) : "memory");
-        if (k + kTile < k_hi) {
-            fetch<T>(j.a, m0, j.rows, k + kTile, k_hi, t, nullptr, 0, xa);
-            fetch<T>(j.b, n0, j.cols, k + kTile, k_hi, t, j.live, prm.V, xb);
-        } else {
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    const int per = (j.K + j.splits - 1) / j.splits;
+    const int k_lo = min(j.K, split * per), k_hi = min(j.K, k_lo + per);
+    const int rounds = (k_hi - k_lo + kDepth - 1) / kDepth, depth = rounds ? (k_hi - k_lo + rounds - 1) / rounds : 0;
+    // 4 x 4 results of a group: rows 4 ty .. + 3, columns 4 tx .. + 3
+    const int g = t >> 6, ty = (t >> 3) & 7, tx = t & 7;
+    float c[4][4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) xa[u] = xb[u] = 0.f;
-        }
-#pragma unroll 8
-        for (int i = 0; i < kTile; ++i) {
-            const float2 a = *reinterpret_cast<const float2 *>(&sa[g][i][2 * ty]);
-            const float2 b = *reinterpret_cast<const float2 *>(&sb[g][i][2 * tx]);
-            c[0][0] = fmaf(a.x, b.x, c[0][0]);
-            c[0][1] = fmaf(a.x, b.y, c[0][1]);
-            c[1][0] = fmaf(a.y, b.x, c[1][0]);
-            c[1][1] = fmaf(a.y, b.y, c[1][1]);
-        }
-        asm volatile("bar.sync %0, 256;" ::"r"(g + 1) : "memory");
-    }
-    // the groups' sums, in order
-    float4 *red = reinterpret_cast<float4 *>(&sa[0][0][0]);
-    __syncthreads();
-    if (g > 0) red[(g - 1) * 256 + t] = make_float4(c[0][0], c[0][1], c[1][0], c[1][1]);
-    __syncthreads();
-    if (g > 0) return;
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
-    for (int i = 0; i < kGroups - 1; ++i) {
-        const float4 y = red[i * 256 + t];
-        c[0][0] += y.x;
-        c[0][1] += y.y;
-        c[1][0] += y.z;
-        c[1][1] += y.w;
+        for (int e = 0; e < 4; ++e) c[r][e] = 0.f;
+    constexpr bool kBAcross = MODE == SMALL_OUT;
+    const bool a_across = MODE == SMALL_OUT && j.a_across;
+    float xa[kLoads], xb[kLoads];
+    auto fetch_a = [&](int k, int n) {
+        if (a_across) fetch<true>(j.a, m0, j.rows, k, n, nullptr, 0, xa);
+        else fetch<false>(j.a, m0, j.rows, k, n, nullptr, 0, xa);
+    };
+    if (rounds) fetch<kBAcross>(j.b, n0, j.cols, k_lo, depth, j.live, prm.V, xb);
+    if (MODE == SMALL_OUT) pdl_wait();        // the first operand is the kernel's before this one
+    if (rounds) fetch_a(k_lo, depth);
+    for (int k0 = k_lo; k0 < k_hi; k0 += depth) {
+        if (k0 > k_lo) __syncthreads();
+        if (a_across) put<true>(sa, xa);
+        else put<false>(sa, xa);
+        put<kBAcross>(sb, xb);
+        __syncthreads();
+        const int here = min(depth, k_hi - k0), next = min(depth, k_hi - k0 - depth);
+        if (next > 0) {
+            fetch_a(k0 + depth, next);
+            fetch<kBAcross>(j.b, n0, j.cols, k0 + depth, next, j.live, prm.V, xb);
+        }
+        const int share = (here + kGroups - 1) / kGroups, i1 = min(here, (g + 1) * share);
+#pragma unroll 4
+        for (int i = g * share; i < i1; ++i) {
+            const float4 a = *reinterpret_cast<const float4 *>(sa + i * kPitch + 4 * ty), b = *reinterpret_cast<const float4 *>(sb + i * kPitch + 4 * tx);
+            const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) c[r][e] = fmaf(av[r], bv[e], c[r][e]);
+        }
     }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<float4 *>(smem + (g * kTile + 4 * ty + r) * kTile + 4 * tx) = make_float4(c[r][0], c[r][1], c[r][2], c[r][3]);
+    __syncthreads();
+    float x = smem[t];               // row `warp`, column `lane` of the tile
+#pragma unroll
+    for (int i = 1; i < kGroups; ++i) x += smem[i * kTile * kTile + t];
     if (MODE == SMALL_OUT && j.splits > 1) {
         // the CTA that takes the tile's last ticket adds the splits' sums up, in order
         __shared__ int last;
-        float4 *mine = reinterpret_cast<float4 *>(j.acc) + ((int64_t)split * tiles + tile) * 256 + t;
-        *mine = make_float4(c[0][0], c[0][1], c[1][0], c[1][1]);
+        j.acc[((int64_t)split * tiles + tile) * kSmallThreads + t] = x;
         __threadfence();
-        asm volatile("bar.sync 1, 256;" ::: "memory");
+        __syncthreads();
         if (t == 0) last = take_ticket(&j.tickets[tile], j.splits);
-        asm volatile("bar.sync 1, 256;" ::: "memory");
+        __syncthreads();
         if (!last) return;
         __threadfence();
-        const float4 *from = reinterpret_cast<const float4 *>(j.acc) + (int64_t)tile * 256 + t;
-        float4 sum = __ldcg(from);
-#pragma unroll 4
-        for (int s = 1; s < j.splits; ++s) {
-            const float4 y = __ldcg(from + (int64_t)s * tiles * 256);
-            sum = make_float4(sum.x + y.x, sum.y + y.y, sum.z + y.z, sum.w + y.w);
-        }
-        c[0][0] = sum.x;
-        c[0][1] = sum.y;
-        c[1][0] = sum.z;
-        c[1][1] = sum.w;
+        const float *from = j.acc + (int64_t)tile * kSmallThreads + t;
+        x = __ldcg(from);
+#pragma unroll 8
+        for (int s = 1; s < j.splits; ++s) x += __ldcg(from + (int64_t)s * tiles * kSmallThreads);
     }
-    const int col = n0 + 2 * tx;
+    const int row = m0 + warp, col = n0 + lane;
+    if (row >= j.rows) return;       // a whole warp
+    if (MODE == SMALL_STATS) {
+        // (max, sum of exp) over the tile's columns
+        float m = col < j.cols ? x : neg_inf();
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int row = m0 + 2 * ty + h;
-        if (MODE == SMALL_STATS) {
-            // (max, sum of exp) over the tile's columns: a row is 16 lanes
-            float m = fmaxf(col < j.cols ? c[h][0] : neg_inf(), col + 1 < j.cols ? c[h][1] : neg_inf());
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        float s = col < j.cols ? ex2((x - (m == neg_inf() ? 0.f : m)) * kLog2e) : 0.f;
 #pragma unroll
-            for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-            const float ref = m == neg_inf() ? 0.f : m;
-            float s = (col < j.cols ? ex2((c[h][0] - ref) * kLog2e) : 0.f) + (col + 1 < j.cols ? ex2((c[h][1] - ref) * kLog2e) : 0.f);
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-            if (tx == 0 && row < j.rows) j.part[(int64_t)row * j.tiles_n + n0 / kTile] = make_float2(m, s);
-        } else if (row < j.rows) {
-            if (MODE == SMALL_DLOGITS) {
-                const int tok = j.targets[row];
-                const bool keep = tok >= 0 && tok < prm.V;
-                if (tok >= prm.V && n0 == 0 && tx == 0) raise_status(prm.status, SPR_ERR_BAD_TOKEN);
-                const float lse = keep ? j.lse[row] : 0.f, w = keep ? j.grad_loss[row] : 0.f;
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    if (col + e < j.cols)
-                        j.d[(int64_t)row * j.d_pitch + col + e] = keep ? w * expf(c[h][e] - lse) - (col + e == tok ? w : 0.f) : 0.f;
-            } else {
-                T *o = static_cast<T *>(j.out) + (int64_t)row * j.out_pitch + col;
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    if (col + e < j.cols) o[e] = (T)c[h][e];
-            }
-        }
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (lane == 0) j.part[(int64_t)row * j.tiles_n + n0 / kTile] = make_float2(m, s);
+    } else if (MODE == SMALL_DLOGITS) {
+        const int tok = j.targets[row];
+        const bool keep = tok >= 0 && tok < prm.V;
+        if (tok >= prm.V && n0 == 0 && lane == 0) raise_status(prm.status, SPR_ERR_BAD_TOKEN);
+        const float lse = keep ? j.lse[row] : 0.f, w = keep ? j.grad_loss[row] : 0.f;
+        if (col < j.cols) j.d[(int64_t)row * j.d_pitch + col] = keep ? w * expf(x - lse) - (col == tok ? w : 0.f) : 0.f;
+    } else if (col < j.cols) {
+        j.out[(int64_t)row * j.out_pitch + col] = x;
     }
 }
 
 template <int MODE>
-cudaError_t launch_mode(const SmallParams &prm, unsigned ctas, bool f32, bool behind, cudaStream_t st)
+cudaError_t launch_mode(const SmallParams &prm, unsigned ctas, bool behind, cudaStream_t st)
 {
+    static std::atomic<bool> attr_set[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
+        e = cudaFuncSetAttribute(small_kernel<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas);
     cfg.blockDim = dim3(kSmallThreads);
+    cfg.dynamicSmemBytes = kSmallSmem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = behind ? 1 : 0;
-    return f32 ? cudaLaunchKernelEx(&cfg, small_kernel<MODE, float>, prm) : cudaLaunchKernelEx(&cfg, small_kernel<MODE, __nv_bfloat16>, prm);
+    return cudaLaunchKernelEx(&cfg, small_kernel<MODE>, prm);
 }
 
 }  // namespace
 
-cudaError_t launch_small(SmallMode mode, bool f32, SmallParams &prm, int njobs, cudaStream_t st)
+cudaError_t launch_small(SmallMode mode, SmallParams &prm, int njobs, cudaStream_t st)
 {
     int64_t ctas = 0;
     for (int i = 0; i < njobs; ++i) {
@@ -195,9 +210,9 @@ cudaError_t launch_small(SmallMode mode, bool f32, SmallParams &prm, int njobs, 
     }
     if (ctas > 0x7fffffff) return cudaErrorInvalidValue;
     switch (mode) {
-    case SMALL_STATS: return launch_mode<SMALL_STATS>(prm, (unsigned)ctas, f32, false, st);
-    case SMALL_DLOGITS: return launch_mode<SMALL_DLOGITS>(prm, (unsigned)ctas, f32, false, st);
-    default: return launch_mode<SMALL_OUT>(prm, (unsigned)ctas, f32, true, st);
+    case SMALL_STATS: return launch_mode<SMALL_STATS>(prm, (unsigned)ctas, false, st);
+    case SMALL_DLOGITS: return launch_mode<SMALL_DLOGITS>(prm, (unsigned)ctas, false, st);
+    default: return launch_mode<SMALL_OUT>(prm, (unsigned)ctas, true, st);
     }
 }
 

@@ -1,4 +1,4 @@
-// Small products of the vocabulary head on the CUDA cores (head_small.cu): parameter blocks and launcher.
+// Small fp32 products of the vocabulary head on the CUDA cores (head_small.cu): parameter blocks and launcher.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -11,18 +11,17 @@ constexpr int kSmallTile = 32;
 enum SmallMode {
     SMALL_STATS = 0,   // (max, sum of exp) of each row over the tile's 32 columns
     SMALL_DLOGITS,     // softmax gradient of each logit, fp32
-    SMALL_OUT          // the product in the caller's type (launched behind the kernel before it)
+    SMALL_OUT          // the product itself (launched behind the kernel before it)
 };
 
-// element (m, k) of an operand is p[m sm + k sk], fp32 or the caller's type
+// element (m, k) of an operand is p[m sm + k sk]
 struct SmallOperand {
-    const void *p;
+    const float *p;
     int64_t sm, sk;
-    int f32;
-    int across;        // the contiguous axis is m, not k
 };
 struct SmallJob {
-    SmallOperand a, b;
+    SmallOperand a, b;          // k is the contiguous axis (SMALL_OUT: m is that of b)
+    int a_across;               // SMALL_OUT: m is that of a, too
     int rows, cols, K;
     int splits;                 // CTAs that share a tile's contraction (SMALL_OUT; 0 counts as 1)
     float *acc;                 // splits > 1: their sums, [splits][tiles][1024]
@@ -34,7 +33,7 @@ struct SmallJob {
     int64_t d_pitch;
     const int32_t *targets;
     const float *lse, *grad_loss;
-    void *out;                  // SMALL_OUT
+    float *out;                 // SMALL_OUT
     int64_t out_pitch;
 };
 struct SmallParams {
@@ -42,6 +41,6 @@ struct SmallParams {
     int V;
     int *status;
 };
-cudaError_t launch_small(SmallMode mode, bool f32, SmallParams &prm, int njobs, cudaStream_t st);
+cudaError_t launch_small(SmallMode mode, SmallParams &prm, int njobs, cudaStream_t st);
 
 }  // namespace spr
