@@ -293,22 +293,25 @@ bool needs_pack(int d, int dt) { return dt == SPR_F32 || d % 8 != 0; }
 int parts(int dt) { return dt == SPR_F32 ? 3 : 1; }
 size_t packed_bytes(int64_t rows, int d, int dt) { return 2 * (size_t)rows * parts(dt) * (size_t)round_up(d, 64); }
 
-// fp32 problems of up to 2^26 multiply-adds, rows counted in tiles of 32, go to the CUDA cores
-// (head_small.cu); above that the six bf16 products on the tensor cores are faster.  Measured (us, CUDA cores /
-// tensor cores): loss 4x256x1000 9 / 19, 64x256x4000 18.5 / 20, 64x512x4000 31 / 30; gradient 67x257x1003
-// 30 / 69, 64x256x4000 66 / 76, 256x128x4000 103 / 71.  (bf16: 16x256x4000 11 / 9 and worse from there.)
-bool small_head(int64_t N, int d, int64_t V, int dt)
-{
-    return dt == SPR_F32 && (double)round_up(N, 32) * (double)V * (double)d <= (double)(1 << 26);
-}
-// A handful of tokens: one pass over W as it is (head_stream.cu).  fp32 heads that would have to be laid out in
-// three parts first: up to eight tokens; bf16 heads with rows that TMA cannot take: up to four; others: one.
-// Measured (us, one pass / tensor cores, d = 2048, V = 32000): f32 N = 8 loss 99 / 293, gradient 259 / 887; bf16
-// N = 1 34 / 46 and 119 / 145, N = 4 46 / 39 and 159 / 135; bf16 d = 1001, N = 4 40 / 55 and 155 / 187.
-bool stream_head(bool grad, int64_t N, int d, int64_t V, int dt)
+// A handful of tokens: one pass over W as it is (head_stream.cu).  fp32: up to eight tokens, whatever the size; bf16 heads
+// with rows that TMA cannot take: up to four; others: one.  Measured (us, one pass / tensor cores, d = 2048,
+// V = 32000): f32 N = 8 loss 99 / 293, gradient 259 / 887; bf16 N = 1 34 / 46 and 119 / 145, N = 4 46 / 39 and 159 / 135;
+// bf16 d = 1001, N = 4 40 / 55 and 155 / 187.  (us, one pass / tiles of head_small.cu): f32 4x256x1000 5.4 / 8.2 and
+// 10.2 / 16.8, 8x64x500 5.3 / 6.8 and 11.3 / 11.7, 8x1024x512 14 / 18 and 24 / 37, 1x768x1000 6.3 / 15 and 10 / 41.
+bool stream_head(bool grad, int64_t N, int d, int dt)
 {
     const int most = dt == SPR_F32 ? kStreamTokens : d % 8 != 0 ? 4 : 1;
-    return N <= most && !small_head(N, d, V, dt) && stream_fits(grad, (int)N, d, dt == SPR_F32);
+    return N <= most && stream_fits(grad, (int)N, d, dt == SPR_F32);
+}
+// More fp32 tokens go to the CUDA cores where that is less than 2^27 multiply-adds (head_small.cu: whole tiles of 32 x 32,
+// each of which costs what 200 entries of its contraction do); above that the six bf16 products on the tensor cores are
+// faster.  Measured (us, CUDA cores / tensor cores): loss 64x256x4000 15 / 20, 128x512x1000 13 / 28, 9x1024x2000 19 / 46,
+// 64x512x4000 29 / 29, 256x128x2000 23 / 15; gradient 67x257x1003 24.5 / 69, 64x256x4000 60 / 73, 256x128x2000 47 / 56,
+// 32x128x16000 95 / 79, 256x128x4000 103 / 71.  (bf16: 16x256x4000 11 / 9 and worse from there.)
+bool small_head(bool grad, int64_t N, int d, int64_t V, int dt)
+{
+    return dt == SPR_F32 && !stream_head(grad, N, d, dt) &&
+           (double)round_up(N, kSmallTile) * (double)round_up(V, kSmallTile) * (d + 200.0) <= (double)(1 << 27);
 }
 // dH's contraction over the vocabulary there: 256 of it per CTA
 int small_splits(int V) { return (int)(ceil_div(V, 256) < 64 ? ceil_div(V, 256) : 64); }
@@ -320,12 +323,12 @@ struct HeadLossWs {
 HeadLossWs head_loss_layout(Carver &c, int64_t N, int d, int V, int dt)
 {
     HeadLossWs w;
-    if (small_head(N, d, V, dt)) {
+    if (small_head(false, N, d, V, dt)) {
         w.hidden = w.W = 0;
         w.part = c.take_data(8 * (size_t)N * (size_t)ceil_div(V, kSmallTile));
         return w;
     }
-    if (stream_head(false, N, d, V, dt)) {
+    if (stream_head(false, N, d, dt)) {
         w.hidden = w.W = 0;
         w.part = c.take_data(8 * (size_t)N * (size_t)stream_ctas(false, (int)N, d, V));
         return w;
@@ -372,7 +375,7 @@ struct HeadGradWs {
 HeadGradWs head_grad_layout(Carver &c, int64_t N, int d, int V, int dt)
 {
     HeadGradWs w;
-    if (small_head(N, d, V, dt)) {
+    if (small_head(true, N, d, V, dt)) {
         const size_t tiles = (size_t)ceil_div(N, kSmallTile) * (size_t)ceil_div(d, kSmallTile);
         w.hidden = w.W = 0;
         w.tickets = c.take_tickets(tiles);
@@ -380,7 +383,7 @@ HeadGradWs head_grad_layout(Carver &c, int64_t N, int d, int V, int dt)
         w.acc = c.take_data(4 * 1024 * tiles * (size_t)small_splits(V));
         return w;
     }
-    if (stream_head(true, N, d, V, dt)) {
+    if (stream_head(true, N, d, dt)) {
         w.hidden = w.W = w.tickets = w.dlogits = 0;
         w.acc = c.take_data(4 * (size_t)stream_ctas(true, (int)N, d, V) * (size_t)N * (size_t)round_up(d, 64));
         return w;
@@ -520,7 +523,7 @@ StreamParams stream_params(const void *hidden, const void *W, int N, int d, int 
 // row statistics of one model by whichever kernel the sizes call for, except the tensor cores'
 cudaError_t other_stats(HeadRow &r, int N, int V, int dt, int *status, cudaStream_t st)
 {
-    if (stream_head(false, N, r.d, V, dt)) {
+    if (stream_head(false, N, r.d, dt)) {
         StreamParams p = stream_params(r.hidden, r.W, N, r.d, V, dt);
         p.part = const_cast<float2 *>(r.part);
         r.parts = stream_ctas(false, N, r.d, V);
@@ -629,7 +632,7 @@ int head_loss(const void *hidden, const void *W, const int32_t *targets, int N, 
     prm.status = at<int>(ws, 0);
     HeadRow h = {hidden, W, at<float2>(ws, lay.part), d, 0};
     cudaError_t e;
-    if (small_head(N, d, V, dt) || stream_head(false, N, d, V, dt)) {
+    if (small_head(false, N, d, V, dt) || stream_head(false, N, d, dt)) {
         e = other_stats(h, N, V, dt, prm.status, st);
     } else {
         PairOperand a, b;
@@ -666,12 +669,12 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
     int rc = device_supported();
     if (rc != SPR_OK) return rc;
 
-    if (small_head(N, d, V, dt))
+    if (small_head(true, N, d, V, dt))
         return finish(small_grad(hidden, W, targets, lse, grad_loss, N, d, V, d_hidden, d_W, at<float>(ws, lay.dlogits),
                                  at<float>(ws, lay.acc), at<int>(ws, lay.tickets), at<int>(ws, 0), st));
     const bool f32 = dt == SPR_F32;
     const size_t es = elem_size(dt);
-    if (stream_head(true, N, d, V, dt)) {
+    if (stream_head(true, N, d, dt)) {
         StreamParams p = stream_params(hidden, W, N, d, V, dt);
         p.targets = targets;
         p.lse = lse;
@@ -803,7 +806,7 @@ int verifier_labels_head(const void *p_hidden, const void *p_W, int dp, const vo
     for (int i = 0; i < 2 && e == cudaSuccess; ++i) {
         const bool is_p = (i == 0) == (dp >= dq);
         HeadRow &r = is_p ? p : q;
-        if (small_head(N, r.d, V, dt) || stream_head(false, N, r.d, V, dt)) {
+        if (small_head(false, N, r.d, V, dt) || stream_head(false, N, r.d, dt)) {
             e = other_stats(r, N, V, dt, prm.status, st);
         } else {
             e = stats_job(prm.job[pairs], a[pairs], b[pairs], r.hidden, r.W, N, r.d, V, dt, ws, is_p ? lay.p : lay.q, st);

@@ -116,6 +116,15 @@ def test_loss_and_gradient(spr, N, d, V, dtype):
     check_grad(spr, h, w, t, gl, lse)
 
 
+@pytest.mark.parametrize("N,d,V", [(20, 40, 17001), (500, 8, 1001), (33, 900, 1500), (9, 1001, 2003), (257, 257, 257), (31, 513, 33),
+                                   (8, 770, 1001), (7, 1, 3), (1, 4001, 999)])
+def test_small_fp32_heads(spr, N, d, V):
+    """Contractions of one round and of several, cut among CTAs or not; and a handful of tokens of a small head."""
+    h, w, t, gl = problem(N, d, V, torch.float32, seed=N + d + V)
+    _, lse = check_loss(spr, h, w, t)
+    check_grad(spr, h, w, t, gl, lse)
+
+
 @pytest.mark.parametrize("N,d,V,dtype", [(2048, 512, 30011, torch.bfloat16), (4096, 256, 128256, torch.bfloat16),
                                          (700, 264, 50257, torch.bfloat16), (1500, 136, 33000, torch.float32)],
                          ids=lambda v: str(v).replace("torch.", ""))
