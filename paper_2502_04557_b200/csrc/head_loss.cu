@@ -28,8 +28,11 @@ namespace spr {
 namespace {
 
 constexpr int kHeadMaxLambdas = 8;
-// Blocks of 64 that an accumulator takes (head_gemm.cu): results in bf16 do not show its truncation.
-constexpr int kChunkStats = 8, kChunkF32 = 2;
+// Blocks of 64 that an accumulator takes (head_gemm.cu): results in bf16 do not show its truncation.  For row statistics
+// the contraction is cut into chunks of one length, at most 8: what truncation takes off grows with the length (N(0, 9)
+// logits: a log-sum-exp is 2.2e-7 of itself low with 8, 1.2e-7 with 4), and so does the rate (4096x2048x128256: 1570 us
+// with 8, 1728 with 4).
+constexpr int kChunkStats = 8, kChunkStatsLeast = 5, kChunkF32 = 2;
 constexpr size_t kPieceBytes = (size_t)256 << 20;        // D of one vocabulary piece (see pieces())
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -473,7 +476,7 @@ cudaError_t stats_job(PairJob &j, PairOperand &a, PairOperand &b, const void *hi
     }
     memset(&j, 0, sizeof j);
     contraction(j, d, dt);
-    if (dt != SPR_F32) j.kc = kChunkStats;
+    if (dt != SPR_F32) j.kc = (int)ceil_div(j.kb, ceil_div(j.kb, kChunkStats));
     j.tiles_m = (int)ceil_div(N, kPairTile);
     j.tiles_n = (int)ceil_div(V, kPairTile);
     j.a_seg = j.b_seg = (int)round_up(d, 64);
@@ -813,6 +816,13 @@ int verifier_labels_head(const void *p_hidden, const void *p_W, int dp, const vo
             ++pairs;
             r.parts = 2 * (int)ceil_div(V, kPairTile);
         }
+    }
+    if (dt != SPR_F32 && pairs == 2) {
+        // Chunks of one length in both products, so that truncation does the same to both log-sum-exps and cancels in the
+        // ratio (768 and 1536 elements: ratios off by 4e-7 instead of 1.3e-6); short ones would slow the longer product down.
+        int kc = prm.job[0].kc < prm.job[1].kc ? prm.job[0].kc : prm.job[1].kc;
+        if (kc < kChunkStatsLeast) kc = kChunkStatsLeast;
+        prm.job[0].kc = prm.job[1].kc = kc;
     }
     if (e == cudaSuccess && pairs) e = launch_pair(PAIR_STATS, dt == SPR_F32, prm, pairs, a, b, false, st);
     if (e == cudaSuccess) {
