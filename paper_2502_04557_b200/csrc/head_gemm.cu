@@ -27,10 +27,18 @@
 //
 // Warp roles (320 threads): warp 0 = TMA producer, warp 1 = TMEM owner and MMA issuer, warps
 // 2..9 = epilogue (warp w reads TMEM lanes 32 (w % 4) .. + 31, one row per thread, and half of the
-// tile's 256 columns: all 128 in registers where chunks are added up, else 32 at a time).  Results go out through 4 KB of shared memory per warp, so that a store instruction writes whole 128-byte
-// lines (a thread per row would touch 32 lines with each).  Every wait is bounded: when one
+// tile's 256 columns: all 128 in registers where chunks are added up, else 32 at a time).  Results go
+// out through 4 KB of shared memory per warp: bf16 as TMA boxes of 64 columns by 32 rows (against stores from
+// registers: gradient of 256x768x50257 86 -> 84 us, 128x4096x32000 241 -> 229 us), the rest in store instructions that
+// write whole 128-byte lines (a thread per row would touch 32 lines with each).  Every wait is bounded: when one
 // runs out the status word becomes SPR_ERR_TIMEOUT, all roles leave their loops, the even CTA
 // waits (again bounded) for the copies and products in flight, and both CTAs meet before they exit.
+//
+// What bounds it.  An SM takes in some 41 bytes a clock from L2 whatever the tiles, so that a step of 64 KB per pair
+// takes 0.42 us (1424 TFLOP/s over 74 pairs; measured 4096x2048x128256: loss 1510 - 1770 us, 1.22 - 1.43 PFLOP/s as the
+// power cap allows, the library's plain bf16 product 1.39 sustained).  With a few hundred tokens: one sweep over W in
+// waves of 74 tiles (256x768x50257: 197 tiles, three waves where 2.66 are work), and for the gradient the write
+// of dW (memory takes in 3.9 TB/s of pure writes: 20 us there).
 #include <atomic>
 
 #include "head_gemm.h"
@@ -189,6 +197,7 @@ template <int EPI, typename T>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ CUtensorMap map_b0,
             const __grid_constant__ CUtensorMap map_a1, const __grid_constant__ CUtensorMap map_b1,
+            const __grid_constant__ CUtensorMap map_out0, const __grid_constant__ CUtensorMap map_out1,
             const __grid_constant__ PairParams prm)
 {
     extern __shared__ unsigned char smem_raw[];
@@ -374,6 +383,19 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                     return x[0];
                 }
             };
+            // 64 columns of bf16 (16 of two each), h = 0 or 1, as a box of 32 rows: written swizzled, so that no bank is met
+            // twice, and on their way while the next ones are formed
+            const CUtensorMap *map_out = it.job ? &map_out1 : &map_out0;
+            auto put_box = [&](int h, const float(&line)[32], int c, int64_t r, int64_t cols) {
+                if (lane == 0) stores_read();
+                __syncwarp();
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    stage[lane * 8 + (e ^ (lane & 7))] = make_float4(line[4 * e], line[4 * e + 1], line[4 * e + 2], line[4 * e + 3]);
+                fence_stores();
+                __syncwarp();
+                if (lane == 0 && c + 64 * h < cols && r < j.rows) store_box(map_out, c + 64 * h, (int)r, stage);
+            };
             const int64_t row = (int64_t)it.m * kPairTile + r_in;
             const bool live = row < j.rows;
             const int c0 = it.n * kPairTile + half * 128;
@@ -414,13 +436,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                         // 64 columns of bf16 are a line of 128 bytes: two groups go out as one
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) line[16 * (q & 1) + e / 2] = __uint_as_float(pack_bf16(y[e], y[e + 1]));
-                        if (q & 1) {
-                            by_rows(line, v, stage, lane);
-                            __nv_bfloat16 *o = dst + 64 * (q >> 1);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i, o += step)
-                                if (4 * i < rows) *reinterpret_cast<float4 *>(o) = v[i];
-                        }
+                        if (q & 1) put_box(q >> 1, line, c0, row - lane, seg);
                         continue;
                     }
                     by_rows(y, v, stage, lane);
@@ -449,9 +465,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                 T *o = static_cast<T *>(j.out) + r0 * j.out_pitch + cl;                         // used where there is an out
                 // four elements of the caller's type are stored at once where every row allows it
                 const bool vec = ((reinterpret_cast<uintptr_t>(j.out) | (uintptr_t)(j.out_pitch * (int64_t)sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
-                if (sizeof(T) == 2 && to_out && !add && width == 128 && (((uintptr_t)j.out | (uintptr_t)(2 * j.out_pitch)) & 15) == 0) {
-                    // 64 columns of bf16 are a line of 128 bytes: whole lines where nothing is added and no column missing
-                    T *p0 = static_cast<T *>(j.out) + r0 * j.out_pitch + c0 + 8 * (lane & 7);
+                if (sizeof(T) == 2 && j.boxes) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         float line[32];
@@ -461,12 +475,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
 #pragma unroll
                             for (int e = 0; e < 32; e += 2) line[16 * (q & 1) + e / 2] = __uint_as_float(pack_bf16(y[e], y[e + 1]));
                         }
-                        float4 v[8];
-                        by_rows(line, v, stage, lane);
-                        T *p = p0 + 64 * h;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i, p += out_step)
-                            if (4 * i < rows) *reinterpret_cast<float4 *>(p) = v[i];
+                        put_box(h, line, c0, row - lane, j.cols);
                     }
                 } else
 #pragma unroll
@@ -507,6 +516,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
             }
             __syncwarp();
         }
+        if (sizeof(T) == 2 && lane == 0) stores_done();
     }
 
     // ---------------- way out
@@ -551,14 +561,14 @@ EncodeTiledFn encode_fn()
     return fn;
 }
 
-// boxes of 64 x 64 elements, 128-byte swizzle, zeros outside
-bool make_map(CUtensorMap *map, const PairOperand &t)
+// boxes of 64 x `rows` elements, 128-byte swizzle, zeros outside
+bool make_map(CUtensorMap *map, const PairOperand &t, int rows)
 {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     const cuuint64_t dims[2] = {(cuuint64_t)t.cols, (cuuint64_t)t.rows};
     const cuuint64_t strides[1] = {(cuuint64_t)t.pitch * 2};
-    const cuuint32_t box[2] = {64, 64};
+    const cuuint32_t box[2] = {64, (cuuint32_t)rows};
     const cuuint32_t elem[2] = {1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(t.base), dims, strides, box, elem,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
@@ -566,7 +576,7 @@ bool make_map(CUtensorMap *map, const PairOperand &t)
 }
 
 template <int EPI, typename T>
-cudaError_t launch(const CUtensorMap (&maps)[4], const PairParams &prm, int ctas, int dev, bool behind, cudaStream_t st)
+cudaError_t launch(const CUtensorMap (&maps)[6], const PairParams &prm, int ctas, int dev, bool behind, cudaStream_t st)
 {
     static std::atomic<bool> attr_set[64];   // host threads may race to set it: all of them store `true`
     if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
@@ -585,7 +595,7 @@ cudaError_t launch(const CUtensorMap (&maps)[4], const PairParams &prm, int ctas
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = behind ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, pair_kernel<EPI, T>, maps[0], maps[1], maps[2], maps[3], prm);
+    return cudaLaunchKernelEx(&cfg, pair_kernel<EPI, T>, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], prm);
 }
 
 }  // namespace
@@ -601,12 +611,22 @@ cudaError_t launch_pair(PairEpilogue epi, bool f32, PairParams &prm, int njobs, 
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
-    CUtensorMap maps[4];
-    for (int i = 0; i < njobs; ++i)
-        if (!make_map(&maps[2 * i], a[i]) || !make_map(&maps[2 * i + 1], b[i])) return cudaErrorInvalidValue;
+    CUtensorMap maps[6];
+    for (int i = 0; i < njobs; ++i) {
+        if (!make_map(&maps[2 * i], a[i], 64) || !make_map(&maps[2 * i + 1], b[i], 64)) return cudaErrorInvalidValue;
+        // bf16 results go out as boxes where nothing is added to them and their rows are whole 16-byte vectors
+        PairJob &j = prm.job[i];
+        PairOperand out = {nullptr, j.rows, 0, 0};
+        if (!f32 && epi == PAIR_DLOGITS) out = PairOperand{j.dlogits, j.rows, j.dl_seg, j.dl_pitch};
+        if (!f32 && epi == PAIR_OUT && !j.add_acc && j.out_pitch % 8 == 0) out = PairOperand{j.out, j.rows, j.cols, j.out_pitch};
+        j.boxes = out.base != nullptr;
+        maps[4 + i] = maps[0];
+        if (j.boxes && !make_map(&maps[4 + i], out, 32)) return cudaErrorInvalidValue;
+    }
     if (njobs == 1) {       // not used
         maps[2] = maps[0];
         maps[3] = maps[1];
+        maps[5] = maps[0];
     }
     int pairs = sms / 2 < kMaxPairs ? sms / 2 : kMaxPairs;
     int64_t total = 0;

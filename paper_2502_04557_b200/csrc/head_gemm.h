@@ -45,6 +45,7 @@ struct PairJob {
     // acc[split * acc_stride + row * acc_pitch + column]; add_acc: acc is added to the product first
     void *out;
     int64_t out_pitch;
+    int boxes;                    // PAIR_DLOGITS, PAIR_OUT: bf16 results go out as TMA boxes (set by launch_pair)
     float *acc;
     int64_t acc_stride, acc_pitch;
     int add_acc;

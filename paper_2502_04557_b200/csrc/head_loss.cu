@@ -6,11 +6,12 @@
 //   D_iv = g_i (exp(l_iv - lse_i) - [v = t_i]),  dH = D W,  dW = D^T H
 //   log p(x_i) = l_{i,x_i} - lse_i
 // The products run on CTA pairs (head_gemm.cu).  Forward: one product whose epilogue leaves (max,
-// sum of exp) per row and 128 columns, then a warp per row that merges them and forms the target's
+// sum of exp) per row and 128 columns, then a CTA per row that merges them and forms the target's
 // logit as a dot product of its own - N rows of W, nothing beside the product, and exact to a few
 // units of fp32 however the product's accumulator rounds.  Backward: the vocabulary goes by in
 // pieces; a piece's D is kept in the workspace (bf16, or three bf16 parts for fp32), and one launch
-// then adds D W to dH and writes the piece's rows of dW.
+// then adds D W to dH and writes the piece's rows of dW.  Small fp32 problems and a handful of tokens take
+// kernels of their own on the CUDA cores (head_small.cu, head_stream.cu; see small_head() and stream_head()).
 //
 // Rounding D to bf16 costs a relative 2^-9 per element, the size of the rounding of the bf16
 // result itself; sums over D are held in fp32 throughout.

@@ -71,6 +71,18 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, i
         : "memory");
 }
 
+// box of shared memory into a 2-D tensor (what lies outside is left out), as one group of this thread's copies
+__device__ __forceinline__ void store_box(const CUtensorMap *map, int c0, int c1, const void *src)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];\n\t"
+        "cp.async.bulk.commit_group;" ::"l"(map), "r"(c0), "r"(c1), "r"(smem_addr(src))
+        : "memory");
+}
+__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }      // the source is free
+__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void fence_stores() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }      // behind writes to the source
+
 // Shared-memory matrix descriptor of a tile made of 64 x 64 boxes (128-byte swizzle, 8 KB each).
 //   along K  (K contiguous): rows of 128 bytes, 8-row groups 1024 bytes apart
 //   across K (M or N contiguous): a box holds 64 of M or N by 64 of K; 8-deep groups of K are
