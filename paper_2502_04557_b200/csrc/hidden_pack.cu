@@ -7,7 +7,8 @@
 // 2^e (a whole step above 127.5, where q is clamped): between 1/128 and 1/256 of the block's
 // largest magnitude.  Scales are powers of two so that nothing but q is rounded: 2^-e x is exact, and
 // q 2^e is a bf16 number (7 bits), so states unpacked to bf16 are what the packed ones stand for,
-// bit for bit.  Both directions are bound by memory: es + 1 + 1/32 bytes per element.
+// bit for bit.  Both directions are bound by memory: es + 1 + 1/32 bytes per element (measured, 2^18 x 2048 bf16: packing
+// 287 us, 5.7 TB/s; unpacking 243 us, 6.7 TB/s; 2^17 x 2048 fp32 packing 202 us, 6.7 TB/s; 4096 x 2048 bf16 6.3 and 4.7 us).
 #include "common.cuh"
 #include "host_util.h"
 #include "launch.h"
