@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) stream_grad_kernel(const Stre
                 }
                 if (dw) {
                     T *p = dw + (base + r) * prm.d + c0;
-                    T y[N];
+                    __align__(16) T y[N];
 #pragma unroll
                     for (int e = 0; e < N; ++e) y[e] = (T)o[e];
                     if (prm.vec) {
