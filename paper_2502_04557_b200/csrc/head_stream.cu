@@ -31,14 +31,20 @@ template <typename T>
 __device__ __forceinline__ void stage_hidden(const StreamParams &prm, int nt, float *h, bool masked)
 {
     const T *src = static_cast<const T *>(prm.hidden);
-    for (int i = threadIdx.x; i < nt * prm.pitch; i += blockDim.x) {
-        const int n = i / prm.pitch, c = i - n * prm.pitch;
-        bool there = n < prm.N && c < prm.d;
-        if (there && masked) {
-            const int t = prm.targets[n];
-            there = t >= 0 && t < prm.V;
+    const int total = nt * prm.pitch;
+    for (int i0 = threadIdx.x; i0 < total; i0 += 8 * blockDim.x) {
+        float x[8];
+        int tok[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {              // addresses that exist, all loads at once
+            const int i = min(i0 + u * (int)blockDim.x, total - 1), n = i / prm.pitch, c = i - n * prm.pitch, m = min(n, prm.N - 1);
+            x[u] = (float)src[(int64_t)m * prm.d + min(c, prm.d - 1)];
+            tok[u] = masked ? prm.targets[m] : 0;
+            if (n >= prm.N || c >= prm.d) tok[u] = -1;
         }
-        h[i] = there ? (float)src[(int64_t)n * prm.d + c] : 0.f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (i0 + u * (int)blockDim.x < total) h[i0 + u * (int)blockDim.x] = tok[u] >= 0 && tok[u] < prm.V ? x[u] : 0.f;
     }
 }
 
@@ -78,8 +84,10 @@ __device__ __forceinline__ float scatter_sum(float (&v)[NV], int lane)
 }
 __host__ __device__ constexpr int log2i(int x) { return x <= 1 ? 0 : 1 + log2i(x / 2); }
 
-// logits of R rows of W (row0, row0 + 1, ...) and NT tokens; the lane's is the one that scatter_sum gives it
-template <typename T, int NT, int R>
+// logits of R rows of W (row0, row0 + 1, ...) and NT tokens; the lane's is the one that scatter_sum gives it.  U vectors
+// of every row are asked for at once, from addresses that are always inside the row: what does not exist is dropped
+// behind the loads (loads that depend on a condition would wait for one another).
+template <typename T, int NT, int R, int U>
 __device__ __forceinline__ float row_logits(const StreamParams &prm, const float *h, int64_t row0, int lane)
 {
     constexpr int N = Vec<T>::N;
@@ -87,14 +95,11 @@ __device__ __forceinline__ float row_logits(const StreamParams &prm, const float
     uint64_t acc[R * NT];
 #pragma unroll
     for (int i = 0; i < R * NT; ++i) acc[i] = pack2(0.f, 0.f);
-#pragma unroll 2
-    for (int c = lane * N; c < prm.pitch; c += 32 * N) {
-        uint4 x[R];
+    const T *row[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) x[r] = load_vec(w + min(row0 + r, (int64_t)prm.V - 1) * prm.d, c, prm.d, prm.vec);
-        float f[R][N];
-#pragma unroll
-        for (int r = 0; r < R; ++r) Vec<T>::unpack(x[r], f[r]);
+    for (int r = 0; r < R; ++r) row[r] = w + min(row0 + r, (int64_t)prm.V - 1) * prm.d;
+    const int last = (prm.d - 1) / N * N;
+    auto add = [&](const float (&f)[R][N], int c) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -105,6 +110,39 @@ __device__ __forceinline__ float row_logits(const StreamParams &prm, const float
                 for (int r = 0; r < R; ++r)
                     acc[r * NT + n] = fma2(pack2(f[r][e + 2], f[r][e + 3]), y1, fma2(pack2(f[r][e], f[r][e + 1]), y0, acc[r * NT + n]));
             }
+        }
+    };
+    if (prm.vec) {
+        for (int c = lane * N; c < prm.d; c += U * 32 * N) {
+            uint4 x[U][R];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int r = 0; r < R; ++r) x[u][r] = __ldg(reinterpret_cast<const uint4 *>(row[r] + min(c + u * 32 * N, last)));
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (c + u * 32 * N > last)
+#pragma unroll
+                    for (int r = 0; r < R; ++r) x[u][r] = make_uint4(0u, 0u, 0u, 0u);
+                float f[R][N];
+#pragma unroll
+                for (int r = 0; r < R; ++r) Vec<T>::unpack(x[u][r], f[r]);
+                add(f, min(c + u * 32 * N, last));
+            }
+        }
+    } else {
+        for (int c = lane * N; c < prm.d; c += 32 * N) {
+            float f[R][N];
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int e = 0; e < N; ++e) f[r][e] = (float)row[r][min(c + e, prm.d - 1)];
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (c + e >= prm.d) f[r][e] = 0.f;
+            add(f, c);
         }
     }
     float v[R * NT];
@@ -132,7 +170,7 @@ __global__ void __launch_bounds__(32 * kStatWarps) stream_stats_kernel(const Str
     const int idx = lane >> kShift, my_row = idx / NT;
     const int64_t stride = (int64_t)gridDim.x * kStatWarps * R;
     for (int64_t row0 = ((int64_t)blockIdx.x * kStatWarps + warp) * R; row0 < prm.V; row0 += stride) {
-        const float l = row_logits<T, NT, R>(prm, h, row0, lane);
+        const float l = row_logits<T, NT, R, NT <= 2 ? 4 : 2>(prm, h, row0, lane);
         if (row0 + my_row < prm.V) a = ms_merge(a, MS{l, 1.f});
     }
     // merge the four rows' slots of a token (the lanes that differ in the row bits), then the warps
@@ -189,27 +227,40 @@ __global__ void __launch_bounds__(kGradThreads, 1) stream_grad_kernel(const Stre
         }
     int buf = 0;
     for (int64_t base = (int64_t)blockIdx.x * kGradRows; base < prm.V; base += (int64_t)gridDim.x * kGradRows, buf ^= 1) {
+        // the next rows are asked for as far as L2 while these are worked on
+        const int64_t next = base + (int64_t)gridDim.x * kGradRows + threadIdx.x;
+        if (threadIdx.x < kGradRows && prm.vec && next < prm.V)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(w + next * prm.d), "r"((uint32_t)(prm.d * sizeof(T))) : "memory");
         const int64_t row = base + warp * R + my_row;
-        const float l = row_logits<T, NT, R>(prm, h, base + warp * R, lane);
+        const float l = row_logits<T, NT, R, NT <= 2 ? 4 : 2>(prm, h, base + warp * R, lane);
         if ((lane & ((1 << kShift) - 1)) == 0 && idx < R * NT)
             D[buf][warp * R + my_row][my_tok] = keep && row < prm.V ? g * expf(l - lse) - (row == tok ? g : 0.f) : 0.f;
         __syncthreads();          // D is there; the other buffer's readers are a barrier behind
         const int rows = (int)min((int64_t)kGradRows, prm.V - base);
-        if (mine) {
-#pragma unroll 4
-            for (int r = 0; r < rows; ++r) {
+        // Four rows of W at a time, all loads of them ahead of the stores (which might be to the same place for all the
+        // compiler knows)
+        for (int r0 = 0; mine && r0 < rows; r0 += 4) {
+            uint4 x[4];
+            if (prm.d_hidden) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = load_vec(w + (base + min(r0 + i, rows - 1)) * prm.d, c0, prm.d, prm.vec);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = r0 + i;
+                if (r >= rows) break;
                 float f[N];
-                if (prm.d_hidden) Vec<T>::unpack(load_vec(w + (base + r) * prm.d, c0, prm.d, prm.vec), f);
+                if (prm.d_hidden) Vec<T>::unpack(x[i], f);
                 float o[N];
 #pragma unroll
                 for (int e = 0; e < N; ++e) o[e] = 0.f;
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const float x = D[buf][r][n];
+                    const float y = D[buf][r][n];
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
-                        o[e] = fmaf(x, hr[n][e], o[e]);
-                        if (prm.d_hidden) acc[n][e] = fmaf(x, f[e], acc[n][e]);
+                        o[e] = fmaf(y, hr[n][e], o[e]);
+                        if (prm.d_hidden) acc[n][e] = fmaf(y, f[e], acc[n][e]);
                     }
                 }
                 if (dw) {
@@ -260,7 +311,8 @@ cudaError_t start_typed(bool grad, const StreamParams &prm, int ctas, cudaStream
     if (prm.N <= 1) return start_any<T, 1>(grad, prm, ctas, st);
     if (prm.N <= 2) return start_any<T, 2>(grad, prm, ctas, st);
     if (prm.N <= 4) return start_any<T, 4>(grad, prm, ctas, st);
-    return start_any<T, 8>(grad, prm, ctas, st);
+    if constexpr (sizeof(T) == 4) return start_any<T, 8>(grad, prm, ctas, st);
+    return cudaErrorInvalidValue;          // bf16: at most four
 }
 
 }  // namespace
