@@ -297,14 +297,15 @@ bool needs_pack(int d, int dt) { return dt == SPR_F32 || d % 8 != 0; }
 int parts(int dt) { return dt == SPR_F32 ? 3 : 1; }
 size_t packed_bytes(int64_t rows, int d, int dt) { return 2 * (size_t)rows * parts(dt) * (size_t)round_up(d, 64); }
 
-// A handful of tokens: one pass over W as it is (head_stream.cu).  fp32: up to eight tokens, whatever the size; bf16 heads
-// with rows that TMA cannot take: up to four; others: one.  Measured (us, one pass / tensor cores, d = 2048,
-// V = 32000): f32 N = 8 loss 99 / 293, gradient 259 / 887; bf16 N = 1 34 / 46 and 119 / 145, N = 4 46 / 39 and 159 / 135;
-// bf16 d = 1001, N = 4 40 / 55 and 155 / 187.  (us, one pass / tiles of head_small.cu): f32 4x256x1000 5.4 / 8.2 and
-// 10.2 / 16.8, 8x64x500 5.3 / 6.8 and 11.3 / 11.7, 8x1024x512 14 / 18 and 24 / 37, 1x768x1000 6.3 / 15 and 10 / 41.
+// A handful of tokens: one pass over W as it is (head_stream.cu).  fp32: up to eight tokens, whatever the size; bf16: up
+// to four, two for the gradient where TMA can take the rows.  Measured (us, one pass / tensor cores, loss and
+// gradient), d = 2048, V = 32000: f32 N = 8 82 / 293 and 218 / 887; bf16 N = 1 27 / 46 and 79 / 139, N = 2 29 / 44 and
+// 85 / 134, N = 4 37 / 40 and 121 / 129 (768 x 50257: N = 2 22 / 28 and 86 / 86, N = 4 28 / 28 and 110 / 87); bf16
+// d = 1001, N = 4 41 / 53 and 131 / 183.  One pass / tiles of head_small.cu: f32 4x256x1000 5.4 / 8.2 and 9 / 16.8,
+// 8x64x500 5.3 / 6.8 and 11 / 11.7, 8x1024x512 14 / 18 and 24 / 37, 1x768x1000 6.3 / 15 and 10 / 41.
 bool stream_head(bool grad, int64_t N, int d, int dt)
 {
-    const int most = dt == SPR_F32 ? kStreamTokens : d % 8 != 0 ? 4 : 1;
+    const int most = dt == SPR_F32 ? kStreamTokens : grad && d % 8 == 0 ? 2 : 4;
     return N <= most && stream_fits(grad, (int)N, d, dt == SPR_F32);
 }
 // More fp32 tokens go to the CUDA cores where that is less than 2^27 multiply-adds (head_small.cu: whole tiles of 32 x 32,

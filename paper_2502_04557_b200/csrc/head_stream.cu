@@ -9,9 +9,10 @@
 //              thread per 16 bytes of columns reads the rows again (out of L2), writes dW = D^T H for them and adds
 //              D W to its columns of dH, which it keeps in registers.  W is read from memory once, dW
 //              written once: the floor.  The CTAs' dH are added up in order by the kernel behind.
-// Measured (d = 2048, V = 32000): loss fp32 N = 1 61 us (4.3 TB/s), N = 8 104 us, bf16 N = 1 35 us; gradient fp32 N = 1 196 us,
-// N = 8 259 us, bf16 N = 1 120 us (memory takes in pure writes at 3.9 TB/s: 108 us for fp32, 54 us for bf16).  A small
-// head takes 4 to 7 us for the loss and 10 us for the gradient: launches.
+// Measured (d = 2048, V = 32000): loss fp32 N = 1 46 us (5.7 TB/s), N = 8 82 us, bf16 N = 1 27 us; gradient fp32 N = 1 141 us,
+// N = 8 218 us, bf16 N = 1 79 us (memory takes in pure writes at 3.9 TB/s: 67 us for fp32, 34 us for bf16, beside the reads).
+// With more tokens it is the products of every vector of W with all of them.  A small head takes 4 to 7 us for
+// the loss and 9 us for the gradient: launches.
 #include "head_stream.h"
 
 #include "common.cuh"

@@ -125,6 +125,15 @@ def test_small_fp32_heads(spr, N, d, V):
     check_grad(spr, h, w, t, gl, lse)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=IDS.get)
+@pytest.mark.parametrize("N,d,V", [(1, 2048, 32000), (2, 136, 20011), (4, 1001, 12007), (8, 264, 15013), (3, 100, 9999), (4, 4096, 10007)])
+def test_a_handful_of_tokens_of_a_large_head(spr, N, d, V, dtype):
+    """Every CTA goes round its rows of W more than once."""
+    h, w, t, gl = problem(N, d, V, dtype, seed=N + d + V)
+    _, lse = check_loss(spr, h, w, t)
+    check_grad(spr, h, w, t, gl, lse)
+
+
 @pytest.mark.parametrize("N,d,V,dtype", [(2048, 512, 30011, torch.bfloat16), (4096, 256, 128256, torch.bfloat16),
                                          (700, 264, 50257, torch.bfloat16), (1500, 136, 33000, torch.float32)],
                          ids=lambda v: str(v).replace("torch.", ""))
