@@ -444,3 +444,85 @@ def test_a_handful_of_tokens(spr, N, d, V, dtype):
         dh, dw = check_grad(spr, h, w, t, gl, lse)
         assert torch.equal(check_grad(spr, h, w, t, gl, lse, want_W=False)[0], dh)
         assert torch.equal(check_grad(spr, h, w, t, gl, lse, want_hidden=False)[1], dw)
+
+
+def framed(shape, dtype):
+    """A contiguous tensor of this shape in the middle of a buffer of sevens, 64 of them on either side."""
+    n = int(np.prod(shape))
+    buf = torch.full((n + 128,), 7.0, device="cuda").to(dtype)
+    return buf, buf[64:64 + n].view(shape)
+
+
+def untouched(buf):
+    return bool((buf[:64] == 7).all()) and bool((buf[-64:] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=IDS.get)
+@pytest.mark.parametrize("N,d,V", [(130, 72, 515), (257, 264, 1025), (33, 100, 700), (2, 72, 515), (300, 8, 9001), (129, 67, 300)])
+def test_nothing_is_written_beside_the_outputs(spr, N, d, V, dtype):
+    h, w, t, gl = problem(N, d, V, dtype, seed=N + V)
+    ws = workspace(spr, spr.OP_HEAD_LOSS, N, V, d, dtype)
+    (lb, loss), (zb, lse) = framed((N,), torch.float32), framed((N,), torch.float32)
+    spr.head_loss(h, w, t, ws, out=(loss, lse))
+    ws = workspace(spr, spr.OP_HEAD_LOSS_GRAD, N, V, d, dtype)
+    (hb, dh), (wb, dw) = framed((N, d), dtype), framed((V, d), dtype)
+    check_grad(spr, h, w, t, gl, lse, ws=ws, out=(dh, dw))
+    assert all(untouched(b) for b in (lb, zb, hb, wb))
+
+
+def test_two_calls_at_once(spr):
+    """Two streams, a workspace each: the results are those of the calls alone."""
+    a = problem(300, 264, 9001, torch.bfloat16, seed=1)
+    b = problem(67, 257, 1003, torch.float32, seed=2)
+    def both(h, w, t, gl, ws1, ws2):
+        loss, lse = spr.head_loss(h, w, t, ws1)
+        return (loss, lse) + tuple(spr.head_loss_grad(h, w, t, lse, gl, ws2))
+    def spaces(h, w):
+        return [workspace(spr, op, h.shape[0], w.shape[0], h.shape[1], h.dtype) for op in (spr.OP_HEAD_LOSS, spr.OP_HEAD_LOSS_GRAD)]
+    spaces_a, spaces_b = spaces(a[0], a[1]), spaces(b[0], b[1])
+    want = both(*a, *spaces_a), both(*b, *spaces_b)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for _ in range(5):
+        with torch.cuda.stream(s1):
+            x = both(*a, *spaces_a)
+        with torch.cuda.stream(s2):
+            y = both(*b, *spaces_b)
+        got.append((x, y))
+    torch.cuda.synchronize()
+    for x, y in got:
+        assert all(torch.equal(p, q) for p, q in zip(x, want[0])) and all(torch.equal(p, q) for p, q in zip(y, want[1]))
+
+
+def test_a_draft_head_fitted_labelled_and_its_verifier_fitted(spr):
+    """The operators one after the other, as they are used: a step on the draft's head along its gradient, labels from
+    the new head, states packed, a step of the verifier on them, each against float64 on what it was given."""
+    from oracle import training
+    N, d, V = 600, 128, 3001
+    h, w, t, gl = problem(N, d, V, torch.float32, seed=21, ignore=0.1)
+    loss, lse = check_loss(spr, h, w, t)
+    dh, dw = check_grad(spr, h, w, t, gl, lse)
+    new = (w - 0.5 * dw).to(torch.bfloat16)
+    hb, pw = h.to(torch.bfloat16), w.to(torch.bfloat16)
+    x = torch.randint(0, V, (N,), generator=torch.Generator().manual_seed(5), dtype=torch.int32).cuda()
+    ws = workspace(spr, spr.OP_VERIFIER_LABELS_HEAD, N, V, d, torch.bfloat16, h=d)
+    labels, ratio = spr.verifier_labels_head(hb, pw, hb, new, x, [1.0], ws)
+    assert ws.device_status() == 0
+    logp = [torch.log_softmax(hb.double() @ m.double().T, 1).gather(1, x.long()[:, None])[:, 0] for m in (pw, new)]
+    want = torch.exp(logp[1] - logp[0])
+    off = 2 * (logit_bound(hb, pw).amax(1) + logit_bound(hb, new).amax(1)) + 64 * U * (1 + logp[0].abs() + logp[1].abs())
+    assert bool(((ratio.double() - want).abs() <= want * (torch.exp(off) - 1) + U).all())
+    clear = (want - 1).abs() > want * (torch.exp(off) - 1)
+    assert torch.equal(labels[0][clear].bool(), (want <= 1)[clear])
+    packed = spr.hidden_pack8(hb)
+    S = spr.hidden_unpack8(packed, d, dtype=torch.float32)
+    st = [torch.zeros(d + 1, device="cuda") for _ in range(3)]
+    ws = spr.Workspace(spr.workspace_bytes(spr.OP_VERIFIER_TRAIN8, 0, 0, 0, d, 0, spr.BF16))
+    got = spr.verifier_train_step8(packed, d, labels[0].contiguous(), *st, 1, 0.01, ws)
+    zero = np.zeros(d + 1)
+    ref, theta, _, _ = training.verifier_train_step(S.cpu().double().numpy(), labels[0].cpu().numpy(), zero, zero, zero, 1, 0.01)
+    # all logits are zero: the loss is ln 2 to a rounding; a first step of Adam is lr g / (|g| + eps), and the bound of
+    # tests/test_gpu_pack8.py for one step
+    assert float(got) == pytest.approx(ref, rel=1e-6)
+    assert np.abs(st[0].cpu().double().numpy() - theta).max() <= 1e-3 * 0.01
