@@ -299,3 +299,36 @@ def test_states_labelled_packed_fitted_and_used(spr):
 
 def to_float(t):
     return t.cpu().double().numpy()
+
+
+def framed(shape, dtype, fill=7):
+    n = int(np.prod(shape))
+    buf = torch.full((n + 128,), fill, device="cuda", dtype=dtype)
+    return buf, buf[64:64 + n].view(shape)
+
+
+def untouched(buf, fill=7):
+    return bool((buf[:64] == fill).all()) and bool((buf[-64:] == fill).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("N,d", [(1, 1), (3, 33), (5, 255), (7, 768), (130, 1000), (3, 2048)])
+def test_nothing_is_written_beside_packed_and_unpacked_states(spr, N, d, dtype):
+    x = values(N, d, dtype, seed=d).cuda()
+    pb, p = framed((N, spr.pack8_pitch(d)), torch.uint8)
+    spr.hidden_pack8(x, out=p)
+    assert np.array_equal(p.cpu().numpy(), spr.hidden_pack8(x).cpu().numpy()) and untouched(pb)
+    ub, u = framed((N, d), dtype)
+    spr.hidden_unpack8(p, d, dtype=dtype, out=u)
+    assert untouched(ub)
+
+
+@pytest.mark.parametrize("N,d", [(1, 16), (33, 528), (500, 1040), (40, 2064)])
+def test_nothing_is_written_beside_the_parameters(spr, N, d):
+    S, y = teacher_problem(N, d, torch.bfloat16, seed=N)
+    packed, ws = spr.hidden_pack8(S.cuda()), step_ws(spr, d)
+    frames = [framed((d + 1,), torch.float32) for _ in range(3)] + [framed((1,), torch.float32)]
+    for _, t in frames:
+        t.zero_()
+    spr.verifier_train_step8(packed, d, y.cuda(), frames[0][1], frames[1][1], frames[2][1], 1, 0.01, ws, loss=frames[3][1])
+    assert all(untouched(b) for b, _ in frames) and float(frames[3][1]) == pytest.approx(np.log(2.0), rel=1e-6)
