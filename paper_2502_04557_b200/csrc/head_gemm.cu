@@ -153,20 +153,19 @@ __device__ __forceinline__ Stats row_stats(float (&x)[4][32], int v)
     return a;
 }
 
-// A warp's block of 32 rows x 32 columns, a row per thread, turned so that eight lanes hold a row:
-// v[i] gets columns 4 (lane % 8) .. + 3 of row 4 i + lane / 8.
-__device__ __forceinline__ void by_rows(const float (&x)[32], float4 (&v)[8], float4 *stage, int lane)
+// A warp's block of 32 rows x 32 columns, a row per thread, into its buffer, to be read so that eight lanes hold a row:
+// staged(i) is columns 4 (lane % 8) .. + 3 of row 4 i + lane / 8.
+__device__ __forceinline__ void to_stage(const float (&x)[32], float4 *stage, int lane)
 {
 #pragma unroll
     for (int c = 0; c < 8; ++c)
         stage[lane * 8 + (c ^ (lane & 7))] = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
     __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = 4 * i + (lane >> 3);
-        v[i] = stage[r * 8 + ((lane & 7) ^ (r & 7))];
-    }
-    __syncwarp();
+}
+__device__ __forceinline__ float4 &staged(float4 *stage, int i, int lane)
+{
+    const int r = 4 * i + (lane >> 3);
+    return stage[r * 8 + ((lane & 7) ^ (r & 7))];
 }
 // four elements of a row
 __device__ __forceinline__ void store4(float *p, float4 x) { *reinterpret_cast<float4 *>(p) = x; }
@@ -174,22 +173,15 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 x)
 {
     *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
 }
-// The same block where rows start anywhere or columns are missing: out[r * pitch] of the first `rows` rows, a lane per
-// column (a store instruction is then one run of a row), lanes below `width`.  v is as by_rows leaves it.
+// The staged block where rows start anywhere or columns are missing: out[r * pitch] of the first `rows` rows, a lane per
+// column (a store instruction is then one run of a row), lanes below `width`.
 template <typename T>
-__device__ __forceinline__ void store_any(T *out, int64_t pitch, const float4 (&v)[8], float4 *stage, int lane, int rows, int width)
+__device__ __forceinline__ void store_any(T *out, int64_t pitch, const float4 *stage, int lane, int rows, int width)
 {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = 4 * i + (lane >> 3);
-        stage[r * 8 + ((lane & 7) ^ (r & 7))] = v[i];
-    }
-    __syncwarp();
     const float *s = reinterpret_cast<const float *>(stage);
-#pragma unroll 8
+#pragma unroll 4
     for (int r = 0; r < 32; ++r, out += pitch)
         if (r < rows && lane < width) out[0] = (T)s[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)];
-    __syncwarp();
 }
 __device__ __forceinline__ float minus_bf16(float x) { return x - __bfloat162float(__float2bfloat16(x)); }
 
@@ -431,7 +423,6 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                             if (hot == 32 * q + e) y[e] -= g;
                     }
                     __syncwarp();
-                    float4 v[8];
                     if constexpr (sizeof(T) == 2) {
                         // 64 columns of bf16 are a line of 128 bytes: two groups go out as one
 #pragma unroll
@@ -439,20 +430,20 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                         if (q & 1) put_box(q >> 1, line, c0, row - lane, seg);
                         continue;
                     }
-                    by_rows(y, v, stage, lane);
+                    to_stage(y, stage, lane);
                     __nv_bfloat16 *o = dst + 32 * q;
-#pragma unroll
+#pragma unroll 2
                     for (int i = 0; i < 8; ++i, o += step) {
                         if (4 * i < rows) {
-                            store4(o, v[i]);
-                            if (sizeof(T) == 4) {
-                                v[i] = make_float4(minus_bf16(v[i].x), minus_bf16(v[i].y), minus_bf16(v[i].z), minus_bf16(v[i].w));
-                                store4(o + seg, v[i]);
-                                v[i] = make_float4(minus_bf16(v[i].x), minus_bf16(v[i].y), minus_bf16(v[i].z), minus_bf16(v[i].w));
-                                store4(o + 2 * (int64_t)seg, v[i]);
-                            }
+                            float4 v = staged(stage, i, lane);
+                            store4(o, v);
+                            v = make_float4(minus_bf16(v.x), minus_bf16(v.y), minus_bf16(v.z), minus_bf16(v.w));
+                            store4(o + seg, v);
+                            v = make_float4(minus_bf16(v.x), minus_bf16(v.y), minus_bf16(v.z), minus_bf16(v.w));
+                            store4(o + 2 * (int64_t)seg, v);
                         }
                     }
+                    __syncwarp();
                 }
             } else {
                 // this lane's part of a block: columns 4 (lane % 8) .. + 3 of rows lane / 8, + 4, ...
@@ -481,32 +472,34 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     if (32 * q >= width) break;
-                    float4 v[8];
-                    by_rows(columns(q), v, stage, lane);
+                    to_stage(columns(q), stage, lane);
                     if (add) {                   // acc's pitch covers whole groups of 32
                         const float *p = a + 32 * q;
-                        float4 y[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i, p += acc_step) y[i] = 4 * i < rows ? *reinterpret_cast<const float4 *>(p) : v[i];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) v[i] = make_float4(v[i].x + y[i].x, v[i].y + y[i].y, v[i].z + y[i].z, v[i].w + y[i].w);
+#pragma unroll 4
+                        for (int i = 0; i < 8; ++i, p += acc_step) {
+                            if (4 * i < rows) {
+                                const float4 y = *reinterpret_cast<const float4 *>(p);
+                                float4 &v = staged(stage, i, lane);
+                                v = make_float4(v.x + y.x, v.y + y.y, v.z + y.z, v.w + y.w);
+                            }
+                        }
+                        __syncwarp();
                     }
                     if (!to_out) {
                         float *p = a + 32 * q;
-#pragma unroll
+#pragma unroll 4
                         for (int i = 0; i < 8; ++i, p += acc_step)
-                            if (4 * i < rows) store4(p, v[i]);
-                    } else {
+                            if (4 * i < rows) store4(p, staged(stage, i, lane));
+                    } else if (vec && width - 32 * q >= 32) {
                         T *p = o + 32 * q;
-                        if (vec && width - 32 * q >= 32) {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i, p += out_step)
-                                if (4 * i < rows) store4(p, v[i]);
-                        } else {
-                            store_any(static_cast<T *>(j.out) + (row - lane) * j.out_pitch + c0 + 32 * q + lane, j.out_pitch, v, stage, lane,
-                                      rows + (lane >> 3), width - 32 * q);
-                        }
+#pragma unroll 4
+                        for (int i = 0; i < 8; ++i, p += out_step)
+                            if (4 * i < rows) store4(p, staged(stage, i, lane));
+                    } else {
+                        store_any(static_cast<T *>(j.out) + (row - lane) * j.out_pitch + c0 + 32 * q + lane, j.out_pitch, stage, lane,
+                                  rows + (lane >> 3), width - 32 * q);
                     }
+                    __syncwarp();
                 }
             }
             if constexpr (!kChunked) {
