@@ -308,15 +308,17 @@ bool stream_head(bool grad, int64_t N, int d, int dt)
     const int most = dt == SPR_F32 ? kStreamTokens : grad && d % 8 == 0 ? 2 : 4;
     return N <= most && stream_fits(grad, (int)N, d, dt == SPR_F32);
 }
-// More fp32 tokens go to the CUDA cores where that is less than 2^27 multiply-adds (head_small.cu: whole tiles of 32 x 32,
-// each of which costs what 200 entries of its contraction do); above that the six bf16 products on the tensor cores are
-// faster.  Measured (us, CUDA cores / tensor cores): loss 64x256x4000 15 / 20, 128x512x1000 13 / 28, 9x1024x2000 19 / 46,
-// 64x512x4000 29 / 29, 256x128x2000 23 / 15; gradient 67x257x1003 24.5 / 69, 64x256x4000 60 / 73, 256x128x2000 47 / 56,
-// 32x128x16000 95 / 79, 256x128x4000 103 / 71.  (bf16: 16x256x4000 11 / 9 and worse from there.)
+// More fp32 tokens go to the CUDA cores where that is less than 2^27 multiply-adds, 3/4 of it for the gradient
+// (head_small.cu: whole tiles of 32 x 32, each of which costs what 200 entries of its contraction do); above that the six
+// bf16 products on the tensor cores are faster.  Measured (us, CUDA cores / tensor cores), below: loss 67x257x1003
+// 10 / 21.5, 64x256x4000 15 / 19.5, 128x512x1000 13 / 28, 9x1024x2000 19 / 46, 300x64x1000 16 / 13; gradient 67x257x1003
+// 24.5 / 56, 128x512x1000 44 / 61, 200x100x1000 23 / 46, 9x1024x2000 88 / 85.  Above: loss 64x512x4000 29 / 29, 256x128x2000
+// 23 / 15; gradient 64x256x4000 60 / 58, 9x256x8000 83 / 59, 256x128x4000 103 / 57.  (bf16: 16x256x4000 11 / 9 and
+// worse from there.)
 bool small_head(bool grad, int64_t N, int d, int64_t V, int dt)
 {
     return dt == SPR_F32 && !stream_head(grad, N, d, dt) &&
-           (double)round_up(N, kSmallTile) * (double)round_up(V, kSmallTile) * (d + 200.0) <= (double)(1 << 27);
+           (double)round_up(N, kSmallTile) * (double)round_up(V, kSmallTile) * (d + 200.0) <= (grad ? 0.75 : 1.0) * (1 << 27);
 }
 // dH's contraction over the vocabulary there: 256 of it per CTA
 int small_splits(int V) { return (int)(ceil_div(V, 256) < 64 ? ceil_div(V, 256) : 64); }
