@@ -335,7 +335,8 @@ int head_loss(const void *hidden, const void *W, const int32_t *targets, int N, 
  *   D_iv = grad_loss[i] * (exp(l_iv - lse[i]) - [v = targets[i]]),  0 where targets[i] < 0:
  *   d_hidden [N,d] dt = D W,   d_W [V,d] dt = D^T hidden   (either may be NULL, not both)
  * The logits are formed again, a piece of the vocabulary at a time; a piece's D is held in the
- * workspace, rounded to bf16 (bf16 operands) or kept to fp32 (three bf16 parts); all sums are fp32.
+ * workspace, rounded to bf16 (bf16 operands; in two parts up to 128 tokens) or kept to fp32 (three bf16 parts);
+ * all sums are fp32.
  * Rows without a target have no part in d_W whatever they hold, and a zero row in d_hidden.
  * All-padded batches and N = 0 give zeros.  hidden, W, d_hidden, d_W are 16-byte aligned; outputs
  * must not overlap inputs.  Device-detected: targets[i] >= V is treated as padding,

@@ -108,9 +108,9 @@ __device__ __forceinline__ Item get_item(const PairParams &prm, int pair, int pa
 }
 __device__ __forceinline__ int item_blocks(const PairJob &j, int split) { return min(j.kb_per, j.kb - split * j.kb_per); }
 
-// parts of A and B in product p of 6: (0,2) (2,0) (1,1) (0,1) (1,0) (0,0)
-__device__ __forceinline__ int part_a(int nprod, int p) { return nprod == 1 ? 0 : (0x021010 >> (4 * (5 - p))) & 15; }
-__device__ __forceinline__ int part_b(int nprod, int p) { return nprod == 1 ? 0 : (0x201100 >> (4 * (5 - p))) & 15; }
+// parts of A and B in product p of 6: (0,2) (2,0) (1,1) (0,1) (1,0) (0,0); of 2: (1,0) (0,0)
+__device__ __forceinline__ int part_a(int nprod, int p) { return nprod == 6 ? (0x021010 >> (4 * (5 - p))) & 15 : nprod - 1 - p; }
+__device__ __forceinline__ int part_b(int nprod, int p) { return nprod == 6 ? (0x201100 >> (4 * (5 - p))) & 15 : 0; }
 
 // ---------------------------------------------------------------- epilogues (one thread = one row)
 struct Stats {
@@ -407,7 +407,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                 const int64_t step = 4 * j.dl_pitch;
                 const int seg = j.dl_seg;
                 __nv_bfloat16 *dst = j.dlogits + (row - lane + (lane >> 3)) * j.dl_pitch + c0 + (sizeof(T) == 2 ? 8 : 4) * (lane & 7);
-                float line[32];
+                float line[32], rest[32];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     if (32 * q >= stored) break;
@@ -426,8 +426,14 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                     if constexpr (sizeof(T) == 2) {
                         // 64 columns of bf16 are a line of 128 bytes: two groups go out as one
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) line[16 * (q & 1) + e / 2] = __uint_as_float(pack_bf16(y[e], y[e + 1]));
-                        if (q & 1) put_box(q >> 1, line, c0, row - lane, seg);
+                        for (int e = 0; e < 32; e += 2) {
+                            line[16 * (q & 1) + e / 2] = __uint_as_float(pack_bf16(y[e], y[e + 1]));
+                            rest[16 * (q & 1) + e / 2] = __uint_as_float(pack_bf16(minus_bf16(y[e]), minus_bf16(y[e + 1])));
+                        }
+                        if (q & 1) {
+                            put_box(q >> 1, line, c0, row - lane, seg);
+                            if (j.dl_parts == 2) put_box(q >> 1, rest, seg + c0, row - lane, 2 * (int64_t)seg);
+                        }
                         continue;
                     }
                     to_stage(y, stage, lane);
@@ -610,7 +616,7 @@ cudaError_t launch_pair(PairEpilogue epi, bool f32, PairParams &prm, int njobs, 
         // bf16 results go out as boxes where nothing is added to them and their rows are whole 16-byte vectors
         PairJob &j = prm.job[i];
         PairOperand out = {nullptr, j.rows, 0, 0};
-        if (!f32 && epi == PAIR_DLOGITS) out = PairOperand{j.dlogits, j.rows, j.dl_seg, j.dl_pitch};
+        if (!f32 && epi == PAIR_DLOGITS) out = PairOperand{j.dlogits, j.rows, (int64_t)j.dl_parts * j.dl_seg, j.dl_pitch};
         if (!f32 && epi == PAIR_OUT && !j.add_acc && j.out_pitch % 8 == 0) out = PairOperand{j.out, j.rows, j.cols, j.out_pitch};
         j.boxes = out.base != nullptr;
         maps[4 + i] = maps[0];

@@ -15,7 +15,7 @@ constexpr int kMaxPairs = 128;       // CTA pairs of a launch (74 on a B200)
 // What happens to a finished accumulator tile.
 enum PairEpilogue {
     PAIR_STATS = 0,   // (max, sum of exp) of each row over the tile's columns
-    PAIR_DLOGITS,     // softmax gradient of each logit, rounded to bf16 (three parts for fp32)
+    PAIR_DLOGITS,     // softmax gradient of each logit in bf16 parts (dl_parts; three for fp32)
     PAIR_OUT          // the product itself, added to what is there or stored in the caller's type
 };
 
@@ -27,7 +27,7 @@ struct PairJob {
     int tiles_m, tiles_n;         // tiles of 256 x 256
     int splits;                   // ranges of the contraction, each with a result of its own
     int kb, kb_per;               // blocks of the contraction; blocks per split
-    int nprod;                    // 1, or 6
+    int nprod;                    // products of parts: 1; 2 (A in two parts); 6 (A and B in three)
     int kc;                       // blocks that one accumulator takes before registers add it up
     int a_across, b_across;
     int a_seg, b_seg;
@@ -38,6 +38,7 @@ struct PairJob {
     // PAIR_DLOGITS: dlogits[row * dl_pitch + part * dl_seg + column], columns v0 .. v0 + cols of the vocabulary
     __nv_bfloat16 *dlogits;
     int64_t dl_pitch;
+    int dl_parts;                 // bf16 operands: parts that D is kept in, 1 or 2
     int dl_seg, v0, V;
     const float *lse, *grad_loss;
     const int32_t *targets;

@@ -9,12 +9,11 @@
 // sum of exp) per row and 128 columns, then a CTA per row that merges them and forms the target's
 // logit as a dot product of its own - N rows of W, nothing beside the product, and exact to a few
 // units of fp32 however the product's accumulator rounds.  Backward: the vocabulary goes by in
-// pieces; a piece's D is kept in the workspace (bf16, or three bf16 parts for fp32), and one launch
+// pieces; a piece's D is kept in the workspace (one or two bf16 parts, three for fp32), and one launch
 // then adds D W to dH and writes the piece's rows of dW.  Small fp32 problems and a handful of tokens take
 // kernels of their own on the CUDA cores (head_small.cu, head_stream.cu; see small_head() and stream_head()).
 //
-// Rounding D to bf16 costs a relative 2^-9 per element, the size of the rounding of the bf16
-// result itself; sums over D are held in fp32 throughout.
+// D is kept in bf16, in two parts for few tokens (see d_parts()); sums over D are held in fp32 throughout.
 #include <string.h>
 
 #include "common.cuh"
@@ -295,6 +294,13 @@ __global__ void __launch_bounds__(256) head_sum_kernel(const float *acc, int sli
 // ---------------------------------------------------------------- workspace
 bool needs_pack(int d, int dt) { return dt == SPR_F32 || d % 8 != 0; }
 int parts(int dt) { return dt == SPR_F32 ? 3 : 1; }
+// Parts that D is kept in.  Rounded to bf16 it brings the error of a gradient from that of rounding the result,
+// 0.0017, to 0.0024 where there are many tokens.  With few of them the rounding of the targets' entries does not average
+// out (measured up to 0.0026 of 9 or 128 tokens, against 0.0017 with two parts), and a second part of the contraction
+// is beside sweeps over W and dW (64x768x50257 86 -> 104 us, 128x4096x32000 222 -> 280 us; 256x768x50257 would take 117
+// for 88).
+constexpr int kTwoPartTokens = 128;
+int d_parts(int64_t N, int dt) { return dt == SPR_F32 ? 3 : N <= kTwoPartTokens ? 2 : 1; }
 size_t packed_bytes(int64_t rows, int d, int dt) { return 2 * (size_t)rows * parts(dt) * (size_t)round_up(d, 64); }
 
 // A handful of tokens: one pass over W as it is (head_stream.cu).  fp32: up to eight tokens, whatever the size; bf16: up
@@ -356,7 +362,7 @@ struct Pieces {
 Pieces pieces(int64_t N, int d, int V, int dt)
 {
     Pieces p;
-    int64_t most = (int64_t)(kPieceBytes / (2 * (size_t)parts(dt) * (size_t)N)) / kPairTile * kPairTile;
+    int64_t most = (int64_t)(kPieceBytes / (2 * (size_t)d_parts(N, dt) * (size_t)N)) / kPairTile * kPairTile;
     if (most < 8192) most = 8192;
     p.count = (int)ceil_div(V, most);
     p.width = (int)round_up(ceil_div(V, p.count), kPairTile);
@@ -399,7 +405,7 @@ HeadGradWs head_grad_layout(Carver &c, int64_t N, int d, int V, int dt)
     w.tickets = 0;
     w.hidden = c.take_data(packed_bytes(N, d, dt));
     w.W = c.take_data(needs_pack(d, dt) ? packed_bytes(V, d, dt) : 0);
-    w.dlogits = c.take_data(2 * (size_t)N * parts(dt) * (size_t)p.width);
+    w.dlogits = c.take_data(2 * (size_t)N * d_parts(N, dt) * (size_t)p.width);
     w.acc = c.take_data(p.count * p.splits > 1 ? 4 * (size_t)p.splits * (size_t)N * (size_t)round_up(d, 64) : 0);
     return w;
 }
@@ -704,7 +710,8 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
         wv = packed_operand(at<char>(ws, lay.W), V, d, dt);
     }
     const PairOperand hv = packed_operand(hp, N, d, dt);
-    const PairOperand dv = {at<char>(ws, lay.dlogits), N, (int64_t)parts(dt) * pc.width, (int64_t)parts(dt) * pc.width};
+    const int dparts = d_parts(N, dt);
+    const PairOperand dv = {at<char>(ws, lay.dlogits), N, (int64_t)dparts * pc.width, (int64_t)dparts * pc.width};
     for (int i = 0; i < pc.count && e == cudaSuccess; ++i) {
         const int v0 = i * pc.width, width = V - v0 < pc.width ? V - v0 : pc.width;
         PairOperand wp = wv;      // the piece's rows of W
@@ -722,6 +729,7 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
         j.cols = width;
         j.dlogits = at<__nv_bfloat16>(ws, lay.dlogits);
         j.dl_pitch = dv.pitch;
+        j.dl_parts = dparts;
         j.dl_seg = pc.width;
         j.v0 = v0;
         j.V = V;
@@ -738,6 +746,7 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
         if (d_hidden) {           // dH [N, d] += D [N, width] W [width, d]
             PairJob &h = prm.job[jobs];
             contraction(h, width, dt);
+            if (dparts == 2) h.nprod = 2;
             h.kb_per = pc.kb_per;
             h.splits = (int)ceil_div(h.kb, h.kb_per);
             h.tiles_m = (int)ceil_div(N, kPairTile);
@@ -764,6 +773,7 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
         if (d_W) {                // dW [width, d] = D^T [width, N] H [N, d]
             PairJob &w = prm.job[jobs];
             contraction(w, N, dt);
+            if (dparts == 2) w.nprod = 2;
             w.tiles_m = (int)ceil_div(width, kPairTile);
             w.tiles_n = (int)ceil_div(d, kPairTile);
             w.a_across = w.b_across = 1;
