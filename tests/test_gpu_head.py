@@ -73,7 +73,7 @@ def check_loss(spr, h, w, t, ws=None):
     return loss, lse
 
 
-def check_grad(spr, h, w, t, gl, lse, ws=None, **kw):
+def check_grad(spr, h, w, t, gl, lse, ws=None, d_rounding=2.0 ** -8, **kw):
     N, d = h.shape
     V = w.shape[0]
     ws = ws or workspace(spr, spr.OP_HEAD_LOSS_GRAD, N, V, d, h.dtype)
@@ -90,7 +90,7 @@ def check_grad(spr, h, w, t, gl, lse, ws=None, **kw):
     # a probability below the smallest normal number, 2^-126, counts as zero (and products of g with one as
     # small): off by less than (1 + g) 2^-126, which is all there is where the true value is of that size
     dD += torch.where(keep, (1 + g.abs()) * 2.0 ** -126, 0.0)
-    dD += (2.0 ** -8 if h.dtype == torch.bfloat16 else 2.0 ** -23) * D.abs()
+    dD += (d_rounding if h.dtype == torch.bfloat16 else 2.0 ** -23) * D.abs()
     for got, X, off, k in ((dh, W, dD, V), (dw, H, dD.T, N)):
         if got is None:
             continue
@@ -444,6 +444,15 @@ def test_a_handful_of_tokens(spr, N, d, V, dtype):
         dh, dw = check_grad(spr, h, w, t, gl, lse)
         assert torch.equal(check_grad(spr, h, w, t, gl, lse, want_W=False)[0], dh)
         assert torch.equal(check_grad(spr, h, w, t, gl, lse, want_hidden=False)[1], dw)
+
+
+@pytest.mark.parametrize("N,d,V", [(3, 768, 4001), (9, 256, 5000), (64, 768, 3001), (128, 264, 9001), (100, 1001, 700), (128, 72, 128256)])
+def test_few_tokens_keep_their_gradient_of_the_logits(spr, N, d, V):
+    """Up to 128 bf16 tokens D has two bf16 parts: rounding the first leaves at most 2^-8 of D, and rounding that
+    at most 2^-8 of it again: 2^-16 in all."""
+    h, w, t, gl = problem(N, d, V, torch.bfloat16, seed=V)
+    _, lse = check_loss(spr, h, w, t)
+    check_grad(spr, h, w, t, gl, lse, d_rounding=2.0 ** -16)
 
 
 def framed(shape, dtype):
