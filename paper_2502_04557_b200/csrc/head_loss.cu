@@ -303,17 +303,31 @@ constexpr int kTwoPartTokens = 128;
 int d_parts(int64_t N, int dt) { return dt == SPR_F32 ? 3 : N <= kTwoPartTokens ? 2 : 1; }
 size_t packed_bytes(int64_t rows, int d, int dt) { return 2 * (size_t)rows * parts(dt) * (size_t)round_up(d, 64); }
 
-// A handful of tokens: one pass over W as it is (head_stream.cu).  fp32: up to eight tokens, whatever the size; bf16: up
-// to four, two for the gradient where TMA can take the rows.  Measured (us, one pass / tensor cores, loss and
-// gradient), d = 2048, V = 32000: f32 N = 8 82 / 293 and 218 / 887; bf16 N = 1 27 / 46 and 79 / 139, N = 2 29 / 44 and
-// 85 / 134, N = 4 37 / 40 and 121 / 129 (768 x 50257: N = 2 22 / 28 and 86 / 86, N = 4 28 / 28 and 110 / 87); bf16
-// d = 1001, N = 4 41 / 53 and 131 / 183.  One pass / tiles of head_small.cu: f32 4x256x1000 5.4 / 8.2 and 9 / 16.8,
-// 8x64x500 5.3 / 6.8 and 11 / 11.7, 8x1024x512 14 / 18 and 24 / 37, 1x768x1000 6.3 / 15 and 10 / 41.
-bool stream_head(bool grad, int64_t N, int d, int dt)
+// Whether an fp32 problem is small enough for tiles of 32 x 32 on the CUDA cores (see small_head()).
+bool small_size(bool grad, int64_t N, int d, int64_t V)
 {
-    const int most = dt == SPR_F32 ? kStreamTokens : grad && d % 8 == 0 ? 2 : 4;
+    return (double)round_up(N, kSmallTile) * (double)round_up(V, kSmallTile) * (d + 200.0) <= (grad ? 0.75 : 1.0) * (1 << 27);
+}
+// A handful of tokens: passes over W as it is (head_stream.cu), one for every eight tokens.  fp32: up to eight tokens,
+// whatever the size, and up to 24 (16 for the gradient, which has a thread per four columns: from 512 columns) where W
+// has 2^24 elements; bf16: up to four, two for the gradient where TMA can take the rows.  Measured (us, passes / tensor cores, loss and gradient), d = 2048, V = 32000: f32
+// N = 8 82 / 293 and 218 / 730, N = 16 163 / 274 and 579 / 730, N = 24 243 / 275 and 878 / 734; d = 960, V = 116326: f32 N = 9
+// 190 / 518 and 844 / 1347, N = 32 480 / 465; d = 256, V = 70000: N = 16 54 / 91 and 384 / 240; d = 256, V = 20000: N = 24 40 / 40 and 187 / 100; bf16 N = 1 27 / 46 and
+// 79 / 139, N = 2 29 / 44 and 85 / 134, N = 4 37 / 40 and 121 / 129 (768 x 50257: N = 2 22 / 28 and 86 / 86, N = 4 28 / 28
+// and 110 / 87); bf16 d = 1001, N = 4 41 / 53 and 131 / 183.  One pass / tiles of head_small.cu: f32 4x256x1000 5.4 / 8.2
+// and 9 / 16.8, 8x64x500 5.3 / 6.8 and 11 / 11.7, 8x1024x512 14 / 18 and 24 / 37, 1x768x1000 6.3 / 15 and 10 / 41.
+constexpr int kMostLoss = 24, kMostGrad = 16;
+bool stream_head(bool grad, int64_t N, int d, int64_t V, int dt)
+{
+    int64_t most = grad && d % 8 == 0 ? 2 : 4;
+    if (dt == SPR_F32) {
+        const bool passes = V * d >= (1 << 24) && (!grad || d >= 512) && !small_size(grad, N, d, V);
+        most = !passes ? kStreamTokens : grad ? kMostGrad : kMostLoss;
+    }
     return N <= most && stream_fits(grad, (int)N, d, dt == SPR_F32);
 }
+// tokens of pass i
+int pass_tokens(int N, int i) { return N - i * kStreamTokens < kStreamTokens ? N - i * kStreamTokens : kStreamTokens; }
 // More fp32 tokens go to the CUDA cores where that is less than 2^27 multiply-adds, 3/4 of it for the gradient
 // (head_small.cu: whole tiles of 32 x 32, each of which costs what 200 entries of its contraction do); above that the six
 // bf16 products on the tensor cores are faster.  Measured (us, CUDA cores / tensor cores), below: loss 67x257x1003
@@ -323,8 +337,7 @@ bool stream_head(bool grad, int64_t N, int d, int dt)
 // worse from there.)
 bool small_head(bool grad, int64_t N, int d, int64_t V, int dt)
 {
-    return dt == SPR_F32 && !stream_head(grad, N, d, dt) &&
-           (double)round_up(N, kSmallTile) * (double)round_up(V, kSmallTile) * (d + 200.0) <= (grad ? 0.75 : 1.0) * (1 << 27);
+    return dt == SPR_F32 && !stream_head(grad, N, d, V, dt) && small_size(grad, N, d, V);
 }
 // dH's contraction over the vocabulary there: 256 of it per CTA
 int small_splits(int V) { return (int)(ceil_div(V, 256) < 64 ? ceil_div(V, 256) : 64); }
@@ -341,7 +354,7 @@ HeadLossWs head_loss_layout(Carver &c, int64_t N, int d, int V, int dt)
         w.part = c.take_data(8 * (size_t)N * (size_t)ceil_div(V, kSmallTile));
         return w;
     }
-    if (stream_head(false, N, d, dt)) {
+    if (stream_head(false, N, d, V, dt)) {
         w.hidden = w.W = 0;
         w.part = c.take_data(8 * (size_t)N * (size_t)stream_ctas(false, (int)N, d, V));
         return w;
@@ -396,9 +409,9 @@ HeadGradWs head_grad_layout(Carver &c, int64_t N, int d, int V, int dt)
         w.acc = c.take_data(4 * 1024 * tiles * (size_t)small_splits(V));
         return w;
     }
-    if (stream_head(true, N, d, dt)) {
+    if (stream_head(true, N, d, V, dt)) {
         w.hidden = w.W = w.tickets = w.dlogits = 0;
-        w.acc = c.take_data(4 * (size_t)stream_ctas(true, (int)N, d, V) * (size_t)N * (size_t)round_up(d, 64));
+        w.acc = c.take_data(4 * (size_t)stream_ctas(true, (int)N, d, V) * (size_t)(N < kStreamTokens ? N : kStreamTokens) * (size_t)round_up(d, 64));
         return w;
     }
     const Pieces p = pieces(N, d, V, dt);
@@ -536,11 +549,17 @@ StreamParams stream_params(const void *hidden, const void *W, int N, int d, int 
 // row statistics of one model by whichever kernel the sizes call for, except the tensor cores'
 cudaError_t other_stats(HeadRow &r, int N, int V, int dt, int *status, cudaStream_t st)
 {
-    if (stream_head(false, N, r.d, dt)) {
-        StreamParams p = stream_params(r.hidden, r.W, N, r.d, V, dt);
-        p.part = const_cast<float2 *>(r.part);
+    if (stream_head(false, N, r.d, V, dt)) {
         r.parts = stream_ctas(false, N, r.d, V);
-        return launch_stream(false, dt == SPR_F32, p, st);
+        cudaError_t e = cudaSuccess;
+        for (int i = 0; i * kStreamTokens < N && e == cudaSuccess; ++i) {
+            const int64_t n0 = i * kStreamTokens;
+            StreamParams p = stream_params(static_cast<const char *>(r.hidden) + n0 * r.d * elem_size(dt), r.W, pass_tokens(N, i), r.d, V, dt);
+            p.part = const_cast<float2 *>(r.part) + n0 * r.parts;
+            p.ctas = r.parts;
+            e = launch_stream(false, dt == SPR_F32, p, st);
+        }
+        return e;
     }
     SmallParams sp;
     memset(&sp, 0, sizeof sp);
@@ -645,7 +664,7 @@ int head_loss(const void *hidden, const void *W, const int32_t *targets, int N, 
     prm.status = at<int>(ws, 0);
     HeadRow h = {hidden, W, at<float2>(ws, lay.part), d, 0};
     cudaError_t e;
-    if (small_head(false, N, d, V, dt) || stream_head(false, N, d, dt)) {
+    if (small_head(false, N, d, V, dt) || stream_head(false, N, d, V, dt)) {
         e = other_stats(h, N, V, dt, prm.status, st);
     } else {
         PairOperand a, b;
@@ -687,17 +706,23 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
                                  at<float>(ws, lay.acc), at<int>(ws, lay.tickets), at<int>(ws, 0), st));
     const bool f32 = dt == SPR_F32;
     const size_t es = elem_size(dt);
-    if (stream_head(true, N, d, dt)) {
-        StreamParams p = stream_params(hidden, W, N, d, V, dt);
-        p.targets = targets;
-        p.lse = lse;
-        p.grad_loss = grad_loss;
-        p.d_hidden = d_hidden;
-        p.d_W = d_W;
-        p.acc = at<float>(ws, lay.acc);
-        p.status = at<int>(ws, 0);
-        cudaError_t e = launch_stream(true, f32, p, st);
-        if (e == cudaSuccess && d_hidden) e = sum_slices(p.acc, stream_ctas(true, N, d, V), N, d, dt, d_hidden, st);
+    if (stream_head(true, N, d, V, dt)) {
+        cudaError_t e = cudaSuccess;
+        for (int i = 0; i * kStreamTokens < N && e == cudaSuccess; ++i) {
+            const int64_t n0 = i * kStreamTokens;
+            StreamParams p = stream_params(static_cast<const char *>(hidden) + n0 * d * es, W, pass_tokens(N, i), d, V, dt);
+            p.targets = targets + n0;
+            p.lse = lse + n0;
+            p.grad_loss = grad_loss + n0;
+            p.d_hidden = d_hidden ? static_cast<char *>(d_hidden) + n0 * d * es : nullptr;
+            p.d_W = d_W;
+            p.add = i > 0;
+            p.acc = at<float>(ws, lay.acc);      // of one pass after the other
+            p.ctas = stream_ctas(true, N, d, V);
+            p.status = at<int>(ws, 0);
+            e = launch_stream(true, f32, p, st);
+            if (e == cudaSuccess && d_hidden) e = sum_slices(p.acc, p.ctas, p.N, d, dt, p.d_hidden, st);
+        }
         return finish(e);
     }
     const Pieces pc = pieces(N, d, V, dt);
@@ -823,7 +848,7 @@ int verifier_labels_head(const void *p_hidden, const void *p_W, int dp, const vo
     for (int i = 0; i < 2 && e == cudaSuccess; ++i) {
         const bool is_p = (i == 0) == (dp >= dq);
         HeadRow &r = is_p ? p : q;
-        if (small_head(false, N, r.d, V, dt) || stream_head(false, N, r.d, dt)) {
+        if (small_head(false, N, r.d, V, dt) || stream_head(false, N, r.d, V, dt)) {
             e = other_stats(r, N, V, dt, prm.status, st);
         } else {
             e = stats_job(prm.job[pairs], a[pairs], b[pairs], r.hidden, r.W, N, r.d, V, dt, ws, is_p ? lay.p : lay.q, st);

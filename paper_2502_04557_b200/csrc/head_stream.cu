@@ -1,4 +1,4 @@
-// The vocabulary head for a handful of tokens (at most eight): one pass over W.
+// The vocabulary head for a handful of tokens: a pass over W for every eight of them.
 //
 // With so few rows a product reads W and does little with it: it is bound by memory, and the tensor-core
 // kernels would lay out fp32 or unaligned heads in the workspace first, three to six times the traffic.
@@ -49,10 +49,12 @@ __device__ __forceinline__ void stage_hidden(const StreamParams &prm, int nt, fl
     }
 }
 
-template <typename T>
-__device__ __forceinline__ uint4 load_vec(const T *row, int c, int d, bool vec)      // elements c .. of a row, zeros past d
+// elements c .. of a row, zeros past d; CHANGED: by this call
+template <typename T, bool CHANGED>
+__device__ __forceinline__ uint4 load_vec(const T *row, int c, int d, bool vec)
 {
     constexpr int N = Vec<T>::N;
+    if (vec && CHANGED) return c < d ? *reinterpret_cast<const uint4 *>(row + c) : make_uint4(0u, 0u, 0u, 0u);
     if (vec) return c < d ? __ldg(reinterpret_cast<const uint4 *>(row + c)) : make_uint4(0u, 0u, 0u, 0u);
     T x[N];
 #pragma unroll
@@ -241,10 +243,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) stream_grad_kernel(const Stre
         // Four rows of W at a time, all loads of them ahead of the stores (which might be to the same place for all the
         // compiler knows)
         for (int r0 = 0; mine && r0 < rows; r0 += 4) {
-            uint4 x[4];
+            uint4 x[4], before[4];
+            if (sizeof(T) == 4 && dw && prm.add) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) before[i] = load_vec<T, true>(dw + (base + min(r0 + i, rows - 1)) * prm.d, c0, prm.d, prm.vec);
+            }
             if (prm.d_hidden) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = load_vec(w + (base + min(r0 + i, rows - 1)) * prm.d, c0, prm.d, prm.vec);
+                for (int i = 0; i < 4; ++i) x[i] = load_vec<T, false>(w + (base + min(r0 + i, rows - 1)) * prm.d, c0, prm.d, prm.vec);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -253,8 +259,12 @@ __global__ void __launch_bounds__(kGradThreads, 1) stream_grad_kernel(const Stre
                 float f[N];
                 if (prm.d_hidden) Vec<T>::unpack(x[i], f);
                 float o[N];
+                if (sizeof(T) == 4 && dw && prm.add) {
+                    Vec<T>::unpack(before[i], o);
+                } else {
 #pragma unroll
-                for (int e = 0; e < N; ++e) o[e] = 0.f;
+                    for (int e = 0; e < N; ++e) o[e] = 0.f;
+                }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const float y = D[buf][r][n];
@@ -320,8 +330,7 @@ cudaError_t start_typed(bool grad, const StreamParams &prm, int ctas, cudaStream
 
 cudaError_t launch_stream(bool grad, bool f32, const StreamParams &prm, cudaStream_t st)
 {
-    const int ctas = stream_ctas(grad, prm.N, prm.d, prm.V);
-    return f32 ? start_typed<float>(grad, prm, ctas, st) : start_typed<__nv_bfloat16>(grad, prm, ctas, st);
+    return f32 ? start_typed<float>(grad, prm, prm.ctas, st) : start_typed<__nv_bfloat16>(grad, prm, prm.ctas, st);
 }
 
 }  // namespace spr

@@ -1,4 +1,4 @@
-// The vocabulary head for at most eight tokens, one pass over W (head_stream.cu).
+// The vocabulary head for a handful of tokens, a pass over W for every eight of them (head_stream.cu).
 #pragma once
 
 #include <cuda_runtime.h>
@@ -6,11 +6,13 @@
 
 namespace spr {
 
-constexpr int kStreamTokens = 8;
+constexpr int kStreamTokens = 8;       // of a pass
 
 struct StreamParams {
     const void *hidden, *W;         // [N, d], [V, d]
-    int N, d, V;
+    int N, d, V;                    // N: tokens of this pass
+    int ctas;                       // of the launch: stream_ctas()
+    int add;                        // gradient, fp32: dW is added to what an earlier pass left
     int pitch;                      // d rounded up to 64
     int vec;                        // rows of W (and dW) are 16-byte aligned
     float2 *part;                   // forward: [N, ctas] (max, sum of exp)
@@ -25,9 +27,9 @@ inline int stream_rows(int N) { return N <= 1 ? 1 : N <= 2 ? 2 : N <= 4 ? 4 : 8;
 // d that the kernels take: the states in shared memory, and for the gradient a thread per 16 bytes of columns
 inline bool stream_fits(bool grad, int N, int d, bool f32)
 {
-    return N <= kStreamTokens && (int64_t)4 * stream_rows(N) * ((d + 63) / 64 * 64) <= 160 * 1024 && (!grad || d <= 512 * (f32 ? 4 : 8));
+    return (int64_t)4 * stream_rows(N) * ((d + 63) / 64 * 64) <= 160 * 1024 && (!grad || d <= 512 * (f32 ? 4 : 8));
 }
-// CTAs of a launch, from the sizes alone (the workspace holds a partial result of each)
+// CTAs of a pass, from the sizes alone (the workspace holds a partial result of each)
 inline int stream_ctas(bool grad, int N, int d, int V)
 {
     const int rows = grad ? 32 : 64;                                   // of W, per CTA and round

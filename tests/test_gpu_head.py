@@ -134,6 +134,21 @@ def test_a_handful_of_tokens_of_a_large_head(spr, N, d, V, dtype):
     check_grad(spr, h, w, t, gl, lse)
 
 
+@pytest.mark.parametrize("N,d,V", [(9, 1024, 16401), (16, 2048, 8200), (17, 1001, 17011), (24, 520, 32300), (25, 520, 32300)])
+def test_fp32_tokens_in_several_passes(spr, N, d, V):
+    """Eight tokens at a time under a head of 2^24 elements: the loss up to 24 tokens, the gradient, which adds to its dW,
+    up to 16; the workspace of one call serves the next."""
+    h, w, t, gl = problem(N, d, V, torch.float32, seed=N + d)
+    _, lse = check_loss(spr, h, w, t)
+    ws = workspace(spr, spr.OP_HEAD_LOSS_GRAD, N, V, d, torch.float32)
+    first = check_grad(spr, h, w, t, gl, lse, ws=ws)
+    again = spr.head_loss_grad(h, w, t, lse, gl, ws)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    dh, none = spr.head_loss_grad(h, w, t, lse, gl, ws, want_W=False)
+    none2, dw = spr.head_loss_grad(h, w, t, lse, gl, ws, want_hidden=False)
+    assert none is None and none2 is None and torch.equal(dh, first[0]) and torch.equal(dw, first[1])
+
+
 @pytest.mark.parametrize("N,d,V,dtype", [(2048, 512, 30011, torch.bfloat16), (4096, 256, 128256, torch.bfloat16),
                                          (700, 264, 50257, torch.bfloat16), (1500, 136, 33000, torch.float32)],
                          ids=lambda v: str(v).replace("torch.", ""))
