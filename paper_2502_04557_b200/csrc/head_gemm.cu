@@ -461,7 +461,8 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                 float *a = j.acc + (int64_t)it.split * j.acc_stride + r0 * j.acc_pitch + cl;    // used where there is an acc
                 T *o = static_cast<T *>(j.out) + r0 * j.out_pitch + cl;                         // used where there is an out
                 // four elements of the caller's type are stored at once where every row allows it
-                const bool vec = ((reinterpret_cast<uintptr_t>(j.out) | (uintptr_t)(j.out_pitch * (int64_t)sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
+                const uintptr_t where = reinterpret_cast<uintptr_t>(j.out) | (uintptr_t)(j.out_pitch * (int64_t)sizeof(T));
+                const bool vec = (where & (4 * sizeof(T) - 1)) == 0;
                 if (sizeof(T) == 2 && j.boxes) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {

@@ -310,12 +310,16 @@ bool small_size(bool grad, int64_t N, int d, int64_t V)
 }
 // A handful of tokens: passes over W as it is (head_stream.cu), one for every eight tokens.  fp32: up to eight tokens,
 // whatever the size, and up to 24 (16 for the gradient, which has a thread per four columns: from 512 columns) where W
-// has 2^24 elements; bf16: up to four, two for the gradient where TMA can take the rows.  Measured (us, passes / tensor cores, loss and gradient), d = 2048, V = 32000: f32
-// N = 8 82 / 293 and 218 / 730, N = 16 163 / 274 and 579 / 730, N = 24 243 / 275 and 878 / 734; d = 960, V = 116326: f32 N = 9
-// 190 / 518 and 844 / 1347, N = 32 480 / 465; d = 256, V = 70000: N = 16 54 / 91 and 384 / 240; d = 256, V = 20000: N = 24 40 / 40 and 187 / 100; bf16 N = 1 27 / 46 and
-// 79 / 139, N = 2 29 / 44 and 85 / 134, N = 4 37 / 40 and 121 / 129 (768 x 50257: N = 2 22 / 28 and 86 / 86, N = 4 28 / 28
-// and 110 / 87); bf16 d = 1001, N = 4 41 / 53 and 131 / 183.  One pass / tiles of head_small.cu: f32 4x256x1000 5.4 / 8.2
-// and 9 / 16.8, 8x64x500 5.3 / 6.8 and 11 / 11.7, 8x1024x512 14 / 18 and 24 / 37, 1x768x1000 6.3 / 15 and 10 / 41.
+// has 2^24 elements; bf16: up to four, two for the gradient where TMA can take the rows.  Measured (us, passes / tensor
+// cores, loss and gradient):
+//   d = 2048, V = 32000   f32 N = 8 82 / 293 and 218 / 730, N = 16 163 / 274 and 579 / 730, N = 24 243 / 275 and 878 / 734
+//                         bf16 N = 1 27 / 46 and 79 / 139, N = 2 29 / 44 and 85 / 134, N = 4 37 / 40 and 121 / 129
+//   d = 960, V = 116326   f32 N = 9 190 / 518 and 844 / 1347, N = 32 loss 480 / 465
+//   d = 256, V = 70000    f32 N = 16 54 / 91 and 384 / 240;  V = 20000: N = 24 40 / 40 and 187 / 100
+//   d = 768, V = 50257    bf16 N = 2 22 / 28 and 86 / 86, N = 4 28 / 28 and 110 / 87
+//   d = 1001, V = 32000   bf16 N = 4 41 / 53 and 131 / 183
+// One pass / tiles of head_small.cu: f32 4x256x1000 5.4 / 8.2 and 9 / 16.8, 8x64x500 5.3 / 6.8 and 11 / 11.7, 8x1024x512
+// 14 / 18 and 24 / 37, 1x768x1000 6.3 / 15 and 10 / 41.
 constexpr int kMostLoss = 24, kMostGrad = 16;
 bool stream_head(bool grad, int64_t N, int d, int64_t V, int dt)
 {
@@ -411,7 +415,8 @@ HeadGradWs head_grad_layout(Carver &c, int64_t N, int d, int V, int dt)
     }
     if (stream_head(true, N, d, V, dt)) {
         w.hidden = w.W = w.tickets = w.dlogits = 0;
-        w.acc = c.take_data(4 * (size_t)stream_ctas(true, (int)N, d, V) * (size_t)(N < kStreamTokens ? N : kStreamTokens) * (size_t)round_up(d, 64));
+        const int64_t tokens = N < kStreamTokens ? N : kStreamTokens;      // of a pass
+        w.acc = c.take_data(4 * (size_t)stream_ctas(true, (int)N, d, V) * (size_t)tokens * (size_t)round_up(d, 64));
         return w;
     }
     const Pieces p = pieces(N, d, V, dt);
@@ -554,7 +559,8 @@ cudaError_t other_stats(HeadRow &r, int N, int V, int dt, int *status, cudaStrea
         cudaError_t e = cudaSuccess;
         for (int i = 0; i * kStreamTokens < N && e == cudaSuccess; ++i) {
             const int64_t n0 = i * kStreamTokens;
-            StreamParams p = stream_params(static_cast<const char *>(r.hidden) + n0 * r.d * elem_size(dt), r.W, pass_tokens(N, i), r.d, V, dt);
+            const char *h = static_cast<const char *>(r.hidden) + n0 * r.d * elem_size(dt);
+            StreamParams p = stream_params(h, r.W, pass_tokens(N, i), r.d, V, dt);
             p.part = const_cast<float2 *>(r.part) + n0 * r.parts;
             p.ctas = r.parts;
             e = launch_stream(false, dt == SPR_F32, p, st);

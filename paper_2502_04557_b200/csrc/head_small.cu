@@ -118,7 +118,8 @@ __global__ void __launch_bounds__(kSmallThreads) small_kernel(const SmallParams 
         const int share = (here + kGroups - 1) / kGroups, i1 = min(here, (g + 1) * share);
 #pragma unroll 4
         for (int i = g * share; i < i1; ++i) {
-            const float4 a = *reinterpret_cast<const float4 *>(sa + i * kPitch + 4 * ty), b = *reinterpret_cast<const float4 *>(sb + i * kPitch + 4 * tx);
+            const float4 a = *reinterpret_cast<const float4 *>(sa + i * kPitch + 4 * ty);
+            const float4 b = *reinterpret_cast<const float4 *>(sb + i * kPitch + 4 * tx);
             const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
             for (int r = 0; r < 4; ++r)

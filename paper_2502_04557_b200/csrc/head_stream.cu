@@ -233,7 +233,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) stream_grad_kernel(const Stre
         // the next rows are asked for as far as L2 while these are worked on
         const int64_t next = base + (int64_t)gridDim.x * kGradRows + threadIdx.x;
         if (threadIdx.x < kGradRows && prm.vec && next < prm.V)
-            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(w + next * prm.d), "r"((uint32_t)(prm.d * sizeof(T))) : "memory");
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(w + next * prm.d), "r"((uint32_t)(prm.d * sizeof(T)))
+                         : "memory");
         const int64_t row = base + warp * R + my_row;
         const float l = row_logits<T, NT, R, NT <= 2 ? 4 : 2>(prm, h, base + warp * R, lane);
         if ((lane & ((1 << kShift) - 1)) == 0 && idx < R * NT)

@@ -81,7 +81,8 @@ __device__ __forceinline__ void store_box(const CUtensorMap *map, int c0, int c1
 }
 __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }      // the source is free
 __device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-__device__ __forceinline__ void fence_stores() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }      // behind writes to the source
+// behind writes to the source
+__device__ __forceinline__ void fence_stores() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // Shared-memory matrix descriptor of a tile made of 64 x 64 boxes (128-byte swizzle, 8 KB each).
 //   along K  (K contiguous): rows of 128 bytes, 8-row groups 1024 bytes apart

@@ -163,7 +163,8 @@ __device__ __forceinline__ uint32_t unit_at(uint32_t base, int k) { return base 
 // Behind the boxes of the d bytes a box of the rows' exponent bytes: 16, 32, 64 or 128 bytes x T rows, swizzled in as many bytes.
 __host__ __device__ constexpr int tile_boxes(int d) { return (d + 127) / 128; }
 __host__ __device__ constexpr int exponent_width(int d) { return d <= 512 ? 16 : d <= 1024 ? 32 : d <= 2048 ? 64 : 128; }
-__host__ __device__ constexpr int tile_share(int d, int rows) { return rows * (tile_boxes(d) * 128 + 2 * exponent_width(d)); }       // of the ring
+// a tile's share of the ring
+__host__ __device__ constexpr int tile_share(int d, int rows) { return rows * (tile_boxes(d) * 128 + 2 * exponent_width(d)); }
 __device__ __forceinline__ uint32_t exponent_at(int width, int r, int b)
 {
     return (uint32_t)(r * width + (((b >> 4) ^ ((r * width) >> 7)) & (width / 16 - 1)) * 16 + (b & 15));
@@ -442,7 +443,8 @@ __global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainPara
                         float *g = grad[i0 + i];
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const uint32_t at = unit_at(tile + a2 + (uint32_t)((i0 + i) / 4 * (T * 128)), 2 * ((i0 + i) & 3) + h);      // a last block of 16 reads on, into what follows in the row
+                            // a last block of 16 reads on, into what follows in the row
+                            const uint32_t at = unit_at(tile + a2 + (uint32_t)((i0 + i) / 4 * (T * 128)), 2 * ((i0 + i) & 3) + h);
                             int c[4];
                             if constexpr (T == 32) {
                                 uint32_t a[4];
@@ -452,7 +454,9 @@ __global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainPara
                                 mma_s8(c, a, bd);
                             } else {
                                 uint32_t a0, a4;
-                                asm volatile("ldmatrix.sync.aligned.m16n16.x1.trans.shared.b8 {%0,%1}, [%2];" : "=r"(a0), "=r"(a4) : "r"(at));
+                                asm volatile("ldmatrix.sync.aligned.m16n16.x1.trans.shared.b8 {%0,%1}, [%2];"
+                                             : "=r"(a0), "=r"(a4)
+                                             : "r"(at));
                                 mma_s8_k16(c, a0, a4, bd.x);
                             }
                             g[2 * h] = fmaf((float)(c[0] * m0 + c[1]), scale[i], g[2 * h]);
@@ -597,8 +601,10 @@ cudaError_t launch_train8(const TrainParams &tp, cudaStream_t st)
     if (ring < 3 && most >= 3) return cudaErrorInvalidConfiguration;      // two tiles are in use while the next arrives
     if (ring > most) ring = most;
     CUtensorMap map, emap;
-    if (!packed_map(&map, tp.hidden, tp.N, tp.d, 128, T) || !packed_map(&emap, tp.hidden, tp.N, tp.d, exponent_width(tp.d), T)) return cudaErrorInvalidValue;
-    train8_kernel<NB, T, W, C><<<p.ctas, Fit8<NB, T, W>::kThreads, (size_t)ring * tile + Fit8<NB, T, W>::kBytes, st>>>(p, map, emap, (int)ring);
+    if (!packed_map(&map, tp.hidden, tp.N, tp.d, 128, T) || !packed_map(&emap, tp.hidden, tp.N, tp.d, exponent_width(tp.d), T))
+        return cudaErrorInvalidValue;
+    const size_t smem = (size_t)ring * tile + Fit8<NB, T, W>::kBytes;
+    train8_kernel<NB, T, W, C><<<p.ctas, Fit8<NB, T, W>::kThreads, smem, st>>>(p, map, emap, (int)ring);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};          // set up while the gradient kernel ends
