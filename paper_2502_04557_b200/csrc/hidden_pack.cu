@@ -101,14 +101,15 @@ __device__ __forceinline__ uint2 quantise(const float (&x)[8], uint32_t top, int
     }
     return q;
 }
-// byte + 128 as the low mantissa byte of 2^23; (2^23 + 128 + q) 2^e - (2^23 + 128) 2^e is exact
+// byte + 128 as the low mantissa byte of 2^23; less 2^23 + 128 that is q, and q 2^e is exact.  (With the subtraction behind
+// the scaling, as (2^23 + 128) 2^e, it would be beyond fp32 from e = 105 on.)
 __device__ __forceinline__ void dequantise(uint2 q, int e2, float (&x)[8])
 {
     const float scale = e2 == kBadBlock ? __int_as_float(0x7fc00000) : __int_as_float((e2 + 127) << 23);
-    const float off = -8388736.f * scale;
     const uint32_t w[2] = {q.x ^ 0x80808080u, q.y ^ 0x80808080u};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = fmaf(__uint_as_float(__byte_perm(w[e >> 2], 0x4b000000u, 0x7440 + (e & 3))), scale, off);
+    for (int e = 0; e < 8; ++e)
+        x[e] = (__uint_as_float(__byte_perm(w[e >> 2], 0x4b000000u, 0x7440 + (e & 3))) - 8388736.f) * scale;
 }
 
 // ---------------------------------------------------------------- any width and alignment

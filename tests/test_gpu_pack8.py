@@ -332,3 +332,37 @@ def test_nothing_is_written_beside_the_parameters(spr, N, d):
         t.zero_()
     spr.verifier_train_step8(packed, d, y.cuda(), frames[0][1], frames[1][1], frames[2][1], 1, 0.01, ws, loss=frames[3][1])
     assert all(untouched(b) for b, _ in frames) and float(frames[3][1]) == pytest.approx(np.log(2.0), rel=1e-6)
+
+
+@pytest.mark.parametrize("d", [32, 96, 40], ids=lambda d: f"d{d}")
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_every_exponent_is_packed_and_unpacked_exactly(spr, dtype, d):
+    """A row for each exponent that packing gives, -126 to 121, of numbers q 2^e with |q| <= 127 and a largest one of 64
+    and more: nothing is rounded either way, through whole rows of blocks (d = 32, 96) and through the form for any width."""
+    e = torch.arange(-126, 122).repeat_interleave(2)
+    g = torch.Generator().manual_seed(d)
+    q = torch.randint(-127, 128, (len(e), d), generator=g)
+    q[:, ::32] = torch.where(torch.rand(q[:, ::32].shape, generator=g) < 0.5, -1, 1) * torch.randint(64, 128, q[:, ::32].shape, generator=g)
+    q[:, 1::32] = 0
+    x = torch.ldexp(q.double(), e[:, None].double())
+    assert bool(x.isfinite().all()) and torch.equal(x.to(dtype).double(), x)
+    packed = spr.hidden_pack8(x.to(dtype).cuda())
+    assert np.array_equal(packed.cpu().numpy(), pack_ref(x.numpy()))
+    assert torch.equal(packed[:, d].cpu().view(torch.int8), e.to(torch.int8))
+    for ty in (torch.float32, torch.bfloat16):
+        assert torch.equal(spr.hidden_unpack8(packed, d, ty).cpu().double(), x)
+
+
+def test_all_of_the_extremes_come_back(spr):
+    """The largest and smallest numbers of either type beside infinities and NaN: every element as its bytes say."""
+    big = torch.finfo(torch.float32).max
+    x = torch.zeros((6, 64))
+    x[0, :3], x[1, 40:42], x[2, 5] = torch.tensor([big, -big, big / 2]), torch.tensor([2.0 ** 111, -1.0]), 2.0 ** -149
+    x[3, 7], x[4, 33], x[5] = float("inf"), float("nan"), -2.0 ** 127
+    for dtype in (torch.float32, torch.bfloat16):
+        y = x.to(dtype)
+        packed = spr.hidden_pack8(y.cuda())
+        want = pack_ref(y.double().numpy())
+        assert np.array_equal(packed.cpu().numpy(), want)
+        for ty in (torch.float32, torch.bfloat16):
+            assert np.array_equal(spr.hidden_unpack8(packed, 64, ty).cpu().double().numpy(), unpack_ref(want, 64), equal_nan=True)
