@@ -31,7 +31,8 @@
  *   - Problems a kernel detects (a draft token id outside [0,V), a row index
  *     outside the logits tensor, a bounded wait that ran out) never trap: the
  *     affected outputs are set to -1, a sticky status word in `ws` records the
- *     first such code, and spr_device_status() returns and clears it.
+ *     first such code - or SPR_ERR_TIMEOUT, which replaces any other - and
+ *     spr_device_status() returns and clears it.
  *   - Outputs are fully overwritten and are bit-identical from run to run for
  *     identical inputs (fixed reduction orders, no floating-point atomics).
  *   - Logits must be finite or -inf; uniforms must lie in [0,1); V <= 2^30.

@@ -246,8 +246,11 @@ __device__ __forceinline__ bool take_ticket(int *counter, int total, int n = 1)
     return true;
 }
 
-// first error wins; the word stays set until the host clears it
+// First error wins; the word stays set until the host clears it.
 __device__ __forceinline__ void raise_status(int *status, int code) { atomicCAS(status, 0, code); }
+// A wait that ran out replaces whatever stands there, and nothing replaces it: the kernels that finish a call ask the word
+// whether its results exist, and a bad token that nobody has read yet must not hide that they do not.
+__device__ __forceinline__ void raise_timeout(int *status) { atomicExch(status, SPR_ERR_TIMEOUT); }
 
 __device__ __forceinline__ float warp_max(float v)
 {

@@ -44,7 +44,7 @@ __device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, int *ab
         if ((i & 255u) == 255u && *reinterpret_cast<volatile int *>(abort)) return false;
     }
     *reinterpret_cast<volatile int *>(abort) = 1;
-    raise_status(status, SPR_ERR_TIMEOUT);
+    raise_timeout(status);
     return false;
 }
 __device__ __forceinline__ void bar_wait_quiet(uint64_t *bar, uint32_t parity, uint32_t limit)

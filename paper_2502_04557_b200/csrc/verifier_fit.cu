@@ -290,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, ring_ctas_per_sm(VPL, WPR, G)) train
     if (!ok) {
         // A wait ran out: report it, then give the copies still on their way the same bounded
         // time to land before the CTA's shared memory goes away: the blocks from fail_at's on.
-        if (lane == 0) raise_status(prm.status, SPR_ERR_TIMEOUT);
+        if (lane == 0) raise_timeout(prm.status);
         for (int k = fail_at / G; feeder_team_has_copies(prm) && k < nb && k < fail_at / G + SLOTS; ++k)
             ring_wait(&bar[k % SLOTS], (uint32_t)(k / SLOTS) & 1u, limit);
     }

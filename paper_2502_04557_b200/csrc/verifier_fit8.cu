@@ -279,7 +279,7 @@ __global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainPara
         if (!ok) {
             // A wait ran out: report it, then give the copies still on their way the same bounded time to land
             // before the CTA's shared memory goes away.
-            if (lane == 0) raise_status(prm.status, SPR_ERR_TIMEOUT);
+            if (lane == 0) raise_timeout(prm.status);
             for (int i = max(0, asked - ring_exps); feed && i < asked; ++i)
                 fit_wait(&ethere[i % ring_exps], (uint32_t)(i / ring_exps) & 1u, prm.spin_limit);
         }
@@ -490,7 +490,7 @@ __global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainPara
         }
     }
     if (!ok) {                                 // as above
-        if (lane == 0) raise_status(prm.status, SPR_ERR_TIMEOUT);
+        if (lane == 0) raise_timeout(prm.status);
         for (int i = max(0, asked - ring_tiles); feed && i < asked; ++i)
             fit_wait(&mine[i % ring_tiles], (uint32_t)(i / ring_tiles) & 1u, prm.spin_limit);
     }

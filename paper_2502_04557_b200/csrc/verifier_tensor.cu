@@ -130,7 +130,7 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, Contro
         if ((i & 255u) == 255u && *reinterpret_cast<volatile int *>(&ctl->abort)) return false;
     }
     *reinterpret_cast<volatile int *>(&ctl->abort) = 1;
-    raise_status(status, SPR_ERR_TIMEOUT);
+    raise_timeout(status);
     return false;
 }
 // the same without side effects: used on the way out, when the CTA has already given up
