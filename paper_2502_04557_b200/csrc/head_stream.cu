@@ -13,6 +13,8 @@
 // N = 8 218 us, bf16 N = 1 79 us (memory takes in pure writes at 3.9 TB/s: 67 us for fp32, 34 us for bf16, beside the reads).
 // With more tokens it is the products of every vector of W with all of them.  A small head takes 4 to 7 us for
 // the loss and 9 us for the gradient: launches.
+#include <atomic>
+
 #include "head_stream.h"
 
 #include "common.cuh"
@@ -302,20 +304,29 @@ __global__ void __launch_bounds__(kGradThreads, 1) stream_grad_kernel(const Stre
     }
 }
 
-template <typename K>
-cudaError_t start(K kernel, const StreamParams &prm, int ctas, int threads, size_t smem, cudaStream_t st)
+// The attribute belongs to the kernel and the device, not to the call: it is set once, to the most that any call takes, so that
+// host threads with states of different widths do not take shared memory from each other.
+template <auto KERNEL>
+cudaError_t start(const StreamParams &prm, int ctas, int threads, size_t smem, cudaStream_t st)
 {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static std::atomic<bool> attr_set[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    kernel<<<ctas, threads, smem, st>>>(prm);
+    if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
+        e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStreamSmem);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
+    }
+    KERNEL<<<ctas, threads, smem, st>>>(prm);
     return cudaGetLastError();
 }
 template <typename T, int NT>
 cudaError_t start_any(bool grad, const StreamParams &prm, int ctas, cudaStream_t st)
 {
     const size_t smem = 4 * (size_t)NT * prm.pitch;
-    return grad ? start(stream_grad_kernel<T, NT>, prm, ctas, kGradThreads, smem, st)
-                : start(stream_stats_kernel<T, NT>, prm, ctas, 32 * kStatWarps, smem, st);
+    return grad ? start<stream_grad_kernel<T, NT>>(prm, ctas, kGradThreads, smem, st)
+                : start<stream_stats_kernel<T, NT>>(prm, ctas, 32 * kStatWarps, smem, st);
 }
 template <typename T>
 cudaError_t start_typed(bool grad, const StreamParams &prm, int ctas, cudaStream_t st)

@@ -2,11 +2,13 @@
 #pragma once
 
 #include <cuda_runtime.h>
+#include <stddef.h>
 #include <stdint.h>
 
 namespace spr {
 
 constexpr int kStreamTokens = 8;       // of a pass
+constexpr size_t kStreamSmem = 160 * 1024;      // most that the states of a pass take
 
 struct StreamParams {
     const void *hidden, *W;         // [N, d], [V, d]
@@ -27,7 +29,7 @@ inline int stream_rows(int N) { return N <= 1 ? 1 : N <= 2 ? 2 : N <= 4 ? 4 : 8;
 // d that the kernels take: the states in shared memory, and for the gradient a thread per 16 bytes of columns
 inline bool stream_fits(bool grad, int N, int d, bool f32)
 {
-    return (int64_t)4 * stream_rows(N) * ((d + 63) / 64 * 64) <= 160 * 1024 && (!grad || d <= 512 * (f32 ? 4 : 8));
+    return (int64_t)4 * stream_rows(N) * ((d + 63) / 64 * 64) <= (int64_t)kStreamSmem && (!grad || d <= 512 * (f32 ? 4 : 8));
 }
 // CTAs of a pass, from the sizes alone (the workspace holds a partial result of each)
 inline int stream_ctas(bool grad, int N, int d, int V)

@@ -550,3 +550,44 @@ def test_a_draft_head_fitted_labelled_and_its_verifier_fitted(spr):
     # tests/test_gpu_pack8.py for one step
     assert float(got) == pytest.approx(ref, rel=1e-6)
     assert np.abs(st[0].cpu().double().numpy() - theta).max() <= 1e-3 * 0.01
+
+
+@pytest.mark.parametrize("grad", [False, True], ids=["loss", "gradient"])
+def test_two_host_threads_with_heads_of_different_widths(spr, grad):
+    """Two threads, a stream and a workspace each, call the kernel for a handful of tokens over and over, one with 64 KB and
+    more of states in shared memory and one with 8 KB: neither call depends on what the other asked for.  (The calls are made
+    without the binding's checks, so that the threads spend their time in the library.)"""
+    import threading
+    N, V, L = 8, 64, spr.lib()
+    jobs = []
+    for d in (2048 if grad else 4096, 256):
+        h, w, t, gl = problem(N, d, V, torch.float32, seed=d)
+        # small enough for one round of a CTA or two
+        ws = workspace(spr, spr.OP_HEAD_LOSS_GRAD if grad else spr.OP_HEAD_LOSS, N, V, d, torch.float32)
+        loss, lse = check_loss(spr, h, w, t)
+        want = check_grad(spr, h, w, t, gl, lse) if grad else (loss, lse)
+        out = tuple(torch.empty_like(x) for x in want)
+        stream = torch.cuda.Stream()
+        p = lambda x: x.data_ptr()
+        tail = (N, d, V, spr.F32, p(out[0]), p(out[1]), p(ws.buf), ws.nbytes, stream.cuda_stream)
+        args = (p(h), p(w), p(t), p(lse), p(gl)) + tail if grad else (p(h), p(w), p(t)) + tail
+        jobs.append((args, stream, (h, w, t, gl, lse, ws), out, want))
+    torch.cuda.synchronize()
+    call, failed = L.head_loss_grad if grad else L.head_loss, []
+
+    def run(args, *rest):
+        for _ in range(20000):
+            rc = call(*args)
+            if rc != 0:
+                failed.append(rc)
+                return
+
+    threads = [threading.Thread(target=run, args=j) for j in jobs]
+    for x in threads:
+        x.start()
+    for x in threads:
+        x.join()
+    torch.cuda.synchronize()
+    assert not failed
+    for _, _, (*_, ws), out, want in jobs:
+        assert ws.device_status() == 0 and all(torch.equal(a, b) for a, b in zip(out, want))
