@@ -3,6 +3,7 @@
 // linear-layer + sigmoid verifier on the draft model's hidden states.
 #include <string.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "host_util.h"
@@ -366,13 +367,21 @@ cudaError_t launch_grad_ring(const TrainParams &tp, cudaStream_t st)
 {
     TrainParams p = tp;
     constexpr int kTeams = kWarps / WPR;
-    const size_t smem = (size_t)kTeams * SLOTS * VPL * WPR * 32 * G * 16 + sizeof(float) * ((size_t)tp.d + 2);
+    constexpr size_t kRing = (size_t)kTeams * SLOTS * VPL * WPR * 32 * G * 16;
+    // the most that any d of this form takes: the attribute belongs to the kernel, and host threads share it
+    constexpr size_t kMost = kRing + sizeof(float) * ((size_t)VPL * WPR * 32 * Vec<T>::N + 2);
+    const size_t smem = kRing + sizeof(float) * ((size_t)tp.d + 2);
     auto kernel = train_grad_ring_kernel<T, VPL, WPR, R, SLOTS, G>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static std::atomic<bool> attr_set[64];
     int per_sm = 0, dev = 0, sms = 0;
-    if (e != cudaSuccess ||
-        (e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kThreads, smem)) != cudaSuccess ||
-        (e = cudaGetDevice(&dev)) != cudaSuccess ||
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMost);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
+    }
+    if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kThreads, smem)) != cudaSuccess ||
         (e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess)
         return e;
     if (per_sm < 1) return cudaErrorInvalidConfiguration;

@@ -273,3 +273,39 @@ def test_train_step_at_the_benchmark_size(spr):
     l0, t0, _, _ = training.verifier_train_step(to_np(S[:n]), y[:n].cpu().numpy(), np.zeros(d + 1), np.zeros(d + 1),
                                                 np.zeros(d + 1), 1, lr)
     assert abs(float(loss) / l0 - 1.0) < 2e-5 and np.abs(theta.cpu().double().numpy() - t0).max() <= 1e-3 * lr
+
+
+def test_two_host_threads_with_states_of_different_widths(spr):
+    """Two threads, a stream and a workspace each, take steps over and over on states of two widths that share a kernel:
+    neither step depends on how much shared memory the other asked for.  (The calls are made without the binding's checks,
+    so that the threads spend their time in the library.)"""
+    import threading
+    N, L = 8, spr.lib()
+    jobs = []
+    for d in (512, 264):
+        S, y = teacher_problem(N, d, torch.bfloat16, seed=d)
+        S, y = S.cuda(), y.cuda()
+        ws = spr.Workspace(spr.workspace_bytes(bd(spr).OP_VERIFIER_TRAIN, 0, 0, 0, d, 0, spr.BF16))
+        state, loss, stream = [torch.zeros(d + 1, device="cuda") for _ in range(3)], torch.empty(1, device="cuda"), torch.cuda.Stream()
+        p = lambda x: x.data_ptr()
+        args = (p(S), p(y), N, d, spr.BF16, *map(p, state), 1, 0.0, 0.9, 0.999, 1e-8, p(loss), p(ws.buf), ws.nbytes, stream.cuda_stream)
+        jobs.append((args, (S, y, ws, state, loss, stream)))
+    torch.cuda.synchronize()
+    failed = []
+
+    def run(args, keep):
+        for _ in range(20000):
+            rc = L.verifier_train_step(*args)
+            if rc != 0:
+                failed.append(rc)
+                return
+
+    threads = [threading.Thread(target=run, args=j) for j in jobs]
+    for x in threads:
+        x.start()
+    for x in threads:
+        x.join()
+    torch.cuda.synchronize()
+    assert not failed
+    for _, (_, _, ws, state, loss, _) in jobs:
+        assert ws.device_status() == 0 and not state[0].any() and float(loss) == pytest.approx(float(np.log(2.0)), rel=1e-6)
