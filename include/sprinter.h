@@ -87,8 +87,8 @@ typedef enum { SPR_VERIFIER_AUTO = 0, SPR_VERIFIER_SIMT = 1, SPR_VERIFIER_TENSOR
  * shard and d, h are ignored; SPR_OP_VERIFIER_LABELS uses B, K, V; SPR_OP_VERIFIER_TRAIN and
  * SPR_OP_VERIFIER_TRAIN8 use d only; SPR_OP_HEAD_LOSS, SPR_OP_HEAD_LOSS_GRAD and
  * SPR_OP_VERIFIER_LABELS_HEAD are for N = B*K >= 1 hidden states of width d, and
- * SPR_OP_VERIFIER_LABELS_HEAD takes the target's width as d and the draft's as h.  Returns 0 for invalid arguments.  A workspace sized for the
- * largest op serves all of them. */
+ * SPR_OP_VERIFIER_LABELS_HEAD takes the target's width as d and the draft's as h; what these three get serves every
+ * smaller N as well.  Returns 0 for invalid arguments.  A workspace sized for the largest op serves all of them. */
 size_t spr_workspace_bytes(int op, int B, int K, int V, int d, int h, int dt);
 
 /* Clears a freshly allocated workspace (enqueues a memset on the stream). */

@@ -304,9 +304,10 @@ int d_parts(int64_t N, int dt) { return dt == SPR_F32 ? 3 : N <= kTwoPartTokens 
 size_t packed_bytes(int64_t rows, int d, int dt) { return 2 * (size_t)rows * parts(dt) * (size_t)round_up(d, 64); }
 
 // Whether an fp32 problem is small enough for tiles of 32 x 32 on the CUDA cores (see small_head()).
+double small_limit(bool grad) { return (grad ? 0.75 : 1.0) * (1 << 27); }
 bool small_size(bool grad, int64_t N, int d, int64_t V)
 {
-    return (double)round_up(N, kSmallTile) * (double)round_up(V, kSmallTile) * (d + 200.0) <= (grad ? 0.75 : 1.0) * (1 << 27);
+    return (double)round_up(N, kSmallTile) * (double)round_up(V, kSmallTile) * (d + 200.0) <= small_limit(grad);
 }
 // A handful of tokens: passes over W as it is (head_stream.cu), one for every eight tokens.  fp32: up to eight tokens,
 // whatever the size, and up to 24 (16 for the gradient, which has a thread per four columns: from 512 columns) where W
@@ -426,6 +427,79 @@ HeadGradWs head_grad_layout(Carver &c, int64_t N, int d, int V, int dt)
     w.dlogits = c.take_data(2 * (size_t)N * d_parts(N, dt) * (size_t)p.width);
     w.acc = c.take_data(p.count * p.splits > 1 ? 4 * (size_t)p.splits * (size_t)N * (size_t)round_up(d, 64) : 0);
     return w;
+}
+
+// ---------------------------------------------------------------- workspace that serves every number of tokens up to N
+// What a call takes does not simply grow with its tokens: few of them keep D in two parts, dH's contraction is cut into fewer
+// ranges as the tiles of tokens become more, pieces are of whole tiles, and kernels change.  The size that is asked for is
+// the most of any call up to N, so that a short batch at the end of a run fits where the others did.
+struct Need {
+    size_t tickets, data;
+    template <typename F>
+    void at_least(F layout)
+    {
+        Carver c;
+        c.tickets = c.data = 0;
+        c.tickets_end = c.data_end = ~(size_t)0;
+        layout(c);
+        if (c.tickets > tickets) tickets = c.tickets;
+        if (c.data > data) data = c.data;
+    }
+};
+// Numbers of tokens up to N at which a kernel other than the pair's needs most: every handful, and the most that tiles on the
+// CUDA cores are taken for (what those need grows with the tokens).  f(n) for each of them, and for N.
+template <typename F>
+void for_token_counts(bool grad, int64_t N, int d, int64_t V, F f)
+{
+    for (int64_t n = 1; n <= N && n <= kMostLoss; ++n) f(n);
+    const double tile = (double)kSmallTile * (double)round_up(V, kSmallTile) * (d + 200.0);
+    const int64_t most = kSmallTile * (int64_t)(small_limit(grad) / tile);
+    if (most >= 1) f(most < N ? most : N);
+    f(N);
+}
+Need head_loss_need(int64_t N, int d, int V, int dt)
+{
+    Need need = {0, 0};
+    for_token_counts(false, N, d, V, [&](int64_t n) { need.at_least([&](Carver &c) { head_loss_layout(c, n, d, V, dt); }); });
+    return need;
+}
+// D of a piece: 2 parts n width bytes, and width is at most V and at most 256 MB of it or 8192 columns
+size_t most_dlogits(int64_t n, int parts, int V)
+{
+    const size_t row = 2 * (size_t)parts * (size_t)n, all = row * (size_t)round_up(V, kPairTile);
+    const size_t piece = row * 8192 > kPieceBytes ? row * 8192 : kPieceBytes;
+    return all < piece ? all : piece;
+}
+// the layout of the gradient on CTA pairs with the most of every part for any number of tokens up to N
+void most_pair_grad(Carver &c, int64_t N, int d, int V, int dt)
+{
+    const int64_t few = N < kTwoPartTokens ? N : kTwoPartTokens;
+    size_t D = most_dlogits(N, d_parts(N, dt), V);
+    const size_t D_few = most_dlogits(few, d_parts(few, dt), V);
+    if (D_few > D) D = D_few;
+    const bool cut = pieces(N, d, V, dt).count > 1 || pieces(few, d, V, dt).count > 1;
+    int64_t rows = cut ? N : 0;        // of acc: N in one range, or those of every number of tiles of tokens that has more
+    const int64_t kb = ceil_div(V, kPairBlockK), across = ceil_div(d, kPairTile);
+    for (int64_t m = 1; m <= ceil_div(N, kPairTile); ++m) {
+        int64_t s = 74 / (m * across);
+        if (s > kb / 4) s = kb / 4;
+        if (s < 2) break;
+        if (!cut) s = ceil_div(kb, ceil_div(kb, s));      // as pieces() rounds it; of a piece's blocks it is at most s
+        const int64_t n = m * kPairTile < N ? m * kPairTile : N;
+        if (n * s > rows) rows = n * s;
+    }
+    c.take_data(packed_bytes(N, d, dt));
+    c.take_data(needs_pack(d, dt) ? packed_bytes(V, d, dt) : 0);
+    c.take_data(D);
+    c.take_data(4 * (size_t)rows * (size_t)round_up(d, 64));
+}
+Need head_grad_need(int64_t N, int d, int V, int dt)
+{
+    Need need = {0, 0};
+    for_token_counts(true, N, d, V, [&](int64_t n) { need.at_least([&](Carver &c) { head_grad_layout(c, n, d, V, dt); }); });
+    if (!small_head(true, N, d, V, dt) && !stream_head(true, N, d, V, dt))
+        need.at_least([&](Carver &c) { most_pair_grad(c, N, d, V, dt); });
+    return need;
 }
 
 struct HeadLabelsWs {
@@ -630,17 +704,19 @@ bool head_sizes_ok(int64_t N, int d, int V) { return N >= 0 && d > 0 && d <= (1 
 size_t head_loss_ws_bytes(int64_t N, int d, int V, int dt)
 {
     if (N <= 0 || !head_sizes_ok(N, d, V)) return 0;
-    return ws_bytes_of([&](Carver &c) { head_loss_layout(c, N, d, V, dt); });
+    const Need need = head_loss_need(N, d, V, dt);
+    return ws_bytes_for(need.tickets, need.data);
 }
 size_t head_grad_ws_bytes(int64_t N, int d, int V, int dt)
 {
     if (N <= 0 || !head_sizes_ok(N, d, V)) return 0;
-    return ws_bytes_of([&](Carver &c) { head_grad_layout(c, N, d, V, dt); });
+    const Need need = head_grad_need(N, d, V, dt);
+    return ws_bytes_for(need.tickets, need.data);
 }
 size_t head_labels_ws_bytes(int64_t N, int dp, int dq, int V, int dt)
 {
     if (N <= 0 || !head_sizes_ok(N, dp, V) || !head_sizes_ok(N, dq, V)) return 0;
-    return ws_bytes_of([&](Carver &c) { head_labels_layout(c, N, dp, dq, V, dt); });
+    return ws_bytes_for(0, head_loss_need(N, dp, V, dt).data + head_loss_need(N, dq, V, dt).data);
 }
 
 }  // namespace spr

@@ -591,3 +591,18 @@ def test_two_host_threads_with_heads_of_different_widths(spr, grad):
     assert not failed
     for _, _, (*_, ws), out, want in jobs:
         assert ws.device_status() == 0 and all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("sizes,d,V,dtype", [((150, 128, 3), 768, 50257, torch.bfloat16), ((300, 256, 1), 2048, 32000, torch.bfloat16),
+                                             ((600, 512, 130), 100, 5000, torch.bfloat16), ((25, 24, 16, 8, 4), 520, 32300, torch.float32),
+                                             ((400, 129, 67, 9), 64, 1003, torch.float32)], ids=lambda v: str(v).replace("torch.", ""))
+def test_a_workspace_made_for_the_largest_batch_serves_smaller_ones(spr, sizes, d, V, dtype):
+    """A training run's last batch is a short one."""
+    spaces = [workspace(spr, op, sizes[0], V, d, dtype, h=d)
+              for op in (spr.OP_HEAD_LOSS, spr.OP_HEAD_LOSS_GRAD, spr.OP_VERIFIER_LABELS_HEAD)]
+    for N in sizes:
+        h, w, t, gl = problem(N, d, V, dtype, seed=N)
+        _, lse = check_loss(spr, h, w, t, ws=spaces[0])
+        check_grad(spr, h, w, t, gl, lse, ws=spaces[1])
+        _, ratio = spr.verifier_labels_head(h, w, h, w, t.clamp(min=0), [1.0], spaces[2])
+        assert bool((ratio == 1).all()) and spaces[2].device_status() == 0

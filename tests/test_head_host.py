@@ -223,3 +223,17 @@ def test_binding_refuses_host_tensors_types_and_shapes():
         binding._result(-1, out, (4,), torch.float32, "loss")
     with pytest.raises(TypeError, match="loss must be"):
         binding._result(-1, out.double(), (3,), torch.float32, "loss")
+
+
+@pytest.mark.parametrize("dt", [0, 1], ids=["f32", "bf16"])
+@pytest.mark.parametrize("d,V", [(768, 50257), (2048, 32000), (100, 5000), (64, 1003), (520, 32300), (257, 1003), (8, 9), (4104, 700),
+                                 (64, 128256), (1024, 300000), (136, 1000000), (30000, 2000)])
+def test_workspace_sizes_do_not_fall_as_tokens_are_added(d, V, dt):
+    """A workspace for the largest batch is one for every smaller batch: what follows from sizes that never fall, as each size
+    is at least what the call of that size takes."""
+    counts = sorted({*range(1, 700), *(256 * m + k for m in range(1, 80) for k in (-1, 0, 1)), *(2 ** b + k for b in range(9, 19) for k in (-1, 0, 1)),
+                     *(int(700 * 1.07 ** i) for i in range(90))})
+    for op in (spr.OP_HEAD_LOSS, spr.OP_HEAD_LOSS_GRAD, spr.OP_VERIFIER_LABELS_HEAD):
+        sizes = [spr.workspace_bytes(op, n, 1, V, d, max(8, d // 2), dt) for n in counts]
+        falls = [(n, a, b) for n, a, b in zip(counts[1:], sizes, sizes[1:]) if b < a]
+        assert not falls, (op, falls[:3])
