@@ -1,27 +1,32 @@
 // One Adam step of the linear verifier on hidden states kept in 8 bits (hidden_pack.cu):
 //   z_i = b + sum_j w_j q_ij 2^e_ij,  r = sigma(z) - y,  grad_j = sum_i r_i 2^e_ij q_ij
-// Floor: the packed rows once, 1.03 d bytes a sample (2^18 rows of 2048: 554 MB, 86 us; measured 111 us).  At that
+// Floor: the packed rows once, 1.03 d bytes a sample (2^18 rows of 2048: 554 MB, 86 us; measured 113 us).  At that
 // rate an SM takes in some 24 elements a clock, and on the CUDA cores it is instructions that bound the pass: a byte
 // turned into a float costs as much as the two products it goes into (measured: 244 us that way, 180 us with the
 // dot products in dp4a).  So both sums are integer products on the tensor cores (mma.m16n8k32, s8 x s8 -> s32):
 //   - a block of 32 columns shares its exponent within a row, so a block is one step of the contraction of
-//     the dot products.  A weight is written as 24 bits relative to the largest of its block, in three balanced
-//     signed digits, w = 2^E (256^2 d0 + 256 d1 + d2): three columns of the second operand.  What is left per
-//     block and row is one conversion and the row's scale.  Rounding a weight costs at most 2^-24 of twice
-//     the largest weight of its block, what fp32 products cost.
-//   - for the gradient the contraction runs over the rows of a tile: r_i 2^e_ij of the block, written as 22 bits
-//     relative to the largest of the tile in three digits, times the bytes, which ldmatrix transposes.  The
-//     integer sums are exact; per tile and column one conversion, and an fp32 sum over tiles.
+//     the dot products.  A weight is written relative to the largest of its block, in six balanced signed digits
+//     (six_digits(): 46 bits), six of the eight columns of the second operand.  What is left per block and row is one
+//     conversion and the row's scale.
+//   - for the gradient the contraction runs over the rows of a tile: r_i 2^e_ij of the block, written relative to the
+//     largest of the tile in six digits, too, times the bytes, which ldmatrix transposes.  The integer sums are
+//     exact; per tile and column one conversion for every two digits, and an fp32 sum over tiles.
+// Six digits, because the largest of a group need not have a part in a sum beside it: a state whose one huge column sets the
+// exponent of its block has bytes of zero in the other 31, and a large weight may meet a zero.  What is left out is 2^-46 of
+// the largest, so the other terms keep their 24 bits up to 2^22 below it (with three digits they lost a bit for every factor of
+// two).  The products work on eight columns whatever these hold; the digits themselves cost 110 -> 113 us at 2^18 x 2048, 67 ->
+// 69 us at 2^19 x 512 and 157 -> 172 us at 2^17 x 4096.
 // A CTA takes tiles of consecutive rows through a ring in shared memory.  A warp has 128 columns (256 above 2048) of
 // every tile: it fetches them itself, by TMA in boxes of 128 bytes by all rows with the 128-byte swizzle, which keeps
 // ldmatrix free of bank conflicts; it forms its part of the tile's dot products, then the sums of its columns of
 // the tile before, and asks for the next columns at once.  One more warp turns dot products into residuals in the
 // meantime and fetches the exponent bytes, which all warps read.  Nothing but these residuals joins the warps: with a
 // barrier per tile and the tile fetched as one the step took 158 us at 2^18 x 2048, with the residuals by a warp of
-// their own 132 us, with every warp its own fetches 111 us (5.0 TB/s).  What is left to the floor is the
+// their own 132 us, with every warp its own fetches 111 us, now 113 us (4.9 TB/s).  What is left to the floor is the
 // latency of a tile: two of the three that fit are in use, and the third arrives while they are worked on.  Up to 1024
 // columns shared memory holds several CTAs, which fill each other's gaps (2^18 x 1024: 113 us with one, 65 us; 2^19 x 512:
-// 198, 67 us).  Below some 10^4 rows the step is two launches and one trip to memory, 8 us.
+// 198, 69 us).  Above 2048 columns a tile has 16 rows, and what is done once per tile is done twice as often: 2^17 x 4096, the
+// same bytes but for the exponents, takes 172 us (3.2 TB/s).  Below some 10^4 rows the step is two launches and one trip to memory, 8.5 us.
 // Tiles are dealt in a fixed pattern and all sums have a fixed order: a step is reproducible bit for bit.
 #include <cuda.h>
 #include <math.h>
@@ -102,32 +107,38 @@ __device__ __forceinline__ void load_exponents(uint32_t (&x)[N / 4], uint32_t ad
     if constexpr (N == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x[0]) : "r"(addr));
     else asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(addr));
 }
-// three balanced digits of a 24-bit integer: v = 256^2 d0 + 256 d1 + d2, as the bytes 2, 1, 0
-__device__ __forceinline__ uint32_t digits(int v) { return ((uint32_t)v + 0x808080u) ^ 0x808080u; }
-
-// Digits of number i of K (16 or 32) where the lanes of a product want them: plane p (d0, d1, d2), then of 32 numbers for each t
-// of 4 the numbers 4 t .. 4 t + 3 and 16 + 4 t .. + 3, of 16 numbers one after the other.  3 K bytes.
-template <int K>
-__device__ __forceinline__ void put_digits(uint32_t dst, uint32_t u, int i)
+// A number in units of its group as six balanced digits of a byte: x = 256^2 d0 + 256 d1 + d2 + 2^-23 (256^2 d3 + 256 d4 + d5),
+// |x| <= 8355711.  hi is x rounded to the unit, lo the rest of it in units of 2^-23, so |lo| <= 2^22; both are exact, and so is
+// every number of fp32 down to 2^-22 of the largest that the group can hold.  The digits stand in the order d0 .. d5, 0, 0.
+__device__ __forceinline__ uint32_t digits(int v) { return ((uint32_t)v + 0x808080u) ^ 0x808080u; }      // bytes 2, 1, 0
+__device__ __forceinline__ uint2 six_digits(int hi, int lo)
 {
-    const uint32_t at = dst + (uint32_t)(K == 32 ? ((i & 15) >> 2) * 8 + (i >> 4) * 4 + (i & 3) : i);
-    asm volatile("st.shared.u8 [%0], %1;\n\tst.shared.u8 [%0 + %4], %2;\n\tst.shared.u8 [%0 + %5], %3;" ::"r"(at), "r"(u >> 16),
-                 "r"(u >> 8), "r"(u), "n"(K), "n"(2 * K)
+    const uint32_t h = digits(hi), l = digits(lo);
+    return make_uint2(__byte_perm(h, l, 0x6012), __byte_perm(l, 0u, 0x4401));
+}
+// An operand of the products is put together in shared memory: a row of 16 bytes for each number of the contraction, the digits
+// of two groups side by side.  Read transposed, eight of the columns are then a product's second operand: column n is digit n,
+// the seventh and eighth are zero.
+__device__ __forceinline__ void put_digits(uint32_t row, uint2 a, uint2 b)
+{
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(row), "r"(a.x), "r"(a.y), "r"(b.x), "r"(b.y) : "memory");
+}
+__device__ __forceinline__ void put_digits(uint32_t half_row, uint2 a)
+{
+    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(half_row), "r"(a.x), "r"(a.y) : "memory");
+}
+// 32 numbers of two groups; row: that of number `lane`
+__device__ __forceinline__ void get_digits(uint32_t row, uint2 &a, uint2 &b)
+{
+    asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(a.x), "=r"(b.x), "=r"(a.y), "=r"(b.y)
+                 : "r"(row)
                  : "memory");
 }
-// The second operand of a product: column n is plane n, and the columns from the fourth on are zero (lanes that stand for
-// them read a place that holds zeros).
-__device__ __forceinline__ uint2 get_digits(uint32_t addr)
+// 16 numbers of two groups; row: that of number `lane` % 16
+__device__ __forceinline__ void get_digits_k16(uint32_t row, uint32_t &a, uint32_t &b)
 {
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint32_t get_digits_k16(uint32_t addr)
-{
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-    return v;
+    asm volatile("ldmatrix.sync.aligned.m16n16.x1.trans.shared.b8 {%0,%1}, [%2];" : "=r"(a), "=r"(b) : "r"(row) : "memory");
 }
 
 __device__ __forceinline__ void mma_s8(int (&c)[4], const uint32_t (&a)[4], uint2 b)      // c = A (16 x 32) B (32 x 8)
@@ -143,12 +154,14 @@ __device__ __forceinline__ void mma_s8_k16(int (&c)[4], uint32_t a0, uint32_t a1
                  : "r"(a0), "r"(a1), "r"(b), "r"(0));
 }
 
-// Residuals of a tile relative to the largest of them (its bits): |v| < 2^22 units of 2^E
+// Scaled residuals of a tile relative to the largest of them (its bits): less than 2^22 units of 2^E
 __device__ __forceinline__ int residual_exponent(uint32_t top) { return max((int)(top >> 23), 27) - 148; }
-// v 2^-E + 1.5 2^23 rounds to the unit; the integer stands in the low bits of the sum
-__device__ __forceinline__ int residual_integer(float v, int E)
+// v 2^-E + 1.5 2^23 rounds to the unit, and the integer stands in the low bits of the sum; the rest is exact
+__device__ __forceinline__ uint2 residual_digits(float v, int E)
 {
-    return (int)(__float_as_uint(fmaf(v, __int_as_float((127 - E) << 23), 12582912.f)) - 0x4b400000u);
+    const float scale = __int_as_float((127 - E) << 23), t = fmaf(v, scale, 12582912.f);
+    const float rest = fmaf(v, scale, 12582912.f - t);
+    return six_digits((int)(__float_as_uint(t) - 0x4b400000u), (int)(__float_as_uint(fmaf(rest, 8388608.f, 12582912.f)) - 0x4b400000u));
 }
 
 // A tile in shared memory: boxes of 128 bytes x T rows, one after the other; inside, 16-byte units are swizzled.
@@ -174,15 +187,14 @@ __device__ __forceinline__ uint32_t exponent_at(int width, int r, int b)
 template <int NB, int T, int W>
 struct Fit8 {
     static constexpr int kThreads = (W + 1) * 32;
-    static constexpr int kDig = 2;                         // blocks whose residuals a warp splits at a time
-    // shared memory behind the ring: digits of the weights, of the scaled residuals, units of the weights, parts of the
-    // dot products, residuals, zeros, barriers (a warp's columns of a tile there, exponents there, exponents done with, dot
-    // products there, residuals there)
-    static constexpr int kWdig = 0, kRdig = kWdig + W * NB * 96, kUnit = kRdig + W * kDig * 3 * T, kZpart = kUnit + W * NB * 4;
-    static constexpr int kResidual = kZpart + 2 * W * T * 4, kZeros = kResidual + 2 * 32 * 4, kBars = kZeros + 16;
+    // shared memory behind the ring: digits of numbers that a warp puts into operands, two blocks' at a time; units of the
+    // weights, parts of the dot products, residuals, barriers (a warp's columns of a tile there, exponents there, exponents
+    // done with, dot products there, residuals there)
+    static constexpr int kDigits = 0, kDigitBytes = 32 * 16, kUnit = kDigits + W * kDigitBytes, kZpart = kUnit + W * NB * 4;
+    static constexpr int kResidual = kZpart + 2 * W * T * 4, kBars = kResidual + 2 * 32 * 4;
     static constexpr int kBytes = kBars + (kMaxTiles * W + 4 * kMaxTiles + 4) * 8;
     static constexpr int kBoxes = NB / 4;      // a warp's columns are as many boxes
-    static_assert(NB % 4 == 0 && kUnit % 16 == 0 && kZeros % 16 == 0 && kBars % 8 == 0, "alignment");
+    static_assert(NB % 4 == 0 && kDigits % 16 == 0 && kUnit % 4 == 0 && kBars % 8 == 0, "alignment");
 };
 
 template <int NB, int T, int W, int C>
@@ -190,7 +202,7 @@ __global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainPara
                                                                      const __grid_constant__ CUtensorMap emap, int ring_tiles)
 {
     using F = Fit8<NB, T, W>;
-    constexpr int kRowGroups = T / 16, kDig = F::kDig, kWords = NB / 4;
+    constexpr int kRowGroups = T / 16, kWords = NB / 4;
     extern __shared__ __align__(1024) unsigned char smem[];        // the ring comes first: swizzled boxes repeat every 1024 bytes
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int d = prm.d, blocks = (d + 31) / 32, workers = (blocks + NB - 1) / NB;
@@ -198,11 +210,9 @@ __global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainPara
     const int ring_exps = 2 * ring_tiles;
     const uint32_t ring = fit_addr(smem), exps = ring + (uint32_t)(ring_tiles * tile_bytes);
     unsigned char *tables = smem + ring_tiles * tile_bytes + ring_exps * exp_bytes;
-    const uint32_t wdig = fit_addr(tables + F::kWdig);
     float *unit = reinterpret_cast<float *>(tables + F::kUnit);
     float(*zpart)[W][T] = reinterpret_cast<float(*)[W][T]>(tables + F::kZpart);
     float(*residual)[32] = reinterpret_cast<float(*)[32]>(tables + F::kResidual);
-    uint32_t *zeros = reinterpret_cast<uint32_t *>(tables + F::kZeros);
     uint64_t *there = reinterpret_cast<uint64_t *>(tables + F::kBars), *ethere = there + kMaxTiles * W, *edone = ethere + 2 * kMaxTiles;
     uint64_t *dots = edone + 2 * kMaxTiles, *resid = dots + 2;
     pdl_trigger();
@@ -213,7 +223,6 @@ __global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainPara
     const int n = (int)blockIdx.x < all ? (all - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
     const int row_step = (int)gridDim.x * T;
     float *out = prm.part + (int64_t)blockIdx.x * (d + 2);
-    if (tid < 4) zeros[tid] = 0u;
     bool ok = true;
     const bool feed = !(prm.test_flags & TRAIN_TEST_NO_FETCH);
     int row0 = (int)blockIdx.x * T, asked = 0;             // first row of the tile at hand; tiles asked for
@@ -317,34 +326,40 @@ __global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainPara
     }
     asked = min(ring_tiles, n);
 
-    for (int b = warp; b < W * NB; b += W) {
-        const int c = b * 32 + lane;
-        const float w = c < d ? prm.theta[c] : 0.f;
-        const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(w) & 0x7fffffffu);
-        // unit 2^E with |w| <= 8355711 units (three digits reach that); weights below 2^-100 count as zero
-        int E = max((int)(top >> 23) - 127, -100) - 22;
-        if (rintf(ldexpf(__uint_as_float(top), -E)) > 8355711.f) ++E;
-        const bool finite = top < 0x7f800000u;             // a weight that is not finite shows in every sum
-        put_digits<32>(wdig + (uint32_t)(b * 96), finite ? digits(__float2int_rn(ldexpf(w, -E))) : 0u, lane);
-        if (lane == 0) unit[b] = finite ? ldexpf(1.f, E) : __int_as_float(0x7fc00000);
+    // This warp's weights, block by block, as operands in registers.
+    const uint32_t dig = fit_addr(tables + F::kDigits) + (uint32_t)(warp * F::kDigitBytes), dig_row = dig + (uint32_t)(lane * 16);
+    uint2 wdig[NB];
+#pragma unroll
+    for (int i = 0; i < NB; i += 2) {
+        uint2 two[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int b = b0 + i + k, c = b * 32 + lane;
+            const float w = c < d ? prm.theta[c] : 0.f;
+            const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(w) & 0x7fffffffu);
+            // unit 2^E with |w| <= 8355711 units (three digits reach that), at least 2^-122
+            int E = max((int)(top >> 23) - 127, -100) - 22;
+            if (rintf(ldexpf(__uint_as_float(top), -E)) > 8355711.f) ++E;
+            const bool finite = top < 0x7f800000u;         // a weight that is not finite shows in every sum
+            const float x = finite ? ldexpf(w, -E) : 0.f, hi = rintf(x);
+            two[k] = six_digits(__float2int_rn(hi), __float2int_rn((x - hi) * 8388608.f));
+            if (lane == 0) unit[b] = finite ? ldexpf(1.f, E) : __int_as_float(0x7fc00000);
+        }
+        __syncwarp();                          // what stood there is read
+        put_digits(dig_row, two[0], two[1]);
+        __syncwarp();
+        get_digits(dig_row, wdig[i], wdig[i + 1]);
     }
 
-    // A lane's part of a product's result: columns 2 (lane % 4) and + 1, hence d0 and d1, or d2 and 0, or nothing.  The
-    // integers 256 d0 + d1 and d2 are added up apart and weighted at the very end.
-    const int m0 = (lane & 3) == 0 ? 256 : 1;
-    const float weight = (lane & 3) == 0 ? 256.f : 1.f;
-    // where the second operand stands, block by block
-    const bool holds = lane < 12;
-    const uint32_t dig_lane = (uint32_t)((lane >> 2) * 32 + (lane & 3) * 8), dig_step = holds ? 96u : 0u;
+    // A lane's part of a product's result: columns 2 (lane % 4) and + 1, hence d0 and d1, d2 and d3, d4 and d5, or nothing.
+    // The integers 256 d0 + d1, 128 d2 + d3 and 256 d4 + d5 are added up apart and weighted at the very end.
+    const int m0 = (lane & 3) == 1 ? 128 : 256;
+    const float weight = (lane & 3) == 0 ? 256.f : (lane & 3) == 1 ? 1.f / 128.f : (lane & 3) == 2 ? 1.f / 8388608.f : 0.f;
     // blocks b0 .. b0 + NB - 1 are this warp's: dot products by 16 rows at a time, columns with a row per lane
     const uint32_t a1 = tile_at<T>((lane & 7) + ((lane >> 3) & 1) * 8, b0 * 32 + (lane >> 4) * 16);      // ldmatrix of 16 x 32
     const uint32_t e1 = exponent_at(ewidth, lane >> 2, b0);         // rows lane / 4 and, 8 * ewidth on, + 8
-    const uint32_t d1 = holds ? wdig + (uint32_t)(b0 * 96) + dig_lane : fit_addr(zeros);
     const int my_row = lane & (T - 1);
     const uint32_t a2 = tile_at<T>(my_row, b0 * 32), e2 = exponent_at(ewidth, my_row, b0);
-    const uint32_t rdig = fit_addr(tables + F::kRdig) + (uint32_t)(warp * kDig * 3 * T);
-    const uint32_t d2 = holds ? rdig + (T == 32 ? dig_lane : (uint32_t)((lane >> 2) * 16 + (lane & 3) * 4)) : fit_addr(zeros);
-    const uint32_t d2_step = holds ? 3u * T : 0u;
     float grad[NB][4];
 #pragma unroll
     for (int i = 0; i < NB; ++i)
@@ -375,7 +390,6 @@ __global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainPara
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
                 if (i < nb) {
-                    const uint2 bd = get_digits(d1 + (uint32_t)i * dig_step);
                     const float u = unit[b0 + i];
 #pragma unroll
                     for (int g = 0; g < kRowGroups; ++g) {
@@ -384,7 +398,7 @@ __global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainPara
                                      : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3])
                                      : "r"(unit_at(now + a1 + (uint32_t)(g * 2048 + (i / 4) * (T * 128)), 2 * (i & 3))));
                         int c[4];
-                        mma_s8(c, a, bd);
+                        mma_s8(c, a, wdig[i]);
                         z[2 * g] = fmaf((float)(c[0] * m0 + c[1]) * u, block_scale(x1[2 * g][i / 4], i & 3), z[2 * g]);
                         z[2 * g + 1] = fmaf((float)(c[2] * m0 + c[3]) * u, block_scale(x1[2 * g + 1][i / 4], i & 3), z[2 * g + 1]);
                     }
@@ -394,6 +408,7 @@ __global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainPara
             for (int g = 0; g < 2 * kRowGroups; ++g) {
                 z[g] *= weight;
                 z[g] += __shfl_xor_sync(0xffffffffu, z[g], 1);
+                z[g] += __shfl_xor_sync(0xffffffffu, z[g], 2);
                 if ((lane & 3) == 0) zpart[k & 1][warp][g * 8 + (lane >> 2)] = z[g];
             }
             fit_arrive(&dots[k & 1], lane);
@@ -411,35 +426,38 @@ __global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainPara
 #pragma unroll
                 for (int w = 0; w < kWords; ++w) x[w] >>= (lane >> 4) * 8;
 #pragma unroll
-            for (int i0 = 0; i0 < NB; i0 += kDig) {
-                float scale[kDig];
+            for (int i0 = 0; i0 < NB; i0 += 2) {
+                float scale[2];
+                uint2 bd[2];
                 __syncwarp();                      // the digits that stood there are read
                 // a row that does not exist has r = 0, a block that does not exist is not read below
                 if constexpr (T == 32) {
+                    uint2 two[2];
 #pragma unroll
-                    for (int i = 0; i < kDig; ++i) {
+                    for (int i = 0; i < 2; ++i) {
                         const float v = r != 0.f ? r * block_scale(x[(i0 + i) / 4], (i0 + i) & 3) : 0.f;
                         const int E = residual_exponent(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu));
-                        put_digits<T>(rdig + (uint32_t)(i * 3 * T), digits(residual_integer(v, E)), lane);
+                        two[i] = residual_digits(v, E);
                         scale[i] = __int_as_float((E + 127) << 23) * show;
                     }
+                    put_digits(dig_row, two[0], two[1]);
+                    __syncwarp();
+                    get_digits(dig_row, bd[0], bd[1]);
                 } else {
                     // 16 rows: two blocks at a time, one by each half of the warp
                     const float v = r != 0.f ? r * block_scale(x[i0 / 4], i0 & 3) : 0.f;
                     const uint32_t size = __float_as_uint(v) & 0x7fffffffu;
                     const int Ea = residual_exponent(__reduce_max_sync(0xffffffffu, lane < 16 ? size : 0u));
                     const int Eb = residual_exponent(__reduce_max_sync(0xffffffffu, lane < 16 ? 0u : size));
-                    put_digits<T>(rdig + (uint32_t)((lane >> 4) * 3 * T), digits(residual_integer(v, lane < 16 ? Ea : Eb)), lane & 15);
                     scale[0] = __int_as_float((Ea + 127) << 23) * show;
                     scale[1] = __int_as_float((Eb + 127) << 23) * show;
+                    put_digits(dig + (uint32_t)((lane & 15) * 16 + (lane >> 4) * 8), residual_digits(v, lane < 16 ? Ea : Eb));
+                    __syncwarp();
+                    get_digits_k16(dig + (uint32_t)((lane & 15) * 16), bd[0].x, bd[1].x);
                 }
-                __syncwarp();
 #pragma unroll
-                for (int i = 0; i < kDig; ++i) {
+                for (int i = 0; i < 2; ++i) {
                     if (i0 + i < nb) {
-                        uint2 bd;
-                        if constexpr (T == 32) bd = get_digits(d2 + (uint32_t)i * d2_step);
-                        else bd.x = get_digits_k16(d2 + (uint32_t)i * d2_step);
                         float *g = grad[i0 + i];
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
@@ -451,13 +469,13 @@ __global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainPara
                                 asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];"
                                              : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3])
                                              : "r"(at));
-                                mma_s8(c, a, bd);
+                                mma_s8(c, a, bd[i]);
                             } else {
                                 uint32_t a0, a4;
                                 asm volatile("ldmatrix.sync.aligned.m16n16.x1.trans.shared.b8 {%0,%1}, [%2];"
                                              : "=r"(a0), "=r"(a4)
                                              : "r"(at));
-                                mma_s8_k16(c, a0, a4, bd.x);
+                                mma_s8_k16(c, a0, a4, bd[i].x);
                             }
                             g[2 * h] = fmaf((float)(c[0] * m0 + c[1]), scale[i], g[2 * h]);
                             g[2 * h + 1] = fmaf((float)(c[2] * m0 + c[3]), scale[i], g[2 * h + 1]);
@@ -498,7 +516,9 @@ __global__ void __launch_bounds__((W + 1) * 32, C) train8_kernel(const TrainPara
     for (int i = 0; i < NB; ++i) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float g = grad[i][e] * weight, s = g + __shfl_xor_sync(0xffffffffu, g, 1);
+            float s = grad[i][e] * weight;
+            s += __shfl_xor_sync(0xffffffffu, s, 1);
+            s += __shfl_xor_sync(0xffffffffu, s, 2);
             const int c = (warp * NB + i) * 32 + (e >> 1) * 16 + (e & 1) * 8 + (lane >> 2);
             if ((lane & 3) == 0 && c < d) out[c] = s;
         }

@@ -366,3 +366,61 @@ def test_all_of_the_extremes_come_back(spr):
         assert np.array_equal(packed.cpu().numpy(), want)
         for ty in (torch.float32, torch.bfloat16):
             assert np.array_equal(spr.hidden_unpack8(packed, 64, ty).cpu().double().numpy(), unpack_ref(want, 64), equal_nan=True)
+
+
+@pytest.mark.parametrize("factor", [10, 14, 18], ids=lambda f: f"2^{f}")
+@pytest.mark.parametrize("N,d", [(96, 64), (130, 512), (96, 528), (200, 1040), (70, 2048), (100, 2064)])
+def test_one_column_far_above_the_rest_costs_the_others_nothing(spr, N, d, factor):
+    """In every sixteenth row one column is 2^factor times the others, as some channels of a model's states are, and those
+    rows' residuals are near 1 while most others' are small.  The block's other bytes are zero in those rows, so the large
+    numbers have no part in the other columns, and each column is held to its own terms:
+      r      a logit's terms are added up in fp32 in runs of at most 8 blocks and 16 parts: off by dz = 30 2^-24 sum_j |s_ij w_j|,
+             so r by dz / 4 and two roundings of its own
+      r 2^e  in 46 bits relative to the largest of a tile: 2^-46 max_i 2^e_i |q_ij|
+      sums   a rounding for each of at most two tiles and four more, 6 2^-24 of sum_i |r_i s_ij|
+    m = 0.1 grad, rounded once more."""
+    g = torch.Generator().manual_seed(N + d + factor)
+    hot, col = torch.arange(3, N, 16), d // 2 + 5
+    S = torch.randn((N, d), generator=g)
+    w = 4.0 * torch.randn(d + 1, generator=g) / d ** 0.5
+    S[hot, col] = 2.0 ** factor * (1 + torch.rand(len(hot), generator=g))
+    w[col] = 2.0 ** -factor
+    packed = spr.hidden_pack8(S.to(torch.bfloat16).cuda())
+    X = torch.from_numpy(unpack_ref(packed.cpu().numpy(), d))
+    z = X @ w[:d].double() + w[d].double()
+    y = z > 0
+    y[hot] = ~y[hot]
+    r = torch.sigmoid(z) - y.double()
+    ws = step_ws(spr, d)
+    state = [w.cuda(), torch.zeros(d + 1, device="cuda"), torch.zeros(d + 1, device="cuda")]
+    spr.verifier_train_step8(packed, d, y.to(torch.uint8).cuda(), *state, 1, 0.01, ws)
+    assert ws.device_status() == 0
+    u, A = 2.0 ** -24, X.abs()
+    dz = 30 * u * (A @ w[:d].abs().double() + w[d].abs().double())
+    dr = dz / 4 + 2 * u
+    e = packed.cpu().view(torch.int8)[:, d:d + (d + 31) // 32].double().repeat_interleave(32, 1)[:, :d]
+    q = packed.cpu().view(torch.int8)[:, :d].double().abs()
+    tol = (A * dr[:, None]).mean(0) + 2.0 ** -46 * torch.exp2(e).amax(0) * q.mean(0) + 7 * u * (A * r.abs()[:, None]).mean(0)
+    off = (state[1][:d].cpu().double() - 0.1 * (X * r[:, None]).mean(0)).abs()
+    assert bool((off <= 0.1 * tol + 1e-45).all()), float((off / (0.1 * tol + 1e-45)).max())
+
+
+@pytest.mark.parametrize("factor", [10, 16, 24], ids=lambda f: f"2^{f}")
+@pytest.mark.parametrize("d", [64, 512, 1040, 2064])
+def test_one_weight_far_above_the_rest_costs_the_others_nothing(spr, d, factor):
+    """A weight 2^factor times the others of its block, in a column where the state is zero: the logit, seen through the loss
+    of a single row (1 at most per unit of it), keeps what fp32 products keep: 30 2^-24 of its terms, and the weights
+    46 bits relative to the largest, 2^-46 2^factor sum_j |s_j|, beside four roundings of the loss."""
+    g = torch.Generator().manual_seed(d + factor)
+    for _ in range(8):
+        w = torch.randn(d + 1, generator=g) / d ** 0.5
+        s = torch.randn((1, d), generator=g)
+        w[d // 2 + 3], s[0, d // 2 + 3] = 2.0 ** factor, 0.0
+        packed = spr.hidden_pack8(s.to(torch.bfloat16).cuda())
+        x = torch.from_numpy(unpack_ref(packed.cpu().numpy(), d))[0]
+        z = float(x @ w[:d].double() + w[d].double())
+        state = [w.cuda(), torch.zeros(d + 1, device="cuda"), torch.zeros(d + 1, device="cuda")]
+        loss = float(spr.verifier_train_step8(packed, d, torch.ones(1, dtype=torch.uint8).cuda(), *state, 1, 0.01, step_ws(spr, d)))
+        want = np.log1p(np.exp(-z))
+        terms = float((x * w[:d].double()).abs().sum() + w[d].double().abs())
+        assert abs(loss - want) <= 30 * 2.0 ** -24 * terms + 2.0 ** (factor - 46) * float(x.abs().sum()) + 4 * 2.0 ** -24 * want
