@@ -390,7 +390,7 @@ int hidden_unpack8(const void *packed, int64_t N, int d, int dt, void *hidden, v
  * rows stand for (hidden_pack8), read once: 1.03 d bytes per sample.  The hyper-parameters are
  * doubles: 1 - beta2 would lose 1e-5 of itself if 0.999 were rounded to float.  Weights are held to 2^-46 of the
  * largest of their block of 32, residuals times 2^e to 2^-46 of the largest of a block's 32 rows; sums are fp32 and
- * wider.  packed: 16-byte aligned; d a
+ * wider.  N = 0 takes no step and makes *loss NaN.  packed: 16-byte aligned; d a
  * multiple of 16 and at most 4096, N at most 0x7fff0000 (otherwise SPR_ERR_UNSUPPORTED).
  * Workspace: spr_workspace_bytes(SPR_OP_VERIFIER_TRAIN8, 0, 0, 0, d, 0, SPR_F32 or SPR_BF16).
  */

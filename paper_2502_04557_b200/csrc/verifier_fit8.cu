@@ -662,7 +662,12 @@ static int train_step8(const void *packed, const uint8_t *labels, int64_t N, int
     if (N < 0 || d <= 0 || t < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) || !(lr == lr))
         return SPR_ERR_INVALID_ARG;
     if (d % 16 != 0 || d > 4096 || N > 0x7fff0000) return SPR_ERR_UNSUPPORTED;      // rows are 32-bit coordinates
-    if (N == 0) return SPR_OK;
+    if (N == 0) {        // no samples: no step, and the mean of nothing is not a number (all bits set)
+        if (!loss) return SPR_OK;
+        if (!aligned(loss, 4)) return SPR_ERR_INVALID_ARG;
+        const int rc = device_supported();
+        return rc != SPR_OK ? rc : finish(cudaMemsetAsync(loss, 0xff, sizeof(float), static_cast<cudaStream_t>(cuda_stream)));
+    }
     if (!packed || !labels || !theta || !adam_m || !adam_v) return SPR_ERR_INVALID_ARG;
     if (!aligned(packed, 16) || !aligned(theta, 4) || !aligned(adam_m, 4) || !aligned(adam_v, 4) || (loss && !aligned(loss, 4)))
         return SPR_ERR_INVALID_ARG;

@@ -424,3 +424,15 @@ def test_one_weight_far_above_the_rest_costs_the_others_nothing(spr, d, factor):
         want = np.log1p(np.exp(-z))
         terms = float((x * w[:d].double()).abs().sum() + w[d].double().abs())
         assert abs(loss - want) <= 30 * 2.0 ** -24 * terms + 2.0 ** (factor - 46) * float(x.abs().sum()) + 4 * 2.0 ** -24 * want
+
+
+def test_a_step_on_no_samples_says_so(spr):
+    """The mean loss of nothing is not a number, and nothing is stepped."""
+    d = 64
+    state = [torch.rand(d + 1, device="cuda") for _ in range(3)]
+    before = [x.clone() for x in state]
+    packed, y = (torch.empty(shape, dtype=torch.uint8, device="cuda") for shape in ((0, spr.pack8_pitch(d)), (0,)))
+    ws = step_ws(spr, d)
+    loss = torch.full((1,), 7.0, device="cuda")
+    assert bool(spr.verifier_train_step8(packed, d, y, *state, 1, 0.01, ws, loss=loss).isnan().all())
+    assert all(torch.equal(a, b) for a, b in zip(state, before)) and ws.device_status() == 0
