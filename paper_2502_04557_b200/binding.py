@@ -559,6 +559,10 @@ def verifier_train_step(hidden, labels, theta, adam_m, adam_v, t: int, lr: float
 # plain integers, and devices are compared by index.
 
 
+_INT_MAX = 0x7fffffff
+_PACK8_MOST = 1 << 20          # elements of a packed row
+
+
 def _on(device: int, dtype, name: str, t: torch.Tensor) -> int:
     """Address of a contiguous tensor of this type on this device."""
     if t.get_device() != device:
@@ -603,7 +607,10 @@ def _head(device, hidden, W, tokens, name="hidden", W_name="W", token_name="targ
     N, d = hidden.shape
     if tokens.numel() != N:
         raise ValueError(f"{token_name} must have one entry per hidden state")
-    return N, d, W.shape[0], h, w, t, dt
+    V = W.shape[0]
+    if N > _INT_MAX or d > _INT_MAX or V > _INT_MAX:      # ctypes would cut them to 32 bits
+        raise ValueError(f"{name} [N,d] and {W_name} [V,d] must have N, d and V below 2^31")
+    return N, d, V, h, w, t, dt
 
 
 def head_loss(hidden, W, targets, ws: Workspace, want_lse: bool = True, out=None):
@@ -676,9 +683,18 @@ def pack8_pitch(d: int) -> int:
 
 def _packed(device: int, packed, d: int):
     p = _on(device, torch.uint8, "packed", packed)
+    if d > _PACK8_MOST:
+        raise ValueError(f"packed rows have at most 2^20 elements, got {d}")
     if d <= 0 or packed.dim() != 2 or packed.shape[1] != (d + (d + 31) // 32 + 15) // 16 * 16:
         raise ValueError(f"packed must be [N, {pack8_pitch(d)}] for d = {d}, got {tuple(packed.shape)}")
     return packed.shape[0], p
+
+
+def _rows(hidden):
+    N, d = hidden.shape
+    if d > _PACK8_MOST:            # ctypes would cut it to 32 bits
+        raise ValueError(f"packed rows have at most 2^20 elements, got {d}")
+    return N, d
 
 
 def hidden_pack8(hidden, out=None):
@@ -686,7 +702,7 @@ def hidden_pack8(hidden, out=None):
     dev = torch.cuda.current_device()
     dt = _dt(hidden)
     h = _on(dev, hidden.dtype, "hidden", hidden)
-    N, d = hidden.shape
+    N, d = _rows(hidden)
     packed, p = _result(dev, out, (N, (d + (d + 31) // 32 + 15) // 16 * 16), torch.uint8, "packed")
     rc = lib().hidden_pack8(h, N, d, dt, p, _raw_stream(dev))
     if rc != 0:

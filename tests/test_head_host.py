@@ -237,3 +237,21 @@ def test_workspace_sizes_do_not_fall_as_tokens_are_added(d, V, dt):
         sizes = [spr.workspace_bytes(op, n, 1, V, d, max(8, d // 2), dt) for n in counts]
         falls = [(n, a, b) for n, a, b in zip(counts[1:], sizes, sizes[1:]) if b < a]
         assert not falls, (op, falls[:3])
+
+
+def test_binding_refuses_sizes_that_do_not_fit_32_bits():
+    """N, d and V travel as 32-bit integers: 2^32 + 3 rows must not be taken for three.  (Tensors without storage.)"""
+    def meta(*shape, dtype=torch.bfloat16):
+        return torch.empty(shape, dtype=dtype, device="meta")
+    big = (1 << 32) + 3
+    for h, W, t in ((meta(big, 8), meta(16, 8), meta(big, dtype=torch.int32)), (meta(3, 8), meta(big, 8), meta(3, dtype=torch.int32)),
+                    (meta(3, big), meta(16, big), meta(3, dtype=torch.int32)), (meta(1 << 31, 8), meta(16, 8), meta(1 << 31, dtype=torch.int32))):
+        with pytest.raises(ValueError, match="below 2\\^31"):
+            binding._head(-1, h, W, t)
+    d = (1 << 32) + 32
+    with pytest.raises(ValueError, match="at most 2\\^20"):
+        binding._packed(-1, meta(2, (d + d // 32 + 15) // 16 * 16, dtype=torch.uint8), d)
+    for d in (d, (1 << 20) + 1):
+        with pytest.raises(ValueError, match="at most 2\\^20"):
+            binding._rows(meta(2, d))
+    assert binding._rows(meta(2, 1 << 20)) == (2, 1 << 20) and binding._head(-1, meta(3, 8), meta(16, 8), meta(3, dtype=torch.int32))[:3] == (3, 8, 16)
