@@ -19,6 +19,7 @@
 // wanted to fp32 - row statistics, and everything with fp32 operands - an accumulator therefore
 // takes only `kc` blocks of 64, and the epilogue warps add such chunks up in registers, rounding
 // to nearest.  They have the time: a chunk is read in about a quarter of the time it takes to form.
+// Results that are rounded to bf16 do so, too, where a contraction is long enough to show (head_loss.cu).
 //
 // fp32 operands: x = x0 + x1 + x2 with bf16 parts (8 significant bits each: the remainder is
 // below 2^-24 |x|).  The six products of parts with i + j <= 2 make the result exact to about
@@ -185,7 +186,9 @@ __device__ __forceinline__ void store_any(T *out, int64_t pitch, const float4 *s
 }
 __device__ __forceinline__ float minus_bf16(float x) { return x - __bfloat162float(__float2bfloat16(x)); }
 
-template <int EPI, typename T>
+// CHUNKED: the whole row's columns in registers, added up over chunks of the contraction; else 32 columns at a time, straight
+// from the one accumulator
+template <int EPI, typename T, bool CHUNKED>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ CUtensorMap map_b0,
             const __grid_constant__ CUtensorMap map_a1, const __grid_constant__ CUtensorMap map_b1,
@@ -330,9 +333,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
         for (int i = 0; i < n_items && ok; ++i) {
             const Item it = get_item(prm, pair, pairs, i);
             const PairJob &j = prm.job[it.job];
-            // kChunked: the whole row's columns in registers, added up over chunks; else 32 columns at a time
-            constexpr bool kChunked = EPI == PAIR_STATS || sizeof(T) == 4;
-            constexpr int kGroups = kChunked ? 4 : 1;
+            constexpr int kGroups = CHUNKED ? 4 : 1;
             float x[kGroups][32];
             const int kbs = item_blocks(j, it.split);
             uint32_t acc = 0;
@@ -343,7 +344,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                 if (!ok) break;
                 fence_after();
                 acc = lane_base + (uint32_t)(buf * kPairTile);
-                if constexpr (kChunked) {
+                if constexpr (CHUNKED) {
                     if (kc == 0) {
 #pragma unroll
                         for (int q = 0; q < 4; ++q) tmem_read32(acc + 32 * q, x[q]);
@@ -367,7 +368,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
             }
             if (!ok) break;
             auto columns = [&](int q) -> float(&)[32] {      // columns 32 q .. of the row
-                if constexpr (kChunked) {
+                if constexpr (CHUNKED) {
                     return x[q];
                 } else {
                     tmem_read32(acc + 32 * q, x[0]);
@@ -394,7 +395,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
             const int width = min(128, j.cols - c0);              // columns that exist (not positive: none)
             if (EPI == PAIR_STATS) {
                 Stats st = {0.f, 0.f};
-                if constexpr (kChunked) st = row_stats(x, width);
+                if constexpr (CHUNKED) st = row_stats(x, width);
                 if (live) j.part[row * (2 * j.tiles_n) + 2 * it.n + half] = make_float2(st.m, st.s);
             } else if (EPI == PAIR_DLOGITS) {
                 // D = g (exp(l - lse) - [v = target]); rows without a target are zero whatever they hold
@@ -509,7 +510,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                     __syncwarp();
                 }
             }
-            if constexpr (!kChunked) {
+            if constexpr (!CHUNKED) {
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive_even(&ctl->acc_empty[(chunk - 1u) & 1u]);
@@ -575,12 +576,12 @@ bool make_map(CUtensorMap *map, const PairOperand &t, int rows)
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int EPI, typename T>
+template <int EPI, typename T, bool CHUNKED>
 cudaError_t launch(const CUtensorMap (&maps)[6], const PairParams &prm, int ctas, int dev, bool behind, cudaStream_t st)
 {
     static std::atomic<bool> attr_set[64];   // host threads may race to set it: all of them store `true`
     if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-        const cudaError_t e = cudaFuncSetAttribute(pair_kernel<EPI, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        const cudaError_t e = cudaFuncSetAttribute(pair_kernel<EPI, T, CHUNKED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                    (int)kPairSmem);
         if (e != cudaSuccess) return e;
         if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
@@ -595,7 +596,7 @@ cudaError_t launch(const CUtensorMap (&maps)[6], const PairParams &prm, int ctas
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = behind ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, pair_kernel<EPI, T>, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], prm);
+    return cudaLaunchKernelEx(&cfg, pair_kernel<EPI, T, CHUNKED>, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], prm);
 }
 
 }  // namespace
@@ -631,6 +632,7 @@ cudaError_t launch_pair(PairEpilogue epi, bool f32, PairParams &prm, int njobs, 
     int pairs = sms / 2 < kMaxPairs ? sms / 2 : kMaxPairs;
     int64_t total = 0;
     double work = 0.0, len[2] = {0.0, 0.0};
+    bool chunked = epi == PAIR_STATS || f32;
     for (int i = 0; i < 2; ++i) {
         prm.items[i] = 0;
         if (i >= njobs) continue;
@@ -639,6 +641,7 @@ cudaError_t launch_pair(PairEpilogue epi, bool f32, PairParams &prm, int njobs, 
         if (n > 0x3fffffff) return cudaErrorInvalidValue;
         prm.items[i] = (int)n;
         total += n;
+        chunked = chunked || j.kc < j.kb_per;
         len[i] = (double)j.nprod * j.kb_per + 2.0;      // in blocks, with about two blocks' time of turn-around
         work += len[i] * (double)n;
     }
@@ -662,11 +665,15 @@ cudaError_t launch_pair(PairEpilogue epi, bool f32, PairParams &prm, int njobs, 
     prm.spin_limit = t_spin_limit ? t_spin_limit : kSpinLimit;
     prm.test_flags = t_test_flags;
     switch (epi) {
-    case PAIR_STATS: return launch<PAIR_STATS, float>(maps, prm, 2 * pairs, dev, behind, st);    // the same for both types
-    case PAIR_DLOGITS: return f32 ? launch<PAIR_DLOGITS, float>(maps, prm, 2 * pairs, dev, behind, st)
-                                  : launch<PAIR_DLOGITS, __nv_bfloat16>(maps, prm, 2 * pairs, dev, behind, st);
-    default: return f32 ? launch<PAIR_OUT, float>(maps, prm, 2 * pairs, dev, behind, st)
-                        : launch<PAIR_OUT, __nv_bfloat16>(maps, prm, 2 * pairs, dev, behind, st);
+    case PAIR_STATS: return launch<PAIR_STATS, float, true>(maps, prm, 2 * pairs, dev, behind, st);      // the same for both types
+    case PAIR_DLOGITS:
+        return f32       ? launch<PAIR_DLOGITS, float, true>(maps, prm, 2 * pairs, dev, behind, st)
+               : chunked ? launch<PAIR_DLOGITS, __nv_bfloat16, true>(maps, prm, 2 * pairs, dev, behind, st)
+                         : launch<PAIR_DLOGITS, __nv_bfloat16, false>(maps, prm, 2 * pairs, dev, behind, st);
+    default:
+        return f32       ? launch<PAIR_OUT, float, true>(maps, prm, 2 * pairs, dev, behind, st)
+               : chunked ? launch<PAIR_OUT, __nv_bfloat16, true>(maps, prm, 2 * pairs, dev, behind, st)
+                         : launch<PAIR_OUT, __nv_bfloat16, false>(maps, prm, 2 * pairs, dev, behind, st);
     }
 }
 

@@ -28,11 +28,14 @@ namespace spr {
 namespace {
 
 constexpr int kHeadMaxLambdas = 8;
-// Blocks of 64 that an accumulator takes (head_gemm.cu): results in bf16 do not show its truncation.  For row statistics
+// Blocks of 64 that an accumulator takes at most (head_gemm.cu): it truncates, up to 2^-23 of the running sum per 16 elements.
+// A sum that is rounded to bf16 (2^-8 at most) may be low by 1/16 of that rounding at the very most, 2^-12: 512 blocks.  (All of
+// a contraction of 2^20 tokens came out 1.4e-3 low.)  A logit behind an exponential counts by its absolute error: 64 blocks leave
+// at most 3e-5 of it, 6e-4 of D for a logit of 20 (65536 columns in one accumulator: 1.8e-3 low).  For row statistics
 // the contraction is cut into chunks of one length, at most 8: what truncation takes off grows with the length (N(0, 9)
 // logits: a log-sum-exp is 2.2e-7 of itself low with 8, 1.2e-7 with 4), and so does the rate (4096x2048x128256: 1570 us
 // with 8, 1728 with 4).
-constexpr int kChunkStats = 8, kChunkStatsLeast = 5, kChunkF32 = 2;
+constexpr int kChunkStats = 8, kChunkStatsLeast = 5, kChunkF32 = 2, kChunkLogits = 64, kChunkOut = 512;
 constexpr size_t kPieceBytes = (size_t)256 << 20;        // D of one vocabulary piece (see pieces())
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -553,12 +556,15 @@ PairOperand packed_operand(const void *base, int64_t rows, int d, int dt)
 }
 PairOperand plain_operand(const void *base, int64_t rows, int d) { return PairOperand{base, rows, d, d}; }
 
-void contraction(PairJob &j, int64_t k, int dt)      // over k elements, in one range
+// over k elements, in ranges of kb_per blocks (0: in one)
+void contraction(PairJob &j, int64_t k, int dt, int kb_per, int most)
 {
-    j.kb = j.kb_per = (int)ceil_div(k, kPairBlockK);
-    j.splits = 1;
+    j.kb = (int)ceil_div(k, kPairBlockK);
+    j.kb_per = kb_per ? kb_per : j.kb;
+    j.splits = (int)ceil_div(j.kb, j.kb_per);
     j.nprod = dt == SPR_F32 ? 6 : 1;
-    j.kc = dt == SPR_F32 ? kChunkF32 : j.kb;
+    // bf16: chunks of one length
+    j.kc = dt == SPR_F32 ? kChunkF32 : (int)ceil_div(j.kb_per, ceil_div(j.kb_per, most));
 }
 
 // job and operands of the row statistics of hidden [N,d] under W [V,d]; packs what has to be packed
@@ -577,8 +583,7 @@ cudaError_t stats_job(PairJob &j, PairOperand &a, PairOperand &b, const void *hi
         b = plain_operand(W, V, d);
     }
     memset(&j, 0, sizeof j);
-    contraction(j, d, dt);
-    if (dt != SPR_F32) j.kc = (int)ceil_div(j.kb, ceil_div(j.kb, kChunkStats));
+    contraction(j, d, dt, 0, kChunkStats);
     j.tiles_m = (int)ceil_div(N, kPairTile);
     j.tiles_n = (int)ceil_div(V, kPairTile);
     j.a_seg = j.b_seg = (int)round_up(d, 64);
@@ -828,7 +833,7 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
         memset(&prm, 0, sizeof prm);
         prm.status = at<int>(ws, 0);
         PairJob &j = prm.job[0];
-        contraction(j, d, dt);
+        contraction(j, d, dt, 0, kChunkLogits);
         j.tiles_m = (int)ceil_div(N, kPairTile);
         j.tiles_n = (int)ceil_div(width, kPairTile);
         j.a_seg = j.b_seg = dp;
@@ -852,10 +857,8 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
         int jobs = 0;
         if (d_hidden) {           // dH [N, d] += D [N, width] W [width, d]
             PairJob &h = prm.job[jobs];
-            contraction(h, width, dt);
+            contraction(h, width, dt, pc.kb_per, kChunkOut);
             if (dparts == 2) h.nprod = 2;
-            h.kb_per = pc.kb_per;
-            h.splits = (int)ceil_div(h.kb, h.kb_per);
             h.tiles_m = (int)ceil_div(N, kPairTile);
             h.tiles_n = (int)ceil_div(d, kPairTile);
             h.b_across = 1;
@@ -879,7 +882,7 @@ int head_loss_grad(const void *hidden, const void *W, const int32_t *targets, co
         }
         if (d_W) {                // dW [width, d] = D^T [width, N] H [N, d]
             PairJob &w = prm.job[jobs];
-            contraction(w, N, dt);
+            contraction(w, N, dt, 0, kChunkOut);
             if (dparts == 2) w.nprod = 2;
             w.tiles_m = (int)ceil_div(width, kPairTile);
             w.tiles_n = (int)ceil_div(d, kPairTile);

@@ -606,3 +606,50 @@ def test_a_workspace_made_for_the_largest_batch_serves_smaller_ones(spr, sizes, 
         check_grad(spr, h, w, t, gl, lse, ws=spaces[1])
         _, ratio = spr.verifier_labels_head(h, w, h, w, t.clamp(min=0), [1.0], spaces[2])
         assert bool((ratio == 1).all()) and spaces[2].device_status() == 0
+
+
+def mean_offset(h, w, t, gl, lse, dw):
+    """Mean relative error of the rows of dW from the ninth on, none of which is a target's: sums of one sign."""
+    want = torch.zeros((w.shape[0] - 8, h.shape[1]), dtype=torch.float64, device="cuda")
+    for n in range(0, len(h), 1 << 16):
+        x, z, g = (a[n:n + (1 << 16)].double() for a in (h, lse, gl))
+        want += (torch.exp(x @ w[8:].double().T - z[:, None]) * g[:, None]).T @ x
+    return float((dw[8:].double() / want - 1).mean()), want.numel()
+
+
+def test_a_gradient_over_a_million_tokens_is_not_off_to_one_side(spr):
+    """The tensor pipe truncates what it adds up, by up to 2^-23 of the running sum per 16 tokens and always towards zero: a sum
+    of one sign over 2^20 tokens in one accumulator would come out some 1.4e-3 low.  One takes at most 2^15 of them, which is
+    2^11 2^-23 = 2^-12 at the very most.  Beside it D (a factor of two and more apart from token to token) and the result are
+    rounded to bf16, to either side: the mean of n results is off by less than five deviations, 5 2^-8 / sqrt(3 n)."""
+    N, d, V = 1 << 20, 8, 300
+    g = torch.Generator(device="cuda").manual_seed(1)
+    h = (torch.rand((N, d), generator=g, device="cuda") + 0.5).to(torch.bfloat16)
+    w = (torch.randn((V, d), generator=g, device="cuda") * 0.5).to(torch.bfloat16)
+    t = torch.randint(0, 8, (N,), generator=g, dtype=torch.int32, device="cuda")
+    gl = torch.full((N,), 1.0 / N, device="cuda")
+    _, lse = spr.head_loss(h, w, t, workspace(spr, spr.OP_HEAD_LOSS, N, V, d, torch.bfloat16))
+    ws = workspace(spr, spr.OP_HEAD_LOSS_GRAD, N, V, d, torch.bfloat16)
+    _, dw = spr.head_loss_grad(h, w, t, lse, gl, ws, want_hidden=False)
+    assert ws.device_status() == 0
+    off, n = mean_offset(h, w, t, gl, lse, dw)
+    assert abs(off) <= 2.0 ** -12 + 5 * 2.0 ** -8 / (3 * n) ** 0.5
+
+
+def test_the_gradient_of_wide_states_is_not_off_to_one_side(spr):
+    """Logits of 20 as sums of one sign over 65536 columns: an accumulator takes at most 4096 of them, so a logit is low by at
+    most 2^8 2^-23 of itself, 6.1e-4, and D by as much (in one accumulator: some 1.8e-3; 64 tokens keep D in two parts).
+    The mean of 10^7 results, rounded to bf16 to either side, adds less than 1e-5."""
+    N, d, V = 64, 65536, 200
+    g = torch.Generator(device="cuda").manual_seed(1)
+    h = (torch.rand((N, d), generator=g, device="cuda") + 0.5).to(torch.bfloat16)
+    w = ((torch.rand((V, d), generator=g, device="cuda") + 0.5) * (20.0 / d)).to(torch.bfloat16)
+    t = torch.randint(0, 8, (N,), generator=g, dtype=torch.int32, device="cuda")
+    gl = torch.rand(N, generator=g, device="cuda") + 0.5
+    _, lse = spr.head_loss(h, w, t, workspace(spr, spr.OP_HEAD_LOSS, N, V, d, torch.bfloat16))
+    ws = workspace(spr, spr.OP_HEAD_LOSS_GRAD, N, V, d, torch.bfloat16)
+    _, dw = spr.head_loss_grad(h, w, t, lse, gl, ws, want_hidden=False)
+    assert ws.device_status() == 0
+    logit = float((h.double() @ w.double().T).max())
+    off, _ = mean_offset(h, w, t, gl, lse, dw)
+    assert abs(off) <= logit * 2.0 ** -15 + 1e-5
