@@ -398,12 +398,12 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                 if constexpr (CHUNKED) st = row_stats(x, width);
                 if (live) j.part[row * (2 * j.tiles_n) + 2 * it.n + half] = make_float2(st.m, st.s);
             } else if (EPI == PAIR_DLOGITS) {
-                // D = g (exp(l - lse) - [v = target]); rows without a target are zero whatever they hold
+                // D = g (exp(l - lse) - [v = target]); rows without a target are zero whatever they hold, and so are the
+                // columns behind the last: a part of D is whole tiles wide
                 const int t = live ? j.targets[row] : -1;
                 const bool keep = t >= 0 && t < j.V;
                 const float lse = keep ? j.lse[row] : 0.f, g = keep ? j.grad_loss[row] : 0.f;
                 const int hot = keep ? t - j.v0 - c0 : -1;
-                const int stored = min(128, j.dl_seg - c0);       // the padding up to a multiple of 64 is zeroed
                 const int rows = (int)min((int64_t)32, j.rows - (row - lane)) - (lane >> 3);
                 const int64_t step = 4 * j.dl_pitch;
                 const int seg = j.dl_seg;
@@ -411,7 +411,6 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ 
                 float line[32], rest[32];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    if (32 * q >= stored) break;
                     float(&y)[32] = columns(q);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
