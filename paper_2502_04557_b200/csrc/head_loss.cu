@@ -354,15 +354,16 @@ struct HeadLossWs {
     size_t hidden, W;     // packed operands (0 bytes where the caller's tensors serve)
     size_t part;          // float2 [N, tiles]
 };
-HeadLossWs head_loss_layout(Carver &c, int64_t N, int d, int V, int dt)
+// pair: on CTA pairs whatever the sizes
+HeadLossWs head_loss_layout(Carver &c, int64_t N, int d, int V, int dt, bool pair = false)
 {
     HeadLossWs w;
-    if (small_head(false, N, d, V, dt)) {
+    if (!pair && small_head(false, N, d, V, dt)) {
         w.hidden = w.W = 0;
         w.part = c.take_data(8 * (size_t)N * (size_t)ceil_div(V, kSmallTile));
         return w;
     }
-    if (stream_head(false, N, d, V, dt)) {
+    if (!pair && stream_head(false, N, d, V, dt)) {
         w.hidden = w.W = 0;
         w.part = c.take_data(8 * (size_t)N * (size_t)stream_ctas(false, (int)N, d, V));
         return w;
@@ -505,15 +506,31 @@ Need head_grad_need(int64_t N, int d, int V, int dt)
     return need;
 }
 
+// A ratio is as exact as what truncation takes off both log-sum-exps alike (see verifier_labels_head).  The kernels on the CUDA
+// cores round to nearest: where one model of bf16 would be theirs and the other the tensor pipe's, the pipe takes both.
+// (4 tokens, 20480 and 2048 columns, V = 32000: ratios off by 3.9e-6 on two kernels at 310 us, by 0.8e-6 on one at 293 us, and by as
+// much on two with chunks of two blocks at 505 us.  Two widths that are chunks of their own are left as they are: 2048 and 128
+// columns 1.2e-6, 4096 and 64 1.7e-6.)
+bool both_on_pairs(int64_t N, int dp, int dq, int V, int dt)
+{
+    return dt != SPR_F32 && stream_head(false, N, dp, V, dt) != stream_head(false, N, dq, V, dt);
+}
 struct HeadLabelsWs {
     HeadLossWs p, q;
 };
 HeadLabelsWs head_labels_layout(Carver &c, int64_t N, int dp, int dq, int V, int dt)
 {
+    const bool pair = both_on_pairs(N, dp, dq, V, dt);
     HeadLabelsWs w;
-    w.p = head_loss_layout(c, N, dp, V, dt);
-    w.q = head_loss_layout(c, N, dq, V, dt);
+    w.p = head_loss_layout(c, N, dp, V, dt, pair);
+    w.q = head_loss_layout(c, N, dq, V, dt, pair);
     return w;
+}
+Need head_labels_need(int64_t N, int dp, int dq, int V, int dt)
+{
+    Need need = {0, head_loss_need(N, dp, V, dt).data + head_loss_need(N, dq, V, dt).data};
+    for (int64_t n = 1; n <= N && n <= kStreamTokens; ++n) need.at_least([&](Carver &c) { head_labels_layout(c, n, dp, dq, V, dt); });
+    return need;
 }
 
 // ---------------------------------------------------------------- launches
@@ -721,7 +738,8 @@ size_t head_grad_ws_bytes(int64_t N, int d, int V, int dt)
 size_t head_labels_ws_bytes(int64_t N, int dp, int dq, int V, int dt)
 {
     if (N <= 0 || !head_sizes_ok(N, dp, V) || !head_sizes_ok(N, dq, V)) return 0;
-    return ws_bytes_for(0, head_loss_need(N, dp, V, dt).data + head_loss_need(N, dq, V, dt).data);
+    const Need need = head_labels_need(N, dp, dq, V, dt);
+    return ws_bytes_for(need.tickets, need.data);
 }
 
 }  // namespace spr
@@ -929,11 +947,12 @@ int verifier_labels_head(const void *p_hidden, const void *p_W, int dp, const vo
     HeadRow p = {p_hidden, p_W, at<float2>(ws, lay.p.part), dp, 0}, q = {q_hidden, q_W, at<float2>(ws, lay.q.part), dq, 0};
     cudaError_t e = cudaSuccess;
     int pairs = 0;
+    const bool on_pairs = both_on_pairs(N, dp, dq, V, dt);
     // the longer products first
     for (int i = 0; i < 2 && e == cudaSuccess; ++i) {
         const bool is_p = (i == 0) == (dp >= dq);
         HeadRow &r = is_p ? p : q;
-        if (small_head(false, N, r.d, V, dt) || stream_head(false, N, r.d, V, dt)) {
+        if (!on_pairs && (small_head(false, N, r.d, V, dt) || stream_head(false, N, r.d, V, dt))) {
             e = other_stats(r, N, V, dt, prm.status, st);
         } else {
             e = stats_job(prm.job[pairs], a[pairs], b[pairs], r.hidden, r.W, N, r.d, V, dt, ws, is_p ? lay.p : lay.q, st);

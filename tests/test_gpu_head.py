@@ -653,3 +653,24 @@ def test_the_gradient_of_wide_states_is_not_off_to_one_side(spr):
     logit = float((h.double() @ w.double().T).max())
     off, _ = mean_offset(h, w, t, gl, lse, dw)
     assert abs(off) <= logit * 2.0 ** -15 + 1e-5
+
+
+@pytest.mark.parametrize("p_wide", [True, False], ids=["target", "draft"])
+def test_a_ratio_from_two_kernels_is_as_exact_as_from_one(spr, p_wide):
+    """Four tokens of one model are too wide for the pass over W and take the tensor pipe, which truncates what it adds up; in a
+    ratio to a model that does not, nothing of that cancels.  It is held to what the shortest chunks that are used anywhere,
+    of two blocks, would leave: a truncation takes half a unit on average, at most 2^-24 of the running sum, and there are
+    eight to a chunk, on average of half the chunk's share of a logit: 4 2^-24 of the mean logit under the softmax, beside
+    2^-21 for the roundings of both models' statistics."""
+    N, V, wide, narrow = 4, 32000, 20480, 2048
+    ph, pw, x, _ = problem(N, wide, V, torch.bfloat16, seed=1, ignore=0.0)
+    qh, qw, _, _ = problem(N, narrow, V, torch.bfloat16, seed=2)
+    a = (ph, pw, qh, qw) if p_wide else (qh, qw, ph, pw)
+    ws = workspace(spr, spr.OP_VERIFIER_LABELS_HEAD, N, V, a[0].shape[1], torch.bfloat16, h=a[2].shape[1])
+    _, ratio = spr.verifier_labels_head(*a, x, [1.0], ws)
+    assert ws.device_status() == 0
+    l = [h.double() @ w.double().T for h, w in ((a[0], a[1]), (a[2], a[3]))]
+    p, q = (torch.log_softmax(m, 1).gather(1, x.long()[:, None])[:, 0] for m in l)
+    off = float((ratio.double() / torch.exp(q - p) - 1).mean())
+    logit = max(float((torch.softmax(m, 1) * m).sum(1).mean()) for m in l)
+    assert abs(off) <= 4 * 2.0 ** -24 * logit + 2.0 ** -21
