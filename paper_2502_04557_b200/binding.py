@@ -616,7 +616,8 @@ def _head(device, hidden, W, tokens, name="hidden", W_name="W", token_name="targ
 def head_loss(hidden, W, targets, ws: Workspace, want_lse: bool = True, out=None):
     """Softmax cross entropy of hidden [N,d] under the head W [V,d]; targets i32 [N], negative = padding.
 
-    Returns (loss f32 [N], lse f32 [N] or None); out: the same two tensors."""
+    Returns (loss f32 [N], lse f32 [N] or None); out: the same two tensors.  No autograd graph is recorded, whether or not
+    hidden and W require gradients: those come from head_loss_grad."""
     dev = torch.cuda.current_device()
     N, d, V, h, w, t, dt = _head(dev, hidden, W, targets)
     loss, lse = (None, None) if out is None else out
@@ -633,7 +634,8 @@ def head_loss_grad(hidden, W, targets, lse, grad_loss, ws: Workspace, want_hidde
                    out=None):
     """Gradient of sum(grad_loss * loss) of head_loss; lse as head_loss returned it, grad_loss f32 [N].
 
-    Returns (d_hidden [N,d] or None, d_W [V,d] or None) in the operands' type; out: the same two tensors."""
+    Returns (d_hidden [N,d] or None, d_W [V,d] or None) in the operands' type; out: the same two tensors.  They are returned,
+    not added to hidden.grad and W.grad."""
     dev = torch.cuda.current_device()
     N, d, V, h, w, t, dt = _head(dev, hidden, W, targets)
     z, g = _on(dev, torch.float32, "lse", lse), _on(dev, torch.float32, "grad_loss", grad_loss)
