@@ -35,7 +35,7 @@ constexpr int kHeadMaxLambdas = 8;
 // the contraction is cut into chunks of one length, at most 8: what truncation takes off grows with the length (N(0, 9)
 // logits: a log-sum-exp is 2.2e-7 of itself low with 8, 1.2e-7 with 4), and so does the rate (4096x2048x128256: 1570 us
 // with 8, 1728 with 4).
-constexpr int kChunkStats = 8, kChunkStatsLeast = 5, kChunkF32 = 2, kChunkLogits = 64, kChunkOut = 512;
+constexpr int kChunkStats = 8, kChunkStatsLeast = 2, kChunkF32 = 2, kChunkLogits = 64, kChunkOut = 512;
 constexpr size_t kPieceBytes = (size_t)256 << 20;        // D of one vocabulary piece (see pieces())
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -509,8 +509,7 @@ Need head_grad_need(int64_t N, int d, int V, int dt)
 // A ratio is as exact as what truncation takes off both log-sum-exps alike (see verifier_labels_head).  The kernels on the CUDA
 // cores round to nearest: where one model of bf16 would be theirs and the other the tensor pipe's, the pipe takes both.
 // (4 tokens, 20480 and 2048 columns, V = 32000: ratios off by 3.9e-6 on two kernels at 310 us, by 0.8e-6 on one at 293 us, and by as
-// much on two with chunks of two blocks at 505 us.  Two widths that are chunks of their own are left as they are: 2048 and 128
-// columns 1.2e-6, 4096 and 64 1.7e-6.)
+// much on two with chunks of two blocks at 505 us.)
 bool both_on_pairs(int64_t N, int dp, int dq, int V, int dt)
 {
     return dt != SPR_F32 && stream_head(false, N, dp, V, dt) != stream_head(false, N, dq, V, dt);
@@ -962,7 +961,11 @@ int verifier_labels_head(const void *p_hidden, const void *p_W, int dp, const vo
     }
     if (dt != SPR_F32 && pairs == 2) {
         // Chunks of one length in both products, so that truncation does the same to both log-sum-exps and cancels in the
-        // ratio (768 and 1536 elements: ratios off by 4e-7 instead of 1.3e-6); short ones would slow the longer product down.
+        // ratio (768 and 1536 elements: off by 3e-7, where chunks of their own leave 1.3e-6).  A narrow model's chunk is all of its
+        // blocks, and sets the length for the other down to two: with at least five, 128 and 256 elements were off by
+        // 2.4e-6 instead of 2e-7, 64 and 576 by 4.2e-6 instead of 1.1e-6 (plain fp32: 0.5e-6 and 0.9e-6).  That is 48.7 ->
+        // 52.5 us for the former (1024 tokens, V = 32000), 64 -> 79 us for the latter and 132 -> 170 us for 128 and 2048, whose
+        // ratios were off by 2.9e-6; a single block as the least would take 64 and 2048 from 136 to 268 us.
         int kc = prm.job[0].kc < prm.job[1].kc ? prm.job[0].kc : prm.job[1].kc;
         if (kc < kChunkStatsLeast) kc = kChunkStatsLeast;
         prm.job[0].kc = prm.job[1].kc = kc;

@@ -674,3 +674,24 @@ def test_a_ratio_from_two_kernels_is_as_exact_as_from_one(spr, p_wide):
     off = float((ratio.double() / torch.exp(q - p) - 1).mean())
     logit = max(float((torch.softmax(m, 1) * m).sum(1).mean()) for m in l)
     assert abs(off) <= 4 * 2.0 ** -24 * logit + 2.0 ** -21
+
+
+@pytest.mark.parametrize("dq,dp", [(128, 256), (192, 384), (256, 768), (320, 640), (768, 1536)])
+def test_ratios_of_narrow_models_are_not_off_to_one_side(spr, dq, dp):
+    """Both models' logits are added up in chunks of one length, so what truncation takes off their log-sum-exps is the same and
+    the mean of many ratios shows none of it.  What is left goes either way: a logit is rounded at most twice per model behind
+    its chunks, 2^-24 of itself each (the softmax of logits this far apart is that of the few largest), so a ratio is off by at
+    most 4 2^-24 of the mean logit under the softmax, and the mean of N of them by less than five times that over sqrt(N)."""
+    N, V = 2000, 3000
+    ph, pw, x, _ = problem(N, dp, V, torch.bfloat16, seed=dp, ignore=0.0, scale=8.0)
+    qh, qw, _, _ = problem(N, dq, V, torch.bfloat16, seed=dq + 1, scale=8.0)
+    ws = workspace(spr, spr.OP_VERIFIER_LABELS_HEAD, N, V, dp, torch.bfloat16, h=dq)
+    _, ratio = spr.verifier_labels_head(ph, pw, qh, qw, x, [1.0], ws)
+    assert ws.device_status() == 0
+    l = [h.double() @ w.double().T for h, w in ((ph, pw), (qh, qw))]
+    p, q = (torch.log_softmax(m, 1).gather(1, x.long()[:, None])[:, 0] for m in l)
+    ok = (q - p).abs() < 60                          # a ratio is a float: larger ones are rounded to infinity or nothing
+    off = (ratio.double() / torch.exp(q - p) - 1)[ok]
+    logit = max(float((torch.softmax(m, 1) * m).sum(1).mean()) for m in l)
+    assert int(ok.sum()) > N // 2
+    assert abs(float(off.mean())) <= 5 * 4 * 2.0 ** -24 * logit / float(ok.sum()) ** 0.5
