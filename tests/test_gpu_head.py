@@ -695,3 +695,14 @@ def test_ratios_of_narrow_models_are_not_off_to_one_side(spr, dq, dp):
     logit = max(float((torch.softmax(m, 1) * m).sum(1).mean()) for m in l)
     assert int(ok.sum()) > N // 2
     assert abs(float(off.mean())) <= 5 * 4 * 2.0 ** -24 * logit / float(ok.sum()) ** 0.5
+
+
+@pytest.mark.parametrize("N,d,V", [(40000, 67, 300), (33000, 72, 300), (256, 8192, 70000), (300, 8200, 700), (20, 4200, 3000), (20, 4203, 3000)])
+def test_long_bf16_contractions_in_every_form(spr, N, d, V):
+    """Contractions of more than one chunk: dW over the tokens, stored as boxes or from rows that start anywhere; dH over the
+    vocabulary, in ranges that are added up; logits of wide states, with D in one part and in two."""
+    h, w, t, gl = problem(N, d, V, torch.bfloat16, seed=N + d)
+    _, lse = check_loss(spr, h, w, t)
+    dh, dw = check_grad(spr, h, w, t, gl, lse, d_rounding=2.0 ** -8 if N > 128 else 2.0 ** -16)
+    assert torch.equal(check_grad(spr, h, w, t, gl, lse, want_W=False)[0], dh)
+    assert torch.equal(check_grad(spr, h, w, t, gl, lse, want_hidden=False)[1], dw)
