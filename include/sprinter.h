@@ -57,7 +57,9 @@ typedef enum {
     SPR_ERR_CUDA = 4,        /* a CUDA runtime call failed (see spr_last_cuda_error)          */
     SPR_ERR_TIMEOUT = 5,     /* device: a bounded wait inside a kernel expired                */
     SPR_ERR_BAD_TOKEN = 6,   /* device: draft token id outside [0, V)                         */
-    SPR_ERR_BAD_ROW = 7      /* device: selected logits row outside [0, R)                    */
+    SPR_ERR_BAD_ROW = 7,     /* device: selected logits row outside [0, R)                    */
+    SPR_ERR_BAD_PAGE = 8,    /* device: a cache slot without a page in [0, num_pages)         */
+    SPR_ERR_BAD_TREE = 9     /* device: a node's parent does not come before it               */
 } spr_status;
 
 typedef enum { SPR_F32 = 0, SPR_BF16 = 1 } spr_dtype;
@@ -73,7 +75,10 @@ typedef enum {
     SPR_OP_HEAD_LOSS = 7,
     SPR_OP_HEAD_LOSS_GRAD = 8,
     SPR_OP_VERIFIER_LABELS_HEAD = 10,
-    SPR_OP_VERIFIER_TRAIN8 = 11
+    SPR_OP_VERIFIER_TRAIN8 = 11,
+    SPR_OP_CACHE_APPEND = 12,
+    SPR_OP_TREE_ATTENTION = 13,
+    SPR_OP_LOGITS_RULES = 14
 } spr_op;
 
 /* Which verifier kernel sprinter_verify() uses.  AUTO picks the tensor-core
@@ -88,7 +93,8 @@ typedef enum { SPR_VERIFIER_AUTO = 0, SPR_VERIFIER_SIMT = 1, SPR_VERIFIER_TENSOR
  * SPR_OP_VERIFIER_TRAIN8 use d only; SPR_OP_HEAD_LOSS, SPR_OP_HEAD_LOSS_GRAD and
  * SPR_OP_VERIFIER_LABELS_HEAD are for N = B*K >= 1 hidden states of width d, and
  * SPR_OP_VERIFIER_LABELS_HEAD takes the target's width as d and the draft's as h; what these three get serves every
- * smaller N as well.  Returns 0 for invalid arguments.  A workspace sized for the largest op serves all of them. */
+ * smaller N as well.  SPR_OP_TREE_ATTENTION takes the head dimension as d and nothing else; SPR_OP_CACHE_APPEND and
+ * SPR_OP_LOGITS_RULES need no more than the status word, whatever the sizes.  Returns 0 for invalid arguments.  A workspace sized for the largest op serves all of them. */
 size_t spr_workspace_bytes(int op, int B, int K, int V, int d, int h, int dt);
 
 /* Clears a freshly allocated workspace (enqueues a memset on the stream). */
@@ -402,6 +408,95 @@ int verifier_train_step8(const void *packed, const uint8_t *labels, int64_t N, i
                          void *ws, size_t ws_bytes, void *cuda_stream);
 
 /*
+ * cache_append, tree_attention, logits_rules - the target model's pass over drafted tokens.
+ *
+ * The paper has no counterpart: its single target call (Algorithm 2) and the exact check (Section 2) start from that
+ * pass's logits.  These are the parts of the pass that depend on which tokens were drafted, and they share one
+ * description of them:
+ *
+ *   B sequences have T nodes each, the tokens that the pass works on - for the exact check of K draft
+ *   tokens T = K + 1: the last token before them, then the drafts.
+ *   lens [B] int32        tokens of the sequence in the cache before this pass; negative: the sequence is not used
+ *   counts [B] int32      how many of the T nodes are used (clamped to [0, T]); NULL: all
+ *   parents [B,T] int32   the node that a node follows, an earlier one of the same sequence, or negative: the cached
+ *                         prefix.  NULL: a chain, node i follows node i - 1.  A parent that is not an earlier node
+ *                         counts as negative, SPR_ERR_BAD_TREE.  Trees have at most 256 nodes.
+ *
+ * Node i lies in slot lens[b] + i of its sequence and at position lens[b] + depth (0 for nodes that follow the
+ * prefix).  Slot s is entry s % page_size of page page_table[b, s / page_size]; caches are
+ * [num_pages, Hkv, page_size, D] dt, page_table [B, max_pages] int32.  Pages behind a sequence's last slot are not
+ * looked at.  A slot without a page in [0, num_pages) raises SPR_ERR_BAD_PAGE.
+ *
+ * ----------------------------------------------------------------------------------------------------------------
+ * cache_append - rotates queries and keys by their positions, and puts keys and values into the cache.
+ *
+ * q [B,T,Hq,D], k and v [B,T,Hkv,D] dt; *_stride is the distance from one node to the next in elements (Hq*D or Hkv*D for
+ * dense tensors; larger where one projection gives all three side by side).  The first `rot` elements of each head
+ * (even, 0 <= rot <= D) are rotated in pairs: elements j and j + rot/2, or with interleaved != 0 elements 2j and 2j + 1,
+ * by the angle position * inv_freq[j], inv_freq [rot/2] f32.  Angles are formed in double, rotations in fp32, and results
+ * are rounded once; the rest is copied bit for bit.
+ *   q_out [B,T,Hq,D]: rotated queries, zeros for nodes that are not used.  q and q_out may both be NULL, and q_out may be q
+ *   where q is dense; otherwise nothing may overlap.
+ *   slots [B,T] int32 (optional): the slot to put a node in instead of lens[b] + i, negative: none (its query is rotated
+ *   all the same); positions stay what they are.  After the check of a tree this puts the nodes that were kept at the
+ *   slots behind the prefix: slot = position.  No two nodes may be given one slot.
+ * Entries of the cache that no node is put in are left as they were.  T is not limited for chains: prompts go the
+ * same way.  A node whose slot has no page is put nowhere.  D <= 1024.
+ * Workspace: the status word (spr_workspace_bytes(SPR_OP_CACHE_APPEND, ...)).
+ */
+int cache_append(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                 int B, int T, int Hq, int Hkv, int D, int dt, const int32_t *lens, const int32_t *counts,
+                 const int32_t *parents, const int32_t *slots, const float *inv_freq, int rot, int interleaved,
+                 const int32_t *page_table, int max_pages, int num_pages, int page_size, void *k_cache,
+                 void *v_cache, void *q_out, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * tree_attention - attention of the nodes over the cache that they were appended to.
+ *
+ *   out[b,i,h] = sum_s p_s v_s,  p = softmax over s of scale * q[b,i,h] . k_s,
+ * s running over the slots of the prefix, [0, lens[b]), and those of node i and the nodes before it on its path; head h reads
+ * head h / (Hq / Hkv) of the cache.  T = 1 is ordinary decoding.
+ * q, out [B,T,Hq,D] dt (dense, 16-byte aligned, as are the caches); Hkv divides Hq; D a multiple of 8 up to 128 and
+ * page_size a multiple of 8 (otherwise SPR_ERR_UNSUPPORTED), T <= 256.  Rows of nodes that are not used are zeros.
+ * Scores, maxima and sums are fp32; with bf16 tensors the weights enter the second product as two bf16 numbers.
+ * Keys and values of slots that a row does not see have no part in it, whatever they hold; infinities and NaN in
+ * those that it does see make it infinite or NaN.  A slot without a page is left out (SPR_ERR_BAD_PAGE), and a row
+ * that sees no slot at all is zeros.  After SPR_ERR_TIMEOUT rows whose keys did not arrive are NaN.
+ * Launches do not depend on the lengths: a captured call serves whatever lens, counts, parents and page_table hold
+ * when it is replayed.  Workspace: spr_workspace_bytes(SPR_OP_TREE_ATTENTION, B, T, 1, D, 0, dt).
+ */
+int tree_attention(const void *q, const void *k_cache, const void *v_cache, int B, int T, int Hq, int Hkv, int D, int dt,
+                   const int32_t *lens, const int32_t *counts, const int32_t *parents, const int32_t *page_table,
+                   int max_pages, int num_pages, int page_size, float scale, void *out, void *ws, size_t ws_bytes,
+                   void *cuda_stream);
+
+/*
+ * logits_rules - penalties for repeated tokens, biases and grammar masks on rows of logits.
+ *
+ * Row i of sequence b of logits [B,T,ldv] dt holds what the model says after node i (with the nodes given above, the rows
+ * that sd_verify, replace_sample and verifier_labels read as p_logits; q_logits [B,K,ldv] are those of the first K nodes).
+ * With c_t the number of times that token t stands in history[b, 0 .. history_len[b]) and among the tokens of node i and
+ * the nodes before it on its path:
+ *   l <- (l > 0 ? l / r : l * r) - f * c_t - s   where c_t > 0, (r, f, s) = penalties[b]
+ *   l <- l + bias                                where t is in bias_tokens[b]; the last entry counts if it is there twice
+ *   l <- -inf                                    where bit t % 32 of masks[mask_rows[b,i], t / 32] is 0
+ * in fp32, rounded once; other entries go by bit for bit, and so do rows of nodes that are not used.
+ * history [B,ld_history] int32 with history_len [B] (clamped to [0, ld_history]), tokens [B,T] int32, penalties [B,3] f32 (r > 0):
+ * each optional; without penalties the first two are not looked at.  bias_tokens [B,n_bias] int32, bias_values [B,n_bias] f32,
+ * n_bias <= 1024.
+ * masks [num_masks,ld_mask] (ld_mask >= ceil(V/32)) with mask_rows [B,T] int32, negative: no mask.  Negative entries of
+ * history, tokens and bias_tokens are padding.
+ * out [B,T,ld_out] dt: logits itself (ld_out = ldv), or not overlapping it.  A row whose mask allows nothing is -inf throughout.
+ * Device-detected: history, tokens or bias_tokens >= V are passed over, SPR_ERR_BAD_TOKEN; mask_rows >= num_masks: no mask,
+ * SPR_ERR_BAD_ROW.  T <= 256.  Workspace: the status word.
+ */
+int logits_rules(const void *logits, int64_t ldv, int V, int B, int T, int dt, const int32_t *history,
+                 int64_t ld_history, const int32_t *history_len, const int32_t *tokens, const int32_t *parents,
+                 const int32_t *counts, const float *penalties, const int32_t *bias_tokens, const float *bias_values,
+                 int n_bias, const uint32_t *masks, int64_t ld_mask, int num_masks, const int32_t *mask_rows,
+                 void *out, int64_t ld_out, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
  * sprinter_simulate - run lengths of an i.i.d. verifier (Monte-Carlo of Theorems 2 and 3).
  *
  * Defined by: Section 3.1(b), the scenario of Theorem 2: the draft produces r acceptable
@@ -527,19 +622,21 @@ int spr_test_verifier_train_step(const void *hidden, const uint8_t *labels, int6
                                  void *cuda_stream, int flags, unsigned spin_limit);
 
 /*
- * spr_test_verifier_train_step8, spr_test_pair_kernels - test hooks, not part of the stable interface.
+ * spr_test_verifier_train_step8, spr_test_pair_kernels, spr_test_tree_attention - test hooks, not part of the stable interface.
  *
  * The paper has no counterpart.  The first is verifier_train_step8 with flags and spin_limit as for
  * spr_test_verifier_train_step.  The second makes the head_loss, head_loss_grad and verifier_labels_head
  * calls that this host thread makes afterwards load nothing (flags bit 0), so that the first bounded wait of
  * every CTA pair runs out after spin_limit polls (0 = the library's limit), with the outcome that those calls
  * document for SPR_ERR_TIMEOUT, nothing left in flight and the workspace usable; (0, 0) ends it.
+ * spr_test_tree_attention does the same for tree_attention on bf16 tensors.
  */
 int spr_test_verifier_train_step8(const void *packed, const uint8_t *labels, int64_t N, int d, float *theta,
                                   float *adam_m, float *adam_v, int t, double lr, double beta1, double beta2,
                                   double eps, float *loss, void *ws, size_t ws_bytes, void *cuda_stream, int flags,
                                   unsigned spin_limit);
 void spr_test_pair_kernels(int flags, unsigned spin_limit);
+void spr_test_tree_attention(int flags, unsigned spin_limit);
 
 /* Synchronises the stream, returns the sticky device status word of `ws`
  * (SPR_OK if nothing was detected) and clears it. */

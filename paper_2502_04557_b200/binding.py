@@ -18,6 +18,7 @@ F32, BF16 = 0, 1
 OP_SPRINTER_VERIFY, OP_REPLACE_SAMPLE, OP_SD_VERIFY, OP_SPRINTER_STEP, OP_SD_SHARD = 0, 1, 2, 3, 4
 OP_VERIFIER_LABELS, OP_VERIFIER_TRAIN = 5, 6
 OP_HEAD_LOSS, OP_HEAD_LOSS_GRAD, OP_VERIFIER_LABELS_HEAD, OP_VERIFIER_TRAIN8 = 7, 8, 10, 11
+OP_CACHE_APPEND, OP_TREE_ATTENTION, OP_LOGITS_RULES = 12, 13, 14
 PATH_AUTO, PATH_SIMT, PATH_TENSOR = 0, 1, 2
 
 EXPORTS = [
@@ -29,6 +30,7 @@ EXPORTS = [
     "verifier_labels", "verifier_train_step", "spr_test_sprinter_verify", "spr_test_verifier_train_step",
     "head_loss", "head_loss_grad", "verifier_labels_head", "spr_pack8_pitch", "hidden_pack8", "hidden_unpack8",
     "verifier_train_step8", "spr_test_verifier_train_step8", "spr_test_pair_kernels",
+    "cache_append", "tree_attention", "logits_rules", "spr_test_tree_attention",
 ]
 
 
@@ -114,6 +116,14 @@ def lib():
         L.spr_test_verifier_train_step8.argtypes = L.verifier_train_step8.argtypes + [i32, C.c_uint]
         L.spr_test_pair_kernels.restype = None
         L.spr_test_pair_kernels.argtypes = [i32, C.c_uint]
+        L.cache_append.restype = i32
+        L.cache_append.argtypes = [vp, i64, vp, i64, vp, i64] + [i32] * 6 + [vp] * 5 + [i32, i32, vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.tree_attention.restype = i32
+        L.tree_attention.argtypes = [vp] * 3 + [i32] * 6 + [vp] * 4 + [i32] * 3 + [f32, vp, vp, sz, vp]
+        L.logits_rules.restype = i32
+        L.logits_rules.argtypes = [vp, i64, i32, i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, i32, vp, i64, i32, vp, vp, i64, vp, sz, vp]
+        L.spr_test_tree_attention.restype = None
+        L.spr_test_tree_attention.argtypes = [i32, C.c_uint]
         L.spr_host_arena_bytes.restype = sz
         L.spr_host_arena_bytes.argtypes = [i32, i32, i32, i32, i64, i32, i32, i32]
         L.sprinter_verify_host.restype = i32
@@ -746,6 +756,187 @@ def verifier_train_step8(packed, d: int, labels, theta, adam_m, adam_v, t: int, 
     if rc != 0:
         _check("verifier_train_step8", rc)
     return loss
+
+
+# ---------------------------------------------------------------------------- the target's pass over drafted tokens
+
+
+def _optional(device: int, t, dtype, shape, name: str):
+    """Address of an optional tensor of this shape, or None."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    return _on(device, dtype, name, t)
+
+
+def _nodes(device: int, B: int, T: int, lens, counts, parents):
+    return (_optional(device, lens, torch.int32, (B,), "lens"), _optional(device, counts, torch.int32, (B,), "counts"),
+            _optional(device, parents, torch.int32, (B, T), "parents"))
+
+
+def _caches(device: int, k_cache, v_cache, page_table, dtype, B: int, D: int):
+    """(addresses, Hkv, page_size, num_pages, max_pages) of paged caches [num_pages, Hkv, page_size, D]."""
+    k, v = _on(device, dtype, "k_cache", k_cache), _on(device, dtype, "v_cache", v_cache)
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.shape[3] != D:
+        raise ValueError(f"k_cache and v_cache must be [num_pages, Hkv, page_size, {D}]")
+    table = _on(device, torch.int32, "page_table", page_table)
+    if page_table.dim() != 2 or page_table.shape[0] != B:
+        raise ValueError(f"page_table must be [{B}, max_pages]")
+    num_pages, Hkv, page_size, _ = k_cache.shape
+    if max(num_pages, Hkv, page_size, page_table.shape[1]) > _INT_MAX:
+        raise ValueError("caches and page_table must have sizes below 2^31")
+    return k, v, table, Hkv, page_size, num_pages, page_table.shape[1]
+
+
+def _node_rows(device: int, t, dtype, B: int, T: int, H: int, D: int, name: str):
+    """Address and distance between nodes (in elements) of [B,T,H,D], dense but for that distance: a projection that gives
+    queries, keys and values side by side is read where it is."""
+    if t.get_device() != device:
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a CUDA tensor")
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, the current device is cuda:{device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if tuple(t.shape) != (B, T, H, D):
+        raise ValueError(f"{name} must be {(B, T, H, D)}, got {tuple(t.shape)}")
+    if t.is_contiguous() or t.numel() == 0:
+        return t.data_ptr(), H * D
+    b, n, h, d = t.stride()
+    stride = n if T > 1 else b if B > 1 else H * D
+    if (d != 1 and D > 1) or (h != D and H > 1) or stride < H * D or (T > 1 and B > 1 and b != T * n):
+        raise ValueError(f"{name} must have dense heads and one distance between nodes, got strides {t.stride()}")
+    return t.data_ptr(), stride
+
+
+def cache_append(k, v, k_cache, v_cache, page_table, lens, ws: Workspace, q=None, inv_freq=None, interleaved: bool = False,
+                 counts=None, parents=None, slots=None, q_out=None):
+    """Puts the keys and values k, v [B,T,Hkv,D] of T nodes per sequence into a paged cache, keys (and the queries
+    q [B,T,Hq,D]) rotated by their positions.
+
+    k_cache, v_cache [num_pages,Hkv,page_size,D]; page_table i32 [B,max_pages]; lens i32 [B] tokens in the cache before;
+    inv_freq f32 [rot/2] (None: no rotation); counts i32 [B], parents i32 [B,T] (None: a chain), slots i32 [B,T]: see
+    include/sprinter.h.  q, k, v may be parts of one tensor [B,T,Hq+2*Hkv,D].  Returns q_out, or None without q."""
+    dev = torch.cuda.current_device()
+    dtype, dt = k.dtype, _dt(k)
+    if k.dim() != 4:
+        raise ValueError("k must be [B,T,Hkv,D]")
+    B, T, Hkv, D = k.shape
+    if max(B, T, Hkv, D) > _INT_MAX:
+        raise ValueError("k [B,T,Hkv,D] must have sizes below 2^31")
+    kc, vc, table, heads, page_size, num_pages, max_pages = _caches(dev, k_cache, v_cache, page_table, dtype, B, D)
+    if heads != Hkv:
+        raise ValueError(f"the caches have {heads} heads, k has {Hkv}")
+    ka, ks = _node_rows(dev, k, dtype, B, T, Hkv, D, "k")
+    va, vs = _node_rows(dev, v, dtype, B, T, Hkv, D, "v")
+    qa, qs, Hq, oa = None, 0, 0, None
+    if q is not None:
+        if q.dim() != 4 or q.shape[2] > _INT_MAX:
+            raise ValueError("q must be [B,T,Hq,D]")
+        Hq = q.shape[2]
+        qa, qs = _node_rows(dev, q, dtype, B, T, Hq, D, "q")
+    elif q_out is not None:
+        raise ValueError("q_out needs q")
+    rot, fa = 0, None
+    if inv_freq is not None:
+        fa, rot = _on(dev, torch.float32, "inv_freq", inv_freq), 2 * inv_freq.numel()
+        if rot > D:
+            raise ValueError(f"inv_freq must have at most D / 2 = {D // 2} entries, got {inv_freq.numel()}")
+    n, c, par = _nodes(dev, B, T, lens, counts, parents)
+    sl = _optional(dev, slots, torch.int32, (B, T), "slots")
+    p, size = _ws(dev, ws)
+    if q is not None:
+        q_out, oa = _result(dev, q_out, (B, T, Hq, D), dtype, "q_out")
+    rc = lib().cache_append(qa, qs, ka, ks, va, vs, B, T, Hq, Hkv, D, dt, n, c, par, sl, fa, rot, int(interleaved), table,
+                            max_pages, num_pages, page_size, kc, vc, oa, p, size, _raw_stream(dev))
+    if rc != 0:
+        _check("cache_append", rc)
+    return q_out
+
+
+def tree_attention(q, k_cache, v_cache, page_table, lens, ws: Workspace, scale=None, counts=None, parents=None, out=None):
+    """Attention of q [B,T,Hq,D], T nodes per sequence, over the paged cache that cache_append has put them into: each
+    sees the lens[b] tokens before the pass and the nodes on its path.  scale: 1 / sqrt(D) unless given.
+
+    counts i32 [B] and parents i32 [B,T] as for cache_append.  Returns out [B,T,Hq,D]."""
+    dev = torch.cuda.current_device()
+    dt = _dt(q)
+    if q.dim() != 4:
+        raise ValueError("q must be [B,T,Hq,D]")
+    B, T, Hq, D = q.shape
+    if max(B, T, Hq, D) > _INT_MAX:
+        raise ValueError("q [B,T,Hq,D] must have sizes below 2^31")
+    qa = _on(dev, q.dtype, "q", q)
+    kc, vc, table, Hkv, page_size, num_pages, max_pages = _caches(dev, k_cache, v_cache, page_table, q.dtype, B, D)
+    n, c, par = _nodes(dev, B, T, lens, counts, parents)
+    p, size = _ws(dev, ws)
+    out, oa = _result(dev, out, (B, T, Hq, D), q.dtype, "out")
+    rc = lib().tree_attention(qa, kc, vc, B, T, Hq, Hkv, D, dt, n, c, par, table, max_pages, num_pages, page_size,
+                              D ** -0.5 if scale is None else scale, oa, p, size, _raw_stream(dev))
+    if rc != 0:
+        _check("tree_attention", rc)
+    return out
+
+
+def logits_rules(logits, V: int, ws: Workspace, history=None, history_len=None, tokens=None, parents=None, counts=None,
+                 penalties=None, bias_tokens=None, bias_values=None, masks=None, mask_rows=None, out=None):
+    """Penalties for repeated tokens, biases and grammar masks on logits [B,T,ldv], row i of a sequence being what the
+    model says after node i.
+
+    history i32 [B,L] with history_len i32 [B], tokens i32 [B,T] (the nodes' own), parents and counts as for
+    cache_append; penalties f32 [B,3]: repetition, frequency, presence; bias_tokens i32 [B,n] with bias_values f32 [B,n];
+    masks i32 [M,words], a bit per token, with mask_rows i32 [B,T], negative: none.  Returns out [B,T,ld_out] (new
+    rows have ldv entries, those behind V not written); out may be logits."""
+    dev = torch.cuda.current_device()
+    dt = _dt(logits)
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B,T,ldv]")
+    B, T, ldv = logits.shape
+    if max(B, T, V) > _INT_MAX:
+        raise ValueError("logits [B,T,ldv] and V must be below 2^31")
+    la = _on(dev, logits.dtype, "logits", logits)
+    if (history is None) != (history_len is None):
+        raise ValueError("history and history_len go together")
+    L, ha = 0, None
+    if history is not None:
+        if history.dim() != 2 or history.shape[0] != B:
+            raise ValueError(f"history must be [{B}, L]")
+        ha, L = _on(dev, torch.int32, "history", history), history.shape[1]
+    hl = _optional(dev, history_len, torch.int32, (B,), "history_len")
+    ta = _optional(dev, tokens, torch.int32, (B, T), "tokens")
+    _, c, par = _nodes(dev, B, T, None, counts, parents)
+    pa = _optional(dev, penalties, torch.float32, (B, 3), "penalties")
+    if (bias_tokens is None) != (bias_values is None):
+        raise ValueError("bias_tokens and bias_values go together")
+    nb, ba, bv = 0, None, None
+    if bias_tokens is not None:
+        if bias_tokens.dim() != 2 or bias_tokens.shape[0] != B or bias_tokens.shape[1] > _INT_MAX:
+            raise ValueError(f"bias_tokens must be [{B}, n]")
+        nb = bias_tokens.shape[1]
+        ba = _on(dev, torch.int32, "bias_tokens", bias_tokens)
+        bv = _optional(dev, bias_values, torch.float32, (B, nb), "bias_values")
+    if (masks is None) != (mask_rows is None):
+        raise ValueError("masks and mask_rows go together")
+    ma, ld_mask, num_masks, mr = None, 0, 0, None
+    if masks is not None:
+        if masks.dim() != 2 or not 0 < masks.shape[0] <= _INT_MAX:
+            raise ValueError("masks must be [M, words] with M >= 1")
+        num_masks, ld_mask = masks.shape
+        ma = _on(dev, torch.int32, "masks", masks)
+        mr = _optional(dev, mask_rows, torch.int32, (B, T), "mask_rows")
+    p, size = _ws(dev, ws)
+    if out is None:
+        out, ld_out = torch.empty_like(logits), ldv
+        oa = out.data_ptr()
+    else:
+        if out.dim() != 3 or out.shape[0] != B or out.shape[1] != T:
+            raise ValueError(f"out must be [{B}, {T}, ld_out]")
+        oa, ld_out = _on(dev, logits.dtype, "out", out), out.shape[2]
+    rc = lib().logits_rules(la, ldv, V, B, T, dt, ha, L, hl, ta, par, c, pa, ba, bv, nb, ma, ld_mask, num_masks, mr, oa, ld_out,
+                            p, size, _raw_stream(dev))
+    if rc != 0:
+        _check("logits_rules", rc)
+    return out
 
 
 # ---------------------------------------------------------------------------- host buffers

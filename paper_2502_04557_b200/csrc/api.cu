@@ -211,6 +211,11 @@ size_t spr_workspace_bytes(int op, int B, int K, int V, int d, int h, int dt)
     case SPR_OP_VERIFIER_TRAIN8:
         if (d <= 0) return 0;
         return ws_bytes_of([&](Carver &c) { train_ws_layout(c, d); });
+    case SPR_OP_CACHE_APPEND:
+    case SPR_OP_LOGITS_RULES:
+        return kHeaderBytes;      // the status word
+    case SPR_OP_TREE_ATTENTION:
+        return attention_ws_bytes(d, dt);
     default:
         return 0;
     }
@@ -451,6 +456,8 @@ const char *spr_status_string(int status)
     case SPR_ERR_TIMEOUT: return "a bounded wait inside a kernel expired";
     case SPR_ERR_BAD_TOKEN: return "draft token id outside the vocabulary";
     case SPR_ERR_BAD_ROW: return "logits row index outside the tensor";
+    case SPR_ERR_BAD_PAGE: return "cache slot without a page";
+    case SPR_ERR_BAD_TREE: return "a node's parent does not come before it";
     default: return "unknown status";
     }
 }

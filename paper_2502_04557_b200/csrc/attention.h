@@ -1,0 +1,42 @@
+// Parameters and launchers of tree_attention's kernels.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "draft_tree.cuh"
+
+namespace spr {
+
+constexpr int kAttnTile = 64;            // keys per tile, the unit in which work is dealt out
+constexpr int kAttnMaxCtas = 148;        // one CTA per SM
+constexpr int kAttnMaxDim = 128;
+
+struct AttnParams {
+    const void *q, *k, *v;               // [B,T,Hq,D]; caches [num_pages,Hkv,page_size,D]
+    void *out;                           // [B,T,Hq,D]
+    const int32_t *page_table;           // [B,max_pages]
+    DraftNodes nodes;
+    int B, Hq, Hkv, G, D;                // G = Hq / Hkv query heads share a cached head
+    int max_pages, num_pages, page_size;
+    float scale_log2;                    // scale * log2(e): scores are kept as exponents of two
+    int box;                             // keys per copy: gcd(page_size, kAttnTile)
+    int ctas;
+    // workspace
+    int *status;
+    int *counters;                       // [ctas] tickets of the items that several CTAs share, by the first of them
+    float *part;                         // [2 * ctas][rows][D]   unnormalised results of parts of such items
+    float2 *part_ml;                     // [2 * ctas][rows]      their maxima and sums
+    uint32_t spin_limit;
+    int test_flags;                      // ATTN_TEST_NO_LOADS
+};
+enum { ATTN_TEST_NO_LOADS = 1 };
+
+// rows of a row block (queries of one cached head that are worked on together) for these sizes
+int attention_block_rows(int T, int G, int dt);
+
+cudaError_t launch_attention_f32(const AttnParams &p, int rows, cudaStream_t st);
+cudaError_t launch_attention_mma(const AttnParams &p, int rows, const CUtensorMap &k, const CUtensorMap &v, int dev, cudaStream_t st);
+
+}  // namespace spr

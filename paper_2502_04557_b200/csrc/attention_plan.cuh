@@ -1,0 +1,226 @@
+// How tree_attention's work is dealt out, and how the parts of an item are joined.
+//
+// An item is a row block of one cached head of one sequence: up to ROWS of its count * G queries (rows are ordered by
+// node, then by query head), over all of the sequence's keys in tiles of 64.  The tiles of all items stand in one line
+// (by sequence, head, row block, tile) and each CTA takes an equal stretch of it, whatever the lengths, so that
+// the split follows the lengths that the device holds and a captured launch serves all of them.  A stretch begins and
+// ends inside items.  Parts of an item go to the workspace, and the CTA that takes the last ticket of an item joins
+// its parts in their order; nothing waits on another CTA.
+#pragma once
+
+#include "attention.h"
+
+namespace spr {
+
+struct AttnSeq {
+    int b, len, count, tiles, blocks;    // blocks = row blocks
+    __device__ __forceinline__ int64_t total(int Hkv) const { return (int64_t)tiles * blocks * Hkv; }
+};
+
+template <int ROWS>
+__device__ __forceinline__ AttnSeq attn_seq(const AttnParams &p, int b)
+{
+    AttnSeq s;
+    s.b = b;
+    s.len = __ldg(p.nodes.lens + b);
+    s.count = s.len < 0 ? 0 : node_count(p.nodes, b);
+    const int64_t keys = min((int64_t)s.len + s.count, (int64_t)p.max_pages * p.page_size);
+    s.tiles = s.count ? (int)((keys + kAttnTile - 1) / kAttnTile) : 0;
+    s.blocks = (s.count * p.G + ROWS - 1) / ROWS;
+    return s;
+}
+
+// Where this CTA's stretch lies.
+struct AttnStretch {
+    int64_t pos, end;        // in tiles of the line
+    int64_t total;
+    int active;              // CTAs that have a stretch
+    AttnSeq seq;             // the sequence that pos lies in
+    int64_t at;              // pos within it
+
+    __device__ __forceinline__ int owner(int64_t x) const { return (int)(((x + 1) * active - 1) / total); }
+};
+
+// Part of an item: tiles [t0, t0 + n) of it.
+struct AttnPart {
+    int head, block, t0, n;
+};
+
+template <int ROWS>
+__device__ __forceinline__ bool attn_next(const AttnParams &p, AttnStretch &s, AttnPart &part)
+{
+    if (s.pos >= s.end) return false;
+    while (s.at >= s.seq.total(p.Hkv)) {
+        s.at -= s.seq.total(p.Hkv);
+        s.seq = attn_seq<ROWS>(p, s.seq.b + 1);
+    }
+    const int item = (int)(s.at / s.seq.tiles);
+    part.t0 = (int)(s.at - (int64_t)item * s.seq.tiles);
+    part.head = item / s.seq.blocks;
+    part.block = item - part.head * s.seq.blocks;
+    part.n = (int)min((int64_t)(s.seq.tiles - part.t0), s.end - s.pos);
+    s.pos += part.n;
+    s.at += part.n;
+    return true;
+}
+
+// Called by all THREADS threads of the CTA.  `scratch`: 2 * THREADS / 32 + 4 words of 8 bytes.
+template <int ROWS, int THREADS>
+__device__ __forceinline__ AttnStretch attn_plan(const AttnParams &p, int64_t *scratch)
+{
+    constexpr int W = THREADS / 32;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // (a part costs some two tiles' time to join: no CTA is given less)
+    constexpr int kLeast = 2;
+    int64_t mine = 0;
+    for (int b = tid; b < p.B; b += THREADS) mine += attn_seq<ROWS>(p, b).total(p.Hkv);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    if (lane == 0) scratch[warp] = mine;
+    __syncthreads();
+    AttnStretch s;
+    s.total = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) s.total += scratch[w];
+    s.active = (int)min((int64_t)p.ctas, (s.total + kLeast - 1) / kLeast);
+    const int c = blockIdx.x;
+    if (c >= s.active) {
+        s.pos = s.end = 0;
+        s.at = 0;
+        s.seq = AttnSeq{0, 0, 0, 0, 0};
+        return s;
+    }
+    s.pos = c * s.total / s.active;
+    s.end = (c + 1) * s.total / s.active;
+    // the sequence that holds tile `pos`
+    int64_t before = 0;
+    for (int b0 = 0;; b0 += THREADS) {
+        const int b = b0 + tid;
+        const int64_t n = b < p.B ? attn_seq<ROWS>(p, b).total(p.Hkv) : 0;
+        int64_t incl = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += up;
+        }
+        __syncthreads();
+        if (lane == 31) scratch[warp] = incl;
+        __syncthreads();
+        int64_t lower = before, sum = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            if (w < warp) lower += scratch[w];
+            sum += scratch[w];
+        }
+        const int64_t at = s.pos - (lower + incl - n);
+        if (at >= 0 && at < n) {
+            scratch[W] = b;
+            scratch[W + 1] = at;
+        }
+        before += sum;
+        if (before > s.pos) break;
+    }
+    __syncthreads();
+    s.seq = attn_seq<ROWS>(p, (int)scratch[W]);
+    s.at = scratch[W + 1];
+    return s;
+}
+
+// Rows of nodes that are not used: zeros.  Dealt out over all CTAs by sequence.
+template <typename T>
+__device__ __forceinline__ void attn_clear_unused(const AttnParams &p, int threads)
+{
+    for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
+        const int used = __ldg(p.nodes.lens + b) < 0 ? 0 : node_count(p.nodes, b);
+        const int64_t row = (int64_t)p.Hq * p.D;
+        uint4 *out = reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + ((int64_t)b * p.nodes.T + used) * row);
+        const int64_t n = (p.nodes.T - used) * row * (int64_t)sizeof(T) / 16;
+        for (int64_t i = threadIdx.x; i < n; i += threads) out[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
+// Bits of the nodes that node i sees: itself and its path.  `tree`: the sequence's parents in shared memory, or null.
+__device__ __forceinline__ void attn_path_bits(const int *tree, int i, uint32_t *bits, int words, int *status)
+{
+    for (int w = 0; w < words; ++w) {
+        const int below = i + 1 - 32 * w;
+        bits[w] = tree ? 0u : below >= 32 ? 0xffffffffu : below > 0 ? (1u << below) - 1 : 0u;
+    }
+    if (!tree) return;
+    for (int j = i; j >= 0; j = checked_parent(tree[j], j, status)) bits[j >> 5] |= 1u << (j & 31);
+}
+
+// four results of one row, as they are written
+__device__ __forceinline__ void store_out(float *p, float4 x, int left)
+{
+    if (left >= 4)
+        *reinterpret_cast<float4 *>(p) = x;
+}
+__device__ __forceinline__ void store_out(__nv_bfloat16 *p, float4 x, int left)
+{
+    if (left < 4) return;
+    const __nv_bfloat162 a = __floats2bfloat162_rn(x.x, x.y), b = __floats2bfloat162_rn(x.z, x.w);
+    *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+}
+
+// What becomes of a part: the item's result where the part is all of it, else a record in the workspace.
+struct AttnTarget {
+    bool whole;
+    int slot;            // record of this part
+    int first, parts;    // (parts of an item) the CTA that has its first tile, and how many have some
+    int64_t row0;        // first row of the block
+    int rows;            // rows of the block in use
+};
+template <int ROWS>
+__device__ __forceinline__ AttnTarget attn_target(const AttnParams &p, const AttnStretch &s, const AttnPart &part)
+{
+    AttnTarget t;
+    t.whole = part.n == s.seq.tiles;
+    t.slot = 2 * blockIdx.x + (part.t0 == 0 ? 1 : 0);
+    t.first = t.parts = 0;
+    if (!t.whole) {
+        const int64_t begin = s.pos - part.n - part.t0;      // (pos already behind the part)
+        t.first = s.owner(begin);
+        t.parts = s.owner(begin + s.seq.tiles - 1) - t.first + 1;
+    }
+    t.row0 = (int64_t)part.block * ROWS;
+    t.rows = min(ROWS, s.seq.count * p.G - part.block * ROWS);
+    return t;
+}
+__device__ __forceinline__ int64_t attn_out_at(const AttnParams &p, const AttnStretch &s, const AttnPart &part, int64_t row)
+{
+    const int i = (int)(row / p.G), g = (int)(row - (int64_t)i * p.G);
+    return (((int64_t)s.seq.b * p.nodes.T + i) * p.Hq + (int64_t)part.head * p.G + g) * p.D;
+}
+
+// Joins the parts of an item; called by `threads` threads of the CTA that took its last ticket.
+template <int ROWS, typename T>
+__device__ __forceinline__ void attn_join(const AttnParams &p, const AttnStretch &s, const AttnPart &part, const AttnTarget &t,
+                                          int tid, int threads)
+{
+    const int cols = p.D / 4;
+    for (int i = tid; i < t.rows * cols; i += threads) {
+        const int row = i / cols, c = (i - row * cols) * 4;
+        float m = neg_inf();
+        for (int k = 0; k < t.parts; ++k) {
+            const int slot = 2 * (t.first + k) + (k == 0 ? 1 : 0);
+            m = fmaxf(m, __ldcg(&p.part_ml[(int64_t)slot * ROWS + row]).x);
+        }
+        const float ref = m == neg_inf() ? 0.f : m;
+        float l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < t.parts; ++k) {
+            const int slot = 2 * (t.first + k) + (k == 0 ? 1 : 0);
+            const float2 ml = __ldcg(&p.part_ml[(int64_t)slot * ROWS + row]);
+            const float4 x = __ldcg(reinterpret_cast<const float4 *>(p.part + ((int64_t)slot * ROWS + row) * p.D + c));
+            const float w = ex2(ml.x - ref);
+            l = fmaf(w, ml.y, l);
+            // (a part that saw nothing has w = 0 and zeros)
+            o.x = fmaf(w, x.x, o.x), o.y = fmaf(w, x.y, o.y), o.z = fmaf(w, x.z, o.z), o.w = fmaf(w, x.w, o.w);
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        store_out(static_cast<T *>(p.out) + attn_out_at(p, s, part, t.row0 + row) + c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), 4);
+    }
+}
+
+}  // namespace spr

@@ -188,6 +188,20 @@ __host__ __device__ inline size_t train_ws_layout(Carver &c, int d)
     return c.take_data(4 * (size_t)kTrainMaxCtas * ((size_t)d + 2));
 }
 
+struct AttentionWs {         // tree_attention
+    size_t counters;         // int32 [ctas]               (ticket zone) parts finished of the items that CTAs share
+    size_t part;             // float [2*ctas, rows, D]    parts of such items, two per CTA
+    size_t part_ml;          // float2 [2*ctas, rows]      their maxima and sums
+};
+__host__ __device__ inline AttentionWs attention_ws_layout(Carver &c, int ctas, int rows, int D)
+{
+    AttentionWs w;
+    w.counters = c.take_tickets((size_t)ctas);
+    w.part = c.take_data(8 * (size_t)ctas * rows * D);
+    w.part_ml = c.take_data(16 * (size_t)ctas * rows);
+    return w;
+}
+
 struct VerifyWs {
     size_t zacc;             // uint64 [M], K = 1 only (ticket zone, first: 8-byte aligned): per-token sum of
                              //   partial logits in fixed point with an arrival count; zero between launches

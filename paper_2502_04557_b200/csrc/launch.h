@@ -173,6 +173,9 @@ size_t head_loss_ws_bytes(int64_t N, int d, int V, int dt);
 size_t head_grad_ws_bytes(int64_t N, int d, int V, int dt);
 size_t head_labels_ws_bytes(int64_t N, int dp, int dq, int V, int dt);
 
+// workspace of tree_attention (tree_attention.cu) for heads of D columns; 0 for bad sizes
+size_t attention_ws_bytes(int D, int dt);
+
 struct SimParams {
     uint64_t seed;
     int64_t first_run, runs;

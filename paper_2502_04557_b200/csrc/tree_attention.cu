@@ -1,0 +1,128 @@
+// tree_attention: entry point, workspace, and which kernel takes which call.
+#include <math.h>
+
+#include "attention.h"
+#include "host_util.h"
+#include "launch.h"
+#include "tensor_pair.cuh"
+
+namespace spr {
+
+namespace {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                  CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn()
+{
+    static const EncodeTiledFn fn = [] {   // initialised once, thread-safe
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            return reinterpret_cast<EncodeTiledFn>(p);
+        return static_cast<EncodeTiledFn>(nullptr);
+    }();
+    return fn;
+}
+
+// a cache as rows of D elements, one per (page, head, entry); boxes of 64 columns by `box` rows, zeros outside
+bool cache_map(CUtensorMap *map, const void *cache, const AttnParams &p)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)p.D, (cuuint64_t)p.num_pages * p.Hkv * p.page_size};
+    const cuuint64_t strides[1] = {(cuuint64_t)p.D * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)p.box};
+    const cuuint32_t elem[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(cache), dims, strides, box, elem,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// most rows of a row block, for the workspace
+int most_rows(int dt) { return dt == SPR_F32 ? 16 : 32; }
+
+thread_local int t_test_flags = 0;
+thread_local unsigned t_spin_limit = 0;
+
+}  // namespace
+
+int attention_block_rows(int T, int G, int dt)
+{
+    const int64_t rows = (int64_t)T * G;
+    if (dt == SPR_F32) return rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
+    return rows <= 16 ? 16 : 32;
+}
+
+size_t attention_ws_bytes(int D, int dt)
+{
+    if (D <= 0 || D > kAttnMaxDim) return 0;
+    return ws_bytes_of([&](Carver &c) { attention_ws_layout(c, kAttnMaxCtas, most_rows(dt), D); });
+}
+
+}  // namespace spr
+
+using namespace spr;
+
+extern "C" {
+
+int tree_attention(const void *q, const void *k_cache, const void *v_cache, int B, int T, int Hq, int Hkv, int D, int dt,
+                   const int32_t *lens, const int32_t *counts, const int32_t *parents, const int32_t *page_table,
+                   int max_pages, int num_pages, int page_size, float scale, void *out, void *ws, size_t ws_bytes,
+                   void *cuda_stream)
+{
+    if (!dtype_ok(dt)) return SPR_ERR_UNSUPPORTED;
+    if (B < 0 || T < 0 || Hkv <= 0 || Hq <= 0 || Hq % Hkv || D <= 0 || max_pages <= 0 || num_pages <= 0 || page_size <= 0 ||
+        !isfinite(scale) || (int64_t)B * T > 0x7fffffff || Hq > 65536)
+        return SPR_ERR_INVALID_ARG;
+    if (D % 8 || D > kAttnMaxDim || page_size % 8 || T > kMaxTreeNodes || (int64_t)num_pages * Hkv > 0x7fffffff / page_size)
+        return SPR_ERR_UNSUPPORTED;
+    if (B == 0 || T == 0) return SPR_OK;
+    if (!q || !k_cache || !v_cache || !out || !lens || !page_table) return SPR_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16) || !aligned(lens, 4) ||
+        !aligned(counts, 4) || !aligned(parents, 4) || !aligned(page_table, 4))
+        return SPR_ERR_INVALID_ARG;
+    const int rows = attention_block_rows(T, Hq / Hkv, dt);
+    if (!ws || !aligned(ws, 256) || ws_bytes < (size_t)kHeaderBytes) return SPR_ERR_WORKSPACE;
+    Carver c = carve(ws_bytes);
+    const AttentionWs w = attention_ws_layout(c, kAttnMaxCtas, rows, D);
+    if (!c.fits()) return SPR_ERR_WORKSPACE;
+    const int rc = device_supported();
+    if (rc != SPR_OK) return rc;
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return finish(e);
+
+    AttnParams p = {};
+    p.q = q, p.k = k_cache, p.v = v_cache, p.out = out, p.page_table = page_table;
+    p.nodes = DraftNodes{lens, counts, parents, T};
+    p.B = B, p.Hq = Hq, p.Hkv = Hkv, p.G = Hq / Hkv, p.D = D;
+    p.max_pages = max_pages, p.num_pages = num_pages, p.page_size = page_size;
+    p.scale_log2 = scale * kLog2e;
+    p.box = kAttnTile;
+    while (page_size % p.box) p.box /= 2;
+    p.ctas = sms < kAttnMaxCtas ? sms : kAttnMaxCtas;
+    p.status = static_cast<int *>(ws);
+    p.counters = at<int>(ws, w.counters);
+    p.part = at<float>(ws, w.part);
+    p.part_ml = at<float2>(ws, w.part_ml);
+    p.spin_limit = t_spin_limit ? t_spin_limit : pairtc::kSpinLimit;
+    p.test_flags = t_test_flags;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (dt == SPR_F32) return finish(launch_attention_f32(p, rows, st));
+    CUtensorMap k_map, v_map;
+    if (!cache_map(&k_map, k_cache, p) || !cache_map(&v_map, v_cache, p)) return finish(cudaErrorInvalidValue);
+    return finish(launch_attention_mma(p, rows, k_map, v_map, dev, st));
+}
+
+void spr_test_tree_attention(int flags, unsigned spin_limit)
+{
+    t_test_flags = flags & ATTN_TEST_NO_LOADS;
+    t_spin_limit = spin_limit;
+}
+
+}  // extern "C"
