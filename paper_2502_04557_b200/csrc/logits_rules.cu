@@ -14,12 +14,16 @@
 #include "draft_tree.cuh"
 #include "host_util.h"
 #include "launch.h"
+#include "tensor_pair.cuh"
 
 namespace spr {
 
 namespace {
 
-constexpr int kRuleThreads = 256;
+using namespace pairtc;
+
+constexpr int kStages = 3;
+constexpr int kOnPath = (int)0x80000000u;
 
 struct RuleParams {
     const void *logits;
@@ -41,18 +45,13 @@ struct RuleParams {
     const int32_t *mask_rows;    // [B,T]
     int *status;
     int chunks, row_groups, rows_per_group;
+    int same;                    // rows of both tensors lie alike on 16-byte boundaries
 };
-
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 
 template <typename T>
 struct Lanes;            // a 16-byte vector as elements
 template <>
 struct Lanes<float> {
-    static constexpr int n = 4;
-    static __device__ __forceinline__ float get(const uint32_t (&w)[4], int e) { return __uint_as_float(w[e]); }
-    static __device__ __forceinline__ void set(uint32_t (&w)[4], int e, float x) { w[e] = __float_as_uint(x); }
     static __device__ __forceinline__ void forbid(uint32_t (&w)[4], uint32_t allowed)
     {
 #pragma unroll
@@ -62,16 +61,6 @@ struct Lanes<float> {
 };
 template <>
 struct Lanes<__nv_bfloat16> {
-    static constexpr int n = 8;
-    static __device__ __forceinline__ float get(const uint32_t (&w)[4], int e)
-    {
-        return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
-    }
-    static __device__ __forceinline__ void set(uint32_t (&w)[4], int e, float x)
-    {
-        const uint32_t b = __bfloat16_as_ushort(__float2bfloat16(x));
-        w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | b << 16 : (w[e >> 1] & 0xffff0000u) | b;
-    }
     static __device__ __forceinline__ void forbid(uint32_t (&w)[4], uint32_t allowed)
     {
 #pragma unroll
@@ -90,77 +79,156 @@ __device__ __forceinline__ uint32_t bits_at(const uint32_t *row, int at, int wor
     return __funnelshift_r(lo, hi, at & 31);
 }
 
-// A CTA's stretch: 16-byte vectors [chunk * VECS, (chunk + 1) * VECS) of a row, counted from the 16-byte boundary at or
-// before the row's first element, so that the stretch begins up to n - 1 tokens earlier in some rows.
-template <typename T, int VECS, bool ALIGNED>
-__global__ void __launch_bounds__(kRuleThreads) rules_kernel(const RuleParams p)
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint64_t *bar)
 {
-    constexpr int n = Lanes<T>::n, es = sizeof(T);
-    constexpr int kTokens = VECS * n + n;               // tokens first .. first + kTokens - 1 can be met
-    constexpr int kWords = (kTokens + 31) / 32;
-    extern __shared__ int sm[];
-    int *count = sm;                                    // [kTokens]
-    int *bias = sm + kTokens;                           // [kTokens] 1 + index of the bias that counts; only with biases
-    __shared__ uint32_t touched[kWords + 1];
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_addr(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void bulk_store(void *dst, uint32_t src, uint32_t bytes)
+{
+    asm volatile(
+        "cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes)
+        : "memory");
+}
+
+// A CTA's stretch: BYTES bytes of each row, counted from the 16-byte boundary at or before the row's first element, so that
+// the stretch begins up to a vector less one token earlier in some rows.
+template <typename T, int BYTES>
+struct Stretch {
+    static constexpr int n = 16 / sizeof(T), vecs = BYTES / 16;
+    static constexpr int tokens = vecs * n + n;         // tokens first .. first + tokens - 1 can be met
+    static constexpr int words = (tokens + 31) / 32;
+    static constexpr int threads = BYTES / 32;          // two vectors each
+    static size_t smem(bool biases) { return (size_t)kStages * BYTES + tokens * 4 + (biases ? tokens * 2 + 4 : 0); }
+};
+
+template <typename T, int BYTES>
+__global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const RuleParams p)
+{
+    using S = Stretch<T, BYTES>;
+    constexpr int n = S::n, es = sizeof(T), kTokens = S::tokens, kWords = S::words, kRuleThreads = S::threads;
+    extern __shared__ __align__(128) uint8_t sm[];
+    int *count = reinterpret_cast<int *>(sm + kStages * BYTES);                      // [kTokens]; kOnPath: some node has the token
+    uint32_t *bias = reinterpret_cast<uint32_t *>(count + kTokens);                  // [kTokens] of 16 bits: 1 + the bias that counts
+    __shared__ uint64_t full[kStages];
+    __shared__ uint32_t touched[kWords];
     __shared__ int near[kMaxTreeNodes];                 // nodes whose token lies in the stretch
     __shared__ int tree[kMaxTreeNodes];
-    __shared__ int n_near;
+    __shared__ int mask_of[kMaxTreeNodes];              // the rows' masks, negative: none
+    __shared__ int n_near, abort;
 
     const int tid = threadIdx.x;
     const int chunk = blockIdx.x % p.chunks, group = blockIdx.x / p.chunks % p.row_groups, b = blockIdx.x / p.chunks / p.row_groups;
     const int TT = p.nodes.T, used = node_count(p.nodes, b);
-    const int first = chunk * VECS * n - n;             // (n - 1 tokens would do; whole vectors are easier on the eye)
+    const int v0 = chunk * S::vecs;                     // the stretch's first vector
+    const int first = v0 * n - n;                       // (n - 1 tokens would do; whole vectors are easier on the eye)
     const int row0 = group * p.rows_per_group, row1 = min(row0 + p.rows_per_group, TT);
 
-    for (int i = tid; i < kTokens; i += kRuleThreads) {
-        count[i] = 0;
-        if (p.n_bias) bias[i] = 0;
-    }
-    for (int i = tid; i <= kWords; i += kRuleThreads) touched[i] = 0;
-    if (tid == 0) n_near = 0;
-    if (p.nodes.parents)
-        for (int i = tid; i < TT; i += kRuleThreads) tree[i] = p.nodes.parents[(int64_t)b * TT + i];
-    __syncthreads();
+    // a row's elements before its first 16-byte boundary, and its vectors [va, vb) in the stretch that are whole: those
+    // are copied by the copy engine, others one element at a time
+    struct Span {
+        const T *src;
+        T *dst;
+        int lead, va, vb;
+    };
+    auto span = [&](int row) {
+        Span s;
+        const int64_t r = (int64_t)b * TT + row;
+        s.src = static_cast<const T *>(p.logits) + r * p.ldv;
+        s.dst = static_cast<T *>(p.out) + r * p.ld_out;
+        s.lead = p.same ? (int)(reinterpret_cast<uintptr_t>(s.src) % 16) / es : 0;
+        s.va = v0 + (v0 == 0 && s.lead ? 1 : 0);
+        s.vb = p.same ? min(v0 + S::vecs, (p.V + s.lead) / n) : s.va;
+        return s;
+    };
+    auto fetch = [&](int row) {
+        const Span s = span(row);
+        const int stage = (row - row0) % kStages;
+        const uint32_t bytes = s.vb > s.va ? (uint32_t)(s.vb - s.va) * 16 : 0u;
+        bar_expect(&full[stage], bytes);        // (a phase for every row, whatever there is to copy)
+        if (bytes) bulk_load(smem_addr(sm) + stage * BYTES + (s.va - v0) * 16, s.src + (s.va * n - s.lead), bytes, &full[stage]);
+    };
 
-    auto touch = [&](int at) { atomicOr(&touched[at >> 5], 1u << (at & 31)); };
-    if (p.penalties) {
-        if (p.history) {
-            const int len = min((int64_t)max(__ldg(p.history_len + b), 0), p.ld_history);
-            const int32_t *h = p.history + (int64_t)b * p.ld_history;
-            for (int i = tid; i < len; i += kRuleThreads) {
-                const int t = __ldg(h + i);
-                if (t >= p.V && chunk == 0) raise_status(p.status, SPR_ERR_BAD_TOKEN);
-                if (t >= 0 && t < p.V && t >= first && t - first < kTokens) {
-                    if (atomicAdd(&count[t - first], 1) == 0) touch(t - first);
-                }
-            }
-        }
-        if (p.tokens)
-            for (int i = tid; i < used; i += kRuleThreads) {
-                const int t = __ldg(p.tokens + (int64_t)b * TT + i);
-                if (t >= p.V && chunk == 0) raise_status(p.status, SPR_ERR_BAD_TOKEN);
-                if (t >= 0 && t < p.V && t >= first && t - first < kTokens) {
-                    near[atomicAdd(&n_near, 1)] = i | (t - first) << 8;
-                    touch(t - first);
-                }
-            }
+    int fetched = min(row0 + kStages, row1);            // thread 0: the row that is fetched next
+    if (tid == 0) {
+        for (int i = 0; i < kStages; ++i) bar_init(&full[i], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        n_near = abort = 0;
+        for (int row = row0; row < fetched; ++row) fetch(row);
     }
-    for (int i = tid; i < p.n_bias; i += kRuleThreads) {
-        const int t = __ldg(p.bias_tokens + (int64_t)b * p.n_bias + i);
-        if (t >= p.V && chunk == 0) raise_status(p.status, SPR_ERR_BAD_TOKEN);
-        if (t >= 0 && t < p.V && t >= first && t - first < kTokens) {
-            atomicMax(&bias[t - first], i + 1);
-            touch(t - first);
-        }
-    }
-    __syncthreads();
-
+    // everything that the stretch's counts are made of is asked for before any of it is looked at
+    constexpr int kAhead = 8;
+    const bool counted = p.penalties && p.history;
+    const int32_t *h = p.history + (int64_t)b * p.ld_history;
+    int ahead[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) ahead[u] = counted && u * kRuleThreads + tid < p.ld_history ? __ldg(h + u * kRuleThreads + tid) : -1;
+    const int64_t len = counted ? min((int64_t)max(__ldg(p.history_len + b), 0), p.ld_history) : 0;
+    const int my_token = p.penalties && p.tokens && tid < used ? __ldg(p.tokens + (int64_t)b * TT + tid) : -1;
+    const int my_bias = tid < p.n_bias ? __ldg(p.bias_tokens + (int64_t)b * p.n_bias + tid) : -1;
     float repeat = 1.f, often = 0.f, there = 0.f;
     if (p.penalties) {
         repeat = __ldg(p.penalties + 3 * b);
         often = __ldg(p.penalties + 3 * b + 1);
         there = __ldg(p.penalties + 3 * b + 2);
     }
+    for (int i = tid; i < kTokens / 4; i += kRuleThreads) reinterpret_cast<int4 *>(count)[i] = make_int4(0, 0, 0, 0);
+    if (p.n_bias)
+        for (int i = tid; i < (kTokens + 1) / 2; i += kRuleThreads) bias[i] = 0;
+    for (int i = tid; i < kWords; i += kRuleThreads) touched[i] = 0;
+    if (p.nodes.parents)
+        for (int i = tid; i < TT; i += kRuleThreads) tree[i] = p.nodes.parents[(int64_t)b * TT + i];
+    for (int i = row0 + tid; i < row1; i += kRuleThreads) {
+        int m = p.masks && i < used ? __ldg(p.mask_rows + (int64_t)b * TT + i) : -1;
+        if (m >= p.num_masks) {
+            if (chunk == 0) raise_status(p.status, SPR_ERR_BAD_ROW);
+            m = -1;
+        }
+        mask_of[i] = m;
+    }
+    __syncthreads();
+
+    auto within = [&](int t) {
+        if (t >= p.V && chunk == 0) raise_status(p.status, SPR_ERR_BAD_TOKEN);
+        return t >= 0 && t < p.V && t >= first && t - first < kTokens;
+    };
+    auto touch = [&](int at) { atomicOr(&touched[at >> 5], 1u << (at & 31)); };
+    auto count_one = [&](int t) {
+        if (within(t)) {
+            atomicAdd(&count[t - first], 1);
+            touch(t - first);
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+        if (u * kRuleThreads + tid < len) count_one(ahead[u]);
+    for (int64_t i = kAhead * kRuleThreads + tid; i < len; i += kRuleThreads) count_one(__ldg(h + i));
+    auto node_token = [&](int i, int t) {
+        if (within(t)) {
+            near[atomicAdd(&n_near, 1)] = i | (t - first) << 8;
+            atomicOr(&count[t - first], kOnPath);
+            touch(t - first);
+        }
+    };
+    if (my_token >= 0) node_token(tid, my_token);
+    if (p.penalties && p.tokens)
+        for (int i = tid + kRuleThreads; i < used; i += kRuleThreads) node_token(i, __ldg(p.tokens + (int64_t)b * TT + i));
+    auto bias_token = [&](int i, int t) {
+        if (!within(t)) return;
+        const int at = t - first, sh = 16 * (at & 1);
+        uint32_t old = bias[at >> 1];
+        while ((old >> sh & 0xffffu) < (uint32_t)i + 1) {        // the largest index stays
+            const uint32_t seen = atomicCAS(&bias[at >> 1], old, (old & ~(0xffffu << sh)) | (uint32_t)(i + 1) << sh);
+            if (seen == old) break;
+            old = seen;
+        }
+        touch(at);
+    };
+    if (my_bias >= 0) bias_token(tid, my_bias);
+    for (int i = tid + kRuleThreads; i < p.n_bias; i += kRuleThreads) bias_token(i, __ldg(p.bias_tokens + (int64_t)b * p.n_bias + i));
+    __syncthreads();
+
     const int nn = n_near;
     const int mask_words = (p.V + 31) / 32;
 
@@ -170,111 +238,127 @@ __global__ void __launch_bounds__(kRuleThreads) rules_kernel(const RuleParams p)
         while (i > j) i = checked_parent(tree[i], i, p.status);
         return i == j;
     };
-    auto changed = [&](float x, int at, int row) {
-        int c = count[at];
-        for (int m = 0; m < nn; ++m)
-            if (near[m] >> 8 == at && on_path(near[m] & 255, row)) ++c;
-        if (c > 0) x = (x > 0.f ? x / repeat : x * repeat) - often * (float)c - there;
-        if (p.n_bias) {
-            const int k = bias[at];
-            if (k) x += __ldg(p.bias_values + (int64_t)b * p.n_bias + k - 1);
-        }
-        return x;
-    };
 
-    for (int row = row0; row < row1; ++row) {
-        const int64_t r = (int64_t)b * TT + row;
-        const T *src = static_cast<const T *>(p.logits) + r * p.ldv;
-        T *dst = static_cast<T *>(p.out) + r * p.ld_out;
+    // the mask's bits of this thread's vectors of a row, read one row ahead
+    constexpr int kEach = S::vecs / kRuleThreads;
+    uint32_t allowed[kEach], allowed_next[kEach];
+    auto mask_bits = [&](int row, uint32_t (&bits)[kEach]) {
+        if (row >= row1 || mask_of[row] < 0) return;
+        const uint32_t *mask = p.masks + mask_of[row] * p.ld_mask;
+        const int shift = span(row).lead - v0 * n;
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) bits[u] = bits_at(mask, (u * kRuleThreads + tid) * n - shift, mask_words);
+    };
+    mask_bits(row0, allowed_next);
+    int row = row0;
+    for (; row < row1; ++row) {
+        const Span s = span(row);
+        const int stage = (row - row0) % kStages;
+        T *buf = reinterpret_cast<T *>(sm + stage * BYTES);         // token c at c + lead - v0 n
+        const int shift = s.lead - v0 * n;
         const bool rules = row < used;
-        const uint32_t *mask = nullptr;
-        if (rules && p.masks) {
-            const int m = __ldg(p.mask_rows + r);
-            if (m >= p.num_masks) {
-                if (tid == 0 && chunk == 0) raise_status(p.status, SPR_ERR_BAD_ROW);
-            } else if (m >= 0)
-                mask = p.masks + (int64_t)m * p.ld_mask;
-        }
-        if (ALIGNED) {
-            const int lead = (int)(reinterpret_cast<uintptr_t>(src) % 16) / es;   // the same in dst
+        const uint32_t *mask = mask_of[row] >= 0 ? p.masks + mask_of[row] * p.ld_mask : nullptr;
 #pragma unroll
-            for (int u = 0; u < VECS / kRuleThreads; ++u) {
-                const int v = chunk * VECS + u * kRuleThreads + tid;
-                const int c = v * n - lead;                  // the vector's first token
-                if (c >= p.V) continue;
-                if (c >= 0 && c + n <= p.V) {
-                    const uint4 a = __ldcs(reinterpret_cast<const uint4 *>(src + c));
-                    uint32_t w[4] = {a.x, a.y, a.z, a.w};
-                    if (rules) {
-                        uint32_t t = bits_at(touched, c - first, kWords + 1) & ((1u << n) - 1);
-                        while (t) {
-                            const int e = __ffs(t) - 1;
-                            t &= t - 1;
-#pragma unroll
-                            for (int f = 0; f < n; ++f)
-                                if (f == e) Lanes<T>::set(w, f, changed(Lanes<T>::get(w, f), c + f - first, row));
-                        }
-                        if (mask) Lanes<T>::forbid(w, bits_at(mask, c, mask_words));
-                    }
-                    __stcs(reinterpret_cast<uint4 *>(dst + c), make_uint4(w[0], w[1], w[2], w[3]));
-                    continue;
-                }
-                for (int e = 0; e < n; ++e)
-                    if (c + e >= 0 && c + e < p.V) {
-                        T x = src[c + e];
-                        if (rules) {
-                            if (bits_at(touched, c + e - first, kWords + 1) & 1) x = (T)changed(to_float(x), c + e - first, row);
-                            if (mask && !(bits_at(mask, c + e, mask_words) & 1)) x = (T)neg_inf();
-                        }
-                        dst[c + e] = x;
-                    }
+        for (int u = 0; u < kEach; ++u) allowed[u] = allowed_next[u];
+        mask_bits(row + 1, allowed_next);
+        // tokens [c0, c1) that go one by one: of the vector before va and of the one at vb, or all of them
+        auto singles = [&](auto f) {
+            if (!p.same) {
+                const int end = min(p.V, (v0 + S::vecs) * n);
+                for (int c = v0 * n + tid; c < end; c += kRuleThreads) f(c);
+                return;
             }
-        } else {
-            // rows of input and output that lie differently on 16-byte boundaries: one element at a time
-            for (int i = tid; i < VECS * n; i += kRuleThreads) {
-                const int c = chunk * VECS * n + i;
+            if (tid >= 2 * n) return;
+            const int v = tid < n ? v0 : s.vb, c = v * n + tid % n - s.lead;
+            const bool mine = tid < n ? s.va > v0 : s.vb >= s.va && s.vb < v0 + S::vecs;
+            if (mine && c >= 0 && c < p.V) f(c);
+        };
+        singles([&](int c) { buf[c + shift] = s.src[c]; });
+        bar_wait(&full[stage], (uint32_t)((row - row0) / kStages) & 1, &abort, p.status, kSpinLimit);
+        __syncthreads();
+        if (abort) break;
+        if (mask) {
+#pragma unroll
+            for (int u = 0; u < kEach; ++u) {
+                const int v = u * kRuleThreads + tid, c = v * n - shift;
                 if (c >= p.V) break;
-                T x = src[c];
-                if (rules) {
-                    if (bits_at(touched, c - first, kWords + 1) & 1) x = (T)changed(to_float(x), c - first, row);
-                    if (mask && !(bits_at(mask, c, mask_words) & 1)) x = (T)neg_inf();
-                }
-                dst[c] = x;
+                uint4 *at = reinterpret_cast<uint4 *>(buf) + v;
+                const uint4 a = *at;
+                uint32_t w[4] = {a.x, a.y, a.z, a.w};
+                Lanes<T>::forbid(w, allowed[u]);
+                *at = make_uint4(w[0], w[1], w[2], w[3]);
             }
+            __syncthreads();
         }
+        if (rules)
+            for (int k = tid; k < kWords; k += kRuleThreads) {
+                uint32_t left = touched[k];
+                while (left) {
+                    const int at = 32 * k + __ffs(left) - 1, t = at + first, pos = t + shift;
+                    left &= left - 1;
+                    if (pos < 0 || pos >= S::vecs * n) continue;
+                    if (mask && !(bits_at(mask, t, mask_words) & 1)) continue;
+                    float x = (float)buf[pos];
+                    int c = count[at];
+                    if (c & kOnPath) {
+                        c &= ~kOnPath;
+                        for (int m = 0; m < nn; ++m)
+                            if (near[m] >> 8 == at && on_path(near[m] & 255, row)) ++c;
+                    }
+                    const uint32_t i = p.n_bias ? bias[at >> 1] >> (16 * (at & 1)) & 0xffffu : 0u;
+                    if (c == 0 && i == 0) continue;          // on other paths only: its bits stay as they are
+                    if (c > 0) x = (x > 0.f ? x / repeat : x * repeat) - often * (float)c - there;
+                    if (i) x += __ldg(p.bias_values + (int64_t)b * p.n_bias + i - 1);
+                    buf[pos] = (T)x;
+                }
+            }
+        fence_stores();
+        __syncthreads();
+        singles([&](int c) { s.dst[c] = buf[c + shift]; });
+        if (tid == 0) {
+            if (s.vb > s.va)
+                bulk_store(s.dst + (s.va * n - s.lead), smem_addr(buf) + (s.va - v0) * 16, (uint32_t)(s.vb - s.va) * 16);
+            // the row before this one has left its stage: the next one may come
+            asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group.read 1;" ::: "memory");
+            if (row > row0 && fetched < row1) fetch(fetched++);
+        }
+    }
+    if (tid == 0) {
+        stores_done();
+        // copies in flight write shared memory: none may be left when the CTA ends
+        for (; row < fetched; ++row) bar_wait_quiet(&full[(row - row0) % kStages], (uint32_t)((row - row0) / kStages) & 1, kSpinLimit);
     }
 }
 
-template <typename T, int VECS, bool ALIGNED>
+template <typename T, int BYTES>
 cudaError_t launch_rules(const RuleParams &p, unsigned ctas, cudaStream_t st)
 {
-    constexpr int tokens = VECS * Lanes<T>::n + Lanes<T>::n;
-    const size_t smem = (size_t)tokens * 4 * (p.n_bias ? 2 : 1);
+    const size_t smem = Stretch<T, BYTES>::smem(p.n_bias > 0);
     if (smem > 40000) {
-        const cudaError_t e = cudaFuncSetAttribute(rules_kernel<T, VECS, ALIGNED>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * tokens * 4);
+        const cudaError_t e = cudaFuncSetAttribute(rules_kernel<T, BYTES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   (int)Stretch<T, BYTES>::smem(true));
         if (e != cudaSuccess) return e;
     }
-    rules_kernel<T, VECS, ALIGNED><<<ctas, kRuleThreads, smem, st>>>(p);
+    rules_kernel<T, BYTES><<<ctas, Stretch<T, BYTES>::threads, smem, st>>>(p);
     return cudaGetLastError();
 }
 
 template <typename T>
-cudaError_t pick_rules(RuleParams &p, bool same, cudaStream_t st)
+cudaError_t pick_rules(RuleParams &p, cudaStream_t st)
 {
-    constexpr int n = Lanes<T>::n, kLong = 1024, kShort = 256;
-    const int T_ = p.nodes.T;
-    auto chunks_of = [&](int vecs) { return (int)(((int64_t)p.V + n - 1 + (int64_t)vecs * n - 1) / ((int64_t)vecs * n)); };
+    constexpr int n = 16 / sizeof(T), kLong = 8192, kShort = 4096;
+    const int rows = p.nodes.T;
+    auto chunks_of = [&](int bytes) { return (int)(((int64_t)p.V + n - 1 + bytes / sizeof(T) - 1) / (bytes / (int64_t)sizeof(T))); };
     const bool wide = (int64_t)p.B * chunks_of(kLong) >= 148 * 2;
     p.chunks = chunks_of(wide ? kLong : kShort);
     // few sequences: their rows are dealt out too
     int64_t groups = (148 * 4 + (int64_t)p.B * p.chunks - 1) / ((int64_t)p.B * p.chunks);
-    if (groups > T_) groups = T_;
-    p.rows_per_group = (int)((T_ + groups - 1) / groups);
-    p.row_groups = (T_ + p.rows_per_group - 1) / p.rows_per_group;
+    if (groups > rows) groups = rows;
+    p.rows_per_group = (int)((rows + groups - 1) / groups);
+    p.row_groups = (rows + p.rows_per_group - 1) / p.rows_per_group;
     const int64_t ctas = (int64_t)p.B * p.chunks * p.row_groups;
     if (ctas > 0x7fffffff) return cudaErrorInvalidValue;
-    if (wide) return same ? launch_rules<T, kLong, true>(p, (unsigned)ctas, st) : launch_rules<T, kLong, false>(p, (unsigned)ctas, st);
-    return same ? launch_rules<T, kShort, true>(p, (unsigned)ctas, st) : launch_rules<T, kShort, false>(p, (unsigned)ctas, st);
+    return wide ? launch_rules<T, kLong>(p, (unsigned)ctas, st) : launch_rules<T, kShort>(p, (unsigned)ctas, st);
 }
 
 }  // namespace
@@ -313,7 +397,7 @@ extern "C" int logits_rules(const void *logits, int64_t ldv, int V, int B, int T
     p.masks = masks, p.ld_mask = ld_mask, p.num_masks = num_masks, p.mask_rows = mask_rows;
     p.status = static_cast<int *>(ws);
     // every row of both lies alike on 16-byte boundaries
-    const bool same = (reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(out)) % 16 == 0 && (ldv - ld_out) * (int64_t)es % 16 == 0;
+    p.same = (reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(out)) % 16 == 0 && (ldv - ld_out) * (int64_t)es % 16 == 0;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return finish(dt == SPR_F32 ? pick_rules<float>(p, same, st) : pick_rules<__nv_bfloat16>(p, same, st));
+    return finish(dt == SPR_F32 ? pick_rules<float>(p, st) : pick_rules<__nv_bfloat16>(p, st));
 }
