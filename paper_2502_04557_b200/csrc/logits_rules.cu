@@ -22,7 +22,8 @@ namespace {
 
 using namespace pairtc;
 
-constexpr int kStages = 3;
+constexpr int kMaxStages = 3;         // rows of a CTA that are on their way
+constexpr int kMaxBiases = 1024;
 constexpr int kOnPath = (int)0x80000000u;
 
 struct RuleParams {
@@ -45,8 +46,12 @@ struct RuleParams {
     const int32_t *mask_rows;    // [B,T]
     int *status;
     int chunks, row_groups, rows_per_group;
+    int stages;                  // of the ring
     int same;                    // rows of both tensors lie alike on 16-byte boundaries
 };
+
+// a bit for each byte, as that byte's highest
+__device__ __forceinline__ uint32_t byte_signs(uint32_t four) { return ((four & 0xfu) * 0x00204081u & 0x01010101u) << 7; }
 
 template <typename T>
 struct Lanes;            // a 16-byte vector as elements
@@ -55,18 +60,19 @@ struct Lanes<float> {
     static __device__ __forceinline__ void forbid(uint32_t (&w)[4], uint32_t allowed)
     {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (!(allowed >> e & 1)) w[e] = 0xff800000u;
+        for (int e = 0; e < 4; ++e) w[e] = allowed >> e & 1 ? w[e] : 0xff800000u;
     }
 };
 template <>
 struct Lanes<__nv_bfloat16> {
     static __device__ __forceinline__ void forbid(uint32_t (&w)[4], uint32_t allowed)
     {
+        const uint32_t s[2] = {byte_signs(allowed), byte_signs(allowed >> 4)};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (!(allowed >> (2 * e) & 1)) w[e] = (w[e] & 0xffff0000u) | 0xff80u;
-            if (!(allowed >> (2 * e + 1) & 1)) w[e] = (w[e] & 0xffffu) | 0xff800000u;
+        for (int e = 0; e < 4; ++e) {       // a half of all ones where the element is allowed
+            uint32_t m;
+            asm("prmt.b32 %0, %1, %1, %2;" : "=r"(m) : "r"(s[e >> 1]), "r"(e & 1 ? 0xbbaa : 0x9988));    // signs of two bytes
+            w[e] = (w[e] & m) | (0xff80ff80u & ~m);
         }
     }
 };
@@ -100,23 +106,25 @@ struct Stretch {
     static constexpr int tokens = vecs * n + n;         // tokens first .. first + tokens - 1 can be met
     static constexpr int words = (tokens + 31) / 32;
     static constexpr int threads = BYTES / 32;          // two vectors each
-    static size_t smem(bool biases) { return (size_t)kStages * BYTES + tokens * 4 + (biases ? tokens * 2 + 4 : 0); }
+    static size_t smem(int stages, int biases) { return (size_t)stages * BYTES + tokens * 4 + (biases ? tokens * 2 + 4 * biases : 0); }
 };
 
 template <typename T, int BYTES>
 __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const RuleParams p)
 {
     using S = Stretch<T, BYTES>;
-    constexpr int n = S::n, es = sizeof(T), kTokens = S::tokens, kWords = S::words, kRuleThreads = S::threads;
+    constexpr int n = S::n, es = sizeof(T), kTokens = S::tokens, kWords = S::words, kRuleThreads = S::threads, kListed = 2 * kRuleThreads;
     extern __shared__ __align__(128) uint8_t sm[];
-    int *count = reinterpret_cast<int *>(sm + kStages * BYTES);                      // [kTokens]; kOnPath: some node has the token
+    int *count = reinterpret_cast<int *>(sm + p.stages * BYTES);                      // [kTokens]; kOnPath: some node has the token
     uint32_t *bias = reinterpret_cast<uint32_t *>(count + kTokens);                  // [kTokens] of 16 bits: 1 + the bias that counts
-    __shared__ uint64_t full[kStages];
+    float *bias_value = reinterpret_cast<float *>(bias + kTokens / 2);              // [n_bias]
+    __shared__ uint64_t full[kMaxStages];
+    __shared__ uint16_t listed[kListed];                // touched tokens, in any order
     __shared__ uint32_t touched[kWords];
     __shared__ int near[kMaxTreeNodes];                 // nodes whose token lies in the stretch
     __shared__ int tree[kMaxTreeNodes];
     __shared__ int mask_of[kMaxTreeNodes];              // the rows' masks, negative: none
-    __shared__ int n_near, abort;
+    __shared__ int n_near, n_listed, abort;
 
     const int tid = threadIdx.x;
     const int chunk = blockIdx.x % p.chunks, group = blockIdx.x / p.chunks % p.row_groups, b = blockIdx.x / p.chunks / p.row_groups;
@@ -144,17 +152,17 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
     };
     auto fetch = [&](int row) {
         const Span s = span(row);
-        const int stage = (row - row0) % kStages;
+        const int stage = (row - row0) % p.stages;
         const uint32_t bytes = s.vb > s.va ? (uint32_t)(s.vb - s.va) * 16 : 0u;
         bar_expect(&full[stage], bytes);        // (a phase for every row, whatever there is to copy)
         if (bytes) bulk_load(smem_addr(sm) + stage * BYTES + (s.va - v0) * 16, s.src + (s.va * n - s.lead), bytes, &full[stage]);
     };
 
-    int fetched = min(row0 + kStages, row1);            // thread 0: the row that is fetched next
+    int fetched = min(row0 + p.stages, row1);            // thread 0: the row that is fetched next
     if (tid == 0) {
-        for (int i = 0; i < kStages; ++i) bar_init(&full[i], 1);
+        for (int i = 0; i < kMaxStages; ++i) bar_init(&full[i], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        n_near = abort = 0;
+        n_near = n_listed = abort = 0;
         for (int row = row0; row < fetched; ++row) fetch(row);
     }
     // everything that the stretch's counts are made of is asked for before any of it is looked at
@@ -167,6 +175,7 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
     const int64_t len = counted ? min((int64_t)max(__ldg(p.history_len + b), 0), p.ld_history) : 0;
     const int my_token = p.penalties && p.tokens && tid < used ? __ldg(p.tokens + (int64_t)b * TT + tid) : -1;
     const int my_bias = tid < p.n_bias ? __ldg(p.bias_tokens + (int64_t)b * p.n_bias + tid) : -1;
+    for (int i = tid; i < p.n_bias; i += kRuleThreads) bias_value[i] = __ldg(p.bias_values + (int64_t)b * p.n_bias + i);
     float repeat = 1.f, often = 0.f, there = 0.f;
     if (p.penalties) {
         repeat = __ldg(p.penalties + 3 * b);
@@ -175,7 +184,7 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
     }
     for (int i = tid; i < kTokens / 4; i += kRuleThreads) reinterpret_cast<int4 *>(count)[i] = make_int4(0, 0, 0, 0);
     if (p.n_bias)
-        for (int i = tid; i < (kTokens + 1) / 2; i += kRuleThreads) bias[i] = 0;
+        for (int i = tid; i < kTokens / 2; i += kRuleThreads) bias[i] = 0;
     for (int i = tid; i < kWords; i += kRuleThreads) touched[i] = 0;
     if (p.nodes.parents)
         for (int i = tid; i < TT; i += kRuleThreads) tree[i] = p.nodes.parents[(int64_t)b * TT + i];
@@ -193,7 +202,12 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
         if (t >= p.V && chunk == 0) raise_status(p.status, SPR_ERR_BAD_TOKEN);
         return t >= 0 && t < p.V && t >= first && t - first < kTokens;
     };
-    auto touch = [&](int at) { atomicOr(&touched[at >> 5], 1u << (at & 31)); };
+    auto touch = [&](int at) {
+        const uint32_t bit = 1u << (at & 31);
+        if (atomicOr(&touched[at >> 5], bit) & bit) return;
+        const int i = atomicAdd(&n_listed, 1);
+        if (i < kListed) listed[i] = (uint16_t)at;
+    };
     auto count_one = [&](int t) {
         if (within(t)) {
             atomicAdd(&count[t - first], 1);
@@ -229,7 +243,7 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
     for (int i = tid + kRuleThreads; i < p.n_bias; i += kRuleThreads) bias_token(i, __ldg(p.bias_tokens + (int64_t)b * p.n_bias + i));
     __syncthreads();
 
-    const int nn = n_near;
+    const int nn = n_near, nl = n_listed;
     const int mask_words = (p.V + 31) / 32;
 
     // whether node j is node i or on its path
@@ -239,6 +253,33 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
         return i == j;
     };
 
+    auto bias_of = [&](int at) {
+        const uint32_t i = p.n_bias ? bias[at >> 1] >> (16 * (at & 1)) & 0xffffu : 0u;
+        return i ? make_float2(bias_value[i - 1], 1.f) : make_float2(0.f, 0.f);
+    };
+    // the rules for one token of a row; c: its count with kOnPath, w: its bias and whether there is one
+    auto fix = [&](int at, int c, float2 w, int shift, int row, T *buf) {
+        const int pos = at + first + shift;
+        if (pos < 0 || pos >= S::vecs * n) return;
+        if (c & kOnPath) {
+            c &= ~kOnPath;
+            for (int m = 0; m < nn; ++m)
+                if (near[m] >> 8 == at && on_path(near[m] & 255, row)) ++c;
+        }
+        if (c == 0 && w.y == 0.f) return;           // on other paths only: its bits stay as they are
+        float x = (float)buf[pos];
+        if (c > 0) x = (x > 0.f ? x / repeat : x * repeat) - often * (float)c - there;
+        if (w.y != 0.f) x += w.x;
+        buf[pos] = (T)x;
+    };
+    // a thread keeps its first token
+    int mine_at = 0, mine_count = 0;
+    float2 mine_bias = make_float2(0.f, 0.f);
+    if (tid < min(nl, kListed)) {
+        mine_at = listed[tid];
+        mine_count = count[mine_at];
+        mine_bias = bias_of(mine_at);
+    }
     // the mask's bits of this thread's vectors of a row, read one row ahead
     constexpr int kEach = S::vecs / kRuleThreads;
     uint32_t allowed[kEach], allowed_next[kEach];
@@ -253,11 +294,10 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
     int row = row0;
     for (; row < row1; ++row) {
         const Span s = span(row);
-        const int stage = (row - row0) % kStages;
+        const int stage = (row - row0) % p.stages;
         T *buf = reinterpret_cast<T *>(sm + stage * BYTES);         // token c at c + lead - v0 n
         const int shift = s.lead - v0 * n;
         const bool rules = row < used;
-        const uint32_t *mask = mask_of[row] >= 0 ? p.masks + mask_of[row] * p.ld_mask : nullptr;
 #pragma unroll
         for (int u = 0; u < kEach; ++u) allowed[u] = allowed_next[u];
         mask_bits(row + 1, allowed_next);
@@ -274,46 +314,37 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
             if (mine && c >= 0 && c < p.V) f(c);
         };
         singles([&](int c) { buf[c + shift] = s.src[c]; });
-        bar_wait(&full[stage], (uint32_t)((row - row0) / kStages) & 1, &abort, p.status, kSpinLimit);
-        __syncthreads();
-        if (abort) break;
-        if (mask) {
-#pragma unroll
-            for (int u = 0; u < kEach; ++u) {
-                const int v = u * kRuleThreads + tid, c = v * n - shift;
-                if (c >= p.V) break;
-                uint4 *at = reinterpret_cast<uint4 *>(buf) + v;
-                const uint4 a = *at;
-                uint32_t w[4] = {a.x, a.y, a.z, a.w};
-                Lanes<T>::forbid(w, allowed[u]);
-                *at = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-            __syncthreads();
-        }
-        if (rules)
-            for (int k = tid; k < kWords; k += kRuleThreads) {
-                uint32_t left = touched[k];
-                while (left) {
-                    const int at = 32 * k + __ffs(left) - 1, t = at + first, pos = t + shift;
-                    left &= left - 1;
-                    if (pos < 0 || pos >= S::vecs * n) continue;
-                    if (mask && !(bits_at(mask, t, mask_words) & 1)) continue;
-                    float x = (float)buf[pos];
-                    int c = count[at];
-                    if (c & kOnPath) {
-                        c &= ~kOnPath;
-                        for (int m = 0; m < nn; ++m)
-                            if (near[m] >> 8 == at && on_path(near[m] & 255, row)) ++c;
+        bar_wait(&full[stage], (uint32_t)((row - row0) / p.stages) & 1, &abort, p.status, kSpinLimit);
+        if (!p.same || s.va != v0 || s.vb != v0 + S::vecs) __syncthreads();         // (those that went one by one)
+        if (rules) {
+            if (nl <= kListed) {
+                if (tid < nl) fix(mine_at, mine_count, mine_bias, shift, row, buf);
+                if (tid + kRuleThreads < nl) {
+                    const int at = listed[tid + kRuleThreads];
+                    fix(at, count[at], bias_of(at), shift, row, buf);
+                }
+            } else {
+                for (int k = tid; k < kWords; k += kRuleThreads)
+                    for (uint32_t left = touched[k]; left; left &= left - 1) {
+                        const int at = 32 * k + __ffs(left) - 1;
+                        fix(at, count[at], bias_of(at), shift, row, buf);
                     }
-                    const uint32_t i = p.n_bias ? bias[at >> 1] >> (16 * (at & 1)) & 0xffffu : 0u;
-                    if (c == 0 && i == 0) continue;          // on other paths only: its bits stay as they are
-                    if (c > 0) x = (x > 0.f ? x / repeat : x * repeat) - often * (float)c - there;
-                    if (i) x += __ldg(p.bias_values + (int64_t)b * p.n_bias + i - 1);
-                    buf[pos] = (T)x;
+            }
+            if (mask_of[row] >= 0) {
+                __syncthreads();
+#pragma unroll
+                for (int u = 0; u < kEach; ++u) {
+                    uint4 *at = reinterpret_cast<uint4 *>(buf) + u * kRuleThreads + tid;
+                    const uint4 a = *at;
+                    uint32_t w[4] = {a.x, a.y, a.z, a.w};
+                    Lanes<T>::forbid(w, allowed[u]);
+                    *at = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
+        }
         fence_stores();
         __syncthreads();
+        if (abort) break;
         singles([&](int c) { s.dst[c] = buf[c + shift]; });
         if (tid == 0) {
             if (s.vb > s.va)
@@ -324,19 +355,19 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
         }
     }
     if (tid == 0) {
-        stores_done();
+        stores_read();
         // copies in flight write shared memory: none may be left when the CTA ends
-        for (; row < fetched; ++row) bar_wait_quiet(&full[(row - row0) % kStages], (uint32_t)((row - row0) / kStages) & 1, kSpinLimit);
+        for (; row < fetched; ++row) bar_wait_quiet(&full[(row - row0) % p.stages], (uint32_t)((row - row0) / p.stages) & 1, kSpinLimit);
     }
 }
 
 template <typename T, int BYTES>
 cudaError_t launch_rules(const RuleParams &p, unsigned ctas, cudaStream_t st)
 {
-    const size_t smem = Stretch<T, BYTES>::smem(p.n_bias > 0);
+    const size_t smem = Stretch<T, BYTES>::smem(p.stages, p.n_bias);
     if (smem > 40000) {
         const cudaError_t e = cudaFuncSetAttribute(rules_kernel<T, BYTES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   (int)Stretch<T, BYTES>::smem(true));
+                                                   (int)Stretch<T, BYTES>::smem(kMaxStages, kMaxBiases));
         if (e != cudaSuccess) return e;
     }
     rules_kernel<T, BYTES><<<ctas, Stretch<T, BYTES>::threads, smem, st>>>(p);
@@ -352,9 +383,10 @@ cudaError_t pick_rules(RuleParams &p, cudaStream_t st)
     const bool wide = (int64_t)p.B * chunks_of(kLong) >= 148 * 2;
     p.chunks = chunks_of(wide ? kLong : kShort);
     // few sequences: their rows are dealt out too
-    int64_t groups = (148 * 4 + (int64_t)p.B * p.chunks - 1) / ((int64_t)p.B * p.chunks);
-    if (groups > rows) groups = rows;
+    int64_t groups = 148 * 4 / ((int64_t)p.B * p.chunks);
+    groups = groups < 1 ? 1 : groups > rows ? rows : groups;
     p.rows_per_group = (int)((rows + groups - 1) / groups);
+    p.stages = p.rows_per_group < kMaxStages ? p.rows_per_group : kMaxStages;
     p.row_groups = (rows + p.rows_per_group - 1) / p.rows_per_group;
     const int64_t ctas = (int64_t)p.B * p.chunks * p.row_groups;
     if (ctas > 0x7fffffff) return cudaErrorInvalidValue;
@@ -374,7 +406,7 @@ extern "C" int logits_rules(const void *logits, int64_t ldv, int V, int B, int T
                             int64_t ld_out, void *ws, size_t ws_bytes, void *cuda_stream)
 {
     if (!dtype_ok(dt)) return SPR_ERR_UNSUPPORTED;
-    if (B < 0 || T < 0 || V <= 0 || V > 1 << 30 || ldv < V || ld_out < V || (int64_t)B * T > 0x7fffffff || n_bias < 0 || n_bias > 1024)
+    if (B < 0 || T < 0 || V <= 0 || V > 1 << 30 || ldv < V || ld_out < V || (int64_t)B * T > 0x7fffffff || n_bias < 0 || n_bias > kMaxBiases)
         return SPR_ERR_INVALID_ARG;
     if (T > kMaxTreeNodes) return SPR_ERR_UNSUPPORTED;
     if (B == 0 || T == 0) return SPR_OK;
