@@ -1,7 +1,6 @@
 // Parameters and launchers of tree_attention's kernels.
 #pragma once
 
-#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -20,23 +19,21 @@ struct AttnParams {
     DraftNodes nodes;
     int B, Hq, Hkv, G, D;                // G = Hq / Hkv query heads share a cached head
     int max_pages, num_pages, page_size;
-    float scale_log2;                    // scale * log2(e): scores are kept as exponents of two
-    int box;                             // keys per copy: gcd(page_size, kAttnTile)
+    float scale_log2;                    // scale * log2(e): scores are exponents of two
+    float abs_scale_log2;                // its magnitude (not zero: masked scores, -inf, stay what they are under it) ...
+    uint32_t flip;                       // ... and sign, as the sign bits of two bf16 numbers: queries take it over
     int ctas;
     // workspace
     int *status;
     int *counters;                       // [ctas] tickets of the items that several CTAs share, by the first of them
     float *part;                         // [2 * ctas][rows][D]   unnormalised results of parts of such items
     float2 *part_ml;                     // [2 * ctas][rows]      their maxima and sums
-    uint32_t spin_limit;
-    int test_flags;                      // ATTN_TEST_NO_LOADS
 };
-enum { ATTN_TEST_NO_LOADS = 1 };
 
 // rows of a row block (queries of one cached head that are worked on together) for these sizes
 int attention_block_rows(int T, int G, int dt);
 
 cudaError_t launch_attention_f32(const AttnParams &p, int rows, cudaStream_t st);
-cudaError_t launch_attention_mma(const AttnParams &p, int rows, const CUtensorMap &k, const CUtensorMap &v, int dev, cudaStream_t st);
+cudaError_t launch_attention_mma(const AttnParams &p, int rows, int dev, cudaStream_t st);
 
 }  // namespace spr

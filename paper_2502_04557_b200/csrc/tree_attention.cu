@@ -4,49 +4,13 @@
 #include "attention.h"
 #include "host_util.h"
 #include "launch.h"
-#include "tensor_pair.cuh"
 
 namespace spr {
 
 namespace {
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
-                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                  CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn()
-{
-    static const EncodeTiledFn fn = [] {   // initialised once, thread-safe
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            return reinterpret_cast<EncodeTiledFn>(p);
-        return static_cast<EncodeTiledFn>(nullptr);
-    }();
-    return fn;
-}
-
-// a cache as rows of D elements, one per (page, head, entry); boxes of 64 columns by `box` rows, zeros outside
-bool cache_map(CUtensorMap *map, const void *cache, const AttnParams &p)
-{
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)p.D, (cuuint64_t)p.num_pages * p.Hkv * p.page_size};
-    const cuuint64_t strides[1] = {(cuuint64_t)p.D * 2};
-    const cuuint32_t box[2] = {64, (cuuint32_t)p.box};
-    const cuuint32_t elem[2] = {1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(cache), dims, strides, box, elem,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // most rows of a row block, for the workspace
 int most_rows(int dt) { return dt == SPR_F32 ? 16 : 32; }
-
-thread_local int t_test_flags = 0;
-thread_local unsigned t_spin_limit = 0;
 
 }  // namespace
 
@@ -103,26 +67,16 @@ int tree_attention(const void *q, const void *k_cache, const void *v_cache, int 
     p.B = B, p.Hq = Hq, p.Hkv = Hkv, p.G = Hq / Hkv, p.D = D;
     p.max_pages = max_pages, p.num_pages = num_pages, p.page_size = page_size;
     p.scale_log2 = scale * kLog2e;
-    p.box = kAttnTile;
-    while (page_size % p.box) p.box /= 2;
+    p.abs_scale_log2 = fmaxf(fabsf(p.scale_log2), 1e-37f);
+    p.flip = scale < 0.f ? 0x80008000u : 0u;
     p.ctas = sms < kAttnMaxCtas ? sms : kAttnMaxCtas;
     p.status = static_cast<int *>(ws);
     p.counters = at<int>(ws, w.counters);
     p.part = at<float>(ws, w.part);
     p.part_ml = at<float2>(ws, w.part_ml);
-    p.spin_limit = t_spin_limit ? t_spin_limit : pairtc::kSpinLimit;
-    p.test_flags = t_test_flags;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (dt == SPR_F32) return finish(launch_attention_f32(p, rows, st));
-    CUtensorMap k_map, v_map;
-    if (!cache_map(&k_map, k_cache, p) || !cache_map(&v_map, v_cache, p)) return finish(cudaErrorInvalidValue);
-    return finish(launch_attention_mma(p, rows, k_map, v_map, dev, st));
-}
-
-void spr_test_tree_attention(int flags, unsigned spin_limit)
-{
-    t_test_flags = flags & ATTN_TEST_NO_LOADS;
-    t_spin_limit = spin_limit;
+    return finish(launch_attention_mma(p, rows, dev, st));
 }
 
 }  // extern "C"
