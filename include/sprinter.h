@@ -461,7 +461,7 @@ int cache_append(const void *q, int64_t q_stride, const void *k, int64_t k_strid
  * Scores, maxima and sums are fp32; with bf16 tensors the weights enter the second product as two bf16 numbers.
  * Keys and values of slots that a row does not see have no part in it, whatever they hold; infinities and NaN in
  * those that it does see make it infinite or NaN.  A slot without a page is left out (SPR_ERR_BAD_PAGE), and a row
- * that sees no slot at all is zeros.
+ * that sees no slot at all is zeros.  After SPR_ERR_TIMEOUT rows whose keys did not arrive are NaN.
  * Launches do not depend on the lengths: a captured call serves whatever lens, counts, parents and page_table hold
  * when it is replayed.  Workspace: spr_workspace_bytes(SPR_OP_TREE_ATTENTION, B, T, 1, D, 0, dt).
  */
@@ -622,19 +622,22 @@ int spr_test_verifier_train_step(const void *hidden, const uint8_t *labels, int6
                                  void *cuda_stream, int flags, unsigned spin_limit);
 
 /*
- * spr_test_verifier_train_step8, spr_test_pair_kernels - test hooks, not part of the stable interface.
+ * spr_test_verifier_train_step8, spr_test_pair_kernels, spr_test_tree_attention - test hooks, not part of the stable interface.
  *
  * The paper has no counterpart.  The first is verifier_train_step8 with flags and spin_limit as for
  * spr_test_verifier_train_step.  The second makes the head_loss, head_loss_grad and verifier_labels_head
  * calls that this host thread makes afterwards load nothing (flags bit 0), so that the first bounded wait of
  * every CTA pair runs out after spin_limit polls (0 = the library's limit), with the outcome that those calls
  * document for SPR_ERR_TIMEOUT, nothing left in flight and the workspace usable; (0, 0) ends it.
+ * spr_test_tree_attention does the same for tree_attention on bf16 tensors with more than 16 queries per cached head
+ * (the other forms of it wait for nothing).
  */
 int spr_test_verifier_train_step8(const void *packed, const uint8_t *labels, int64_t N, int d, float *theta,
                                   float *adam_m, float *adam_v, int t, double lr, double beta1, double beta2,
                                   double eps, float *loss, void *ws, size_t ws_bytes, void *cuda_stream, int flags,
                                   unsigned spin_limit);
 void spr_test_pair_kernels(int flags, unsigned spin_limit);
+void spr_test_tree_attention(int flags, unsigned spin_limit);
 
 /* Synchronises the stream, returns the sticky device status word of `ws`
  * (SPR_OK if nothing was detected) and clears it. */

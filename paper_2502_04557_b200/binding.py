@@ -30,7 +30,7 @@ EXPORTS = [
     "verifier_labels", "verifier_train_step", "spr_test_sprinter_verify", "spr_test_verifier_train_step",
     "head_loss", "head_loss_grad", "verifier_labels_head", "spr_pack8_pitch", "hidden_pack8", "hidden_unpack8",
     "verifier_train_step8", "spr_test_verifier_train_step8", "spr_test_pair_kernels",
-    "cache_append", "tree_attention", "logits_rules",
+    "cache_append", "tree_attention", "logits_rules", "spr_test_tree_attention",
 ]
 
 
@@ -122,6 +122,8 @@ def lib():
         L.tree_attention.argtypes = [vp] * 3 + [i32] * 6 + [vp] * 4 + [i32] * 3 + [f32, vp, vp, sz, vp]
         L.logits_rules.restype = i32
         L.logits_rules.argtypes = [vp, i64, i32, i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, i32, vp, i64, i32, vp, vp, i64, vp, sz, vp]
+        L.spr_test_tree_attention.restype = None
+        L.spr_test_tree_attention.argtypes = [i32, C.c_uint]
         L.spr_host_arena_bytes.restype = sz
         L.spr_host_arena_bytes.argtypes = [i32, i32, i32, i32, i64, i32, i32, i32]
         L.sprinter_verify_host.restype = i32

@@ -28,12 +28,16 @@ struct AttnParams {
     int *counters;                       // [ctas] tickets of the items that several CTAs share, by the first of them
     float *part;                         // [2 * ctas][rows][D]   unnormalised results of parts of such items
     float2 *part_ml;                     // [2 * ctas][rows]      their maxima and sums
+    uint32_t spin_limit;                 // polls after which a bounded wait gives up
+    int test_flags;                      // ATTN_TEST_*
 };
+enum { ATTN_TEST_NO_LOADS = 1 };         // test hook: no tile is ever loaded, so that the first waits run out
 
 // rows of a row block (queries of one cached head that are worked on together) for these sizes
 int attention_block_rows(int T, int G, int dt);
 
 cudaError_t launch_attention_f32(const AttnParams &p, int rows, cudaStream_t st);
-cudaError_t launch_attention_mma(const AttnParams &p, int rows, int dev, cudaStream_t st);
+cudaError_t launch_attention_mma(const AttnParams &p, int dev, cudaStream_t st);
+cudaError_t launch_attention_tc(const AttnParams &p, int rows, int dev, cudaStream_t st);
 
 }  // namespace spr

@@ -458,10 +458,9 @@ cudaError_t launch_mma(const AttnParams &p, int dev, cudaStream_t st)
 
 }  // namespace
 
-cudaError_t launch_attention_mma(const AttnParams &p, int rows, int dev, cudaStream_t st)
+cudaError_t launch_attention_mma(const AttnParams &p, int dev, cudaStream_t st)
 {
-    if (rows == 16) return p.D <= 64 ? launch_mma<1, 1>(p, dev, st) : launch_mma<1, 2>(p, dev, st);
-    return p.D <= 64 ? launch_mma<2, 1>(p, dev, st) : launch_mma<2, 2>(p, dev, st);
+    return p.D <= 64 ? launch_mma<1, 1>(p, dev, st) : launch_mma<1, 2>(p, dev, st);
 }
 
 }  // namespace spr

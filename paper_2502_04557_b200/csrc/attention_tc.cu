@@ -1,0 +1,556 @@
+// tree_attention on bf16 tensors, many rows per cached head (long chains, trees): tcgen05.
+//
+//   S = Q K^T   128 rows by a tile of 64 keys, into TMEM;   P = exp2(c (S - m)), back into TMEM;   O += P V, in TMEM
+//
+// One CTA per SM walks its stretch of tiles.  Two loader warps bring keys and values into a ring (cp.async, 16 bytes per
+// lane, into the 128-byte swizzle that the matrix descriptors name: pages of 16 entries would be 2 KB boxes for the copy
+// engine, whose number sets its time).  One thread issues the products: S of the next tile goes ahead of P V of
+// this one, S and P are double-buffered.  Four softmax warps have a row per thread.  The maximum that exponents are
+// taken against is only raised when a score passes it by 2^8 (weights then stay below 2^8, and sums and
+// products in fp32 keep their relative precision), so that O, which lives in TMEM, is hardly ever rescaled.
+//
+// Weights are used as two bf16 numbers, their rounding and what is left of it: one would put an error of 2^-9 on the
+// result, as much as its own rounding.  Up to 64 rows (DUP) the tile's other half holds the same queries again and
+// takes the second number, so that the one product does both; above, there is a second product.
+//
+// Every wait is bounded: when one runs out the status word becomes SPR_ERR_TIMEOUT, loaders and the issuing thread stop and
+// wait (again bounded) for what is in flight, and the softmax warps go on without waiting and give NaN.
+#include <atomic>
+
+#include "attention_plan.cuh"
+#include "host_util.h"
+#include "launch.h"
+#include "tensor_pair.cuh"
+
+namespace spr {
+
+namespace {
+
+using namespace pairtc;
+
+constexpr int kTcThreads = 256;
+constexpr int kSoftmaxThreads = 128;
+constexpr int kMmaWarp = 4, kFirstLoader = 6, kLoaders = 2;      // (warp 5 only makes registers come out even)
+constexpr int kPanel = kAttnTile * 128;                         // 64 keys by 64 columns
+constexpr float kRaise = 8.f;                                   // by how much scores may pass the maximum in use
+// TMEM columns
+constexpr int kColS = 0, kColP = 128, kColO = 256, kTmemCols = 512;       // P: 2 buffers of 32 columns, each twice
+
+template <int PANELS>
+struct TcShape {
+    static constexpr int stage = 2 * PANELS * kPanel;            // keys, then values
+    static constexpr int stages = PANELS == 2 ? 5 : 10;
+    static constexpr int behind = stages - 3;                    // copies of as many tiles are in flight behind the newest
+    static constexpr int q_bytes = PANELS * 128 * 128;
+    static constexpr size_t smem = (size_t)q_bytes + (size_t)stages * stage + 1024;
+};
+
+struct TcControl {
+    uint64_t full[10], empty[10];
+    uint64_t s_full[2], s_free[2], p_ready[2], pv_done[2];
+    uint64_t q_ready, drain;
+    uint32_t valid[10][kLoaders];            // a bit for each key of the stage's tile that is there
+    int64_t scratch[2 * (kTcThreads / 32) + 4];
+    unsigned long long odd;
+    int64_t o_live;
+    uint32_t tmem;
+    int abort, last;
+    int tree[kMaxTreeNodes];
+    uint32_t path[128][kMaxTreeNodes / 32];
+};
+
+__device__ __forceinline__ void softmax_meet() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there)
+{
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void mma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+}
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t *bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void tmem_write32(uint32_t taddr, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ bool finite_bf16x2(uint32_t w) { return (w & 0x7f80u) != 0x7f80u && (w & 0x7f800000u) != 0x7f800000u; }
+// 64 bits of a path from node `at` on
+__device__ __forceinline__ uint64_t path_bits64(const uint32_t *path, int at)
+{
+    constexpr int n = kMaxTreeNodes / 32;
+    const int w = at >> 5;
+    const uint32_t a = w < n ? path[w] : 0u, b = w + 1 < n ? path[w + 1] : 0u, c = w + 2 < n ? path[w + 2] : 0u;
+    return (uint64_t)__funnelshift_r(a, b, at & 31) | (uint64_t)__funnelshift_r(b, c, at & 31) << 32;
+}
+
+template <int PANELS, bool DUP>
+__global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnParams p)
+{
+    constexpr int ROWS = DUP ? 64 : 128, COLS = 64 * PANELS;
+    using Shape = TcShape<PANELS>;
+    extern __shared__ uint8_t raw[];
+    __shared__ TcControl ctl;
+    const uint32_t q_tile = (smem_addr(raw) + 1023u) & ~1023u, ring = q_tile + Shape::q_bytes;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t limit = p.spin_limit;
+
+    if (tid == 0) {
+        for (int i = 0; i < Shape::stages; ++i) {
+            bar_init(&ctl.full[i], kLoaders);
+            bar_init(&ctl.empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(&ctl.s_full[i], 1);
+            bar_init(&ctl.s_free[i], 4);
+            bar_init(&ctl.p_ready[i], 4);
+            bar_init(&ctl.pv_done[i], 1);
+        }
+        bar_init(&ctl.q_ready, 4);
+        bar_init(&ctl.drain, 1);
+        ctl.abort = 0;
+        ctl.odd = 0;
+        ctl.o_live = -1;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&ctl.tmem)), "r"((uint32_t)kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    AttnStretch s = attn_plan<ROWS, kTcThreads>(p, ctl.scratch);
+    attn_clear_unused<__nv_bfloat16>(p, kTcThreads);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = ctl.tmem;
+
+    if (warp >= kFirstLoader) {
+        // ------------------------------------------------------------ loaders: 32 of a tile's keys each
+        constexpr int kChunks = 8 * PANELS, kRowsAtOnce = 32 / kChunks;
+        const int half = warp - kFirstLoader;
+        const int c_row = lane / kChunks, c_chunk = lane % kChunks;
+        const bool c_in = c_chunk * 8 < p.D;
+        // rows r0 + c_row of this warp's keys lie at to(r0) = (c_dst + 128 r0) ^ (r0 % 8 << 4): r0 is a multiple of kRowsAtOnce
+        const uint32_t c_dst = (c_chunk >> 3) * kPanel + half * 32 * 128 + c_row * 128 + (((c_chunk & 7) ^ c_row) << 4);
+        AttnPart part = {0, 0, 0, 0};
+        int64_t issued = 0;
+        bool alive = !(p.test_flags & ATTN_TEST_NO_LOADS);
+        auto complete = [&](int64_t tile) {         // this thread's copies of the tile have come
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) arrive(&ctl.full[tile % Shape::stages]);
+        };
+        while (alive && attn_next<ROWS>(p, s, part)) {
+            int64_t keys = (int64_t)s.seq.len + s.seq.count;
+            if (keys > (int64_t)p.max_pages * p.page_size) {
+                raise_status(p.status, SPR_ERR_BAD_PAGE);
+                keys = (int64_t)p.max_pages * p.page_size;
+            }
+            const int end = part.t0 + part.n;
+            auto find = [&](int tile) {             // lane 4 j + r: where run r (8 keys) of tile + j begins in the caches
+                const int t = tile + (lane >> 2);
+                const int64_t slot = (int64_t)t * kAttnTile + half * 32 + 8 * (lane & 3);
+                if (t >= end || slot >= keys) return -1;
+                const uint32_t at = (uint32_t)((uint64_t)slot >> 3) / (uint32_t)(p.page_size >> 3);       // pages are whole runs
+                const int page = __ldg(p.page_table + (int64_t)s.seq.b * p.max_pages + at);
+                if (page < 0 || page >= p.num_pages) {
+                    raise_status(p.status, SPR_ERR_BAD_PAGE);
+                    return -1;
+                }
+                return (page * p.Hkv + part.head) * p.page_size + (int)(slot - (int64_t)at * p.page_size);
+            };
+            int next = find(part.t0);
+            for (int n = 0; alive && n < part.n; n += 8) {
+                const int rows = next;
+                next = find(part.t0 + n + 8);
+                for (int u = 0; u < 8 && n + u < part.n; ++u, ++issued) {
+                    const int stage = (int)(issued % Shape::stages);
+                    const uint32_t round = (uint32_t)(issued / Shape::stages);
+                    if (round > 0 && !__all_sync(0xffffffffu, bar_wait(&ctl.empty[stage], (round - 1) & 1, &ctl.abort, p.status, limit))) {
+                        alive = false;
+                        break;
+                    }
+                    const int64_t left = keys - ((int64_t)part.t0 + n + u) * kAttnTile - half * 32;
+                    uint32_t valid = left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1;
+                    int run[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        run[r] = __shfl_sync(0xffffffffu, rows, 4 * u + r);
+                        if (run[r] < 0) valid &= ~(0xffu << (8 * r));
+                    }
+                    if (lane == 0) ctl.valid[stage][half] = valid;
+                    const uint32_t dst = ring + stage * Shape::stage + c_dst;
+#pragma unroll
+                    for (int i = 0; i < 32 / kRowsAtOnce; ++i) {
+                        const int r0 = i * kRowsAtOnce, r = r0 + c_row;
+                        const bool there = c_in && (valid >> r & 1);
+                        const int64_t at = there ? ((int64_t)run[r0 >> 3] + (r & 7)) * p.D + c_chunk * 8 : 0;
+                        const uint32_t to = (dst + r0 * 128) ^ ((r0 & 7) << 4);
+                        copy16(to, static_cast<const __nv_bfloat16 *>(p.k) + at, there);
+                        copy16(to + PANELS * kPanel, static_cast<const __nv_bfloat16 *>(p.v) + at, there);
+                    }
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                    if (issued >= Shape::behind) {
+                        asm volatile("cp.async.wait_group %0;" ::"n"(Shape::behind) : "memory");
+                        complete(issued - Shape::behind);
+                    }
+                }
+            }
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        if (alive)
+            for (int64_t i = issued > Shape::behind ? issued - Shape::behind : 0; i < issued; ++i) complete(i);
+    } else if (warp == kMmaWarp) {
+        // ------------------------------------------------------------ products
+        if (lane == 0) {
+            constexpr uint32_t kQk = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kAttnTile >> 3) << 17) | (8u << 24);
+            constexpr uint32_t kPv = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(COLS >> 3) << 17) | (8u << 24);
+            AttnPart part;
+            int64_t at = 0;                 // tiles of the stretch
+            uint32_t parts = 0;
+            bool alive = true;
+            auto wait = [&](uint64_t *bar, uint32_t parity) {
+                if (alive && !bar_wait(bar, parity & 1, &ctl.abort, p.status, limit)) alive = false;
+                return alive;
+            };
+            auto scores = [&](int64_t i) {
+                const int stage = (int)(i % Shape::stages), b = (int)(i & 1);
+                if (!wait(&ctl.full[stage], (uint32_t)(i / Shape::stages))) return;
+                if (i >= 2 && !wait(&ctl.s_free[b], (uint32_t)(i >> 1) - 1)) return;
+                fence_after();
+                const uint32_t k = ring + stage * Shape::stage;
+#pragma unroll
+                for (int q = 0; q < 4 * PANELS; ++q)
+                    mma_smem(tmem + kColS + 64 * b, tile_desc(q_tile + (q >> 2) * 128 * 128 + (q & 3) * 32, false),
+                             tile_desc(k + (q >> 2) * kPanel + (q & 3) * 32, false), kQk, q != 0);
+                commit(&ctl.s_full[b]);
+            };
+            while (alive && attn_next<ROWS>(p, s, part)) {
+                if (!wait(&ctl.q_ready, parts++)) break;
+                scores(at);
+                for (int n = 0; alive && n < part.n; ++n, ++at) {
+                    if (n + 1 < part.n) scores(at + 1);
+                    const int stage = (int)(at % Shape::stages), b = (int)(at & 1);
+                    if (!wait(&ctl.p_ready[b], (uint32_t)(at >> 1))) break;
+                    fence_after();
+                    const uint32_t v = ring + stage * Shape::stage + PANELS * kPanel;
+                    const bool live = n > 0 || *reinterpret_cast<volatile int64_t *>(&ctl.o_live) == at;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        mma_tmem(tmem + kColO, tmem + kColP + 64 * b + 8 * q, tile_desc(v + q * 2048, true), kPv, live || q != 0);
+                        if (!DUP) mma_tmem(tmem + kColO, tmem + kColP + 64 * b + 32 + 8 * q, tile_desc(v + q * 2048, true), kPv, 1u);
+                    }
+                    commit(&ctl.pv_done[b]);
+                    commit(&ctl.empty[stage]);
+                }
+            }
+            commit(&ctl.drain);             // nothing of this CTA's products is left when its TMEM is given back
+            bar_wait_quiet(&ctl.drain, 0, limit);
+        }
+        __syncwarp();
+    } else if (warp < 4) {
+        // ------------------------------------------------------------ softmax: a row per thread
+        const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+        const int row = DUP ? tid & 63 : tid;               // in the block
+        const bool second = DUP && tid >= 64;               // this thread's weights are what rounding left
+        const float c = p.abs_scale_log2;
+        AttnPart part;
+        int64_t at = 0;
+        int tree_of = -1;
+        bool dead = false;
+        auto wait = [&](uint64_t *bar, uint32_t parity) {
+            if (!dead) dead = !__all_sync(0xffffffffu, bar_wait(bar, parity & 1, &ctl.abort, p.status, limit));
+        };
+        auto warp_arrive = [&](uint64_t *bar) {
+            __syncwarp();
+            if (lane == 0) arrive(bar);
+        };
+        while (attn_next<ROWS>(p, s, part)) {
+            const AttnTarget t = attn_target<ROWS>(p, s, part);
+            const int i0 = (int)(t.row0 / p.G);
+            const int nodes = (int)((t.row0 + t.rows - 1) / p.G) - i0 + 1;
+            softmax_meet();
+            if (p.nodes.parents && tree_of != s.seq.b) {
+                for (int j = tid; j < s.seq.count; j += kSoftmaxThreads) ctl.tree[j] = p.nodes.parents[(int64_t)s.seq.b * p.nodes.T + j];
+                tree_of = s.seq.b;
+                softmax_meet();
+            }
+            if (tid < nodes) {
+                for (int w = (s.seq.count + 31) / 32; w < kMaxTreeNodes / 32; ++w) ctl.path[tid][w] = 0u;
+                attn_path_bits(p.nodes.parents ? ctl.tree : nullptr, i0 + tid, ctl.path[tid], (s.seq.count + 31) / 32, p.status);
+            }
+            // this row's query (zeros where there is none; all products of the part before have been formed)
+            const bool in = row < t.rows;
+            const int64_t out_at = in ? attn_out_at(p, s, part, t.row0 + row) : 0;
+            {
+                const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + out_at);
+#pragma unroll
+                for (int k = 0; k < 8 * PANELS; ++k) {
+                    uint4 x = in && k * 8 < p.D ? __ldg(src + k) : make_uint4(0u, 0u, 0u, 0u);
+                    x.x ^= p.flip, x.y ^= p.flip, x.z ^= p.flip, x.w ^= p.flip;
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};"
+                                 ::"r"(q_tile + (k >> 3) * 128 * 128 + tid * 128 + (((k & 7) ^ (tid & 7)) << 4)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            warp_arrive(&ctl.q_ready);
+            softmax_meet();                                 // (paths)
+            const uint32_t *path = ctl.path[in ? (int)((t.row0 + row) / p.G) - i0 : 0];
+
+            float m = neg_inf(), l = 0.f;
+            for (int n = 0; n < part.n; ++n, ++at) {
+                const int b = (int)(at & 1), stage = (int)(at % Shape::stages);
+                const uint32_t phase = (uint32_t)(at >> 1);
+                float x[64];
+                wait(&ctl.s_full[b], phase);
+                fence_after();
+                tmem_read32(lanes + kColS + 64 * b, *reinterpret_cast<float (*)[32]>(x));
+                tmem_read32(lanes + kColS + 64 * b + 32, *reinterpret_cast<float (*)[32]>(x + 32));
+                tmem_wait();
+                fence_before();
+                warp_arrive(&ctl.s_free[b]);
+                const int64_t slot0 = ((int64_t)part.t0 + n) * kAttnTile;
+                const uint64_t valid = (uint64_t)ctl.valid[stage][0] | (uint64_t)ctl.valid[stage][1] << 32;
+                const bool tail = slot0 + kAttnTile > s.seq.len;      // (alike in all threads, whatever went wrong: they meet)
+                unsigned long long odd = 0;
+                uint64_t vis = valid;
+                if (tail) {
+                    const int64_t d = s.seq.len - slot0;     // keys of the prefix
+                    vis &= d <= 0 ? path_bits64(path, (int)-d) : path_bits64(path, 0) << d | ((1ull << d) - 1);
+                }
+                if (vis != ~0ull) {
+#pragma unroll
+                    for (int i = 0; i < 64; ++i)
+                        if (!((i < 32 ? (uint32_t)vis : (uint32_t)(vis >> 32)) >> (i & 31) & 1)) x[i] = neg_inf();
+                }
+                if (tail) {
+                    // values that are not finite, where not every row sees every key: each thread looks at half a key
+                    const uint32_t v = ring + stage * Shape::stage + PANELS * kPanel + (tid >> 1) * 128 + (tid & 1) * 64;
+                    bool bad = false;
+#pragma unroll
+                    for (int k = 0; k < 4 * PANELS; ++k) {
+                        uint32_t w[4];
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(v + (k >> 2) * kPanel + (k & 3) * 16) : "memory");
+                        bad = bad || !(finite_bf16x2(w[0]) && finite_bf16x2(w[1]) && finite_bf16x2(w[2]) && finite_bf16x2(w[3]));
+                    }
+                    softmax_meet();
+                    if (bad) atomicOr(&ctl.odd, 1ull << (tid >> 1));
+                    softmax_meet();
+                    odd = *reinterpret_cast<volatile unsigned long long *>(&ctl.odd);
+                }
+                float t4[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+                for (int i = 4; i < 64; ++i) t4[i & 3] = fmaxf(t4[i & 3], x[i]);
+                const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+                // (m = -inf: nothing seen so far, and O holds nothing of this row)
+                const bool raise = top > m && (m == neg_inf() || (top - m) * c > kRaise);
+                if (__any_sync(0xffffffffu, raise)) {
+                    const float a = raise && m != neg_inf() ? ex2((m - top) * c) : 1.f;
+                    if (raise) m = top;
+                    l *= a;
+                    if (n > 0 && __any_sync(0xffffffffu, a != 1.f)) {
+                        wait(&ctl.pv_done[b ^ 1], (uint32_t)((at - 1) >> 1));
+                        fence_after();
+#pragma unroll
+                        for (int k = 0; k < 2 * PANELS; ++k) {
+                            float o[32];
+                            uint32_t w[32];
+                            tmem_read32(lanes + kColO + 32 * k, o);
+                            tmem_wait();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(o[i] * a);
+                            tmem_write32(lanes + kColO + 32 * k, w);
+                        }
+                    }
+                }
+                const float ref = m == neg_inf() ? 0.f : -m * c;
+                float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < 64; ++i) {
+                    x[i] = ex2(fmaf(x[i], c, ref));
+                    s4[i & 3] += x[i];
+                }
+                l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                if (odd) {
+                    // taken out of the product, and added one by one to the rows that see them
+                    if (n > 0) wait(&ctl.pv_done[b ^ 1], (uint32_t)((at - 1) >> 1));
+                    fence_after();
+                    const uint32_t v = ring + stage * Shape::stage + PANELS * kPanel;
+#pragma unroll 1
+                    for (int k = 0; k < 2 * PANELS; ++k) {
+                        float o[32];
+                        uint32_t w[32];
+                        tmem_read32(lanes + kColO + 32 * k, o);
+                        tmem_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (n == 0) o[i] = 0.f;
+                        for (unsigned long long rest = odd & vis; rest && !second; rest &= rest - 1) {
+                            const int key = __ffsll((long long)rest) - 1;
+                            float weight = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 64; ++i) weight = i == key ? x[i] : weight;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                uint32_t y;
+                                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(y)
+                                             : "r"(v + (k >> 1) * kPanel + key * 128 + ((((k & 1) * 4 + (i >> 2)) ^ (key & 7)) << 4) + (i & 3) * 4) : "memory");
+                                o[2 * i] = fmaf(weight, __uint_as_float(y << 16), o[2 * i]);
+                                o[2 * i + 1] = fmaf(weight, __uint_as_float(y & 0xffff0000u), o[2 * i + 1]);
+                            }
+                        }
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(o[i]);
+                        tmem_write32(lanes + kColO + 32 * k, w);
+                    }
+                    softmax_meet();
+                    if (odd >> (tid >> 1) & 1)
+                        for (int k = 0; k < 4 * PANELS; ++k)
+                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v + (tid >> 1) * 128 + (tid & 1) * 64 + (k >> 2) * kPanel + (k & 3) * 16), "r"(0u) : "memory");
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    if (tid == 0) {
+                        ctl.odd = 0;
+                        if (n == 0) ctl.o_live = at;
+                    }
+                    softmax_meet();
+                }
+                if (at >= 2) wait(&ctl.pv_done[b], phase - 1);
+                fence_after();
+                uint32_t w[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+                    x[2 * i] -= __uint_as_float(w[i] << 16);
+                    x[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
+                }
+                if (!DUP || !second) tmem_write32(lanes + kColP + 64 * b, w);
+                if (!DUP || second) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+                    tmem_write32(lanes + kColP + 64 * b + (DUP ? 0 : 32), w);
+                }
+                tmem_wait_st();
+                fence_before();
+                warp_arrive(&ctl.p_ready[b]);
+            }
+
+            // -------------------------------------------------------- the part's results
+            wait(&ctl.pv_done[(at - 1) & 1], (uint32_t)((at - 1) >> 1));
+            fence_after();
+            if (dead) l = __int_as_float(0x7fc00000);       // what a wait that ran out leaves is no result
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            if (DUP) {      // the second numbers' results, by way of the query tile
+                if (second) {
+#pragma unroll
+                    for (int k = 0; k < 2 * PANELS; ++k) {
+                        float o[32];
+                        tmem_read32(lanes + kColO + 32 * k, o);
+                        tmem_wait();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};"
+                                         ::"r"(q_tile + row * COLS * 4 + (((8 * k + i) ^ (row & 7)) << 4)), "f"(o[4 * i]), "f"(o[4 * i + 1]), "f"(o[4 * i + 2]), "f"(o[4 * i + 3]) : "memory");
+                    }
+                }
+                softmax_meet();
+            }
+            if (!second) {
+#pragma unroll
+                for (int k = 0; k < 2 * PANELS; ++k) {
+                    float o[32];
+                    tmem_read32(lanes + kColO + 32 * k, o);
+                    tmem_wait();
+                    if (!in) continue;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int col = 32 * k + 4 * i;
+                        if (DUP) {
+                            float y[4];
+                            asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(y[0]), "=f"(y[1]), "=f"(y[2]), "=f"(y[3])
+                                         : "r"(q_tile + row * COLS * 4 + (((8 * k + i) ^ (row & 7)) << 4)) : "memory");
+                            o[4 * i] += y[0], o[4 * i + 1] += y[1], o[4 * i + 2] += y[2], o[4 * i + 3] += y[3];
+                        }
+                        if (!t.whole && col < p.D)
+                            __stcg(reinterpret_cast<float4 *>(p.part + ((int64_t)t.slot * ROWS + row) * p.D + col), make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
+                    }
+                    if (t.whole) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (32 * k + 8 * i < p.D)
+                                *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + out_at + 32 * k + 8 * i) =
+                                    make_uint4(pack_bf16(o[8 * i] * inv, o[8 * i + 1] * inv), pack_bf16(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
+                                               pack_bf16(o[8 * i + 4] * inv, o[8 * i + 5] * inv), pack_bf16(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
+                    }
+                }
+                if (!t.whole && in) __stcg(&p.part_ml[(int64_t)t.slot * ROWS + row], make_float2(m * c, l));
+            }
+            fence_before();
+            if (!t.whole) {
+                __threadfence();
+                softmax_meet();
+                if (tid == 0) ctl.last = take_ticket(p.counters + t.first, t.parts);
+                softmax_meet();
+                if (ctl.last) {
+                    __threadfence();
+                    attn_join<ROWS, __nv_bfloat16>(p, s, part, t, tid, kSoftmaxThreads);
+                }
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kTmemCols) : "memory");
+    }
+}
+
+template <int PANELS, bool DUP>
+cudaError_t launch_tc(const AttnParams &p, int dev, cudaStream_t st)
+{
+    static std::atomic<bool> attr_set[64];   // host threads may race to set it: all of them store `true`
+    if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
+        const cudaError_t e = cudaFuncSetAttribute(attention_tc_kernel<PANELS, DUP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   (int)TcShape<PANELS>::smem);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
+    }
+    attention_tc_kernel<PANELS, DUP><<<p.ctas, kTcThreads, TcShape<PANELS>::smem, st>>>(p);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_attention_tc(const AttnParams &p, int rows, int dev, cudaStream_t st)
+{
+    if (rows == 64) return p.D <= 64 ? launch_tc<1, true>(p, dev, st) : launch_tc<2, true>(p, dev, st);
+    return p.D <= 64 ? launch_tc<1, false>(p, dev, st) : launch_tc<2, false>(p, dev, st);
+}
+
+}  // namespace spr

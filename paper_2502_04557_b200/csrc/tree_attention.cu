@@ -4,13 +4,17 @@
 #include "attention.h"
 #include "host_util.h"
 #include "launch.h"
+#include "tensor_pair.cuh"
 
 namespace spr {
 
 namespace {
 
 // most rows of a row block, for the workspace
-int most_rows(int dt) { return dt == SPR_F32 ? 16 : 32; }
+int most_rows(int dt) { return dt == SPR_F32 ? 16 : 128; }
+
+thread_local int t_test_flags = 0;
+thread_local unsigned t_spin_limit = 0;
 
 }  // namespace
 
@@ -18,7 +22,7 @@ int attention_block_rows(int T, int G, int dt)
 {
     const int64_t rows = (int64_t)T * G;
     if (dt == SPR_F32) return rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
-    return rows <= 16 ? 16 : 32;
+    return rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
 }
 
 size_t attention_ws_bytes(int D, int dt)
@@ -74,9 +78,17 @@ int tree_attention(const void *q, const void *k_cache, const void *v_cache, int 
     p.counters = at<int>(ws, w.counters);
     p.part = at<float>(ws, w.part);
     p.part_ml = at<float2>(ws, w.part_ml);
+    p.spin_limit = t_spin_limit ? t_spin_limit : pairtc::kSpinLimit;
+    p.test_flags = t_test_flags;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (dt == SPR_F32) return finish(launch_attention_f32(p, rows, st));
-    return finish(launch_attention_mma(p, rows, dev, st));
+    return finish(rows == 16 ? launch_attention_mma(p, dev, st) : launch_attention_tc(p, rows, dev, st));
+}
+
+void spr_test_tree_attention(int flags, unsigned spin_limit)
+{
+    t_test_flags = flags & ATTN_TEST_NO_LOADS;
+    t_spin_limit = spin_limit;
 }
 
 }  // extern "C"

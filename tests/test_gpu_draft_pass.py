@@ -323,6 +323,22 @@ def test_attention_runs_alike(spr, dtype):
     assert torch.equal(b, a) and torch.equal(c, a)
 
 
+def test_attention_timeout(spr):
+    """No tile is ever loaded: every wait runs out, results are NaN, and the workspace stays usable."""
+    x = attend_case(2, 3, 8, 2, 64, 16, BF16, seed=35, lens=[3000, 20])
+    ws = workspace(spr, spr.OP_TREE_ATTENTION, 64)
+    want = run_attend(spr, x, ws=ws)
+    for T, G in ((5, 4), (40, 4)):
+        y = attend_case(2, T, 2 * G, 2, 64, 16, BF16, seed=36, lens=[3000, 20])
+        spr.lib().spr_test_tree_attention(1, 2000)
+        try:
+            got = run_attend(spr, y, status=TIMEOUT, ws=ws)
+        finally:
+            spr.lib().spr_test_tree_attention(0, 0)
+        assert bool(got.isnan().all())
+    assert torch.equal(run_attend(spr, x, ws=ws), want)
+
+
 # ---------------------------------------------------------------------------- logits_rules
 
 
