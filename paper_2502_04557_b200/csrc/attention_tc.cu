@@ -4,10 +4,12 @@
 //
 // One CTA per SM walks its stretch of tiles.  Two loader warps bring keys and values into a ring (cp.async, 16 bytes per
 // lane, into the 128-byte swizzle that the matrix descriptors name: pages of 16 entries would be 2 KB boxes for the copy
-// engine, whose number sets its time).  One thread issues the products: S of the next tile goes ahead of P V of
-// this one, S and P are double-buffered.  Four softmax warps have a row per thread.  The maximum that exponents are
-// taken against is only raised when a score passes it by 2^8 (weights then stay below 2^8, and sums and
-// products in fp32 keep their relative precision), so that O, which lives in TMEM, is hardly ever rescaled.
+// engine, whose number sets its time).  One thread issues the products: S of the next tiles goes ahead of P V of this one.
+// Two groups of four softmax warps take tiles in turn, a row per thread, each with its own maxima, sums, S, P and O
+// (all 512 columns of TMEM are in use): a tile takes a warp some thousand clocks, much of it latency, and the groups
+// wait for nothing of one another until the end of a part.  The maximum that exponents are taken against is only
+// raised when a score passes it by 2^8 (weights then stay below 2^8, and sums and products in fp32 keep their relative
+// precision), so that O is hardly ever rescaled.
 //
 // Weights are used as two bf16 numbers, their rounding and what is left of it: one would put an error of 2^-9 on the
 // result, as much as its own rounding.  Up to 64 rows (DUP) the tile's other half holds the same queries again and
@@ -21,6 +23,7 @@
 #include "host_util.h"
 #include "launch.h"
 #include "tensor_pair.cuh"
+#include "vocab_common.cuh"
 
 namespace spr {
 
@@ -28,20 +31,20 @@ namespace {
 
 using namespace pairtc;
 
-constexpr int kTcThreads = 256;
-constexpr int kSoftmaxThreads = 128;
-constexpr int kMmaWarp = 4, kFirstLoader = 6, kLoaders = 2;      // (warp 5 only makes registers come out even)
+constexpr int kTcThreads = 384;
+constexpr int kSoftmaxThreads = 256;                            // two groups of 128
+constexpr int kMmaWarp = 8, kFirstLoader = 10, kLoaders = 2;     // (a warp of each four of a kind: registers go by fours)
 constexpr int kPanel = kAttnTile * 128;                         // 64 keys by 64 columns
 constexpr float kRaise = 8.f;                                   // by how much scores may pass the maximum in use
 // TMEM columns
-constexpr int kColS = 0, kColP = 128, kColO = 256, kTmemCols = 512;       // P: 2 buffers of 32 columns, each twice
+constexpr int kColS = 0, kColP = 128, kColO = 256, kTmemCols = 512;       // two of each: 64, 2 x 32 and 128 columns
 
 template <int PANELS>
 struct TcShape {
     static constexpr int stage = 2 * PANELS * kPanel;            // keys, then values
     static constexpr int stages = PANELS == 2 ? 5 : 10;
     static constexpr int behind = stages - 3;                    // copies of as many tiles are in flight behind the newest
-    static constexpr int q_bytes = PANELS * 128 * 128;
+    static constexpr int q_bytes = PANELS == 2 ? 32768 : 24576;  // queries; later results of up to three quarters of the block's pieces
     static constexpr size_t smem = (size_t)q_bytes + (size_t)stages * stage + 1024;
 };
 
@@ -51,15 +54,17 @@ struct TcControl {
     uint64_t q_ready, drain;
     uint32_t valid[10][kLoaders];            // a bit for each key of the stage's tile that is there
     int64_t scratch[2 * (kTcThreads / 32) + 4];
-    unsigned long long odd;
-    int64_t o_live;
+    unsigned long long odd[2];
+    int64_t o_live[2];
+    float2 ml[2][128];
     uint32_t tmem;
     int abort, last;
     int tree[kMaxTreeNodes];
     uint32_t path[128][kMaxTreeNodes / 32];
 };
 
-__device__ __forceinline__ void softmax_meet() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void softmax_meet() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ void group_meet(int group) { asm volatile("bar.sync %0, 128;" ::"r"(2 + group) : "memory"); }
 __device__ __forceinline__ void arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there)
 {
@@ -131,11 +136,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             bar_init(&ctl.p_ready[i], 4);
             bar_init(&ctl.pv_done[i], 1);
         }
-        bar_init(&ctl.q_ready, 4);
+        bar_init(&ctl.q_ready, 8);
         bar_init(&ctl.drain, 1);
         ctl.abort = 0;
-        ctl.odd = 0;
-        ctl.o_live = -1;
+        ctl.odd[0] = ctl.odd[1] = 0;
+        ctl.o_live[0] = ctl.o_live[1] = -1;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kMmaWarp) {
@@ -205,14 +210,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                     }
                     if (lane == 0) ctl.valid[stage][half] = valid;
                     const uint32_t dst = ring + stage * Shape::stage + c_dst;
+                    const bool all = valid == 0xffffffffu;
 #pragma unroll
-                    for (int i = 0; i < 32 / kRowsAtOnce; ++i) {
-                        const int r0 = i * kRowsAtOnce, r = r0 + c_row;
-                        const bool there = c_in && (valid >> r & 1);
-                        const int64_t at = there ? ((int64_t)run[r0 >> 3] + (r & 7)) * p.D + c_chunk * 8 : 0;
-                        const uint32_t to = (dst + r0 * 128) ^ ((r0 & 7) << 4);
-                        copy16(to, static_cast<const __nv_bfloat16 *>(p.k) + at, there);
-                        copy16(to + PANELS * kPanel, static_cast<const __nv_bfloat16 *>(p.v) + at, there);
+                    for (int r = 0; r < 4; ++r) {
+                        const int64_t from = run[r] < 0 ? 0 : ((int64_t)run[r] + c_row) * p.D + c_chunk * 8;
+                        const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(p.k) + from, *v = static_cast<const __nv_bfloat16 *>(p.v) + from;
+#pragma unroll
+                        for (int i = 0; i < 8 / kRowsAtOnce; ++i) {
+                            const int r0 = i * kRowsAtOnce;
+                            const bool there = c_in && (all || (valid >> (8 * r + r0 + c_row) & 1));
+                            const uint32_t to = (dst + (8 * r + r0) * 128) ^ (r0 << 4);
+                            copy16(to, there ? k : p.k, there);
+                            copy16(to + PANELS * kPanel, there ? v : p.v, there);
+                            k += kRowsAtOnce * p.D, v += kRowsAtOnce * p.D;
+                        }
                     }
                     asm volatile("cp.async.commit_group;" ::: "memory");
                     if (issued >= Shape::behind) {
@@ -253,31 +264,35 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             while (alive && attn_next<ROWS>(p, s, part)) {
                 if (!wait(&ctl.q_ready, parts++)) break;
                 scores(at);
+                if (part.n > 1) scores(at + 1);
                 for (int n = 0; alive && n < part.n; ++n, ++at) {
-                    if (n + 1 < part.n) scores(at + 1);
                     const int stage = (int)(at % Shape::stages), b = (int)(at & 1);
                     if (!wait(&ctl.p_ready[b], (uint32_t)(at >> 1))) break;
                     fence_after();
                     const uint32_t v = ring + stage * Shape::stage + PANELS * kPanel;
-                    const bool live = n > 0 || *reinterpret_cast<volatile int64_t *>(&ctl.o_live) == at;
+                    const bool live = n > 1 || *reinterpret_cast<volatile int64_t *>(&ctl.o_live[b]) == at;
+                    const uint32_t o = tmem + kColO + 128 * b, w = tmem + kColP + 64 * b;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        mma_tmem(tmem + kColO, tmem + kColP + 64 * b + 8 * q, tile_desc(v + q * 2048, true), kPv, live || q != 0);
-                        if (!DUP) mma_tmem(tmem + kColO, tmem + kColP + 64 * b + 32 + 8 * q, tile_desc(v + q * 2048, true), kPv, 1u);
+                        mma_tmem(o, w + 8 * q, tile_desc(v + q * 2048, true), kPv, live || q != 0);
+                        if (!DUP) mma_tmem(o, w + 32 + 8 * q, tile_desc(v + q * 2048, true), kPv, 1u);
                     }
                     commit(&ctl.pv_done[b]);
                     commit(&ctl.empty[stage]);
+                    if (n + 2 < part.n) scores(at + 2);
                 }
             }
             commit(&ctl.drain);             // nothing of this CTA's products is left when its TMEM is given back
             bar_wait_quiet(&ctl.drain, 0, limit);
         }
         __syncwarp();
-    } else if (warp < 4) {
+    } else if (warp < 8) {
         // ------------------------------------------------------------ softmax: a row per thread
-        const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
-        const int row = DUP ? tid & 63 : tid;               // in the block
-        const bool second = DUP && tid >= 64;               // this thread's weights are what rounding left
+        const int group = warp >> 2, gid = tid & 127;
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t col_s = lanes + kColS + 64 * group, col_p = lanes + kColP + 64 * group, col_o = lanes + kColO + 128 * group;
+        const int row = DUP ? gid & 63 : gid;               // in the block
+        const bool second = DUP && gid >= 64;               // this thread's weights are what rounding left
         const float c = p.abs_scale_log2;
         AttnPart part;
         int64_t at = 0;
@@ -309,12 +324,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             const int64_t out_at = in ? attn_out_at(p, s, part, t.row0 + row) : 0;
             {
                 const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + out_at);
+                // (the groups have half of it each)
 #pragma unroll
-                for (int k = 0; k < 8 * PANELS; ++k) {
+                for (int i = 0; i < 4 * PANELS; ++i) {
+                    const int k = group * 4 * PANELS + i;
                     uint4 x = in && k * 8 < p.D ? __ldg(src + k) : make_uint4(0u, 0u, 0u, 0u);
                     x.x ^= p.flip, x.y ^= p.flip, x.z ^= p.flip, x.w ^= p.flip;
                     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};"
-                                 ::"r"(q_tile + (k >> 3) * 128 * 128 + tid * 128 + (((k & 7) ^ (tid & 7)) << 4)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+                                 ::"r"(q_tile + (k >> 3) * 128 * 128 + gid * 128 + (((k & 7) ^ (gid & 7)) << 4)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -323,18 +340,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             const uint32_t *path = ctl.path[in ? (int)((t.row0 + row) / p.G) - i0 : 0];
 
             float m = neg_inf(), l = 0.f;
-            for (int n = 0; n < part.n; ++n, ++at) {
-                const int b = (int)(at & 1), stage = (int)(at % Shape::stages);
-                const uint32_t phase = (uint32_t)(at >> 1);
+            int64_t mine = at + ((at ^ group) & 1);             // this group's next tile
+            const int64_t end = at + part.n;
+            const bool any = mine < end;
+            for (bool begun = false; mine < end; mine += 2, begun = true) {
+                const int stage = (int)(mine % Shape::stages);
+                const uint32_t phase = (uint32_t)(mine >> 1);
                 float x[64];
-                wait(&ctl.s_full[b], phase);
+                wait(&ctl.s_full[group], phase);
                 fence_after();
-                tmem_read32(lanes + kColS + 64 * b, *reinterpret_cast<float (*)[32]>(x));
-                tmem_read32(lanes + kColS + 64 * b + 32, *reinterpret_cast<float (*)[32]>(x + 32));
+                tmem_read32(col_s, *reinterpret_cast<float (*)[32]>(x));
+                tmem_read32(col_s + 32, *reinterpret_cast<float (*)[32]>(x + 32));
                 tmem_wait();
                 fence_before();
-                warp_arrive(&ctl.s_free[b]);
-                const int64_t slot0 = ((int64_t)part.t0 + n) * kAttnTile;
+                warp_arrive(&ctl.s_free[group]);
+                const int64_t slot0 = (part.t0 + (mine - at)) * kAttnTile;
                 const uint64_t valid = (uint64_t)ctl.valid[stage][0] | (uint64_t)ctl.valid[stage][1] << 32;
                 const bool tail = slot0 + kAttnTile > s.seq.len;      // (alike in all threads, whatever went wrong: they meet)
                 unsigned long long odd = 0;
@@ -350,7 +370,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 }
                 if (tail) {
                     // values that are not finite, where not every row sees every key: each thread looks at half a key
-                    const uint32_t v = ring + stage * Shape::stage + PANELS * kPanel + (tid >> 1) * 128 + (tid & 1) * 64;
+                    const uint32_t v = ring + stage * Shape::stage + PANELS * kPanel + (gid >> 1) * 128 + (gid & 1) * 64;
                     bool bad = false;
 #pragma unroll
                     for (int k = 0; k < 4 * PANELS; ++k) {
@@ -358,58 +378,63 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                         asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(v + (k >> 2) * kPanel + (k & 3) * 16) : "memory");
                         bad = bad || !(finite_bf16x2(w[0]) && finite_bf16x2(w[1]) && finite_bf16x2(w[2]) && finite_bf16x2(w[3]));
                     }
-                    softmax_meet();
-                    if (bad) atomicOr(&ctl.odd, 1ull << (tid >> 1));
-                    softmax_meet();
-                    odd = *reinterpret_cast<volatile unsigned long long *>(&ctl.odd);
+                    group_meet(group);
+                    if (bad) atomicOr(&ctl.odd[group], 1ull << (gid >> 1));
+                    group_meet(group);
+                    odd = *reinterpret_cast<volatile unsigned long long *>(&ctl.odd[group]);
                 }
                 float t4[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-                for (int i = 4; i < 64; ++i) t4[i & 3] = fmaxf(t4[i & 3], x[i]);
+                for (int i = 4; i < 64; i += 2) t4[(i >> 1) & 3] = fmaxf(fmaxf(t4[(i >> 1) & 3], x[i]), x[i + 1]);
                 const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
                 // (m = -inf: nothing seen so far, and O holds nothing of this row)
                 const bool raise = top > m && (m == neg_inf() || (top - m) * c > kRaise);
+                const bool waited = __any_sync(0xffffffffu, raise) && begun;
+                if (begun && mine >= 2 && (waited || odd)) wait(&ctl.pv_done[group], phase - 1);
                 if (__any_sync(0xffffffffu, raise)) {
                     const float a = raise && m != neg_inf() ? ex2((m - top) * c) : 1.f;
                     if (raise) m = top;
                     l *= a;
-                    if (n > 0 && __any_sync(0xffffffffu, a != 1.f)) {
-                        wait(&ctl.pv_done[b ^ 1], (uint32_t)((at - 1) >> 1));
+                    if (begun && __any_sync(0xffffffffu, a != 1.f)) {
                         fence_after();
-#pragma unroll
+#pragma unroll 1
                         for (int k = 0; k < 2 * PANELS; ++k) {
                             float o[32];
                             uint32_t w[32];
-                            tmem_read32(lanes + kColO + 32 * k, o);
+                            tmem_read32(col_o + 32 * k, o);
                             tmem_wait();
 #pragma unroll
                             for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(o[i] * a);
-                            tmem_write32(lanes + kColO + 32 * k, w);
+                            tmem_write32(col_o + 32 * k, w);
                         }
                     }
                 }
                 const float ref = m == neg_inf() ? 0.f : -m * c;
-                float s4[4] = {0.f, 0.f, 0.f, 0.f};
+                const uint64_t c2 = pack2(c, c), ref2 = pack2(ref, ref);
+                uint64_t s2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
 #pragma unroll
-                for (int i = 0; i < 64; ++i) {
-                    x[i] = ex2(fmaf(x[i], c, ref));
-                    s4[i & 3] += x[i];
+                for (int i = 0; i < 32; ++i) {
+                    unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), c2, ref2), x[2 * i], x[2 * i + 1]);
+                    x[2 * i] = ex2(x[2 * i]);
+                    x[2 * i + 1] = ex2(x[2 * i + 1]);
+                    s2[i & 1] = add2(s2[i & 1], pack2(x[2 * i], x[2 * i + 1]));
                 }
-                l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                float sum0, sum1;
+                unpack2(add2(s2[0], s2[1]), sum0, sum1);
+                l += sum0 + sum1;
                 if (odd) {
                     // taken out of the product, and added one by one to the rows that see them
-                    if (n > 0) wait(&ctl.pv_done[b ^ 1], (uint32_t)((at - 1) >> 1));
                     fence_after();
                     const uint32_t v = ring + stage * Shape::stage + PANELS * kPanel;
 #pragma unroll 1
                     for (int k = 0; k < 2 * PANELS; ++k) {
                         float o[32];
                         uint32_t w[32];
-                        tmem_read32(lanes + kColO + 32 * k, o);
+                        tmem_read32(col_o + 32 * k, o);
                         tmem_wait();
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (n == 0) o[i] = 0.f;
+                            if (!begun) o[i] = 0.f;
                         for (unsigned long long rest = odd & vis; rest && !second; rest &= rest - 1) {
                             const int key = __ffsll((long long)rest) - 1;
                             float weight = 0.f;
@@ -427,89 +452,98 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                         __syncwarp();
 #pragma unroll
                         for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(o[i]);
-                        tmem_write32(lanes + kColO + 32 * k, w);
+                        tmem_write32(col_o + 32 * k, w);
                     }
-                    softmax_meet();
-                    if (odd >> (tid >> 1) & 1)
+                    group_meet(group);
+                    if (odd >> (gid >> 1) & 1)
                         for (int k = 0; k < 4 * PANELS; ++k)
-                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v + (tid >> 1) * 128 + (tid & 1) * 64 + (k >> 2) * kPanel + (k & 3) * 16), "r"(0u) : "memory");
+                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v + (gid >> 1) * 128 + (gid & 1) * 64 + (k >> 2) * kPanel + (k & 3) * 16), "r"(0u) : "memory");
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    if (tid == 0) {
-                        ctl.odd = 0;
-                        if (n == 0) ctl.o_live = at;
+                    if (gid == 0) {
+                        ctl.odd[group] = 0;
+                        if (!begun) ctl.o_live[group] = mine;
                     }
-                    softmax_meet();
+                    group_meet(group);
                 }
-                if (at >= 2) wait(&ctl.pv_done[b], phase - 1);
+                if (mine >= 2 && !(begun && (waited || odd))) wait(&ctl.pv_done[group], phase - 1);
                 fence_after();
                 uint32_t w[32];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-                    x[2 * i] -= __uint_as_float(w[i] << 16);
-                    x[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
-                }
-                if (!DUP || !second) tmem_write32(lanes + kColP + 64 * b, w);
+                for (int i = 0; i < 32; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+                if (!DUP || !second) tmem_write32(col_p, w);
                 if (!DUP || second) {
+                    const uint64_t minus = pack2(-1.f, -1.f);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-                    tmem_write32(lanes + kColP + 64 * b + (DUP ? 0 : 32), w);
+                    for (int i = 0; i < 32; ++i) {
+                        float a, b;
+                        unpack2(fma2(pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)), minus, pack2(x[2 * i], x[2 * i + 1])), a, b);
+                        w[i] = pack_bf16(a, b);
+                    }
+                    tmem_write32(col_p + (DUP ? 0 : 32), w);
                 }
                 tmem_wait_st();
                 fence_before();
-                warp_arrive(&ctl.p_ready[b]);
+                warp_arrive(&ctl.p_ready[group]);
             }
+            at = end;
 
-            // -------------------------------------------------------- the part's results
-            wait(&ctl.pv_done[(at - 1) & 1], (uint32_t)((at - 1) >> 1));
+            // -------------------------------------------------------- the part's results: both groups', and both numbers'
+            if (any) wait(&ctl.pv_done[group], (uint32_t)((mine - 2) >> 1));
             fence_after();
             if (dead) l = __int_as_float(0x7fc00000);       // what a wait that ran out leaves is no result
+            ctl.ml[group][gid] = make_float2(m, l);
+            softmax_meet();
+            const float2 other = ctl.ml[group ^ 1][gid];
+            const float top = fmaxf(m, other.x), shift = top == neg_inf() ? 0.f : top;
+            const float mine_by = any ? ex2((m - shift) * c) : 0.f;
+            l = l * ex2((m - shift) * c) + other.y * ex2((other.x - shift) * c);
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            if (DUP) {      // the second numbers' results, by way of the query tile
-                if (second) {
+            const bool last_hand = group == 0 && !second;       // adds up and writes
+            // the others' results go through the query tile, 32 columns at a time
+            constexpr int kPieces = DUP ? 3 : 1;
+            const uint32_t piece = q_tile + (DUP ? 2 * group + (second ? 1 : 0) - 1 : 0) * ROWS * 128;
+#pragma unroll 1
+            for (int k = 0; k < 2 * PANELS; ++k) {
+                float o[32];
+                tmem_read32(col_o + 32 * k, o);
+                tmem_wait();
 #pragma unroll
-                    for (int k = 0; k < 2 * PANELS; ++k) {
-                        float o[32];
-                        tmem_read32(lanes + kColO + 32 * k, o);
-                        tmem_wait();
+                for (int i = 0; i < 32; ++i) o[i] = any ? o[i] * mine_by : 0.f;        // (without a tile O is not this part's)
+                if (!last_hand) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};"
-                                         ::"r"(q_tile + row * COLS * 4 + (((8 * k + i) ^ (row & 7)) << 4)), "f"(o[4 * i]), "f"(o[4 * i + 1]), "f"(o[4 * i + 2]), "f"(o[4 * i + 3]) : "memory");
+                    for (int i = 0; i < 8; ++i)
+                        asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};"
+                                     ::"r"(piece + row * 128 + ((i ^ (row & 7)) << 4)), "f"(o[4 * i]), "f"(o[4 * i + 1]), "f"(o[4 * i + 2]), "f"(o[4 * i + 3]) : "memory");
+                }
+                softmax_meet();
+                if (last_hand && in) {
+#pragma unroll
+                    for (int h = 0; h < kPieces; ++h)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            float y[4];
+                            asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(y[0]), "=f"(y[1]), "=f"(y[2]), "=f"(y[3])
+                                         : "r"(q_tile + h * ROWS * 128 + row * 128 + ((i ^ (row & 7)) << 4)) : "memory");
+                            o[4 * i] += y[0], o[4 * i + 1] += y[1], o[4 * i + 2] += y[2], o[4 * i + 3] += y[3];
+                        }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int col = 32 * k + 8 * i;
+                        if (col >= p.D) continue;
+                        if (t.whole) {
+                            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + out_at + col) =
+                                make_uint4(pack_bf16(o[8 * i] * inv, o[8 * i + 1] * inv), pack_bf16(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
+                                           pack_bf16(o[8 * i + 4] * inv, o[8 * i + 5] * inv), pack_bf16(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
+                        } else {
+                            float4 *to = reinterpret_cast<float4 *>(p.part + ((int64_t)t.slot * ROWS + row) * p.D + col);
+                            __stcg(to, make_float4(o[8 * i], o[8 * i + 1], o[8 * i + 2], o[8 * i + 3]));
+                            __stcg(to + 1, make_float4(o[8 * i + 4], o[8 * i + 5], o[8 * i + 6], o[8 * i + 7]));
+                        }
                     }
                 }
                 softmax_meet();
             }
-            if (!second) {
-#pragma unroll
-                for (int k = 0; k < 2 * PANELS; ++k) {
-                    float o[32];
-                    tmem_read32(lanes + kColO + 32 * k, o);
-                    tmem_wait();
-                    if (!in) continue;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int col = 32 * k + 4 * i;
-                        if (DUP) {
-                            float y[4];
-                            asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(y[0]), "=f"(y[1]), "=f"(y[2]), "=f"(y[3])
-                                         : "r"(q_tile + row * COLS * 4 + (((8 * k + i) ^ (row & 7)) << 4)) : "memory");
-                            o[4 * i] += y[0], o[4 * i + 1] += y[1], o[4 * i + 2] += y[2], o[4 * i + 3] += y[3];
-                        }
-                        if (!t.whole && col < p.D)
-                            __stcg(reinterpret_cast<float4 *>(p.part + ((int64_t)t.slot * ROWS + row) * p.D + col), make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
-                    }
-                    if (t.whole) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (32 * k + 8 * i < p.D)
-                                *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + out_at + 32 * k + 8 * i) =
-                                    make_uint4(pack_bf16(o[8 * i] * inv, o[8 * i + 1] * inv), pack_bf16(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
-                                               pack_bf16(o[8 * i + 4] * inv, o[8 * i + 5] * inv), pack_bf16(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
-                    }
-                }
-                if (!t.whole && in) __stcg(&p.part_ml[(int64_t)t.slot * ROWS + row], make_float2(m * c, l));
-            }
+            if (!t.whole && last_hand && in) __stcg(&p.part_ml[(int64_t)t.slot * ROWS + row], make_float2(top * c, l));
             fence_before();
             if (!t.whole) {
                 __threadfence();
