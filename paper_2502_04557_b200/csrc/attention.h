@@ -9,7 +9,8 @@
 namespace spr {
 
 constexpr int kAttnTile = 64;            // keys per tile, the unit in which work is dealt out
-constexpr int kAttnMaxCtas = 148;        // one CTA per SM
+constexpr int kAttnCtasPerSm = 2;
+constexpr int kAttnMaxCtas = 148 * kAttnCtasPerSm;
 constexpr int kAttnMaxDim = 128;
 
 struct AttnParams {

@@ -3,7 +3,7 @@
 // A warp walks its keys on its own, with a running maximum and sum: a lane holds E columns of all the block's queries
 // and of their results in registers, a key's row is one coalesced load, and the products of a key with the block's ROWS
 // queries are added up over the lanes by halves (half of the rows to the other half of the lanes, five times over), so
-// that ROWS scores cost some ROWS shuffles.  The eight warps of a CTA take eight keys of a tile each and are joined
+// that ROWS scores cost some ROWS shuffles.  The four warps of a CTA take 16 keys of a tile each and are joined
 // through shared memory at the end of a part.  Up to 16 rows the loads bound it, above that the block is read again.
 #include "attention_plan.cuh"
 #include "host_util.h"
@@ -13,9 +13,9 @@ namespace spr {
 
 namespace {
 
-constexpr int kF32Threads = 256;
+constexpr int kF32Threads = 128;
 constexpr int kF32Warps = kF32Threads / 32;
-constexpr int kKeys = 8;             // of a tile, per warp
+constexpr int kKeys = kAttnTile / kF32Warps;    // of a tile, per warp
 constexpr int kGroup = 4;            // keys worked on at once
 
 template <int E>
@@ -37,7 +37,7 @@ struct Cols {
 };
 
 template <int ROWS, int E>
-__global__ void __launch_bounds__(kF32Threads, 1) attention_f32_kernel(const AttnParams p)
+__global__ void __launch_bounds__(kF32Threads, 2) attention_f32_kernel(const AttnParams p)
 {
     constexpr int kLanes = 32 / ROWS;               // lanes that share a row's score
     __shared__ int64_t scratch[2 * kF32Warps + 4];
@@ -176,11 +176,17 @@ __global__ void __launch_bounds__(kF32Threads, 1) attention_f32_kernel(const Att
         int64_t rows = find(part.t0), next = -1;
         fetch(rows, 0, kk, vv);
         for (int n = 0; n < part.n; ++n) {
-            fetch(rows, 1, kn, vn);
             if (n + 1 < part.n) next = find(part.t0 + n + 1);
-            use(rows, part.t0 + n, 0, kk, vv);
-            if (n + 1 < part.n) fetch(next, 0, kk, vv);
-            use(rows, part.t0 + n, 1, kn, vn);
+#pragma unroll
+            for (int g = 0; g < kKeys / kGroup; g += 2) {
+                fetch(rows, g + 1, kn, vn);
+                use(rows, part.t0 + n, g, kk, vv);
+                if (g + 2 < kKeys / kGroup)
+                    fetch(rows, g + 2, kk, vv);
+                else if (n + 1 < part.n)
+                    fetch(next, 0, kk, vv);
+                use(rows, part.t0 + n, g + 1, kn, vn);
+            }
             rows = next;
         }
 
@@ -224,7 +230,7 @@ __global__ void __launch_bounds__(kF32Threads, 1) attention_f32_kernel(const Att
             __syncthreads();
             if (last) {
                 __threadfence();
-                attn_join<ROWS, float>(p, s, part, t, tid, kF32Threads);
+                attn_join<ROWS, float>(p, s, part, t, warp, kF32Warps);
             }
         }
     }
@@ -233,12 +239,7 @@ __global__ void __launch_bounds__(kF32Threads, 1) attention_f32_kernel(const Att
 template <int ROWS, int E>
 cudaError_t launch_rows(const AttnParams &p, cudaStream_t st)
 {
-    const size_t smem = sizeof(float) * kF32Warps * ROWS * p.D;
-    if (smem > 40000) {
-        const cudaError_t e = cudaFuncSetAttribute(attention_f32_kernel<ROWS, E>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   (int)sizeof(float) * kF32Warps * ROWS * kAttnMaxDim);
-        if (e != cudaSuccess) return e;
-    }
+    const size_t smem = sizeof(float) * kF32Warps * ROWS * p.D;      // 32 KB at most
     attention_f32_kernel<ROWS, E><<<p.ctas, kF32Threads, smem, st>>>(p);
     return cudaGetLastError();
 }

@@ -1,10 +1,10 @@
 // tree_attention on bf16 tensors, few rows per cached head (decoding, chains).
 //
 // out_i = sum_j softmax_j(scale q_i . k_j) v_j in one pass over the keys, with a running maximum and sum.  Bound by the
-// read of the caches: a key and its value (4 D bytes) meet ROWS queries.  The eight warps of a CTA form two teams that take
-// tiles of 64 keys in turn, each warp 16 of a tile's keys, which it brings into a ring of its own (cp.async, 16 bytes per
+// read of the caches: a key and its value (4 D bytes) meet ROWS queries.  Each of a CTA's four warps takes 16 keys of
+// every tile of 64, which it brings into a ring of its own (cp.async, 16 bytes per
 // lane, three to five steps ahead) and works on alone: it has its own maxima, sums and results (mma.sync m16n8k16, the
-// block's rows as M), and warps meet only at the end of a part.  Copies by lanes take pages as they come: the copy
+// block's rows as M), and warps meet only at the end of a part, behind which the SM's other CTA goes on.  Copies by lanes take pages as they come: the copy
 // engine's boxes of a page of 16 entries are 2 KB each, and their number, not their bytes, sets the time (64 sequences
 // of 4096 tokens, 8 heads of 128: 195 us with such boxes).  mma.sync suffices here: at 16 rows a tile of 32 KB (the time of
 // 1400 clocks at the memory's rate) takes 128 products per tensor core, some 300 clocks; tcgen05's smallest tile has 64 rows.
@@ -26,9 +26,8 @@ namespace {
 using pairtc::pack_bf16;
 using pairtc::smem_addr;
 
-constexpr int kMmaThreads = 256;
+constexpr int kMmaThreads = 128;
 constexpr int kMmaWarps = kMmaThreads / 32;
-constexpr int kTeams = 2;
 constexpr int kJoinCols = 32;                           // columns that are joined at once
 constexpr int kJoinPitch = kJoinCols + 4;               // floats per row of the joining buffer
 constexpr int kJoinBytes = kMmaWarps * 16 * kJoinPitch * 4;
@@ -80,7 +79,7 @@ __device__ __forceinline__ bool finite_bf16x2(uint32_t w) { return (w & 0x7f80u)
 
 // MT: row tiles of 16; PANELS: 64-column halves of the head dimension
 template <int MT, int PANELS>
-__global__ void __launch_bounds__(kMmaThreads, 1) attention_mma_kernel(const AttnParams p)
+__global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const AttnParams p)
 {
     constexpr int ROWS = 16 * MT, KSTEPS = 4 * PANELS, NTILES = 8 * PANELS;
     using Shape = MmaShape<PANELS>;
@@ -90,7 +89,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) attention_mma_kernel(const Att
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t ring = smem_addr(raw) + warp * Shape::stages * Shape::step;
     float *join = reinterpret_cast<float *>(raw + (size_t)kMmaWarps * Shape::stages * Shape::step);
-    const int team = warp / (kMmaWarps / kTeams), w16 = (warp % (kMmaWarps / kTeams)) * 16;     // keys w16 .. + 15 of a tile
+    const int w16 = warp * 16;                              // keys w16 .. + 15 of a tile
     const int64_t capacity = (int64_t)p.max_pages * p.page_size;
 
     AttnStretch s = attn_plan<ROWS, kMmaThreads>(p, ctl.scratch);
@@ -100,13 +99,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1) attention_mma_kernel(const Att
     AttnStretch ahead = s;
     AttnPart next_part = {0, 0, 0, 0};
     bool more = true;
-    int next_tile = 0, end_tile = 0, left_rows = 0;     // this team's next tile; left_rows: steps whose rows are in `rows`
-    int64_t next_taken = 0;
+    int next_tile = 0, end_tile = 0, left_rows = 0;     // the next tile; left_rows: steps whose rows are in `rows`
     int64_t next_keys = 0;
     int next_stage = 0;
     int rows = -1, rows_behind = -1;                    // lane 2 j + r: row of the caches where run r (8 keys) of step j begins
     auto find = [&](int tile) {                         // for 16 steps from this tile on
-        const int t = tile + kTeams * (lane >> 1);
+        const int t = tile + (lane >> 1);
         const int64_t slot = (int64_t)t * kAttnTile + w16 + 8 * (lane & 1);
         if (t >= end_tile || slot >= next_keys) return -1;
         const uint32_t at = (uint32_t)((uint64_t)slot >> 3) / (uint32_t)(p.page_size >> 3);       // pages are whole runs
@@ -123,7 +121,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) attention_mma_kernel(const Att
     const bool c_in = c_chunk * 8 < p.D;
     const uint32_t c_dst = c_row * Shape::row + ((c_chunk ^ c_row) << 4);
     auto issue = [&]() {
-        while (more && next_tile >= end_tile) {         // on to the next part that has a tile for this team
+        while (more && next_tile >= end_tile) {         // on to the next part
             more = attn_next<ROWS>(p, ahead, next_part);
             if (!more) break;
             next_keys = (int64_t)ahead.seq.len + ahead.seq.count;
@@ -131,9 +129,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) attention_mma_kernel(const Att
                 raise_status(p.status, SPR_ERR_BAD_PAGE);
                 next_keys = capacity;
             }
-            next_tile = next_part.t0 + (int)((next_taken ^ team) & 1);
+            next_tile = next_part.t0;
             end_tile = next_part.t0 + next_part.n;
-            next_taken += next_part.n;
             left_rows = 0;
             rows_behind = find(next_tile);
         }
@@ -141,7 +138,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) attention_mma_kernel(const Att
             if (left_rows == 0) {
                 rows = rows_behind;
                 left_rows = 16;
-                rows_behind = find(next_tile + 16 * kTeams);
+                rows_behind = find(next_tile + 16);
             }
             const int from = 2 * (16 - left_rows);
             const uint32_t dst = ring + next_stage * Shape::step + c_dst;
@@ -158,7 +155,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) attention_mma_kernel(const Att
                 copy16(to, static_cast<const __nv_bfloat16 *>(p.k) + at, there);
                 copy16(to + 16 * Shape::row, static_cast<const __nv_bfloat16 *>(p.v) + at, there);
             }
-            next_tile += kTeams;
+            ++next_tile;
             --left_rows;
         }
         copies_commit();
@@ -175,19 +172,19 @@ __global__ void __launch_bounds__(kMmaThreads, 1) attention_mma_kernel(const Att
     const int swz = lane & 7;                               // both rows are lane & 7 modulo 8
     const int quad = lane >> 2, pair = lane & 3;
     AttnPart part;
-    int64_t taken = 0;                                      // tiles of this CTA's stretch before the part
     int tree_of = -1, stage = 0;
     while (attn_next<ROWS>(p, s, part)) {
         const AttnTarget t = attn_target<ROWS>(p, s, part);
         const int i0 = (int)(t.row0 / p.G);
         const int nodes = (int)((t.row0 + t.rows - 1) / p.G) - i0 + 1;
         __syncthreads();
-        if (p.nodes.parents && tree_of != s.seq.b) {
+        const bool holds_nodes = (int64_t)(part.t0 + part.n) * kAttnTile > s.seq.len;
+        if (holds_nodes && p.nodes.parents && tree_of != s.seq.b) {
             for (int j = tid; j < s.seq.count; j += kMmaThreads) ctl.tree[j] = p.nodes.parents[(int64_t)s.seq.b * p.nodes.T + j];
             tree_of = s.seq.b;
             __syncthreads();
         }
-        if (tid < nodes)
+        if (holds_nodes && tid < nodes)
             attn_path_bits(p.nodes.parents ? ctl.tree : nullptr, i0 + tid, ctl.path[tid], (s.seq.count + 31) / 32, p.status);
 
         // queries as A fragments: rows quad and quad + 8 of each row tile
@@ -219,7 +216,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) attention_mma_kernel(const Att
 #pragma unroll
             for (int n = 0; n < NTILES; ++n) o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.f;
         }
-        for (int n = (int)((taken ^ team) & 1); n < part.n; n += kTeams) {
+        for (int n = 0; n < part.n; ++n) {
             copies_wait<Shape::stages - 1>();
             __syncwarp();
             const uint32_t base = ring + stage * Shape::step;
@@ -362,7 +359,6 @@ __global__ void __launch_bounds__(kMmaThreads, 1) attention_mma_kernel(const Att
             issue();
             stage = stage + 1 == Shape::stages ? 0 : stage + 1;
         }
-        taken += part.n;
 
         // ------------------------------------------------------------ the warps' results joined
 #pragma unroll
@@ -389,7 +385,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) attention_mma_kernel(const Att
                     o[mt][i][2 * g + 1] *= a;
                 }
             }
-            const int row = tid >> 4, c2 = (tid & 15) * 2;      // what this thread adds up
+            const int row = tid >> 3, c4 = (tid & 7) * 4;       // what this thread adds up
             float tall = neg_inf(), sum = 0.f;
 #pragma unroll
             for (int w = 0; w < kMmaWarps; ++w) tall = fmaxf(tall, ctl.ml[w][mt * 16 + row].x);
@@ -410,18 +406,18 @@ __global__ void __launch_bounds__(kMmaThreads, 1) attention_mma_kernel(const Att
                         *reinterpret_cast<float2 *>(join + (warp * 16 + g * 8 + quad) * kJoinPitch + i * 8 + pair * 2) =
                             make_float2(o[mt][h * 4 + i][2 * g], o[mt][h * 4 + i][2 * g + 1]);
                 __syncthreads();
-                float2 y = make_float2(0.f, 0.f);
+                float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < kMmaWarps; ++w) {
-                    const float2 x = *reinterpret_cast<const float2 *>(join + (w * 16 + row) * kJoinPitch + c2);
-                    y.x += x.x, y.y += x.y;
+                    const float4 x = *reinterpret_cast<const float4 *>(join + (w * 16 + row) * kJoinPitch + c4);
+                    y.x += x.x, y.y += x.y, y.z += x.z, y.w += x.w;
                 }
-                const int c = h * kJoinCols + c2;
+                const int c = h * kJoinCols + c4;
                 if (r < t.rows && c < p.D) {
                     if (t.whole) {
-                        *reinterpret_cast<uint32_t *>(static_cast<__nv_bfloat16 *>(p.out) + out_at + c) = pack_bf16(y.x * inv, y.y * inv);
+                        store_out(static_cast<__nv_bfloat16 *>(p.out) + out_at + c, make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv), 4);
                     } else {
-                        __stcg(reinterpret_cast<float2 *>(p.part + ((int64_t)t.slot * ROWS + r) * p.D + c), y);
+                        __stcg(reinterpret_cast<float4 *>(p.part + ((int64_t)t.slot * ROWS + r) * p.D + c), y);
                         if (c == 0) __stcg(&p.part_ml[(int64_t)t.slot * ROWS + r], make_float2(tall, sum));
                     }
                 }
@@ -435,7 +431,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) attention_mma_kernel(const Att
             __syncthreads();
             if (ctl.last) {
                 __threadfence();
-                attn_join<ROWS, __nv_bfloat16>(p, s, part, t, tid, kMmaThreads);
+                attn_join<ROWS, __nv_bfloat16>(p, s, part, t, warp, kMmaWarps);
             }
         }
     }

@@ -72,8 +72,9 @@ __device__ __forceinline__ AttnStretch attn_plan(const AttnParams &p, int64_t *s
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     // (a part costs some two tiles' time to join: no CTA is given less)
     constexpr int kLeast = 2;
-    int64_t mine = 0;
-    for (int b = tid; b < p.B; b += THREADS) mine += attn_seq<ROWS>(p, b).total(p.Hkv);
+    const int64_t own = tid < p.B ? attn_seq<ROWS>(p, tid).total(p.Hkv) : 0;
+    int64_t mine = own;
+    for (int b = tid + THREADS; b < p.B; b += THREADS) mine += attn_seq<ROWS>(p, b).total(p.Hkv);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
     if (lane == 0) scratch[warp] = mine;
@@ -96,7 +97,7 @@ __device__ __forceinline__ AttnStretch attn_plan(const AttnParams &p, int64_t *s
     int64_t before = 0;
     for (int b0 = 0;; b0 += THREADS) {
         const int b = b0 + tid;
-        const int64_t n = b < p.B ? attn_seq<ROWS>(p, b).total(p.Hkv) : 0;
+        const int64_t n = b0 == 0 ? own : b < p.B ? attn_seq<ROWS>(p, b).total(p.Hkv) : 0;
         int64_t incl = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -193,33 +194,62 @@ __device__ __forceinline__ int64_t attn_out_at(const AttnParams &p, const AttnSt
     return (((int64_t)s.seq.b * p.nodes.T + i) * p.Hq + (int64_t)part.head * p.G + g) * p.D;
 }
 
-// Joins the parts of an item; called by `threads` threads of the CTA that took its last ticket.
+// Joins the parts of an item; called by all lanes of `warps` warps of the CTA that took its last ticket.  A warp has a row at
+// a time, a lane one part's maximum and sum and then four columns; ROWS_AT_ONCE rows are on their way together.
 template <int ROWS, typename T>
 __device__ __forceinline__ void attn_join(const AttnParams &p, const AttnStretch &s, const AttnPart &part, const AttnTarget &t,
-                                          int tid, int threads)
+                                          int warp, int warps)
 {
-    const int cols = p.D / 4;
-    for (int i = tid; i < t.rows * cols; i += threads) {
-        const int row = i / cols, c = (i - row * cols) * 4;
-        float m = neg_inf();
-        for (int k = 0; k < t.parts; ++k) {
-            const int slot = 2 * (t.first + k) + (k == 0 ? 1 : 0);
-            m = fmaxf(m, __ldcg(&p.part_ml[(int64_t)slot * ROWS + row]).x);
+    constexpr int N = 4;
+    const int lane = threadIdx.x & 31, c = lane * 4;
+    auto slot_of = [&](int k) { return 2 * (t.first + k) + (k == 0 ? 1 : 0); };
+    for (int row0 = warp * N; row0 < t.rows; row0 += warps * N) {
+        float top[N], sum[N];
+        float4 o[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            top[i] = neg_inf();
+            sum[i] = 0.f;
+            o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        const float ref = m == neg_inf() ? 0.f : m;
-        float l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < t.parts; ++k) {
-            const int slot = 2 * (t.first + k) + (k == 0 ? 1 : 0);
-            const float2 ml = __ldcg(&p.part_ml[(int64_t)slot * ROWS + row]);
-            const float4 x = __ldcg(reinterpret_cast<const float4 *>(p.part + ((int64_t)slot * ROWS + row) * p.D + c));
-            const float w = ex2(ml.x - ref);
-            l = fmaf(w, ml.y, l);
-            // (a part that saw nothing has w = 0 and zeros)
-            o.x = fmaf(w, x.x, o.x), o.y = fmaf(w, x.y, o.y), o.z = fmaf(w, x.z, o.z), o.w = fmaf(w, x.w, o.w);
+        for (int k0 = 0; k0 < t.parts; k0 += 32) {      // 32 parts at a time, as in one pass over keys
+            float2 ml[N];
+            float w[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const bool there = k0 + lane < t.parts && row0 + i < t.rows;
+                ml[i] = there ? __ldcg(&p.part_ml[(int64_t)slot_of(k0 + lane) * ROWS + row0 + i]) : make_float2(neg_inf(), 0.f);
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float m = fmaxf(top[i], warp_max(ml[i].x)), ref = m == neg_inf() ? 0.f : m, a = ex2(top[i] - ref);
+                top[i] = m;
+                w[i] = ex2(ml[i].x - ref);          // (a part that saw nothing has 0 and zeros)
+                sum[i] = sum[i] * a + warp_sum(w[i] * ml[i].y);
+                o[i].x *= a, o[i].y *= a, o[i].z *= a, o[i].w *= a;
+            }
+            const int n = min(32, t.parts - k0);
+#pragma unroll 2
+            for (int k = 0; k < n; ++k) {
+                const float *from = p.part + ((int64_t)slot_of(k0 + k) * ROWS + row0) * p.D + c;
+                float4 x[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    x[i] = c < p.D && row0 + i < t.rows ? __ldcg(reinterpret_cast<const float4 *>(from + (int64_t)i * p.D)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float a = __shfl_sync(0xffffffffu, w[i], k);
+                    o[i].x = fmaf(a, x[i].x, o[i].x), o[i].y = fmaf(a, x[i].y, o[i].y), o[i].z = fmaf(a, x[i].z, o[i].z), o[i].w = fmaf(a, x[i].w, o[i].w);
+                }
+            }
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        store_out(static_cast<T *>(p.out) + attn_out_at(p, s, part, t.row0 + row) + c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), 4);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (row0 + i < t.rows) {
+                const float inv = sum[i] == 0.f ? 0.f : 1.f / sum[i];
+                store_out(static_cast<T *>(p.out) + attn_out_at(p, s, part, t.row0 + row0 + i) + c,
+                          make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv), p.D - c);
+            }
     }
 }
 

@@ -2,20 +2,19 @@
 //
 //   S = Q K^T   128 rows by a tile of 64 keys, into TMEM;   P = exp2(c (S - m)), back into TMEM;   O += P V, in TMEM
 //
-// One CTA per SM walks its stretch of tiles.  Two loader warps bring keys and values into a ring (cp.async, 16 bytes per
-// lane, into the 128-byte swizzle that the matrix descriptors name: pages of 16 entries would be 2 KB boxes for the copy
-// engine, whose number sets its time).  One thread issues the products: S of the next tiles goes ahead of P V of this one.
-// Two groups of four softmax warps take tiles in turn, a row per thread, each with its own maxima, sums, S, P and O
-// (all 512 columns of TMEM are in use): a tile takes a warp some thousand clocks, much of it latency, and the groups
-// wait for nothing of one another until the end of a part.  The maximum that exponents are taken against is only
-// raised when a score passes it by 2^8 (weights then stay below 2^8, and sums and products in fp32 keep their relative
-// precision), so that O is hardly ever rescaled.
+// Two CTAs per SM walk a stretch of tiles each, so that one's waits, beginnings and ends of parts hide behind the other's
+// work.  A loader warp brings keys and values into a ring (cp.async, 16 bytes per lane, into the 128-byte swizzle that
+// the matrix descriptors name: pages of 16 entries would be 2 KB boxes for the copy engine, whose number sets its
+// time).  One thread issues the products: S of the next tile goes ahead of P V of this one.  Four softmax warps have a row
+// per thread.  S is double-buffered, and P takes the place of the S it comes from.  The maximum that exponents are taken
+// against is only raised when a score passes it by 2^8 (weights then stay below 2^8, and sums and products in fp32 keep
+// their relative precision), so that O, which lives in TMEM, is hardly ever rescaled.
 //
 // Weights are used as two bf16 numbers, their rounding and what is left of it: one would put an error of 2^-9 on the
 // result, as much as its own rounding.  Up to 64 rows (DUP) the tile's other half holds the same queries again and
 // takes the second number, so that the one product does both; above, there is a second product.
 //
-// Every wait is bounded: when one runs out the status word becomes SPR_ERR_TIMEOUT, loaders and the issuing thread stop and
+// Every wait is bounded: when one runs out the status word becomes SPR_ERR_TIMEOUT, loader and issuing thread stop and
 // wait (again bounded) for what is in flight, and the softmax warps go on without waiting and give NaN.
 #include <atomic>
 
@@ -31,40 +30,38 @@ namespace {
 
 using namespace pairtc;
 
-constexpr int kTcThreads = 384;
-constexpr int kSoftmaxThreads = 256;                            // two groups of 128
-constexpr int kMmaWarp = 8, kFirstLoader = 10, kLoaders = 2;     // (a warp of each four of a kind: registers go by fours)
+constexpr int kTcThreads = 192;
+constexpr int kSoftmaxThreads = 128;
+constexpr int kMmaWarp = 4, kLoader = 5;
 constexpr int kPanel = kAttnTile * 128;                         // 64 keys by 64 columns
 constexpr float kRaise = 8.f;                                   // by how much scores may pass the maximum in use
-// TMEM columns
-constexpr int kColS = 0, kColP = 128, kColO = 256, kTmemCols = 512;       // two of each: 64, 2 x 32 and 128 columns
+// TMEM columns: two buffers of S, 64 each, where P's two numbers take 32 and 32; O
+constexpr int kColS = 0, kColO = 128, kTmemCols = 256;
 
 template <int PANELS>
 struct TcShape {
-    static constexpr int stage = 2 * PANELS * kPanel;            // keys, then values
-    static constexpr int stages = PANELS == 2 ? 5 : 10;
-    static constexpr int behind = stages - 3;                    // copies of as many tiles are in flight behind the newest
-    static constexpr int q_bytes = PANELS == 2 ? 32768 : 24576;  // queries; later results of up to three quarters of the block's pieces
-    static constexpr size_t smem = (size_t)q_bytes + (size_t)stages * stage + 1024;
+    static constexpr int unit = PANELS * kPanel;                 // a tile's keys, or its values
+    static constexpr int units = 8 / PANELS;                     // of the ring: keys and values by turns
+    static constexpr int behind = units - 2;                     // copies of as many units are in flight behind the newest
+    static constexpr int q_bytes = PANELS * 128 * 128;
+    static constexpr size_t smem = (size_t)q_bytes + (size_t)units * unit + 1024;
 };
 
 struct TcControl {
-    uint64_t full[10], empty[10];
-    uint64_t s_full[2], s_free[2], p_ready[2], pv_done[2];
+    uint64_t full[8], empty[8];
+    uint64_t s_full[2], p_ready[2], pv_done[2];   // by turns: a softmax warp may be a tile ahead of another, and of P V
     uint64_t q_ready, drain;
-    uint32_t valid[10][kLoaders];            // a bit for each key of the stage's tile that is there
+    uint64_t valid[8];                       // a bit for each key of a tile that is there
     int64_t scratch[2 * (kTcThreads / 32) + 4];
-    unsigned long long odd[2];
-    int64_t o_live[2];
-    float2 ml[2][128];
+    unsigned long long odd;
+    int64_t o_live;
     uint32_t tmem;
     int abort, last;
     int tree[kMaxTreeNodes];
     uint32_t path[128][kMaxTreeNodes / 32];
 };
 
-__device__ __forceinline__ void softmax_meet() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-__device__ __forceinline__ void group_meet(int group) { asm volatile("bar.sync %0, 128;" ::"r"(2 + group) : "memory"); }
+__device__ __forceinline__ void softmax_meet() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 __device__ __forceinline__ void arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there)
 {
@@ -115,7 +112,7 @@ __device__ __forceinline__ uint64_t path_bits64(const uint32_t *path, int at)
 }
 
 template <int PANELS, bool DUP>
-__global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnParams p)
+__global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnParams p)
 {
     constexpr int ROWS = DUP ? 64 : 128, COLS = 64 * PANELS;
     using Shape = TcShape<PANELS>;
@@ -126,21 +123,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
     const uint32_t limit = p.spin_limit;
 
     if (tid == 0) {
-        for (int i = 0; i < Shape::stages; ++i) {
-            bar_init(&ctl.full[i], kLoaders);
+        for (int i = 0; i < Shape::units; ++i) {
+            bar_init(&ctl.full[i], 1);
             bar_init(&ctl.empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(&ctl.s_full[i], 1);
-            bar_init(&ctl.s_free[i], 4);
             bar_init(&ctl.p_ready[i], 4);
             bar_init(&ctl.pv_done[i], 1);
         }
-        bar_init(&ctl.q_ready, 8);
+        bar_init(&ctl.q_ready, 4);
         bar_init(&ctl.drain, 1);
         ctl.abort = 0;
-        ctl.odd[0] = ctl.odd[1] = 0;
-        ctl.o_live[0] = ctl.o_live[1] = -1;
+        ctl.odd = 0;
+        ctl.o_live = -1;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kMmaWarp) {
@@ -154,21 +150,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
     fence_after();
     const uint32_t tmem = ctl.tmem;
 
-    if (warp >= kFirstLoader) {
-        // ------------------------------------------------------------ loaders: 32 of a tile's keys each
+    if (warp == kLoader) {
+        // ------------------------------------------------------------ loader
         constexpr int kChunks = 8 * PANELS, kRowsAtOnce = 32 / kChunks;
-        const int half = warp - kFirstLoader;
         const int c_row = lane / kChunks, c_chunk = lane % kChunks;
         const bool c_in = c_chunk * 8 < p.D;
-        // rows r0 + c_row of this warp's keys lie at to(r0) = (c_dst + 128 r0) ^ (r0 % 8 << 4): r0 is a multiple of kRowsAtOnce
-        const uint32_t c_dst = (c_chunk >> 3) * kPanel + half * 32 * 128 + c_row * 128 + (((c_chunk & 7) ^ c_row) << 4);
+        // rows 8 r + r0 + c_row of a unit lie at (c_dst + 128 (8 r + r0)) ^ (r0 << 4): r0 is a multiple of kRowsAtOnce
+        const uint32_t c_dst = (c_chunk >> 3) * kPanel + c_row * 128 + (((c_chunk & 7) ^ c_row) << 4);
         AttnPart part = {0, 0, 0, 0};
-        int64_t issued = 0;
+        int64_t issued = 0;                         // units
         bool alive = !(p.test_flags & ATTN_TEST_NO_LOADS);
-        auto complete = [&](int64_t tile) {         // this thread's copies of the tile have come
+        auto complete = [&](int64_t unit) {         // this warp's copies of the unit have come
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) arrive(&ctl.full[tile % Shape::stages]);
+            if (lane == 0) arrive(&ctl.full[unit % Shape::units]);
         };
         while (alive && attn_next<ROWS>(p, s, part)) {
             int64_t keys = (int64_t)s.seq.len + s.seq.count;
@@ -177,9 +172,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 keys = (int64_t)p.max_pages * p.page_size;
             }
             const int end = part.t0 + part.n;
-            auto find = [&](int tile) {             // lane 4 j + r: where run r (8 keys) of tile + j begins in the caches
-                const int t = tile + (lane >> 2);
-                const int64_t slot = (int64_t)t * kAttnTile + half * 32 + 8 * (lane & 3);
+            auto find = [&](int tile) {             // lane 8 j + r: where run r (8 keys) of tile + j begins in the caches
+                const int t = tile + (lane >> 3);
+                const int64_t slot = (int64_t)t * kAttnTile + 8 * (lane & 7);
                 if (t >= end || slot >= keys) return -1;
                 const uint32_t at = (uint32_t)((uint64_t)slot >> 3) / (uint32_t)(p.page_size >> 3);       // pages are whole runs
                 const int page = __ldg(p.page_table + (int64_t)s.seq.b * p.max_pages + at);
@@ -190,45 +185,45 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 return (page * p.Hkv + part.head) * p.page_size + (int)(slot - (int64_t)at * p.page_size);
             };
             int next = find(part.t0);
-            for (int n = 0; alive && n < part.n; n += 8) {
+            for (int n = 0; alive && n < part.n; n += 4) {
                 const int rows = next;
-                next = find(part.t0 + n + 8);
-                for (int u = 0; u < 8 && n + u < part.n; ++u, ++issued) {
-                    const int stage = (int)(issued % Shape::stages);
-                    const uint32_t round = (uint32_t)(issued / Shape::stages);
-                    if (round > 0 && !__all_sync(0xffffffffu, bar_wait(&ctl.empty[stage], (round - 1) & 1, &ctl.abort, p.status, limit))) {
-                        alive = false;
-                        break;
-                    }
-                    const int64_t left = keys - ((int64_t)part.t0 + n + u) * kAttnTile - half * 32;
-                    uint32_t valid = left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1;
-                    int run[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        run[r] = __shfl_sync(0xffffffffu, rows, 4 * u + r);
-                        if (run[r] < 0) valid &= ~(0xffu << (8 * r));
-                    }
-                    if (lane == 0) ctl.valid[stage][half] = valid;
-                    const uint32_t dst = ring + stage * Shape::stage + c_dst;
-                    const bool all = valid == 0xffffffffu;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int64_t from = run[r] < 0 ? 0 : ((int64_t)run[r] + c_row) * p.D + c_chunk * 8;
-                        const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(p.k) + from, *v = static_cast<const __nv_bfloat16 *>(p.v) + from;
-#pragma unroll
-                        for (int i = 0; i < 8 / kRowsAtOnce; ++i) {
-                            const int r0 = i * kRowsAtOnce;
-                            const bool there = c_in && (all || (valid >> (8 * r + r0 + c_row) & 1));
-                            const uint32_t to = (dst + (8 * r + r0) * 128) ^ (r0 << 4);
-                            copy16(to, there ? k : p.k, there);
-                            copy16(to + PANELS * kPanel, there ? v : p.v, there);
-                            k += kRowsAtOnce * p.D, v += kRowsAtOnce * p.D;
+                next = find(part.t0 + n + 4);
+                for (int u = 0; alive && u < 4 && n + u < part.n; ++u) {
+                    const int64_t left = keys - ((int64_t)part.t0 + n + u) * kAttnTile;
+                    uint64_t valid = left >= 64 ? ~0ull : (1ull << left) - 1;
+                    const uint32_t runs = __ballot_sync(0xffffffffu, rows >= 0) >> (8 * u) & 0xffu;
+                    if (runs != 0xffu)
+                        for (int r = 0; r < 8; ++r)
+                            if (!(runs >> r & 1)) valid &= ~(0xffull << (8 * r));
+                    const bool all = valid == ~0ull;
+#pragma unroll 1
+                    for (int kv = 0; kv < 2; ++kv, ++issued) {
+                        const int slot = (int)(issued % Shape::units);
+                        const uint32_t round = (uint32_t)(issued / Shape::units);
+                        if (round > 0 && !__all_sync(0xffffffffu, bar_wait(&ctl.empty[slot], (round - 1) & 1, &ctl.abort, p.status, limit))) {
+                            alive = false;
+                            break;
                         }
-                    }
-                    asm volatile("cp.async.commit_group;" ::: "memory");
-                    if (issued >= Shape::behind) {
-                        asm volatile("cp.async.wait_group %0;" ::"n"(Shape::behind) : "memory");
-                        complete(issued - Shape::behind);
+                        if (kv == 0 && lane == 0) ctl.valid[(issued >> 1) & 7] = valid;
+                        const __nv_bfloat16 *cache = static_cast<const __nv_bfloat16 *>(kv ? p.v : p.k);
+                        const uint32_t dst = ring + slot * Shape::unit + c_dst;
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) {
+                            const int run = __shfl_sync(0xffffffffu, rows, 8 * u + r);
+                            const __nv_bfloat16 *from = cache + (run < 0 ? 0 : ((int64_t)run + c_row) * p.D + c_chunk * 8);
+#pragma unroll
+                            for (int i = 0; i < 8 / kRowsAtOnce; ++i) {
+                                const int r0 = i * kRowsAtOnce;
+                                const bool there = c_in && (all || (valid >> (8 * r + r0 + c_row) & 1));
+                                copy16((dst + (8 * r + r0) * 128) ^ (r0 << 4), there ? from : cache, there);
+                                from += kRowsAtOnce * p.D;
+                            }
+                        }
+                        asm volatile("cp.async.commit_group;" ::: "memory");
+                        if (issued >= Shape::behind) {
+                            asm volatile("cp.async.wait_group %0;" ::"n"(Shape::behind) : "memory");
+                            complete(issued - Shape::behind);
+                        }
                     }
                 }
             }
@@ -249,50 +244,51 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 if (alive && !bar_wait(bar, parity & 1, &ctl.abort, p.status, limit)) alive = false;
                 return alive;
             };
+            // (where S of tile i goes P of tile i - 2 was: the product with it is complete when this is called)
             auto scores = [&](int64_t i) {
-                const int stage = (int)(i % Shape::stages), b = (int)(i & 1);
-                if (!wait(&ctl.full[stage], (uint32_t)(i / Shape::stages))) return;
-                if (i >= 2 && !wait(&ctl.s_free[b], (uint32_t)(i >> 1) - 1)) return;
+                const int slot = (int)((2 * i) % Shape::units), b = (int)(i & 1);
+                if (!wait(&ctl.full[slot], (uint32_t)((2 * i) / Shape::units))) return;
                 fence_after();
-                const uint32_t k = ring + stage * Shape::stage;
+                const uint32_t k = ring + slot * Shape::unit;
 #pragma unroll
                 for (int q = 0; q < 4 * PANELS; ++q)
                     mma_smem(tmem + kColS + 64 * b, tile_desc(q_tile + (q >> 2) * 128 * 128 + (q & 3) * 32, false),
                              tile_desc(k + (q >> 2) * kPanel + (q & 3) * 32, false), kQk, q != 0);
                 commit(&ctl.s_full[b]);
+                commit(&ctl.empty[slot]);
             };
             while (alive && attn_next<ROWS>(p, s, part)) {
                 if (!wait(&ctl.q_ready, parts++)) break;
                 scores(at);
                 if (part.n > 1) scores(at + 1);
                 for (int n = 0; alive && n < part.n; ++n, ++at) {
-                    const int stage = (int)(at % Shape::stages), b = (int)(at & 1);
-                    if (!wait(&ctl.p_ready[b], (uint32_t)(at >> 1))) break;
+                    const int slot = (int)((2 * at + 1) % Shape::units);
+                    if (!wait(&ctl.full[slot], (uint32_t)((2 * at + 1) / Shape::units)) || !wait(&ctl.p_ready[at & 1], (uint32_t)(at >> 1))) break;
                     fence_after();
-                    const uint32_t v = ring + stage * Shape::stage + PANELS * kPanel;
-                    const bool live = n > 1 || *reinterpret_cast<volatile int64_t *>(&ctl.o_live[b]) == at;
-                    const uint32_t o = tmem + kColO + 128 * b, w = tmem + kColP + 64 * b;
+                    const uint32_t v = ring + slot * Shape::unit, w = tmem + kColS + 64 * (int)(at & 1);
+                    const bool live = n > 0 || *reinterpret_cast<volatile int64_t *>(&ctl.o_live) == at;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        mma_tmem(o, w + 8 * q, tile_desc(v + q * 2048, true), kPv, live || q != 0);
-                        if (!DUP) mma_tmem(o, w + 32 + 8 * q, tile_desc(v + q * 2048, true), kPv, 1u);
+                        mma_tmem(tmem + kColO, w + 8 * q, tile_desc(v + q * 2048, true), kPv, live || q != 0);
+                        if (!DUP) mma_tmem(tmem + kColO, w + 32 + 8 * q, tile_desc(v + q * 2048, true), kPv, 1u);
                     }
-                    commit(&ctl.pv_done[b]);
-                    commit(&ctl.empty[stage]);
-                    if (n + 2 < part.n) scores(at + 2);
+                    commit(&ctl.pv_done[at & 1]);
+                    commit(&ctl.empty[slot]);
+                    if (n + 2 < part.n) {
+                        if (!wait(&ctl.pv_done[at & 1], (uint32_t)(at >> 1))) break;
+                        scores(at + 2);
+                    }
                 }
             }
             commit(&ctl.drain);             // nothing of this CTA's products is left when its TMEM is given back
             bar_wait_quiet(&ctl.drain, 0, limit);
         }
         __syncwarp();
-    } else if (warp < 8) {
+    } else {
         // ------------------------------------------------------------ softmax: a row per thread
-        const int group = warp >> 2, gid = tid & 127;
-        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t col_s = lanes + kColS + 64 * group, col_p = lanes + kColP + 64 * group, col_o = lanes + kColO + 128 * group;
-        const int row = DUP ? gid & 63 : gid;               // in the block
-        const bool second = DUP && gid >= 64;               // this thread's weights are what rounding left
+        const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16), col_o = lanes + kColO;
+        const int row = DUP ? tid & 63 : tid;               // in the block
+        const bool second = DUP && tid >= 64;               // this thread's weights are what rounding left
         const float c = p.abs_scale_log2;
         AttnPart part;
         int64_t at = 0;
@@ -307,55 +303,52 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
         };
         while (attn_next<ROWS>(p, s, part)) {
             const AttnTarget t = attn_target<ROWS>(p, s, part);
-            const int i0 = (int)(t.row0 / p.G);
-            const int nodes = (int)((t.row0 + t.rows - 1) / p.G) - i0 + 1;
-            softmax_meet();
-            if (p.nodes.parents && tree_of != s.seq.b) {
-                for (int j = tid; j < s.seq.count; j += kSoftmaxThreads) ctl.tree[j] = p.nodes.parents[(int64_t)s.seq.b * p.nodes.T + j];
-                tree_of = s.seq.b;
-                softmax_meet();
-            }
-            if (tid < nodes) {
-                for (int w = (s.seq.count + 31) / 32; w < kMaxTreeNodes / 32; ++w) ctl.path[tid][w] = 0u;
-                attn_path_bits(p.nodes.parents ? ctl.tree : nullptr, i0 + tid, ctl.path[tid], (s.seq.count + 31) / 32, p.status);
-            }
             // this row's query (zeros where there is none; all products of the part before have been formed)
             const bool in = row < t.rows;
             const int64_t out_at = in ? attn_out_at(p, s, part, t.row0 + row) : 0;
+            softmax_meet();
             {
                 const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + out_at);
-                // (the groups have half of it each)
 #pragma unroll
-                for (int i = 0; i < 4 * PANELS; ++i) {
-                    const int k = group * 4 * PANELS + i;
+                for (int k = 0; k < 8 * PANELS; ++k) {
                     uint4 x = in && k * 8 < p.D ? __ldg(src + k) : make_uint4(0u, 0u, 0u, 0u);
                     x.x ^= p.flip, x.y ^= p.flip, x.z ^= p.flip, x.w ^= p.flip;
                     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};"
-                                 ::"r"(q_tile + (k >> 3) * 128 * 128 + gid * 128 + (((k & 7) ^ (gid & 7)) << 4)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+                                 ::"r"(q_tile + (k >> 3) * 128 * 128 + tid * 128 + (((k & 7) ^ (tid & 7)) << 4)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             warp_arrive(&ctl.q_ready);
-            softmax_meet();                                 // (paths)
-            const uint32_t *path = ctl.path[in ? (int)((t.row0 + row) / p.G) - i0 : 0];
+            const uint32_t *path = ctl.path[0];
+            if ((int64_t)(part.t0 + part.n) * kAttnTile > s.seq.len) {       // some tile holds nodes
+                const int i0 = (int)(t.row0 / p.G);
+                const int nodes = (int)((t.row0 + t.rows - 1) / p.G) - i0 + 1;
+                if (p.nodes.parents && tree_of != s.seq.b) {
+                    for (int j = tid; j < s.seq.count; j += kSoftmaxThreads) ctl.tree[j] = p.nodes.parents[(int64_t)s.seq.b * p.nodes.T + j];
+                    tree_of = s.seq.b;
+                    softmax_meet();
+                }
+                if (tid < nodes) {
+                    for (int w = (s.seq.count + 31) / 32; w < kMaxTreeNodes / 32; ++w) ctl.path[tid][w] = 0u;
+                    attn_path_bits(p.nodes.parents ? ctl.tree : nullptr, i0 + tid, ctl.path[tid], (s.seq.count + 31) / 32, p.status);
+                }
+                if (in) path = ctl.path[(int)((t.row0 + row) / p.G) - i0];
+                softmax_meet();
+            }
 
             float m = neg_inf(), l = 0.f;
-            int64_t mine = at + ((at ^ group) & 1);             // this group's next tile
-            const int64_t end = at + part.n;
-            const bool any = mine < end;
-            for (bool begun = false; mine < end; mine += 2, begun = true) {
-                const int stage = (int)(mine % Shape::stages);
-                const uint32_t phase = (uint32_t)(mine >> 1);
+            for (int n = 0; n < part.n; ++n, ++at) {
+                const uint32_t col_s = lanes + kColS + 64 * (uint32_t)(at & 1);
+                const bool begun = n > 0;
                 float x[64];
-                wait(&ctl.s_full[group], phase);
+                wait(&ctl.s_full[at & 1], (uint32_t)(at >> 1));
                 fence_after();
                 tmem_read32(col_s, *reinterpret_cast<float (*)[32]>(x));
                 tmem_read32(col_s + 32, *reinterpret_cast<float (*)[32]>(x + 32));
                 tmem_wait();
-                fence_before();
-                warp_arrive(&ctl.s_free[group]);
-                const int64_t slot0 = (part.t0 + (mine - at)) * kAttnTile;
-                const uint64_t valid = (uint64_t)ctl.valid[stage][0] | (uint64_t)ctl.valid[stage][1] << 32;
+                const int64_t slot0 = ((int64_t)part.t0 + n) * kAttnTile;
+                const uint64_t valid = ctl.valid[at & 7];
+                const uint32_t v_unit = ring + (int)((2 * at + 1) % Shape::units) * Shape::unit;
                 const bool tail = slot0 + kAttnTile > s.seq.len;      // (alike in all threads, whatever went wrong: they meet)
                 unsigned long long odd = 0;
                 uint64_t vis = valid;
@@ -370,7 +363,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 }
                 if (tail) {
                     // values that are not finite, where not every row sees every key: each thread looks at half a key
-                    const uint32_t v = ring + stage * Shape::stage + PANELS * kPanel + (gid >> 1) * 128 + (gid & 1) * 64;
+                    wait(&ctl.full[(2 * at + 1) % Shape::units], (uint32_t)((2 * at + 1) / Shape::units));
+                    const uint32_t v = v_unit + (tid >> 1) * 128 + (tid & 1) * 64;
                     bool bad = false;
 #pragma unroll
                     for (int k = 0; k < 4 * PANELS; ++k) {
@@ -378,10 +372,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                         asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(v + (k >> 2) * kPanel + (k & 3) * 16) : "memory");
                         bad = bad || !(finite_bf16x2(w[0]) && finite_bf16x2(w[1]) && finite_bf16x2(w[2]) && finite_bf16x2(w[3]));
                     }
-                    group_meet(group);
-                    if (bad) atomicOr(&ctl.odd[group], 1ull << (gid >> 1));
-                    group_meet(group);
-                    odd = *reinterpret_cast<volatile unsigned long long *>(&ctl.odd[group]);
+                    softmax_meet();
+                    if (bad) atomicOr(&ctl.odd, 1ull << (tid >> 1));
+                    softmax_meet();
+                    odd = *reinterpret_cast<volatile unsigned long long *>(&ctl.odd);
                 }
                 float t4[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
@@ -389,8 +383,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
                 // (m = -inf: nothing seen so far, and O holds nothing of this row)
                 const bool raise = top > m && (m == neg_inf() || (top - m) * c > kRaise);
-                const bool waited = __any_sync(0xffffffffu, raise) && begun;
-                if (begun && mine >= 2 && (waited || odd)) wait(&ctl.pv_done[group], phase - 1);
+                if (begun && (__any_sync(0xffffffffu, raise) || odd)) wait(&ctl.pv_done[(at - 1) & 1], (uint32_t)((at - 1) >> 1));
                 if (__any_sync(0xffffffffu, raise)) {
                     const float a = raise && m != neg_inf() ? ex2((m - top) * c) : 1.f;
                     if (raise) m = top;
@@ -425,7 +418,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 if (odd) {
                     // taken out of the product, and added one by one to the rows that see them
                     fence_after();
-                    const uint32_t v = ring + stage * Shape::stage + PANELS * kPanel;
+                    const uint32_t v = v_unit;
 #pragma unroll 1
                     for (int k = 0; k < 2 * PANELS; ++k) {
                         float o[32];
@@ -454,23 +447,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                         for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(o[i]);
                         tmem_write32(col_o + 32 * k, w);
                     }
-                    group_meet(group);
-                    if (odd >> (gid >> 1) & 1)
+                    softmax_meet();
+                    if (odd >> (tid >> 1) & 1)
                         for (int k = 0; k < 4 * PANELS; ++k)
-                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v + (gid >> 1) * 128 + (gid & 1) * 64 + (k >> 2) * kPanel + (k & 3) * 16), "r"(0u) : "memory");
+                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v + (tid >> 1) * 128 + (tid & 1) * 64 + (k >> 2) * kPanel + (k & 3) * 16), "r"(0u) : "memory");
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    if (gid == 0) {
-                        ctl.odd[group] = 0;
-                        if (!begun) ctl.o_live[group] = mine;
+                    if (tid == 0) {
+                        ctl.odd = 0;
+                        if (!begun) ctl.o_live = at;
                     }
-                    group_meet(group);
+                    softmax_meet();
                 }
-                if (mine >= 2 && !(begun && (waited || odd))) wait(&ctl.pv_done[group], phase - 1);
-                fence_after();
                 uint32_t w[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-                if (!DUP || !second) tmem_write32(col_p, w);
+                if (!DUP || !second) tmem_write32(col_s, w);
                 if (!DUP || second) {
                     const uint64_t minus = pack2(-1.f, -1.f);
 #pragma unroll
@@ -479,71 +470,68 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                         unpack2(fma2(pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)), minus, pack2(x[2 * i], x[2 * i + 1])), a, b);
                         w[i] = pack_bf16(a, b);
                     }
-                    tmem_write32(col_p + (DUP ? 0 : 32), w);
+                    tmem_write32(col_s + (DUP ? 0 : 32), w);
                 }
                 tmem_wait_st();
                 fence_before();
-                warp_arrive(&ctl.p_ready[group]);
+                warp_arrive(&ctl.p_ready[at & 1]);
             }
-            at = end;
 
-            // -------------------------------------------------------- the part's results: both groups', and both numbers'
-            if (any) wait(&ctl.pv_done[group], (uint32_t)((mine - 2) >> 1));
+            // -------------------------------------------------------- the part's results
+            wait(&ctl.pv_done[(at - 1) & 1], (uint32_t)((at - 1) >> 1));
             fence_after();
             if (dead) l = __int_as_float(0x7fc00000);       // what a wait that ran out leaves is no result
-            ctl.ml[group][gid] = make_float2(m, l);
-            softmax_meet();
-            const float2 other = ctl.ml[group ^ 1][gid];
-            const float top = fmaxf(m, other.x), shift = top == neg_inf() ? 0.f : top;
-            const float mine_by = any ? ex2((m - shift) * c) : 0.f;
-            l = l * ex2((m - shift) * c) + other.y * ex2((other.x - shift) * c);
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            const bool last_hand = group == 0 && !second;       // adds up and writes
-            // the others' results go through the query tile, 32 columns at a time
-            constexpr int kPieces = DUP ? 3 : 1;
-            const uint32_t piece = q_tile + (DUP ? 2 * group + (second ? 1 : 0) - 1 : 0) * ROWS * 128;
+            if (DUP) {      // the second numbers' results, by way of the query tile
+                if (second) {
 #pragma unroll 1
-            for (int k = 0; k < 2 * PANELS; ++k) {
-                float o[32];
-                tmem_read32(col_o + 32 * k, o);
-                tmem_wait();
+                    for (int k = 0; k < 2 * PANELS; ++k) {
+                        float o[32];
+                        tmem_read32(col_o + 32 * k, o);
+                        tmem_wait();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = any ? o[i] * mine_by : 0.f;        // (without a tile O is not this part's)
-                if (!last_hand) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};"
-                                     ::"r"(piece + row * 128 + ((i ^ (row & 7)) << 4)), "f"(o[4 * i]), "f"(o[4 * i + 1]), "f"(o[4 * i + 2]), "f"(o[4 * i + 3]) : "memory");
-                }
-                softmax_meet();
-                if (last_hand && in) {
-#pragma unroll
-                    for (int h = 0; h < kPieces; ++h)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            float y[4];
-                            asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(y[0]), "=f"(y[1]), "=f"(y[2]), "=f"(y[3])
-                                         : "r"(q_tile + h * ROWS * 128 + row * 128 + ((i ^ (row & 7)) << 4)) : "memory");
-                            o[4 * i] += y[0], o[4 * i + 1] += y[1], o[4 * i + 2] += y[2], o[4 * i + 3] += y[3];
-                        }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int col = 32 * k + 8 * i;
-                        if (col >= p.D) continue;
-                        if (t.whole) {
-                            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + out_at + col) =
-                                make_uint4(pack_bf16(o[8 * i] * inv, o[8 * i + 1] * inv), pack_bf16(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
-                                           pack_bf16(o[8 * i + 4] * inv, o[8 * i + 5] * inv), pack_bf16(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
-                        } else {
-                            float4 *to = reinterpret_cast<float4 *>(p.part + ((int64_t)t.slot * ROWS + row) * p.D + col);
-                            __stcg(to, make_float4(o[8 * i], o[8 * i + 1], o[8 * i + 2], o[8 * i + 3]));
-                            __stcg(to + 1, make_float4(o[8 * i + 4], o[8 * i + 5], o[8 * i + 6], o[8 * i + 7]));
-                        }
+                        for (int i = 0; i < 8; ++i)
+                            asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};"
+                                         ::"r"(q_tile + row * COLS * 4 + (((8 * k + i) ^ (row & 7)) << 4)), "f"(o[4 * i]), "f"(o[4 * i + 1]), "f"(o[4 * i + 2]), "f"(o[4 * i + 3]) : "memory");
                     }
                 }
                 softmax_meet();
             }
-            if (!t.whole && last_hand && in) __stcg(&p.part_ml[(int64_t)t.slot * ROWS + row], make_float2(top * c, l));
+            if (!second) {
+#pragma unroll 1
+                for (int k = 0; k < 2 * PANELS; ++k) {
+                    float o[32];
+                    tmem_read32(col_o + 32 * k, o);
+                    tmem_wait();
+                    if (DUP) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            float y[4];
+                            asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(y[0]), "=f"(y[1]), "=f"(y[2]), "=f"(y[3])
+                                         : "r"(q_tile + row * COLS * 4 + (((8 * k + i) ^ (row & 7)) << 4)) : "memory");
+                            o[4 * i] += y[0], o[4 * i + 1] += y[1], o[4 * i + 2] += y[2], o[4 * i + 3] += y[3];
+                        }
+                    }
+                    if (in) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int col = 32 * k + 8 * i;
+                            if (col >= p.D) continue;
+                            if (t.whole) {
+                                *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + out_at + col) =
+                                    make_uint4(pack_bf16(o[8 * i] * inv, o[8 * i + 1] * inv), pack_bf16(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
+                                               pack_bf16(o[8 * i + 4] * inv, o[8 * i + 5] * inv), pack_bf16(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
+                            } else {
+                                float4 *to = reinterpret_cast<float4 *>(p.part + ((int64_t)t.slot * ROWS + row) * p.D + col);
+                                __stcg(to, make_float4(o[8 * i], o[8 * i + 1], o[8 * i + 2], o[8 * i + 3]));
+                                __stcg(to + 1, make_float4(o[8 * i + 4], o[8 * i + 5], o[8 * i + 6], o[8 * i + 7]));
+                            }
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (!t.whole && in) __stcg(&p.part_ml[(int64_t)t.slot * ROWS + row], make_float2(m * c, l));
+            }
             fence_before();
             if (!t.whole) {
                 __threadfence();
@@ -552,7 +540,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 softmax_meet();
                 if (ctl.last) {
                     __threadfence();
-                    attn_join<ROWS, __nv_bfloat16>(p, s, part, t, tid, kSoftmaxThreads);
+                    attn_join<ROWS, __nv_bfloat16>(p, s, part, t, warp, kSoftmaxThreads / 32);
                 }
             }
         }

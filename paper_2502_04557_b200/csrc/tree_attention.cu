@@ -73,7 +73,7 @@ int tree_attention(const void *q, const void *k_cache, const void *v_cache, int 
     p.scale_log2 = scale * kLog2e;
     p.abs_scale_log2 = fmaxf(fabsf(p.scale_log2), 1e-37f);
     p.flip = scale < 0.f ? 0x80008000u : 0u;
-    p.ctas = sms < kAttnMaxCtas ? sms : kAttnMaxCtas;
+    p.ctas = sms * kAttnCtasPerSm < kAttnMaxCtas ? sms * kAttnCtasPerSm : kAttnMaxCtas;
     p.status = static_cast<int *>(ws);
     p.counters = at<int>(ws, w.counters);
     p.part = at<float>(ws, w.part);

@@ -196,7 +196,8 @@ def check_attend(spr, x, scale=None, **kw):
     s = x["q"].shape[-1] ** -0.5 if scale is None else scale
     c = {n: None if t is None else t.cuda() for n, t in x.items()}
     want, tol = ref.attend(c["q"], c["k_cache"], c["v_cache"], x["page_table"], x["lens"], x["counts"], x["parents"], s)
-    assert ref.within(got, want, tol), ref.worst(got, want, tol)
+    ok = ref.within(got, want, tol)
+    assert ok, ref.worst(got, want, tol)
     return got
 
 
