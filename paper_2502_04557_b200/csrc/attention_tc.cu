@@ -3,12 +3,14 @@
 //   S = Q K^T   128 rows by a tile of 64 keys, into TMEM;   P = exp2(c (S - m)), back into TMEM;   O += P V, in TMEM
 //
 // Two CTAs per SM walk a stretch of tiles each, so that one's waits, beginnings and ends of parts hide behind the other's
-// work.  A loader warp brings keys and values into a ring (cp.async, 16 bytes per lane, into the 128-byte swizzle that
-// the matrix descriptors name: pages of 16 entries would be 2 KB boxes for the copy engine, whose number sets its
-// time).  One thread issues the products: S of the next tile goes ahead of P V of this one.  Four softmax warps have a row
-// per thread.  S is double-buffered, and P takes the place of the S it comes from.  The maximum that exponents are taken
-// against is only raised when a score passes it by 2^8 (weights then stay below 2^8, and sums and products in fp32 keep
-// their relative precision), so that O, which lives in TMEM, is hardly ever rescaled.
+// work.  One loader warp brings keys and one values into a ring of units (cp.async, 16 bytes per lane, into the 128-byte
+// swizzle that the matrix descriptors name; a warp takes 1500 clocks to ask for 16 KB, so that one would not do for both,
+// and pages of 16 entries would be 2 KB boxes for the copy engine, whose number sets its time).  Copies report to the ring's
+// barriers themselves.  One thread issues the products: S of the next tile goes ahead of P V of this one.  Four softmax
+// warps have a row per thread, and the registers that the others do without.  S is double-buffered, and P takes the place
+// of the S it comes from.  The maximum that exponents are taken against is only raised when a score passes it by 2^8
+// (weights then stay below 2^8, and sums and products in fp32 keep their relative precision), so that O, which lives in
+// TMEM, is hardly ever rescaled.
 //
 // Weights are used as two bf16 numbers, their rounding and what is left of it: one would put an error of 2^-9 on the
 // result, as much as its own rounding.  Up to 64 rows (DUP) the tile's other half holds the same queries again and
@@ -30,9 +32,9 @@ namespace {
 
 using namespace pairtc;
 
-constexpr int kTcThreads = 192;
+constexpr int kTcThreads = 256;
 constexpr int kSoftmaxThreads = 128;
-constexpr int kMmaWarp = 4, kLoader = 5;
+constexpr int kMmaWarp = 4, kFirstLoader = 5;    // one for keys, one for values (warp 7 idles)
 constexpr int kPanel = kAttnTile * 128;                         // 64 keys by 64 columns
 constexpr float kRaise = 8.f;                                   // by how much scores may pass the maximum in use
 // TMEM columns: two buffers of S, 64 each, where P's two numbers take 32 and 32; O
@@ -42,7 +44,6 @@ template <int PANELS>
 struct TcShape {
     static constexpr int unit = PANELS * kPanel;                 // a tile's keys, or its values
     static constexpr int units = 8 / PANELS;                     // of the ring: keys and values by turns
-    static constexpr int behind = units - 2;                     // copies of as many units are in flight behind the newest
     static constexpr int q_bytes = PANELS * 128 * 128;
     static constexpr size_t smem = (size_t)q_bytes + (size_t)units * unit + 1024;
 };
@@ -124,7 +125,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
 
     if (tid == 0) {
         for (int i = 0; i < Shape::units; ++i) {
-            bar_init(&ctl.full[i], 1);
+            bar_init(&ctl.full[i], 32);          // each lane of the warp that brings it
             bar_init(&ctl.empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -150,22 +151,22 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
     fence_after();
     const uint32_t tmem = ctl.tmem;
 
-    if (warp == kLoader) {
-        // ------------------------------------------------------------ loader
+    // (256 threads start with 128 registers each: 168 and 88 make the same sum)
+    if (warp >= 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+      if (warp >= kFirstLoader) {
+        // ------------------------------------------------------------ loaders (the ring holds an even number of units: each
+        // has stages of its own, and sees every phase of their barriers)
         constexpr int kChunks = 8 * PANELS, kRowsAtOnce = 32 / kChunks;
         const int c_row = lane / kChunks, c_chunk = lane % kChunks;
         const bool c_in = c_chunk * 8 < p.D;
         // rows 8 r + r0 + c_row of a unit lie at (c_dst + 128 (8 r + r0)) ^ (r0 << 4): r0 is a multiple of kRowsAtOnce
         const uint32_t c_dst = (c_chunk >> 3) * kPanel + c_row * 128 + (((c_chunk & 7) ^ c_row) << 4);
         AttnPart part = {0, 0, 0, 0};
-        int64_t issued = 0;                         // units
+        const int kv = warp - kFirstLoader;
+        int64_t unit = kv;
         bool alive = !(p.test_flags & ATTN_TEST_NO_LOADS);
-        auto complete = [&](int64_t unit) {         // this warp's copies of the unit have come
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) arrive(&ctl.full[unit % Shape::units]);
-        };
-        while (alive && attn_next<ROWS>(p, s, part)) {
+        while (kv < 2 && alive && attn_next<ROWS>(p, s, part)) {
             int64_t keys = (int64_t)s.seq.len + s.seq.count;
             if (keys > (int64_t)p.max_pages * p.page_size) {
                 raise_status(p.status, SPR_ERR_BAD_PAGE);
@@ -196,42 +197,38 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
                         for (int r = 0; r < 8; ++r)
                             if (!(runs >> r & 1)) valid &= ~(0xffull << (8 * r));
                     const bool all = valid == ~0ull;
-#pragma unroll 1
-                    for (int kv = 0; kv < 2; ++kv, ++issued) {
-                        const int slot = (int)(issued % Shape::units);
-                        const uint32_t round = (uint32_t)(issued / Shape::units);
-                        if (round > 0 && !__all_sync(0xffffffffu, bar_wait(&ctl.empty[slot], (round - 1) & 1, &ctl.abort, p.status, limit))) {
-                            alive = false;
-                            break;
-                        }
-                        if (kv == 0 && lane == 0) ctl.valid[(issued >> 1) & 7] = valid;
-                        const __nv_bfloat16 *cache = static_cast<const __nv_bfloat16 *>(kv ? p.v : p.k);
-                        const uint32_t dst = ring + slot * Shape::unit + c_dst;
+                    const int slot = (int)(unit % Shape::units);
+                    const uint32_t round = (uint32_t)(unit / Shape::units);
+                    if (round > 0 && !__all_sync(0xffffffffu, bar_wait(&ctl.empty[slot], (round - 1) & 1, &ctl.abort, p.status, limit))) {
+                        alive = false;
+                        break;
+                    }
+                    if (kv == 0 && lane == 0) {
+                        ctl.valid[(unit >> 1) & 7] = valid;
+                        __threadfence_block();
+                    }
+                    const __nv_bfloat16 *cache = static_cast<const __nv_bfloat16 *>(kv ? p.v : p.k);
+                    const uint32_t dst = ring + slot * Shape::unit + c_dst;
 #pragma unroll
-                        for (int r = 0; r < 8; ++r) {
-                            const int run = __shfl_sync(0xffffffffu, rows, 8 * u + r);
-                            const __nv_bfloat16 *from = cache + (run < 0 ? 0 : ((int64_t)run + c_row) * p.D + c_chunk * 8);
+                    for (int r = 0; r < 8; ++r) {
+                        const int run = __shfl_sync(0xffffffffu, rows, 8 * u + r);
+                        const __nv_bfloat16 *from = cache + (run < 0 ? 0 : ((int64_t)run + c_row) * p.D + c_chunk * 8);
 #pragma unroll
-                            for (int i = 0; i < 8 / kRowsAtOnce; ++i) {
-                                const int r0 = i * kRowsAtOnce;
-                                const bool there = c_in && (all || (valid >> (8 * r + r0 + c_row) & 1));
-                                copy16((dst + (8 * r + r0) * 128) ^ (r0 << 4), there ? from : cache, there);
-                                from += kRowsAtOnce * p.D;
-                            }
-                        }
-                        asm volatile("cp.async.commit_group;" ::: "memory");
-                        if (issued >= Shape::behind) {
-                            asm volatile("cp.async.wait_group %0;" ::"n"(Shape::behind) : "memory");
-                            complete(issued - Shape::behind);
+                        for (int i = 0; i < 8 / kRowsAtOnce; ++i) {
+                            const int r0 = i * kRowsAtOnce;
+                            const bool there = c_in && (all || (valid >> (8 * r + r0 + c_row) & 1));
+                            copy16((dst + (8 * r + r0) * 128) ^ (r0 << 4), there ? from : cache, there);
+                            from += kRowsAtOnce * p.D;
                         }
                     }
+                    // this lane arrives when its copies have
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_addr(&ctl.full[slot])) : "memory");
+                    unit += 2;
                 }
             }
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        if (alive)
-            for (int64_t i = issued > Shape::behind ? issued - Shape::behind : 0; i < issued; ++i) complete(i);
-    } else if (warp == kMmaWarp) {
+        asm volatile("cp.async.wait_all;" ::: "memory");       // none is left when the CTA ends
+      } else {
         // ------------------------------------------------------------ products
         if (lane == 0) {
             constexpr uint32_t kQk = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kAttnTile >> 3) << 17) | (8u << 24);
@@ -248,6 +245,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
             auto scores = [&](int64_t i) {
                 const int slot = (int)((2 * i) % Shape::units), b = (int)(i & 1);
                 if (!wait(&ctl.full[slot], (uint32_t)((2 * i) / Shape::units))) return;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // the lanes' copies, for the tensor core
                 fence_after();
                 const uint32_t k = ring + slot * Shape::unit;
 #pragma unroll
@@ -264,6 +262,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
                 for (int n = 0; alive && n < part.n; ++n, ++at) {
                     const int slot = (int)((2 * at + 1) % Shape::units);
                     if (!wait(&ctl.full[slot], (uint32_t)((2 * at + 1) / Shape::units)) || !wait(&ctl.p_ready[at & 1], (uint32_t)(at >> 1))) break;
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     fence_after();
                     const uint32_t v = ring + slot * Shape::unit, w = tmem + kColS + 64 * (int)(at & 1);
                     const bool live = n > 0 || *reinterpret_cast<volatile int64_t *>(&ctl.o_live) == at;
@@ -284,8 +283,10 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
             bar_wait_quiet(&ctl.drain, 0, limit);
         }
         __syncwarp();
+      }
     } else {
         // ------------------------------------------------------------ softmax: a row per thread
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
         const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16), col_o = lanes + kColO;
         const int row = DUP ? tid & 63 : tid;               // in the block
         const bool second = DUP && tid >= 64;               // this thread's weights are what rounding left
