@@ -9,7 +9,7 @@
 namespace spr {
 
 constexpr int kAttnTile = 64;            // keys per tile, the unit in which work is dealt out
-constexpr int kAttnCtasPerSm = 2;
+constexpr int kAttnCtasPerSm = 2;        // at most
 constexpr int kAttnMaxCtas = 148 * kAttnCtasPerSm;
 constexpr int kAttnMaxDim = 128;
 
@@ -39,6 +39,6 @@ int attention_block_rows(int T, int G, int dt);
 
 cudaError_t launch_attention_f32(const AttnParams &p, int rows, cudaStream_t st);
 cudaError_t launch_attention_mma(const AttnParams &p, int dev, cudaStream_t st);
-cudaError_t launch_attention_tc(const AttnParams &p, int rows, int dev, cudaStream_t st);
+cudaError_t launch_attention_tc(const AttnParams &p, int dev, cudaStream_t st);
 
 }  // namespace spr

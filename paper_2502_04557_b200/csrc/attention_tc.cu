@@ -2,21 +2,23 @@
 //
 //   S = Q K^T   128 rows by a tile of 64 keys, into TMEM;   P = exp2(c (S - m)), back into TMEM;   O += P V, in TMEM
 //
-// Two CTAs per SM walk a stretch of tiles each, so that one's waits, beginnings and ends of parts hide behind the other's
-// work.  One loader warp brings keys and one values into a ring of units (cp.async, 16 bytes per lane, into the 128-byte
-// swizzle that the matrix descriptors name; a warp takes 1500 clocks to ask for 16 KB, so that one would not do for both,
-// and pages of 16 entries would be 2 KB boxes for the copy engine, whose number sets its time).  Copies report to the ring's
-// barriers themselves.  One thread issues the products: S of the next tile goes ahead of P V of this one.  Four softmax
-// warps have a row per thread, and the registers that the others do without.  S is double-buffered, and P takes the place
-// of the S it comes from.  The maximum that exponents are taken against is only raised when a score passes it by 2^8
-// (weights then stay below 2^8, and sums and products in fp32 keep their relative precision), so that O, which lives in
-// TMEM, is hardly ever rescaled.
+// One CTA per SM walks its stretch of tiles; tiles go to two groups by turns.  Four softmax warps of a group have a row
+// per thread, and one warp issues the group's products: S of the next tile goes ahead of P V of this one (S is
+// double-buffered, P takes the place of the S it comes from).  The groups have maxima, sums and an O of their own and wait for
+// nothing of one another until the end of a part: a tile takes a softmax warp some 2000 clocks, most of it latency.
+// All 512 columns of TMEM are in use: 2 x 2 S, 2 O.
 //
+// Four loader warps bring keys and values into a ring of six tiles (cp.async, 16 bytes per lane, into the 128-byte
+// swizzle that the matrix descriptors name: a warp takes 1500 clocks to ask for 16 KB, and pages of 16 entries would be 2 KB
+// boxes for the copy engine, whose number sets its time), another the queries.  Copies report to the barriers themselves.
+// Loaders run ahead into the next part while this one ends.  Every warp that waits on a barrier sees all of its phases.
+//
+// The maximum that exponents are taken against is only raised when a score passes it by 2^8 (weights then stay below
+// 2^8, and sums and products in fp32 keep their relative precision), so that O, which lives in TMEM, is hardly ever rescaled.
 // Weights are used as two bf16 numbers, their rounding and what is left of it: one would put an error of 2^-9 on the
-// result, as much as its own rounding.  Up to 64 rows (DUP) the tile's other half holds the same queries again and
-// takes the second number, so that the one product does both; above, there is a second product.
+// result, as much as its own rounding.
 //
-// Every wait is bounded: when one runs out the status word becomes SPR_ERR_TIMEOUT, loader and issuing thread stop and
+// Every wait is bounded: when one runs out the status word becomes SPR_ERR_TIMEOUT, loaders and issuing threads stop and
 // wait (again bounded) for what is in flight, and the softmax warps go on without waiting and give NaN.
 #include <atomic>
 
@@ -32,41 +34,59 @@ namespace {
 
 using namespace pairtc;
 
-constexpr int kTcThreads = 256;
-constexpr int kSoftmaxThreads = 128;
-constexpr int kMmaWarp = 4, kFirstLoader = 5;    // one for keys, one for values (warp 7 idles)
+constexpr int kTcThreads = 512;
+constexpr int kGroupThreads = 128, kSoftmaxThreads = 2 * kGroupThreads;
+constexpr int kMmaWarp = 8, kQueryWarp = 10, kFirstLoader = 12;  // (warp 11 idles: registers are dealt out by fours of warps)
+constexpr int kTcRows = 128;
 constexpr int kPanel = kAttnTile * 128;                         // 64 keys by 64 columns
 constexpr float kRaise = 8.f;                                   // by how much scores may pass the maximum in use
-// TMEM columns: two buffers of S, 64 each, where P's two numbers take 32 and 32; O
-constexpr int kColS = 0, kColO = 128, kTmemCols = 256;
+// TMEM columns: two buffers of S for each group, 64 each, where P's two numbers take 32 and 32; each group's O
+constexpr int kColS = 0, kColO = 256, kTmemCols = 512;
 
 template <int PANELS>
 struct TcShape {
     static constexpr int unit = PANELS * kPanel;                 // a tile's keys, or its values
-    static constexpr int units = 8 / PANELS;                     // of the ring: keys and values by turns
+    static constexpr int units = 12;                             // of the ring: keys and values by turns.  A multiple of four:
+                                                                 // a unit's place then always is the same loader's and group's
     static constexpr int q_bytes = PANELS * 128 * 128;
-    static constexpr size_t smem = (size_t)q_bytes + (size_t)units * unit + 1024;
+    static constexpr size_t smem = (size_t)q_bytes + (size_t)units * unit;
 };
 
 struct TcControl {
-    uint64_t full[8], empty[8];
-    uint64_t s_full[2], p_ready[2], pv_done[2];   // by turns: a softmax warp may be a tile ahead of another, and of P V
-    uint64_t q_ready, drain;
-    uint64_t valid[8];                       // a bit for each key of a tile that is there
-    int64_t scratch[2 * (kTcThreads / 32) + 4];
-    unsigned long long odd;
-    int64_t o_live;
+    uint64_t full[12], empty[12];
+    uint64_t s_full[2][2], p_ready[2][2], pv_done[2][2];         // [group][buffer]
+    uint64_t q_full, q_empty, drain[2];
+    uint64_t valid[12];                      // a bit for each key of a tile that is there, of two rounds of the ring: keys leave it
+                                             // before the softmax warps have seen to their scores
+    unsigned long long odd[2];
+    int64_t o_live[2];
     uint32_t tmem;
     int abort, last;
-    int tree[kMaxTreeNodes];
-    uint32_t path[128][kMaxTreeNodes / 32];
+    int16_t tree[kMaxTreeNodes];             // parents, checked
+    union {
+        int64_t scratch[2 * (kTcThreads / 32) + 4];
+        float2 ml[2][kGroupThreads];
+    };
 };
+static_assert(TcShape<2>::smem + sizeof(TcControl) <= 232448, "shared memory of one CTA");
 
-__device__ __forceinline__ void softmax_meet() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void softmax_meet() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ void group_meet(int group)
+{
+    if (group)
+        asm volatile("bar.sync 3, 128;" ::: "memory");
+    else
+        asm volatile("bar.sync 2, 128;" ::: "memory");
+}
 __device__ __forceinline__ void arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there)
 {
     asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+// this lane arrives when its copies so far have come
+__device__ __forceinline__ void copies_arrive(uint64_t *bar)
+{
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
 __device__ __forceinline__ void mma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc)
 {
@@ -103,23 +123,27 @@ __device__ __forceinline__ void tmem_write32(uint32_t taddr, const uint32_t (&r)
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ bool finite_bf16x2(uint32_t w) { return (w & 0x7f80u) != 0x7f80u && (w & 0x7f800000u) != 0x7f800000u; }
-// 64 bits of a path from node `at` on
-__device__ __forceinline__ uint64_t path_bits64(const uint32_t *path, int at)
+// which of the nodes first .. first + 63 node i sees: itself and its path
+__device__ __forceinline__ uint64_t seen_nodes(const int16_t *tree, int i, int first)
 {
-    constexpr int n = kMaxTreeNodes / 32;
-    const int w = at >> 5;
-    const uint32_t a = w < n ? path[w] : 0u, b = w + 1 < n ? path[w + 1] : 0u, c = w + 2 < n ? path[w + 2] : 0u;
-    return (uint64_t)__funnelshift_r(a, b, at & 31) | (uint64_t)__funnelshift_r(b, c, at & 31) << 32;
+    if (!tree) {
+        const int n = i + 1 - first;
+        return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1;
+    }
+    uint64_t bits = 0;
+    for (; i >= first && i >= 0; i = tree[i])        // (parents come first)
+        if (i - first < 64) bits |= 1ull << (i - first);
+    return bits;
 }
 
-template <int PANELS, bool DUP>
-__global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnParams p)
+template <int PANELS>
+__global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnParams p)
 {
-    constexpr int ROWS = DUP ? 64 : 128, COLS = 64 * PANELS;
+    constexpr int ROWS = kTcRows, COLS = 64 * PANELS;
     using Shape = TcShape<PANELS>;
-    extern __shared__ uint8_t raw[];
+    extern __shared__ __align__(1024) uint8_t raw[];
     __shared__ TcControl ctl;
-    const uint32_t q_tile = (smem_addr(raw) + 1023u) & ~1023u, ring = q_tile + Shape::q_bytes;
+    const uint32_t q_tile = smem_addr(raw), ring = q_tile + Shape::q_bytes;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t limit = p.spin_limit;
 
@@ -128,16 +152,23 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
             bar_init(&ctl.full[i], 32);          // each lane of the warp that brings it
             bar_init(&ctl.empty[i], 1);
         }
-        for (int i = 0; i < 2; ++i) {
-            bar_init(&ctl.s_full[i], 1);
-            bar_init(&ctl.p_ready[i], 4);
-            bar_init(&ctl.pv_done[i], 1);
+        for (int i = 0; i < 4; ++i) {
+            bar_init(&ctl.s_full[i >> 1][i & 1], 1);
+            bar_init(&ctl.p_ready[i >> 1][i & 1], 4);
+            bar_init(&ctl.pv_done[i >> 1][i & 1], 1);
         }
-        bar_init(&ctl.q_ready, 4);
-        bar_init(&ctl.drain, 1);
+        bar_init(&ctl.q_full, 32);
+        bar_init(&ctl.q_empty, 2);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(&ctl.drain[i], 1);
+            ctl.odd[i] = 0;
+            ctl.o_live[i] = -1;
+        }
         ctl.abort = 0;
-        ctl.odd = 0;
-        ctl.o_live = -1;
+        if (q_tile & 1023u) {                    // the swizzle goes by address (the array's alignment sees to it)
+            ctl.abort = 1;
+            raise_timeout(p.status);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kMmaWarp) {
@@ -150,31 +181,33 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
     __syncthreads();
     fence_after();
     const uint32_t tmem = ctl.tmem;
+    // lane's 16 bytes of a row of keys, values or queries
+    constexpr int kChunks = 8 * PANELS, kRowsAtOnce = 32 / kChunks;
+    const int c_row = lane / kChunks, c_chunk = lane % kChunks;
+    const bool c_in = c_chunk * 8 < p.D;
 
-    // (256 threads start with 128 registers each: 168 and 88 make the same sum)
-    if (warp >= 4) {
+    // 512 threads start with 128 registers each: 2 x 168 and 2 x 88 make the same sum
+    if (warp >= kFirstLoader) {
+        // ------------------------------------------------------------ loaders: keys or values of every other tile
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-      if (warp >= kFirstLoader) {
-        // ------------------------------------------------------------ loaders (the ring holds an even number of units: each
-        // has stages of its own, and sees every phase of their barriers)
-        constexpr int kChunks = 8 * PANELS, kRowsAtOnce = 32 / kChunks;
-        const int c_row = lane / kChunks, c_chunk = lane % kChunks;
-        const bool c_in = c_chunk * 8 < p.D;
+        const int kv = warp & 1, parity = (warp - kFirstLoader) >> 1;
         // rows 8 r + r0 + c_row of a unit lie at (c_dst + 128 (8 r + r0)) ^ (r0 << 4): r0 is a multiple of kRowsAtOnce
         const uint32_t c_dst = (c_chunk >> 3) * kPanel + c_row * 128 + (((c_chunk & 7) ^ c_row) << 4);
+        const __nv_bfloat16 *cache = static_cast<const __nv_bfloat16 *>(kv ? p.v : p.k);
         AttnPart part = {0, 0, 0, 0};
-        const int kv = warp - kFirstLoader;
-        int64_t unit = kv;
+        int64_t at = 0;                             // tiles of the stretch before the part
+        int unit = 2 * parity + kv;                 // place in the ring
+        uint32_t round = 0;
         bool alive = !(p.test_flags & ATTN_TEST_NO_LOADS);
-        while (kv < 2 && alive && attn_next<ROWS>(p, s, part)) {
+        while (alive && attn_next<ROWS>(p, s, part)) {
             int64_t keys = (int64_t)s.seq.len + s.seq.count;
             if (keys > (int64_t)p.max_pages * p.page_size) {
                 raise_status(p.status, SPR_ERR_BAD_PAGE);
                 keys = (int64_t)p.max_pages * p.page_size;
             }
             const int end = part.t0 + part.n;
-            auto find = [&](int tile) {             // lane 8 j + r: where run r (8 keys) of tile + j begins in the caches
-                const int t = tile + (lane >> 3);
+            auto find = [&](int tile) {             // lane 8 j + r: where run r (8 keys) of tile + 2 j begins in the caches
+                const int t = tile + 2 * (lane >> 3);
                 const int64_t slot = (int64_t)t * kAttnTile + 8 * (lane & 7);
                 if (t >= end || slot >= keys) return -1;
                 const uint32_t at = (uint32_t)((uint64_t)slot >> 3) / (uint32_t)(p.page_size >> 3);       // pages are whole runs
@@ -185,30 +218,29 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
                 }
                 return (page * p.Hkv + part.head) * p.page_size + (int)(slot - (int64_t)at * p.page_size);
             };
-            int next = find(part.t0);
-            for (int n = 0; alive && n < part.n; n += 4) {
+            int tile = part.t0 + (int)((at ^ parity) & 1);
+            at += part.n;
+            int next = find(tile);
+            while (alive && tile < end) {
                 const int rows = next;
-                next = find(part.t0 + n + 4);
-                for (int u = 0; alive && u < 4 && n + u < part.n; ++u) {
-                    const int64_t left = keys - ((int64_t)part.t0 + n + u) * kAttnTile;
+                next = find(tile + 8);
+                for (int u = 0; u < 4 && tile < end; ++u, tile += 2) {
+                    const int64_t left = keys - (int64_t)tile * kAttnTile;
                     uint64_t valid = left >= 64 ? ~0ull : (1ull << left) - 1;
                     const uint32_t runs = __ballot_sync(0xffffffffu, rows >= 0) >> (8 * u) & 0xffu;
                     if (runs != 0xffu)
                         for (int r = 0; r < 8; ++r)
                             if (!(runs >> r & 1)) valid &= ~(0xffull << (8 * r));
                     const bool all = valid == ~0ull;
-                    const int slot = (int)(unit % Shape::units);
-                    const uint32_t round = (uint32_t)(unit / Shape::units);
-                    if (round > 0 && !__all_sync(0xffffffffu, bar_wait(&ctl.empty[slot], (round - 1) & 1, &ctl.abort, p.status, limit))) {
+                    if (round > 0 && !__all_sync(0xffffffffu, bar_wait(&ctl.empty[unit], (round - 1) & 1, &ctl.abort, p.status, limit))) {
                         alive = false;
                         break;
                     }
                     if (kv == 0 && lane == 0) {
-                        ctl.valid[(unit >> 1) & 7] = valid;
+                        ctl.valid[(unit >> 1) + (round & 1) * (Shape::units / 2)] = valid;
                         __threadfence_block();
                     }
-                    const __nv_bfloat16 *cache = static_cast<const __nv_bfloat16 *>(kv ? p.v : p.k);
-                    const uint32_t dst = ring + slot * Shape::unit + c_dst;
+                    const uint32_t dst = ring + unit * Shape::unit + c_dst;
 #pragma unroll
                     for (int r = 0; r < 8; ++r) {
                         const int run = __shfl_sync(0xffffffffu, rows, 8 * u + r);
@@ -221,75 +253,111 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
                             from += kRowsAtOnce * p.D;
                         }
                     }
-                    // this lane arrives when its copies have
-                    asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_addr(&ctl.full[slot])) : "memory");
-                    unit += 2;
+                    copies_arrive(&ctl.full[unit]);
+                    unit += 4;
+                    if (unit >= Shape::units) {
+                        unit -= Shape::units;
+                        ++round;
+                    }
                 }
             }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");       // none is left when the CTA ends
-      } else {
-        // ------------------------------------------------------------ products
-        if (lane == 0) {
+    } else if (warp >= kMmaWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (warp == kQueryWarp) {
+            // -------------------------------------------------------- queries of a part, zeros behind them
+            AttnPart part;
+            uint32_t parts = 0;
+            bool alive = !(p.test_flags & ATTN_TEST_NO_LOADS);
+            while (alive && attn_next<ROWS>(p, s, part)) {
+                if (parts > 0 && !__all_sync(0xffffffffu, bar_wait(&ctl.q_empty, (parts - 1) & 1, &ctl.abort, p.status, limit))) break;
+                const int row0 = part.block * ROWS, rows = min(ROWS, s.seq.count * p.G - row0);
+                const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p.q);
+#pragma unroll 4
+                for (int r0 = 0; r0 < ROWS; r0 += kRowsAtOnce) {
+                    const int r = r0 + c_row, i = (row0 + r) / p.G, g = row0 + r - i * p.G;
+                    const bool there = c_in && r < rows;
+                    const int64_t from = there ? (((int64_t)s.seq.b * p.nodes.T + i) * p.Hq + part.head * p.G + g) * p.D + c_chunk * 8 : 0;
+                    copy16(q_tile + (c_chunk >> 3) * ROWS * 128 + r * 128 + (((c_chunk & 7) ^ (r & 7)) << 4), q + from, there);
+                }
+                copies_arrive(&ctl.q_full);
+                ++parts;
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+        } else if (warp < kQueryWarp && lane == 0) {
+            // -------------------------------------------------------- products of a group
+            const int group = warp - kMmaWarp;
             constexpr uint32_t kQk = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kAttnTile >> 3) << 17) | (8u << 24);
             constexpr uint32_t kPv = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(COLS >> 3) << 17) | (8u << 24);
+            const uint32_t col_s = tmem + kColS + 128 * group, col_o = tmem + kColO + 128 * group;
             AttnPart part;
-            int64_t at = 0;                 // tiles of the stretch
+            int64_t at = 0;                 // tiles of the stretch before the part
             uint32_t parts = 0;
             bool alive = true;
             auto wait = [&](uint64_t *bar, uint32_t parity) {
                 if (alive && !bar_wait(bar, parity & 1, &ctl.abort, p.status, limit)) alive = false;
                 return alive;
             };
-            // (where S of tile i goes P of tile i - 2 was: the product with it is complete when this is called)
+            // (where S of tile i goes P of tile i - 4, this group's last but one, was: the product with it is complete)
             auto scores = [&](int64_t i) {
-                const int slot = (int)((2 * i) % Shape::units), b = (int)(i & 1);
-                if (!wait(&ctl.full[slot], (uint32_t)((2 * i) / Shape::units))) return;
+                const int unit = (int)((2 * i) % Shape::units), b = (int)(i >> 1 & 1);
+                if (!wait(&ctl.full[unit], (uint32_t)((2 * i) / Shape::units))) return;
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // the lanes' copies, for the tensor core
                 fence_after();
-                const uint32_t k = ring + slot * Shape::unit;
+                const uint32_t k = ring + unit * Shape::unit;
 #pragma unroll
                 for (int q = 0; q < 4 * PANELS; ++q)
-                    mma_smem(tmem + kColS + 64 * b, tile_desc(q_tile + (q >> 2) * 128 * 128 + (q & 3) * 32, false),
+                    mma_smem(col_s + 64 * b, tile_desc(q_tile + (q >> 2) * ROWS * 128 + (q & 3) * 32, false),
                              tile_desc(k + (q >> 2) * kPanel + (q & 3) * 32, false), kQk, q != 0);
-                commit(&ctl.s_full[b]);
-                commit(&ctl.empty[slot]);
+                commit(&ctl.s_full[group][b]);
+                commit(&ctl.empty[unit]);
             };
             while (alive && attn_next<ROWS>(p, s, part)) {
-                if (!wait(&ctl.q_ready, parts++)) break;
-                scores(at);
-                if (part.n > 1) scores(at + 1);
-                for (int n = 0; alive && n < part.n; ++n, ++at) {
-                    const int slot = (int)((2 * at + 1) % Shape::units);
-                    if (!wait(&ctl.full[slot], (uint32_t)((2 * at + 1) / Shape::units)) || !wait(&ctl.p_ready[at & 1], (uint32_t)(at >> 1))) break;
+                const int64_t end = at + part.n;
+                int64_t mine = at + ((at ^ group) & 1);
+                at = end;
+                if (!wait(&ctl.q_full, parts++)) break;
+                if (mine < end) scores(mine);
+                if (mine + 2 < end) scores(mine + 2);
+                if (mine + 4 >= end) {          // no more scores of this part from this group
+                    if (mine < end)
+                        commit(&ctl.q_empty);
+                    else
+                        arrive(&ctl.q_empty);
+                }
+                for (bool begun = false; alive && mine < end; mine += 2, begun = true) {
+                    const int unit = (int)((2 * mine + 1) % Shape::units), b = (int)(mine >> 1 & 1);
+                    const uint32_t phase = (uint32_t)(mine >> 2);
+                    if (!wait(&ctl.full[unit], (uint32_t)((2 * mine + 1) / Shape::units)) || !wait(&ctl.p_ready[group][b], phase)) break;
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     fence_after();
-                    const uint32_t v = ring + slot * Shape::unit, w = tmem + kColS + 64 * (int)(at & 1);
-                    const bool live = n > 0 || *reinterpret_cast<volatile int64_t *>(&ctl.o_live) == at;
+                    const uint32_t v = ring + unit * Shape::unit, w = col_s + 64 * b;
+                    const bool live = begun || *reinterpret_cast<volatile int64_t *>(&ctl.o_live[group]) == mine;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        mma_tmem(tmem + kColO, w + 8 * q, tile_desc(v + q * 2048, true), kPv, live || q != 0);
-                        if (!DUP) mma_tmem(tmem + kColO, w + 32 + 8 * q, tile_desc(v + q * 2048, true), kPv, 1u);
+                        mma_tmem(col_o, w + 8 * q, tile_desc(v + q * 2048, true), kPv, live || q != 0);
+                        mma_tmem(col_o, w + 32 + 8 * q, tile_desc(v + q * 2048, true), kPv, 1u);
                     }
-                    commit(&ctl.pv_done[at & 1]);
-                    commit(&ctl.empty[slot]);
-                    if (n + 2 < part.n) {
-                        if (!wait(&ctl.pv_done[at & 1], (uint32_t)(at >> 1))) break;
-                        scores(at + 2);
+                    commit(&ctl.pv_done[group][b]);
+                    commit(&ctl.empty[unit]);
+                    if (mine + 4 < end) {
+                        if (!wait(&ctl.pv_done[group][b], phase)) break;
+                        scores(mine + 4);
+                        if (mine + 6 >= end) commit(&ctl.q_empty);
                     }
                 }
             }
-            commit(&ctl.drain);             // nothing of this CTA's products is left when its TMEM is given back
-            bar_wait_quiet(&ctl.drain, 0, limit);
+            commit(&ctl.drain[group]);      // nothing of this thread's products is left when TMEM is given back
+            bar_wait_quiet(&ctl.drain[group], 0, limit);
         }
         __syncwarp();
-      }
     } else {
         // ------------------------------------------------------------ softmax: a row per thread
         asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
-        const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16), col_o = lanes + kColO;
-        const int row = DUP ? tid & 63 : tid;               // in the block
-        const bool second = DUP && tid >= 64;               // this thread's weights are what rounding left
+        const int group = warp >> 2, row = tid & (kGroupThreads - 1);
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t col_o = lanes + kColO + 128 * group;
         const float c = p.abs_scale_log2;
         AttnPart part;
         int64_t at = 0;
@@ -304,68 +372,37 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
         };
         while (attn_next<ROWS>(p, s, part)) {
             const AttnTarget t = attn_target<ROWS>(p, s, part);
-            // this row's query (zeros where there is none; all products of the part before have been formed)
-            const bool in = row < t.rows;
-            const int64_t out_at = in ? attn_out_at(p, s, part, t.row0 + row) : 0;
-            softmax_meet();
-            {
-                const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + out_at);
-#pragma unroll
-                for (int k = 0; k < 8 * PANELS; ++k) {
-                    uint4 x = in && k * 8 < p.D ? __ldg(src + k) : make_uint4(0u, 0u, 0u, 0u);
-                    x.x ^= p.flip, x.y ^= p.flip, x.z ^= p.flip, x.w ^= p.flip;
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};"
-                                 ::"r"(q_tile + (k >> 3) * 128 * 128 + tid * 128 + (((k & 7) ^ (tid & 7)) << 4)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
-                }
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            warp_arrive(&ctl.q_ready);
-            const uint32_t *path = ctl.path[0];
-            if ((int64_t)(part.t0 + part.n) * kAttnTile > s.seq.len) {       // some tile holds nodes
-                const int i0 = (int)(t.row0 / p.G);
-                const int nodes = (int)((t.row0 + t.rows - 1) / p.G) - i0 + 1;
-                if (p.nodes.parents && tree_of != s.seq.b) {
-                    for (int j = tid; j < s.seq.count; j += kSoftmaxThreads) ctl.tree[j] = p.nodes.parents[(int64_t)s.seq.b * p.nodes.T + j];
-                    tree_of = s.seq.b;
-                    softmax_meet();
-                }
-                if (tid < nodes) {
-                    for (int w = (s.seq.count + 31) / 32; w < kMaxTreeNodes / 32; ++w) ctl.path[tid][w] = 0u;
-                    attn_path_bits(p.nodes.parents ? ctl.tree : nullptr, i0 + tid, ctl.path[tid], (s.seq.count + 31) / 32, p.status);
-                }
-                if (in) path = ctl.path[(int)((t.row0 + row) / p.G) - i0];
+            const bool in = row < t.rows, warp_in = (warp & 3) * 32 < t.rows;
+            const int node = in ? (int)((t.row0 + row) / p.G) : 0;
+            softmax_meet();                                 // (both groups have read both O, and the tree)
+            if (p.nodes.parents && tree_of != s.seq.b && (int64_t)(part.t0 + part.n) * kAttnTile > s.seq.len) {
+                for (int j = tid; j < s.seq.count; j += kSoftmaxThreads)
+                    ctl.tree[j] = (int16_t)checked_parent(p.nodes.parents[(int64_t)s.seq.b * p.nodes.T + j], j, p.status);
+                tree_of = s.seq.b;
                 softmax_meet();
             }
-
             float m = neg_inf(), l = 0.f;
-            for (int n = 0; n < part.n; ++n, ++at) {
-                const uint32_t col_s = lanes + kColS + 64 * (uint32_t)(at & 1);
-                const bool begun = n > 0;
+            int64_t mine = at + ((at ^ group) & 1);         // this group's next tile
+            const int64_t begin = at, end = at + part.n;
+            at = end;
+            const bool any = mine < end;
+            for (bool begun = false; mine < end; mine += 2, begun = true) {
+                const int b = (int)(mine >> 1 & 1);
+                const uint32_t phase = (uint32_t)(mine >> 2), col_s = lanes + kColS + 128 * group + 64 * b;
+                const uint32_t v_unit = ring + (int)((2 * mine + 1) % Shape::units) * Shape::unit;
                 float x[64];
-                wait(&ctl.s_full[at & 1], (uint32_t)(at >> 1));
-                fence_after();
-                tmem_read32(col_s, *reinterpret_cast<float (*)[32]>(x));
-                tmem_read32(col_s + 32, *reinterpret_cast<float (*)[32]>(x + 32));
-                tmem_wait();
-                const int64_t slot0 = ((int64_t)part.t0 + n) * kAttnTile;
-                const uint64_t valid = ctl.valid[at & 7];
-                const uint32_t v_unit = ring + (int)((2 * at + 1) % Shape::units) * Shape::unit;
+                wait(&ctl.s_full[group][b], phase);
+                const int64_t slot0 = (part.t0 + (mine - begin)) * kAttnTile;
                 const bool tail = slot0 + kAttnTile > s.seq.len;      // (alike in all threads, whatever went wrong: they meet)
                 unsigned long long odd = 0;
-                uint64_t vis = valid;
+                uint64_t vis = ctl.valid[mine % Shape::units];
                 if (tail) {
                     const int64_t d = s.seq.len - slot0;     // keys of the prefix
-                    vis &= d <= 0 ? path_bits64(path, (int)-d) : path_bits64(path, 0) << d | ((1ull << d) - 1);
-                }
-                if (vis != ~0ull) {
-#pragma unroll
-                    for (int i = 0; i < 64; ++i)
-                        if (!((i < 32 ? (uint32_t)vis : (uint32_t)(vis >> 32)) >> (i & 31) & 1)) x[i] = neg_inf();
-                }
-                if (tail) {
+                    const int16_t *tree = p.nodes.parents ? ctl.tree : nullptr;
+                    vis &= d <= 0 ? seen_nodes(tree, node, (int)-d) : seen_nodes(tree, node, 0) << d | ((1ull << d) - 1);
                     // values that are not finite, where not every row sees every key: each thread looks at half a key
-                    wait(&ctl.full[(2 * at + 1) % Shape::units], (uint32_t)((2 * at + 1) / Shape::units));
-                    const uint32_t v = v_unit + (tid >> 1) * 128 + (tid & 1) * 64;
+                    wait(&ctl.full[(2 * mine + 1) % Shape::units], (uint32_t)((2 * mine + 1) / Shape::units));
+                    const uint32_t v = v_unit + (row >> 1) * 128 + (row & 1) * 64;
                     bool bad = false;
 #pragma unroll
                     for (int k = 0; k < 4 * PANELS; ++k) {
@@ -373,10 +410,27 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
                         asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(v + (k >> 2) * kPanel + (k & 3) * 16) : "memory");
                         bad = bad || !(finite_bf16x2(w[0]) && finite_bf16x2(w[1]) && finite_bf16x2(w[2]) && finite_bf16x2(w[3]));
                     }
-                    softmax_meet();
-                    if (bad) atomicOr(&ctl.odd, 1ull << (tid >> 1));
-                    softmax_meet();
-                    odd = *reinterpret_cast<volatile unsigned long long *>(&ctl.odd);
+                    group_meet(group);
+                    if (bad) atomicOr(&ctl.odd[group], 1ull << (row >> 1));
+                    group_meet(group);
+                    odd = *reinterpret_cast<volatile unsigned long long *>(&ctl.odd[group]);
+                }
+                if (!warp_in && !odd) {                      // no row of this warp is in use: its part of P is not looked at
+                    warp_arrive(&ctl.p_ready[group][b]);
+                    continue;
+                }
+                fence_after();
+                tmem_read32(col_s, *reinterpret_cast<float (*)[32]>(x));
+                tmem_read32(col_s + 32, *reinterpret_cast<float (*)[32]>(x + 32));
+                tmem_wait();
+                if (p.flip) {
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) x[i] = -x[i];
+                }
+                if (vis != ~0ull) {
+#pragma unroll
+                    for (int i = 0; i < 64; ++i)
+                        if (!((i < 32 ? (uint32_t)vis : (uint32_t)(vis >> 32)) >> (i & 31) & 1)) x[i] = neg_inf();
                 }
                 float t4[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
@@ -384,7 +438,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
                 const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
                 // (m = -inf: nothing seen so far, and O holds nothing of this row)
                 const bool raise = top > m && (m == neg_inf() || (top - m) * c > kRaise);
-                if (begun && (__any_sync(0xffffffffu, raise) || odd)) wait(&ctl.pv_done[(at - 1) & 1], (uint32_t)((at - 1) >> 1));
+                if (begun && (__any_sync(0xffffffffu, raise) || odd)) wait(&ctl.pv_done[group][b ^ 1], (uint32_t)((mine - 2) >> 2));
                 if (__any_sync(0xffffffffu, raise)) {
                     const float a = raise && m != neg_inf() ? ex2((m - top) * c) : 1.f;
                     if (raise) m = top;
@@ -419,7 +473,6 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
                 if (odd) {
                     // taken out of the product, and added one by one to the rows that see them
                     fence_after();
-                    const uint32_t v = v_unit;
 #pragma unroll 1
                     for (int k = 0; k < 2 * PANELS; ++k) {
                         float o[32];
@@ -429,7 +482,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             if (!begun) o[i] = 0.f;
-                        for (unsigned long long rest = odd & vis; rest && !second; rest &= rest - 1) {
+                        for (unsigned long long rest = odd & vis; rest; rest &= rest - 1) {
                             const int key = __ffsll((long long)rest) - 1;
                             float weight = 0.f;
 #pragma unroll
@@ -438,7 +491,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
                             for (int i = 0; i < 16; ++i) {
                                 uint32_t y;
                                 asm volatile("ld.shared.u32 %0, [%1];" : "=r"(y)
-                                             : "r"(v + (k >> 1) * kPanel + key * 128 + ((((k & 1) * 4 + (i >> 2)) ^ (key & 7)) << 4) + (i & 3) * 4) : "memory");
+                                             : "r"(v_unit + (k >> 1) * kPanel + key * 128 + ((((k & 1) * 4 + (i >> 2)) ^ (key & 7)) << 4) + (i & 3) * 4) : "memory");
                                 o[2 * i] = fmaf(weight, __uint_as_float(y << 16), o[2 * i]);
                                 o[2 * i + 1] = fmaf(weight, __uint_as_float(y & 0xffff0000u), o[2 * i + 1]);
                             }
@@ -448,70 +501,60 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
                         for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(o[i]);
                         tmem_write32(col_o + 32 * k, w);
                     }
-                    softmax_meet();
-                    if (odd >> (tid >> 1) & 1)
+                    group_meet(group);
+                    if (odd >> (row >> 1) & 1)
                         for (int k = 0; k < 4 * PANELS; ++k)
-                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v + (tid >> 1) * 128 + (tid & 1) * 64 + (k >> 2) * kPanel + (k & 3) * 16), "r"(0u) : "memory");
+                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v_unit + (row >> 1) * 128 + (row & 1) * 64 + (k >> 2) * kPanel + (k & 3) * 16), "r"(0u) : "memory");
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    if (tid == 0) {
-                        ctl.odd = 0;
-                        if (!begun) ctl.o_live = at;
+                    if (row == 0) {
+                        ctl.odd[group] = 0;
+                        if (!begun) ctl.o_live[group] = mine;
                     }
-                    softmax_meet();
+                    group_meet(group);
                 }
                 uint32_t w[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-                if (!DUP || !second) tmem_write32(col_s, w);
-                if (!DUP || second) {
-                    const uint64_t minus = pack2(-1.f, -1.f);
+                tmem_write32(col_s, w);
+                const uint64_t minus = pack2(-1.f, -1.f);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        float a, b;
-                        unpack2(fma2(pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)), minus, pack2(x[2 * i], x[2 * i + 1])), a, b);
-                        w[i] = pack_bf16(a, b);
-                    }
-                    tmem_write32(col_s + (DUP ? 0 : 32), w);
+                for (int i = 0; i < 32; ++i) {
+                    float a, b;
+                    unpack2(fma2(pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)), minus, pack2(x[2 * i], x[2 * i + 1])), a, b);
+                    w[i] = pack_bf16(a, b);
                 }
+                tmem_write32(col_s + 32, w);
                 tmem_wait_st();
                 fence_before();
-                warp_arrive(&ctl.p_ready[at & 1]);
+                warp_arrive(&ctl.p_ready[group][b]);
             }
 
-            // -------------------------------------------------------- the part's results
-            wait(&ctl.pv_done[(at - 1) & 1], (uint32_t)((at - 1) >> 1));
-            fence_after();
+            // -------------------------------------------------------- the part's results: each group has half of the columns
+            if (any) wait(&ctl.pv_done[group][(mine - 2) >> 1 & 1], (uint32_t)((mine - 2) >> 2));
             if (dead) l = __int_as_float(0x7fc00000);       // what a wait that ran out leaves is no result
+            ctl.ml[group][row] = make_float2(m, l);
+            softmax_meet();
+            fence_after();
+            const float2 other = ctl.ml[group ^ 1][row];
+            const float top = fmaxf(m, other.x), shift = top == neg_inf() ? 0.f : top;
+            float by[2] = {ex2((m - shift) * c), ex2((other.x - shift) * c)};
+            l = l * by[0] + other.y * by[1];
+            const bool all = part.n > 1;                    // else the other group's O is not of this part, or this group's
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            if (DUP) {      // the second numbers' results, by way of the query tile
-                if (second) {
+            const int64_t out_at = in ? attn_out_at(p, s, part, t.row0 + row) : 0;
+            if (warp_in) {
 #pragma unroll 1
-                    for (int k = 0; k < 2 * PANELS; ++k) {
-                        float o[32];
-                        tmem_read32(col_o + 32 * k, o);
+                for (int k = group * PANELS; k < (group + 1) * PANELS; ++k) {
+                    float o[32], y[32];
+                    tmem_read32(lanes + kColO + 128 * (any ? group : group ^ 1) + 32 * k, o);
+                    tmem_wait();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] *= any ? by[0] : by[1];
+                    if (all) {
+                        tmem_read32(lanes + kColO + 128 * (group ^ 1) + 32 * k, y);
                         tmem_wait();
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};"
-                                         ::"r"(q_tile + row * COLS * 4 + (((8 * k + i) ^ (row & 7)) << 4)), "f"(o[4 * i]), "f"(o[4 * i + 1]), "f"(o[4 * i + 2]), "f"(o[4 * i + 3]) : "memory");
-                    }
-                }
-                softmax_meet();
-            }
-            if (!second) {
-#pragma unroll 1
-                for (int k = 0; k < 2 * PANELS; ++k) {
-                    float o[32];
-                    tmem_read32(col_o + 32 * k, o);
-                    tmem_wait();
-                    if (DUP) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            float y[4];
-                            asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(y[0]), "=f"(y[1]), "=f"(y[2]), "=f"(y[3])
-                                         : "r"(q_tile + row * COLS * 4 + (((8 * k + i) ^ (row & 7)) << 4)) : "memory");
-                            o[4 * i] += y[0], o[4 * i + 1] += y[1], o[4 * i + 2] += y[2], o[4 * i + 3] += y[3];
-                        }
+                        for (int i = 0; i < 32; ++i) o[i] = fmaf(y[i], by[1], o[i]);
                     }
                     if (in) {
 #pragma unroll
@@ -531,8 +574,8 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
                     }
                     __syncwarp();
                 }
-                if (!t.whole && in) __stcg(&p.part_ml[(int64_t)t.slot * ROWS + row], make_float2(m * c, l));
             }
+            if (!t.whole && group == 0 && in) __stcg(&p.part_ml[(int64_t)t.slot * ROWS + row], make_float2(top * c, l));
             fence_before();
             if (!t.whole) {
                 __threadfence();
@@ -554,26 +597,25 @@ __global__ void __launch_bounds__(kTcThreads, 2) attention_tc_kernel(const AttnP
     }
 }
 
-template <int PANELS, bool DUP>
+template <int PANELS>
 cudaError_t launch_tc(const AttnParams &p, int dev, cudaStream_t st)
 {
     static std::atomic<bool> attr_set[64];   // host threads may race to set it: all of them store `true`
     if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-        const cudaError_t e = cudaFuncSetAttribute(attention_tc_kernel<PANELS, DUP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        const cudaError_t e = cudaFuncSetAttribute(attention_tc_kernel<PANELS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                    (int)TcShape<PANELS>::smem);
         if (e != cudaSuccess) return e;
         if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
     }
-    attention_tc_kernel<PANELS, DUP><<<p.ctas, kTcThreads, TcShape<PANELS>::smem, st>>>(p);
+    attention_tc_kernel<PANELS><<<p.ctas, kTcThreads, TcShape<PANELS>::smem, st>>>(p);
     return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_attention_tc(const AttnParams &p, int rows, int dev, cudaStream_t st)
+cudaError_t launch_attention_tc(const AttnParams &p, int dev, cudaStream_t st)
 {
-    if (rows == 64) return p.D <= 64 ? launch_tc<1, true>(p, dev, st) : launch_tc<2, true>(p, dev, st);
-    return p.D <= 64 ? launch_tc<1, false>(p, dev, st) : launch_tc<2, false>(p, dev, st);
+    return p.D <= 64 ? launch_tc<1>(p, dev, st) : launch_tc<2>(p, dev, st);
 }
 
 }  // namespace spr

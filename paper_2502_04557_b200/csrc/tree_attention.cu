@@ -22,7 +22,7 @@ int attention_block_rows(int T, int G, int dt)
 {
     const int64_t rows = (int64_t)T * G;
     if (dt == SPR_F32) return rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
-    return rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
+    return rows <= 16 ? 16 : 128;
 }
 
 size_t attention_ws_bytes(int D, int dt)
@@ -73,7 +73,8 @@ int tree_attention(const void *q, const void *k_cache, const void *v_cache, int 
     p.scale_log2 = scale * kLog2e;
     p.abs_scale_log2 = fmaxf(fabsf(p.scale_log2), 1e-37f);
     p.flip = scale < 0.f ? 0x80008000u : 0u;
-    p.ctas = sms * kAttnCtasPerSm < kAttnMaxCtas ? sms * kAttnCtasPerSm : kAttnMaxCtas;
+    const int per_sm = rows == 128 ? 1 : kAttnCtasPerSm;
+    p.ctas = sms < 148 ? sms * per_sm : 148 * per_sm;
     p.status = static_cast<int *>(ws);
     p.counters = at<int>(ws, w.counters);
     p.part = at<float>(ws, w.part);
@@ -82,7 +83,7 @@ int tree_attention(const void *q, const void *k_cache, const void *v_cache, int 
     p.test_flags = t_test_flags;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (dt == SPR_F32) return finish(launch_attention_f32(p, rows, st));
-    return finish(rows == 16 ? launch_attention_mma(p, dev, st) : launch_attention_tc(p, rows, dev, st));
+    return finish(rows == 16 ? launch_attention_mma(p, dev, st) : launch_attention_tc(p, dev, st));
 }
 
 void spr_test_tree_attention(int flags, unsigned spin_limit)
