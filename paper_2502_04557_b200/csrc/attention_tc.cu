@@ -8,10 +8,10 @@
 // nothing of one another until the end of a part: a tile takes a softmax warp some 2000 clocks, most of it latency.
 // All 512 columns of TMEM are in use: 2 x 2 S, 2 O.
 //
-// Four loader warps bring keys and values into a ring of six tiles (cp.async, 16 bytes per lane, into the 128-byte
-// swizzle that the matrix descriptors name: a warp takes 1500 clocks to ask for 16 KB, and pages of 16 entries would be 2 KB
-// boxes for the copy engine, whose number sets its time), another the queries.  Copies report to the barriers themselves.
-// Loaders run ahead into the next part while this one ends.  Every warp that waits on a barrier sees all of its phases.
+// A loader warp brings keys and values into a ring of six tiles (cp.async, 16 bytes per lane, into the 128-byte
+// swizzle that the matrix descriptors name: pages of 16 entries would be 2 KB boxes for the copy engine, whose
+// number sets its time), another the queries.  Copies report to the barriers themselves.
+// The loader runs ahead into the next part while this one ends.  Every warp that waits on a barrier sees all of its phases.
 //
 // The maximum that exponents are taken against is only raised when a score passes it by 2^8 (weights then stay below
 // 2^8, and sums and products in fp32 keep their relative precision), so that O, which lives in TMEM, is hardly ever rescaled.
@@ -34,9 +34,9 @@ namespace {
 
 using namespace pairtc;
 
-constexpr int kTcThreads = 512;
+constexpr int kTcThreads = 384;
 constexpr int kGroupThreads = 128, kSoftmaxThreads = 2 * kGroupThreads;
-constexpr int kMmaWarp = 8, kQueryWarp = 10, kFirstLoader = 12;  // (warp 11 idles: registers are dealt out by fours of warps)
+constexpr int kMmaWarp = 8, kQueryWarp = 10, kLoader = 11;
 constexpr int kTcRows = 128;
 constexpr int kPanel = kAttnTile * 128;                         // 64 keys by 64 columns
 constexpr float kRaise = 8.f;                                   // by how much scores may pass the maximum in use
@@ -47,7 +47,7 @@ template <int PANELS>
 struct TcShape {
     static constexpr int unit = PANELS * kPanel;                 // a tile's keys, or its values
     static constexpr int units = 12;                             // of the ring: keys and values by turns.  A multiple of four:
-                                                                 // a unit's place then always is the same loader's and group's
+                                                                 // a unit's place then always is the same group's
     static constexpr int q_bytes = PANELS * 128 * 128;
     static constexpr size_t smem = (size_t)q_bytes + (size_t)units * unit;
 };
@@ -79,7 +79,11 @@ __device__ __forceinline__ void group_meet(int group)
         asm volatile("bar.sync 2, 128;" ::: "memory");
 }
 __device__ __forceinline__ void arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there)
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there)      // or zeros
 {
     asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
@@ -136,7 +140,8 @@ __device__ __forceinline__ uint64_t seen_nodes(const int16_t *tree, int i, int f
     return bits;
 }
 
-template <int PANELS>
+// WHOLE: heads are whole panels, so that the distances between rows are known
+template <int PANELS, bool WHOLE>
 __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnParams p)
 {
     constexpr int ROWS = kTcRows, COLS = 64 * PANELS;
@@ -186,17 +191,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
     const int c_row = lane / kChunks, c_chunk = lane % kChunks;
     const bool c_in = c_chunk * 8 < p.D;
 
-    // 512 threads start with 128 registers each: 2 x 168 and 2 x 88 make the same sum
-    if (warp >= kFirstLoader) {
-        // ------------------------------------------------------------ loaders: keys or values of every other tile
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        const int kv = warp & 1, parity = (warp - kFirstLoader) >> 1;
+    if (warp == kLoader) {
+        // ------------------------------------------------------------ keys and values
         // rows 8 r + r0 + c_row of a unit lie at (c_dst + 128 (8 r + r0)) ^ (r0 << 4): r0 is a multiple of kRowsAtOnce
         const uint32_t c_dst = (c_chunk >> 3) * kPanel + c_row * 128 + (((c_chunk & 7) ^ c_row) << 4);
-        const __nv_bfloat16 *cache = static_cast<const __nv_bfloat16 *>(kv ? p.v : p.k);
+        const int D = WHOLE ? COLS : p.D;
         AttnPart part = {0, 0, 0, 0};
-        int64_t at = 0;                             // tiles of the stretch before the part
-        int unit = 2 * parity + kv;                 // place in the ring
+        int unit = 0;                               // place in the ring
         uint32_t round = 0;
         bool alive = !(p.test_flags & ATTN_TEST_NO_LOADS);
         while (alive && attn_next<ROWS>(p, s, part)) {
@@ -206,8 +207,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 keys = (int64_t)p.max_pages * p.page_size;
             }
             const int end = part.t0 + part.n;
-            auto find = [&](int tile) {             // lane 8 j + r: where run r (8 keys) of tile + 2 j begins in the caches
-                const int t = tile + 2 * (lane >> 3);
+            auto find = [&](int tile) {             // lane 8 j + r: where run r (8 keys) of tile + j begins in the caches
+                const int t = tile + (lane >> 3);
                 const int64_t slot = (int64_t)t * kAttnTile + 8 * (lane & 7);
                 if (t >= end || slot >= keys) return -1;
                 const uint32_t at = (uint32_t)((uint64_t)slot >> 3) / (uint32_t)(p.page_size >> 3);       // pages are whole runs
@@ -218,53 +219,57 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 }
                 return (page * p.Hkv + part.head) * p.page_size + (int)(slot - (int64_t)at * p.page_size);
             };
-            int tile = part.t0 + (int)((at ^ parity) & 1);
-            at += part.n;
-            int next = find(tile);
+            int tile = part.t0, next = find(tile);
             while (alive && tile < end) {
                 const int rows = next;
-                next = find(tile + 8);
-                for (int u = 0; u < 4 && tile < end; ++u, tile += 2) {
+                next = find(tile + 4);
+                for (int u = 0; alive && u < 4 && tile < end; ++u, ++tile) {
                     const int64_t left = keys - (int64_t)tile * kAttnTile;
                     uint64_t valid = left >= 64 ? ~0ull : (1ull << left) - 1;
                     const uint32_t runs = __ballot_sync(0xffffffffu, rows >= 0) >> (8 * u) & 0xffu;
                     if (runs != 0xffu)
                         for (int r = 0; r < 8; ++r)
                             if (!(runs >> r & 1)) valid &= ~(0xffull << (8 * r));
-                    const bool all = valid == ~0ull;
-                    if (round > 0 && !__all_sync(0xffffffffu, bar_wait(&ctl.empty[unit], (round - 1) & 1, &ctl.abort, p.status, limit))) {
-                        alive = false;
-                        break;
-                    }
-                    if (kv == 0 && lane == 0) {
-                        ctl.valid[(unit >> 1) + (round & 1) * (Shape::units / 2)] = valid;
-                        __threadfence_block();
-                    }
-                    const uint32_t dst = ring + unit * Shape::unit + c_dst;
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        const int run = __shfl_sync(0xffffffffu, rows, 8 * u + r);
-                        const __nv_bfloat16 *from = cache + (run < 0 ? 0 : ((int64_t)run + c_row) * p.D + c_chunk * 8);
-#pragma unroll
-                        for (int i = 0; i < 8 / kRowsAtOnce; ++i) {
-                            const int r0 = i * kRowsAtOnce;
-                            const bool there = c_in && (all || (valid >> (8 * r + r0 + c_row) & 1));
-                            copy16((dst + (8 * r + r0) * 128) ^ (r0 << 4), there ? from : cache, there);
-                            from += kRowsAtOnce * p.D;
+#pragma unroll 1
+                    for (int kv = 0; kv < 2; ++kv) {
+                        if (round > 0 && !__all_sync(0xffffffffu, bar_wait(&ctl.empty[unit], (round - 1) & 1, &ctl.abort, p.status, limit))) {
+                            alive = false;
+                            break;
                         }
-                    }
-                    copies_arrive(&ctl.full[unit]);
-                    unit += 4;
-                    if (unit >= Shape::units) {
-                        unit -= Shape::units;
-                        ++round;
+                        if (kv == 0 && lane == 0) {
+                            ctl.valid[(unit >> 1) + (round & 1) * (Shape::units / 2)] = valid;
+                            __threadfence_block();
+                        }
+                        const __nv_bfloat16 *cache = static_cast<const __nv_bfloat16 *>(kv ? p.v : p.k) + c_row * D + c_chunk * 8;
+                        const uint32_t dst = ring + unit * Shape::unit + c_dst;
+                        if (WHOLE && valid == ~0ull) {
+#pragma unroll
+                            for (int r = 0; r < 8; ++r) {
+                                const __nv_bfloat16 *from = cache + (int64_t)__shfl_sync(0xffffffffu, rows, 8 * u + r) * COLS;
+#pragma unroll
+                                for (int r0 = 0; r0 < 8; r0 += kRowsAtOnce) copy16((dst ^ (r0 << 4)) + (8 * r + r0) * 128, from + r0 * COLS);
+                            }
+                        } else {
+#pragma unroll 1
+                            for (int r = 0; r < 8; ++r) {
+                                const int run = __shfl_sync(0xffffffffu, rows, 8 * u + r);
+                                for (int r0 = 0; r0 < 8; r0 += kRowsAtOnce) {
+                                    const bool there = c_in && (valid >> (8 * r + r0 + c_row) & 1);
+                                    copy16((dst ^ (r0 << 4)) + (8 * r + r0) * 128, there ? cache + ((int64_t)run + r0) * D : p.k, there);
+                                }
+                            }
+                        }
+                        copies_arrive(&ctl.full[unit]);
+                        if (++unit == Shape::units) {
+                            unit = 0;
+                            ++round;
+                        }
                     }
                 }
             }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");       // none is left when the CTA ends
     } else if (warp >= kMmaWarp) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (warp == kQueryWarp) {
             // -------------------------------------------------------- queries of a part, zeros behind them
             AttnPart part;
@@ -354,7 +359,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
         __syncwarp();
     } else {
         // ------------------------------------------------------------ softmax: a row per thread
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
         const int group = warp >> 2, row = tid & (kGroupThreads - 1);
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t col_o = lanes + kColO + 128 * group;
@@ -597,17 +601,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
     }
 }
 
-template <int PANELS>
+template <int PANELS, bool WHOLE>
 cudaError_t launch_tc(const AttnParams &p, int dev, cudaStream_t st)
 {
     static std::atomic<bool> attr_set[64];   // host threads may race to set it: all of them store `true`
     if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-        const cudaError_t e = cudaFuncSetAttribute(attention_tc_kernel<PANELS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        const cudaError_t e = cudaFuncSetAttribute(attention_tc_kernel<PANELS, WHOLE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                    (int)TcShape<PANELS>::smem);
         if (e != cudaSuccess) return e;
         if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
     }
-    attention_tc_kernel<PANELS><<<p.ctas, kTcThreads, TcShape<PANELS>::smem, st>>>(p);
+    attention_tc_kernel<PANELS, WHOLE><<<p.ctas, kTcThreads, TcShape<PANELS>::smem, st>>>(p);
     return cudaGetLastError();
 }
 
@@ -615,7 +619,9 @@ cudaError_t launch_tc(const AttnParams &p, int dev, cudaStream_t st)
 
 cudaError_t launch_attention_tc(const AttnParams &p, int dev, cudaStream_t st)
 {
-    return p.D <= 64 ? launch_tc<1>(p, dev, st) : launch_tc<2>(p, dev, st);
+    if (p.D == 128) return launch_tc<2, true>(p, dev, st);
+    if (p.D == 64) return launch_tc<1, true>(p, dev, st);
+    return p.D < 64 ? launch_tc<1, false>(p, dev, st) : launch_tc<2, false>(p, dev, st);
 }
 
 }  // namespace spr
