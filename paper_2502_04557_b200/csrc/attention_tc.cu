@@ -277,14 +277,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             bool alive = !(p.test_flags & ATTN_TEST_NO_LOADS);
             while (alive && attn_next<ROWS>(p, s, part)) {
                 if (parts > 0 && !__all_sync(0xffffffffu, bar_wait(&ctl.q_empty, (parts - 1) & 1, &ctl.abort, p.status, limit))) break;
+                // (rows behind the block's last are whatever was there: nobody looks at what becomes of them)
                 const int row0 = part.block * ROWS, rows = min(ROWS, s.seq.count * p.G - row0);
-                const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p.q);
-#pragma unroll 4
-                for (int r0 = 0; r0 < ROWS; r0 += kRowsAtOnce) {
-                    const int r = r0 + c_row, i = (row0 + r) / p.G, g = row0 + r - i * p.G;
-                    const bool there = c_in && r < rows;
-                    const int64_t from = there ? (((int64_t)s.seq.b * p.nodes.T + i) * p.Hq + part.head * p.G + g) * p.D + c_chunk * 8 : 0;
-                    copy16(q_tile + (c_chunk >> 3) * ROWS * 128 + r * 128 + (((c_chunk & 7) ^ (r & 7)) << 4), q + from, there);
+                int i = (row0 + c_row) / p.G, g = row0 + c_row - i * p.G;
+                const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p.q) + ((int64_t)s.seq.b * p.nodes.T * p.Hq + part.head * p.G) * p.D + c_chunk * 8;
+                const uint32_t dst = q_tile + (c_chunk >> 3) * ROWS * 128 + c_row * 128 + (((c_chunk & 7) ^ c_row) << 4);
+                for (int r0 = 0; r0 < rows; r0 += kRowsAtOnce) {
+                    const bool there = c_in && r0 + c_row < rows;
+                    copy16((dst ^ ((r0 & 7) << 4)) + r0 * 128, there ? q + ((int64_t)i * p.Hq + g) * p.D : static_cast<const __nv_bfloat16 *>(p.q), there);
+                    for (g += kRowsAtOnce; g >= p.G; g -= p.G) ++i;
                 }
                 copies_arrive(&ctl.q_full);
                 ++parts;
@@ -299,15 +300,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             AttnPart part;
             int64_t at = 0;                 // tiles of the stretch before the part
             uint32_t parts = 0;
+            int v_unit = 2 * group + 1;     // place of the values of this group's next tile
+            uint32_t v_round = 0;
             bool alive = true;
             auto wait = [&](uint64_t *bar, uint32_t parity) {
                 if (alive && !bar_wait(bar, parity & 1, &ctl.abort, p.status, limit)) alive = false;
                 return alive;
             };
             // (where S of tile i goes P of tile i - 4, this group's last but one, was: the product with it is complete)
+            int k_unit = 2 * group;             // place of the keys of this group's next tile
+            uint32_t k_round = 0;
             auto scores = [&](int64_t i) {
-                const int unit = (int)((2 * i) % Shape::units), b = (int)(i >> 1 & 1);
-                if (!wait(&ctl.full[unit], (uint32_t)((2 * i) / Shape::units))) return;
+                const int unit = k_unit, b = (int)i >> 1 & 1;
+                if (!wait(&ctl.full[unit], k_round)) return;
+                k_unit += 4;
+                if (k_unit >= Shape::units) {
+                    k_unit -= Shape::units;
+                    ++k_round;
+                }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // the lanes' copies, for the tensor core
                 fence_after();
                 const uint32_t k = ring + unit * Shape::unit;
@@ -332,9 +342,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                         arrive(&ctl.q_empty);
                 }
                 for (bool begun = false; alive && mine < end; mine += 2, begun = true) {
-                    const int unit = (int)((2 * mine + 1) % Shape::units), b = (int)(mine >> 1 & 1);
+                    const int unit = v_unit, b = (int)mine >> 1 & 1;
                     const uint32_t phase = (uint32_t)(mine >> 2);
-                    if (!wait(&ctl.full[unit], (uint32_t)((2 * mine + 1) / Shape::units)) || !wait(&ctl.p_ready[group][b], phase)) break;
+                    if (!wait(&ctl.full[unit], v_round) || !wait(&ctl.p_ready[group][b], phase)) break;
+                    v_unit += 4;
+                    if (v_unit >= Shape::units) {
+                        v_unit -= Shape::units;
+                        ++v_round;
+                    }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     fence_after();
                     const uint32_t v = ring + unit * Shape::unit, w = col_s + 64 * b;
@@ -368,7 +383,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
         int tree_of = -1;
         bool dead = false;
         auto wait = [&](uint64_t *bar, uint32_t parity) {
-            if (!dead) dead = !__all_sync(0xffffffffu, bar_wait(bar, parity & 1, &ctl.abort, p.status, limit));
+            if (!dead && !bar_poll(bar, parity & 1)) dead = !bar_wait(bar, parity & 1, &ctl.abort, p.status, limit);
         };
         auto warp_arrive = [&](uint64_t *bar) {
             __syncwarp();
@@ -390,23 +405,23 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             const int64_t begin = at, end = at + part.n;
             at = end;
             const bool any = mine < end;
-            for (bool begun = false; mine < end; mine += 2, begun = true) {
-                const int b = (int)(mine >> 1 & 1);
+            int64_t slot0 = (part.t0 + (mine - begin)) * kAttnTile;
+            int place = (int)(mine % Shape::units);         // of the tile in two rounds of the ring
+            for (bool begun = false; mine < end; mine += 2, begun = true, slot0 += 2 * kAttnTile, place = place < Shape::units - 2 ? place + 2 : place + 2 - Shape::units) {
+                const int b = (int)mine >> 1 & 1;
                 const uint32_t phase = (uint32_t)(mine >> 2), col_s = lanes + kColS + 128 * group + 64 * b;
-                const uint32_t v_unit = ring + (int)((2 * mine + 1) % Shape::units) * Shape::unit;
                 float x[64];
                 wait(&ctl.s_full[group][b], phase);
-                const int64_t slot0 = (part.t0 + (mine - begin)) * kAttnTile;
                 const bool tail = slot0 + kAttnTile > s.seq.len;      // (alike in all threads, whatever went wrong: they meet)
                 unsigned long long odd = 0;
-                uint64_t vis = ctl.valid[mine % Shape::units];
+                uint64_t vis = ctl.valid[place];
                 if (tail) {
                     const int64_t d = s.seq.len - slot0;     // keys of the prefix
                     const int16_t *tree = p.nodes.parents ? ctl.tree : nullptr;
                     vis &= d <= 0 ? seen_nodes(tree, node, (int)-d) : seen_nodes(tree, node, 0) << d | ((1ull << d) - 1);
                     // values that are not finite, where not every row sees every key: each thread looks at half a key
-                    wait(&ctl.full[(2 * mine + 1) % Shape::units], (uint32_t)((2 * mine + 1) / Shape::units));
-                    const uint32_t v = v_unit + (row >> 1) * 128 + (row & 1) * 64;
+                    wait(&ctl.full[(2 * place + 1) % Shape::units], (uint32_t)(mine / (Shape::units / 2)));
+                    const uint32_t v = ring + (2 * place + 1) % Shape::units * Shape::unit + (row >> 1) * 128 + (row & 1) * 64;
                     bool bad = false;
 #pragma unroll
                     for (int k = 0; k < 4 * PANELS; ++k) {
@@ -442,8 +457,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
                 // (m = -inf: nothing seen so far, and O holds nothing of this row)
                 const bool raise = top > m && (m == neg_inf() || (top - m) * c > kRaise);
-                if (begun && (__any_sync(0xffffffffu, raise) || odd)) wait(&ctl.pv_done[group][b ^ 1], (uint32_t)((mine - 2) >> 2));
-                if (__any_sync(0xffffffffu, raise)) {
+                const bool some = __any_sync(0xffffffffu, raise);
+                if (begun && (some || odd)) wait(&ctl.pv_done[group][b ^ 1], (uint32_t)((mine - 2) >> 2));
+                if (some) {
                     const float a = raise && m != neg_inf() ? ex2((m - top) * c) : 1.f;
                     if (raise) m = top;
                     l *= a;
@@ -476,6 +492,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 l += sum0 + sum1;
                 if (odd) {
                     // taken out of the product, and added one by one to the rows that see them
+                    const uint32_t v_unit = ring + (2 * place + 1) % Shape::units * Shape::unit;
                     fence_after();
 #pragma unroll 1
                     for (int k = 0; k < 2 * PANELS; ++k) {
