@@ -8,10 +8,10 @@
 // nothing of one another until the end of a part: a tile takes a softmax warp some 2000 clocks, most of it latency.
 // All 512 columns of TMEM are in use: 2 x 2 S, 2 O.
 //
-// A loader warp brings keys and values into a ring of six tiles (cp.async, 16 bytes per lane, into the 128-byte
-// swizzle that the matrix descriptors name: pages of 16 entries would be 2 KB boxes for the copy engine, whose
-// number sets its time), another the queries.  Copies report to the barriers themselves.
-// The loader runs ahead into the next part while this one ends.  Every warp that waits on a barrier sees all of its phases.
+// One loader warp brings keys, one values and queries, into a ring of six tiles (cp.async, 16 bytes per lane, into the
+// 128-byte swizzle that the matrix descriptors name: pages of 16 entries would be 2 KB boxes for the copy engine, whose
+// number sets its time; a warp takes some 800 clocks per 16 KB).  Copies report to the barriers themselves.
+// Loaders run ahead into the next part while this one ends.  Every warp that waits on a barrier sees all of its phases.
 //
 // The maximum that exponents are taken against is only raised when a score passes it by 2^8 (weights then stay below
 // 2^8, and sums and products in fp32 keep their relative precision), so that O, which lives in TMEM, is hardly ever rescaled.
@@ -36,7 +36,7 @@ using namespace pairtc;
 
 constexpr int kTcThreads = 384;
 constexpr int kGroupThreads = 128, kSoftmaxThreads = 2 * kGroupThreads;
-constexpr int kMmaWarp = 8, kQueryWarp = 10, kLoader = 11;
+constexpr int kMmaWarp = 8, kFirstLoader = 10;                  // (keys, values)
 constexpr int kTcRows = 128;
 constexpr int kPanel = kAttnTile * 128;                         // 64 keys by 64 columns
 constexpr float kRaise = 8.f;                                   // by how much scores may pass the maximum in use
@@ -191,16 +191,36 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
     const int c_row = lane / kChunks, c_chunk = lane % kChunks;
     const bool c_in = c_chunk * 8 < p.D;
 
-    if (warp == kLoader) {
-        // ------------------------------------------------------------ keys and values
+    // a wait that is most often over
+    auto quick_wait = [&](uint64_t *bar, uint32_t parity) {
+        return bar_poll(bar, parity & 1) || bar_wait(bar, parity & 1, &ctl.abort, p.status, limit);
+    };
+    if (warp >= kFirstLoader) {
+        // ------------------------------------------------------------ keys; values and queries
+        const int kv = warp - kFirstLoader;
         // rows 8 r + r0 + c_row of a unit lie at (c_dst + 128 (8 r + r0)) ^ (r0 << 4): r0 is a multiple of kRowsAtOnce
         const uint32_t c_dst = (c_chunk >> 3) * kPanel + c_row * 128 + (((c_chunk & 7) ^ c_row) << 4);
         const int D = WHOLE ? COLS : p.D;
         AttnPart part = {0, 0, 0, 0};
-        int unit = 0;                               // place in the ring
-        uint32_t round = 0;
+        int unit = kv;                              // place in the ring
+        uint32_t round = 0, parts = 0;
         bool alive = !(p.test_flags & ATTN_TEST_NO_LOADS);
         while (alive && attn_next<ROWS>(p, s, part)) {
+            if (kv) {
+                // the part's queries (rows behind the block's last are whatever was there: nobody looks at what becomes of them)
+                if (parts > 0 && !__all_sync(0xffffffffu, quick_wait(&ctl.q_empty, parts - 1))) break;
+                ++parts;
+                const int row0 = part.block * ROWS, rows = min(ROWS, s.seq.count * p.G - row0);
+                int i = (row0 + c_row) / p.G, g = row0 + c_row - i * p.G;
+                const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p.q) + ((int64_t)s.seq.b * p.nodes.T * p.Hq + part.head * p.G) * D + c_chunk * 8;
+                const uint32_t dst = q_tile + (c_chunk >> 3) * ROWS * 128 + c_row * 128 + (((c_chunk & 7) ^ c_row) << 4);
+                for (int r0 = 0; r0 < rows; r0 += kRowsAtOnce) {
+                    const bool there = c_in && r0 + c_row < rows;
+                    copy16((dst ^ ((r0 & 7) << 4)) + r0 * 128, there ? q + ((int64_t)i * p.Hq + g) * D : static_cast<const __nv_bfloat16 *>(p.q), there);
+                    for (g += kRowsAtOnce; g >= p.G; g -= p.G) ++i;
+                }
+                copies_arrive(&ctl.q_full);
+            }
             int64_t keys = (int64_t)s.seq.len + s.seq.count;
             if (keys > (int64_t)p.max_pages * p.page_size) {
                 raise_status(p.status, SPR_ERR_BAD_PAGE);
@@ -230,68 +250,45 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                     if (runs != 0xffu)
                         for (int r = 0; r < 8; ++r)
                             if (!(runs >> r & 1)) valid &= ~(0xffull << (8 * r));
-#pragma unroll 1
-                    for (int kv = 0; kv < 2; ++kv) {
-                        if (round > 0 && !__all_sync(0xffffffffu, bar_wait(&ctl.empty[unit], (round - 1) & 1, &ctl.abort, p.status, limit))) {
-                            alive = false;
-                            break;
-                        }
-                        if (kv == 0 && lane == 0) {
-                            ctl.valid[(unit >> 1) + (round & 1) * (Shape::units / 2)] = valid;
-                            __threadfence_block();
-                        }
-                        const __nv_bfloat16 *cache = static_cast<const __nv_bfloat16 *>(kv ? p.v : p.k) + c_row * D + c_chunk * 8;
-                        const uint32_t dst = ring + unit * Shape::unit + c_dst;
-                        if (WHOLE && valid == ~0ull) {
+                    if (round > 0 && !__all_sync(0xffffffffu, quick_wait(&ctl.empty[unit], round - 1))) {
+                        alive = false;
+                        break;
+                    }
+                    if (kv == 0 && lane == 0) {
+                        ctl.valid[(unit >> 1) + (round & 1) * (Shape::units / 2)] = valid;
+                        __threadfence_block();
+                    }
+                    const __nv_bfloat16 *cache = static_cast<const __nv_bfloat16 *>(kv ? p.v : p.k) + c_row * D + c_chunk * 8;
+                    const uint32_t dst = ring + unit * Shape::unit + c_dst;
+                    if (WHOLE && valid == ~0ull) {
 #pragma unroll
-                            for (int r = 0; r < 8; ++r) {
-                                const __nv_bfloat16 *from = cache + (int64_t)__shfl_sync(0xffffffffu, rows, 8 * u + r) * COLS;
+                        for (int r = 0; r < 8; ++r) {
+                            const __nv_bfloat16 *from = cache + (int64_t)__shfl_sync(0xffffffffu, rows, 8 * u + r) * COLS;
 #pragma unroll
-                                for (int r0 = 0; r0 < 8; r0 += kRowsAtOnce) copy16((dst ^ (r0 << 4)) + (8 * r + r0) * 128, from + r0 * COLS);
-                            }
-                        } else {
+                            for (int r0 = 0; r0 < 8; r0 += kRowsAtOnce) copy16((dst ^ (r0 << 4)) + (8 * r + r0) * 128, from + r0 * COLS);
+                        }
+                    } else {
 #pragma unroll 1
-                            for (int r = 0; r < 8; ++r) {
-                                const int run = __shfl_sync(0xffffffffu, rows, 8 * u + r);
-                                for (int r0 = 0; r0 < 8; r0 += kRowsAtOnce) {
-                                    const bool there = c_in && (valid >> (8 * r + r0 + c_row) & 1);
-                                    copy16((dst ^ (r0 << 4)) + (8 * r + r0) * 128, there ? cache + ((int64_t)run + r0) * D : p.k, there);
-                                }
+                        for (int r = 0; r < 8; ++r) {
+                            const int run = __shfl_sync(0xffffffffu, rows, 8 * u + r);
+                            for (int r0 = 0; r0 < 8; r0 += kRowsAtOnce) {
+                                const bool there = c_in && (valid >> (8 * r + r0 + c_row) & 1);
+                                copy16((dst ^ (r0 << 4)) + (8 * r + r0) * 128, there ? cache + ((int64_t)run + r0) * D : p.k, there);
                             }
                         }
-                        copies_arrive(&ctl.full[unit]);
-                        if (++unit == Shape::units) {
-                            unit = 0;
-                            ++round;
-                        }
+                    }
+                    copies_arrive(&ctl.full[unit]);
+                    unit += 2;
+                    if (unit >= Shape::units) {
+                        unit -= Shape::units;
+                        ++round;
                     }
                 }
             }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");       // none is left when the CTA ends
     } else if (warp >= kMmaWarp) {
-        if (warp == kQueryWarp) {
-            // -------------------------------------------------------- queries of a part, zeros behind them
-            AttnPart part;
-            uint32_t parts = 0;
-            bool alive = !(p.test_flags & ATTN_TEST_NO_LOADS);
-            while (alive && attn_next<ROWS>(p, s, part)) {
-                if (parts > 0 && !__all_sync(0xffffffffu, bar_wait(&ctl.q_empty, (parts - 1) & 1, &ctl.abort, p.status, limit))) break;
-                // (rows behind the block's last are whatever was there: nobody looks at what becomes of them)
-                const int row0 = part.block * ROWS, rows = min(ROWS, s.seq.count * p.G - row0);
-                int i = (row0 + c_row) / p.G, g = row0 + c_row - i * p.G;
-                const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p.q) + ((int64_t)s.seq.b * p.nodes.T * p.Hq + part.head * p.G) * p.D + c_chunk * 8;
-                const uint32_t dst = q_tile + (c_chunk >> 3) * ROWS * 128 + c_row * 128 + (((c_chunk & 7) ^ c_row) << 4);
-                for (int r0 = 0; r0 < rows; r0 += kRowsAtOnce) {
-                    const bool there = c_in && r0 + c_row < rows;
-                    copy16((dst ^ ((r0 & 7) << 4)) + r0 * 128, there ? q + ((int64_t)i * p.Hq + g) * p.D : static_cast<const __nv_bfloat16 *>(p.q), there);
-                    for (g += kRowsAtOnce; g >= p.G; g -= p.G) ++i;
-                }
-                copies_arrive(&ctl.q_full);
-                ++parts;
-            }
-            asm volatile("cp.async.wait_all;" ::: "memory");
-        } else if (warp < kQueryWarp && lane == 0) {
+        if (lane == 0) {
             // -------------------------------------------------------- products of a group
             const int group = warp - kMmaWarp;
             constexpr uint32_t kQk = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kAttnTile >> 3) << 17) | (8u << 24);
@@ -304,15 +301,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             uint32_t v_round = 0;
             bool alive = true;
             auto wait = [&](uint64_t *bar, uint32_t parity) {
-                if (alive && !bar_wait(bar, parity & 1, &ctl.abort, p.status, limit)) alive = false;
+                if (alive && !quick_wait(bar, parity)) alive = false;
                 return alive;
             };
-            // (where S of tile i goes P of tile i - 4, this group's last but one, was: the product with it is complete)
+            // where S of tile i goes P of tile i - 4, this group's last but one, was: the product with it has to be complete
             int k_unit = 2 * group;             // place of the keys of this group's next tile
             uint32_t k_round = 0;
-            auto scores = [&](int64_t i) {
+            auto scores = [&](int64_t i, bool behind) {
                 const int unit = k_unit, b = (int)i >> 1 & 1;
-                if (!wait(&ctl.full[unit], k_round)) return;
+                if (!wait(&ctl.full[unit], k_round) || (behind && !wait(&ctl.pv_done[group][b], (uint32_t)(i >> 2) - 1))) return;
                 k_unit += 4;
                 if (k_unit >= Shape::units) {
                     k_unit -= Shape::units;
@@ -333,8 +330,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 int64_t mine = at + ((at ^ group) & 1);
                 at = end;
                 if (!wait(&ctl.q_full, parts++)) break;
-                if (mine < end) scores(mine);
-                if (mine + 2 < end) scores(mine + 2);
+                if (mine < end) scores(mine, false);
+                if (mine + 2 < end) scores(mine + 2, false);
                 if (mine + 4 >= end) {          // no more scores of this part from this group
                     if (mine < end)
                         commit(&ctl.q_empty);
@@ -362,8 +359,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                     commit(&ctl.pv_done[group][b]);
                     commit(&ctl.empty[unit]);
                     if (mine + 4 < end) {
-                        if (!wait(&ctl.pv_done[group][b], phase)) break;
-                        scores(mine + 4);
+                        scores(mine + 4, true);
                         if (mine + 6 >= end) commit(&ctl.q_empty);
                     }
                 }
@@ -383,7 +379,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
         int tree_of = -1;
         bool dead = false;
         auto wait = [&](uint64_t *bar, uint32_t parity) {
-            if (!dead && !bar_poll(bar, parity & 1)) dead = !bar_wait(bar, parity & 1, &ctl.abort, p.status, limit);
+            if (!dead) dead = !quick_wait(bar, parity);
         };
         auto warp_arrive = [&](uint64_t *bar) {
             __syncwarp();
