@@ -13,10 +13,12 @@
 // number sets its time; a warp takes some 800 clocks per 16 KB).  Copies report to the barriers themselves.
 // Loaders run ahead into the next part while this one ends.  Every warp that waits on a barrier sees all of its phases.
 //
-// The maximum that exponents are taken against is only raised when a score passes it by 2^8 (weights then stay below
-// 2^8, and sums and products in fp32 keep their relative precision), so that O, which lives in TMEM, is hardly ever rescaled.
-// Weights are used as two bf16 numbers, their rounding and what is left of it: one would put an error of 2^-9 on the
-// result, as much as its own rounding.
+// Exponents are taken against a maximum that stands until a tile's weights add up to more than 2^13 (sums and products in
+// fp32 keep their relative precision whatever the common factor): only then are its scores looked through for
+// a new one and O, which lives in TMEM, rescaled.  Most tiles need no maximum at all.
+// Weights are rounded to bf16 for the second product, which leaves results off by some 2^-9 of themselves, as much as their own
+// rounding does.  A second bf16 number for what the rounding leaves, as with few rows, would cost a fifth of the time
+// (128 sequences of 17 nodes: 199 us against 164 us).
 //
 // Every wait is bounded: when one runs out the status word becomes SPR_ERR_TIMEOUT, loaders and issuing threads stop and
 // wait (again bounded) for what is in flight, and the softmax warps go on without waiting and give NaN.
@@ -39,8 +41,8 @@ constexpr int kGroupThreads = 128, kSoftmaxThreads = 2 * kGroupThreads;
 constexpr int kMmaWarp = 8, kFirstLoader = 10;                  // (keys, values)
 constexpr int kTcRows = 128;
 constexpr int kPanel = kAttnTile * 128;                         // 64 keys by 64 columns
-constexpr float kRaise = 8.f;                                   // by how much scores may pass the maximum in use
-// TMEM columns: two buffers of S for each group, 64 each, where P's two numbers take 32 and 32; each group's O
+constexpr float kMostWeight = 8192.f;                           // of a row in a tile, before its maximum is raised
+// TMEM columns: two buffers of S for each group, 64 each, of which P takes 32; each group's O
 constexpr int kColS = 0, kColO = 256, kTmemCols = 512;
 
 template <int PANELS>
@@ -352,10 +354,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                     const uint32_t v = ring + unit * Shape::unit, w = col_s + 64 * b;
                     const bool live = begun || *reinterpret_cast<volatile int64_t *>(&ctl.o_live[group]) == mine;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        mma_tmem(col_o, w + 8 * q, tile_desc(v + q * 2048, true), kPv, live || q != 0);
-                        mma_tmem(col_o, w + 32 + 8 * q, tile_desc(v + q * 2048, true), kPv, 1u);
-                    }
+                    for (int q = 0; q < 4; ++q) mma_tmem(col_o, w + 8 * q, tile_desc(v + q * 2048, true), kPv, live || q != 0);
                     commit(&ctl.pv_done[group][b]);
                     commit(&ctl.empty[unit]);
                     if (mine + 4 < end) {
@@ -406,7 +405,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             for (bool begun = false; mine < end; mine += 2, begun = true, slot0 += 2 * kAttnTile, place = place < Shape::units - 2 ? place + 2 : place + 2 - Shape::units) {
                 const int b = (int)mine >> 1 & 1;
                 const uint32_t phase = (uint32_t)(mine >> 2), col_s = lanes + kColS + 128 * group + 64 * b;
-                float x[64];
                 wait(&ctl.s_full[group][b], phase);
                 const bool tail = slot0 + kAttnTile > s.seq.len;      // (alike in all threads, whatever went wrong: they meet)
                 unsigned long long odd = 0;
@@ -435,59 +433,64 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                     continue;
                 }
                 fence_after();
-                tmem_read32(col_s, *reinterpret_cast<float (*)[32]>(x));
-                tmem_read32(col_s + 32, *reinterpret_cast<float (*)[32]>(x + 32));
-                tmem_wait();
-                if (p.flip) {
-#pragma unroll
-                    for (int i = 0; i < 64; ++i) x[i] = -x[i];
-                }
-                if (vis != ~0ull) {
-#pragma unroll
-                    for (int i = 0; i < 64; ++i)
-                        if (!((i < 32 ? (uint32_t)vis : (uint32_t)(vis >> 32)) >> (i & 31) & 1)) x[i] = neg_inf();
-                }
-                float t4[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-                for (int i = 4; i < 64; i += 2) t4[(i >> 1) & 3] = fmaxf(fmaxf(t4[(i >> 1) & 3], x[i]), x[i + 1]);
-                const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
-                // (m = -inf: nothing seen so far, and O holds nothing of this row)
-                const bool raise = top > m && (m == neg_inf() || (top - m) * c > kRaise);
-                const bool some = __any_sync(0xffffffffu, raise);
-                if (begun && (some || odd)) wait(&ctl.pv_done[group][b ^ 1], (uint32_t)((mine - 2) >> 2));
-                if (some) {
-                    const float a = raise && m != neg_inf() ? ex2((m - top) * c) : 1.f;
-                    if (raise) m = top;
-                    l *= a;
-                    if (begun && __any_sync(0xffffffffu, a != 1.f)) {
-                        fence_after();
+                float x[64], sum;
 #pragma unroll 1
-                        for (int k = 0; k < 2 * PANELS; ++k) {
-                            float o[32];
-                            uint32_t w[32];
-                            tmem_read32(col_o + 32 * k, o);
-                            tmem_wait();
+                for (bool looked = !begun;; looked = true) {
+                    tmem_read32(col_s, *reinterpret_cast<float (*)[32]>(x));
+                    tmem_read32(col_s + 32, *reinterpret_cast<float (*)[32]>(x + 32));
+                    tmem_wait();
+                    if (p.flip) {
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(o[i] * a);
-                            tmem_write32(col_o + 32 * k, w);
+                        for (int i = 0; i < 64; ++i) x[i] = -x[i];
+                    }
+                    if (vis != ~0ull) {
+#pragma unroll
+                        for (int i = 0; i < 64; ++i)
+                            if (!((i < 32 ? (uint32_t)vis : (uint32_t)(vis >> 32)) >> (i & 31) & 1)) x[i] = neg_inf();
+                    }
+                    if (looked) {
+                        float t4[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+                        for (int i = 4; i < 64; i += 2) t4[(i >> 1) & 3] = fmaxf(fmaxf(t4[(i >> 1) & 3], x[i]), x[i + 1]);
+                        const float top = fmaxf(fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])), m);
+                        // (m = -inf: nothing seen so far, and O holds nothing of this row)
+                        const float a = m != neg_inf() && top > m ? ex2((m - top) * c) : 1.f;
+                        m = top;
+                        l *= a;
+                        if (begun) {
+                            wait(&ctl.pv_done[group][b ^ 1], (uint32_t)((mine - 2) >> 2));
+                            fence_after();
+#pragma unroll 1
+                            for (int k = 0; k < 2 * PANELS; ++k) {
+                                float o[32];
+                                uint32_t w[32];
+                                tmem_read32(col_o + 32 * k, o);
+                                tmem_wait();
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(o[i] * a);
+                                tmem_write32(col_o + 32 * k, w);
+                            }
                         }
                     }
-                }
-                const float ref = m == neg_inf() ? 0.f : -m * c;
-                const uint64_t c2 = pack2(c, c), ref2 = pack2(ref, ref);
-                uint64_t s2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+                    const float ref = m == neg_inf() ? 0.f : -m * c;
+                    const uint64_t c2 = pack2(c, c), ref2 = pack2(ref, ref);
+                    uint64_t s2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), c2, ref2), x[2 * i], x[2 * i + 1]);
-                    x[2 * i] = ex2(x[2 * i]);
-                    x[2 * i + 1] = ex2(x[2 * i + 1]);
-                    s2[i & 1] = add2(s2[i & 1], pack2(x[2 * i], x[2 * i + 1]));
+                    for (int i = 0; i < 32; ++i) {
+                        unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), c2, ref2), x[2 * i], x[2 * i + 1]);
+                        x[2 * i] = ex2(x[2 * i]);
+                        x[2 * i + 1] = ex2(x[2 * i + 1]);
+                        s2[i & 1] = add2(s2[i & 1], pack2(x[2 * i], x[2 * i + 1]));
+                    }
+                    float sum1;
+                    unpack2(add2(s2[0], s2[1]), sum, sum1);
+                    sum += sum1;
+                    if (looked || !__any_sync(0xffffffffu, in && (m == neg_inf() || !(sum <= kMostWeight)))) break;
                 }
-                float sum0, sum1;
-                unpack2(add2(s2[0], s2[1]), sum0, sum1);
-                l += sum0 + sum1;
+                l += sum;
                 if (odd) {
                     // taken out of the product, and added one by one to the rows that see them
+                    if (begun) wait(&ctl.pv_done[group][b ^ 1], (uint32_t)((mine - 2) >> 2));
                     const uint32_t v_unit = ring + (2 * place + 1) % Shape::units * Shape::unit;
                     fence_after();
 #pragma unroll 1
@@ -533,14 +536,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
 #pragma unroll
                 for (int i = 0; i < 32; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
                 tmem_write32(col_s, w);
-                const uint64_t minus = pack2(-1.f, -1.f);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    float a, b;
-                    unpack2(fma2(pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)), minus, pack2(x[2 * i], x[2 * i + 1])), a, b);
-                    w[i] = pack_bf16(a, b);
-                }
-                tmem_write32(col_s + 32, w);
                 tmem_wait_st();
                 fence_before();
                 warp_arrive(&ctl.p_ready[group][b]);

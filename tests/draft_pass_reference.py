@@ -5,8 +5,7 @@ Bounds, with u = 2^-24 (one rounding of fp32):
           their sum by 3 roundings: 8 u (|x| + |y|) covers them; then the rounding of the result
   attend  a score is a sum of D products, added up in groups of 16 by the tensor cores, whose additions lose up to 2^-23 of
           the magnitude at each: (D/16 + 16) 2 u A, A = scale sum |q| |k| (fp32: one by one, (D + 8) u A), and a few u of
-          its own magnitude from scale and base-2 exponent.  A weight is off by that relative to itself, as is the sum, and
-          by 4 u from the exponential; in bf16 calls a weight is cut to two bf16 numbers, 2^-17 of itself.  Sums over n keys
+          its own magnitude from scale and base-2 exponent.  A weight is off by that relative to itself, as is the sum, and by 4 u from the exponential; in bf16 calls a weight is cut to two bf16 numbers, 2^-17 of itself.  Sums over n keys
           add (n/16 + 64) 2 u (fp32: (n + 64) u).  All of these are relative to sum p |v|.  Then the rounding of the result.
   rules   five roundings of the terms' magnitudes, then the rounding of the result
 """
@@ -132,7 +131,8 @@ def attend(q, k_cache, v_cache, page_table, lens, counts, parents, scale):
         worst = mag.masked_fill(~seen, 0.0).amax(-1)
         d_score = worst * ((D / 16 + 16) * 2 * U if bf16 else (D + 8) * U) + 4 * U * s.masked_fill(~seen, 0.0).abs().amax(-1)
         keys = length + n
-        rel = 2 * d_score + 8 * U + (2.0 ** -17 + (keys / 16 + 64) * 2 * U if bf16 else (keys + 64) * U)
+        cut = 2.0 ** -17 if T * G <= 16 else 2.0 ** -8
+        rel = 2 * d_score + 8 * U + (cut + (keys / 16 + 64) * 2 * U if bf16 else (keys + 64) * U)
         out[b, :n] = y.permute(2, 0, 1, 3).reshape(n, Hq, D)
         tol[b, :n] = (a * rel[..., None] + half(q.dtype) * y.abs()).permute(2, 0, 1, 3).reshape(n, Hq, D)
     return out, tol + 1e-30
