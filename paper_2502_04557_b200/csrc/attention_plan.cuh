@@ -54,7 +54,7 @@ __device__ __forceinline__ bool attn_next(const AttnParams &p, AttnStretch &s, A
         s.at -= s.seq.total(p.Hkv);
         s.seq = attn_seq<ROWS>(p, s.seq.b + 1);
     }
-    const int item = (int)(s.at / s.seq.tiles);
+    const int item = s.at >> 31 ? (int)(s.at / s.seq.tiles) : (int)((uint32_t)s.at / (uint32_t)s.seq.tiles);
     part.t0 = (int)(s.at - (int64_t)item * s.seq.tiles);
     part.head = item / s.seq.blocks;
     part.block = item - part.head * s.seq.blocks;

@@ -213,13 +213,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 if (parts > 0 && !__all_sync(0xffffffffu, quick_wait(&ctl.q_empty, parts - 1))) break;
                 ++parts;
                 const int row0 = part.block * ROWS, rows = min(ROWS, s.seq.count * p.G - row0);
-                int i = (row0 + c_row) / p.G, g = row0 + c_row - i * p.G;
-                const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p.q) + ((int64_t)s.seq.b * p.nodes.T * p.Hq + part.head * p.G) * D + c_chunk * 8;
+                const int i0 = row0 / p.G, g0 = row0 - i0 * p.G;
+                const float per_node = 1.f / (float)p.G;
+                const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p.q) +
+                                         (((int64_t)s.seq.b * p.nodes.T + i0) * p.Hq + part.head * p.G + g0) * D + c_chunk * 8;
+                const int hop = (p.Hq - p.G) * D;           // from a node's last row to the next one's first, in elements
                 const uint32_t dst = q_tile + (c_chunk >> 3) * ROWS * 128 + c_row * 128 + (((c_chunk & 7) ^ c_row) << 4);
+#pragma unroll 4
                 for (int r0 = 0; r0 < rows; r0 += kRowsAtOnce) {
-                    const bool there = c_in && r0 + c_row < rows;
-                    copy16((dst ^ ((r0 & 7) << 4)) + r0 * 128, there ? q + ((int64_t)i * p.Hq + g) * D : static_cast<const __nv_bfloat16 *>(p.q), there);
-                    for (g += kRowsAtOnce; g >= p.G; g -= p.G) ++i;
+                    const int r = r0 + c_row;
+                    const int i = (int)(((float)(g0 + r) + 0.5f) * per_node);       // (g0 + r) / G: both are small
+                    const bool there = c_in && r < rows;
+                    copy16((dst ^ ((r0 & 7) << 4)) + r0 * 128, q + (there ? r * D + (int64_t)i * hop : 0), there);
                 }
                 copies_arrive(&ctl.q_full);
             }
@@ -309,9 +314,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             // where S of tile i goes P of tile i - 4, this group's last but one, was: the product with it has to be complete
             int k_unit = 2 * group;             // place of the keys of this group's next tile
             uint32_t k_round = 0;
-            auto scores = [&](int64_t i, bool behind) {
+            auto scores = [&](int64_t i) {
                 const int unit = k_unit, b = (int)i >> 1 & 1;
-                if (!wait(&ctl.full[unit], k_round) || (behind && !wait(&ctl.pv_done[group][b], (uint32_t)(i >> 2) - 1))) return;
+                if (!wait(&ctl.full[unit], k_round) || (i >= 4 && !wait(&ctl.pv_done[group][b], (uint32_t)(i >> 2) - 1))) return;
                 k_unit += 4;
                 if (k_unit >= Shape::units) {
                     k_unit -= Shape::units;
@@ -332,8 +337,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 int64_t mine = at + ((at ^ group) & 1);
                 at = end;
                 if (!wait(&ctl.q_full, parts++)) break;
-                if (mine < end) scores(mine, false);
-                if (mine + 2 < end) scores(mine + 2, false);
+                if (mine < end) scores(mine);
+                if (mine + 2 < end) scores(mine + 2);
                 if (mine + 4 >= end) {          // no more scores of this part from this group
                     if (mine < end)
                         commit(&ctl.q_empty);
@@ -358,7 +363,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                     commit(&ctl.pv_done[group][b]);
                     commit(&ctl.empty[unit]);
                     if (mine + 4 < end) {
-                        scores(mine + 4, true);
+                        scores(mine + 4);
                         if (mine + 6 >= end) commit(&ctl.q_empty);
                     }
                 }
