@@ -441,7 +441,7 @@ int verifier_train_step8(const void *packed, const uint8_t *labels, int64_t N, i
  *   all the same); positions stay what they are.  After the check of a tree this puts the nodes that were kept at the
  *   slots behind the prefix: slot = position.  No two nodes may be given one slot.
  * Entries of the cache that no node is put in are left as they were.  T is not limited for chains: prompts go the
- * same way.  A node whose slot has no page is put nowhere.  D <= 1024.
+ * same way.  A node whose slot has no page is put nowhere.  D <= 1024, Hq + 2 Hkv <= 4096.
  * Workspace: the status word (spr_workspace_bytes(SPR_OP_CACHE_APPEND, ...)).
  */
 int cache_append(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,

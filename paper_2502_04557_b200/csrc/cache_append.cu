@@ -5,7 +5,8 @@
 // The product is formed in double and reduced to [-pi, pi] there: at position 131072 an fp32 product would be off
 // by 0.008 rad.  Sine and cosine of the reduced angle are fp32, and so is the rotation; results are rounded once.
 // Bound by memory: every element is read once and written once.  One CTA has one node (all heads of a token share
-// its angles, which are formed once into shared memory).
+// its angles, which are formed once into shared memory).  A thread asks for its first vectors before it looks up where
+// they go: the length, the parents, the page and the angles take some 2000 clocks one after the other.
 #include "common.cuh"
 #include "draft_tree.cuh"
 #include "host_util.h"
@@ -30,36 +31,38 @@ struct AppendParams {
     int Hq, Hkv, D, pairs;                   // pairs = rotated elements / 2
     int interleaved;
     int max_pages, num_pages, page_size;
+    int rotated, copied;                     // units of a rotated head, of a value head (see append_kernel)
+    uint32_t rotated_inv, copied_inv;        // 2^32 / these, rounded up
 };
 
+// what a thread moves at once, as it lies in memory, and as numbers
 template <typename T>
 struct Vec;
 template <>
 struct Vec<float> {
     static constexpr int n = 4;
-    float x[4];
-    __device__ __forceinline__ void load(const float *p)
-    {
-        const float4 a = *reinterpret_cast<const float4 *>(p);
-        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
-    }
-    __device__ __forceinline__ void store(float *p) const { *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]); }
+    float4 raw;
+    __device__ __forceinline__ void load(const float *p) { raw = __ldcs(reinterpret_cast<const float4 *>(p)); }
+    __device__ __forceinline__ void store(float *p) const { *reinterpret_cast<float4 *>(p) = raw; }
+    __device__ __forceinline__ void get(float (&x)[4]) const { x[0] = raw.x, x[1] = raw.y, x[2] = raw.z, x[3] = raw.w; }
+    __device__ __forceinline__ void set(const float (&x)[4]) { raw = make_float4(x[0], x[1], x[2], x[3]); }
 };
 template <>
 struct Vec<__nv_bfloat16> {
     static constexpr int n = 8;
-    float x[8];
-    __device__ __forceinline__ void load(const __nv_bfloat16 *p)
+    uint4 raw;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { raw = __ldcs(reinterpret_cast<const uint4 *>(p)); }
+    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = raw; }
+    __device__ __forceinline__ void get(float (&x)[8]) const
     {
-        const uint4 a = *reinterpret_cast<const uint4 *>(p);
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             x[2 * e] = __uint_as_float(w[e] << 16);
             x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
         }
     }
-    __device__ __forceinline__ void store(__nv_bfloat16 *p) const
+    __device__ __forceinline__ void set(const float (&x)[8])
     {
         uint32_t w[4];
 #pragma unroll
@@ -67,131 +70,172 @@ struct Vec<__nv_bfloat16> {
             const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * e], x[2 * e + 1]);
             w[e] = *reinterpret_cast<const uint32_t *>(&b);
         }
-        *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        raw = make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
 // one element at a time, for rows that are not made of whole aligned vectors
 template <typename T>
 struct One {
     static constexpr int n = 1;
-    float x[1];
-    __device__ __forceinline__ void load(const T *p) { x[0] = (float)*p; }
-    __device__ __forceinline__ void store(T *p) const { *p = (T)x[0]; }
+    T raw;
+    __device__ __forceinline__ void load(const T *p) { raw = *p; }
+    __device__ __forceinline__ void store(T *p) const { *p = raw; }
+    __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = (float)raw; }
+    __device__ __forceinline__ void set(const float (&x)[1]) { raw = (T)x[0]; }
 };
 
-// V: the vector that a thread moves; x runs over a head's vectors, y over heads
-template <typename T, typename V>
+__device__ __forceinline__ int divide(int x, int by, uint32_t inv) { return by == 1 ? x : (int)__umulhi((uint32_t)x, inv); }
+
+// A unit is what a thread moves at once.  Pairs of halves: a vector V and its partner `pairs` elements on; behind them, in
+// the rest of a head, and in value heads: one vector.  Adjacent pairs: one vector (of one element: two).
+template <typename T, typename V, bool ADJACENT>
+struct Unit {
+    static constexpr int n = V::n;
+    static constexpr bool kTwo = !ADJACENT || n == 1;      // a rotated unit is two vectors
+    V a, o;
+    int head, col, by;                                     // by: distance of the partner, 0 where there is none
+    __device__ __forceinline__ void place(const AppendParams &p, int u)
+    {
+        const int turned = (p.Hq + p.Hkv) * p.rotated;
+        const bool is_v = u >= turned;
+        if (is_v) u -= turned;
+        const int h = is_v ? divide(u, p.copied, p.copied_inv) : divide(u, p.rotated, p.rotated_inv);
+        const int j = u - h * (is_v ? p.copied : p.rotated);
+        head = is_v ? h + p.Hq + p.Hkv : h;
+        const int two = is_v || !kTwo ? 0 : p.pairs / n;   // units of two vectors
+        by = j < two ? (ADJACENT ? 1 : p.pairs) : 0;
+        col = j < two ? (ADJACENT ? 2 * j : j * n) : (is_v || !kTwo ? j * n : 2 * p.pairs + (j - two) * n);
+    }
+    __device__ __forceinline__ void load(const AppendParams &p, int64_t node)
+    {
+        const bool is_q = head < p.Hq, is_v = head >= p.Hq + p.Hkv;
+        const T *src = is_q   ? static_cast<const T *>(p.q) + node * p.q_stride + (int64_t)head * p.D
+                       : is_v ? static_cast<const T *>(p.v) + node * p.v_stride + (int64_t)(head - p.Hq - p.Hkv) * p.D
+                              : static_cast<const T *>(p.k) + node * p.k_stride + (int64_t)(head - p.Hq) * p.D;
+        a.load(src + col);
+        if (by) o.load(src + col + by);
+    }
+    // entry: where head 0's row of the node lies in the caches, in rows; negative: nowhere
+    __device__ __forceinline__ void store(const AppendParams &p, int64_t node, int64_t entry, const float2 *turn)
+    {
+        const bool is_q = head < p.Hq, is_v = head >= p.Hq + p.Hkv;
+        if (!is_q && entry < 0) return;
+        T *dst = is_q   ? static_cast<T *>(p.q_out) + (node * p.Hq + head) * p.D
+                 : is_v ? static_cast<T *>(p.v_cache) + (entry + (int64_t)(head - p.Hq - p.Hkv) * p.page_size) * p.D
+                        : static_cast<T *>(p.k_cache) + (entry + (int64_t)(head - p.Hq) * p.page_size) * p.D;
+        if (by) {
+            float x[n], y[n];
+            a.get(x);
+            o.get(y);
+#pragma unroll
+            for (int e = 0; e < n; ++e) {
+                const float2 t = turn[ADJACENT ? col / 2 : col + e];
+                const float z = x[e];
+                x[e] = z * t.x - y[e] * t.y;
+                y[e] = y[e] * t.x + z * t.y;
+            }
+            a.set(x);
+            o.set(y);
+            o.store(dst + col + by);
+        } else if (!kTwo && !is_v && col < 2 * p.pairs) {
+            float x[n];
+            a.get(x);
+#pragma unroll
+            for (int e = 0; e + 1 < n; e += 2)
+                if ((col + e) / 2 < p.pairs) {
+                    const float2 t = turn[(col + e) / 2];
+                    const float z = x[e], y = x[e + 1];
+                    x[e] = z * t.x - y * t.y;
+                    x[e + 1] = y * t.x + z * t.y;
+                }
+            a.set(x);
+        }
+        a.store(dst + col);
+    }
+};
+
+template <typename T, typename V, bool ADJACENT>
 __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendParams p)
 {
+    constexpr int kAhead = ADJACENT ? 3 : 2;
     __shared__ float2 turn[kMaxRotPairs];
     __shared__ int tree[kMaxTreeNodes];
     const int64_t node = blockIdx.x;
+    const int tid = threadIdx.x, units = (p.Hq + p.Hkv) * p.rotated + p.Hkv * p.copied;
+    Unit<T, V, ADJACENT> unit[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+        if (tid + k * kAppendThreads < units) {
+            unit[k].place(p, tid + k * kAppendThreads);
+            unit[k].load(p, node);
+        }
     const int b = (int)(node / p.nodes.T), i = (int)(node - (int64_t)b * p.nodes.T);
+    const int given = p.slots ? __ldg(p.slots + node) : 0;
     const int len = __ldg(p.nodes.lens + b);
     const bool used = len >= 0 && i < node_count(p.nodes, b);
-    const int tid = threadIdx.y * blockDim.x + threadIdx.x, threads = blockDim.x * blockDim.y;
-    T *q_out = static_cast<T *>(p.q_out) + node * p.Hq * p.D;
     if (!used) {
-        if (p.q_out)
-            for (int c = tid; c < p.Hq * p.D; c += threads) q_out[c] = (T)0.f;
+        T *q_out = static_cast<T *>(p.q_out) + node * p.Hq * p.D;
+        for (int c = tid; c < p.Hq * p.D; c += kAppendThreads) q_out[c] = (T)0.f;
         return;
     }
-    int depth = i;
-    if (p.nodes.parents) {
-        for (int j = tid; j <= i; j += threads) tree[j] = p.nodes.parents[(int64_t)b * p.nodes.T + j];
-        __syncthreads();
-        depth = 0;
-        for (int j = checked_parent(tree[i], i, p.status); j >= 0; j = checked_parent(tree[j], j, p.status)) ++depth;
-    }
     // the page and the entry in it; nothing is kept where there is none
-    const int64_t slot = p.slots ? (int64_t)__ldg(p.slots + node) : (int64_t)len + i;
+    const int64_t slot = p.slots ? (int64_t)given : (int64_t)len + i;
     int64_t entry = -1;
     if (slot >= 0) {
-        const int64_t at = slot / p.page_size;
+        const int64_t at = slot >> 31 ? slot / p.page_size : (int64_t)((uint32_t)slot / (uint32_t)p.page_size);
         const int page = at < p.max_pages ? __ldg(p.page_table + (int64_t)b * p.max_pages + at) : -1;
         if (page >= 0 && page < p.num_pages)
             entry = (int64_t)page * p.Hkv * p.page_size + (slot - at * p.page_size);
         else if (tid == 0)
             raise_status(p.status, SPR_ERR_BAD_PAGE);
     }
+    int depth = i;
+    if (p.nodes.parents) {
+        for (int j = tid; j <= i; j += kAppendThreads) tree[j] = p.nodes.parents[(int64_t)b * p.nodes.T + j];
+        __syncthreads();
+        depth = 0;
+        for (int j = checked_parent(tree[i], i, p.status); j >= 0; j = checked_parent(tree[j], j, p.status)) ++depth;
+    }
     const double position = (double)len + depth;
-    for (int j = tid; j < p.pairs; j += threads) {
+    for (int j = tid; j < p.pairs; j += kAppendThreads) {
         double a = position * (double)__ldg(p.inv_freq + j);
         a = fma(-6.283185307179586477, rint(a * 0.15915494309189533577), a);
         sincosf((float)a, &turn[j].y, &turn[j].x);
     }
     __syncthreads();
-    const T *q = static_cast<const T *>(p.q) + node * p.q_stride;
-    const T *k = static_cast<const T *>(p.k) + node * p.k_stride;
-    const T *v = static_cast<const T *>(p.v) + node * p.v_stride;
-    T *k_cache = static_cast<T *>(p.k_cache), *v_cache = static_cast<T *>(p.v_cache);
-    constexpr int n = V::n;
-    const int heads = p.Hq + 2 * p.Hkv;
-    for (int h = threadIdx.y; h < heads; h += blockDim.y) {
-        const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
-        const int hk = is_q ? h : is_v ? h - p.Hq - p.Hkv : h - p.Hq;
-        if (is_q ? !p.q_out : entry < 0) continue;
-        const T *src = (is_q ? q : is_v ? v : k) + (int64_t)hk * p.D;
-        T *dst = is_q ? q_out + (int64_t)hk * p.D
-                      : (is_v ? v_cache : k_cache) + (entry + (int64_t)hk * p.page_size) * p.D;
-        const int pairs = is_v ? 0 : p.pairs;
-        if (p.interleaved && n > 1) {
-            for (int c = threadIdx.x * n; c < p.D; c += blockDim.x * n) {
-                V a;
-                a.load(src + c);
 #pragma unroll
-                for (int e = 0; e + 1 < n; e += 2)
-                    if ((c + e) / 2 < pairs) {
-                        const float2 t = turn[(c + e) / 2];
-                        const float x = a.x[e], y = a.x[e + 1];
-                        a.x[e] = x * t.x - y * t.y;
-                        a.x[e + 1] = y * t.x + x * t.y;
-                    }
-                a.store(dst + c);
-            }
-        } else {
-            // element c and its partner: `pairs` further on, or the next one
-            const int by = p.interleaved ? 1 : pairs, step = p.interleaved ? 2 : 1;
-            for (int c = threadIdx.x * n; c < pairs; c += blockDim.x * n) {
-                V a, o;
-                a.load(src + c * step);
-                o.load(src + c * step + by);
-#pragma unroll
-                for (int e = 0; e < n; ++e) {
-                    const float2 t = turn[c + e];
-                    const float x = a.x[e], y = o.x[e];
-                    a.x[e] = x * t.x - y * t.y;
-                    o.x[e] = y * t.x + x * t.y;
-                }
-                a.store(dst + c * step);
-                o.store(dst + c * step + by);
-            }
-            for (int c = 2 * pairs + threadIdx.x * n; c < p.D; c += blockDim.x * n) {
-                V a;
-                a.load(src + c);
-                a.store(dst + c);
-            }
-        }
+    for (int k = 0; k < kAhead; ++k)
+        if (tid + k * kAppendThreads < units) unit[k].store(p, node, entry, turn);
+    for (int u = tid + kAhead * kAppendThreads; u < units; u += kAppendThreads) {
+        unit[0].place(p, u);
+        unit[0].load(p, node);
+        unit[0].store(p, node, entry, turn);
     }
 }
 
 template <typename T>
-cudaError_t launch_append(const AppendParams &p, int64_t nodes, cudaStream_t st)
+cudaError_t launch_append(AppendParams &p, int64_t nodes, cudaStream_t st)
 {
     constexpr int n = 16 / sizeof(T);
     auto whole = [&](const void *t, int64_t stride) { return !t || (aligned(t, 16) && stride % n == 0); };
     const bool vec = whole(p.q, p.q_stride) && whole(p.k, p.k_stride) && whole(p.v, p.v_stride) && whole(p.q_out, 0) &&
                      whole(p.k_cache, 0) && whole(p.v_cache, 0) && p.D % n == 0 &&
                      (p.interleaved || p.pairs % n == 0);
-    const int per_head = vec ? p.D / n : p.D;
-    int x = 1;
-    while (x < per_head && x < 32) x *= 2;
-    if (!p.interleaved && p.pairs && x > 1) x /= 2;
-    const dim3 threads((unsigned)x, (unsigned)(kAppendThreads / x));
-    if (vec)
-        append_kernel<T, Vec<T>><<<(unsigned)nodes, threads, 0, st>>>(p);
+    const int w = vec ? n : 1;
+    const bool two = !p.interleaved || w == 1;         // (as Unit::kTwo)
+    p.rotated = two ? p.pairs / w + (p.D - 2 * p.pairs) / w : p.D / w;
+    p.copied = p.D / w;
+    p.rotated_inv = (uint32_t)((((uint64_t)1 << 32) + p.rotated - 1) / p.rotated);
+    p.copied_inv = (uint32_t)((((uint64_t)1 << 32) + p.copied - 1) / p.copied);
+    const unsigned ctas = (unsigned)nodes;
+    if (vec && p.interleaved)
+        append_kernel<T, Vec<T>, true><<<ctas, kAppendThreads, 0, st>>>(p);
+    else if (vec)
+        append_kernel<T, Vec<T>, false><<<ctas, kAppendThreads, 0, st>>>(p);
+    else if (p.interleaved)
+        append_kernel<T, One<T>, true><<<ctas, kAppendThreads, 0, st>>>(p);
     else
-        append_kernel<T, One<T>><<<(unsigned)nodes, threads, 0, st>>>(p);
+        append_kernel<T, One<T>, false><<<ctas, kAppendThreads, 0, st>>>(p);
     return cudaGetLastError();
 }
 
@@ -209,7 +253,7 @@ extern "C" int cache_append(const void *q, int64_t q_stride, const void *k, int6
 {
     if (!dtype_ok(dt)) return SPR_ERR_UNSUPPORTED;
     if (B < 0 || T < 0 || Hq < 0 || Hkv <= 0 || D <= 0 || D > 2 * kMaxRotPairs || rot < 0 || rot % 2 || rot > D || max_pages <= 0 ||
-        num_pages <= 0 || page_size <= 0 || (int64_t)B * T > 0x7fffffff || (int64_t)Hq + 2 * (int64_t)Hkv > 65536)
+        num_pages <= 0 || page_size <= 0 || (int64_t)B * T > 0x7fffffff || (int64_t)Hq + 2 * (int64_t)Hkv > 4096)
         return SPR_ERR_INVALID_ARG;
     if (parents && T > kMaxTreeNodes) return SPR_ERR_UNSUPPORTED;
     if (B == 0 || T == 0) return SPR_OK;
