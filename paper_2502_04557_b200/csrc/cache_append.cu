@@ -86,6 +86,23 @@ struct One {
 
 __device__ __forceinline__ int divide(int x, int by, uint32_t inv) { return by == 1 ? x : (int)__umulhi((uint32_t)x, inv); }
 
+// n cosines and sines from `turn` on
+template <int n>
+__device__ __forceinline__ void angles(const float *turn, float (&c)[n], float (&s)[n])
+{
+    if constexpr (n % 4 == 0) {
+#pragma unroll
+        for (int e = 0; e < n; e += 4) {
+            const float4 x = *reinterpret_cast<const float4 *>(turn + e), y = *reinterpret_cast<const float4 *>(turn + kMaxRotPairs + e);
+            c[e] = x.x, c[e + 1] = x.y, c[e + 2] = x.z, c[e + 3] = x.w;
+            s[e] = y.x, s[e + 1] = y.y, s[e + 2] = y.z, s[e + 3] = y.w;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < n; ++e) c[e] = turn[e], s[e] = turn[kMaxRotPairs + e];
+    }
+}
+
 // A unit is what a thread moves at once.  Pairs of halves: a vector V and its partner `pairs` elements on; behind them, in
 // the rest of a head, and in value heads: one vector.  Adjacent pairs: one vector (of one element: two).
 template <typename T, typename V, bool ADJACENT>
@@ -116,7 +133,7 @@ struct Unit {
         if (by) o.load(src + col + by);
     }
     // entry: where head 0's row of the node lies in the caches, in rows; negative: nowhere
-    __device__ __forceinline__ void store(const AppendParams &p, int64_t node, int64_t entry, const float2 *turn)
+    __device__ __forceinline__ void store(const AppendParams &p, int64_t node, int64_t entry, const float *turn)
     {
         const bool is_q = head < p.Hq, is_v = head >= p.Hq + p.Hkv;
         if (!is_q && entry < 0) return;
@@ -124,29 +141,29 @@ struct Unit {
                  : is_v ? static_cast<T *>(p.v_cache) + (entry + (int64_t)(head - p.Hq - p.Hkv) * p.page_size) * p.D
                         : static_cast<T *>(p.k_cache) + (entry + (int64_t)(head - p.Hq) * p.page_size) * p.D;
         if (by) {
-            float x[n], y[n];
+            float x[n], y[n], c[n], w[n];
             a.get(x);
             o.get(y);
+            angles<n>(turn + (ADJACENT ? col / 2 : col), c, w);
 #pragma unroll
             for (int e = 0; e < n; ++e) {
-                const float2 t = turn[ADJACENT ? col / 2 : col + e];
                 const float z = x[e];
-                x[e] = z * t.x - y[e] * t.y;
-                y[e] = y[e] * t.x + z * t.y;
+                x[e] = z * c[e] - y[e] * w[e];
+                y[e] = y[e] * c[e] + z * w[e];
             }
             a.set(x);
             o.set(y);
             o.store(dst + col + by);
         } else if (!kTwo && !is_v && col < 2 * p.pairs) {
-            float x[n];
+            float x[n], c[n > 1 ? n / 2 : 1], w[n > 1 ? n / 2 : 1];
             a.get(x);
+            angles<(n > 1 ? n / 2 : 1)>(turn + col / 2, c, w);
 #pragma unroll
             for (int e = 0; e + 1 < n; e += 2)
                 if ((col + e) / 2 < p.pairs) {
-                    const float2 t = turn[(col + e) / 2];
                     const float z = x[e], y = x[e + 1];
-                    x[e] = z * t.x - y * t.y;
-                    x[e + 1] = y * t.x + z * t.y;
+                    x[e] = z * c[e / 2] - y * w[e / 2];
+                    x[e + 1] = y * c[e / 2] + z * w[e / 2];
                 }
             a.set(x);
         }
@@ -155,10 +172,10 @@ struct Unit {
 };
 
 template <typename T, typename V, bool ADJACENT>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendParams p)
+__global__ void __launch_bounds__(kAppendThreads, 6) append_kernel(const AppendParams p)
 {
     constexpr int kAhead = ADJACENT ? 3 : 2;
-    __shared__ float2 turn[kMaxRotPairs];
+    __shared__ __align__(16) float turn[2 * kMaxRotPairs];       // cosines, then sines
     __shared__ int tree[kMaxTreeNodes];
     const int64_t node = blockIdx.x;
     const int tid = threadIdx.x, units = (p.Hq + p.Hkv) * p.rotated + p.Hkv * p.copied;
@@ -200,12 +217,15 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
     for (int j = tid; j < p.pairs; j += kAppendThreads) {
         double a = position * (double)__ldg(p.inv_freq + j);
         a = fma(-6.283185307179586477, rint(a * 0.15915494309189533577), a);
-        sincosf((float)a, &turn[j].y, &turn[j].x);
+        sincosf((float)a, &turn[kMaxRotPairs + j], &turn[j]);
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
-        if (tid + k * kAppendThreads < units) unit[k].store(p, node, entry, turn);
+        if (tid + k * kAppendThreads < units) {
+            unit[k].place(p, tid + k * kAppendThreads);         // (again: cheaper than registers to keep it)
+            unit[k].store(p, node, entry, turn);
+        }
     for (int u = tid + kAhead * kAppendThreads; u < units; u += kAppendThreads) {
         unit[0].place(p, u);
         unit[0].load(p, node);
