@@ -31,6 +31,7 @@ struct AppendParams {
     int Hq, Hkv, D, pairs;                   // pairs = rotated elements / 2
     int interleaved;
     int max_pages, num_pages, page_size;
+    int wide;                                // heads are made of pairs of vectors
     int rotated, copied;                     // units of a rotated head, of a value head (see append_kernel)
     uint32_t rotated_inv, copied_inv;        // 2^32 / these, rounded up
 };
@@ -43,7 +44,7 @@ struct Vec<float> {
     static constexpr int n = 4;
     float4 raw;
     __device__ __forceinline__ void load(const float *p) { raw = __ldcs(reinterpret_cast<const float4 *>(p)); }
-    __device__ __forceinline__ void store(float *p) const { *reinterpret_cast<float4 *>(p) = raw; }
+    __device__ __forceinline__ void store(float *p) const { __stcs(reinterpret_cast<float4 *>(p), raw); }
     __device__ __forceinline__ void get(float (&x)[4]) const { x[0] = raw.x, x[1] = raw.y, x[2] = raw.z, x[3] = raw.w; }
     __device__ __forceinline__ void set(const float (&x)[4]) { raw = make_float4(x[0], x[1], x[2], x[3]); }
 };
@@ -52,7 +53,7 @@ struct Vec<__nv_bfloat16> {
     static constexpr int n = 8;
     uint4 raw;
     __device__ __forceinline__ void load(const __nv_bfloat16 *p) { raw = __ldcs(reinterpret_cast<const uint4 *>(p)); }
-    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = raw; }
+    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { __stcs(reinterpret_cast<uint4 *>(p), raw); }
     __device__ __forceinline__ void get(float (&x)[8]) const
     {
         const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
@@ -103,14 +104,14 @@ __device__ __forceinline__ void angles(const float *turn, float (&c)[n], float (
     }
 }
 
-// A unit is what a thread moves at once.  Pairs of halves: a vector V and its partner `pairs` elements on; behind them, in
-// the rest of a head, and in value heads: one vector.  Adjacent pairs: one vector (of one element: two).
+// A unit is what a thread moves at once: two vectors V where there are two.  Pairs of halves: a vector and its partner `pairs`
+// elements on; behind them, in the rest of a head, one vector.  Adjacent pairs, and value heads: neighbours.
 template <typename T, typename V, bool ADJACENT>
 struct Unit {
     static constexpr int n = V::n;
-    static constexpr bool kTwo = !ADJACENT || n == 1;      // a rotated unit is two vectors
+    static constexpr bool kPartners = !ADJACENT || n == 1;     // the two vectors of a rotated unit turn with each other
     V a, o;
-    int head, col, by;                                     // by: distance of the partner, 0 where there is none
+    int head, col, by;                                         // by: distance of the second vector, 0 where there is none
     __device__ __forceinline__ void place(const AppendParams &p, int u)
     {
         const int turned = (p.Hq + p.Hkv) * p.rotated;
@@ -119,9 +120,14 @@ struct Unit {
         const int h = is_v ? divide(u, p.copied, p.copied_inv) : divide(u, p.rotated, p.rotated_inv);
         const int j = u - h * (is_v ? p.copied : p.rotated);
         head = is_v ? h + p.Hq + p.Hkv : h;
-        const int two = is_v || !kTwo ? 0 : p.pairs / n;   // units of two vectors
-        by = j < two ? (ADJACENT ? 1 : p.pairs) : 0;
-        col = j < two ? (ADJACENT ? 2 * j : j * n) : (is_v || !kTwo ? j * n : 2 * p.pairs + (j - two) * n);
+        if (is_v || !kPartners) {
+            by = p.wide ? n : 0;
+            col = j * (n + by);
+        } else {
+            const int two = p.pairs / n;
+            by = j < two ? (ADJACENT ? 1 : p.pairs) : 0;
+            col = j < two ? (ADJACENT ? 2 * j : j * n) : 2 * p.pairs + (j - two) * n;
+        }
     }
     __device__ __forceinline__ void load(const AppendParams &p, int64_t node)
     {
@@ -132,6 +138,22 @@ struct Unit {
         a.load(src + col);
         if (by) o.load(src + col + by);
     }
+    // pairs within a vector that begins at column col
+    __device__ __forceinline__ void turn_within(V &v, int col, const AppendParams &p, const float *turn)
+    {
+        if (col >= 2 * p.pairs) return;
+        float x[n], c[n > 1 ? n / 2 : 1], w[n > 1 ? n / 2 : 1];
+        v.get(x);
+        angles<(n > 1 ? n / 2 : 1)>(turn + col / 2, c, w);
+#pragma unroll
+        for (int e = 0; e + 1 < n; e += 2)
+            if ((col + e) / 2 < p.pairs) {
+                const float z = x[e], y = x[e + 1];
+                x[e] = z * c[e / 2] - y * w[e / 2];
+                x[e + 1] = y * c[e / 2] + z * w[e / 2];
+            }
+        v.set(x);
+    }
     // entry: where head 0's row of the node lies in the caches, in rows; negative: nowhere
     __device__ __forceinline__ void store(const AppendParams &p, int64_t node, int64_t entry, const float *turn)
     {
@@ -140,7 +162,7 @@ struct Unit {
         T *dst = is_q   ? static_cast<T *>(p.q_out) + (node * p.Hq + head) * p.D
                  : is_v ? static_cast<T *>(p.v_cache) + (entry + (int64_t)(head - p.Hq - p.Hkv) * p.page_size) * p.D
                         : static_cast<T *>(p.k_cache) + (entry + (int64_t)(head - p.Hq) * p.page_size) * p.D;
-        if (by) {
+        if (!is_v && kPartners && by) {
             float x[n], y[n], c[n], w[n];
             a.get(x);
             o.get(y);
@@ -153,28 +175,20 @@ struct Unit {
             }
             a.set(x);
             o.set(y);
-            o.store(dst + col + by);
-        } else if (!kTwo && !is_v && col < 2 * p.pairs) {
-            float x[n], c[n > 1 ? n / 2 : 1], w[n > 1 ? n / 2 : 1];
-            a.get(x);
-            angles<(n > 1 ? n / 2 : 1)>(turn + col / 2, c, w);
-#pragma unroll
-            for (int e = 0; e + 1 < n; e += 2)
-                if ((col + e) / 2 < p.pairs) {
-                    const float z = x[e], y = x[e + 1];
-                    x[e] = z * c[e / 2] - y * w[e / 2];
-                    x[e + 1] = y * c[e / 2] + z * w[e / 2];
-                }
-            a.set(x);
         }
+        if (!is_v && !kPartners) {
+            turn_within(a, col, p, turn);
+            if (by) turn_within(o, col + by, p, turn);
+        }
+        if (by) o.store(dst + col + by);
         a.store(dst + col);
     }
 };
 
 template <typename T, typename V, bool ADJACENT>
-__global__ void __launch_bounds__(kAppendThreads, 6) append_kernel(const AppendParams p)
+__global__ void __launch_bounds__(kAppendThreads, 5) append_kernel(const AppendParams p)
 {
-    constexpr int kAhead = ADJACENT ? 3 : 2;
+    constexpr int kAhead = 2;
     __shared__ __align__(16) float turn[2 * kMaxRotPairs];       // cosines, then sines
     __shared__ int tree[kMaxTreeNodes];
     const int64_t node = blockIdx.x;
@@ -242,9 +256,9 @@ cudaError_t launch_append(AppendParams &p, int64_t nodes, cudaStream_t st)
                      whole(p.k_cache, 0) && whole(p.v_cache, 0) && p.D % n == 0 &&
                      (p.interleaved || p.pairs % n == 0);
     const int w = vec ? n : 1;
-    const bool two = !p.interleaved || w == 1;         // (as Unit::kTwo)
-    p.rotated = two ? p.pairs / w + (p.D - 2 * p.pairs) / w : p.D / w;
-    p.copied = p.D / w;
+    p.wide = p.D % (2 * w) == 0;
+    p.copied = p.D / w / (p.wide ? 2 : 1);
+    p.rotated = !p.interleaved || w == 1 ? p.pairs / w + (p.D - 2 * p.pairs) / w : p.copied;      // (as Unit::kPartners)
     p.rotated_inv = (uint32_t)((((uint64_t)1 << 32) + p.rotated - 1) / p.rotated);
     p.copied_inv = (uint32_t)((((uint64_t)1 << 32) + p.copied - 1) / p.copied);
     const unsigned ctas = (unsigned)nodes;
