@@ -20,6 +20,7 @@ struct AttnParams {
     DraftNodes nodes;
     int B, Hq, Hkv, G, D;                // G = Hq / Hkv query heads share a cached head
     int max_pages, num_pages, page_size;
+    int64_t capacity;                    // slots of a sequence that the page table can name
     float scale_log2;                    // scale * log2(e): scores are exponents of two
     float abs_scale_log2;                // its magnitude (not zero: masked scores, -inf, stay what they are under it) ...
     uint32_t flip;                       // ... and sign, as the sign bits of two bf16 numbers: queries take it over

@@ -40,7 +40,7 @@ template <int ROWS, int E>
 __global__ void __launch_bounds__(kF32Threads, 2) attention_f32_kernel(const AttnParams p)
 {
     constexpr int kLanes = 32 / ROWS;               // lanes that share a row's score
-    __shared__ int64_t scratch[2 * kF32Warps + 4];
+    __shared__ int scratch[kF32Warps + 2];
     __shared__ int tree[kMaxTreeNodes];
     __shared__ uint32_t path[ROWS][kMaxTreeNodes / 32];
     __shared__ float2 ml[kF32Warps][ROWS];
@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(kF32Threads, 2) attention_f32_kernel(const Att
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int my_row = lane / kLanes, col = lane * E;
     const bool in = col < p.D;
-    AttnStretch s = attn_plan<ROWS, kF32Threads>(p, scratch);
+    AttnStretch s = attn_plan<ROWS, kF32Threads, 1>(p, scratch);
     attn_clear_unused<float>(p, kF32Threads);
     const float *k_cache = static_cast<const float *>(p.k), *v_cache = static_cast<const float *>(p.v);
     AttnPart part;
@@ -78,14 +78,14 @@ __global__ void __launch_bounds__(kF32Threads, 2) attention_f32_kernel(const Att
             for (int e = 0; e < E; ++e) q[r][e] = c.x[e] * p.scale_log2, o[r][e] = 0.f;
         }
         const uint32_t *bits = path[min((int)((t.row0 + my_row) / p.G) - i0, nodes - 1)];
-        const int64_t keys = min((int64_t)s.seq.len + s.seq.count, (int64_t)p.max_pages * p.page_size);
+        const int keys = attn_keys(p, s.seq.len, s.seq.count);
         if (keys < (int64_t)s.seq.len + s.seq.count && tid == 0) raise_status(p.status, SPR_ERR_BAD_PAGE);
 
         // rows of a tile's keys in the caches, key j of the warp's in lane j; -1 where there is none
         auto find = [&](int tile) -> int64_t {
-            const int64_t slot = (int64_t)tile * kAttnTile + warp * kKeys + lane;
+            const int slot = tile * kAttnTile + warp * kKeys + lane;
             if (lane >= kKeys || slot >= keys) return -1;
-            const int64_t at = slot / p.page_size;
+            const int at = slot / p.page_size;
             const int page = __ldg(p.page_table + (int64_t)s.seq.b * p.max_pages + at);
             if (page < 0 || page >= p.num_pages) {
                 raise_status(p.status, SPR_ERR_BAD_PAGE);
@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(kF32Threads, 2) attention_f32_kernel(const Att
         auto use = [&](int64_t rows, int tile, int group, const Cols<E> (&k)[kGroup], const Cols<E> (&v)[kGroup]) {
             float sc[kGroup];
             uint32_t seen[kGroup];
-            const int64_t slot0 = (int64_t)tile * kAttnTile + warp * kKeys + group * kGroup;
+            const int slot0 = tile * kAttnTile + warp * kKeys + group * kGroup;
 #pragma unroll
             for (int j = 0; j < kGroup; ++j) {
                 float x[ROWS];
@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(kF32Threads, 2) attention_f32_kernel(const Att
                 for (int o2 = kLanes / 2; o2 > 0; o2 /= 2) x[0] += __shfl_xor_sync(0xffffffffu, x[0], o2);
                 sc[j] = x[0];
                 const bool there = __shfl_sync(0xffffffffu, rows, group * kGroup + j) >= 0;
-                const int64_t node = slot0 + j - s.seq.len;
+                const int node = slot0 + j - s.seq.len;
                 const bool vis = there && (node < 0 || (bits[node >> 5] >> (node & 31) & 1));
                 if (!vis) sc[j] = neg_inf();
                 seen[j] = __ballot_sync(0xffffffffu, vis);
@@ -224,14 +224,10 @@ __global__ void __launch_bounds__(kF32Threads, 2) attention_f32_kernel(const Att
             }
         }
         if (!t.whole) {
-            __threadfence();
             __syncthreads();
-            if (tid == 0) last = take_ticket(p.counters + t.first, t.parts);
+            if (tid == 0) last = attn_ticket(p, t);
             __syncthreads();
-            if (last) {
-                __threadfence();
-                attn_join<ROWS, float>(p, s, part, t, warp, kF32Warps);
-            }
+            if (last) attn_join<ROWS, float>(p, s, part, t, warp, kF32Warps);
         }
     }
 }

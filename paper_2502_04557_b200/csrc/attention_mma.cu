@@ -41,7 +41,7 @@ struct MmaShape {
 };
 
 struct MmaControl {
-    int64_t scratch[2 * kMmaWarps + 4];
+    int scratch[kMmaWarps + 2];
     int tree[kMaxTreeNodes];
     uint32_t path[32][kMaxTreeNodes / 32];
     float2 ml[kMmaWarps][32];
@@ -64,8 +64,11 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// 16 bytes, or zeros
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there)
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there)      // or zeros
 {
     asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
@@ -77,11 +80,11 @@ __device__ __forceinline__ void copies_wait()
 }
 __device__ __forceinline__ bool finite_bf16x2(uint32_t w) { return (w & 0x7f80u) != 0x7f80u && (w & 0x7f800000u) != 0x7f800000u; }
 
-// MT: row tiles of 16; PANELS: 64-column halves of the head dimension
-template <int MT, int PANELS>
+// PANELS: 64-column halves of the head dimension; WHOLE: which it is made of
+template <int PANELS, bool WHOLE>
 __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const AttnParams p)
 {
-    constexpr int ROWS = 16 * MT, KSTEPS = 4 * PANELS, NTILES = 8 * PANELS;
+    constexpr int MT = 1, ROWS = 16 * MT, KSTEPS = 4 * PANELS, NTILES = 8 * PANELS;
     using Shape = MmaShape<PANELS>;
     extern __shared__ __align__(1024) uint8_t raw[];
     __shared__ MmaControl ctl;
@@ -90,9 +93,8 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
     const uint32_t ring = smem_addr(raw) + warp * Shape::stages * Shape::step;
     float *join = reinterpret_cast<float *>(raw + (size_t)kMmaWarps * Shape::stages * Shape::step);
     const int w16 = warp * 16;                              // keys w16 .. + 15 of a tile
-    const int64_t capacity = (int64_t)p.max_pages * p.page_size;
 
-    AttnStretch s = attn_plan<ROWS, kMmaThreads>(p, ctl.scratch);
+    AttnStretch s = attn_plan<ROWS, kMmaThreads, 4>(p, ctl.scratch);
     attn_clear_unused<__nv_bfloat16>(p, kMmaThreads);
 
     // ---------------------------------------------------------------- copies, some steps ahead of the products
@@ -100,20 +102,20 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
     AttnPart next_part = {0, 0, 0, 0};
     bool more = true;
     int next_tile = 0, end_tile = 0, left_rows = 0;     // the next tile; left_rows: steps whose rows are in `rows`
-    int64_t next_keys = 0;
+    int next_keys = 0;
     int next_stage = 0;
     int rows = -1, rows_behind = -1;                    // lane 2 j + r: row of the caches where run r (8 keys) of step j begins
     auto find = [&](int tile) {                         // for 16 steps from this tile on
         const int t = tile + (lane >> 1);
-        const int64_t slot = (int64_t)t * kAttnTile + w16 + 8 * (lane & 1);
+        const int slot = t * kAttnTile + w16 + 8 * (lane & 1);
         if (t >= end_tile || slot >= next_keys) return -1;
-        const uint32_t at = (uint32_t)((uint64_t)slot >> 3) / (uint32_t)(p.page_size >> 3);       // pages are whole runs
+        const int at = slot / p.page_size;
         const int page = __ldg(p.page_table + (int64_t)ahead.seq.b * p.max_pages + at);
         if (page < 0 || page >= p.num_pages) {
             raise_status(p.status, SPR_ERR_BAD_PAGE);
             return -1;
         }
-        return (page * p.Hkv + next_part.head) * p.page_size + (int)(slot - (int64_t)at * p.page_size);
+        return (page * p.Hkv + next_part.head) * p.page_size + (slot - at * p.page_size);
     };
     // lane's 16 bytes of a row
     constexpr int kChunks = 8 * PANELS, kRowsAtOnce = 32 / kChunks;
@@ -124,11 +126,8 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
         while (more && next_tile >= end_tile) {         // on to the next part
             more = attn_next<ROWS>(p, ahead, next_part);
             if (!more) break;
-            next_keys = (int64_t)ahead.seq.len + ahead.seq.count;
-            if (next_keys > capacity) {
-                raise_status(p.status, SPR_ERR_BAD_PAGE);
-                next_keys = capacity;
-            }
+            next_keys = attn_keys(p, ahead.seq.len, ahead.seq.count);
+            if (next_keys < (int64_t)ahead.seq.len + ahead.seq.count) raise_status(p.status, SPR_ERR_BAD_PAGE);
             next_tile = next_part.t0;
             end_tile = next_part.t0 + next_part.n;
             left_rows = 0;
@@ -143,17 +142,31 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
             const int from = 2 * (16 - left_rows);
             const uint32_t dst = ring + next_stage * Shape::step + c_dst;
             const int run[2] = {__shfl_sync(0xffffffffu, rows, from), __shfl_sync(0xffffffffu, rows, from + 1)};
-            const int64_t keys = next_keys - (int64_t)next_tile * kAttnTile - w16;      // of this step that there are
+            const int keys = next_keys - next_tile * kAttnTile - w16;      // of this step that there are
             const uint32_t valid = ((run[0] >= 0 ? 0xffu : 0u) | (run[1] >= 0 ? 0xff00u : 0u)) & (keys >= 16 ? 0xffffu : keys <= 0 ? 0u : (1u << keys) - 1);
             if (lane == 0) ctl.valid[warp][next_stage] = valid;
+            if (WHOLE && valid == 0xffffu) {
 #pragma unroll
-            for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
-                const int r0 = i * kRowsAtOnce, r = r0 + c_row;
-                const bool there = c_in && (valid >> r & 1);
-                const int64_t at = there ? ((int64_t)run[r0 >> 3] + (r & 7)) * p.D + c_chunk * 8 : 0;
-                const uint32_t to = (dst + r0 * Shape::row) ^ ((r0 & 7) << 4);
-                copy16(to, static_cast<const __nv_bfloat16 *>(p.k) + at, there);
-                copy16(to + 16 * Shape::row, static_cast<const __nv_bfloat16 *>(p.v) + at, there);
+                for (int r = 0; r < 2; ++r) {
+                    const int64_t at = ((int64_t)run[r] + c_row) * (64 * PANELS) + c_chunk * 8;
+                    const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(p.k) + at, *v = static_cast<const __nv_bfloat16 *>(p.v) + at;
+#pragma unroll
+                    for (int r0 = 0; r0 < 8; r0 += kRowsAtOnce) {
+                        const uint32_t to = (dst ^ (r0 << 4)) + (8 * r + r0) * Shape::row;
+                        copy16(to, k + r0 * 64 * PANELS);
+                        copy16(to + 16 * Shape::row, v + r0 * 64 * PANELS);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
+                    const int r0 = i * kRowsAtOnce, r = r0 + c_row;
+                    const bool there = c_in && (valid >> r & 1);
+                    const int64_t at = there ? ((int64_t)run[r0 >> 3] + (r & 7)) * p.D + c_chunk * 8 : 0;
+                    const uint32_t to = (dst ^ ((r0 & 7) << 4)) + r0 * Shape::row;
+                    copy16(to, static_cast<const __nv_bfloat16 *>(p.k) + at, there);
+                    copy16(to + 16 * Shape::row, static_cast<const __nv_bfloat16 *>(p.v) + at, there);
+                }
             }
             ++next_tile;
             --left_rows;
@@ -161,9 +174,6 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
         copies_commit();
         next_stage = next_stage + 1 == Shape::stages ? 0 : next_stage + 1;
     };
-#pragma unroll 1
-    for (int i = 0; i < Shape::stages; ++i) issue();
-
     // ---------------------------------------------------------------- products
     // ldmatrix addresses: keys (non-transposed): matrices (keys 0-7 | 8-15) x (columns 0-7 | 8-15); values transposed
     const int k_row = (lane & 7) + ((lane >> 4) << 3), k_chunk = (lane >> 3) & 1;
@@ -171,14 +181,39 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
     const uint32_t k_off = k_row * Shape::row, v_off = (16 + v_row) * Shape::row;
     const int swz = lane & 7;                               // both rows are lane & 7 modulo 8
     const int quad = lane >> 2, pair = lane & 3;
+    // a part's queries as A fragments: rows quad and quad + 8 of each row tile.  They are asked for while what comes before
+    // the part is still going on.
+    uint32_t qf[MT][KSTEPS][4];
+    auto load_queries = [&](const AttnStretch &s, const AttnPart &part) {
+        const int row0 = part.block * ROWS, rows = s.seq.count * p.G - row0;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = mt * 16 + h * 8 + quad;
+                const bool in = r < rows;
+                const uint32_t *src = reinterpret_cast<const uint32_t *>(static_cast<const __nv_bfloat16 *>(p.q) + (in ? attn_out_at(p, s, part, row0 + r) : 0));
+#pragma unroll
+                for (int k = 0; k < KSTEPS; ++k)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const int col = k * 16 + c * 8 + pair * 2;
+                        qf[mt][k][c * 2 + h] = in && col < p.D ? __ldg(src + col / 2) : 0u;
+                    }
+            }
+    };
     AttnPart part;
     int tree_of = -1, stage = 0;
-    while (attn_next<ROWS>(p, s, part)) {
+    bool have = attn_next<ROWS>(p, s, part);
+    if (have) load_queries(s, part);
+#pragma unroll 1
+    for (int i = 0; i < Shape::stages; ++i) issue();
+    while (have) {
         const AttnTarget t = attn_target<ROWS>(p, s, part);
-        const int i0 = (int)(t.row0 / p.G);
-        const int nodes = (int)((t.row0 + t.rows - 1) / p.G) - i0 + 1;
+        const int i0 = t.row0 / p.G;
+        const int nodes = (t.row0 + t.rows - 1) / p.G - i0 + 1;
         __syncthreads();
-        const bool holds_nodes = (int64_t)(part.t0 + part.n) * kAttnTile > s.seq.len;
+        const bool holds_nodes = (part.t0 + part.n) * kAttnTile > s.seq.len;
         if (holds_nodes && p.nodes.parents && tree_of != s.seq.b) {
             for (int j = tid; j < s.seq.count; j += kMmaThreads) ctl.tree[j] = p.nodes.parents[(int64_t)s.seq.b * p.nodes.T + j];
             tree_of = s.seq.b;
@@ -187,25 +222,22 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
         if (holds_nodes && tid < nodes)
             attn_path_bits(p.nodes.parents ? ctl.tree : nullptr, i0 + tid, ctl.path[tid], (s.seq.count + 31) / 32, p.status);
 
-        // queries as A fragments: rows quad and quad + 8 of each row tile
-        uint32_t qf[MT][KSTEPS][4];
         int node[MT][2];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int r = mt * 16 + h * 8 + quad;
-                const bool in = r < t.rows;
-                node[mt][h] = in ? (int)((t.row0 + r) / p.G) - i0 : 0;
-                const uint32_t *src = reinterpret_cast<const uint32_t *>(static_cast<const __nv_bfloat16 *>(p.q) + (in ? attn_out_at(p, s, part, t.row0 + r) : 0));
+                node[mt][h] = r < t.rows ? (t.row0 + r) / p.G - i0 : 0;
+            }
+        if (p.flip) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                 for (int k = 0; k < KSTEPS; ++k)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const int col = k * 16 + c * 8 + pair * 2;
-                        qf[mt][k][c * 2 + h] = in && col < p.D ? __ldg(src + col / 2) ^ p.flip : 0u;
-                    }
-            }
+                    for (int c = 0; c < 4; ++c) qf[mt][k][c] ^= p.flip;
+        }
         __syncthreads();
 
         float o[MT][NTILES][4], m[MT][2], l[MT][2];
@@ -221,7 +253,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
             __syncwarp();
             const uint32_t base = ring + stage * Shape::step;
             const uint32_t valid = ctl.valid[warp][stage];
-            const int64_t slot0 = ((int64_t)part.t0 + n) * kAttnTile + w16;
+            const int slot0 = (part.t0 + n) * kAttnTile + w16;
             const bool all = valid == 0xffffu && slot0 + 16 <= s.seq.len;
 
             float sc[MT][2][4];
@@ -262,7 +294,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
                             const int key = h * 8 + pair * 2 + (c & 1);
-                            const int64_t j = slot0 + key - s.seq.len;
+                            const int j = slot0 + key - s.seq.len;
                             const bool vis = (valid >> key & 1) && (j < 0 || (ctl.path[node[mt][c >> 1]][j >> 5] >> (j & 31) & 1));
                             if (!vis) sc[mt][h][c] = neg_inf();
                         }
@@ -311,7 +343,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
                             const int h = key >> 3, c = key & 1, from = (lane & 28) | ((key & 7) >> 1);
                             const float w0 = h ? sc[mt][1][2 * g] : sc[mt][0][2 * g], w1 = h ? sc[mt][1][2 * g + 1] : sc[mt][0][2 * g + 1];
                             const float w = __shfl_sync(0xffffffffu, c ? w1 : w0, from);
-                            const int64_t j = slot0 + key - s.seq.len;
+                            const int j = slot0 + key - s.seq.len;
                             if (j < 0 || (ctl.path[node[mt][g]][j >> 5] >> (j & 31) & 1)) {
 #pragma unroll
                                 for (int i = 0; i < NTILES; ++i) {
@@ -359,6 +391,11 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
             issue();
             stage = stage + 1 == Shape::stages ? 0 : stage + 1;
         }
+
+        AttnStretch s_next = s;
+        AttnPart next;
+        have = attn_next<ROWS>(p, s_next, next);
+        if (have) load_queries(s_next, next);
 
         // ------------------------------------------------------------ the warps' results joined
 #pragma unroll
@@ -425,30 +462,28 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
             }
         }
         if (!t.whole) {
-            __threadfence();
             __syncthreads();
-            if (tid == 0) ctl.last = take_ticket(p.counters + t.first, t.parts);
+            if (tid == 0) ctl.last = attn_ticket(p, t);
             __syncthreads();
-            if (ctl.last) {
-                __threadfence();
-                attn_join<ROWS, __nv_bfloat16>(p, s, part, t, warp, kMmaWarps);
-            }
+            if (ctl.last) attn_join<ROWS, __nv_bfloat16>(p, s, part, t, warp, kMmaWarps);
         }
+        s = s_next;
+        part = next;
     }
     copies_wait<0>();
 }
 
-template <int MT, int PANELS>
+template <int PANELS, bool WHOLE>
 cudaError_t launch_mma(const AttnParams &p, int dev, cudaStream_t st)
 {
     static std::atomic<bool> attr_set[64];   // host threads may race to set it: all of them store `true`
     if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-        const cudaError_t e = cudaFuncSetAttribute(attention_mma_kernel<MT, PANELS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        const cudaError_t e = cudaFuncSetAttribute(attention_mma_kernel<PANELS, WHOLE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                    (int)MmaShape<PANELS>::smem);
         if (e != cudaSuccess) return e;
         if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
     }
-    attention_mma_kernel<MT, PANELS><<<p.ctas, kMmaThreads, MmaShape<PANELS>::smem, st>>>(p);
+    attention_mma_kernel<PANELS, WHOLE><<<p.ctas, kMmaThreads, MmaShape<PANELS>::smem, st>>>(p);
     return cudaGetLastError();
 }
 
@@ -456,7 +491,9 @@ cudaError_t launch_mma(const AttnParams &p, int dev, cudaStream_t st)
 
 cudaError_t launch_attention_mma(const AttnParams &p, int dev, cudaStream_t st)
 {
-    return p.D <= 64 ? launch_mma<1, 1>(p, dev, st) : launch_mma<1, 2>(p, dev, st);
+    if (p.D == 128) return launch_mma<2, true>(p, dev, st);
+    if (p.D == 64) return launch_mma<1, true>(p, dev, st);
+    return p.D < 64 ? launch_mma<1, false>(p, dev, st) : launch_mma<2, false>(p, dev, st);
 }
 
 }  // namespace spr

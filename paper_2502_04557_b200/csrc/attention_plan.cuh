@@ -14,8 +14,11 @@ namespace spr {
 
 struct AttnSeq {
     int b, len, count, tiles, blocks;    // blocks = row blocks
-    __device__ __forceinline__ int64_t total(int Hkv) const { return (int64_t)tiles * blocks * Hkv; }
+    __device__ __forceinline__ int total(int Hkv) const { return tiles * blocks * Hkv; }
 };
+
+// keys of a sequence: its prefix and its nodes, as far as the page table goes
+__device__ __forceinline__ int attn_keys(const AttnParams &p, int len, int count) { return (int)min((int64_t)len + count, p.capacity); }
 
 template <int ROWS>
 __device__ __forceinline__ AttnSeq attn_seq(const AttnParams &p, int b)
@@ -24,21 +27,24 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnParams &p, int b)
     s.b = b;
     s.len = __ldg(p.nodes.lens + b);
     s.count = s.len < 0 ? 0 : node_count(p.nodes, b);
-    const int64_t keys = min((int64_t)s.len + s.count, (int64_t)p.max_pages * p.page_size);
-    s.tiles = s.count ? (int)((keys + kAttnTile - 1) / kAttnTile) : 0;
+    s.tiles = s.count ? (int)((uint32_t)(attn_keys(p, s.len, s.count) + kAttnTile - 1) / kAttnTile) : 0;
     s.blocks = (s.count * p.G + ROWS - 1) / ROWS;
     return s;
 }
 
-// Where this CTA's stretch lies.
+// Where this CTA's stretch lies, in tiles of the line (fewer than 2^31: the host sees to it).  The first `longer` CTAs have
+// one tile more than the others.
 struct AttnStretch {
-    int64_t pos, end;        // in tiles of the line
-    int64_t total;
-    int active;              // CTAs that have a stretch
+    int pos, end;
+    int each, longer;
     AttnSeq seq;             // the sequence that pos lies in
-    int64_t at;              // pos within it
+    int at;                  // pos within it
 
-    __device__ __forceinline__ int owner(int64_t x) const { return (int)(((x + 1) * active - 1) / total); }
+    __device__ __forceinline__ int owner(int x) const
+    {
+        const int lower = longer * (each + 1);
+        return x < lower ? x / (each + 1) : longer + (x - lower) / each;
+    }
 };
 
 // Part of an item: tiles [t0, t0 + n) of it.
@@ -50,79 +56,82 @@ template <int ROWS>
 __device__ __forceinline__ bool attn_next(const AttnParams &p, AttnStretch &s, AttnPart &part)
 {
     if (s.pos >= s.end) return false;
-    while (s.at >= s.seq.total(p.Hkv)) {
-        s.at -= s.seq.total(p.Hkv);
+    for (int n; s.at >= (n = s.seq.total(p.Hkv));) {
+        s.at -= n;
         s.seq = attn_seq<ROWS>(p, s.seq.b + 1);
     }
-    const int item = s.at >> 31 ? (int)(s.at / s.seq.tiles) : (int)((uint32_t)s.at / (uint32_t)s.seq.tiles);
-    part.t0 = (int)(s.at - (int64_t)item * s.seq.tiles);
-    part.head = item / s.seq.blocks;
+    const int item = s.at / s.seq.tiles;
+    part.t0 = s.at - item * s.seq.tiles;
+    part.head = s.seq.blocks == 1 ? item : item / s.seq.blocks;
     part.block = item - part.head * s.seq.blocks;
-    part.n = (int)min((int64_t)(s.seq.tiles - part.t0), s.end - s.pos);
+    part.n = min(s.seq.tiles - part.t0, s.end - s.pos);
     s.pos += part.n;
     s.at += part.n;
     return true;
 }
 
-// Called by all THREADS threads of the CTA.  `scratch`: 2 * THREADS / 32 + 4 words of 8 bytes.
-template <int ROWS, int THREADS>
-__device__ __forceinline__ AttnStretch attn_plan(const AttnParams &p, int64_t *scratch)
+// Called by all THREADS threads of the CTA.  `scratch`: THREADS / 32 + 2 words.  LEAST: the fewest tiles that
+// are worth a CTA of their own: an item's parts have to be joined, which takes as long as some tiles.
+template <int ROWS, int THREADS, int LEAST>
+__device__ __forceinline__ AttnStretch attn_plan(const AttnParams &p, int *scratch)
 {
     constexpr int W = THREADS / 32;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    // (a part costs some two tiles' time to join: no CTA is given less)
-    constexpr int kLeast = 2;
-    const int64_t own = tid < p.B ? attn_seq<ROWS>(p, tid).total(p.Hkv) : 0;
-    int64_t mine = own;
-    for (int b = tid + THREADS; b < p.B; b += THREADS) mine += attn_seq<ROWS>(p, b).total(p.Hkv);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-    if (lane == 0) scratch[warp] = mine;
-    __syncthreads();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = blockIdx.x;
     AttnStretch s;
-    s.total = 0;
+    const int own = tid < p.B ? attn_seq<ROWS>(p, tid).total(p.Hkv) : 0;
+    int before = 0, total = 0;       // tiles of the sequences below b0, and of all
+    if (p.B > THREADS) {             // the line's length first
+        int mine = own;
+        for (int b = tid + THREADS; b < p.B; b += THREADS) mine += attn_seq<ROWS>(p, b).total(p.Hkv);
+        mine = __reduce_add_sync(0xffffffffu, mine);
+        if (lane == 0) scratch[warp] = mine;
+        __syncthreads();
 #pragma unroll
-    for (int w = 0; w < W; ++w) s.total += scratch[w];
-    s.active = (int)min((int64_t)p.ctas, (s.total + kLeast - 1) / kLeast);
-    const int c = blockIdx.x;
-    if (c >= s.active) {
-        s.pos = s.end = 0;
-        s.at = 0;
-        s.seq = AttnSeq{0, 0, 0, 0, 0};
-        return s;
+        for (int w = 0; w < W; ++w) total += scratch[w];
+        __syncthreads();
     }
-    s.pos = c * s.total / s.active;
-    s.end = (c + 1) * s.total / s.active;
-    // the sequence that holds tile `pos`
-    int64_t before = 0;
+    // the sequence that holds the stretch's first tile
     for (int b0 = 0;; b0 += THREADS) {
         const int b = b0 + tid;
-        const int64_t n = b0 == 0 ? own : b < p.B ? attn_seq<ROWS>(p, b).total(p.Hkv) : 0;
-        int64_t incl = n;
+        const int n = b0 == 0 ? own : b < p.B ? attn_seq<ROWS>(p, b).total(p.Hkv) : 0;
+        int incl = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
+            const int up = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += up;
         }
-        __syncthreads();
         if (lane == 31) scratch[warp] = incl;
         __syncthreads();
-        int64_t lower = before, sum = 0;
+        int lower = before, sum = 0;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             if (w < warp) lower += scratch[w];
             sum += scratch[w];
         }
-        const int64_t at = s.pos - (lower + incl - n);
+        if (b0 == 0) {
+            if (p.B <= THREADS) total = sum;
+            const int active = min(p.ctas, (int)((uint32_t)(total + LEAST - 1) / LEAST));
+            if (c >= active) {
+                s.pos = s.end = s.at = s.longer = 0;
+                s.each = 1;
+                s.seq = AttnSeq{0, 0, 0, 0, 0};
+                return s;
+            }
+            s.each = total / active;
+            s.longer = total - s.each * active;
+            s.pos = c * s.each + min(c, s.longer);
+            s.end = s.pos + s.each + (c < s.longer ? 1 : 0);
+        }
+        const int at = s.pos - (lower + incl - n);
         if (at >= 0 && at < n) {
             scratch[W] = b;
             scratch[W + 1] = at;
         }
         before += sum;
+        __syncthreads();
         if (before > s.pos) break;
     }
-    __syncthreads();
-    s.seq = attn_seq<ROWS>(p, (int)scratch[W]);
+    s.seq = attn_seq<ROWS>(p, scratch[W]);
     s.at = scratch[W + 1];
     return s;
 }
@@ -169,7 +178,7 @@ struct AttnTarget {
     bool whole;
     int slot;            // record of this part
     int first, parts;    // (parts of an item) the CTA that has its first tile, and how many have some
-    int64_t row0;        // first row of the block
+    int row0;            // first row of the block
     int rows;            // rows of the block in use
 };
 template <int ROWS>
@@ -180,18 +189,28 @@ __device__ __forceinline__ AttnTarget attn_target(const AttnParams &p, const Att
     t.slot = 2 * blockIdx.x + (part.t0 == 0 ? 1 : 0);
     t.first = t.parts = 0;
     if (!t.whole) {
-        const int64_t begin = s.pos - part.n - part.t0;      // (pos already behind the part)
+        const int begin = s.pos - part.n - part.t0;          // (pos already behind the part)
         t.first = s.owner(begin);
         t.parts = s.owner(begin + s.seq.tiles - 1) - t.first + 1;
     }
-    t.row0 = (int64_t)part.block * ROWS;
+    t.row0 = part.block * ROWS;
     t.rows = min(ROWS, s.seq.count * p.G - part.block * ROWS);
     return t;
 }
-__device__ __forceinline__ int64_t attn_out_at(const AttnParams &p, const AttnStretch &s, const AttnPart &part, int64_t row)
+__device__ __forceinline__ int64_t attn_out_at(const AttnParams &p, const AttnStretch &s, const AttnPart &part, int row)
 {
-    const int i = (int)(row / p.G), g = (int)(row - (int64_t)i * p.G);
+    const int i = row / p.G, g = row - i * p.G;
     return (((int64_t)s.seq.b * p.nodes.T + i) * p.Hq + (int64_t)part.head * p.G + g) * p.D;
+}
+
+// One ticket of the part's item, taken by one thread behind a barrier of those that wrote the part's record; true for the
+// last, whose CTA may then read all records (behind another barrier).
+__device__ __forceinline__ bool attn_ticket(const AttnParams &p, const AttnTarget &t)
+{
+    __threadfence();
+    const bool last = take_ticket(p.counters + t.first, t.parts);
+    __threadfence();
+    return last;
 }
 
 // Joins the parts of an item; called by all lanes of `warps` warps of the CTA that took its last ticket.  A warp has a row at
@@ -213,6 +232,16 @@ __device__ __forceinline__ void attn_join(const AttnParams &p, const AttnStretch
             o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
         for (int k0 = 0; k0 < t.parts; k0 += 32) {      // 32 parts at a time, as in one pass over keys
+            auto fetch = [&](int k, float4 (&x)[N]) {
+                const float *from = p.part + ((int64_t)slot_of(k0 + k) * ROWS + row0) * p.D + c;
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    x[i] = c < p.D && row0 + i < t.rows && k0 + k < t.parts ? __ldcg(reinterpret_cast<const float4 *>(from + (int64_t)i * p.D))
+                                                                            : make_float4(0.f, 0.f, 0.f, 0.f);
+            };
+            float4 x[N], y[N];
+            fetch(0, x);            // (two parts' results are asked for before their weights are known)
+            fetch(1, y);
             float2 ml[N];
             float w[N];
 #pragma unroll
@@ -229,18 +258,18 @@ __device__ __forceinline__ void attn_join(const AttnParams &p, const AttnStretch
                 o[i].x *= a, o[i].y *= a, o[i].z *= a, o[i].w *= a;
             }
             const int n = min(32, t.parts - k0);
-#pragma unroll 2
-            for (int k = 0; k < n; ++k) {
-                const float *from = p.part + ((int64_t)slot_of(k0 + k) * ROWS + row0) * p.D + c;
-                float4 x[N];
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    x[i] = c < p.D && row0 + i < t.rows ? __ldcg(reinterpret_cast<const float4 *>(from + (int64_t)i * p.D)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            auto add = [&](int k, const float4 (&x)[N]) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     const float a = __shfl_sync(0xffffffffu, w[i], k);
                     o[i].x = fmaf(a, x[i].x, o[i].x), o[i].y = fmaf(a, x[i].y, o[i].y), o[i].z = fmaf(a, x[i].z, o[i].z), o[i].w = fmaf(a, x[i].w, o[i].w);
                 }
+            };
+            for (int k = 0; k < n; k += 2) {
+                add(k, x);
+                if (k + 2 < n) fetch(k + 2, x);
+                if (k + 1 < n) add(k + 1, y);
+                if (k + 3 < n) fetch(k + 3, y);
             }
         }
 #pragma unroll

@@ -61,12 +61,12 @@ struct TcControl {
     uint64_t valid[12];                      // a bit for each key of a tile that is there, of two rounds of the ring: keys leave it
                                              // before the softmax warps have seen to their scores
     unsigned long long odd[2];
-    int64_t o_live[2];
+    int o_live[2];
     uint32_t tmem;
     int abort, last;
     int16_t tree[kMaxTreeNodes];             // parents, checked
     union {
-        int64_t scratch[2 * (kTcThreads / 32) + 4];
+        int scratch[kTcThreads / 32 + 2];
         float2 ml[2][kGroupThreads];
     };
 };
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&ctl.tmem)), "r"((uint32_t)kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    AttnStretch s = attn_plan<ROWS, kTcThreads>(p, ctl.scratch);
+    AttnStretch s = attn_plan<ROWS, kTcThreads, 4>(p, ctl.scratch);
     attn_clear_unused<__nv_bfloat16>(p, kTcThreads);
     fence_before();
     __syncthreads();
@@ -228,30 +228,27 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 }
                 copies_arrive(&ctl.q_full);
             }
-            int64_t keys = (int64_t)s.seq.len + s.seq.count;
-            if (keys > (int64_t)p.max_pages * p.page_size) {
-                raise_status(p.status, SPR_ERR_BAD_PAGE);
-                keys = (int64_t)p.max_pages * p.page_size;
-            }
+            const int keys = attn_keys(p, s.seq.len, s.seq.count);
+            if (keys < (int64_t)s.seq.len + s.seq.count) raise_status(p.status, SPR_ERR_BAD_PAGE);
             const int end = part.t0 + part.n;
             auto find = [&](int tile) {             // lane 8 j + r: where run r (8 keys) of tile + j begins in the caches
                 const int t = tile + (lane >> 3);
-                const int64_t slot = (int64_t)t * kAttnTile + 8 * (lane & 7);
+                const int slot = t * kAttnTile + 8 * (lane & 7);
                 if (t >= end || slot >= keys) return -1;
-                const uint32_t at = (uint32_t)((uint64_t)slot >> 3) / (uint32_t)(p.page_size >> 3);       // pages are whole runs
+                const int at = slot / p.page_size;
                 const int page = __ldg(p.page_table + (int64_t)s.seq.b * p.max_pages + at);
                 if (page < 0 || page >= p.num_pages) {
                     raise_status(p.status, SPR_ERR_BAD_PAGE);
                     return -1;
                 }
-                return (page * p.Hkv + part.head) * p.page_size + (int)(slot - (int64_t)at * p.page_size);
+                return (page * p.Hkv + part.head) * p.page_size + (slot - at * p.page_size);
             };
             int tile = part.t0, next = find(tile);
             while (alive && tile < end) {
                 const int rows = next;
                 next = find(tile + 4);
                 for (int u = 0; alive && u < 4 && tile < end; ++u, ++tile) {
-                    const int64_t left = keys - (int64_t)tile * kAttnTile;
+                    const int left = keys - tile * kAttnTile;
                     uint64_t valid = left >= 64 ? ~0ull : (1ull << left) - 1;
                     const uint32_t runs = __ballot_sync(0xffffffffu, rows >= 0) >> (8 * u) & 0xffu;
                     if (runs != 0xffu)
@@ -302,7 +299,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             constexpr uint32_t kPv = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(COLS >> 3) << 17) | (8u << 24);
             const uint32_t col_s = tmem + kColS + 128 * group, col_o = tmem + kColO + 128 * group;
             AttnPart part;
-            int64_t at = 0;                 // tiles of the stretch before the part
+            int at = 0;                     // tiles of the stretch before the part
             uint32_t parts = 0;
             int v_unit = 2 * group + 1;     // place of the values of this group's next tile
             uint32_t v_round = 0;
@@ -314,8 +311,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             // where S of tile i goes P of tile i - 4, this group's last but one, was: the product with it has to be complete
             int k_unit = 2 * group;             // place of the keys of this group's next tile
             uint32_t k_round = 0;
-            auto scores = [&](int64_t i) {
-                const int unit = k_unit, b = (int)i >> 1 & 1;
+            auto scores = [&](int i) {
+                const int unit = k_unit, b = i >> 1 & 1;
                 if (!wait(&ctl.full[unit], k_round) || (i >= 4 && !wait(&ctl.pv_done[group][b], (uint32_t)(i >> 2) - 1))) return;
                 k_unit += 4;
                 if (k_unit >= Shape::units) {
@@ -333,8 +330,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 commit(&ctl.empty[unit]);
             };
             while (alive && attn_next<ROWS>(p, s, part)) {
-                const int64_t end = at + part.n;
-                int64_t mine = at + ((at ^ group) & 1);
+                const int end = at + part.n;
+                int mine = at + ((at ^ group) & 1);
                 at = end;
                 if (!wait(&ctl.q_full, parts++)) break;
                 if (mine < end) scores(mine);
@@ -346,7 +343,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                         arrive(&ctl.q_empty);
                 }
                 for (bool begun = false; alive && mine < end; mine += 2, begun = true) {
-                    const int unit = v_unit, b = (int)mine >> 1 & 1;
+                    const int unit = v_unit, b = mine >> 1 & 1;
                     const uint32_t phase = (uint32_t)(mine >> 2);
                     if (!wait(&ctl.full[unit], v_round) || !wait(&ctl.p_ready[group][b], phase)) break;
                     v_unit += 4;
@@ -357,7 +354,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     fence_after();
                     const uint32_t v = ring + unit * Shape::unit, w = col_s + 64 * b;
-                    const bool live = begun || *reinterpret_cast<volatile int64_t *>(&ctl.o_live[group]) == mine;
+                    const bool live = begun || *reinterpret_cast<volatile int *>(&ctl.o_live[group]) == mine;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) mma_tmem(col_o, w + 8 * q, tile_desc(v + q * 2048, true), kPv, live || q != 0);
                     commit(&ctl.pv_done[group][b]);
@@ -379,7 +376,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
         const uint32_t col_o = lanes + kColO + 128 * group;
         const float c = p.abs_scale_log2;
         AttnPart part;
-        int64_t at = 0;
+        int at = 0;
         int tree_of = -1;
         bool dead = false;
         auto wait = [&](uint64_t *bar, uint32_t parity) {
@@ -392,32 +389,32 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
         while (attn_next<ROWS>(p, s, part)) {
             const AttnTarget t = attn_target<ROWS>(p, s, part);
             const bool in = row < t.rows, warp_in = (warp & 3) * 32 < t.rows;
-            const int node = in ? (int)((t.row0 + row) / p.G) : 0;
+            const int node = in ? (t.row0 + row) / p.G : 0;
             softmax_meet();                                 // (both groups have read both O, and the tree)
-            if (p.nodes.parents && tree_of != s.seq.b && (int64_t)(part.t0 + part.n) * kAttnTile > s.seq.len) {
+            if (p.nodes.parents && tree_of != s.seq.b && (part.t0 + part.n) * kAttnTile > s.seq.len) {
                 for (int j = tid; j < s.seq.count; j += kSoftmaxThreads)
                     ctl.tree[j] = (int16_t)checked_parent(p.nodes.parents[(int64_t)s.seq.b * p.nodes.T + j], j, p.status);
                 tree_of = s.seq.b;
                 softmax_meet();
             }
             float m = neg_inf(), l = 0.f;
-            int64_t mine = at + ((at ^ group) & 1);         // this group's next tile
-            const int64_t begin = at, end = at + part.n;
+            int mine = at + ((at ^ group) & 1);             // this group's next tile
+            const int begin = at, end = at + part.n;
             at = end;
             const bool any = mine < end;
-            int64_t slot0 = (part.t0 + (mine - begin)) * kAttnTile;
-            int place = (int)(mine % Shape::units);         // of the tile in two rounds of the ring
+            int slot0 = (part.t0 + (mine - begin)) * kAttnTile;
+            int place = mine % Shape::units;         // of the tile in two rounds of the ring
             for (bool begun = false; mine < end; mine += 2, begun = true, slot0 += 2 * kAttnTile, place = place < Shape::units - 2 ? place + 2 : place + 2 - Shape::units) {
-                const int b = (int)mine >> 1 & 1;
+                const int b = mine >> 1 & 1;
                 const uint32_t phase = (uint32_t)(mine >> 2), col_s = lanes + kColS + 128 * group + 64 * b;
                 wait(&ctl.s_full[group][b], phase);
                 const bool tail = slot0 + kAttnTile > s.seq.len;      // (alike in all threads, whatever went wrong: they meet)
                 unsigned long long odd = 0;
                 uint64_t vis = ctl.valid[place];
                 if (tail) {
-                    const int64_t d = s.seq.len - slot0;     // keys of the prefix
+                    const int d = s.seq.len - slot0;         // keys of the prefix
                     const int16_t *tree = p.nodes.parents ? ctl.tree : nullptr;
-                    vis &= d <= 0 ? seen_nodes(tree, node, (int)-d) : seen_nodes(tree, node, 0) << d | ((1ull << d) - 1);
+                    vis &= d <= 0 ? seen_nodes(tree, node, -d) : seen_nodes(tree, node, 0) << d | ((1ull << d) - 1);
                     // values that are not finite, where not every row sees every key: each thread looks at half a key
                     wait(&ctl.full[(2 * place + 1) % Shape::units], (uint32_t)(mine / (Shape::units / 2)));
                     const uint32_t v = ring + (2 * place + 1) % Shape::units * Shape::unit + (row >> 1) * 128 + (row & 1) * 64;
@@ -595,14 +592,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             if (!t.whole && group == 0 && in) __stcg(&p.part_ml[(int64_t)t.slot * ROWS + row], make_float2(top * c, l));
             fence_before();
             if (!t.whole) {
-                __threadfence();
                 softmax_meet();
-                if (tid == 0) ctl.last = take_ticket(p.counters + t.first, t.parts);
+                if (tid == 0) ctl.last = attn_ticket(p, t);
                 softmax_meet();
-                if (ctl.last) {
-                    __threadfence();
-                    attn_join<ROWS, __nv_bfloat16>(p, s, part, t, warp, kSoftmaxThreads / 32);
-                }
+                if (ctl.last) attn_join<ROWS, __nv_bfloat16>(p, s, part, t, warp, kSoftmaxThreads / 32);
             }
         }
     }

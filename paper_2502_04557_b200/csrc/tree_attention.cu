@@ -54,6 +54,10 @@ int tree_attention(const void *q, const void *k_cache, const void *v_cache, int 
         !aligned(counts, 4) || !aligned(parents, 4) || !aligned(page_table, 4))
         return SPR_ERR_INVALID_ARG;
     const int rows = attention_block_rows(T, Hq / Hkv, dt);
+    // work is counted in tiles, in 32 bits; so are a sequence's slots
+    const int64_t capacity = (int64_t)max_pages * page_size < 0x7fffff00 ? (int64_t)max_pages * page_size : 0x7fffff00;
+    const int64_t blocks = ((int64_t)T * (Hq / Hkv) + rows - 1) / rows;
+    if ((double)B * Hkv * blocks * ((capacity + kAttnTile - 1) / kAttnTile) > 2147483000.0) return SPR_ERR_UNSUPPORTED;
     if (!ws || !aligned(ws, 256) || ws_bytes < (size_t)kHeaderBytes) return SPR_ERR_WORKSPACE;
     Carver c = carve(ws_bytes);
     const AttentionWs w = attention_ws_layout(c, kAttnMaxCtas, rows, D);
@@ -70,6 +74,7 @@ int tree_attention(const void *q, const void *k_cache, const void *v_cache, int 
     p.nodes = DraftNodes{lens, counts, parents, T};
     p.B = B, p.Hq = Hq, p.Hkv = Hkv, p.G = Hq / Hkv, p.D = D;
     p.max_pages = max_pages, p.num_pages = num_pages, p.page_size = page_size;
+    p.capacity = capacity;
     p.scale_log2 = scale * kLog2e;
     p.abs_scale_log2 = fmaxf(fabsf(p.scale_log2), 1e-37f);
     p.flip = scale < 0.f ? 0x80008000u : 0u;
