@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
     float *join = reinterpret_cast<float *>(raw + (size_t)kMmaWarps * Shape::stages * Shape::step);
     const int w16 = warp * 16;                              // keys w16 .. + 15 of a tile
 
-    AttnStretch s = attn_plan<ROWS, kMmaThreads, 4>(p, ctl.scratch);
+    AttnStretch s = attn_plan<ROWS, kMmaThreads, 6>(p, ctl.scratch);
     attn_clear_unused<__nv_bfloat16>(p, kMmaThreads);
 
     // ---------------------------------------------------------------- copies, some steps ahead of the products

@@ -4,8 +4,9 @@
 // node, then by query head), over all of the sequence's keys in tiles of 64.  The tiles of all items stand in one line
 // (by sequence, head, row block, tile) and each CTA takes an equal stretch of it, whatever the lengths, so that
 // the split follows the lengths that the device holds and a captured launch serves all of them.  A stretch begins and
-// ends inside items.  Parts of an item go to the workspace, and the CTA that takes the last ticket of an item joins
-// its parts in their order; nothing waits on another CTA.
+// ends inside items.  Where there is little to do, each CTA gets a piece of one item instead, if there are CTAs enough: a
+// stretch of two parts would take two ends of parts.  Parts of an item go to the workspace, and the CTA that takes the last
+// ticket of an item joins its parts in their order; nothing waits on another CTA.
 #pragma once
 
 #include "attention.h"
@@ -37,6 +38,7 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnParams &p, int b)
 struct AttnStretch {
     int pos, end;
     int each, longer;
+    int first, pieces;       // (pieces > 0) of one item: the CTA with the first, and how many there are
     AttnSeq seq;             // the sequence that pos lies in
     int at;                  // pos within it
 
@@ -78,13 +80,16 @@ __device__ __forceinline__ AttnStretch attn_plan(const AttnParams &p, int *scrat
     constexpr int W = THREADS / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = blockIdx.x;
     AttnStretch s;
-    const int own = tid < p.B ? attn_seq<ROWS>(p, tid).total(p.Hkv) : 0;
+    constexpr int kFewTiles = 16;    // per CTA
+    AttnSeq mine = {0, 0, 0, 0, 0};
+    if (tid < p.B) mine = attn_seq<ROWS>(p, tid);
+    const int own = mine.total(p.Hkv);
     int before = 0, total = 0;       // tiles of the sequences below b0, and of all
     if (p.B > THREADS) {             // the line's length first
-        int mine = own;
-        for (int b = tid + THREADS; b < p.B; b += THREADS) mine += attn_seq<ROWS>(p, b).total(p.Hkv);
-        mine = __reduce_add_sync(0xffffffffu, mine);
-        if (lane == 0) scratch[warp] = mine;
+        int sum = own;
+        for (int b = tid + THREADS; b < p.B; b += THREADS) sum += attn_seq<ROWS>(p, b).total(p.Hkv);
+        sum = __reduce_add_sync(0xffffffffu, sum);
+        if (lane == 0) scratch[warp] = sum;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < W; ++w) total += scratch[w];
@@ -110,7 +115,47 @@ __device__ __forceinline__ AttnStretch attn_plan(const AttnParams &p, int *scrat
         }
         if (b0 == 0) {
             if (p.B <= THREADS) total = sum;
+            s.first = s.pieces = 0;
             const int active = min(p.ctas, (int)((uint32_t)(total + LEAST - 1) / LEAST));
+            if (p.B <= THREADS && total <= p.ctas * kFewTiles && total > 0) {
+                // pieces of items, none longer than the stretches would be
+                const int most = max(LEAST, (total + p.ctas - 1) / p.ctas), per = (mine.tiles + most - 1) / most;
+                const int pieces = per * mine.blocks * p.Hkv;
+                int upto = pieces;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int up = __shfl_up_sync(0xffffffffu, upto, o);
+                    if (lane >= o) upto += up;
+                }
+                __syncthreads();
+                if (lane == 31) scratch[warp] = upto;
+                __syncthreads();
+                int all = 0;
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    if (w < warp) upto += scratch[w];
+                    all += scratch[w];
+                }
+                if (all <= p.ctas) {
+                    s.pos = s.end = s.at = s.longer = 0;
+                    s.each = 1;
+                    s.seq = AttnSeq{0, 0, 0, 0, 0};
+                    if (c >= all) return s;
+                    if (c >= upto - pieces && c < upto) {
+                        scratch[W] = b;
+                        scratch[W + 1] = c - (upto - pieces);
+                    }
+                    __syncthreads();
+                    s.seq = attn_seq<ROWS>(p, scratch[W]);
+                    s.pieces = (s.seq.tiles + most - 1) / most;
+                    const int item = scratch[W + 1] / s.pieces, piece = scratch[W + 1] - item * s.pieces;
+                    const int t0 = piece * s.seq.tiles / s.pieces;
+                    s.first = c - piece;
+                    s.end = (piece + 1) * s.seq.tiles / s.pieces - t0;
+                    s.at = item * s.seq.tiles + t0;
+                    return s;
+                }
+            }
             if (c >= active) {
                 s.pos = s.end = s.at = s.longer = 0;
                 s.each = 1;
@@ -188,7 +233,10 @@ __device__ __forceinline__ AttnTarget attn_target(const AttnParams &p, const Att
     t.whole = part.n == s.seq.tiles;
     t.slot = 2 * blockIdx.x + (part.t0 == 0 ? 1 : 0);
     t.first = t.parts = 0;
-    if (!t.whole) {
+    if (s.pieces) {
+        t.first = s.first;
+        t.parts = s.pieces;
+    } else if (!t.whole) {
         const int begin = s.pos - part.n - part.t0;          // (pos already behind the part)
         t.first = s.owner(begin);
         t.parts = s.owner(begin + s.seq.tiles - 1) - t.first + 1;
@@ -213,15 +261,14 @@ __device__ __forceinline__ bool attn_ticket(const AttnParams &p, const AttnTarge
     return last;
 }
 
-// Joins the parts of an item; called by all lanes of `warps` warps of the CTA that took its last ticket.  A warp has a row at
-// a time, a lane one part's maximum and sum and then four columns; ROWS_AT_ONCE rows are on their way together.
+// Joins the parts of an item; called by all lanes of `warps` warps of the CTA that took its last ticket.  A warp has N rows at a
+// time, a lane four columns of them; K parts are on their way together, and are taken in as a pass over keys takes in keys.
 template <int ROWS, typename T>
 __device__ __forceinline__ void attn_join(const AttnParams &p, const AttnStretch &s, const AttnPart &part, const AttnTarget &t,
                                           int warp, int warps)
 {
-    constexpr int N = 4;
-    const int lane = threadIdx.x & 31, c = lane * 4;
-    auto slot_of = [&](int k) { return 2 * (t.first + k) + (k == 0 ? 1 : 0); };
+    constexpr int N = 4, K = 4;
+    const int c = (threadIdx.x & 31) * 4;
     for (int row0 = warp * N; row0 < t.rows; row0 += warps * N) {
         float top[N], sum[N];
         float4 o[N];
@@ -231,45 +278,35 @@ __device__ __forceinline__ void attn_join(const AttnParams &p, const AttnStretch
             sum[i] = 0.f;
             o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        for (int k0 = 0; k0 < t.parts; k0 += 32) {      // 32 parts at a time, as in one pass over keys
-            auto fetch = [&](int k, float4 (&x)[N]) {
-                const float *from = p.part + ((int64_t)slot_of(k0 + k) * ROWS + row0) * p.D + c;
+#pragma unroll 1
+        for (int k0 = 0; k0 < t.parts; k0 += K) {
+            float2 ml[K][N];
+            float4 x[K][N];
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    x[i] = c < p.D && row0 + i < t.rows && k0 + k < t.parts ? __ldcg(reinterpret_cast<const float4 *>(from + (int64_t)i * p.D))
-                                                                            : make_float4(0.f, 0.f, 0.f, 0.f);
-            };
-            float4 x[N], y[N];
-            fetch(0, x);            // (two parts' results are asked for before their weights are known)
-            fetch(1, y);
-            float2 ml[N];
-            float w[N];
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const bool there = k0 + lane < t.parts && row0 + i < t.rows;
-                ml[i] = there ? __ldcg(&p.part_ml[(int64_t)slot_of(k0 + lane) * ROWS + row0 + i]) : make_float2(neg_inf(), 0.f);
-            }
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float m = fmaxf(top[i], warp_max(ml[i].x)), ref = m == neg_inf() ? 0.f : m, a = ex2(top[i] - ref);
-                top[i] = m;
-                w[i] = ex2(ml[i].x - ref);          // (a part that saw nothing has 0 and zeros)
-                sum[i] = sum[i] * a + warp_sum(w[i] * ml[i].y);
-                o[i].x *= a, o[i].y *= a, o[i].z *= a, o[i].w *= a;
-            }
-            const int n = min(32, t.parts - k0);
-            auto add = [&](int k, const float4 (&x)[N]) {
+            for (int k = 0; k < K; ++k)
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const float a = __shfl_sync(0xffffffffu, w[i], k);
-                    o[i].x = fmaf(a, x[i].x, o[i].x), o[i].y = fmaf(a, x[i].y, o[i].y), o[i].z = fmaf(a, x[i].z, o[i].z), o[i].w = fmaf(a, x[i].w, o[i].w);
+                    const int64_t at = (int64_t)(2 * (t.first + k0 + k) + (k0 + k == 0 ? 1 : 0)) * ROWS + row0 + i;
+                    const bool there = k0 + k < t.parts && row0 + i < t.rows;
+                    ml[k][i] = there ? __ldcg(p.part_ml + at) : make_float2(neg_inf(), 0.f);
+                    x[k][i] = there && c < p.D ? __ldcg(reinterpret_cast<const float4 *>(p.part + at * p.D + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
                 }
-            };
-            for (int k = 0; k < n; k += 2) {
-                add(k, x);
-                if (k + 2 < n) fetch(k + 2, x);
-                if (k + 1 < n) add(k + 1, y);
-                if (k + 3 < n) fetch(k + 3, y);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                float m = top[i];
+#pragma unroll
+                for (int k = 0; k < K; ++k) m = fmaxf(m, ml[k][i].x);
+                const float ref = m == neg_inf() ? 0.f : m, a = ex2(top[i] - ref);
+                top[i] = m;
+                sum[i] *= a;
+                o[i].x *= a, o[i].y *= a, o[i].z *= a, o[i].w *= a;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const float w = ex2(ml[k][i].x - ref);      // (a part that saw nothing has 0 and zeros)
+                    sum[i] = fmaf(w, ml[k][i].y, sum[i]);
+                    o[i].x = fmaf(w, x[k][i].x, o[i].x), o[i].y = fmaf(w, x[k][i].y, o[i].y);
+                    o[i].z = fmaf(w, x[k][i].z, o[i].z), o[i].w = fmaf(w, x[k][i].w, o[i].w);
+                }
             }
         }
 #pragma unroll

@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&ctl.tmem)), "r"((uint32_t)kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    AttnStretch s = attn_plan<ROWS, kTcThreads, 4>(p, ctl.scratch);
+    AttnStretch s = attn_plan<ROWS, kTcThreads, 6>(p, ctl.scratch);
     attn_clear_unused<__nv_bfloat16>(p, kTcThreads);
     fence_before();
     __syncthreads();
