@@ -765,31 +765,28 @@ def _optional(device: int, t, dtype, shape, name: str):
     """Address of an optional tensor of this shape, or None."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
     return _on(device, dtype, name, t)
-
-
-def _nodes(device: int, B: int, T: int, lens, counts, parents):
-    return (_optional(device, lens, torch.int32, (B,), "lens"), _optional(device, counts, torch.int32, (B,), "counts"),
-            _optional(device, parents, torch.int32, (B, T), "parents"))
 
 
 def _caches(device: int, k_cache, v_cache, page_table, dtype, B: int, D: int):
     """(addresses, Hkv, page_size, num_pages, max_pages) of paged caches [num_pages, Hkv, page_size, D]."""
     k, v = _on(device, dtype, "k_cache", k_cache), _on(device, dtype, "v_cache", v_cache)
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.shape[3] != D:
+    shape = k_cache.shape
+    if len(shape) != 4 or shape != v_cache.shape or shape[3] != D:
         raise ValueError(f"k_cache and v_cache must be [num_pages, Hkv, page_size, {D}]")
     table = _on(device, torch.int32, "page_table", page_table)
     if page_table.dim() != 2 or page_table.shape[0] != B:
         raise ValueError(f"page_table must be [{B}, max_pages]")
-    num_pages, Hkv, page_size, _ = k_cache.shape
-    if max(num_pages, Hkv, page_size, page_table.shape[1]) > _INT_MAX:
+    num_pages, Hkv, page_size, _ = shape
+    max_pages = page_table.shape[1]
+    if (num_pages | Hkv | page_size | max_pages) > _INT_MAX:
         raise ValueError("caches and page_table must have sizes below 2^31")
-    return k, v, table, Hkv, page_size, num_pages, page_table.shape[1]
+    return k, v, table, Hkv, page_size, num_pages, max_pages
 
 
-def _node_rows(device: int, t, dtype, B: int, T: int, H: int, D: int, name: str):
+def _node_rows(device: int, t, dtype, shape, name: str):
     """Address and distance between nodes (in elements) of [B,T,H,D], dense but for that distance: a projection that gives
     queries, keys and values side by side is read where it is."""
     if t.get_device() != device:
@@ -798,9 +795,10 @@ def _node_rows(device: int, t, dtype, B: int, T: int, H: int, D: int, name: str)
         raise ValueError(f"{name} is on cuda:{t.get_device()}, the current device is cuda:{device}")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if tuple(t.shape) != (B, T, H, D):
-        raise ValueError(f"{name} must be {(B, T, H, D)}, got {tuple(t.shape)}")
-    if t.is_contiguous() or t.numel() == 0:
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
+    B, T, H, D = shape
+    if t.is_contiguous():
         return t.data_ptr(), H * D
     b, n, h, d = t.stride()
     stride = n if T > 1 else b if B > 1 else H * D
@@ -821,20 +819,20 @@ def cache_append(k, v, k_cache, v_cache, page_table, lens, ws: Workspace, q=None
     dtype, dt = k.dtype, _dt(k)
     if k.dim() != 4:
         raise ValueError("k must be [B,T,Hkv,D]")
-    B, T, Hkv, D = k.shape
-    if max(B, T, Hkv, D) > _INT_MAX:
+    B, T, Hkv, D = shape = tuple(k.shape)
+    if (B | T | Hkv | D) > _INT_MAX:
         raise ValueError("k [B,T,Hkv,D] must have sizes below 2^31")
     kc, vc, table, heads, page_size, num_pages, max_pages = _caches(dev, k_cache, v_cache, page_table, dtype, B, D)
     if heads != Hkv:
         raise ValueError(f"the caches have {heads} heads, k has {Hkv}")
-    ka, ks = _node_rows(dev, k, dtype, B, T, Hkv, D, "k")
-    va, vs = _node_rows(dev, v, dtype, B, T, Hkv, D, "v")
+    ka, ks = _node_rows(dev, k, dtype, shape, "k")
+    va, vs = _node_rows(dev, v, dtype, shape, "v")
     qa, qs, Hq, oa = None, 0, 0, None
     if q is not None:
         if q.dim() != 4 or q.shape[2] > _INT_MAX:
             raise ValueError("q must be [B,T,Hq,D]")
         Hq = q.shape[2]
-        qa, qs = _node_rows(dev, q, dtype, B, T, Hq, D, "q")
+        qa, qs = _node_rows(dev, q, dtype, (B, T, Hq, D), "q")
     elif q_out is not None:
         raise ValueError("q_out needs q")
     rot, fa = 0, None
@@ -842,12 +840,14 @@ def cache_append(k, v, k_cache, v_cache, page_table, lens, ws: Workspace, q=None
         fa, rot = _on(dev, torch.float32, "inv_freq", inv_freq), 2 * inv_freq.numel()
         if rot > D:
             raise ValueError(f"inv_freq must have at most D / 2 = {D // 2} entries, got {inv_freq.numel()}")
-    n, c, par = _nodes(dev, B, T, lens, counts, parents)
+    n = _optional(dev, lens, torch.int32, (B,), "lens")
+    c = _optional(dev, counts, torch.int32, (B,), "counts")
+    par = _optional(dev, parents, torch.int32, (B, T), "parents")
     sl = _optional(dev, slots, torch.int32, (B, T), "slots")
     p, size = _ws(dev, ws)
     if q is not None:
         q_out, oa = _result(dev, q_out, (B, T, Hq, D), dtype, "q_out")
-    rc = lib().cache_append(qa, qs, ka, ks, va, vs, B, T, Hq, Hkv, D, dt, n, c, par, sl, fa, rot, int(interleaved), table,
+    rc = lib().cache_append(qa, qs, ka, ks, va, vs, B, T, Hq, Hkv, D, dt, n, c, par, sl, fa, rot, interleaved, table,
                             max_pages, num_pages, page_size, kc, vc, oa, p, size, _raw_stream(dev))
     if rc != 0:
         _check("cache_append", rc)
@@ -860,17 +860,19 @@ def tree_attention(q, k_cache, v_cache, page_table, lens, ws: Workspace, scale=N
 
     counts i32 [B] and parents i32 [B,T] as for cache_append.  Returns out [B,T,Hq,D]."""
     dev = torch.cuda.current_device()
-    dt = _dt(q)
+    dtype, dt = q.dtype, _dt(q)
     if q.dim() != 4:
         raise ValueError("q must be [B,T,Hq,D]")
-    B, T, Hq, D = q.shape
-    if max(B, T, Hq, D) > _INT_MAX:
+    B, T, Hq, D = shape = tuple(q.shape)
+    if (B | T | Hq | D) > _INT_MAX:
         raise ValueError("q [B,T,Hq,D] must have sizes below 2^31")
-    qa = _on(dev, q.dtype, "q", q)
-    kc, vc, table, Hkv, page_size, num_pages, max_pages = _caches(dev, k_cache, v_cache, page_table, q.dtype, B, D)
-    n, c, par = _nodes(dev, B, T, lens, counts, parents)
+    qa = _on(dev, dtype, "q", q)
+    kc, vc, table, Hkv, page_size, num_pages, max_pages = _caches(dev, k_cache, v_cache, page_table, dtype, B, D)
+    n = _optional(dev, lens, torch.int32, (B,), "lens")
+    c = _optional(dev, counts, torch.int32, (B,), "counts")
+    par = _optional(dev, parents, torch.int32, (B, T), "parents")
     p, size = _ws(dev, ws)
-    out, oa = _result(dev, out, (B, T, Hq, D), q.dtype, "out")
+    out, oa = _result(dev, out, shape, dtype, "out")
     rc = lib().tree_attention(qa, kc, vc, B, T, Hq, Hkv, D, dt, n, c, par, table, max_pages, num_pages, page_size,
                               D ** -0.5 if scale is None else scale, oa, p, size, _raw_stream(dev))
     if rc != 0:
@@ -888,13 +890,13 @@ def logits_rules(logits, V: int, ws: Workspace, history=None, history_len=None, 
     masks i32 [M,words], a bit per token, with mask_rows i32 [B,T], negative: none.  Returns out [B,T,ld_out] (new
     rows have ldv entries, those behind V not written); out may be logits."""
     dev = torch.cuda.current_device()
-    dt = _dt(logits)
+    dtype, dt = logits.dtype, _dt(logits)
     if logits.dim() != 3:
         raise ValueError("logits must be [B,T,ldv]")
     B, T, ldv = logits.shape
-    if max(B, T, V) > _INT_MAX:
+    if (B | T) > _INT_MAX or V > _INT_MAX:
         raise ValueError("logits [B,T,ldv] and V must be below 2^31")
-    la = _on(dev, logits.dtype, "logits", logits)
+    la = _on(dev, dtype, "logits", logits)
     if (history is None) != (history_len is None):
         raise ValueError("history and history_len go together")
     L, ha = 0, None
@@ -904,7 +906,8 @@ def logits_rules(logits, V: int, ws: Workspace, history=None, history_len=None, 
         ha, L = _on(dev, torch.int32, "history", history), history.shape[1]
     hl = _optional(dev, history_len, torch.int32, (B,), "history_len")
     ta = _optional(dev, tokens, torch.int32, (B, T), "tokens")
-    _, c, par = _nodes(dev, B, T, None, counts, parents)
+    c = _optional(dev, counts, torch.int32, (B,), "counts")
+    par = _optional(dev, parents, torch.int32, (B, T), "parents")
     pa = _optional(dev, penalties, torch.float32, (B, 3), "penalties")
     if (bias_tokens is None) != (bias_values is None):
         raise ValueError("bias_tokens and bias_values go together")
@@ -931,7 +934,7 @@ def logits_rules(logits, V: int, ws: Workspace, history=None, history_len=None, 
     else:
         if out.dim() != 3 or out.shape[0] != B or out.shape[1] != T:
             raise ValueError(f"out must be [{B}, {T}, ld_out]")
-        oa, ld_out = _on(dev, logits.dtype, "out", out), out.shape[2]
+        oa, ld_out = _on(dev, dtype, "out", out), out.shape[2]
     rc = lib().logits_rules(la, ldv, V, B, T, dt, ha, L, hl, ta, par, c, pa, ba, bv, nb, ma, ld_mask, num_masks, mr, oa, ld_out,
                             p, size, _raw_stream(dev))
     if rc != 0:

@@ -10,6 +10,8 @@
 // run of its rows: counts and biases of the stretch are gathered into shared memory once (history and biases are
 // read by every stretch, from L2), with integer atomics, so that their order does not matter.  Nearly all tokens are
 // touched by neither: a bitmap says which vectors of a row hold one that is, and all others go by as they came.
+#include <atomic>
+
 #include "common.cuh"
 #include "draft_tree.cuh"
 #include "host_util.h"
@@ -366,9 +368,16 @@ cudaError_t launch_rules(const RuleParams &p, unsigned ctas, cudaStream_t st)
 {
     const size_t smem = Stretch<T, BYTES>::smem(p.stages, p.n_bias);
     if (smem > 40000) {
-        const cudaError_t e = cudaFuncSetAttribute(rules_kernel<T, BYTES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   (int)Stretch<T, BYTES>::smem(kMaxStages, kMaxBiases));
+        static std::atomic<bool> attr_set[64];   // host threads may race to set it: all of them store `true`
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
         if (e != cudaSuccess) return e;
+        if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
+            e = cudaFuncSetAttribute(rules_kernel<T, BYTES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     (int)Stretch<T, BYTES>::smem(kMaxStages, kMaxBiases));
+            if (e != cudaSuccess) return e;
+            if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
+        }
     }
     rules_kernel<T, BYTES><<<ctas, Stretch<T, BYTES>::threads, smem, st>>>(p);
     return cudaGetLastError();
