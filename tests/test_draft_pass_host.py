@@ -112,6 +112,8 @@ def test_attention_arguments_are_checked(mem):
         assert attend(L, p, **bad) == INVALID, bad
     for bad in (dict(D=12), dict(D=136), dict(page=4), dict(page=20), dict(pages=1 << 27)):
         assert attend(L, p, **bad) == UNSUPPORTED, bad
+    # tiles of 64 keys that could pass 2^31: 2^15 sequences of 2 heads with tables of 2^17 pages
+    assert attend(L, p, B=1 << 15, max_pages=1 << 17) == UNSUPPORTED
     n = spr.workspace_bytes(spr.OP_TREE_ATTENTION, 2, 3, 1, 64, 0, spr.BF16)
     assert attend(L, p, T=64, n=n // 8) == WORKSPACE
 
