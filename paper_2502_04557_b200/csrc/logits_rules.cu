@@ -6,16 +6,18 @@
 //        (l > 0 ? l / r : l r) - f c_v - s                   where c_v > 0   (r, f, s: repetition, frequency, presence)
 //   l' = l' + bias_v, and -inf where the row's mask has no bit for v
 //
-// Bound by memory: a row is read and written once.  A CTA has one stretch of the vocabulary of one sequence, for a
-// run of its rows: counts and biases of the stretch are gathered into shared memory once (history and biases are
-// read by every stretch, from L2), with integer atomics, so that their order does not matter.  Nearly all tokens are
-// touched by neither: a bitmap says which vectors of a row hold one that is, and all others go by as they came.
+// Bound by memory: a row is read and written once.  A CTA has one stretch of the vocabulary of one sequence, for a run of
+// its rows, which go through a ring in shared memory by bulk copies.  The stretch's counts and biases are gathered into tables
+// once (history and biases are read by every stretch, from L2), with integer atomics, so that their order does not matter.
+// Nearly all tokens are touched by neither: those that are stand in a list, one or two to a thread, and are put right in the
+// ring; masks are applied there to vectors, with their bits read a row ahead.  Rows by 8 KB for many sequences, 4 KB for few.
+// 256 x 17 rows of 128256 bf16 entries, a quarter masked: 423 us, 5.3 TB/s (no masks 387, 5.8).  More rows in the ring take
+// CTAs from the SM (4 stages 490 us), two leave the copies too little (508 us).
 #include <atomic>
 
-#include "common.cuh"
-#include "draft_tree.cuh"
 #include "host_util.h"
 #include "launch.h"
+#include "rules.cuh"
 #include "tensor_pair.cuh"
 
 namespace spr {
@@ -25,67 +27,6 @@ namespace {
 using namespace pairtc;
 
 constexpr int kMaxStages = 3;         // rows of a CTA that are on their way
-constexpr int kMaxBiases = 1024;
-constexpr int kOnPath = (int)0x80000000u;
-
-struct RuleParams {
-    const void *logits;
-    void *out;
-    int64_t ldv, ld_out;
-    int V, B;
-    DraftNodes nodes;            // lens is not used
-    const int32_t *history;
-    int64_t ld_history;
-    const int32_t *history_len;
-    const int32_t *tokens;       // [B,T] or null
-    const float *penalties;      // [B,3] or null
-    const int32_t *bias_tokens;  // [B,n_bias]
-    const float *bias_values;
-    int n_bias;
-    const uint32_t *masks;       // [num_masks, ld_mask]
-    int64_t ld_mask;
-    int num_masks;
-    const int32_t *mask_rows;    // [B,T]
-    int *status;
-    int chunks, row_groups, rows_per_group;
-    int stages;                  // of the ring
-    int same;                    // rows of both tensors lie alike on 16-byte boundaries
-};
-
-// a bit for each byte, as that byte's highest
-__device__ __forceinline__ uint32_t byte_signs(uint32_t four) { return ((four & 0xfu) * 0x00204081u & 0x01010101u) << 7; }
-
-template <typename T>
-struct Lanes;            // a 16-byte vector as elements
-template <>
-struct Lanes<float> {
-    static __device__ __forceinline__ void forbid(uint32_t (&w)[4], uint32_t allowed)
-    {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = allowed >> e & 1 ? w[e] : 0xff800000u;
-    }
-};
-template <>
-struct Lanes<__nv_bfloat16> {
-    static __device__ __forceinline__ void forbid(uint32_t (&w)[4], uint32_t allowed)
-    {
-        const uint32_t s[2] = {byte_signs(allowed), byte_signs(allowed >> 4)};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {       // a half of all ones where the element is allowed
-            uint32_t m;
-            asm("prmt.b32 %0, %1, %1, %2;" : "=r"(m) : "r"(s[e >> 1]), "r"(e & 1 ? 0xbbaa : 0x9988));    // signs of two bytes
-            w[e] = (w[e] & m) | (0xff80ff80u & ~m);
-        }
-    }
-};
-
-// n <= 8 bits of a bit row from bit `at` on (bits before 0 and behind `words` words read as zero)
-__device__ __forceinline__ uint32_t bits_at(const uint32_t *row, int at, int words)
-{
-    const int w = at >> 5;
-    const uint32_t lo = w >= 0 && w < words ? row[w] : 0u, hi = w + 1 >= 0 && w + 1 < words ? row[w + 1] : 0u;
-    return __funnelshift_r(lo, hi, at & 31);
-}
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint64_t *bar)
 {
@@ -117,7 +58,7 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
     using S = Stretch<T, BYTES>;
     constexpr int n = S::n, es = sizeof(T), kTokens = S::tokens, kWords = S::words, kRuleThreads = S::threads, kListed = 2 * kRuleThreads;
     extern __shared__ __align__(128) uint8_t sm[];
-    int *count = reinterpret_cast<int *>(sm + p.stages * BYTES);                      // [kTokens]; kOnPath: some node has the token
+    int *count = reinterpret_cast<int *>(sm + p.stages * BYTES);                      // [kTokens]; kRuleOnPath: some node has the token
     uint32_t *bias = reinterpret_cast<uint32_t *>(count + kTokens);                  // [kTokens] of 16 bits: 1 + the bias that counts
     float *bias_value = reinterpret_cast<float *>(bias + kTokens / 2);              // [n_bias]
     __shared__ uint64_t full[kMaxStages];
@@ -129,7 +70,7 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
     __shared__ int n_near, n_listed, abort;
 
     const int tid = threadIdx.x;
-    const int chunk = blockIdx.x % p.chunks, group = blockIdx.x / p.chunks % p.row_groups, b = blockIdx.x / p.chunks / p.row_groups;
+    const int chunk = blockIdx.x % p.pieces, group = blockIdx.x / p.pieces % p.row_groups, b = blockIdx.x / p.pieces / p.row_groups;
     const int TT = p.nodes.T, used = node_count(p.nodes, b);
     const int v0 = chunk * S::vecs;                     // the stretch's first vector
     const int first = v0 * n - n;                       // (n - 1 tokens would do; whole vectors are easier on the eye)
@@ -223,7 +164,7 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
     auto node_token = [&](int i, int t) {
         if (within(t)) {
             near[atomicAdd(&n_near, 1)] = i | (t - first) << 8;
-            atomicOr(&count[t - first], kOnPath);
+            atomicOr(&count[t - first], kRuleOnPath);
             touch(t - first);
         }
     };
@@ -259,12 +200,12 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
         const uint32_t i = p.n_bias ? bias[at >> 1] >> (16 * (at & 1)) & 0xffffu : 0u;
         return i ? make_float2(bias_value[i - 1], 1.f) : make_float2(0.f, 0.f);
     };
-    // the rules for one token of a row; c: its count with kOnPath, w: its bias and whether there is one
+    // the rules for one token of a row; c: its count with kRuleOnPath, w: its bias and whether there is one
     auto fix = [&](int at, int c, float2 w, int shift, int row, T *buf) {
         const int pos = at + first + shift;
         if (pos < 0 || pos >= S::vecs * n) return;
-        if (c & kOnPath) {
-            c &= ~kOnPath;
+        if (c & kRuleOnPath) {
+            c &= ~kRuleOnPath;
             for (int m = 0; m < nn; ++m)
                 if (near[m] >> 8 == at && on_path(near[m] & 255, row)) ++c;
         }
@@ -339,7 +280,7 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
                     uint4 *at = reinterpret_cast<uint4 *>(buf) + u * kRuleThreads + tid;
                     const uint4 a = *at;
                     uint32_t w[4] = {a.x, a.y, a.z, a.w};
-                    Lanes<T>::forbid(w, allowed[u]);
+                    RuleLanes<T>::forbid(w, allowed[u]);
                     *at = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
@@ -374,7 +315,7 @@ cudaError_t launch_rules(const RuleParams &p, unsigned ctas, cudaStream_t st)
         if (e != cudaSuccess) return e;
         if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
             e = cudaFuncSetAttribute(rules_kernel<T, BYTES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     (int)Stretch<T, BYTES>::smem(kMaxStages, kMaxBiases));
+                                     (int)Stretch<T, BYTES>::smem(kMaxStages, kRuleMaxBiases));
             if (e != cudaSuccess) return e;
             if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
         }
@@ -383,6 +324,11 @@ cudaError_t launch_rules(const RuleParams &p, unsigned ctas, cudaStream_t st)
     return cudaGetLastError();
 }
 
+// Few rows, and stretches of the vocabulary beyond what is resident at once, go to logits_rules_single.cu: a stretch's tables
+// take longer than its rows.  256x1 over 128256 entries 69 -> 33 us (history of 4000: 102 -> 55), 64x3 34 -> 24 us, 24x1
+// 10.3 -> 7.7 us; but 256x4 147 -> 149 us, and 64x1 over 32000 entries, 512 stretches, 7.0 -> 7.8 us.
+constexpr int kSingleRows = 3, kSingleStretches = 148 * 4;
+
 template <typename T>
 cudaError_t pick_rules(RuleParams &p, cudaStream_t st)
 {
@@ -390,14 +336,15 @@ cudaError_t pick_rules(RuleParams &p, cudaStream_t st)
     const int rows = p.nodes.T;
     auto chunks_of = [&](int bytes) { return (int)(((int64_t)p.V + n - 1 + bytes / sizeof(T) - 1) / (bytes / (int64_t)sizeof(T))); };
     const bool wide = (int64_t)p.B * chunks_of(kLong) >= 148 * 2;
-    p.chunks = chunks_of(wide ? kLong : kShort);
+    if (rows <= kSingleRows && (int64_t)p.B * chunks_of(kLong) >= kSingleStretches) return launch_rules_single<T>(p, st);
+    p.pieces = chunks_of(wide ? kLong : kShort);
     // few sequences: their rows are dealt out too
-    int64_t groups = 148 * 4 / ((int64_t)p.B * p.chunks);
+    int64_t groups = 148 * 4 / ((int64_t)p.B * p.pieces);
     groups = groups < 1 ? 1 : groups > rows ? rows : groups;
     p.rows_per_group = (int)((rows + groups - 1) / groups);
     p.stages = p.rows_per_group < kMaxStages ? p.rows_per_group : kMaxStages;
     p.row_groups = (rows + p.rows_per_group - 1) / p.rows_per_group;
-    const int64_t ctas = (int64_t)p.B * p.chunks * p.row_groups;
+    const int64_t ctas = (int64_t)p.B * p.pieces * p.row_groups;
     if (ctas > 0x7fffffff) return cudaErrorInvalidValue;
     return wide ? launch_rules<T, kLong>(p, (unsigned)ctas, st) : launch_rules<T, kShort>(p, (unsigned)ctas, st);
 }
@@ -415,7 +362,7 @@ extern "C" int logits_rules(const void *logits, int64_t ldv, int V, int B, int T
                             int64_t ld_out, void *ws, size_t ws_bytes, void *cuda_stream)
 {
     if (!dtype_ok(dt)) return SPR_ERR_UNSUPPORTED;
-    if (B < 0 || T < 0 || V <= 0 || V > 1 << 30 || ldv < V || ld_out < V || (int64_t)B * T > 0x7fffffff || n_bias < 0 || n_bias > kMaxBiases)
+    if (B < 0 || T < 0 || V <= 0 || V > 1 << 30 || ldv < V || ld_out < V || (int64_t)B * T > 0x7fffffff || n_bias < 0 || n_bias > kRuleMaxBiases)
         return SPR_ERR_INVALID_ARG;
     if (T > kMaxTreeNodes) return SPR_ERR_UNSUPPORTED;
     if (B == 0 || T == 0) return SPR_OK;

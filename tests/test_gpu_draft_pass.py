@@ -411,6 +411,19 @@ def test_rules_many_sequences(spr, dtype):
     check_rules(spr, x, dims)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=ids)
+@pytest.mark.parametrize("B,T,V,L,few", [(600, 1, 4000, 30, 1000), (40, 3, 70001, 900, 30000), (150, 2, 17001, 6000, 4250), (8, 1, 600007, 3000, 2900)])
+def test_rules_few_rows(spr, B, T, V, L, few, dtype):
+    """The form for few rows: long pieces of a row, in place and apart, off alignment, more touched tokens than its table holds."""
+    x, dims = rules_case(B, T, V, dtype, seed=44, ldv=V + 2, L=L, n_bias=300, masks=3, lead=1, tree=T > 1)
+    x["history"] = torch.randint(-1, few, (B, L), generator=torch.Generator().manual_seed(45)).to(torch.int32)
+    a = check_rules(spr, x, dims, inplace=True)
+    assert torch.equal(check_rules(spr, x, dims), a)
+    out = torch.full((B, T, V + 5), 7.0, dtype=dtype, device="cuda")          # rows that lie otherwise: one by one
+    run_rules(spr, x, dims, out=out)
+    assert torch.equal(out[..., :V].cpu(), a) and bool((out[..., V:] == 7.0).all())
+
+
 @pytest.mark.parametrize("without", ["penalties", "bias", "masks", "history", "tokens", "all"])
 def test_rules_each_is_optional(spr, without):
     x, dims = rules_case(2, 6, 3001, BF16, seed=45, tree=True)
