@@ -3,7 +3,7 @@
 // A warp walks its keys on its own, with a running maximum and sum: a lane holds E columns of all the block's queries
 // and of their results in registers, a key's row is one coalesced load, and the products of a key with the block's ROWS
 // queries are added up over the lanes by halves (half of the rows to the other half of the lanes, five times over), so
-// that ROWS scores cost some ROWS shuffles.  The four warps of a CTA take 16 keys of a tile each and are joined
+// that ROWS scores cost some ROWS shuffles.  The warps of a CTA share a tile's keys and are joined
 // through shared memory at the end of a part.  Up to 16 rows the loads bound it, above that the block is read again.
 #include "attention_plan.cuh"
 #include "host_util.h"
@@ -13,10 +13,10 @@ namespace spr {
 
 namespace {
 
-constexpr int kF32Threads = 128;
-constexpr int kF32Warps = kF32Threads / 32;
-constexpr int kKeys = kAttnTile / kF32Warps;    // of a tile, per warp
 constexpr int kGroup = 4;            // keys worked on at once
+// Warps of a CTA: eight where their registers leave room for two such CTAs on an SM, so that more loads are on their way
+template <int ROWS, int E>
+constexpr int kWarpsFor = ROWS * E <= 16 ? 8 : 4;
 
 template <int E>
 struct Cols {
@@ -37,8 +37,10 @@ struct Cols {
 };
 
 template <int ROWS, int E>
-__global__ void __launch_bounds__(kF32Threads, 2) attention_f32_kernel(const AttnParams p)
+__global__ void __launch_bounds__(32 * kWarpsFor<ROWS, E>, 2) attention_f32_kernel(const AttnParams p)
 {
+    constexpr int kF32Warps = kWarpsFor<ROWS, E>, kF32Threads = 32 * kF32Warps;
+    constexpr int kKeys = kAttnTile / kF32Warps;    // of a tile, per warp
     constexpr int kLanes = 32 / ROWS;               // lanes that share a row's score
     __shared__ int scratch[kF32Warps + 2];
     __shared__ int tree[kMaxTreeNodes];
@@ -107,6 +109,7 @@ __global__ void __launch_bounds__(kF32Threads, 2) attention_f32_kernel(const Att
             float sc[kGroup];
             uint32_t seen[kGroup];
             const int slot0 = tile * kAttnTile + warp * kKeys + group * kGroup;
+            if (slot0 >= keys) return;
 #pragma unroll
             for (int j = 0; j < kGroup; ++j) {
                 float x[ROWS];
@@ -235,8 +238,9 @@ __global__ void __launch_bounds__(kF32Threads, 2) attention_f32_kernel(const Att
 template <int ROWS, int E>
 cudaError_t launch_rows(const AttnParams &p, cudaStream_t st)
 {
-    const size_t smem = sizeof(float) * kF32Warps * ROWS * p.D;      // 32 KB at most
-    attention_f32_kernel<ROWS, E><<<p.ctas, kF32Threads, smem, st>>>(p);
+    constexpr int warps = kWarpsFor<ROWS, E>;
+    const size_t smem = sizeof(float) * warps * ROWS * p.D;      // 32 KB at most
+    attention_f32_kernel<ROWS, E><<<p.ctas, 32 * warps, smem, st>>>(p);
     return cudaGetLastError();
 }
 

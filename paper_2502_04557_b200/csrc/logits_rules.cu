@@ -9,7 +9,7 @@
 // Bound by memory: a row is read and written once.  A CTA has one stretch of the vocabulary of one sequence, for a run of
 // its rows, which go through a ring in shared memory by bulk copies.  The stretch's counts and biases are gathered into tables
 // once (history and biases are read by every stretch, from L2), with integer atomics, so that their order does not matter.
-// Nearly all tokens are touched by neither: those that are stand in a list, one or two to a thread, and are put right in the
+// Nearly all tokens are touched by neither: those that are stand in a list, up to four to a thread (or are looked for), and are put right in the
 // ring; masks are applied there to vectors, with their bits read a row ahead.  Rows by 8 KB for many sequences, 4 KB for few.
 // 256 x 17 rows of 128256 bf16 entries, a quarter masked: 423 us, 5.3 TB/s (no masks 387, 5.8).  More rows in the ring take
 // CTAs from the SM (4 stages 490 us), two leave the copies too little (508 us).
@@ -56,7 +56,7 @@ template <typename T, int BYTES>
 __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const RuleParams p)
 {
     using S = Stretch<T, BYTES>;
-    constexpr int n = S::n, es = sizeof(T), kTokens = S::tokens, kWords = S::words, kRuleThreads = S::threads, kListed = 2 * kRuleThreads;
+    constexpr int n = S::n, es = sizeof(T), kTokens = S::tokens, kWords = S::words, kRuleThreads = S::threads, kListed = 4 * kRuleThreads;
     extern __shared__ __align__(128) uint8_t sm[];
     int *count = reinterpret_cast<int *>(sm + p.stages * BYTES);                      // [kTokens]; kRuleOnPath: some node has the token
     uint32_t *bias = reinterpret_cast<uint32_t *>(count + kTokens);                  // [kTokens] of 16 bits: 1 + the bias that counts
@@ -262,16 +262,13 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
         if (rules) {
             if (nl <= kListed) {
                 if (tid < nl) fix(mine_at, mine_count, mine_bias, shift, row, buf);
-                if (tid + kRuleThreads < nl) {
-                    const int at = listed[tid + kRuleThreads];
+                for (int k = tid + kRuleThreads; k < nl; k += kRuleThreads) {
+                    const int at = listed[k];
                     fix(at, count[at], bias_of(at), shift, row, buf);
                 }
             } else {
-                for (int k = tid; k < kWords; k += kRuleThreads)
-                    for (uint32_t left = touched[k]; left; left &= left - 1) {
-                        const int at = 32 * k + __ffs(left) - 1;
-                        fix(at, count[at], bias_of(at), shift, row, buf);
-                    }
+                for (int at = tid; at < kTokens; at += kRuleThreads)
+                    if (touched[at >> 5] >> (at & 31) & 1) fix(at, count[at], bias_of(at), shift, row, buf);
             }
             if (mask_of[row] >= 0) {
                 __syncthreads();
