@@ -49,7 +49,10 @@ struct Stretch {
     static constexpr int tokens = vecs * n + n;         // tokens first .. first + tokens - 1 can be met
     static constexpr int words = (tokens + 31) / 32;
     static constexpr int threads = BYTES / 32;          // two vectors each
-    static size_t smem(int stages, int biases) { return (size_t)stages * BYTES + tokens * 4 + (biases ? tokens * 2 + 4 * biases : 0); }
+    static size_t smem(int stages, int biases, int nodes)      // nodes of a tree
+    {
+        return (size_t)stages * BYTES + tokens * 4 + (biases ? tokens * 2 + 4 * biases : 0) + (nodes + 31) / 32 * nodes * 4;
+    }
 };
 
 template <typename T, int BYTES>
@@ -61,6 +64,9 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
     int *count = reinterpret_cast<int *>(sm + p.stages * BYTES);                      // [kTokens]; kRuleOnPath: some node has the token
     uint32_t *bias = reinterpret_cast<uint32_t *>(count + kTokens);                  // [kTokens] of 16 bits: 1 + the bias that counts
     float *bias_value = reinterpret_cast<float *>(bias + kTokens / 2);              // [n_bias]
+    // [T][path_words]: a bit for each node on a node's path, where there is a tree
+    uint32_t *path = p.n_bias ? reinterpret_cast<uint32_t *>(bias_value + p.n_bias) : bias;
+    const int path_words = (p.nodes.T + 31) / 32;
     __shared__ uint64_t full[kMaxStages];
     __shared__ uint16_t listed[kListed];                // touched tokens, in any order
     __shared__ uint32_t touched[kWords];
@@ -140,6 +146,11 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
         mask_of[i] = m;
     }
     __syncthreads();
+    if (p.nodes.parents)
+        for (int i = tid; i < used; i += kRuleThreads) {
+            for (int w = 0; w < path_words; ++w) path[i * path_words + w] = 0;
+            for (int j = i; j >= 0; j = checked_parent(tree[j], j, p.status)) path[i * path_words + (j >> 5)] |= 1u << (j & 31);
+        }
 
     auto within = [&](int t) {
         if (t >= p.V && chunk == 0) raise_status(p.status, SPR_ERR_BAD_TOKEN);
@@ -190,11 +201,7 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
     const int mask_words = (p.V + 31) / 32;
 
     // whether node j is node i or on its path
-    auto on_path = [&](int j, int i) {
-        if (!p.nodes.parents) return j <= i;
-        while (i > j) i = checked_parent(tree[i], i, p.status);
-        return i == j;
-    };
+    auto on_path = [&](int j, int i) { return p.nodes.parents ? (path[i * path_words + (j >> 5)] >> (j & 31) & 1) != 0 : j <= i; };
 
     auto bias_of = [&](int at) {
         const uint32_t i = p.n_bias ? bias[at >> 1] >> (16 * (at & 1)) & 0xffffu : 0u;
@@ -304,7 +311,7 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
 template <typename T, int BYTES>
 cudaError_t launch_rules(const RuleParams &p, unsigned ctas, cudaStream_t st)
 {
-    const size_t smem = Stretch<T, BYTES>::smem(p.stages, p.n_bias);
+    const size_t smem = Stretch<T, BYTES>::smem(p.stages, p.n_bias, p.nodes.parents ? p.nodes.T : 0);
     if (smem > 40000) {
         static std::atomic<bool> attr_set[64];   // host threads may race to set it: all of them store `true`
         int dev = 0;
@@ -312,7 +319,7 @@ cudaError_t launch_rules(const RuleParams &p, unsigned ctas, cudaStream_t st)
         if (e != cudaSuccess) return e;
         if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
             e = cudaFuncSetAttribute(rules_kernel<T, BYTES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     (int)Stretch<T, BYTES>::smem(kMaxStages, kRuleMaxBiases));
+                                     (int)Stretch<T, BYTES>::smem(kMaxStages, kRuleMaxBiases, kMaxTreeNodes));
             if (e != cudaSuccess) return e;
             if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
         }
