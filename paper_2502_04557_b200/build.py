@@ -12,7 +12,7 @@ LIB = os.path.join(PKG, "libsprinter.so")
 SOURCES = ["api.cu", "host_api.cu", "sd_row_stats.cu", "draw.cu", "verifier_simt.cu", "verifier_tensor.cu", "no_alloc.cu", "simulate.cu", "sd_shard.cu", "sd_shard_api.cu", "verifier_fit.cu",
            "head_gemm.cu", "head_loss.cu", "hidden_pack.cu", "verifier_fit8.cu", "head_small.cu", "head_stream.cu",
            "cache_append.cu", "logits_rules.cu", "logits_rules_single.cu", "tree_attention.cu",
-           "attention_f32.cu", "attention_mma.cu", "attention_tc.cu"]
+           "attention_f32.cu", "attention_f32_tile.cu", "attention_mma.cu", "attention_tc.cu"]
 HEADERS = ["common.cuh", "launch.h", "verifier_common.cuh", "vocab_common.cuh", "draw_common.cuh", "host_util.h",
            "tensor_pair.cuh", "head_gemm.h", "head_small.h", "head_stream.h",
            "draft_tree.cuh", "rules.cuh", "attention.h", "attention_plan.cuh"]

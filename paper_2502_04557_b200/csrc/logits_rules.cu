@@ -339,7 +339,7 @@ cudaError_t pick_rules(RuleParams &p, cudaStream_t st)
     constexpr int n = 16 / sizeof(T), kLong = 8192, kShort = 4096;
     const int rows = p.nodes.T;
     auto chunks_of = [&](int bytes) { return (int)(((int64_t)p.V + n - 1 + bytes / sizeof(T) - 1) / (bytes / (int64_t)sizeof(T))); };
-    const bool wide = (int64_t)p.B * chunks_of(kLong) >= 148 * 2;
+    const bool wide = (int64_t)p.B * chunks_of(kLong) >= 148 * 4;
     if (rows <= kSingleRows && (int64_t)p.B * chunks_of(kLong) >= kSingleStretches) return launch_rules_single<T>(p, st);
     p.pieces = chunks_of(wide ? kLong : kShort);
     // few sequences: their rows are dealt out too

@@ -11,7 +11,7 @@ namespace spr {
 namespace {
 
 // most rows of a row block, for the workspace
-int most_rows(int dt) { return dt == SPR_F32 ? 16 : 128; }
+int most_rows(int dt) { return dt == SPR_F32 ? 64 : 128; }
 
 thread_local int t_test_flags = 0;
 thread_local unsigned t_spin_limit = 0;
@@ -21,7 +21,7 @@ thread_local unsigned t_spin_limit = 0;
 int attention_block_rows(int T, int G, int dt)
 {
     const int64_t rows = (int64_t)T * G;
-    if (dt == SPR_F32) return rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
+    if (dt == SPR_F32) return rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 16 ? 16 : 64;
     return rows <= 16 ? 16 : 128;
 }
 
@@ -78,7 +78,7 @@ int tree_attention(const void *q, const void *k_cache, const void *v_cache, int 
     p.scale_log2 = scale * kLog2e;
     p.abs_scale_log2 = fmaxf(fabsf(p.scale_log2), 1e-37f);
     p.flip = scale < 0.f ? 0x80008000u : 0u;
-    const int per_sm = rows == 128 ? 1 : kAttnCtasPerSm;
+    const int per_sm = rows > 16 ? 1 : kAttnCtasPerSm;
     p.ctas = sms < 148 ? sms * per_sm : 148 * per_sm;
     p.status = static_cast<int *>(ws);
     p.counters = at<int>(ws, w.counters);
@@ -87,7 +87,7 @@ int tree_attention(const void *q, const void *k_cache, const void *v_cache, int 
     p.spin_limit = t_spin_limit ? t_spin_limit : pairtc::kSpinLimit;
     p.test_flags = t_test_flags;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == SPR_F32) return finish(launch_attention_f32(p, rows, st));
+    if (dt == SPR_F32) return finish(rows > 16 ? launch_attention_f32_tile(p, dev, st) : launch_attention_f32(p, rows, st));
     return finish(rows == 16 ? launch_attention_mma(p, dev, st) : launch_attention_tc(p, dev, st));
 }
 
