@@ -457,8 +457,11 @@ int cache_append(const void *q, int64_t q_stride, const void *k, int64_t k_strid
  * s running over the slots of the prefix, [0, lens[b]), and those of node i and the nodes before it on its path; head h reads
  * head h / (Hq / Hkv) of the cache.  T = 1 is ordinary decoding.
  * q, out [B,T,Hq,D] dt (dense, 16-byte aligned, as are the caches); Hkv divides Hq; D a multiple of 8 up to 128 and
- * page_size a multiple of 8 (otherwise SPR_ERR_UNSUPPORTED), T <= 256.  Rows of nodes that are not used are zeros.
- * Scores, maxima and sums are fp32; with bf16 tensors the weights enter the second product as two bf16 numbers.
+ * page_size a multiple of 8, T <= 256, num_pages * Hkv * page_size and B * T below 2^31, and no more than 2^31 tiles of 64 slots
+ * in all that page_table could name, each counted for every cached head and block of queries (otherwise SPR_ERR_UNSUPPORTED).
+ * Rows of nodes that are not used are zeros.
+ * Scores, maxima and sums are fp32.  With bf16 tensors the weights enter the second product as two bf16 numbers where a cached
+ * head has up to 16 queries (T * Hq / Hkv), and rounded to one where it has more.
  * Keys and values of slots that a row does not see have no part in it, whatever they hold; infinities and NaN in
  * those that it does see make it infinite or NaN.  A slot without a page is left out (SPR_ERR_BAD_PAGE), and a row
  * that sees no slot at all is zeros.  After SPR_ERR_TIMEOUT rows whose keys did not arrive are NaN.
@@ -486,7 +489,7 @@ int tree_attention(const void *q, const void *k_cache, const void *v_cache, int 
  * n_bias <= 1024.
  * masks [num_masks,ld_mask] (ld_mask >= ceil(V/32)) with mask_rows [B,T] int32, negative: no mask.  Negative entries of
  * history, tokens and bias_tokens are padding.
- * out [B,T,ld_out] dt: logits itself (ld_out = ldv), or not overlapping it.  A row whose mask allows nothing is -inf throughout.
+ * out [B,T,ld_out] dt: logits itself (then ld_out = ldv), or not overlapping it.  A row whose mask allows nothing is -inf throughout.
  * Device-detected: history, tokens or bias_tokens >= V are passed over, SPR_ERR_BAD_TOKEN; mask_rows >= num_masks: no mask,
  * SPR_ERR_BAD_ROW.  T <= 256.  Workspace: the status word.
  */

@@ -1,13 +1,16 @@
 // tree_attention on bf16 tensors, few rows per cached head (decoding, chains).
 //
 // out_i = sum_j softmax_j(scale q_i . k_j) v_j in one pass over the keys, with a running maximum and sum.  Bound by the
-// read of the caches: a key and its value (4 D bytes) meet ROWS queries.  Each of a CTA's four warps takes 16 keys of
-// every tile of 64, which it brings into a ring of its own (cp.async, 16 bytes per
-// lane, three to five steps ahead) and works on alone: it has its own maxima, sums and results (mma.sync m16n8k16, the
-// block's rows as M), and warps meet only at the end of a part, behind which the SM's other CTA goes on.  Copies by lanes take pages as they come: the copy
-// engine's boxes of a page of 16 entries are 2 KB each, and their number, not their bytes, sets the time (64 sequences
-// of 4096 tokens, 8 heads of 128: 195 us with such boxes).  mma.sync suffices here: at 16 rows a tile of 32 KB (the time of
-// 1400 clocks at the memory's rate) takes 128 products per tensor core, some 300 clocks; tcgen05's smallest tile has 64 rows.
+// read of the caches: a key and its value (4 D bytes) meet ROWS queries.  Each of a CTA's four warps takes 16 keys of every
+// tile of 64, which it brings into a ring of its own (cp.async, 16 bytes per lane, three to five steps ahead) and works on
+// alone: it has its own maxima, sums and results (mma.sync m16n8k16, the block's rows as M), and warps meet only at the end of
+// a part, behind which the SM's other CTA goes on.  Copies by lanes take pages as they come: the copy engine's boxes of a
+// page of 16 entries are 2 KB each, and their number, not their bytes, sets the time (64 sequences of 4096 tokens, 8 heads
+// of 128: 195 us with such boxes).  mma.sync suffices here: at 16 rows a tile of 32 KB (the time of 1400 clocks at the memory's
+// rate) takes 128 products per tensor core, some 300 clocks; tcgen05's smallest tile has 64 rows.
+//
+// 64 sequences of some 3000 tokens, 32/8 heads of 128: 133 us, 6.1 TB/s; one of 131072: 104 us; one of
+// 300: 11 us, the length of the chain from the plan to the join.
 //
 // Weights are used as two bf16 numbers (their rounding and what is left of it): with one, results would be off by 2^-9
 // of themselves for that alone, as much as by their own rounding.  The second product is free where the
@@ -43,8 +46,8 @@ struct MmaShape {
 struct MmaControl {
     int scratch[kMmaWarps + 2];
     int tree[kMaxTreeNodes];
-    uint32_t path[32][kMaxTreeNodes / 32];
-    float2 ml[kMmaWarps][32];
+    uint32_t path[16][kMaxTreeNodes / 32];
+    float2 ml[kMmaWarps][16];
     uint32_t valid[kMmaWarps][5];           // a bit for each key of a warp's step that is there
     int last;
 };
@@ -84,7 +87,7 @@ __device__ __forceinline__ bool finite_bf16x2(uint32_t w) { return (w & 0x7f80u)
 template <int PANELS, bool WHOLE>
 __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const AttnParams p)
 {
-    constexpr int MT = 1, ROWS = 16 * MT, KSTEPS = 4 * PANELS, NTILES = 8 * PANELS;
+    constexpr int ROWS = 16, KSTEPS = 4 * PANELS, NTILES = 8 * PANELS;
     using Shape = MmaShape<PANELS>;
     extern __shared__ __align__(1024) uint8_t raw[];
     __shared__ MmaControl ctl;
@@ -183,24 +186,22 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
     const int quad = lane >> 2, pair = lane & 3;
     // a part's queries as A fragments: rows quad and quad + 8 of each row tile.  They are asked for while what comes before
     // the part is still going on.
-    uint32_t qf[MT][KSTEPS][4];
+    uint32_t qf[KSTEPS][4];
     auto load_queries = [&](const AttnStretch &s, const AttnPart &part) {
         const int row0 = part.block * ROWS, rows = s.seq.count * p.G - row0;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int h = 0; h < 2; ++h) {
+            const int r = h * 8 + quad;
+            const bool in = r < rows;
+            const uint32_t *src = reinterpret_cast<const uint32_t *>(static_cast<const __nv_bfloat16 *>(p.q) + (in ? attn_out_at(p, s, part, row0 + r) : 0));
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = mt * 16 + h * 8 + quad;
-                const bool in = r < rows;
-                const uint32_t *src = reinterpret_cast<const uint32_t *>(static_cast<const __nv_bfloat16 *>(p.q) + (in ? attn_out_at(p, s, part, row0 + r) : 0));
+            for (int k = 0; k < KSTEPS; ++k)
 #pragma unroll
-                for (int k = 0; k < KSTEPS; ++k)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const int col = k * 16 + c * 8 + pair * 2;
-                        qf[mt][k][c * 2 + h] = in && col < p.D ? __ldg(src + col / 2) : 0u;
-                    }
-            }
+                for (int c = 0; c < 2; ++c) {
+                    const int col = k * 16 + c * 8 + pair * 2;
+                    qf[k][c * 2 + h] = in && col < p.D ? __ldg(src + col / 2) : 0u;
+                }
+        }
     };
     AttnPart part;
     int tree_of = -1, stage = 0;
@@ -222,32 +223,25 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
         if (holds_nodes && tid < nodes)
             attn_path_bits(p.nodes.parents ? ctl.tree : nullptr, i0 + tid, ctl.path[tid], (s.seq.count + 31) / 32, p.status);
 
-        int node[MT][2];
+        int node[2];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = mt * 16 + h * 8 + quad;
-                node[mt][h] = r < t.rows ? (t.row0 + r) / p.G - i0 : 0;
-            }
+        for (int h = 0; h < 2; ++h) {
+            const int r = h * 8 + quad;
+            node[h] = r < t.rows ? (t.row0 + r) / p.G - i0 : 0;
+        }
         if (p.flip) {
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int k = 0; k < KSTEPS; ++k)
 #pragma unroll
-                for (int k = 0; k < KSTEPS; ++k)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) qf[mt][k][c] ^= p.flip;
+                for (int c = 0; c < 4; ++c) qf[k][c] ^= p.flip;
         }
         __syncthreads();
 
-        float o[MT][NTILES][4], m[MT][2], l[MT][2];
+        float o[NTILES][4], m[2], l[2];
+        m[0] = m[1] = neg_inf();
+        l[0] = l[1] = 0.f;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            m[mt][0] = m[mt][1] = neg_inf();
-            l[mt][0] = l[mt][1] = 0.f;
-#pragma unroll
-            for (int n = 0; n < NTILES; ++n) o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.f;
-        }
+        for (int n = 0; n < NTILES; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
         for (int n = 0; n < part.n; ++n) {
             copies_wait<Shape::stages - 1>();
             __syncwarp();
@@ -256,20 +250,15 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
             const int slot0 = (part.t0 + n) * kAttnTile + w16;
             const bool all = valid == 0xffffu && slot0 + 16 <= s.seq.len;
 
-            float sc[MT][2][4];
+            float sc[2][4];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) sc[mt][h][0] = sc[mt][h][1] = sc[mt][h][2] = sc[mt][h][3] = 0.f;
+            for (int h = 0; h < 2; ++h) sc[h][0] = sc[h][1] = sc[h][2] = sc[h][3] = 0.f;
 #pragma unroll
             for (int k = 0; k < KSTEPS; ++k) {
                 uint32_t b[4];
                 ldsm(base + k_off + (((k * 2 + k_chunk) ^ swz) << 4), b);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    mma(sc[mt][0], qf[mt][k], b[0], b[1]);
-                    mma(sc[mt][1], qf[mt][k], b[2], b[3]);
-                }
+                mma(sc[0], qf[k], b[0], b[1]);
+                mma(sc[1], qf[k], b[2], b[3]);
             }
             uint32_t odd = 0;               // keys whose values hold infinities or NaN, where not every row sees every key
             if (!all) {
@@ -285,76 +274,71 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
                 odd = __ballot_sync(0xffffffffu, bad);
                 odd = (odd | odd >> 16) & 0xffffu;
             }
+            // c registers 0, 1: row quad, keys 2 pair, 2 pair + 1; 2, 3: row quad + 8
+            if (!all) {
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                // c registers 0, 1: row quad, keys 2 pair, 2 pair + 1; 2, 3: row quad + 8
-                if (!all) {
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                    for (int c = 0; c < 4; ++c) {
+                        const int key = h * 8 + pair * 2 + (c & 1);
+                        const int j = slot0 + key - s.seq.len;
+                        const bool vis = (valid >> key & 1) && (j < 0 || (ctl.path[node[c >> 1]][j >> 5] >> (j & 31) & 1));
+                        if (!vis) sc[h][c] = neg_inf();
+                    }
+            }
+            float top[2];
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const int key = h * 8 + pair * 2 + (c & 1);
-                            const int j = slot0 + key - s.seq.len;
-                            const bool vis = (valid >> key & 1) && (j < 0 || (ctl.path[node[mt][c >> 1]][j >> 5] >> (j & 31) & 1));
-                            if (!vis) sc[mt][h][c] = neg_inf();
-                        }
-                }
-                float top[2];
+            for (int g = 0; g < 2; ++g) {
+                float x = fmaxf(fmaxf(sc[0][2 * g], sc[0][2 * g + 1]), fmaxf(sc[1][2 * g], sc[1][2 * g + 1]));
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+                top[g] = fmaxf(x, m[g]);
+            }
+            if (__any_sync(0xffffffffu, top[0] > m[0] || top[1] > m[1])) {
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
-                    float x = fmaxf(fmaxf(sc[mt][0][2 * g], sc[mt][0][2 * g + 1]), fmaxf(sc[mt][1][2 * g], sc[mt][1][2 * g + 1]));
-                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-                    top[g] = fmaxf(x, m[mt][g]);
-                }
-                if (__any_sync(0xffffffffu, top[0] > m[mt][0] || top[1] > m[mt][1])) {
+                    const float a = ex2((m[g] - (top[g] == neg_inf() ? 0.f : top[g])) * p.abs_scale_log2);
+                    m[g] = top[g];
+                    l[g] *= a;
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        const float a = ex2((m[mt][g] - (top[g] == neg_inf() ? 0.f : top[g])) * p.abs_scale_log2);
-                        m[mt][g] = top[g];
-                        l[mt][g] *= a;
-#pragma unroll
-                        for (int i = 0; i < NTILES; ++i) {
-                            o[mt][i][2 * g] *= a;
-                            o[mt][i][2 * g + 1] *= a;
-                        }
+                    for (int i = 0; i < NTILES; ++i) {
+                        o[i][2 * g] *= a;
+                        o[i][2 * g + 1] *= a;
                     }
                 }
+            }
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const float ref = m[mt][g] == neg_inf() ? 0.f : -m[mt][g] * p.abs_scale_log2;
+            for (int g = 0; g < 2; ++g) {
+                const float ref = m[g] == neg_inf() ? 0.f : -m[g] * p.abs_scale_log2;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            const float w = ex2(fmaf(sc[mt][h][2 * g + c], p.abs_scale_log2, ref));
-                            sc[mt][h][2 * g + c] = w;
-                            l[mt][g] += w;
-                        }
-                }
+                    for (int c = 0; c < 2; ++c) {
+                        const float w = ex2(fmaf(sc[h][2 * g + c], p.abs_scale_log2, ref));
+                        sc[h][2 * g + c] = w;
+                        l[g] += w;
+                    }
             }
             if (odd) {
                 for (int key = 0; key < 16; ++key) {
                     if (!(odd >> key & 1)) continue;
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
+                    for (int g = 0; g < 2; ++g) {
+                        const int h = key >> 3, c = key & 1, from = (lane & 28) | ((key & 7) >> 1);
+                        const float w0 = h ? sc[1][2 * g] : sc[0][2 * g], w1 = h ? sc[1][2 * g + 1] : sc[0][2 * g + 1];
+                        const float w = __shfl_sync(0xffffffffu, c ? w1 : w0, from);
+                        const int j = slot0 + key - s.seq.len;
+                        if (j < 0 || (ctl.path[node[g]][j >> 5] >> (j & 31) & 1)) {
 #pragma unroll
-                        for (int g = 0; g < 2; ++g) {
-                            const int h = key >> 3, c = key & 1, from = (lane & 28) | ((key & 7) >> 1);
-                            const float w0 = h ? sc[mt][1][2 * g] : sc[mt][0][2 * g], w1 = h ? sc[mt][1][2 * g + 1] : sc[mt][0][2 * g + 1];
-                            const float w = __shfl_sync(0xffffffffu, c ? w1 : w0, from);
-                            const int j = slot0 + key - s.seq.len;
-                            if (j < 0 || (ctl.path[node[mt][g]][j >> 5] >> (j & 31) & 1)) {
-#pragma unroll
-                                for (int i = 0; i < NTILES; ++i) {
-                                    const uint32_t a = base + (16 + key) * Shape::row + ((i ^ (key & 7)) << 4) + pair * 4;
-                                    uint32_t x;
-                                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(a) : "memory");
-                                    o[mt][i][2 * g] = fmaf(w, __uint_as_float(x << 16), o[mt][i][2 * g]);
-                                    o[mt][i][2 * g + 1] = fmaf(w, __uint_as_float(x & 0xffff0000u), o[mt][i][2 * g + 1]);
-                                }
+                            for (int i = 0; i < NTILES; ++i) {
+                                const uint32_t a = base + (16 + key) * Shape::row + ((i ^ (key & 7)) << 4) + pair * 4;
+                                uint32_t x;
+                                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(a) : "memory");
+                                o[i][2 * g] = fmaf(w, __uint_as_float(x << 16), o[i][2 * g]);
+                                o[i][2 * g + 1] = fmaf(w, __uint_as_float(x & 0xffff0000u), o[i][2 * g + 1]);
                             }
                         }
+                    }
                 }
                 __syncwarp();
                 if (odd >> (lane & 15) & 1)
@@ -363,29 +347,24 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
                 __syncwarp();
             }
             // weights as A fragments, in two parts
-            uint32_t hi[MT][4], lo[MT][4];
+            uint32_t hi[4], lo[4];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        const float a = sc[mt][h][2 * g], b = sc[mt][h][2 * g + 1];
-                        const uint32_t w = pack_bf16(a, b);
-                        hi[mt][h * 2 + g] = w;
-                        lo[mt][h * 2 + g] = pack_bf16(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
-                    }
+                for (int g = 0; g < 2; ++g) {
+                    const float a = sc[h][2 * g], b = sc[h][2 * g + 1];
+                    const uint32_t w = pack_bf16(a, b);
+                    hi[h * 2 + g] = w;
+                    lo[h * 2 + g] = pack_bf16(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
+                }
 #pragma unroll
             for (int i = 0; i < NTILES / 2; ++i) {
                 uint32_t b[4];
                 ldsm_t(base + v_off + (((i * 2 + v_chunk) ^ swz) << 4), b);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    mma(o[mt][2 * i], hi[mt], b[0], b[1]);
-                    mma(o[mt][2 * i + 1], hi[mt], b[2], b[3]);
-                    mma(o[mt][2 * i], lo[mt], b[0], b[1]);
-                    mma(o[mt][2 * i + 1], lo[mt], b[2], b[3]);
-                }
+                mma(o[2 * i], hi, b[0], b[1]);
+                mma(o[2 * i + 1], hi, b[2], b[3]);
+                mma(o[2 * i], lo, b[0], b[1]);
+                mma(o[2 * i + 1], lo, b[2], b[3]);
             }
             __syncwarp();
             issue();
@@ -399,67 +378,62 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
 
         // ------------------------------------------------------------ the warps' results joined
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                float x = l[mt][g];
-                x += __shfl_xor_sync(0xffffffffu, x, 1);
-                x += __shfl_xor_sync(0xffffffffu, x, 2);
-                if (pair == 0) ctl.ml[warp][mt * 16 + g * 8 + quad] = make_float2(m[mt][g] * p.abs_scale_log2, x);
-            }
+        for (int g = 0; g < 2; ++g) {
+            float x = l[g];
+            x += __shfl_xor_sync(0xffffffffu, x, 1);
+            x += __shfl_xor_sync(0xffffffffu, x, 2);
+            if (pair == 0) ctl.ml[warp][g * 8 + quad] = make_float2(m[g] * p.abs_scale_log2, x);
+        }
         __syncthreads();
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
+        for (int g = 0; g < 2; ++g) {
+            float top = neg_inf();
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                float top = neg_inf();
+            for (int w = 0; w < kMmaWarps; ++w) top = fmaxf(top, ctl.ml[w][g * 8 + quad].x);
+            const float a = ex2(m[g] * p.abs_scale_log2 - (top == neg_inf() ? 0.f : top));
 #pragma unroll
-                for (int w = 0; w < kMmaWarps; ++w) top = fmaxf(top, ctl.ml[w][mt * 16 + g * 8 + quad].x);
-                const float a = ex2(m[mt][g] * p.abs_scale_log2 - (top == neg_inf() ? 0.f : top));
-#pragma unroll
-                for (int i = 0; i < NTILES; ++i) {
-                    o[mt][i][2 * g] *= a;
-                    o[mt][i][2 * g + 1] *= a;
-                }
+            for (int i = 0; i < NTILES; ++i) {
+                o[i][2 * g] *= a;
+                o[i][2 * g + 1] *= a;
             }
-            const int row = tid >> 3, c4 = (tid & 7) * 4;       // what this thread adds up
-            float tall = neg_inf(), sum = 0.f;
+        }
+        const int row = tid >> 3, c4 = (tid & 7) * 4;       // what this thread adds up
+        float tall = neg_inf(), sum = 0.f;
 #pragma unroll
-            for (int w = 0; w < kMmaWarps; ++w) tall = fmaxf(tall, ctl.ml[w][mt * 16 + row].x);
+        for (int w = 0; w < kMmaWarps; ++w) tall = fmaxf(tall, ctl.ml[w][row].x);
+#pragma unroll
+        for (int w = 0; w < kMmaWarps; ++w) {
+            const float2 x = ctl.ml[w][row];
+            sum = fmaf(ex2(x.x - (tall == neg_inf() ? 0.f : tall)), x.y, sum);
+        }
+        const int r = row;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const int64_t out_at = r < t.rows ? attn_out_at(p, s, part, t.row0 + r) : 0;
+#pragma unroll
+        for (int h = 0; h < 2 * PANELS; ++h) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+                    *reinterpret_cast<float2 *>(join + (warp * 16 + g * 8 + quad) * kJoinPitch + i * 8 + pair * 2) =
+                        make_float2(o[h * 4 + i][2 * g], o[h * 4 + i][2 * g + 1]);
+            __syncthreads();
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < kMmaWarps; ++w) {
-                const float2 x = ctl.ml[w][mt * 16 + row];
-                sum = fmaf(ex2(x.x - (tall == neg_inf() ? 0.f : tall)), x.y, sum);
+                const float4 x = *reinterpret_cast<const float4 *>(join + (w * 16 + row) * kJoinPitch + c4);
+                y.x += x.x, y.y += x.y, y.z += x.z, y.w += x.w;
             }
-            const int r = mt * 16 + row;
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            const int64_t out_at = r < t.rows ? attn_out_at(p, s, part, t.row0 + r) : 0;
-#pragma unroll
-            for (int h = 0; h < 2 * PANELS; ++h) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int g = 0; g < 2; ++g)
-                        *reinterpret_cast<float2 *>(join + (warp * 16 + g * 8 + quad) * kJoinPitch + i * 8 + pair * 2) =
-                            make_float2(o[mt][h * 4 + i][2 * g], o[mt][h * 4 + i][2 * g + 1]);
-                __syncthreads();
-                float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int w = 0; w < kMmaWarps; ++w) {
-                    const float4 x = *reinterpret_cast<const float4 *>(join + (w * 16 + row) * kJoinPitch + c4);
-                    y.x += x.x, y.y += x.y, y.z += x.z, y.w += x.w;
+            const int c = h * kJoinCols + c4;
+            if (r < t.rows && c < p.D) {
+                if (t.whole) {
+                    store_out(static_cast<__nv_bfloat16 *>(p.out) + out_at + c, make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv), 4);
+                } else {
+                    __stcg(reinterpret_cast<float4 *>(p.part + ((int64_t)t.slot * ROWS + r) * p.D + c), y);
+                    if (c == 0) __stcg(&p.part_ml[(int64_t)t.slot * ROWS + r], make_float2(tall, sum));
                 }
-                const int c = h * kJoinCols + c4;
-                if (r < t.rows && c < p.D) {
-                    if (t.whole) {
-                        store_out(static_cast<__nv_bfloat16 *>(p.out) + out_at + c, make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv), 4);
-                    } else {
-                        __stcg(reinterpret_cast<float4 *>(p.part + ((int64_t)t.slot * ROWS + r) * p.D + c), y);
-                        if (c == 0) __stcg(&p.part_ml[(int64_t)t.slot * ROWS + r], make_float2(tall, sum));
-                    }
-                }
-                __syncthreads();
             }
+            __syncthreads();
         }
         if (!t.whole) {
             __syncthreads();

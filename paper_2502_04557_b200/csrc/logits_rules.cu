@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
         for (int i = tid; i < kTokens / 2; i += kRuleThreads) bias[i] = 0;
     for (int i = tid; i < kWords; i += kRuleThreads) touched[i] = 0;
     if (p.nodes.parents)
-        for (int i = tid; i < TT; i += kRuleThreads) tree[i] = p.nodes.parents[(int64_t)b * TT + i];
+        for (int i = tid; i < used; i += kRuleThreads) tree[i] = checked_parent(__ldg(p.nodes.parents + (int64_t)b * TT + i), i, p.status);
     for (int i = row0 + tid; i < row1; i += kRuleThreads) {
         int m = p.masks && i < used ? __ldg(p.mask_rows + (int64_t)b * TT + i) : -1;
         if (m >= p.num_masks) {
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(Stretch<T, BYTES>::threads) rules_kernel(const
     if (p.nodes.parents)
         for (int i = tid; i < used; i += kRuleThreads) {
             for (int w = 0; w < path_words; ++w) path[i * path_words + w] = 0;
-            for (int j = i; j >= 0; j = checked_parent(tree[j], j, p.status)) path[i * path_words + (j >> 5)] |= 1u << (j & 31);
+            for (int j = i; j >= 0; j = tree[j]) path[i * path_words + (j >> 5)] |= 1u << (j & 31);
         }
 
     auto within = [&](int t) {
@@ -371,7 +371,7 @@ extern "C" int logits_rules(const void *logits, int64_t ldv, int V, int B, int T
     if (T > kMaxTreeNodes) return SPR_ERR_UNSUPPORTED;
     if (B == 0 || T == 0) return SPR_OK;
     const size_t es = elem_size(dt);
-    if (!logits || !out || !aligned(logits, es) || !aligned(out, es)) return SPR_ERR_INVALID_ARG;
+    if (!logits || !out || !aligned(logits, es) || !aligned(out, es) || (logits == out && ldv != ld_out)) return SPR_ERR_INVALID_ARG;
     if ((history && (!history_len || ld_history < 0)) || (n_bias && (!bias_tokens || !bias_values)) ||
         (masks && (!mask_rows || num_masks <= 0 || ld_mask < ((int64_t)V + 31) / 32)))
         return SPR_ERR_INVALID_ARG;

@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(kRuleThreads, kRuleCtasPerSm) rules_single_ker
         reinterpret_cast<int4 *>(bias)[i] = make_int4(0, 0, 0, 0);
     }
     if (p.nodes.parents)
-        for (int i = tid; i < TT; i += kRuleThreads) tree[i] = p.nodes.parents[(int64_t)b * TT + i];
+        for (int i = tid; i < used; i += kRuleThreads) tree[i] = checked_parent(__ldg(p.nodes.parents + (int64_t)b * TT + i), i, p.status);
     for (int i = row0 + tid; i < row1; i += kRuleThreads) {
         int m = p.masks && i < used ? __ldg(p.mask_rows + (int64_t)b * TT + i) : -1;
         if (m >= p.num_masks) {
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(kRuleThreads, kRuleCtasPerSm) rules_single_ker
         // whether node j is node i or on its path
         auto on_path = [&](int j, int i) {
             if (!p.nodes.parents) return j <= i;
-            while (i > j) i = checked_parent(tree[i], i, p.status);
+            while (i > j) i = tree[i];
             return i == j;
         };
         // the rules for the token in a slot

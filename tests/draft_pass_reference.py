@@ -5,8 +5,10 @@ Bounds, with u = 2^-24 (one rounding of fp32):
           their sum by 3 roundings: 8 u (|x| + |y|) covers them; then the rounding of the result
   attend  a score is a sum of D products, added up in groups of 16 by the tensor cores, whose additions lose up to 2^-23 of
           the magnitude at each: (D/16 + 16) 2 u A, A = scale sum |q| |k| (fp32: one by one, (D + 8) u A), and a few u of
-          its own magnitude from scale and base-2 exponent.  A weight is off by that relative to itself, as is the sum, and by 4 u from the exponential; in bf16 calls a weight is cut to two bf16 numbers, 2^-17 of itself.  Sums over n keys
-          add (n/16 + 64) 2 u (fp32: (n + 64) u).  All of these are relative to sum p |v|.  Then the rounding of the result.
+          its own magnitude from scale and base-2 exponent.  A weight is off by that relative to itself, as is the sum, and by
+          4 u from the exponential; in bf16 calls a weight is cut to two bf16 numbers, 2^-17 of itself, or above 16 queries per
+          cached head to one, 2^-8.  Sums over n keys add (n/16 + 64) 2 u (fp32: (n + 64) u).  All of these are relative to
+          sum p |v|.  Then the rounding of the result.
   rules   five roundings of the terms' magnitudes, then the rounding of the result
 """
 import math
