@@ -342,8 +342,9 @@ cudaError_t pick_rules(RuleParams &p, cudaStream_t st)
     const bool wide = (int64_t)p.B * chunks_of(kLong) >= 148 * 4;
     if (rows <= kSingleRows && (int64_t)p.B * chunks_of(kLong) >= kSingleStretches) return launch_rules_single<T>(p, st);
     p.pieces = chunks_of(wide ? kLong : kShort);
-    // few sequences: their rows are dealt out too
-    int64_t groups = 148 * 4 / ((int64_t)p.B * p.pieces);
+    // few sequences: their rows are dealt out too, to as many CTAs as are resident (8 short stretches an SM rather than 4: 8x9 over
+    // 50257 entries 12.6 -> 9.5 us, 116x26x6130 90 -> 54 us; 16: 12.4 and 57)
+    int64_t groups = 148 * (wide ? 4 : 8) / ((int64_t)p.B * p.pieces);
     groups = groups < 1 ? 1 : groups > rows ? rows : groups;
     p.rows_per_group = (int)((rows + groups - 1) / groups);
     p.stages = p.rows_per_group < kMaxStages ? p.rows_per_group : kMaxStages;
