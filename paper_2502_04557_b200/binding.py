@@ -575,15 +575,15 @@ _PACK8_MOST = 1 << 20          # elements of a packed row
 
 def _on(device: int, dtype, name: str, t: torch.Tensor) -> int:
     """Address of a contiguous tensor of this type on this device."""
+    if t.get_device() == device and t.dtype == dtype and t.is_contiguous():
+        return t.data_ptr()
     if t.get_device() != device:
         if not t.is_cuda:
             raise ValueError(f"{name} must be a CUDA tensor")
         raise ValueError(f"{name} is on cuda:{t.get_device()}, the current device is cuda:{device}")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _result(device: int, t, shape, dtype, name: str):
@@ -772,15 +772,15 @@ def _optional(device: int, t, dtype, shape, name: str):
 
 def _caches(device: int, k_cache, v_cache, page_table, dtype, B: int, D: int):
     """(addresses, Hkv, page_size, num_pages, max_pages) of paged caches [num_pages, Hkv, page_size, D]."""
-    k, v = _on(device, dtype, "k_cache", k_cache), _on(device, dtype, "v_cache", v_cache)
-    shape = k_cache.shape
+    shape, pages = k_cache.shape, page_table.shape
     if len(shape) != 4 or shape != v_cache.shape or shape[3] != D:
         raise ValueError(f"k_cache and v_cache must be [num_pages, Hkv, page_size, {D}]")
-    table = _on(device, torch.int32, "page_table", page_table)
-    if page_table.dim() != 2 or page_table.shape[0] != B:
+    if len(pages) != 2 or pages[0] != B:
         raise ValueError(f"page_table must be [{B}, max_pages]")
+    k, v = _on(device, dtype, "k_cache", k_cache), _on(device, dtype, "v_cache", v_cache)
+    table = _on(device, torch.int32, "page_table", page_table)
     num_pages, Hkv, page_size, _ = shape
-    max_pages = page_table.shape[1]
+    max_pages = pages[1]
     if (num_pages | Hkv | page_size | max_pages) > _INT_MAX:
         raise ValueError("caches and page_table must have sizes below 2^31")
     return k, v, table, Hkv, page_size, num_pages, max_pages
@@ -789,21 +789,17 @@ def _caches(device: int, k_cache, v_cache, page_table, dtype, B: int, D: int):
 def _node_rows(device: int, t, dtype, shape, name: str):
     """Address and distance between nodes (in elements) of [B,T,H,D], dense but for that distance: a projection that gives
     queries, keys and values side by side is read where it is."""
-    if t.get_device() != device:
-        if not t.is_cuda:
-            raise ValueError(f"{name} must be a CUDA tensor")
-        raise ValueError(f"{name} is on cuda:{t.get_device()}, the current device is cuda:{device}")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
     B, T, H, D = shape
     if t.is_contiguous():
-        return t.data_ptr(), H * D
+        return _on(device, dtype, name, t), H * D
     b, n, h, d = t.stride()
     stride = n if T > 1 else b if B > 1 else H * D
     if (d != 1 and D > 1) or (h != D and H > 1) or stride < H * D or (T > 1 and B > 1 and b != T * n):
         raise ValueError(f"{name} must have dense heads and one distance between nodes, got strides {t.stride()}")
+    if t.get_device() != device or t.dtype != dtype:
+        _on(device, dtype, name, t)             # (says which)
     return t.data_ptr(), stride
 
 
@@ -872,7 +868,11 @@ def tree_attention(q, k_cache, v_cache, page_table, lens, ws: Workspace, scale=N
     c = _optional(dev, counts, torch.int32, (B,), "counts")
     par = _optional(dev, parents, torch.int32, (B, T), "parents")
     p, size = _ws(dev, ws)
-    out, oa = _result(dev, out, shape, dtype, "out")
+    if out is None:
+        out = torch.empty_like(q)
+        oa = out.data_ptr()
+    else:
+        out, oa = _result(dev, out, shape, dtype, "out")
     rc = lib().tree_attention(qa, kc, vc, B, T, Hq, Hkv, D, dt, n, c, par, table, max_pages, num_pages, page_size,
                               D ** -0.5 if scale is None else scale, oa, p, size, _raw_stream(dev))
     if rc != 0:

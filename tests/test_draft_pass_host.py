@@ -176,7 +176,8 @@ def append_args(ws, **kw):
     (dict(inv_freq=fake(8)), TypeError), (dict(counts=fake(3, dtype=I32)), ValueError), (dict(parents=fake(2, 4, dtype=I32)), ValueError),
     (dict(slots=fake(2, dtype=I32)), ValueError), (dict(q=fake(2, 3, 4, 8)), ValueError), (dict(q_out=fake(2, 3, 4, 8)), ValueError),
     (dict(q=None, q_out=fake(2, 3, 4, 16)), ValueError), (dict(k=fake(2, 3, 16, 2).transpose(2, 3)), ValueError),
-    (dict(k=fake(3, 2, 2, 16).transpose(0, 1)), ValueError), (dict(k=fake(6, 2, 16)), ValueError)])
+    (dict(k=fake(3, 2, 2, 16).transpose(0, 1)), ValueError), (dict(k=fake(6, 2, 16)), ValueError),
+    (dict(v=fake(2, 3, 4, 16, dtype=torch.float32)[:, :, :2]), TypeError), (dict(v=torch.zeros(2, 3, 4, 16, dtype=torch.bfloat16)[:, :, :2]), ValueError)])
 def test_binding_refuses_append(device, bad, why):
     with pytest.raises(why):
         spr.cache_append(**append_args(device, **bad))
