@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -122,6 +123,8 @@ def lib():
         L.tree_attention.argtypes = [vp] * 3 + [i32] * 6 + [vp] * 4 + [i32] * 3 + [f32, vp, vp, sz, vp]
         L.logits_rules.restype = i32
         L.logits_rules.argtypes = [vp, i64, i32, i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, i32, vp, i64, i32, vp, vp, i64, vp, sz, vp]
+        L.spr_draft_pass_call.restype = i32
+        L.spr_draft_pass_call.argtypes = [i32, C.c_char_p]
         L.spr_test_tree_attention.restype = None
         L.spr_test_tree_attention.argtypes = [i32, C.c_uint]
         L.spr_host_arena_bytes.restype = sz
@@ -761,10 +764,14 @@ def verifier_train_step8(packed, d: int, labels, theta, adam_m, adam_v, t: int, 
 # ---------------------------------------------------------------------------- the target's pass over drafted tokens
 
 
+# arguments of the three calls of a draft pass, 64 bits each
+_APPEND_ARGS, _ATTENTION_ARGS, _RULES_ARGS = struct.Struct("29q").pack, struct.Struct("16qd4q").pack, struct.Struct("25q").pack
+
+
 def _optional(device: int, t, dtype, shape, name: str):
-    """Address of an optional tensor of this shape, or None."""
+    """Address of an optional tensor of this shape, or 0."""
     if t is None:
-        return None
+        return 0
     if t.shape != shape:
         raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
     return _on(device, dtype, name, t)
@@ -823,7 +830,7 @@ def cache_append(k, v, k_cache, v_cache, page_table, lens, ws: Workspace, q=None
         raise ValueError(f"the caches have {heads} heads, k has {Hkv}")
     ka, ks = _node_rows(dev, k, dtype, shape, "k")
     va, vs = _node_rows(dev, v, dtype, shape, "v")
-    qa, qs, Hq, oa = None, 0, 0, None
+    qa, qs, Hq, oa = 0, 0, 0, 0
     if q is not None:
         if q.dim() != 4 or q.shape[2] > _INT_MAX:
             raise ValueError("q must be [B,T,Hq,D]")
@@ -831,7 +838,7 @@ def cache_append(k, v, k_cache, v_cache, page_table, lens, ws: Workspace, q=None
         qa, qs = _node_rows(dev, q, dtype, (B, T, Hq, D), "q")
     elif q_out is not None:
         raise ValueError("q_out needs q")
-    rot, fa = 0, None
+    rot, fa = 0, 0
     if inv_freq is not None:
         fa, rot = _on(dev, torch.float32, "inv_freq", inv_freq), 2 * inv_freq.numel()
         if rot > D:
@@ -843,8 +850,9 @@ def cache_append(k, v, k_cache, v_cache, page_table, lens, ws: Workspace, q=None
     p, size = _ws(dev, ws)
     if q is not None:
         q_out, oa = _result(dev, q_out, (B, T, Hq, D), dtype, "q_out")
-    rc = lib().cache_append(qa, qs, ka, ks, va, vs, B, T, Hq, Hkv, D, dt, n, c, par, sl, fa, rot, interleaved, table,
-                            max_pages, num_pages, page_size, kc, vc, oa, p, size, _raw_stream(dev))
+    rc = lib().spr_draft_pass_call(OP_CACHE_APPEND, _APPEND_ARGS(
+        qa, qs, ka, ks, va, vs, B, T, Hq, Hkv, D, dt, n, c, par, sl, fa, rot, bool(interleaved), table, max_pages, num_pages, page_size,
+        kc, vc, oa, p, size, _raw_stream(dev)))
     if rc != 0:
         _check("cache_append", rc)
     return q_out
@@ -873,8 +881,9 @@ def tree_attention(q, k_cache, v_cache, page_table, lens, ws: Workspace, scale=N
         oa = out.data_ptr()
     else:
         out, oa = _result(dev, out, shape, dtype, "out")
-    rc = lib().tree_attention(qa, kc, vc, B, T, Hq, Hkv, D, dt, n, c, par, table, max_pages, num_pages, page_size,
-                              D ** -0.5 if scale is None else scale, oa, p, size, _raw_stream(dev))
+    rc = lib().spr_draft_pass_call(OP_TREE_ATTENTION, _ATTENTION_ARGS(
+        qa, kc, vc, B, T, Hq, Hkv, D, dt, n, c, par, table, max_pages, num_pages, page_size, D ** -0.5 if scale is None else scale, oa, p,
+        size, _raw_stream(dev)))
     if rc != 0:
         _check("tree_attention", rc)
     return out
@@ -899,7 +908,7 @@ def logits_rules(logits, V: int, ws: Workspace, history=None, history_len=None, 
     la = _on(dev, dtype, "logits", logits)
     if (history is None) != (history_len is None):
         raise ValueError("history and history_len go together")
-    L, ha = 0, None
+    L, ha = 0, 0
     if history is not None:
         if history.dim() != 2 or history.shape[0] != B:
             raise ValueError(f"history must be [{B}, L]")
@@ -911,7 +920,7 @@ def logits_rules(logits, V: int, ws: Workspace, history=None, history_len=None, 
     pa = _optional(dev, penalties, torch.float32, (B, 3), "penalties")
     if (bias_tokens is None) != (bias_values is None):
         raise ValueError("bias_tokens and bias_values go together")
-    nb, ba, bv = 0, None, None
+    nb, ba, bv = 0, 0, 0
     if bias_tokens is not None:
         if bias_tokens.dim() != 2 or bias_tokens.shape[0] != B or bias_tokens.shape[1] > _INT_MAX:
             raise ValueError(f"bias_tokens must be [{B}, n]")
@@ -920,7 +929,7 @@ def logits_rules(logits, V: int, ws: Workspace, history=None, history_len=None, 
         bv = _optional(dev, bias_values, torch.float32, (B, nb), "bias_values")
     if (masks is None) != (mask_rows is None):
         raise ValueError("masks and mask_rows go together")
-    ma, ld_mask, num_masks, mr = None, 0, 0, None
+    ma, ld_mask, num_masks, mr = 0, 0, 0, 0
     if masks is not None:
         if masks.dim() != 2 or not 0 < masks.shape[0] <= _INT_MAX:
             raise ValueError("masks must be [M, words] with M >= 1")
@@ -935,8 +944,8 @@ def logits_rules(logits, V: int, ws: Workspace, history=None, history_len=None, 
         if out.dim() != 3 or out.shape[0] != B or out.shape[1] != T:
             raise ValueError(f"out must be [{B}, {T}, ld_out]")
         oa, ld_out = _on(dev, dtype, "out", out), out.shape[2]
-    rc = lib().logits_rules(la, ldv, V, B, T, dt, ha, L, hl, ta, par, c, pa, ba, bv, nb, ma, ld_mask, num_masks, mr, oa, ld_out,
-                            p, size, _raw_stream(dev))
+    rc = lib().spr_draft_pass_call(OP_LOGITS_RULES, _RULES_ARGS(
+        la, ldv, V, B, T, dt, ha, L, hl, ta, par, c, pa, ba, bv, nb, ma, ld_mask, num_masks, mr, oa, ld_out, p, size, _raw_stream(dev)))
     if rc != 0:
         _check("logits_rules", rc)
     return out

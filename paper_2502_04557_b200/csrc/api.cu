@@ -477,6 +477,77 @@ int spr_sd_verify_launches(int B, int K, int V, int dt)
     return sd_row_stats_launches(B, K, C, iters) + 1;   // + the correction draw
 }
 
+int spr_draft_pass_call(int op, const int64_t *args)
+{
+    if (!args) return SPR_ERR_INVALID_ARG;
+    auto number = [&] { return *args++; };
+    auto count = [&] { return (int)*args++; };
+    auto real = [&] {
+        double x;
+        memcpy(&x, args++, sizeof x);
+        return (float)x;
+    };
+    struct Address {
+        void *p;
+        operator const int32_t *() const { return static_cast<const int32_t *>(p); }
+        operator const uint32_t *() const { return static_cast<const uint32_t *>(p); }
+        operator const float *() const { return static_cast<const float *>(p); }
+        operator const void *() const { return p; }
+        operator void *() const { return p; }
+    };
+    auto address = [&] { return Address{reinterpret_cast<void *>(*args++)}; };
+    switch (op) {
+    case SPR_OP_CACHE_APPEND: {
+        const Address q = address();
+        const int64_t qs = number();
+        const Address k = address();
+        const int64_t ks = number();
+        const Address v = address();
+        const int64_t vs = number();
+        const int B = count(), T = count(), Hq = count(), Hkv = count(), D = count(), dt = count();
+        const Address lens = address(), counts = address(), parents = address(), slots = address(), inv_freq = address();
+        const int rot = count(), interleaved = count();
+        const Address table = address();
+        const int max_pages = count(), num_pages = count(), page_size = count();
+        const Address k_cache = address(), v_cache = address(), q_out = address(), ws = address();
+        const size_t bytes = (size_t)number();
+        return cache_append(q, qs, k, ks, v, vs, B, T, Hq, Hkv, D, dt, lens, counts, parents, slots, inv_freq, rot, interleaved, table,
+                            max_pages, num_pages, page_size, k_cache, v_cache, q_out, ws, bytes, address());
+    }
+    case SPR_OP_TREE_ATTENTION: {
+        const Address q = address(), k_cache = address(), v_cache = address();
+        const int B = count(), T = count(), Hq = count(), Hkv = count(), D = count(), dt = count();
+        const Address lens = address(), counts = address(), parents = address(), table = address();
+        const int max_pages = count(), num_pages = count(), page_size = count();
+        const float scale = real();
+        const Address out = address(), ws = address();
+        const size_t bytes = (size_t)number();
+        return tree_attention(q, k_cache, v_cache, B, T, Hq, Hkv, D, dt, lens, counts, parents, table, max_pages, num_pages, page_size, scale,
+                              out, ws, bytes, address());
+    }
+    case SPR_OP_LOGITS_RULES: {
+        const Address logits = address();
+        const int64_t ldv = number();
+        const int V = count(), B = count(), T = count(), dt = count();
+        const Address history = address();
+        const int64_t ld_history = number();
+        const Address history_len = address(), tokens = address(), parents = address(), counts = address(), penalties = address(),
+                      bias_tokens = address(), bias_values = address();
+        const int n_bias = count();
+        const Address masks = address();
+        const int64_t ld_mask = number();
+        const int num_masks = count();
+        const Address mask_rows = address(), out = address();
+        const int64_t ld_out = number();
+        const Address ws = address();
+        const size_t bytes = (size_t)number();
+        return logits_rules(logits, ldv, V, B, T, dt, history, ld_history, history_len, tokens, parents, counts, penalties, bias_tokens,
+                            bias_values, n_bias, masks, ld_mask, num_masks, mask_rows, out, ld_out, ws, bytes, address());
+    }
+    default: return SPR_ERR_INVALID_ARG;
+    }
+}
+
 int spr_version(void) { return 100; }
 
 }  // extern "C"

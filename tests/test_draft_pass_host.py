@@ -2,6 +2,7 @@
 host, before any device call."""
 import ctypes
 import math
+import struct
 import os
 import re
 
@@ -123,6 +124,30 @@ def test_rules_arguments_are_checked(mem):
     for bad in (dict(V=0), dict(V=-5), dict(V=(1 << 30) + 1, ldv=1 << 31, ldo=1 << 31), dict(ldv=99), dict(ldo=99), dict(nb=-1), dict(nb=1025),
                 dict(ldh=-1), dict(ldm=3), dict(nm=0), dict(nm=-1)):
         assert rules(L, p, **bad) == INVALID, bad
+
+
+def test_arguments_in_an_array(mem):
+    """Every argument arrives in its place: refusals and empty calls as those of the plain calls."""
+    L, p = spr.lib(), mem[1]
+
+    def call(op, f, real, **kw):
+        got = []
+        f(type("L", (), {"cache_append": lambda *a: got.extend(a[1:]), "tree_attention": lambda *a: got.extend(a[1:]),
+                         "logits_rules": lambda *a: got.extend(a[1:])})(), p, **kw)
+        fmt = "".join("d" if i == real else "q" for i in range(len(got)))
+        return L.spr_draft_pass_call(op, struct.pack(fmt, *[0 if a is None else a for a in got]))
+
+    for op, f, real, cases in (
+            (spr.OP_CACHE_APPEND, append, None, (dict(Hq=0), dict(D=0), dict(rot=3), dict(page=0), dict(ks=31), dict(vs=31), dict(qs=63), dict(kc=0),
+                                                 dict(vc=0), dict(table=0), dict(lens=0), dict(dt=7), dict(n=16), dict(ws=0), dict(B=0), dict(slots=p + 1))),
+            (spr.OP_TREE_ATTENTION, attend, 16, (dict(Hq=3), dict(D=12), dict(page=20), dict(scale=math.nan), dict(out=0), dict(ws=0), dict(n=16),
+                                                        dict(T=0), dict(table=0), dict(max_pages=0), dict(parents=p + 1))),
+            (spr.OP_LOGITS_RULES, rules, None, (dict(V=0), dict(ldv=99), dict(ldo=99), dict(nb=1025), dict(ldh=-1), dict(ldm=3), dict(nm=0), dict(mr=0),
+                                                dict(out=0), dict(ws=0), dict(n=16), dict(B=0), dict(pen=p + 1)))):
+        for kw in cases:
+            plain = f(L, p, **{k: v or None if k in ("kc", "vc", "table", "lens", "ws", "out", "mr") else v for k, v in kw.items()})
+            assert call(op, f, real, **kw) == plain, (op, kw)
+    assert L.spr_draft_pass_call(spr.OP_CACHE_APPEND, None) == INVALID and L.spr_draft_pass_call(3, b"\0" * 256) == INVALID
 
 
 def test_nothing_to_do(mem):
