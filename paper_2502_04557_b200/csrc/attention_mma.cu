@@ -45,8 +45,8 @@ struct MmaShape {
 
 struct MmaControl {
     int scratch[kMmaWarps + 2];
-    int tree[kMaxTreeNodes];
-    uint32_t path[16][kMaxTreeNodes / 32];
+    int tree[16];
+    uint32_t path[16];                      // nodes' paths, a bit for each node
     float2 ml[kMmaWarps][16];
     uint32_t valid[kMmaWarps][5];           // a bit for each key of a warp's step that is there
     int last;
@@ -184,16 +184,23 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
     const uint32_t k_off = k_row * Shape::row, v_off = (16 + v_row) * Shape::row;
     const int swz = lane & 7;                               // both rows are lane & 7 modulo 8
     const int quad = lane >> 2, pair = lane & 3;
+    // There is one block of rows, all of a sequence's queries of a cached head: which node a row belongs to, and where its row of
+    // q and out lies behind the part's first, does not change.
+    auto offset = [&](int r) { return (r / p.G * p.Hq + r % p.G) * p.D; };
+    const int node[2] = {quad / p.G, (quad + 8) / p.G}, q_at[2] = {offset(quad), offset(quad + 8)}, join_at = offset(tid >> 3);
+    auto first_row = [&](const AttnStretch &s, const AttnPart &part) {
+        return ((int64_t)s.seq.b * p.nodes.T * p.Hq + (int64_t)part.head * p.G) * p.D;
+    };
     // a part's queries as A fragments: rows quad and quad + 8 of each row tile.  They are asked for while what comes before
     // the part is still going on.
     uint32_t qf[KSTEPS][4];
     auto load_queries = [&](const AttnStretch &s, const AttnPart &part) {
-        const int row0 = part.block * ROWS, rows = s.seq.count * p.G - row0;
+        const int rows = s.seq.count * p.G;
+        const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p.q) + first_row(s, part);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int r = h * 8 + quad;
-            const bool in = r < rows;
-            const uint32_t *src = reinterpret_cast<const uint32_t *>(static_cast<const __nv_bfloat16 *>(p.q) + (in ? attn_out_at(p, s, part, row0 + r) : 0));
+            const bool in = h * 8 + quad < rows;
+            const uint32_t *src = reinterpret_cast<const uint32_t *>(q + (in ? q_at[h] : 0));
 #pragma unroll
             for (int k = 0; k < KSTEPS; ++k)
 #pragma unroll
@@ -211,23 +218,15 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
     for (int i = 0; i < Shape::stages; ++i) issue();
     while (have) {
         const AttnTarget t = attn_target<ROWS>(p, s, part);
-        const int i0 = t.row0 / p.G;
-        const int nodes = (t.row0 + t.rows - 1) / p.G - i0 + 1;
-        __syncthreads();
-        const bool holds_nodes = (part.t0 + part.n) * kAttnTile > s.seq.len;
-        if (holds_nodes && p.nodes.parents && tree_of != s.seq.b) {
-            for (int j = tid; j < s.seq.count; j += kMmaThreads) ctl.tree[j] = p.nodes.parents[(int64_t)s.seq.b * p.nodes.T + j];
-            tree_of = s.seq.b;
+        if ((part.t0 + part.n) * kAttnTile > s.seq.len) {       // the part holds nodes
             __syncthreads();
-        }
-        if (holds_nodes && tid < nodes)
-            attn_path_bits(p.nodes.parents ? ctl.tree : nullptr, i0 + tid, ctl.path[tid], (s.seq.count + 31) / 32, p.status);
-
-        int node[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = h * 8 + quad;
-            node[h] = r < t.rows ? (t.row0 + r) / p.G - i0 : 0;
+            if (p.nodes.parents && tree_of != s.seq.b) {
+                if (tid < s.seq.count) ctl.tree[tid] = p.nodes.parents[(int64_t)s.seq.b * p.nodes.T + tid];
+                tree_of = s.seq.b;
+                __syncthreads();
+            }
+            if (tid < s.seq.count) attn_path_bits(p.nodes.parents ? ctl.tree : nullptr, tid, ctl.path + tid, 1, p.status);
+            __syncthreads();
         }
         if (p.flip) {
 #pragma unroll
@@ -235,7 +234,6 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
 #pragma unroll
                 for (int c = 0; c < 4; ++c) qf[k][c] ^= p.flip;
         }
-        __syncthreads();
 
         float o[NTILES][4], m[2], l[2];
         m[0] = m[1] = neg_inf();
@@ -282,7 +280,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
                     for (int c = 0; c < 4; ++c) {
                         const int key = h * 8 + pair * 2 + (c & 1);
                         const int j = slot0 + key - s.seq.len;
-                        const bool vis = (valid >> key & 1) && (j < 0 || (ctl.path[node[c >> 1]][j >> 5] >> (j & 31) & 1));
+                        const bool vis = (valid >> key & 1) && (j < 0 || (ctl.path[node[c >> 1]] >> j & 1));
                         if (!vis) sc[h][c] = neg_inf();
                     }
             }
@@ -328,7 +326,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
                         const float w0 = h ? sc[1][2 * g] : sc[0][2 * g], w1 = h ? sc[1][2 * g + 1] : sc[0][2 * g + 1];
                         const float w = __shfl_sync(0xffffffffu, c ? w1 : w0, from);
                         const int j = slot0 + key - s.seq.len;
-                        if (j < 0 || (ctl.path[node[g]][j >> 5] >> (j & 31) & 1)) {
+                        if (j < 0 || (ctl.path[node[g]] >> j & 1)) {
 #pragma unroll
                             for (int i = 0; i < NTILES; ++i) {
                                 const uint32_t a = base + (16 + key) * Shape::row + ((i ^ (key & 7)) << 4) + pair * 4;
@@ -408,7 +406,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
         }
         const int r = row;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int64_t out_at = r < t.rows ? attn_out_at(p, s, part, t.row0 + r) : 0;
+        const int64_t out_at = first_row(s, part) + join_at;
 #pragma unroll
         for (int h = 0; h < 2 * PANELS; ++h) {
 #pragma unroll

@@ -256,13 +256,12 @@ __device__ __forceinline__ int64_t attn_out_at(const AttnParams &p, const AttnSt
 }
 
 // One ticket of the part's item, taken by one thread behind a barrier of those that wrote the part's record; true for the
-// last, whose CTA may then read all records (behind another barrier).
+// last, whose CTA may then read all records (behind another barrier).  The counter is zero again after the last.
 __device__ __forceinline__ bool attn_ticket(const AttnParams &p, const AttnTarget &t)
 {
-    __threadfence();
-    const bool last = take_ticket(p.counters + t.first, t.parts);
-    __threadfence();
-    return last;
+    uint32_t old;
+    asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(old) : "l"(p.counters + t.first), "r"((uint32_t)t.parts - 1u) : "memory");
+    return old == (uint32_t)t.parts - 1u;
 }
 
 // Joins the parts of an item; called by all lanes of `warps` warps of the CTA that took its last ticket.  A warp has N rows at a
