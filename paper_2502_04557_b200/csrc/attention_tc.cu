@@ -129,6 +129,25 @@ __device__ __forceinline__ void tmem_write32(uint32_t taddr, const uint32_t (&r)
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ bool finite_bf16x2(uint32_t w) { return (w & 0x7f80u) != 0x7f80u && (w & 0x7f800000u) != 0x7f800000u; }
+// Four lanes' four vectors each, the other way round: lane j of them has vector j of all.  Rows lie one to a lane, and stores of 16
+// bytes in 32 rows take the memory system 32 requests, however near they lie.
+__device__ __forceinline__ void exchange4(uint4 (&x)[4], int lane)
+{
+#pragma unroll
+    for (int by = 1; by <= 2; by *= 2) {
+        const bool upper = lane & by;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int i = by == 1 ? 2 * k : k, j = i + by;
+            uint4 give = upper ? x[i] : x[j];
+            give.x = __shfl_xor_sync(0xffffffffu, give.x, by);
+            give.y = __shfl_xor_sync(0xffffffffu, give.y, by);
+            give.z = __shfl_xor_sync(0xffffffffu, give.z, by);
+            give.w = __shfl_xor_sync(0xffffffffu, give.w, by);
+            (upper ? x[i] : x[j]) = give;
+        }
+    }
+}
 // which of the nodes first .. first + 63 node i sees: itself and its path
 __device__ __forceinline__ uint64_t seen_nodes(const int16_t *tree, int i, int first)
 {
@@ -555,8 +574,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             l = l * by[0] + other.y * by[1];
             const bool all = part.n > 1;                    // else the other group's O is not of this part, or this group's
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            const int64_t out_at = in ? attn_out_at(p, s, part, t.row0 + row) : 0;
             if (warp_in) {
+                // the rows that this lane writes vectors of, and where they begin
+                const int64_t out_at = in ? attn_out_at(p, s, part, t.row0 + row) : 0;
+                const int first = row & ~3;
+                int64_t to[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) to[i] = __shfl_sync(0xffffffffu, out_at, (lane & ~3) + i);
 #pragma unroll 1
                 for (int k = group * PANELS; k < (group + 1) * PANELS; ++k) {
                     float o[32], y[32];
@@ -570,23 +594,32 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
 #pragma unroll
                         for (int i = 0; i < 32; ++i) o[i] = fmaf(y[i], by[1], o[i]);
                     }
-                    if (in) {
+                    uint4 v[4];
+                    if (t.whole) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int col = 32 * k + 8 * i;
-                            if (col >= p.D) continue;
-                            if (t.whole) {
-                                *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + out_at + col) =
-                                    make_uint4(pack_bf16(o[8 * i] * inv, o[8 * i + 1] * inv), pack_bf16(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
-                                               pack_bf16(o[8 * i + 4] * inv, o[8 * i + 5] * inv), pack_bf16(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
-                            } else {
-                                float4 *to = reinterpret_cast<float4 *>(p.part + ((int64_t)t.slot * ROWS + row) * p.D + col);
-                                __stcg(to, make_float4(o[8 * i], o[8 * i + 1], o[8 * i + 2], o[8 * i + 3]));
-                                __stcg(to + 1, make_float4(o[8 * i + 4], o[8 * i + 5], o[8 * i + 6], o[8 * i + 7]));
-                            }
+                        for (int i = 0; i < 4; ++i)
+                            v[i] = make_uint4(pack_bf16(o[8 * i] * inv, o[8 * i + 1] * inv), pack_bf16(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
+                                              pack_bf16(o[8 * i + 4] * inv, o[8 * i + 5] * inv), pack_bf16(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
+                        exchange4(v, lane);
+                        const int col = 32 * k + 8 * (lane & 3);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (first + i < t.rows && col < p.D) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + to[i] + col) = v[i];
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                v[i] = make_uint4(__float_as_uint(o[16 * h + 4 * i]), __float_as_uint(o[16 * h + 4 * i + 1]),
+                                                  __float_as_uint(o[16 * h + 4 * i + 2]), __float_as_uint(o[16 * h + 4 * i + 3]));
+                            exchange4(v, lane);
+                            const int col = 32 * k + 16 * h + 4 * (lane & 3);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (first + i < t.rows && col < p.D)
+                                    __stcg(reinterpret_cast<uint4 *>(p.part + ((int64_t)t.slot * ROWS + first + i) * p.D + col), v[i]);
                         }
                     }
-                    __syncwarp();
                 }
             }
             if (!t.whole && group == 0 && in) __stcg(&p.part_ml[(int64_t)t.slot * ROWS + row], make_float2(top * c, l));
