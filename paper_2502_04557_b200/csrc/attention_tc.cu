@@ -80,6 +80,16 @@ __device__ __forceinline__ void group_meet(int group)
     else
         asm volatile("bar.sync 2, 128;" ::: "memory");
 }
+// the same, and whether any thread has something
+__device__ __forceinline__ bool group_any(int group, bool x)
+{
+    uint32_t any;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\tbarrier.cta.red.or.pred q, %1, 128, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+                 : "=r"(any)
+                 : "r"(group ? 3 : 2), "r"((int)x)
+                 : "memory");
+    return any != 0;
+}
 __device__ __forceinline__ void arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src)
 {
@@ -441,13 +451,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
 #pragma unroll
                     for (int k = 0; k < 4 * PANELS; ++k) {
                         uint32_t w[4];
-                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(v + (k >> 2) * kPanel + (k & 3) * 16) : "memory");
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(v + (k >> 2) * kPanel + ((k ^ (row >> 1)) & 3) * 16) : "memory");      // (banks)
                         bad = bad || !(finite_bf16x2(w[0]) && finite_bf16x2(w[1]) && finite_bf16x2(w[2]) && finite_bf16x2(w[3]));
                     }
-                    group_meet(group);
-                    if (bad) atomicOr(&ctl.odd[group], 1ull << (row >> 1));
-                    group_meet(group);
-                    odd = *reinterpret_cast<volatile unsigned long long *>(&ctl.odd[group]);
+                    if (group_any(group, bad)) {
+                        if (bad) atomicOr(&ctl.odd[group], 1ull << (row >> 1));
+                        group_meet(group);
+                        odd = *reinterpret_cast<volatile unsigned long long *>(&ctl.odd[group]);
+                    }
                 }
                 if (!warp_in && !odd) {                      // no row of this warp is in use: its part of P is not looked at
                     warp_arrive(&ctl.p_ready[group][b]);
