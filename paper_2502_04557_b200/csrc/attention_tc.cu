@@ -20,6 +20,10 @@
 // rounding does.  A second bf16 number for what the rounding leaves, as with few rows, would cost a fifth of the time
 // (128 sequences of 17 nodes: 199 us against 164 us).
 //
+// 128 sequences of 17 nodes, 32/8 heads of 128, some 1500 tokens: 172 us, 130 of loads; 16 trees of 64 nodes over 8192: 167 us.  Beside its
+// tiles a part takes some 9000 clocks, the latency of its start, its tail (which is masked and looked through) and its results: 128
+// sequences of 17 nodes over 100 tokens take 57 us, 13 of loads.
+//
 // Every wait is bounded: when one runs out the status word becomes SPR_ERR_TIMEOUT, loaders and issuing threads stop and
 // wait (again bounded) for what is in flight, and the softmax warps go on without waiting and give NaN.
 #include <atomic>

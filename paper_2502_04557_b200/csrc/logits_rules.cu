@@ -11,7 +11,7 @@
 // once (history and biases are read by every stretch, from L2), with integer atomics, so that their order does not matter.
 // Nearly all tokens are touched by neither: those that are stand in a list, up to four to a thread (or are looked for), and are put right in the
 // ring; masks are applied there to vectors, with their bits read a row ahead.  Rows by 8 KB for many sequences, 4 KB for few.
-// 256 x 17 rows of 128256 bf16 entries, a quarter masked: 423 us, 5.3 TB/s (no masks 387, 5.8).  More rows in the ring take
+// 256 x 17 rows of 128256 bf16 entries, a quarter masked: 410 us, 5.5 TB/s.  More rows in the ring take
 // CTAs from the SM (4 stages 490 us), two leave the copies too little (508 us).
 #include <atomic>
 

@@ -121,7 +121,7 @@ def test_attention_arguments_are_checked(mem):
 
 def test_rules_arguments_are_checked(mem):
     L, p = spr.lib(), mem[1]
-    for bad in (dict(V=0), dict(V=-5), dict(V=(1 << 30) + 1, ldv=1 << 31, ldo=1 << 31), dict(ldv=99), dict(ldo=99), dict(nb=-1), dict(nb=1025),
+    for bad in (dict(V=0), dict(V=-5), dict(V=(1 << 30) + 1, ldv=1 << 31, ldo=1 << 31), dict(ldv=99), dict(ldo=99), dict(ldo=101), dict(nb=-1), dict(nb=1025),
                 dict(ldh=-1), dict(ldm=3), dict(nm=0), dict(nm=-1)):
         assert rules(L, p, **bad) == INVALID, bad
 
