@@ -39,7 +39,7 @@ enum { ATTN_TEST_NO_LOADS = 1 };         // test hook: no tile is ever loaded, s
 int attention_block_rows(int T, int G, int dt);
 
 cudaError_t launch_attention_f32(const AttnParams &p, int rows, cudaStream_t st);
-cudaError_t launch_attention_f32_tile(const AttnParams &p, int dev, cudaStream_t st);
+cudaError_t launch_attention_f32_tile(const AttnParams &p, int rows, int dev, cudaStream_t st);
 cudaError_t launch_attention_mma(const AttnParams &p, int dev, cudaStream_t st);
 cudaError_t launch_attention_tc(const AttnParams &p, int dev, cudaStream_t st);
 

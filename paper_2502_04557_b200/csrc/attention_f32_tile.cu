@@ -1,6 +1,7 @@
 // tree_attention on fp32 tensors with more than 16 queries per cached head, on the CUDA cores.
 //
-// A CTA has 64 queries and walks their keys by 128 with a running maximum and sum.  A warp owns eight queries throughout, a
+// A CTA has 64 queries (32 where there are no more: 8 x 8, 32/8 heads of 128, 2000 tokens 89 -> 79 us) and walks their keys by 128
+// with a running maximum and sum.  A warp owns eight (four) queries throughout, a
 // lane four keys of each step for the scores, and D / 32 columns for the results: both products take 8 x 4 multiplications per
 // 12 vectors read from shared memory, of which eight are the same for all lanes, and weights never leave the warp's
 // rows of shared memory.  Keys of the next step are on their way (cp.async) while values are worked on, and the other way round.
@@ -19,13 +20,12 @@ namespace spr {
 namespace {
 
 constexpr int kThreads = 256, kWarps = 8;
-constexpr int kRows = 64, kOwn = kRows / kWarps;       // queries of a CTA, of a warp
 constexpr int kStep = 128, kEach = kStep / 32;         // keys of a step, of a lane
 constexpr int kLoads = kStep / kWarps;                 // keys that a warp brings
 constexpr int kPitch = kStep + 4;                      // of a row of weights
 constexpr float kUnseen = -1.f;                        // in place of a weight
 
-size_t tile_smem(int D) { return sizeof(float) * ((size_t)(kRows + kStep) * (D + 4) + (size_t)kStep * D + kRows * kPitch); }
+size_t tile_smem(int rows, int D) { return sizeof(float) * ((size_t)(rows + kStep) * (D + 4) + (size_t)kStep * D + rows * kPitch); }
 
 __device__ __forceinline__ void copy16(float *dst, const float *src, bool there)
 {
@@ -35,10 +35,11 @@ __device__ __forceinline__ void copy16(float *dst, const float *src, bool there)
 __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void all_but_last() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
 
-// E: columns of a lane
-template <int E>
+// kRows: queries of a CTA; E: columns of a lane
+template <int kRows, int E>
 __global__ void __launch_bounds__(kThreads, 1) attention_f32_tile_kernel(const AttnParams p)
 {
+    constexpr int kOwn = kRows / kWarps;           // queries of a warp
     __shared__ int scratch[kWarps + 2];
     __shared__ int tree[kMaxTreeNodes];
     __shared__ uint32_t path[kRows][kMaxTreeNodes / 32];
@@ -269,25 +270,26 @@ __global__ void __launch_bounds__(kThreads, 1) attention_f32_tile_kernel(const A
     }
 }
 
-template <int E>
+template <int ROWS, int E>
 cudaError_t launch_tile(const AttnParams &p, int dev, cudaStream_t st)
 {
     static std::atomic<bool> attr_set[64];   // host threads may race to set it: all of them store `true`
     if (dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-        const cudaError_t e = cudaFuncSetAttribute(attention_f32_tile_kernel<E>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   (int)tile_smem(E * 32));
+        const cudaError_t e = cudaFuncSetAttribute(attention_f32_tile_kernel<ROWS, E>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   (int)tile_smem(ROWS, E * 32));
         if (e != cudaSuccess) return e;
         if (dev < 64) attr_set[dev].store(true, std::memory_order_release);
     }
-    attention_f32_tile_kernel<E><<<p.ctas, kThreads, tile_smem(p.D), st>>>(p);
+    attention_f32_tile_kernel<ROWS, E><<<p.ctas, kThreads, tile_smem(ROWS, p.D), st>>>(p);
     return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_attention_f32_tile(const AttnParams &p, int dev, cudaStream_t st)
+cudaError_t launch_attention_f32_tile(const AttnParams &p, int rows, int dev, cudaStream_t st)
 {
-    return p.D <= 64 ? launch_tile<2>(p, dev, st) : launch_tile<4>(p, dev, st);
+    if (rows == 32) return p.D <= 64 ? launch_tile<32, 2>(p, dev, st) : launch_tile<32, 4>(p, dev, st);
+    return p.D <= 64 ? launch_tile<64, 2>(p, dev, st) : launch_tile<64, 4>(p, dev, st);
 }
 
 }  // namespace spr

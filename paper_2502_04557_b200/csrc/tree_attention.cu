@@ -21,7 +21,7 @@ thread_local unsigned t_spin_limit = 0;
 int attention_block_rows(int T, int G, int dt)
 {
     const int64_t rows = (int64_t)T * G;
-    if (dt == SPR_F32) return rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 16 ? 16 : 64;
+    if (dt == SPR_F32) return rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     return rows <= 16 ? 16 : 128;
 }
 
@@ -87,7 +87,7 @@ int tree_attention(const void *q, const void *k_cache, const void *v_cache, int 
     p.spin_limit = t_spin_limit ? t_spin_limit : pairtc::kSpinLimit;
     p.test_flags = t_test_flags;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == SPR_F32) return finish(rows > 16 ? launch_attention_f32_tile(p, dev, st) : launch_attention_f32(p, rows, st));
+    if (dt == SPR_F32) return finish(rows > 16 ? launch_attention_f32_tile(p, rows, dev, st) : launch_attention_f32(p, rows, st));
     return finish(rows == 16 ? launch_attention_mma(p, dev, st) : launch_attention_tc(p, dev, st));
 }
 
