@@ -506,6 +506,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                                 for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(o[i] * a);
                                 tmem_write32(col_o + 32 * k, w);
                             }
+                            tmem_wait_st();        // (O may be read again below, and stores are not in order with reads)
                         }
                     }
                     const float ref = m == neg_inf() ? 0.f : -m * c;

@@ -1,0 +1,41 @@
+"""tree_attention, cache_append and logits_rules at the edges of what they are documented for: infinities, tensors in place, long
+histories, prompts in pieces.  Bounds in draft_pass_reference.py."""
+import math
+
+import pytest
+import torch
+
+import draft_pass_reference as ref
+from test_gpu_draft_pass import BF16, F32, attend_case, check_attend, ids, run_attend, spr  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def put(cache, x, b, slot, value):
+    """The entry of a sequence's slot, all heads (and columns, or as many as value has)."""
+    page = cache.shape[2]
+    cache[int(x["page_table"][b, slot // page]), :, slot % page] = value
+
+
+@pytest.mark.parametrize("T,G,D,tiles", [(12, 2, 64, 4), (9, 4, 128, 4), (40, 1, 80, 3), (30, 5, 128, 2)])
+def test_a_maximum_is_raised_beside_infinities(spr, T, G, D, tiles):  # noqa: F811
+    """The last tile's keys raise the maximum of rows that have results so far, and hold a value that is infinite for some of them
+    only: the others have what they have where that value is zero."""
+    lens = [64 * tiles + 10, 64 * tiles + 50 - T]
+    x = attend_case(2, T, 2 * G, 2, D, 16, BF16, seed=T, tree=True, lens=lens)
+    x["q"] = (1 + 0.25 * x["q"].float()).to(BF16)
+    for b in range(2):
+        for slot in range(64 * tiles, lens[b]):
+            put(x["k_cache"], x, b, slot, 256.0 / D)      # scores of some 256 / sqrt(D), 32 binary exponents and more
+        x["parents"][b, 1] = 0                             # (node 1 has rows that see it and rows that do not)
+        x["parents"][b, 2] = -1
+    clean = dict(x, v_cache=x["v_cache"].clone())
+    for b in range(2):
+        put(x["v_cache"], x, b, lens[b] + 1, math.inf)
+        put(clean["v_cache"], x, b, lens[b] + 1, 0.0)
+    got, want = check_attend(spr, x).cpu(), check_attend(spr, clean).cpu()
+    for b in range(2):
+        sees = torch.tensor([1 in ref.path(x["parents"][b].tolist(), i) for i in range(T)])
+        assert bool(sees.any()) and not bool(sees.all())
+        assert torch.equal(got[b][~sees], want[b][~sees]) and bool(torch.isfinite(got[b][~sees]).all())
+        assert bool((got[b][sees] == math.inf).all())
