@@ -436,7 +436,7 @@ int verifier_train_step8(const void *packed, const uint8_t *labels, int64_t N, i
  * by the angle position * inv_freq[j], inv_freq [rot/2] f32.  Angles are formed in double, rotations in fp32, and results
  * are rounded once; the rest is copied bit for bit.
  *   q_out [B,T,Hq,D]: rotated queries, zeros for nodes that are not used.  q and q_out may both be NULL, and q_out may be q
- *   where q is dense; otherwise nothing may overlap.
+ *   where q is dense (SPR_ERR_INVALID_ARG where it is not); otherwise nothing may overlap.
  *   slots [B,T] int32 (optional): the slot to put a node in instead of lens[b] + i, negative: none (its query is rotated
  *   all the same); positions stay what they are.  After the check of a tree this puts the nodes that were kept at the
  *   slots behind the prefix: slot = position.  No two nodes may be given one slot.

@@ -300,6 +300,8 @@ extern "C" int cache_append(const void *q, int64_t q_stride, const void *k, int6
         !aligned(page_table, 4))
         return SPR_ERR_INVALID_ARG;
     if (k_stride < (int64_t)Hkv * D || v_stride < (int64_t)Hkv * D || (q && q_stride < (int64_t)Hq * D)) return SPR_ERR_INVALID_ARG;
+    // in place a node's queries would be written over another's that are still to be read
+    if (q && q == q_out && q_stride != (int64_t)Hq * D && (int64_t)B * T > 1) return SPR_ERR_INVALID_ARG;
     if (!ws || !aligned(ws, 256) || ws_bytes < (size_t)kHeaderBytes) return SPR_ERR_WORKSPACE;
     const int rc = device_supported();
     if (rc != SPR_OK) return rc;
