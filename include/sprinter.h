@@ -463,7 +463,8 @@ int cache_append(const void *q, int64_t q_stride, const void *k, int64_t k_strid
  * Scores, maxima and sums are fp32.  With bf16 tensors the weights enter the second product as two bf16 numbers where a cached
  * head has up to 16 queries (T * Hq / Hkv), and rounded to one where it has more.
  * Keys and values of slots that a row does not see have no part in it, whatever they hold; infinities and NaN in
- * those that it does see make it infinite or NaN.  A slot without a page is left out (SPR_ERR_BAD_PAGE), and a row
+ * those that it does see count as the formula has them: a score of -inf is a weight of zero, and a row whose scores are all
+ * -inf is NaN, as is one with a score of +inf or NaN.  A slot without a page is left out (SPR_ERR_BAD_PAGE), and a row
  * that sees no slot at all is zeros.  After SPR_ERR_TIMEOUT rows whose keys did not arrive are NaN.
  * Launches do not depend on the lengths: a captured call serves whatever lens, counts, parents and page_table hold
  * when it is replayed.  Workspace: spr_workspace_bytes(SPR_OP_TREE_ATTENTION, B, T, 1, D, 0, dt).

@@ -106,9 +106,9 @@ __global__ void __launch_bounds__(32 * kWarpsFor<ROWS, E>, 2) attention_f32_kern
                 v[j].load(v_cache + at + col, in && at >= 0);
             }
         };
-        float m = neg_inf(), l = 0.f;
+        float m = neg_inf(), l = 0.f;       // (m is no less than kOnlyMinusInf once a key has been seen)
         auto use = [&](int64_t rows, int tile, int group, const Cols<E> (&k)[kGroup], const Cols<E> (&v)[kGroup]) {
-            float sc[kGroup];
+            float sc[kGroup], top = m;
             uint32_t seen[kGroup];
             const int slot0 = tile * kAttnTile + warp * kKeys + group * kGroup;
             if (slot0 >= keys) return;
@@ -139,8 +139,8 @@ __global__ void __launch_bounds__(32 * kWarpsFor<ROWS, E>, 2) attention_f32_kern
                 const bool vis = there && (node < 0 || (bits[node >> 5] >> (node & 31) & 1));
                 if (!vis) sc[j] = neg_inf();
                 seen[j] = __ballot_sync(0xffffffffu, vis);
+                if (vis) top = fmaxf(top, kOnlyMinusInf);
             }
-            float top = m;
 #pragma unroll
             for (int j = 0; j < kGroup; ++j) top = fmaxf(top, sc[j]);
             const float ref = top == neg_inf() ? 0.f : top;
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(32 * kWarpsFor<ROWS, E>, 2) attention_f32_kern
                 y.x = fmaf(a, x.x, y.x), y.y = fmaf(a, x.y, y.y), y.z = fmaf(a, x.z, y.z), y.w = fmaf(a, x.w, y.w);
             }
             if (t.whole) {
-                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                const float inv = attn_inverse(top, sum);
                 store_out(static_cast<float *>(p.out) + attn_out_at(p, s, part, t.row0 + row) + c, make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv), 4);
             } else {
                 __stcg(reinterpret_cast<float4 *>(p.part + ((int64_t)t.slot * ROWS + row) * p.D + c), y);

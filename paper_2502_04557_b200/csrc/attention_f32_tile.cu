@@ -111,6 +111,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_f32_tile_kernel(const A
 
         const bool busy = row_of < t.rows;
         float o[kOwn][E], m[kOwn], l[kOwn];
+        uint32_t saw = 0;               // queries of the warp that have seen one of the lane's keys
 #pragma unroll
         for (int r = 0; r < kOwn; ++r) {
             m[r] = neg_inf(), l[r] = 0.f;
@@ -169,7 +170,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_f32_tile_kernel(const A
                 for (int r = 0; r < kOwn; ++r)
 #pragma unroll
                     for (int j = 0; j < kEach; ++j)
-                        if (!sees(r, j, have[j])) sc[r][j] = neg_inf();
+                        if (sees(r, j, have[j]))
+                            saw |= 1u << r;
+                        else
+                            sc[r][j] = neg_inf();
+            } else {
+                saw = (1u << kOwn) - 1;
             }
             float *pr = ps + row_of * kPitch;
 #pragma unroll
@@ -240,8 +246,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_f32_tile_kernel(const A
             else
                 commit();
         }
+        saw = __reduce_or_sync(0xffffffffu, saw);
 #pragma unroll
         for (int r = 0; r < kOwn; ++r) {
+            m[r] = attn_top(m[r], saw >> r & 1);
 #pragma unroll
             for (int off = 16; off; off /= 2) l[r] += __shfl_xor_sync(0xffffffffu, l[r], off);
             const int row = row_of + r;
@@ -249,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_f32_tile_kernel(const A
             float inv = 1.f;
             float *to;
             if (t.whole) {
-                inv = l[r] == 0.f ? 0.f : 1.f / l[r];
+                inv = attn_inverse(m[r], l[r]);
                 to = static_cast<float *>(p.out) + attn_out_at(p, s, part, t.row0 + row) + col;
             } else {
                 to = p.part + ((int64_t)t.slot * kRows + row) * D + col;

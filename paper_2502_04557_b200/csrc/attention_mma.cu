@@ -238,6 +238,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
         float o[NTILES][4], m[2], l[2];
         m[0] = m[1] = neg_inf();
         l[0] = l[1] = 0.f;
+        uint32_t saw = 0;                   // a bit for each of the two rows: one of the lane's keys has been seen
 #pragma unroll
         for (int n = 0; n < NTILES; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
         for (int n = 0; n < part.n; ++n) {
@@ -281,8 +282,13 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
                         const int key = h * 8 + pair * 2 + (c & 1);
                         const int j = slot0 + key - s.seq.len;
                         const bool vis = (valid >> key & 1) && (j < 0 || (ctl.path[node[c >> 1]] >> j & 1));
-                        if (!vis) sc[h][c] = neg_inf();
+                        if (vis)
+                            saw |= 1u << (c >> 1);
+                        else
+                            sc[h][c] = neg_inf();
                     }
+            } else {
+                saw = 3;
             }
             float top[2];
 #pragma unroll
@@ -375,12 +381,14 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
         if (have) load_queries(s_next, next);
 
         // ------------------------------------------------------------ the warps' results joined
+        saw |= __shfl_xor_sync(0xffffffffu, saw, 1);
+        saw |= __shfl_xor_sync(0xffffffffu, saw, 2);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             float x = l[g];
             x += __shfl_xor_sync(0xffffffffu, x, 1);
             x += __shfl_xor_sync(0xffffffffu, x, 2);
-            if (pair == 0) ctl.ml[warp][g * 8 + quad] = make_float2(m[g] * p.abs_scale_log2, x);
+            if (pair == 0) ctl.ml[warp][g * 8 + quad] = make_float2(attn_top(m[g] * p.abs_scale_log2, saw >> g & 1), x);
         }
         __syncthreads();
 #pragma unroll
@@ -405,7 +413,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
             sum = fmaf(ex2(x.x - (tall == neg_inf() ? 0.f : tall)), x.y, sum);
         }
         const int r = row;
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const float inv = attn_inverse(tall, sum);
         const int64_t out_at = first_row(s, part) + join_at;
 #pragma unroll
         for (int h = 0; h < 2 * PANELS; ++h) {

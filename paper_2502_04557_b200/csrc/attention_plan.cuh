@@ -18,6 +18,13 @@ struct AttnSeq {
     __device__ __forceinline__ int total(int Hkv) const { return tiles * blocks * Hkv; }
 };
 
+// The maximum of a row that has seen keys, all with scores of -inf.  They have no weight beside any other score (parts are joined as ever),
+// but where there is none the row's softmax is 0 / 0, unlike a row's that has seen no key (-inf): that is zeros.
+constexpr float kOnlyMinusInf = -3.402823466e38f;
+__device__ __forceinline__ float attn_top(float scaled, bool saw) { return scaled == neg_inf() && saw ? kOnlyMinusInf : scaled; }
+// what a row's results are multiplied by in the end
+__device__ __forceinline__ float attn_inverse(float top, float sum) { return sum == 0.f && top == neg_inf() ? 0.f : 1.f / sum; }
+
 // keys of a sequence: its prefix and its nodes, as far as the page table goes
 __device__ __forceinline__ int attn_keys(const AttnParams &p, int len, int count) { return (int)min((int64_t)len + count, p.capacity); }
 
@@ -315,7 +322,7 @@ __device__ __forceinline__ void attn_join(const AttnParams &p, const AttnStretch
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (row0 + i < t.rows) {
-                const float inv = sum[i] == 0.f ? 0.f : 1.f / sum[i];
+                const float inv = attn_inverse(top[i], sum[i]);
                 store_out(static_cast<T *>(p.out) + attn_out_at(p, s, part, t.row0 + row0 + i) + c,
                           make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv), p.D - c);
             }

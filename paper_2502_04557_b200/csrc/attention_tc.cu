@@ -431,6 +431,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                 softmax_meet();
             }
             float m = neg_inf(), l = 0.f;
+            bool saw = false;                               // a key of this group's tiles
             int mine = at + ((at ^ group) & 1);             // this group's next tile
             const int begin = at, end = at + part.n;
             at = end;
@@ -464,6 +465,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                         odd = *reinterpret_cast<volatile unsigned long long *>(&ctl.odd[group]);
                     }
                 }
+                saw = saw || vis != 0;
                 if (!warp_in && !odd) {                      // no row of this warp is in use: its part of P is not looked at
                     warp_arrive(&ctl.p_ready[group][b]);
                     continue;
@@ -581,6 +583,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             // -------------------------------------------------------- the part's results: each group has half of the columns
             if (any) wait(&ctl.pv_done[group][(mine - 2) >> 1 & 1], (uint32_t)((mine - 2) >> 2));
             if (dead) l = __int_as_float(0x7fc00000);       // what a wait that ran out leaves is no result
+            m = attn_top(m, saw);
             ctl.ml[group][row] = make_float2(m, l);
             softmax_meet();
             fence_after();
@@ -589,7 +592,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
             float by[2] = {ex2((m - shift) * c), ex2((other.x - shift) * c)};
             l = l * by[0] + other.y * by[1];
             const bool all = part.n > 1;                    // else the other group's O is not of this part, or this group's
-            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const float inv = attn_inverse(top, l);
             if (warp_in) {
                 // the rows that this lane writes vectors of, and where they begin
                 const int64_t out_at = in ? attn_out_at(p, s, part, t.row0 + row) : 0;
@@ -638,7 +641,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnP
                     }
                 }
             }
-            if (!t.whole && group == 0 && in) __stcg(&p.part_ml[(int64_t)t.slot * ROWS + row], make_float2(top * c, l));
+            if (!t.whole && group == 0 && in) __stcg(&p.part_ml[(int64_t)t.slot * ROWS + row], make_float2(attn_top(top * c, top != neg_inf()), l));
             fence_before();
             if (!t.whole) {
                 softmax_meet();

@@ -39,3 +39,39 @@ def test_a_maximum_is_raised_beside_infinities(spr, T, G, D, tiles):  # noqa: F8
         assert bool(sees.any()) and not bool(sees.all())
         assert torch.equal(got[b][~sees], want[b][~sees]) and bool(torch.isfinite(got[b][~sees]).all())
         assert bool((got[b][sees] == math.inf).all())
+
+
+ROWS = [(1, 4), (2, 4), (5, 3), (8, 4), (40, 4)]            # nodes and queries per cached head: every kernel
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=ids)
+@pytest.mark.parametrize("T,G", ROWS)
+def test_scores_of_minus_infinity(spr, T, G, dtype):  # noqa: F811
+    """A score of -inf is a weight of zero, and a row that has no other score is NaN (not zeros: it does see keys), in items of one
+    part and of many."""
+    lens = [70, 70, 9000, 9000, 0]
+    x = attend_case(5, T, 2 * G, 2, 64, 16, dtype, seed=91 + T, lens=lens)
+    x["parents"] = torch.full((5, T), -1, dtype=torch.int32)         # all nodes follow the prefix: a row sees its own only
+    x["q"][..., 0] = 1.0
+    x["k_cache"][..., 0] = 0.0
+    low = dict(x, k_cache=x["k_cache"].clone())
+    for k, value in ((x["k_cache"], -math.inf), (low["k_cache"], -2000.0)):      # (scores of -250: weights of zero too)
+        for b, n in enumerate(lens):
+            own = range(n, n + T, 2)                                  # every other node
+            for slot in [*range(n if b % 2 == 0 else n - 40), *own]:  # all of the prefix, or all but its last 40
+                head = k[int(x["page_table"][b, slot // 16])]
+                head[:, slot % 16, 0] = value
+    got = run_attend(spr, x).cpu()
+    args = {n: None if t is None else t.cuda() for n, t in low.items()}
+    want, tol = ref.attend(args["q"], args["k_cache"], args["v_cache"], x["page_table"], x["lens"], None, x["parents"], 64 ** -0.5)
+    for b, n in enumerate(lens):
+        for i in range(T):
+            if b % 2 == 0 and i % 2 == 0:
+                assert bool(got[b, i].isnan().all()), (b, i)
+            else:
+                assert ref.within(got[b, i], want[b, i].cpu(), tol[b, i].cpu()), (b, i)
+    # the same with signs the other way round
+    y = dict(x, k_cache=x["k_cache"].clone())
+    y["k_cache"].neg_()
+    again = run_attend(spr, y, scale=-64 ** -0.5).cpu()
+    assert torch.equal(again.isnan(), got.isnan()) and torch.equal(again.nan_to_num(), got.nan_to_num())
