@@ -81,6 +81,13 @@ __device__ __forceinline__ void copies_wait()
 {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
+// two values as they are, but the largest finite numbers in place of infinities and NaN
+__device__ __forceinline__ uint32_t finite_part(uint32_t w)
+{
+    uint32_t r;
+    asm("min.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0x7f7f7f7fu));
+    return r;
+}
 __device__ __forceinline__ bool finite_bf16x2(uint32_t w) { return (w & 0x7f80u) != 0x7f80u && (w & 0x7f800000u) != 0x7f800000u; }
 
 // PANELS: 64-column halves of the head dimension; WHOLE: which it is made of
@@ -367,8 +374,9 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
                 ldsm_t(base + v_off + (((i * 2 + v_chunk) ^ swz) << 4), b);
                 mma(o[2 * i], hi, b[0], b[1]);
                 mma(o[2 * i + 1], hi, b[2], b[3]);
-                mma(o[2 * i], lo, b[0], b[1]);
-                mma(o[2 * i + 1], lo, b[2], b[3]);
+                // (infinities are taken in by the first part of their weight, which is positive: the second may be 0 or below)
+                mma(o[2 * i], lo, finite_part(b[0]), finite_part(b[1]));
+                mma(o[2 * i + 1], lo, finite_part(b[2]), finite_part(b[3]));
             }
             __syncwarp();
             issue();

@@ -75,3 +75,22 @@ def test_scores_of_minus_infinity(spr, T, G, dtype):  # noqa: F811
     y["k_cache"].neg_()
     again = run_attend(spr, y, scale=-64 ** -0.5).cpu()
     assert torch.equal(again.isnan(), got.isnan()) and torch.equal(again.nan_to_num(), got.nan_to_num())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=ids)
+@pytest.mark.parametrize("T,G", ROWS)
+def test_infinite_values_that_all_rows_see(spr, T, G, dtype):  # noqa: F811
+    """Weights are positive: an infinite value makes its column infinite, with its sign, wherever it lies in the sequence."""
+    lens = [130, 700, 9000]
+    x = attend_case(3, T, 2 * G, 2, 64, 16, dtype, seed=95 + T, lens=lens)
+    for b, n in enumerate(lens):
+        for column, value, slots in ((3, math.inf, range(n)), (5, -math.inf, range(n)), (8, math.inf, (0, 77)), (9, math.nan, (n // 2,)),
+                                     (10, -math.inf, (n - 1,))):
+            for slot in slots:
+                x["v_cache"][int(x["page_table"][b, slot // 16]), :, slot % 16, column] = value
+    got = check_attend(spr, x)
+    bad = [3, 5, 8, 9, 10]
+    assert bool(torch.isfinite(got[..., [c for c in range(64) if c not in bad]]).all())
+    for column, value in ((3, math.inf), (5, -math.inf), (8, math.inf), (10, -math.inf)):
+        assert bool((got[..., column] == value).all())
+    assert bool(got[..., 9].isnan().all())
