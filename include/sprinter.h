@@ -505,7 +505,7 @@ int logits_rules(const void *logits, int64_t ldv, int V, int B, int T, int dt, c
  *
  * args holds them in the order of their declaration, 64 bits each: addresses and integers as int64_t, scale as a double.  For
  * callers that pay for each argument of a foreign call (from Python cache_append takes 12.5 us, so 10.4).  Returns what the
- * function returns, SPR_ERR_INVALID_ARG for another op or no args.
+ * function returns, SPR_ERR_INVALID_ARG for another op, no args, or a number that does not fit the function's type.
  */
 int spr_draft_pass_call(int op, const int64_t *args);
 

@@ -481,7 +481,12 @@ int spr_draft_pass_call(int op, const int64_t *args)
 {
     if (!args) return SPR_ERR_INVALID_ARG;
     auto number = [&] { return *args++; };
-    auto count = [&] { return (int)*args++; };
+    bool fit = true;            // what the functions take as int has to be one
+    auto count = [&] {
+        const int64_t x = *args++;
+        fit = fit && x == (int)x;
+        return (int)x;
+    };
     auto real = [&] {
         double x;
         memcpy(&x, args++, sizeof x);
@@ -511,6 +516,7 @@ int spr_draft_pass_call(int op, const int64_t *args)
         const int max_pages = count(), num_pages = count(), page_size = count();
         const Address k_cache = address(), v_cache = address(), q_out = address(), ws = address();
         const size_t bytes = (size_t)number();
+        if (!fit) return SPR_ERR_INVALID_ARG;
         return cache_append(q, qs, k, ks, v, vs, B, T, Hq, Hkv, D, dt, lens, counts, parents, slots, inv_freq, rot, interleaved, table,
                             max_pages, num_pages, page_size, k_cache, v_cache, q_out, ws, bytes, address());
     }
@@ -522,6 +528,7 @@ int spr_draft_pass_call(int op, const int64_t *args)
         const float scale = real();
         const Address out = address(), ws = address();
         const size_t bytes = (size_t)number();
+        if (!fit) return SPR_ERR_INVALID_ARG;
         return tree_attention(q, k_cache, v_cache, B, T, Hq, Hkv, D, dt, lens, counts, parents, table, max_pages, num_pages, page_size, scale,
                               out, ws, bytes, address());
     }
@@ -541,6 +548,7 @@ int spr_draft_pass_call(int op, const int64_t *args)
         const int64_t ld_out = number();
         const Address ws = address();
         const size_t bytes = (size_t)number();
+        if (!fit) return SPR_ERR_INVALID_ARG;
         return logits_rules(logits, ldv, V, B, T, dt, history, ld_history, history_len, tokens, parents, counts, penalties, bias_tokens,
                             bias_values, n_bias, masks, ld_mask, num_masks, mask_rows, out, ld_out, ws, bytes, address());
     }
