@@ -31,7 +31,7 @@ EXPORTS = [
     "verifier_labels", "verifier_train_step", "spr_test_sprinter_verify", "spr_test_verifier_train_step",
     "head_loss", "head_loss_grad", "verifier_labels_head", "spr_pack8_pitch", "hidden_pack8", "hidden_unpack8",
     "verifier_train_step8", "spr_test_verifier_train_step8", "spr_test_pair_kernels",
-    "cache_append", "tree_attention", "logits_rules", "spr_test_tree_attention",
+    "cache_append", "tree_attention", "logits_rules", "spr_draft_pass_call", "spr_test_tree_attention",
 ]
 
 

@@ -5,6 +5,7 @@ import struct
 import pytest
 
 import paper_2502_04557_b200 as spr
+from paper_2502_04557_b200 import binding
 from test_draft_pass_host import INVALID, WORKSPACE, append, attend, mem, rules  # noqa: F401
 
 
@@ -43,3 +44,8 @@ def test_numbers_in_an_array_fit(mem, op, f, real, names):  # noqa: F811
             assert call(**{name: usual[name] + far}) == INVALID, (name, far)
     if "B" in names:
         assert call(B=1 << 32) == INVALID          # (not an empty call)
+
+
+def test_every_declared_function_is_listed():
+    from test_host_api import declared_functions
+    assert set(binding.EXPORTS) == set(declared_functions())
