@@ -882,7 +882,7 @@ def tree_attention(q, k_cache, v_cache, page_table, lens, ws: Workspace, scale=N
     else:
         out, oa = _result(dev, out, shape, dtype, "out")
     rc = lib().spr_draft_pass_call(OP_TREE_ATTENTION, _ATTENTION_ARGS(
-        qa, kc, vc, B, T, Hq, Hkv, D, dt, n, c, par, table, max_pages, num_pages, page_size, D ** -0.5 if scale is None else scale, oa, p,
+        qa, kc, vc, B, T, Hq, Hkv, D, dt, n, c, par, table, max_pages, num_pages, page_size, (D or 1) ** -0.5 if scale is None else scale, oa, p,
         size, _raw_stream(dev)))
     if rc != 0:
         _check("tree_attention", rc)

@@ -3,10 +3,11 @@ any device call."""
 import struct
 
 import pytest
+import torch
 
 import paper_2502_04557_b200 as spr
 from paper_2502_04557_b200 import binding
-from test_draft_pass_host import INVALID, WORKSPACE, append, attend, mem, rules  # noqa: F401
+from test_draft_pass_host import INVALID, WORKSPACE, append, attend, device, fake, mem, rules  # noqa: F401
 
 
 def test_append_in_place_only_where_dense(mem):  # noqa: F811
@@ -49,3 +50,12 @@ def test_numbers_in_an_array_fit(mem, op, f, real, names):  # noqa: F811
 def test_every_declared_function_is_listed():
     from test_host_api import declared_functions
     assert set(binding.EXPORTS) == set(declared_functions())
+
+
+def test_heads_without_columns_are_refused(device, monkeypatch):  # noqa: F811
+    """By the library, like other sizes that it does not take (there is no scale of 1 / sqrt(0) to fall over before)."""
+    monkeypatch.setattr(binding, "_raw_stream", lambda dev: 0)
+    with pytest.raises(spr.SprinterError) as e:
+        spr.tree_attention(fake(2, 3, 4, 0), fake(9, 2, 16, 0), fake(9, 2, 16, 0), fake(2, 4, dtype=torch.int32), fake(2, dtype=torch.int32),
+                           device)
+    assert e.value.status == INVALID
