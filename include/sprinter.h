@@ -459,7 +459,7 @@ int cache_append(const void *q, int64_t q_stride, const void *k, int64_t k_strid
  * q, out [B,T,Hq,D] dt (dense, 16-byte aligned, as are the caches); Hkv divides Hq; D a multiple of 8 up to 128 and
  * page_size a multiple of 8, T <= 256, num_pages * Hkv * page_size and B * T below 2^31, and no more than 2^31 tiles of 64 slots
  * in all that page_table could name, each counted for every cached head and block of queries (otherwise SPR_ERR_UNSUPPORTED).
- * Rows of nodes that are not used are zeros.
+ * Rows of nodes that are not used are zeros.  out may be q; otherwise nothing may overlap.
  * Scores, maxima and sums are fp32.  With bf16 tensors the weights enter the second product as two bf16 numbers where a cached
  * head has up to 16 queries (T * Hq / Hkv), and rounded to one where it has more.
  * Keys and values of slots that a row does not see have no part in it, whatever they hold; infinities and NaN in

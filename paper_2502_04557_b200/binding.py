@@ -862,7 +862,7 @@ def tree_attention(q, k_cache, v_cache, page_table, lens, ws: Workspace, scale=N
     """Attention of q [B,T,Hq,D], T nodes per sequence, over the paged cache that cache_append has put them into: each
     sees the lens[b] tokens before the pass and the nodes on its path.  scale: 1 / sqrt(D) unless given.
 
-    counts i32 [B] and parents i32 [B,T] as for cache_append.  Returns out [B,T,Hq,D]."""
+    counts i32 [B] and parents i32 [B,T] as for cache_append.  Returns out [B,T,Hq,D]; out may be q."""
     dev = torch.cuda.current_device()
     dtype, dt = q.dtype, _dt(q)
     if q.dim() != 4:

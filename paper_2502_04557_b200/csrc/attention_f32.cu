@@ -23,16 +23,17 @@ constexpr int kWarpsFor = ROWS * E <= 16 ? 8 : 4;
 template <int E>
 struct Cols {
     float x[E];
+    template <bool CONSTANT = true>             // nothing is written there while the kernel runs (unlike queries: out may be q)
     __device__ __forceinline__ void load(const float *p, bool there)
     {
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] = 0.f;
         if (!there) return;
         if (E == 4) {
-            const float4 a = __ldg(reinterpret_cast<const float4 *>(p));
+            const float4 *from = reinterpret_cast<const float4 *>(p), a = CONSTANT ? __ldg(from) : *from;
             x[0] = a.x, x[1] = a.y, x[E - 2] = a.z, x[E - 1] = a.w;
         } else {
-            const float2 a = __ldg(reinterpret_cast<const float2 *>(p));
+            const float2 *from = reinterpret_cast<const float2 *>(p), a = CONSTANT ? __ldg(from) : *from;
             x[0] = a.x, x[1] = a.y;
         }
     }
@@ -77,7 +78,7 @@ __global__ void __launch_bounds__(32 * kWarpsFor<ROWS, E>, 2) attention_f32_kern
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             Cols<E> c;
-            c.load(static_cast<const float *>(p.q) + (r < t.rows ? attn_out_at(p, s, part, t.row0 + r) : 0) + col, in && r < t.rows);
+            c.template load<false>(static_cast<const float *>(p.q) + (r < t.rows ? attn_out_at(p, s, part, t.row0 + r) : 0) + col, in && r < t.rows);
 #pragma unroll
             for (int e = 0; e < E; ++e) q[r][e] = c.x[e] * p.scale_log2, o[r][e] = 0.f;
         }

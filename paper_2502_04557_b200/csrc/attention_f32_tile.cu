@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_f32_tile_kernel(const A
         for (int i = tid; i < kRows * (D / 4); i += kThreads) {
             const int r = i / (D / 4), c = (i - r * (D / 4)) * 4;
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (r < t.rows) x = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(p.q) + attn_out_at(p, s, part, t.row0 + r) + c));
+            if (r < t.rows) x = *reinterpret_cast<const float4 *>(static_cast<const float *>(p.q) + attn_out_at(p, s, part, t.row0 + r) + c);     // (not __ldg: out may be q)
             x.x *= p.scale_log2, x.y *= p.scale_log2, x.z *= p.scale_log2, x.w *= p.scale_log2;
             *reinterpret_cast<float4 *>(qs + r * pitch + c) = x;
         }

@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) attention_mma_kernel(const Att
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const int col = k * 16 + c * 8 + pair * 2;
-                    qf[k][c * 2 + h] = in && col < p.D ? __ldg(src + col / 2) : 0u;
+                    qf[k][c * 2 + h] = in && col < p.D ? src[col / 2] : 0u;        // (not __ldg: out may be q)
                 }
         }
     };

@@ -94,3 +94,19 @@ def test_infinite_values_that_all_rows_see(spr, T, G, dtype):  # noqa: F811
     for column, value in ((3, math.inf), (5, -math.inf), (8, math.inf), (10, -math.inf)):
         assert bool((got[..., column] == value).all())
     assert bool(got[..., 9].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=ids)
+@pytest.mark.parametrize("D", [8, 64])
+@pytest.mark.parametrize("T,G", ROWS)
+def test_results_over_the_queries(spr, T, G, D, dtype):  # noqa: F811
+    """In place: the bits that another tensor gets, in items of one part and of many, unused nodes among them."""
+    lens = [30, 9000, 0, 700, -1, 2000]
+    x = attend_case(6, T, 2 * G, 2, D, 16, dtype, seed=97 + T, tree=True, lens=lens, counts=[T, T, T // 2, T, T, 1])
+    want = run_attend(spr, x)
+    ws = spr.Workspace(spr.workspace_bytes(spr.OP_TREE_ATTENTION, 1, 1, 1, D, 0, spr.F32 if dtype == F32 else spr.BF16))
+    c = {n: None if t is None else t.cuda() for n, t in x.items()}
+    for _ in range(3):
+        q = c["q"].clone()
+        got = spr.tree_attention(q, c["k_cache"], c["v_cache"], c["page_table"], c["lens"], ws, counts=c["counts"], parents=c["parents"], out=q)
+        assert got is q and torch.equal(q, want) and ws.device_status() == 0
