@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import draft_pass_reference as ref
-from test_gpu_draft_pass import BF16, F32, attend_case, check_attend, ids, run_attend, spr  # noqa: F401
+from test_gpu_draft_pass import BF16, F32, attend_case, check_attend, check_rules, ids, rules_case, run_attend, spr  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -110,3 +110,32 @@ def test_results_over_the_queries(spr, T, G, D, dtype):  # noqa: F811
         q = c["q"].clone()
         got = spr.tree_attention(q, c["k_cache"], c["v_cache"], c["page_table"], c["lens"], ws, counts=c["counts"], parents=c["parents"], out=q)
         assert got is q and torch.equal(q, want) and ws.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=ids)
+@pytest.mark.parametrize("B,T,V,L", [(2, 5, 3001, 131072), (1, 1, 128256, 131072), (8, 1, 600007, 40000), (1, 40, 5000, 20011)])
+def test_rules_over_long_histories(spr, B, T, V, L, dtype):  # noqa: F811
+    """Tokens that stand hundreds of times in a history as long as a cache: both forms."""
+    x, dims = rules_case(B, T, V, dtype, seed=101, L=L, masks=2)
+    x["history"] = torch.randint(-1, 500, (B, L), generator=torch.Generator().manual_seed(102)).to(torch.int32)
+    x["history_len"] = L - torch.arange(B, dtype=torch.int32) * 7
+    check_rules(spr, x, dims)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=ids)
+@pytest.mark.parametrize("n,piece,Hq,Hkv,D", [(700, 256, 8, 2, 64), (513, 128, 4, 4, 128), (300, 256, 3, 1, 40)])
+def test_a_prompt_in_pieces(spr, n, piece, Hq, Hkv, D, dtype):  # noqa: F811
+    """A prompt goes into the cache at once and is attended to in pieces, each over those before it: causal attention."""
+    x = attend_case(2, n, Hq, Hkv, D, 16, dtype, seed=103, lens=[0, 37])
+    c = {k: None if t is None else t.cuda() for k, t in x.items()}
+    ws = spr.Workspace(spr.workspace_bytes(spr.OP_TREE_ATTENTION, 1, 1, 1, D, 0, spr.F32 if dtype == F32 else spr.BF16))
+    g = torch.Generator().manual_seed(104)
+    k, v = (torch.randn((2, n, Hkv, D), generator=g).to(dtype).cuda() for _ in range(2))
+    spr.cache_append(k, v, c["k_cache"], c["v_cache"], c["page_table"], c["lens"], ws)
+    got = [spr.tree_attention(c["q"][:, at:at + piece].contiguous(), c["k_cache"], c["v_cache"], c["page_table"], c["lens"] + at, ws)
+           for at in range(0, n, piece)]
+    assert ws.device_status() == 0
+    want, tol = ref.attend(c["q"], c["k_cache"], c["v_cache"], x["page_table"], x["lens"], None, None, D ** -0.5)
+    # (a short last piece may be worked on with more precise weights than the bound allows for, never with less)
+    got = torch.cat(got, 1)
+    assert ref.within(got, want, tol), ref.worst(got, want, tol)
