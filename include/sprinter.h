@@ -433,8 +433,9 @@ int verifier_train_step8(const void *packed, const uint8_t *labels, int64_t N, i
  * q [B,T,Hq,D], k and v [B,T,Hkv,D] dt; *_stride is the distance from one node to the next in elements (Hq*D or Hkv*D for
  * dense tensors; larger where one projection gives all three side by side).  The first `rot` elements of each head
  * (even, 0 <= rot <= D) are rotated in pairs: elements j and j + rot/2, or with interleaved != 0 elements 2j and 2j + 1,
- * by the angle position * inv_freq[j], inv_freq [rot/2] f32.  Angles are formed in double, rotations in fp32, and results
- * are rounded once; the rest is copied bit for bit.
+ * by the angle position * inv_freq[j], inv_freq [rot/2] f32.  Angles are formed in double and reduced to [-pi, pi] there; sines and
+ * cosines are those of the reduced angle rounded to fp32, rotations are fp32, and results are rounded once; the rest is
+ * copied bit for bit.
  *   q_out [B,T,Hq,D]: rotated queries, zeros for nodes that are not used.  q and q_out may both be NULL, and q_out may be q
  *   where q is dense (SPR_ERR_INVALID_ARG where it is not); otherwise nothing may overlap.
  *   slots [B,T] int32 (optional): the slot to put a node in instead of lens[b] + i, negative: none (its query is rotated
@@ -461,13 +462,16 @@ int cache_append(const void *q, int64_t q_stride, const void *k, int64_t k_strid
  * in all that page_table could name, each counted for every cached head and block of queries (otherwise SPR_ERR_UNSUPPORTED).
  * Rows of nodes that are not used are zeros.  out may be q; otherwise nothing may overlap.
  * Scores, maxima and sums are fp32.  With bf16 tensors the weights enter the second product as two bf16 numbers where a cached
- * head has up to 16 queries (T * Hq / Hkv), and rounded to one where it has more.
+ * head has up to 16 queries (T * Hq / Hkv), and rounded to one where it has more: each is then off by up to 2^-17 or 2^-8 of
+ * itself, and a result by up to as much of sum_s p_s |v_s| beside its own rounding - which is more of the result itself
+ * where values cancel.
  * Keys and values of slots that a row does not see have no part in it, whatever they hold; infinities and NaN in
  * those that it does see count as the formula has them: a score of -inf is a weight of zero, and a row whose scores are all
  * -inf is NaN, as is one with a score of +inf or NaN.  A slot without a page is left out (SPR_ERR_BAD_PAGE), and a row
  * that sees no slot at all is zeros.  After SPR_ERR_TIMEOUT rows whose keys did not arrive are NaN.
  * Launches do not depend on the lengths: a captured call serves whatever lens, counts, parents and page_table hold
- * when it is replayed.  Workspace: spr_workspace_bytes(SPR_OP_TREE_ATTENTION, B, T, 1, D, 0, dt).
+ * when it is replayed.  Prompts of more than 256 tokens, appended at once, are attended to in pieces, each with the nodes before it
+ * counted in lens.  Workspace: spr_workspace_bytes(SPR_OP_TREE_ATTENTION, B, T, 1, D, 0, dt).
  */
 int tree_attention(const void *q, const void *k_cache, const void *v_cache, int B, int T, int Hq, int Hkv, int D, int dt,
                    const int32_t *lens, const int32_t *counts, const int32_t *parents, const int32_t *page_table,
@@ -492,7 +496,9 @@ int tree_attention(const void *q, const void *k_cache, const void *v_cache, int 
  * history, tokens and bias_tokens are padding.
  * out [B,T,ld_out] dt: logits itself (then ld_out = ldv), or not overlapping it.  A row whose mask allows nothing is -inf throughout.
  * Device-detected: history, tokens or bias_tokens >= V are passed over, SPR_ERR_BAD_TOKEN; mask_rows >= num_masks: no mask,
- * SPR_ERR_BAD_ROW.  T <= 256.  Workspace: the status word.
+ * SPR_ERR_BAD_ROW.  After SPR_ERR_TIMEOUT (a copy on the device that did not end) rows of out, or stretches of them, are not
+ * written: another tensor holds what it held, in place raw logits lie beside those that the rules were applied to, and
+ * nothing should be sampled from either.  T <= 256.  Workspace: the status word.
  */
 int logits_rules(const void *logits, int64_t ldv, int V, int B, int T, int dt, const int32_t *history,
                  int64_t ld_history, const int32_t *history_len, const int32_t *tokens, const int32_t *parents,

@@ -5,7 +5,7 @@
 // queries are added up over the lanes by halves (half of the rows to the other half of the lanes, five times over), so
 // that ROWS scores cost some ROWS shuffles.  The warps of a CTA share a tile's keys and are joined
 // through shared memory at the end of a part.  Up to four
-// rows the loads bound it, above that multiplications and shuffles: 64 x 1, 32/8 heads of 128, some 3000 tokens each: 389 us, 241 us
+// rows the loads bound it, above that multiplications and shuffles: 64 x 1, 32/8 heads of 128, some 3000 tokens each: 396 us, 241 us
 // of loads.
 #include "attention_plan.cuh"
 #include "host_util.h"

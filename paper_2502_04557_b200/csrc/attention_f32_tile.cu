@@ -5,8 +5,10 @@
 // lane four keys of each step for the scores, and D / 32 columns for the results: both products take 8 x 4 multiplications per
 // 12 vectors read from shared memory, of which eight are the same for all lanes, and weights never leave the warp's
 // rows of shared memory.  Keys of the next step are on their way (cp.async) while values are worked on, and the other way round.
-// Bound by the multiplications, of which it does a third of the rate the CUDA cores have: 4 trees of 64 nodes, 32/8 heads of 128,
-// 2000 tokens: 280 us (90 us of multiplications; 16 queries at a time, attention_f32.cu, 639).  16 chains of 17: 363 us (670).
+// Bound by the multiplications, of which it does a third of the rate the CUDA cores have (eight warps on an SM, for 254 registers and 200 KB
+// of shared memory, do not cover their reads of shared memory): 4 x 64 nodes, 32/8 heads of 128, 1500 tokens: 264 us, 89 us of
+// multiplications; 16 x 17: 321 us.  By 16 queries at a time, as in attention_f32.cu, they would take twice as long (639 us against 280
+// and 670 against 363, both measured on ragged batches).
 // Steps that hold nodes, or slots without a page, test each pair of query and key.
 #include <atomic>
 #include <type_traits>

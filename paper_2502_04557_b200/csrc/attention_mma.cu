@@ -9,11 +9,11 @@
 // of 128: 195 us with such boxes).  mma.sync suffices here: at 16 rows a tile of 32 KB (the time of 1400 clocks at the memory's
 // rate) takes 128 products per tensor core, some 300 clocks; tcgen05's smallest tile has 64 rows.
 //
-// 64 sequences of some 3000 tokens, 32/8 heads of 128: 133 us, 6.1 TB/s; one of 131072: 104 us; one of
+// 64 sequences of some 3000 tokens, 32/8 heads of 128: 135 us, 6.0 TB/s; one of 131072: 102 us; one of
 // 300: 11 us, the length of the chain from the plan to the join.
 //
-// Weights are used as two bf16 numbers (their rounding and what is left of it): with one, results would be off by 2^-9
-// of themselves for that alone, as much as by their own rounding.  The second product is free where the
+// Weights are used as two bf16 numbers (their rounding and what is left of it), off by up to 2^-17 of themselves: with one
+// it would be 2^-8, and results could be off by as much of sum p |v|, more than by their own rounding where values cancel.  The second product is free where the
 // memory is what bounds it.
 #include <atomic>
 

@@ -16,13 +16,14 @@
 // Exponents are taken against a maximum that stands until a tile's weights add up to more than 2^13 (sums and products in
 // fp32 keep their relative precision whatever the common factor): only then are its scores looked through for
 // a new one and O, which lives in TMEM, rescaled.  Most tiles need no maximum at all.
-// Weights are rounded to bf16 for the second product, which leaves results off by some 2^-9 of themselves, as much as their own
-// rounding does.  A second bf16 number for what the rounding leaves, as with few rows, would cost a fifth of the time
-// (128 sequences of 17 nodes: 199 us against 164 us).
+// Weights are rounded to bf16 for the second product, each by up to 2^-8 of itself, and a result is off by up to as much of
+// sum p |v|: more than its own rounding where values cancel.  (Values that are independent of one another: 0.0023 of the results, root
+// mean square, where their own rounding is 0.0017.)  A second bf16 number for what the rounding leaves, as with few rows, would
+// cost a fifth of the time (199 us against 164 us when both were measured, at an earlier state of the loaders).
 //
-// 128 sequences of 17 nodes, 32/8 heads of 128, some 1500 tokens: 172 us, 130 of loads; 16 trees of 64 nodes over 8192: 167 us.  Beside its
+// 128 sequences of 17 nodes, 32/8 heads of 128, some 1500 tokens: 175 us, 130 of loads; 16 trees of 64 nodes over 8192: 160 us.  Beside its
 // tiles a part takes some 9000 clocks, the latency of its start, its tail (which is masked and looked through) and its results: 128
-// sequences of 17 nodes over 100 tokens take 57 us, 13 of loads.
+// sequences of 17 nodes over 100 tokens take 54 us, 13 of loads.
 //
 // Every wait is bounded: when one runs out the status word becomes SPR_ERR_TIMEOUT, loaders and issuing threads stop and
 // wait (again bounded) for what is in flight, and the softmax warps go on without waiting and give NaN.

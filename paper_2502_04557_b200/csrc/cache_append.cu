@@ -3,7 +3,8 @@
 //   (x, y) -> (x cos a - y sin a, y cos a + x sin a),  a = position * inv_freq[pair]
 //
 // The product is formed in double and reduced to [-pi, pi] there: at position 131072 an fp32 product would be off
-// by 0.008 rad.  Sine and cosine of the reduced angle are fp32, and so is the rotation; results are rounded once.
+// by 0.008 rad.  Sine and cosine are those of the reduced angle rounded to fp32 (by up to 2^-23 rad), the rotation is fp32, and
+// results are rounded once.
 // Bound by memory: every element is read once and written once.  One CTA has one node (all heads of a token share
 // its angles, which are formed once into shared memory).  A thread asks for its first vectors before it looks up where
 // they go: the length, the parents, the page and the angles take some 2000 clocks one after the other.
